@@ -57,10 +57,11 @@ enum {
                               reductions, no float atomics); this flag also keeps the call on the analytic kernel
                               choice when dp_set_autotune is on, so that the choice cannot differ between processes */
     DP_DX_F32 = 8u,        /* bf16 path only: dx is written as fp32 instead of bf16 */
-    DP_RELU_IN = 16u       /* the layer's input x is the output of a ReLU: backward-data also applies that ReLU's
+    DP_RELU_IN = 16u,      /* the layer's input x is the output of a ReLU: backward-data also applies that ReLU's
                               backward, dx *= [x > 0], in its epilogue (needs the saved input: dp_conv2d_bwd_data_relu,
                               or x in dp_linear_fwd_bwd).  The gradient then reaches the preceding layer already
                               masked, so that layer passes y_saved = NULL and needs no pointwise pass of its own */
+    DP_SILU = 32u          /* group norm only: the activation is u * sigmoid(u) */
 };
 
 enum { DP_PASS_FWD = 0, DP_PASS_DGRAD = 1, DP_PASS_WGRAD = 2 };
@@ -262,6 +263,126 @@ dp_status dp_softmax_xent(int32_t n, int32_t classes, int32_t io_dtype, const vo
  * No dampening, Nesterov term or weight decay.  count elements. */
 dp_status dp_sgd_update(int64_t count, float lr, float momentum, const float *grad, float *mom, float *w32,
                         void *w_bf16, void *hip_stream);
+
+/* ---- Group normalisation with an activation, channels last -----------------------------------------------
+ * The norm of networks that train at 1 ... 32 samples per GPU: its statistics are those of one sample, so they do not change with
+ * the number of GPUs a layer runs on.  Channels c are `groups` groups of c / groups consecutive ones; per sample and group
+ *   mean, var over the h*w pixels and the group's channels (biased);  rstd = 1 / sqrt(var + eps)
+ *   xhat = (x - mean) * rstd;  u = xhat * gamma[c] + beta[c];  y = u, max(u, 0) (DP_RELU) or u * sigmoid(u) (DP_SILU).
+ * x, y, dy, dx [n,h,w,c] in io_dtype (DP_BF16 or DP_F32); gamma, beta [c] fp32, NULL = ones / zeros; mean, rstd [n,groups] fp32.
+ * Statistics, sums and the normalisation are fp32; deterministic; asynchronous on hip_stream.
+ * n*h*w*c < 2^31, h*w <= 2^30, n * ceil(c / 256) <= 2^23. */
+typedef struct {
+    int32_t n, h, w, c, groups; /* groups divides c */
+    int32_t io_dtype;           /* dp_dtype */
+    uint32_t flags;             /* 0, DP_RELU or DP_SILU */
+    float eps;                  /* > 0 */
+} dp_group_norm_desc;
+
+/* Device scratch that the forward (DP_PASS_FWD) or the backward (DP_PASS_DGRAD) call needs; 0 for an invalid descriptor. */
+size_t dp_group_norm_workspace_bytes(const dp_group_norm_desc *desc, int pass);
+
+/* mean and rstd are what the backward call takes; either may be NULL (inference). */
+dp_status dp_group_norm_fwd(const dp_group_norm_desc *desc, const void *x, const float *gamma_or_null, const float *beta_or_null,
+                            void *y, float *mean_or_null, float *rstd_or_null, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* g = dy * (derivative of the activation); dgamma[c] = sum g * xhat, dbeta[c] = sum g over samples and pixels;
+ * dx = rstd * (t - mean(t) - xhat * mean(t * xhat)) with t = g * gamma and means over the group.
+ * DP_RELU: the derivative is [y_saved > 0] if y_saved (the saved output) is given; without it dy has been masked already, by the
+ * layer behind (DP_RELU_IN).  Other activations ignore y_saved; DP_SILU's derivative is recomputed from x.
+ * dx, dgamma, dbeta: each may be NULL, not all three.  dx may be dy's memory (in place); no other overlap. */
+dp_status dp_group_norm_bwd(const dp_group_norm_desc *desc, const void *x, const void *dy, const void *y_saved_or_null,
+                            const float *gamma_or_null, const float *beta_or_null, const float *mean, const float *rstd,
+                            void *dx, float *dgamma, float *dbeta, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* ---- All parameters of a network at once: gradient norm, AdamW -------------------------------------------
+ * A table in device memory, made once for a network, names every tensor; a step is then one launch, whatever the number of
+ * tensors.  Gradients and master weights are fp32, as the backward passes write and read them.
+ * States: DP_STATE_F32: m and v fp32 [count].
+ * DP_STATE_Q8: m and v hold one byte per element, an e4m3 float (OCP, "fn"); a fp32 scale belongs to each 256 elements counted
+ * from the tensor's start (the last may be fewer): m = float8(m8) * m_scale[i / 256], v = (float8(v8) * v_scale[i / 256])^2.
+ * Zeros are a valid first state in both formats. */
+enum { DP_STATE_F32 = 0, DP_STATE_Q8 = 1 };
+
+typedef struct {
+    int64_t count;        /* elements; 0 is allowed, pointers are not looked at then */
+    const float *grad;
+    float *w32;           /* master weights, updated in place */
+    void *w_bf16;         /* the copy that the next forward pass reads, rounded to nearest-even; may be NULL */
+    void *m, *v;
+    float *m_scale, *v_scale; /* DP_STATE_Q8: [ceil(count / 256)]; else NULL */
+    float weight_decay;   /* >= 0; 0 for biases and norms */
+} dp_param;
+
+/* What the calls below take: filled in by dp_param_table_build, a HOST struct without ownership. */
+typedef struct {
+    const void *table; /* device */
+    int64_t n_chunks, n_elements;
+    int32_t n_params, state, updates, reserved; /* updates: 0 if some parameter has a gradient only */
+} dp_param_list;
+
+/* Bytes of the table of these parameters; 0 if there are no elements or a count is out of range. */
+size_t dp_param_table_bytes(const dp_param *params, int32_t n_params);
+
+/* Host only.  Checks the parameters (pointers 16-byte aligned; no two may share memory that a step writes) and writes the table's
+ * contents to host_table; the caller copies them to device_table (device address, 64-byte aligned, as many bytes) before the first
+ * call that uses *list, and keeps that memory and all tensors while it is in use.  Where every member but count, grad and
+ * weight_decay is NULL the list serves dp_grad_norm only. */
+dp_status dp_param_table_build(const dp_param *params, int32_t n_params, int32_t state, void *host_table, size_t host_table_bytes,
+                               const void *device_table, dp_param_list *list);
+
+/* norm_and_scale[0] = 2-norm of all gradients together; norm_and_scale[1] = min(1, max_norm / norm), the factor that clips them, or 0 if
+ * the norm is not finite.  Device, fp32 [2].  max_norm > 0, INFINITY for the norm alone.  Sums are in 64 bits, in a fixed order. */
+size_t dp_grad_norm_workspace_bytes(const dp_param_list *list);
+dp_status dp_grad_norm(const dp_param_list *list, float max_norm, float *norm_and_scale, void *ws, size_t ws_bytes, void *hip_stream);
+
+typedef struct {
+    double lr, beta1, beta2, eps; /* betas in [0, 1), eps > 0 */
+    int64_t step;                 /* of this update, counted from 1 */
+    uint64_t seed;                /* DP_STATE_Q8: of the random rounding; another one for every step */
+} dp_adamw_hyper;
+
+/* In place, for every element: g = grad * *grad_scale (device scalar, e.g. &norm_and_scale[1]; NULL = 1)
+ *   m = beta1*m + (1-beta1)*g;  v = beta2*v + (1-beta2)*g^2
+ *   w32 = w32 - lr*weight_decay*w32 - lr * (m/(1-beta1^step)) / (sqrt(v/(1-beta2^step)) + eps);  w_bf16 = bf16(w32)
+ * in fp32; g, m, v and sqrt(v) with every operation rounded by itself in the order written.
+ * If *grad_scale is 0 or NaN the step is skipped: nothing is written.
+ * DP_STATE_Q8: m and sqrt(v) are stored with scale = largest magnitude of the 256 * (1/448), as value * ((1 / largest) * 448) rounded
+ * to one of its two neighbours in e4m3, the upper with the probability of its distance from the lower; a positive v stays positive.
+ * Random bits: 16 each from SplitMix64(seed) at counter e/2, fields 0 (m) and 1 (v) for even e, 2 and 3 for odd e, where e
+ * numbers the elements of the list with every tensor starting at a multiple of 4096.  A value that is not finite makes its 256
+ * neighbours NaN with it.
+ * The hyper-parameters are read by the call: a captured graph replays the step that it was captured with. */
+dp_status dp_adamw_step(const dp_param_list *list, const dp_adamw_hyper *hyper, const float *grad_scale_or_null, void *hip_stream);
+
+/* ---- Log-probabilities, entropy and the likeliest classes of rows of scores ------------------------------
+ * Evaluation and scoring behind the last dense layer, for any number of classes.  For each row, p = softmax(z):
+ *   lse = log sum exp z;  logp = log p[id];  entropy = -sum p log p;
+ *   top_ids / top_logp [rows, top_k]: the classes with the largest scores and their log p, best first, equal scores by index.
+ * z in io_dtype (DP_BF16 or DP_F32), row r at z + r * row_stride elements (any alignment of the element); ids int32 [rows].
+ * An id outside [0, classes) gives logp 0 and no gradient (a padded row).  Scores of -inf are classes that are ruled out; a row
+ * of nothing else has lse, logp and top_logp -inf, entropy 0 and gradient 0.  A NaN or +inf score makes the row's results NaN (NaN
+ * scores rank above all others).  Arithmetic is fp32; deterministic. */
+#define DP_LOGPROBS_MAX_TOP 64
+typedef struct {
+    int32_t rows, classes; /* rows may be 0 */
+    int64_t row_stride;    /* elements, >= classes; 0 = classes */
+    int32_t top_k;         /* 0 ... min(classes, DP_LOGPROBS_MAX_TOP) */
+    int32_t io_dtype;      /* dp_dtype */
+} dp_logprobs_desc;
+
+size_t dp_logprobs_workspace_bytes(const dp_logprobs_desc *desc);
+
+/* Each output may be NULL (not asked for); ids may be NULL if logp is. top_logp and top_ids go together and are needed if top_k > 0. */
+dp_status dp_logprobs_fwd(const dp_logprobs_desc *desc, const void *z, const int32_t *ids_or_null, float *logp_or_null,
+                          float *entropy_or_null, float *lse_or_null, float *top_logp, int32_t *top_ids, void *ws, size_t ws_bytes,
+                          void *hip_stream);
+
+/* dz[r,j] = dlogp[r] * ([j = id] - p_j) - dentropy[r] * p_j * (log p_j + entropy[r]), in io_dtype, with z's strides; may be z's own
+ * memory.  lse and entropy are the forward call's.  dlogp (with ids) or dentropy (with entropy) may be NULL, not both. */
+dp_status dp_logprobs_bwd(const dp_logprobs_desc *desc, const void *z, const int32_t *ids_or_null, const float *lse,
+                          const float *entropy_or_null, const float *dlogp_or_null, const float *dentropy_or_null, void *dz,
+                          void *hip_stream);
 
 /* ---- Burst-parallel plan of a chain of layers (host only: no GPU call, all pointers host) -------
  * Paper section 4.2, algorithm "Search Linear": dynamic programming over two tables,

@@ -11,13 +11,17 @@ from . import build as _build
 
 DP_OK, DP_ERR_NULL, DP_ERR_BAD_DESC, DP_ERR_UNSUPPORTED, DP_ERR_WORKSPACE, DP_ERR_HIP = range(6)
 DP_F32, DP_BF16 = 0, 1
-DP_BIAS, DP_RELU, DP_DETERMINISTIC, DP_DX_F32, DP_RELU_IN = 1, 2, 4, 8, 16
+DP_BIAS, DP_RELU, DP_DETERMINISTIC, DP_DX_F32, DP_RELU_IN, DP_SILU = 1, 2, 4, 8, 16, 32
+DP_STATE_F32, DP_STATE_Q8 = 0, 1
+DP_LOGPROBS_MAX_TOP = 64
 DP_PASS_FWD, DP_PASS_DGRAD, DP_PASS_WGRAD = 0, 1, 2
 
 EXPORTS = ["dp_conv2d_workspace_bytes", "dp_linear_workspace_bytes", "dp_conv2d_fwd", "dp_conv2d_bwd_data", "dp_conv2d_bwd_data_relu",
            "dp_conv2d_bwd_filter", "dp_conv2d_bwd_filter_noalloc", "dp_linear_fwd_bwd", "dp_relu_bias_grad_workspace_bytes", "dp_relu_bias_grad",
            "dp_profile_layer", "dp_trace_begin", "dp_trace_end", "dp_conv2d_kernel_info", "dp_set_override", "dp_set_autotune", "dp_plan_chain",
            "dp_plan_cost_tables", "dp_plan_graph", "dp_maxpool2x2_fwd", "dp_maxpool2x2_bwd", "dp_softmax_xent", "dp_sgd_update",
+           "dp_group_norm_workspace_bytes", "dp_group_norm_fwd", "dp_group_norm_bwd", "dp_param_table_bytes", "dp_param_table_build",
+           "dp_grad_norm_workspace_bytes", "dp_grad_norm", "dp_adamw_step", "dp_logprobs_workspace_bytes", "dp_logprobs_fwd", "dp_logprobs_bwd",
            "dp_last_error", "dp_version"]
 
 
@@ -55,6 +59,28 @@ class dp_plan_branch(C.Structure):
 
 class dp_plan_graph_desc(C.Structure):
     _fields_ = [("chain", dp_plan_desc), ("n_branches", C.POINTER(C.c_int32)), ("branches", C.POINTER(dp_plan_branch))]
+
+
+class dp_group_norm_desc(C.Structure):
+    _fields_ = [(f, C.c_int32) for f in ("n", "h", "w", "c", "groups", "io_dtype")] + [("flags", C.c_uint32), ("eps", C.c_float)]
+
+
+class dp_param(C.Structure):
+    _fields_ = [("count", C.c_int64)] + [(f, C.c_void_p) for f in ("grad", "w32", "w_bf16", "m", "v", "m_scale", "v_scale")] + \
+               [("weight_decay", C.c_float)]
+
+
+class dp_param_list(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("n_chunks", C.c_int64), ("n_elements", C.c_int64)] + \
+               [(f, C.c_int32) for f in ("n_params", "state", "updates", "reserved")]
+
+
+class dp_adamw_hyper(C.Structure):
+    _fields_ = [(f, C.c_double) for f in ("lr", "beta1", "beta2", "eps")] + [("step", C.c_int64), ("seed", C.c_uint64)]
+
+
+class dp_logprobs_desc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("classes", C.c_int32), ("row_stride", C.c_int64), ("top_k", C.c_int32), ("io_dtype", C.c_int32)]
 
 
 class DpError(RuntimeError):
@@ -99,6 +125,18 @@ def _load():
     lib.dp_maxpool2x2_bwd.argtypes = [i32, i32, i32, i32, i32, vp, vp, vp, vp]
     lib.dp_softmax_xent.argtypes = [i32, i32, i32, vp, vp, vp, vp, vp]
     lib.dp_sgd_update.argtypes = [i64, C.c_float, C.c_float, vp, vp, vp, vp, vp]
+    lib.dp_group_norm_fwd.argtypes = [P(dp_group_norm_desc), vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.dp_group_norm_bwd.argtypes = [P(dp_group_norm_desc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.dp_param_table_build.argtypes = [P(dp_param), i32, i32, vp, sz, vp, P(dp_param_list)]
+    lib.dp_grad_norm.argtypes = [P(dp_param_list), C.c_float, vp, vp, sz, vp]
+    lib.dp_adamw_step.argtypes = [P(dp_param_list), P(dp_adamw_hyper), vp, vp]
+    lib.dp_logprobs_fwd.argtypes = [P(dp_logprobs_desc), vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.dp_logprobs_bwd.argtypes = [P(dp_logprobs_desc), vp, vp, vp, vp, vp, vp, vp, vp]
+    for name in ("dp_group_norm_fwd", "dp_group_norm_bwd", "dp_param_table_build", "dp_grad_norm", "dp_adamw_step", "dp_logprobs_fwd", "dp_logprobs_bwd"):
+        getattr(lib, name).restype = C.c_int
+    for name, args in (("dp_group_norm_workspace_bytes", [P(dp_group_norm_desc), C.c_int]), ("dp_param_table_bytes", [P(dp_param), i32]),
+                       ("dp_grad_norm_workspace_bytes", [P(dp_param_list)]), ("dp_logprobs_workspace_bytes", [P(dp_logprobs_desc)])):
+        getattr(lib, name).restype, getattr(lib, name).argtypes = sz, args
     for name in ("dp_conv2d_fwd", "dp_conv2d_bwd_data", "dp_conv2d_bwd_filter", "dp_conv2d_bwd_filter_noalloc", "dp_linear_fwd_bwd",
                  "dp_relu_bias_grad", "dp_profile_layer", "dp_trace_begin", "dp_trace_end", "dp_set_override", "dp_set_autotune", "dp_plan_chain",
                  "dp_plan_cost_tables", "dp_plan_graph", "dp_maxpool2x2_fwd", "dp_maxpool2x2_bwd", "dp_softmax_xent", "dp_sgd_update"):
@@ -189,6 +227,106 @@ def dp_softmax_xent(n, classes, io_dtype, z, labels, loss, dz=None, stream=None)
 
 def dp_sgd_update(count, lr, momentum, grad, mom, w32, w_bf16=None, stream=None):
     _check(lib.dp_sgd_update(count, lr, momentum, _ptr(grad), _ptr(mom), _ptr(w32), _ptr(w_bf16), _stream(stream)))
+
+
+def group_norm_desc(n, h, w, c, groups, io_dtype=DP_BF16, flags=0, eps=1e-5):
+    return dp_group_norm_desc(n, h, w, c, groups, io_dtype, flags, eps)
+
+
+def dp_group_norm_workspace_bytes(desc, pass_):
+    return int(lib.dp_group_norm_workspace_bytes(C.byref(desc), pass_))
+
+
+def dp_group_norm_fwd(desc, x, gamma, beta, y, mean=None, rstd=None, ws=None, stream=None):
+    p, b = _ws(ws)
+    _check(lib.dp_group_norm_fwd(C.byref(desc), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean), _ptr(rstd), p, b, _stream(stream)))
+
+
+def dp_group_norm_bwd(desc, x, dy, y_saved, gamma, beta, mean, rstd, dx=None, dgamma=None, dbeta=None, ws=None, stream=None):
+    p, b = _ws(ws)
+    _check(lib.dp_group_norm_bwd(C.byref(desc), _ptr(x), _ptr(dy), _ptr(y_saved), _ptr(gamma), _ptr(beta), _ptr(mean), _ptr(rstd), _ptr(dx),
+                                 _ptr(dgamma), _ptr(dbeta), p, b, _stream(stream)))
+
+
+class ParamList:
+    """The parameters of a network as dp_grad_norm and dp_adamw_step take them: the device table, and the tensors that it names."""
+
+    def __init__(self, desc, table, tensors):
+        self.desc, self.table, self.tensors = desc, table, tensors
+
+
+def param_list(params, state=DP_STATE_F32, device=None):
+    """Makes the device table of a network's parameters (once; the tensors must stay where they are).  `params`: dicts with the
+    contiguous tensors `grad` and, unless only gradients are listed, `w32`, `m`, `v` (fp32; with DP_STATE_Q8 m and v of one byte per element, e.g.
+    torch.float8_e4m3fn, and `m_scale`, `v_scale`), optionally `w_bf16` and `weight_decay`.  The table is copied before this returns."""
+    n = len(params)
+    arr = (dp_param * max(1, n))()
+    byte_types = [t for t in (torch.uint8, torch.int8, getattr(torch, "float8_e4m3fn", None)) if t is not None]
+    state_types = byte_types if state == DP_STATE_Q8 else [torch.float32]
+    tensors = []
+    for i, p in enumerate(params):
+        unknown = set(p) - {"grad", "w32", "w_bf16", "m", "v", "m_scale", "v_scale", "weight_decay"}
+        if unknown:
+            raise ValueError(f"parameter {i}: unknown entries {sorted(unknown)}")
+        count = p["grad"].numel()
+        blocks = (count + 255) // 256
+        arr[i].count, arr[i].weight_decay = count, float(p.get("weight_decay", 0.0))
+        for name, size, types in (("grad", count, [torch.float32]), ("w32", count, [torch.float32]), ("w_bf16", count, [torch.bfloat16]),
+                                  ("m", count, state_types), ("v", count, state_types), ("m_scale", blocks, [torch.float32]),
+                                  ("v_scale", blocks, [torch.float32])):
+            t = p.get(name)
+            if t is None:
+                continue
+            if t.numel() != size or t.dtype not in types or not t.is_contiguous():
+                raise ValueError(f"parameter {i}: {name} must be a contiguous tensor of {size} elements of {' or '.join(map(str, types))}")
+            if t.device != p["grad"].device:
+                raise ValueError(f"parameter {i}: {name} is on another device than grad")
+            setattr(arr[i], name, t.data_ptr())
+            tensors.append(t)
+        device = device if device is not None else p["grad"].device
+    nbytes = int(lib.dp_param_table_bytes(arr, n))
+    host = torch.zeros(max(nbytes, 64), dtype=torch.uint8)
+    table = torch.zeros(max(nbytes, 64), dtype=torch.uint8, device=device if device is not None else "cpu")
+    desc = dp_param_list()
+    _check(lib.dp_param_table_build(arr, n, state, host.data_ptr(), nbytes, table.data_ptr(), C.byref(desc)))
+    table.copy_(host)
+    return ParamList(desc, table, tensors)
+
+
+def dp_grad_norm_workspace_bytes(params):
+    return int(lib.dp_grad_norm_workspace_bytes(C.byref(params.desc)))
+
+
+def dp_grad_norm(params, max_norm, norm_and_scale, ws=None, stream=None):
+    p, b = _ws(ws)
+    _check(lib.dp_grad_norm(C.byref(params.desc), max_norm, _ptr(norm_and_scale), p, b, _stream(stream)))
+
+
+def adamw_hyper(lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0):
+    return dp_adamw_hyper(lr, beta1, beta2, eps, step, seed)
+
+
+def dp_adamw_step(params, hyper, grad_scale=None, stream=None):
+    """grad_scale: a device tensor with the factor first in it, e.g. norm_and_scale[1:]; None = 1."""
+    _check(lib.dp_adamw_step(C.byref(params.desc), C.byref(hyper), _ptr(grad_scale), _stream(stream)))
+
+
+def logprobs_desc(rows, classes, top_k=0, io_dtype=DP_BF16, row_stride=0):
+    return dp_logprobs_desc(rows, classes, row_stride, top_k, io_dtype)
+
+
+def dp_logprobs_workspace_bytes(desc):
+    return int(lib.dp_logprobs_workspace_bytes(C.byref(desc)))
+
+
+def dp_logprobs_fwd(desc, z, ids=None, logp=None, entropy=None, lse=None, top_logp=None, top_ids=None, ws=None, stream=None):
+    p, b = _ws(ws)
+    _check(lib.dp_logprobs_fwd(C.byref(desc), _ptr(z), _ptr(ids), _ptr(logp), _ptr(entropy), _ptr(lse), _ptr(top_logp), _ptr(top_ids), p, b,
+                               _stream(stream)))
+
+
+def dp_logprobs_bwd(desc, z, ids, lse, entropy, dlogp, dentropy, dz, stream=None):
+    _check(lib.dp_logprobs_bwd(C.byref(desc), _ptr(z), _ptr(ids), _ptr(lse), _ptr(entropy), _ptr(dlogp), _ptr(dentropy), _ptr(dz), _stream(stream)))
 
 
 def _doubles(rows, n):

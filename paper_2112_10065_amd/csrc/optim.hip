@@ -1,0 +1,461 @@
+// Operators over all parameters of a network in one launch: the 2-norm of the gradients with the factor that clips it,
+// and an AdamW step with its two states in fp32 or in 8 bits.  Bound by HBM: every element is read and written once.
+//
+// A network has hundreds of tensors, most of them a few hundred elements long, so a launch per tensor would cost more than the
+// step.  The tensors are cut into chunks of 4096 elements; a table in device memory, made once per network, has one 64-byte record per
+// chunk with all addresses of the chunk.  A block reads its record with one scalar load (a table of tensors and a search
+// would be two or more loads that depend on each other) and works on one chunk.
+#include "vec_common.h"
+#include <algorithm>
+#include <cmath>
+#include <vector>
+
+namespace {
+
+constexpr int kChunk = 4096;      // elements of a chunk: 16 per thread of a block
+constexpr int kBlock = 256;       // elements that share a scale of an 8-bit state
+constexpr int kNormBlocks = 1024; // four blocks per compute unit
+
+// table record; w16, ms, vs may be null
+struct alignas(64) Chunk {
+    const float *g;
+    float *w;
+    bf16_t *w16;
+    void *m, *v;
+    float *ms, *vs;
+    int count;     // 1 ... kChunk
+    float decay;
+};
+static_assert(sizeof(Chunk) == 64, "one scalar load of 16 dwords");
+
+// ---- norm ---------------------------------------------------------------------------------------------------------
+
+// Squares and sums in 64 bits: the square of a gradient beyond 1e19 is finite, and the result does not depend on how the
+// gradients are spread over the tensors.
+__device__ __forceinline__ double square_sum(const Chunk &c, int t)
+{
+    double s = 0.0;
+    const int nvec = c.count >> 2;
+    float4 v[kChunk / 1024];
+#pragma unroll
+    for (int u = 0; u < kChunk / 1024; ++u) {
+        const int i = u * 256 + t;
+        v[u] = i < nvec ? reinterpret_cast<const float4 *>(c.g)[i] : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int u = 0; u < kChunk / 1024; ++u) {
+        s = fma((double)v[u].x, (double)v[u].x, s); s = fma((double)v[u].y, (double)v[u].y, s);
+        s = fma((double)v[u].z, (double)v[u].z, s); s = fma((double)v[u].w, (double)v[u].w, s);
+    }
+    if (t < (c.count & 3)) { const double e = c.g[nvec * 4 + t]; s = fma(e, e, s); }
+    return s;
+}
+
+// thread 0 of 256 gets the block's sum: wavefronts by shuffles, their sums in order
+__device__ __forceinline__ double block_sum(double s, double *sm)
+{
+    s = wave_sum(s);
+    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = s;
+    __syncthreads();
+    return sm[0] + sm[1] + sm[2] + sm[3];
+}
+
+__device__ __forceinline__ void write_norm(double sum, float max_norm, float *out)
+{
+    const double norm = sqrt(sum);
+    out[0] = (float)norm;
+    // a norm that is not finite gives 0, which dp_adamw_step takes for "skip this step"
+    out[1] = !(norm <= 1.7e308) ? 0.f : norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.f;
+}
+
+__global__ __launch_bounds__(256) void k_norm_partial(const Chunk *__restrict__ table, long long n_chunks, double *__restrict__ partial)
+{
+    __shared__ double sm[4];
+    double s = 0.0;
+    for (long long i = blockIdx.x; i < n_chunks; i += gridDim.x) s += square_sum(table[i], threadIdx.x);
+    s = block_sum(s, sm);
+    if (threadIdx.x == 0) partial[blockIdx.x] = s;
+}
+
+__global__ __launch_bounds__(256) void k_norm_final(const double *__restrict__ partial, int n, float max_norm, float *__restrict__ out)
+{
+    __shared__ double sm[4];
+    double s = 0.0;
+    for (int i = threadIdx.x; i < n; i += 256) s += partial[i];
+    s = block_sum(s, sm);
+    if (threadIdx.x == 0) write_norm(s, max_norm, out);
+}
+
+int norm_blocks(long long n_chunks) { return (int)std::max(1ll, std::min<long long>(n_chunks, kNormBlocks)); }
+
+// ---- AdamW --------------------------------------------------------------------------------------------------------
+
+struct AdamArgs {
+    float beta1, beta2, one_minus_beta1, one_minus_beta2;
+    float step_size;        // lr / (1 - beta1^step)
+    float inv_root_bc2;     // 1 / sqrt(1 - beta2^step)
+    float eps, lr;
+    unsigned long long seed;
+};
+
+// The step's factor on the gradients; a step whose factor is 0 or NaN is skipped as a whole.
+__device__ __forceinline__ bool step_factor(const float *scale, float &s)
+{
+    s = scale != nullptr ? *scale : 1.f;
+    return fabsf(s) > 0.f;
+}
+
+// Each product and sum is rounded by itself, as the definition is written: an 8-bit state then follows from its definition to the
+// last code, whoever computes it (a fused multiply-add would tip one random rounding in 10^6 the other way).  The kernels are bound by memory either way.
+__device__ __forceinline__ void adam_moments(const AdamArgs &a, float g, float &m, float &v)
+{
+#pragma clang fp contract(off)
+    m = a.beta1 * m + a.one_minus_beta1 * g;
+    v = a.beta2 * v + a.one_minus_beta2 * (g * g);
+}
+__device__ __forceinline__ float adam_weight(const AdamArgs &a, float keep, float w, float m, float root)
+{
+    return fmaf(-a.step_size, m / fmaf(root, a.inv_root_bc2, a.eps), keep * w);
+}
+
+__global__ __launch_bounds__(256) void k_adamw(const Chunk *__restrict__ table, AdamArgs a, const float *__restrict__ scale)
+{
+    const Chunk c = table[blockIdx.x];
+    float s;
+    if (!step_factor(scale, s)) return;
+    const int t = threadIdx.x, nvec = c.count >> 2;
+    const float keep = fmaf(-a.lr, c.decay, 1.f);
+    float *m32 = (float *)c.m, *v32 = (float *)c.v;
+    constexpr int U = kChunk / 1024;
+    float4 g[U], w[U], m[U], v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int i = u * 256 + t;
+        if (i < nvec) {
+            g[u] = reinterpret_cast<const float4 *>(c.g)[i];
+            m[u] = reinterpret_cast<const float4 *>(m32)[i];
+            v[u] = reinterpret_cast<const float4 *>(v32)[i];
+            w[u] = reinterpret_cast<const float4 *>(c.w)[i];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int i = u * 256 + t;
+        if (i >= nvec) continue;
+        const float ge[4] = {g[u].x * s, g[u].y * s, g[u].z * s, g[u].w * s};
+        float *me = &m[u].x, *ve = &v[u].x, *we = &w[u].x;
+        Pack<bf16_t, 4> o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            adam_moments(a, ge[e], me[e], ve[e]);
+            we[e] = adam_weight(a, keep, we[e], me[e], sqrtf(ve[e]));
+            o.v[e] = from_f32<bf16_t>(we[e]);
+        }
+        reinterpret_cast<float4 *>(m32)[i] = m[u];
+        reinterpret_cast<float4 *>(v32)[i] = v[u];
+        reinterpret_cast<float4 *>(c.w)[i] = w[u];
+        if (c.w16 != nullptr) reinterpret_cast<Pack<bf16_t, 4> *>(c.w16)[i] = o;
+    }
+    if (t < (c.count & 3)) {
+        const int i = nvec * 4 + t;
+        float me = m32[i], ve = v32[i];
+        adam_moments(a, c.g[i] * s, me, ve);
+        const float we = adam_weight(a, keep, c.w[i], me, sqrtf(ve));
+        m32[i] = me; v32[i] = ve; c.w[i] = we;
+        if (c.w16 != nullptr) c.w16[i] = from_f32<bf16_t>(we);
+    }
+}
+
+// ---- 8-bit states -------------------------------------------------------------------------------------------------
+//
+// m and sqrt(v) (whose range is half of v's in the exponent) are held as e4m3 floats with one fp32 scale for each 256
+// elements, value = float8 * scale, the largest magnitude of a block at 448.  Rounding is stochastic: a step changes v
+// by 0.1 % at beta2 = 0.999 while neighbouring e4m3 values are 6 to 12 % apart, so rounding to the nearest would leave
+// most values where they are for good; taking the upper neighbour with the probability of the distance keeps them right on average.
+// The 16 random bits of each value are fields of a SplitMix64 output (published: Steele, Lea, Flood 2014) whose counter
+// is the element's place in the list, so the result depends on the seed and the list alone and on no launch shape.
+
+__device__ __forceinline__ unsigned long long splitmix64(unsigned long long seed, unsigned long long counter)
+{
+    unsigned long long z = seed + (counter + 1) * 0x9E3779B97F4A7C15ull;
+    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+    return z ^ (z >> 31);
+}
+
+// e4m3 code of a in [0, 448 (1 + 2^-21)]: up from the lower neighbour with probability (distance + rnd16 / 2^16 >= 1).  Normal values
+// add the random bits below the three fraction bits that stay; below 2^-6 the values are multiples of 2^-9.
+__device__ __forceinline__ unsigned encode8(float a, unsigned rnd16)
+{
+    const int normal = (int)((__float_as_uint(a) + (rnd16 << 4)) >> 20) - 960;
+    const int small = (int)(a * 512.f + (float)rnd16 * (1.f / 65536.f));
+    return (unsigned)min(a < 0.015625f ? small : normal, 126);
+}
+
+// scale, and 448 / largest (as reciprocal times 448, each rounded), from the bits of a block's largest magnitude.  Not finite: the scale is NaN, as fp32 states would be.
+// Below 2e-36, where 1 / largest times 448 overflows: the block is zero.
+__device__ __forceinline__ float scale8(unsigned top_bits, float &inv)
+{
+    const float top = __uint_as_float(top_bits);
+    if (top_bits >= 0x7f800000u) { inv = 0.f; return __uint_as_float(0x7fc00000u); }
+    if (top < 2e-36f) { inv = 0.f; return 0.f; }
+    inv = (1.f / top) * 448.f;
+    return top * (1.f / 448.f);
+}
+
+__device__ __forceinline__ unsigned wave_max(unsigned v)
+{
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) v = max(v, (unsigned)__shfl_xor((int)v, o, 64));
+    return v;
+}
+
+// A wavefront works on 256 elements that share scales, four per lane; a block's four wavefronts on four times four of them.
+__global__ __launch_bounds__(256) void k_adamw8(const Chunk *__restrict__ table, AdamArgs a, const float *__restrict__ scale)
+{
+    const Chunk c = table[blockIdx.x];
+    float s;
+    if (!step_factor(scale, s)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float keep = fmaf(-a.lr, c.decay, 1.f);
+    unsigned char *m8 = (unsigned char *)c.m, *v8 = (unsigned char *)c.v;
+    for (int b = wave; b * kBlock < c.count; b += 4) {
+        const int i = b * kBlock + lane * 4, left = min(max(c.count - i, 0), 4);
+        float ge[4] = {0.f, 0.f, 0.f, 0.f}, we[4] = {0.f, 0.f, 0.f, 0.f};
+        unsigned mc = 0, vc = 0;
+        if (left == 4) {
+            *reinterpret_cast<float4 *>(ge) = *reinterpret_cast<const float4 *>(c.g + i);
+            *reinterpret_cast<float4 *>(we) = *reinterpret_cast<const float4 *>(c.w + i);
+            mc = *reinterpret_cast<const unsigned *>(m8 + i);
+            vc = *reinterpret_cast<const unsigned *>(v8 + i);
+        } else {
+            for (int e = 0; e < left; ++e) {
+                ge[e] = c.g[i + e]; we[e] = c.w[i + e];
+                mc |= (unsigned)m8[i + e] << (8 * e); vc |= (unsigned)v8[i + e] << (8 * e);
+            }
+        }
+        const float msc = c.ms[b], vsc = c.vs[b];
+        float me[4] = {__builtin_amdgcn_cvt_f32_fp8(mc, 0), __builtin_amdgcn_cvt_f32_fp8(mc, 1), __builtin_amdgcn_cvt_f32_fp8(mc, 2), __builtin_amdgcn_cvt_f32_fp8(mc, 3)};
+        float re[4] = {__builtin_amdgcn_cvt_f32_fp8(vc, 0), __builtin_amdgcn_cvt_f32_fp8(vc, 1), __builtin_amdgcn_cvt_f32_fp8(vc, 2), __builtin_amdgcn_cvt_f32_fp8(vc, 3)};
+        unsigned mtop = 0, rtop = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            me[e] *= msc;
+            const float root = re[e] * vsc;
+            float v = root * root;
+            adam_moments(a, ge[e] * s, me[e], v);
+            if (e >= left) { me[e] = 0.f; v = 0.f; }   // past the end, also with a scale that is NaN
+            re[e] = sqrtf(v);
+            we[e] = adam_weight(a, keep, we[e], me[e], re[e]);
+            mtop = max(mtop, __float_as_uint(fabsf(me[e])));
+            rtop = max(rtop, __float_as_uint(fabsf(re[e])));
+        }
+        float minv, rinv;
+        const float mscale = scale8(wave_max(mtop), minv), rscale = scale8(wave_max(rtop), rinv);
+        unsigned mo = 0, vo = 0;
+        const unsigned long long pair = ((unsigned long long)blockIdx.x * kChunk + (unsigned)i) >> 1;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const unsigned long long r = splitmix64(a.seed, pair + (e >> 1)) >> (32 * (e & 1));
+            unsigned code = encode8(fabsf(me[e]) * minv, (unsigned)r & 0xffffu);
+            if (me[e] < 0.f) code |= 0x80u;
+            mo |= code << (8 * e);
+            // a positive sqrt(v) stays positive: as 0 it would let the next step's update grow
+            const float ra = re[e] * rinv;
+            code = encode8(ra, (unsigned)(r >> 16) & 0xffffu);
+            vo |= (ra > 0.f ? max(code, 1u) : code) << (8 * e);
+        }
+        if (left == 4) {
+            *reinterpret_cast<float4 *>(c.w + i) = *reinterpret_cast<float4 *>(we);
+            *reinterpret_cast<unsigned *>(m8 + i) = mo;
+            *reinterpret_cast<unsigned *>(v8 + i) = vo;
+            if (c.w16 != nullptr) {
+                Pack<bf16_t, 4> o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o.v[e] = from_f32<bf16_t>(we[e]);
+                *reinterpret_cast<Pack<bf16_t, 4> *>(c.w16 + i) = o;
+            }
+        } else {
+            for (int e = 0; e < left; ++e) {
+                c.w[i + e] = we[e];
+                m8[i + e] = (unsigned char)(mo >> (8 * e)); v8[i + e] = (unsigned char)(vo >> (8 * e));
+                if (c.w16 != nullptr) c.w16[i + e] = from_f32<bf16_t>(we[e]);
+            }
+        }
+        if (lane == 0) { c.ms[b] = mscale; c.vs[b] = rscale; }
+    }
+}
+
+// ---- checks -------------------------------------------------------------------------------------------------------
+
+constexpr int64_t kMaxCount = (int64_t)1 << 40;
+constexpr int64_t kMaxChunks = (1 << 24) - 1;   // a grid has fewer than 2^32 threads
+
+struct Range { uintptr_t lo, hi; int param; };
+
+dp_status check_param(const dp_param &p, int i, int state, bool &updates)
+{
+    if (p.count < 0 || p.count > kMaxCount) { dp_set_error("parameter %d: count %lld", i, (long long)p.count); return DP_ERR_BAD_DESC; }
+    if (p.count == 0) return DP_OK;
+    if (p.grad == nullptr) { dp_set_error("parameter %d: grad is NULL", i); return DP_ERR_NULL; }
+    const bool any = p.w32 != nullptr || p.w_bf16 != nullptr || p.m != nullptr || p.v != nullptr || p.m_scale != nullptr || p.v_scale != nullptr;
+    if (!any) updates = false;
+    else if (p.w32 == nullptr || p.m == nullptr || p.v == nullptr || (state == DP_STATE_Q8 && (p.m_scale == nullptr || p.v_scale == nullptr))) {
+        dp_set_error("parameter %d: w32, m, v%s are needed together", i, state == DP_STATE_Q8 ? ", m_scale, v_scale" : "");
+        return DP_ERR_NULL;
+    }
+    if (!aligned16(p.grad) || !aligned16(p.w32) || !aligned16(p.w_bf16) || !aligned16(p.m) || !aligned16(p.v) || !aligned16(p.m_scale) || !aligned16(p.v_scale)) {
+        dp_set_error("parameter %d: pointers must be 16-byte aligned", i);
+        return DP_ERR_BAD_DESC;
+    }
+    if (!std::isfinite(p.weight_decay) || p.weight_decay < 0.f) { dp_set_error("parameter %d: weight_decay must be finite and not negative", i); return DP_ERR_BAD_DESC; }
+    return DP_OK;
+}
+
+// memory that a step writes: two parameters that share some would race
+dp_status check_overlap(const dp_param *params, int n, int state)
+{
+    std::vector<Range> r;
+    auto add = [&](const void *p, int64_t bytes, int i) { if (p != nullptr) r.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, i}); };
+    for (int i = 0; i < n; ++i) {
+        const dp_param &p = params[i];
+        if (p.count == 0) continue;
+        const int64_t state_bytes = state == DP_STATE_Q8 ? p.count : 4 * p.count, scales = 4 * ((p.count + kBlock - 1) / kBlock);
+        add(p.w32, 4 * p.count, i); add(p.w_bf16, 2 * p.count, i); add(p.m, state_bytes, i); add(p.v, state_bytes, i);
+        if (state == DP_STATE_Q8) { add(p.m_scale, scales, i); add(p.v_scale, scales, i); }
+    }
+    std::sort(r.begin(), r.end(), [](const Range &x, const Range &y) { return x.lo < y.lo; });
+    for (size_t k = 1; k < r.size(); ++k)
+        if (r[k].lo < r[k - 1].hi) { dp_set_error("parameters %d and %d share memory that a step writes", r[k - 1].param, r[k].param); return DP_ERR_BAD_DESC; }
+    return DP_OK;
+}
+
+int64_t chunks_of(int64_t count) { return (count + kChunk - 1) / kChunk; }
+
+dp_status check_list(const dp_param_list *list)
+{
+    if (list == nullptr) { dp_set_error("parameter list is NULL"); return DP_ERR_NULL; }
+    if (list->n_chunks < 0 || list->n_chunks > kMaxChunks || (list->state != DP_STATE_F32 && list->state != DP_STATE_Q8)) {
+        dp_set_error("not a list that dp_param_table_build has filled in");
+        return DP_ERR_BAD_DESC;
+    }
+    if (list->n_chunks > 0 && list->table == nullptr) { dp_set_error("parameter list: no table"); return DP_ERR_NULL; }
+    if ((reinterpret_cast<uintptr_t>(list->table) & 63u) != 0) { dp_set_error("parameter list: the table must be 64-byte aligned"); return DP_ERR_BAD_DESC; }
+    return DP_OK;
+}
+
+}  // namespace
+
+extern "C" size_t dp_param_table_bytes(const dp_param *params, int32_t n_params)
+{
+    if (params == nullptr || n_params < 0) return 0;
+    int64_t chunks = 0;
+    for (int i = 0; i < n_params; ++i) {
+        if (params[i].count < 0 || params[i].count > kMaxCount) return 0;
+        chunks += chunks_of(params[i].count);
+    }
+    return (size_t)chunks * sizeof(Chunk);
+}
+
+extern "C" dp_status dp_param_table_build(const dp_param *params, int32_t n_params, int32_t state, void *host_table, size_t host_table_bytes,
+                                          const void *device_table, dp_param_list *list)
+{
+    if (list == nullptr || (params == nullptr && n_params != 0)) { dp_set_error("parameter table: null pointer"); return DP_ERR_NULL; }
+    if (n_params < 0) { dp_set_error("parameter table: negative number of parameters"); return DP_ERR_BAD_DESC; }
+    if (state != DP_STATE_F32 && state != DP_STATE_Q8) { dp_set_error("parameter table: unknown state format %d", state); return DP_ERR_UNSUPPORTED; }
+    bool updates = true;
+    int64_t chunks = 0, elements = 0;
+    for (int i = 0; i < n_params; ++i) {
+        const dp_status s = check_param(params[i], i, state, updates);
+        if (s != DP_OK) return s;
+        chunks += chunks_of(params[i].count);
+        elements += params[i].count;
+    }
+    if (chunks > kMaxChunks) { dp_set_error("parameter table: too many elements"); return DP_ERR_BAD_DESC; }
+    if (chunks > 0 && (host_table == nullptr || device_table == nullptr)) { dp_set_error("parameter table: null pointer"); return DP_ERR_NULL; }
+    if ((reinterpret_cast<uintptr_t>(device_table) & 63u) != 0) { dp_set_error("parameter table: the device address must be 64-byte aligned"); return DP_ERR_BAD_DESC; }
+    if (host_table_bytes < (size_t)chunks * sizeof(Chunk)) {
+        dp_set_error("parameter table: needs %zu bytes, got %zu", (size_t)chunks * sizeof(Chunk), host_table_bytes);
+        return DP_ERR_WORKSPACE;
+    }
+    if (updates) {
+        dp_status s;
+        try { s = check_overlap(params, n_params, state); }
+        catch (...) { dp_set_error("parameter table: out of host memory"); return DP_ERR_HIP; }
+        if (s != DP_OK) return s;
+    }
+    unsigned char *out = (unsigned char *)host_table;
+    const int64_t es = state == DP_STATE_Q8 ? 1 : 4;
+    for (int i = 0; i < n_params; ++i) {
+        const dp_param &p = params[i];
+        for (int64_t at = 0; at < p.count; at += kChunk, out += sizeof(Chunk)) {
+            Chunk c = {};
+            c.g = p.grad + at;
+            if (updates) {
+                c.w = p.w32 + at;
+                c.w16 = p.w_bf16 != nullptr ? (bf16_t *)p.w_bf16 + at : nullptr;
+                c.m = (char *)p.m + at * es;
+                c.v = (char *)p.v + at * es;
+                if (state == DP_STATE_Q8) { c.ms = p.m_scale + at / kBlock; c.vs = p.v_scale + at / kBlock; }
+            }
+            c.count = (int)std::min<int64_t>(kChunk, p.count - at);
+            c.decay = p.weight_decay;
+            __builtin_memcpy(out, &c, sizeof c);
+        }
+    }
+    list->table = device_table;
+    list->n_chunks = chunks;
+    list->n_elements = elements;
+    list->n_params = n_params;
+    list->state = state;
+    list->updates = updates ? 1 : 0;
+    list->reserved = 0;
+    return DP_OK;
+}
+
+extern "C" size_t dp_grad_norm_workspace_bytes(const dp_param_list *list)
+{
+    if (list == nullptr || list->n_chunks < 0) return 0;
+    return (size_t)norm_blocks(list->n_chunks) * sizeof(double);
+}
+
+extern "C" dp_status dp_grad_norm(const dp_param_list *list, float max_norm, float *norm_and_scale, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    const dp_status s = check_list(list);
+    if (s != DP_OK) return s;
+    if (norm_and_scale == nullptr) { dp_set_error("gradient norm: no output"); return DP_ERR_NULL; }
+    if (!(max_norm > 0.f)) { dp_set_error("gradient norm: max_norm must be positive (INFINITY: no clipping)"); return DP_ERR_BAD_DESC; }
+    if (!aligned16(norm_and_scale) || !aligned16(ws)) { dp_set_error("gradient norm: pointers must be 16-byte aligned"); return DP_ERR_BAD_DESC; }
+    const size_t need = dp_grad_norm_workspace_bytes(list);
+    if (ws == nullptr || ws_bytes < need) { dp_set_error("gradient norm needs %zu workspace bytes, got %zu", need, ws == nullptr ? (size_t)0 : ws_bytes); return DP_ERR_WORKSPACE; }
+    hipStream_t st = (hipStream_t)hip_stream;
+    const int blocks = norm_blocks(list->n_chunks);
+    hipLaunchKernelGGL(k_norm_partial, dim3(blocks), dim3(256), 0, st, (const Chunk *)list->table, (long long)list->n_chunks, (double *)ws);
+    hipLaunchKernelGGL(k_norm_final, dim3(1), dim3(256), 0, st, (const double *)ws, blocks, max_norm, norm_and_scale);
+    return launched("gradient norm");
+}
+
+extern "C" dp_status dp_adamw_step(const dp_param_list *list, const dp_adamw_hyper *h, const float *grad_scale, void *hip_stream)
+{
+    const dp_status s = check_list(list);
+    if (s != DP_OK) return s;
+    if (h == nullptr) { dp_set_error("AdamW: hyper-parameters are NULL"); return DP_ERR_NULL; }
+    if (!list->updates && list->n_chunks > 0) { dp_set_error("AdamW: the list has gradients only"); return DP_ERR_NULL; }
+    if (!(h->beta1 >= 0.0 && h->beta1 < 1.0 && h->beta2 >= 0.0 && h->beta2 < 1.0)) { dp_set_error("AdamW: beta1 and beta2 must be in [0, 1)"); return DP_ERR_BAD_DESC; }
+    // without eps in fp32 an element that never had a gradient would become 0 / 0
+    if (!std::isfinite((float)h->lr) || !((float)h->eps > 0.f) || !std::isfinite((float)h->eps)) { dp_set_error("AdamW: lr must be finite in fp32, eps finite and positive"); return DP_ERR_BAD_DESC; }
+    if (h->step < 1) { dp_set_error("AdamW: steps count from 1"); return DP_ERR_BAD_DESC; }
+    if ((reinterpret_cast<uintptr_t>(grad_scale) & 3u) != 0) { dp_set_error("AdamW: grad_scale must be 4-byte aligned"); return DP_ERR_BAD_DESC; }
+    if (list->n_chunks == 0) return DP_OK;
+    AdamArgs a;
+    a.beta1 = (float)h->beta1; a.beta2 = (float)h->beta2;
+    a.one_minus_beta1 = (float)(1.0 - h->beta1); a.one_minus_beta2 = (float)(1.0 - h->beta2);
+    a.step_size = (float)(h->lr / (1.0 - std::pow(h->beta1, (double)h->step)));
+    a.inv_root_bc2 = (float)(1.0 / std::sqrt(1.0 - std::pow(h->beta2, (double)h->step)));
+    a.eps = (float)h->eps; a.lr = (float)h->lr;
+    a.seed = h->seed;
+    const dim3 grid((unsigned)list->n_chunks), block(256);
+    if (list->state == DP_STATE_Q8) hipLaunchKernelGGL(k_adamw8, grid, block, 0, (hipStream_t)hip_stream, (const Chunk *)list->table, a, grad_scale);
+    else hipLaunchKernelGGL(k_adamw, grid, block, 0, (hipStream_t)hip_stream, (const Chunk *)list->table, a, grad_scale);
+    return launched("AdamW step");
+}

@@ -1,0 +1,259 @@
+"""GPU parity of group normalisation with an activation against oracle/train_ops.py, through the C ABI.
+
+Tolerances, from the arithmetic: statistics and the normalisation are fp32, sums are trees or chains of partial means, so an output's
+error is a few 2^-24 of the largest value that enters it: x's offset over its spread (mean), or 1.  2e-6 of that, plus half a unit of
+bf16 (2^-9, doubled for the neighbour that fp32 may tip it into) where the output is bf16.  Sums over samples and pixels (dgamma,
+dbeta) are measured against the sum of magnitudes."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+EPS = 1e-5
+
+
+@pytest.fixture(scope="module")
+def env():
+    from paper_2112_10065_amd import binding as dp, synth
+    from oracle import train_ops
+    import gpu_util as U
+    assert torch.cuda.is_available()
+    return dp, U, train_ops, synth
+
+
+# n, h, w, c, groups: whole vectors and not, groups inside, across and wider than a vector, one element per group, slabs
+# of channels, one pixel, pixels that no block divides, long images, many samples
+SHAPES = [(1, 1, 1, 8, 1), (1, 1, 1, 32, 32), (2, 1, 3, 16, 4), (1, 14, 14, 512, 32), (2, 7, 9, 64, 32), (3, 5, 4, 80, 8), (2, 6, 6, 12, 3),
+          (2, 33, 31, 24, 24), (1, 9, 9, 7, 7), (2, 5, 5, 15, 5), (1, 3, 3, 2048, 32), (2, 2, 2, 4096, 1), (1, 4, 4, 5000, 8), (1, 2, 2, 601, 1),
+          (5, 17, 13, 48, 2), (2, 112, 111, 64, 32), (1, 300, 1, 16, 2), (40, 2, 3, 32, 8), (1, 57, 56, 256, 32), (3, 28, 28, 512, 32), (1, 61, 3, 264, 33)]
+
+
+def values(synth, tag, shape, bf16, scale=1.0, offset=0.0):
+    x = (synth.normal(tag, shape) * scale + offset).astype(np.float32)
+    return synth.round_bf16(x) if bf16 else x
+
+
+def upload(U, a, bf16):
+    from paper_2112_10065_amd import synth
+    return U.bf16_dev(synth.f32_to_bf16_bits(a)) if bf16 else torch.from_numpy(np.ascontiguousarray(a)).to(U.DEV)
+
+
+class Case:
+    def __init__(self, env, shape, act, bf16, scale=1.0, offset=0.0, affine=True):
+        dp, U, O, synth = env
+        self.dp, self.U, self.O = dp, U, O
+        self.n, self.h, self.w, self.c, self.groups = shape
+        self.act, self.bf16, self.tdt = act, bf16, torch.bfloat16 if bf16 else torch.float32
+        full = shape[:4]
+        tag = f"gn/{shape}/{act}/{scale}/{offset}"
+        self.x = values(synth, tag, full, bf16, scale, offset)
+        self.dy = values(synth, tag + "/dy", full, bf16)
+        self.gamma = (1 + 0.3 * synth.normal(tag + "/g", (self.c,))).astype(np.float32) if affine else None
+        self.beta = (0.3 * synth.normal(tag + "/b", (self.c,))).astype(np.float32) if affine else None
+        flags = {"none": 0, "relu": dp.DP_RELU, "silu": dp.DP_SILU}[act]
+        self.desc = dp.group_norm_desc(self.n, self.h, self.w, self.c, self.groups, dp.DP_BF16 if bf16 else dp.DP_F32, flags, EPS)
+        self.dev = {k: upload(U, v, b) if v is not None else None for k, v, b in
+                    (("x", self.x, bf16), ("dy", self.dy, bf16), ("gamma", self.gamma, False), ("beta", self.beta, False))}
+        self.one = lambda v: np.ones(self.c) if v is None else v.astype(np.float64)    # noqa: E731
+        self.zero = lambda v: np.zeros(self.c) if v is None else v.astype(np.float64)  # noqa: E731
+
+    def ws(self, pass_):
+        return torch.full((self.dp.dp_group_norm_workspace_bytes(self.desc, pass_),), 0xff, dtype=torch.uint8, device=self.U.DEV)
+
+    def forward(self, stats=True, stream=None):
+        d, U = self.dev, self.U
+        y = torch.full((self.n, self.h, self.w, self.c), 7.0, dtype=self.tdt, device=U.DEV)
+        mean, rstd = (torch.full((self.n, self.groups), 7.0, device=U.DEV) for _ in range(2))
+        self.dp.dp_group_norm_fwd(self.desc, d["x"], d["gamma"], d["beta"], y, mean if stats else None, rstd if stats else None, self.ws(0), stream)
+        return y, mean, rstd
+
+    def backward(self, y, mean, rstd, want=(True, True, True), dx=None, stream=None):
+        d, U = self.dev, self.U
+        dx = dx if dx is not None else torch.full((self.n, self.h, self.w, self.c), 7.0, dtype=self.tdt, device=U.DEV)
+        dgamma, dbeta = (torch.full((self.c,), 7.0, device=U.DEV) for _ in range(2))
+        got = [t if w else None for t, w in zip((dx, dgamma, dbeta), want)]
+        self.dp.dp_group_norm_bwd(self.desc, d["x"], d["dy"], y, d["gamma"], d["beta"], mean, rstd, *got, self.ws(1), stream)
+        return got
+
+    def check_forward(self, y, mean, rstd):
+        U, O = self.U, self.O
+        want_y, want_mean, want_rstd = O.group_norm_fwd(self.x, self.one(self.gamma), self.zero(self.beta), self.groups, EPS, self.act)
+        big = np.abs(self.x).max() + 1e-30
+        assert np.abs(U.to_np(mean) - want_mean).max() <= 2e-6 * big
+        # a relative error of the variance, with what the mean's error adds
+        assert np.abs(U.to_np(rstd) / want_rstd - 1).max() <= 2e-6 * max(1.0, (big * want_rstd.max()))
+        lim = 2e-6 * np.repeat(want_rstd, self.c // self.groups, axis=1)[:, None, None, :] * big * np.abs(self.one(self.gamma)) * 4 + 2e-6
+        lim = lim + (2.0 ** -8 * np.abs(want_y) if self.bf16 else 0.0)
+        assert np.all(np.abs(U.to_np(y) - want_y) <= lim)
+
+    def check_backward(self, got, y, mean, rstd):
+        U, O = self.U, self.O
+        y_saved = U.to_np(y) if y is not None else None
+        m, r = U.to_np(mean), U.to_np(rstd)
+        dx, dgamma, dbeta = O.group_norm_bwd(self.x, self.dy, self.one(self.gamma), self.zero(self.beta), m, r, self.groups, self.act, y_saved)
+        xhat = O._xhat(self.x, m.astype(np.float64), r.astype(np.float64), self.groups)
+        off = np.abs(m * r).max()          # x's offset in units of its spread: what x - mean loses
+        big = max(1.0, np.abs(xhat).max()) ** 2 * np.abs(self.dy).max() * np.abs(self.one(self.gamma)).max() * r.max()
+        if got[0] is not None:
+            lim = 2e-6 * (1 + off) * 4 * big + (2.0 ** -8 * np.abs(dx) if self.bf16 else 0.0)
+            assert np.all(np.abs(U.to_np(got[0]) - dx) <= lim)
+        mass = np.abs(self.dy).astype(np.float64)
+        for g, want, m_ in ((got[1], dgamma, (mass * (1 + np.abs(xhat))).sum(axis=(0, 1, 2))), (got[2], dbeta, mass.sum(axis=(0, 1, 2)))):
+            if g is not None:
+                assert np.all(np.abs(U.to_np(g) - want) <= 4e-6 * (1 + off) * m_)
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("act", ["none", "relu", "silu"])
+@pytest.mark.parametrize("shape", SHAPES, ids=["x".join(map(str, s)) for s in SHAPES])
+def test_group_norm(env, shape, act, bf16):
+    k = Case(env, shape, act, bf16, scale=1.5, offset=0.5)
+    y, mean, rstd = k.forward()
+    k.check_forward(y, mean, rstd)
+    got = k.backward(y, mean, rstd)
+    torch.cuda.synchronize()
+    k.check_backward(got, y if act == "relu" else None, mean, rstd)
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("scale,offset", [(1.0, 1000.0), (1e-3, 1.0), (1e4, 0.0), (1e-6, 0.0), (0.0, 3.0)])
+def test_offsets_and_scales(env, scale, offset, bf16):
+    """A large offset costs x - mean its last bits and the variance nothing more; a constant image has variance 0."""
+    k = Case(env, (2, 40, 37, 32, 8), "silu", bf16, scale, offset)
+    y, mean, rstd = k.forward()
+    k.check_forward(y, mean, rstd)
+    k.check_backward(k.backward(y, mean, rstd), None, mean, rstd)
+
+
+def test_relu_gradient_that_is_masked_already(env):
+    k = Case(env, (2, 9, 9, 32, 4), "relu", True)
+    y, mean, rstd = k.forward()
+    k.check_backward(k.backward(None, mean, rstd), None, mean, rstd)
+
+
+@pytest.mark.parametrize("want", [(True, False, False), (False, True, False), (False, False, True), (False, True, True), (True, False, True)])
+def test_outputs_are_optional(env, want):
+    k = Case(env, (2, 9, 11, 48, 3), "silu", True)
+    y, mean, rstd = k.forward()
+    assert torch.equal(k.forward(stats=False)[0], y)
+    whole, some = k.backward(y, mean, rstd), k.backward(y, mean, rstd, want)
+    for a, b, w in zip(whole, some, want):
+        assert (b is None) == (not w) and (not w or torch.equal(a, b))
+
+
+def test_without_gamma_and_beta(env):
+    k = Case(env, (2, 9, 11, 48, 3), "relu", True, affine=False)
+    y, mean, rstd = k.forward()
+    k.check_forward(y, mean, rstd)
+    k.check_backward(k.backward(y, mean, rstd), y, mean, rstd)
+
+
+def test_gradient_in_place_of_dy(env):
+    for shape in ((1, 14, 14, 512, 32), (2, 50, 50, 64, 32)):
+        k = Case(env, shape, "silu", True)
+        y, mean, rstd = k.forward()
+        want = k.backward(y, mean, rstd)
+        got = k.backward(y, mean, rstd, dx=k.dev["dy"])
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+def test_values_that_are_not_finite_stay_in_their_group(env, bf16):
+    dp, U, O, synth = env
+    for shape in ((2, 9, 9, 32, 4), (1, 30, 30, 24, 3)):
+        k = Case(env, shape, "relu", bf16)
+        clean = [t.clone() for t in k.forward()]
+        for bad in (float("nan"), float("inf")):
+            k.dev["x"] = upload(U, k.x, bf16)
+            k.dev["x"][0, 3, 2, 9] = bad
+            y, mean, rstd = k.forward()
+            cg = shape[3] // shape[4]
+            g = 9 // cg
+            hit = torch.zeros_like(y, dtype=torch.bool)
+            hit[0, :, :, g * cg:(g + 1) * cg] = True
+            assert torch.equal(y[~hit], clean[0][~hit]) and bool(torch.isnan(y[0, 3, 2, 9]))
+            assert bool(torch.isnan(rstd[0, g])) and not bool(torch.isfinite(mean[0, g]))
+
+
+def test_results_repeat_and_streams(env):
+    """Bitwise the same every time, on another stream, and while other work runs."""
+    k = Case(env, (4, 56, 56, 64, 32), "silu", True)
+    first = [t.clone() for t in k.forward()]
+    back = [t.clone() for t in k.backward(*first)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            got = k.forward(stream=side)
+            grad = k.backward(*got, stream=side)
+        busy = torch.randn(2048, 2048, device="cuda") @ torch.randn(2048, 2048, device="cuda")
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(first + back, list(got) + list(grad)))
+        del busy
+
+
+def test_in_a_graph(env):
+    """Captured once, replayed on new inputs between eager work: the eager results every time."""
+    dp, U, O, synth = env
+    k = Case(env, (2, 28, 28, 128, 32), "silu", True)
+    d, shape = k.dev, (2, 28, 28, 128)
+    y, dx = (torch.empty(shape, dtype=k.tdt, device=U.DEV) for _ in range(2))
+    mean, rstd = (torch.empty((2, 32), device=U.DEV) for _ in range(2))
+    dgamma, dbeta = (torch.empty(128, device=U.DEV) for _ in range(2))
+    ws = [k.ws(0), k.ws(1)]
+
+    def both():
+        dp.dp_group_norm_fwd(k.desc, d["x"], d["gamma"], d["beta"], y, mean, rstd, ws[0])
+        dp.dp_group_norm_bwd(k.desc, d["x"], d["dy"], None, d["gamma"], d["beta"], mean, rstd, dx, dgamma, dbeta, ws[1])
+
+    both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    outs = (y, mean, rstd, dx, dgamma, dbeta)
+    for i in range(4):
+        d["x"].copy_(torch.randn(shape, device=U.DEV, generator=torch.Generator(U.DEV).manual_seed(i)))
+        both()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in outs]
+        for t in outs:
+            t.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, outs))
+
+
+def test_full_size(env):
+    """The first layers' activation at per-GPU batch 32: two samples against the oracle, all of them by what the norm makes of them."""
+    dp, U, O, synth = env
+    n, h, w, c, groups = 32, 224, 224, 64, 32
+    gen = torch.Generator(U.DEV).manual_seed(3)
+    x = (torch.randn((n, h, w, c), device=U.DEV, generator=gen) * 1.5 + 0.5).to(torch.bfloat16)
+    dy = torch.randn((n, h, w, c), device=U.DEV, generator=gen).to(torch.bfloat16)
+    gamma, beta = (1 + 0.3 * torch.randn(c, device=U.DEV, generator=gen)), 0.3 * torch.randn(c, device=U.DEV, generator=gen)
+    desc = dp.group_norm_desc(n, h, w, c, groups, dp.DP_BF16, dp.DP_SILU, EPS)
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd = (torch.empty((n, groups), device=U.DEV) for _ in range(2))
+    dgamma, dbeta = (torch.empty(c, device=U.DEV) for _ in range(2))
+    ws = U.workspace(max(dp.dp_group_norm_workspace_bytes(desc, p) for p in (0, 1)))
+    dp.dp_group_norm_fwd(desc, x, gamma, beta, y, mean, rstd, ws)
+    dp.dp_group_norm_bwd(desc, x, dy, None, gamma, beta, mean, rstd, dx, dgamma, dbeta, ws)
+    torch.cuda.synchronize()
+    g64, b64 = (t.cpu().numpy().astype(np.float64) for t in (gamma, beta))
+    for i in (0, 31):
+        xi, dyi = U.to_np(x[i:i + 1]), U.to_np(dy[i:i + 1])
+        wy, wm, wr = O.group_norm_fwd(xi, g64, b64, groups, EPS, "silu")
+        wdx, _, _ = O.group_norm_bwd(xi, dyi, g64, b64, wm, wr, groups, "silu")
+        assert np.abs(U.to_np(mean[i:i + 1]) - wm).max() <= 2e-6 * 10 and np.abs(U.to_np(rstd[i:i + 1]) / wr - 1).max() <= 2e-6 * 10
+        assert np.all(np.abs(U.to_np(y[i:i + 1]) - wy) <= 2.0 ** -8 * np.abs(wy) + 1e-4)
+        assert np.all(np.abs(U.to_np(dx[i:i + 1]) - wdx) <= 2.0 ** -8 * np.abs(wdx) + 1e-4)
+    # sums over 1.6 million pixels, in 64 bits on the device
+    xh = (x.double().view(n, h * w, groups, 2) - mean.double()[:, None, :, None]) * rstd.double()[:, None, :, None]
+    u = xh.view(n, h, w, c) * gamma.double() + beta.double()
+    s = torch.sigmoid(u)
+    g = dy.double() * (s + u * s * (1 - s))
+    assert bool(((dbeta - g.sum(dim=(0, 1, 2))).abs() <= 4e-6 * g.abs().sum(dim=(0, 1, 2))).all())
+    gx = g * xh.view(n, h, w, c)
+    assert bool(((dgamma - gx.sum(dim=(0, 1, 2))).abs() <= 4e-6 * (g.abs() + gx.abs()).sum(dim=(0, 1, 2))).all())

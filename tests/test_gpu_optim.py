@@ -1,0 +1,288 @@
+"""GPU parity of the gradient norm and the AdamW step over lists of tensors against oracle/train_ops.py, through the C ABI.
+
+The moments, the 8-bit codes and their scales are defined to the last bit (every operation rounded to fp32 in the order of the definition) and
+have to be equal to the oracle's that does the same; that one is held to the definition in 64 bits by the terms' magnitudes.
+Tolerances of the weights, from the arithmetic: they add an update whose relative error is that of m over sqrt(v) plus a division (1e-6 of the
+update) to a rounded product (1.2e-7 of w)."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+HYPER = dict(lr=2e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=7)
+
+
+@pytest.fixture(scope="module")
+def env():
+    from paper_2112_10065_amd import binding as dp
+    from oracle import train_ops
+    assert torch.cuda.is_available()
+    return dp, train_ops
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+# one tensor of each length class: nothing, one element, inside a vector / a block of 256 / a chunk of 4096, whole ones, and past them
+SIZES = [0, 1, 3, 4, 5, 255, 256, 257, 1000, 4095, 4096, 4097, 64, 8192, 12289, 100003, 0, 300000]
+
+
+class Net:
+    """Tensors of the given sizes on the host and, in one list, on the device."""
+
+    def __init__(self, env, sizes, q8, seed=0, bf16=True, grad_scale=1e-2):
+        self.dp, self.O = env
+        self.sizes, self.q8 = sizes, q8
+        r = np.random.RandomState(seed)
+        self.host, params = [], []
+        first = 0
+        for i, n in enumerate(sizes):
+            h = dict(g=(r.randn(n) * grad_scale * 10.0 ** (i % 3)).astype(np.float32), w=(r.randn(n) * 0.1).astype(np.float32), first=first,
+                     decay=float(np.float32(0.1 * (i % 2))))
+            first += -(-n // 4096) * 4096
+            m, v = (r.randn(n) * 1e-3).astype(np.float32), (r.rand(n) * 1e-5).astype(np.float32)
+            if q8:
+                h["m8"], ms = self.O.store8(m, r.randint(0, 65536, n)) if n else (np.zeros(0, np.uint8), np.zeros(0))
+                h["v8"], vs = self.O.store8(np.sqrt(v), r.randint(0, 65536, n), True) if n else (np.zeros(0, np.uint8), np.zeros(0))
+                h["ms"], h["vs"] = ms.astype(np.float32), vs.astype(np.float32)
+            else:
+                h["m"], h["v"] = m, v
+            self.host.append(h)
+            p = dict(grad=dev(h["g"]), w32=dev(h["w"]), weight_decay=h["decay"])
+            if bf16 and i % 4 != 3:
+                p["w_bf16"] = torch.full((n,), 9.0, dtype=torch.bfloat16, device="cuda")
+            if q8:
+                p.update(m=dev(h["m8"]), v=dev(h["v8"]), m_scale=dev(h["ms"]), v_scale=dev(h["vs"]))
+            else:
+                p.update(m=dev(h["m"]), v=dev(h["v"]))
+            params.append(p)
+        self.params = params
+        self.list = self.dp.param_list(params, self.dp.DP_STATE_Q8 if q8 else self.dp.DP_STATE_F32)
+
+    def state(self):
+        return [t.clone() for p in self.params for k, t in sorted(p.items()) if torch.is_tensor(t)]
+
+    def step(self, scale=None, stream=None, seed=5, **kw):
+        h = {**HYPER, **kw}
+        self.dp.dp_adamw_step(self.list, self.dp.adamw_hyper(seed=seed, **h), scale, stream)
+
+    def check(self, scale=1.0, seed=5, **kw):
+        h = {**HYPER, **kw}
+        for k, p in zip(self.host, self.params):
+            n = len(k["g"])
+            if n == 0:
+                continue
+            got = {a: t.cpu() for a, t in p.items() if torch.is_tensor(t)}
+            hyper = dict(weight_decay=k["decay"], scale=scale, **h)
+            betas = dict(beta1=h["beta1"], beta2=h["beta2"], scale=scale)
+            if self.q8:
+                m, v = self.O.load8_f32(k["m8"], k["ms"]), self.O.load8_f32(k["v8"], k["vs"])
+                v = v * v
+                states = self.O.adamw8_states_f32(k["m8"], k["ms"], k["v8"], k["vs"], k["g"], seed, k["first"], **betas)
+            else:
+                m, v = k["m"], k["v"]
+                states = self.O.moments_f32(m, v, k["g"], **betas)
+            for name, want in zip(("m", "m_scale", "v", "v_scale") if self.q8 else ("m", "v"), states):
+                assert np.array_equal(got[name].numpy(), want), name
+            w, m2, v2 = self.O.adamw(k["w"], m, v, k["g"], **hyper)
+            g = np.abs(k["g"].astype(np.float64)) * abs(scale)
+            fm, fv = self.O.moments_f32(m, v, k["g"], **betas)
+            assert np.all(np.abs(fm - m2) <= 4e-7 * (np.abs(m) + 0.1 * g)) and np.all(np.abs(fv - v2) <= 4e-7 * np.abs(v2))
+            update = np.abs(w - k["w"])
+            # m itself may be the small difference of its terms
+            slack = 4e-7 * h["lr"] * (0.1 * np.abs(k["g"]) * abs(scale) + np.abs(m2)) / (np.sqrt(v2) + 1e-12)
+            assert np.all(np.abs(got["w32"].numpy() - w) <= 1.5e-7 * np.abs(w) + 2e-6 * update + 40 * slack)
+            if "w_bf16" in got:
+                assert torch.equal(got["w_bf16"], got["w32"].to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("q8", [False, True], ids=["f32", "q8"])
+@pytest.mark.parametrize("sizes", [SIZES, SIZES[::-1], [1], [4097], [256] * 300, [0, 0], []], ids=["mixed", "reversed", "one", "odd", "many", "empty", "none"])
+def test_adamw(env, sizes, q8):
+    k = Net(env, sizes, q8)
+    k.step()
+    torch.cuda.synchronize()
+    k.check()
+
+
+@pytest.mark.parametrize("q8", [False, True], ids=["f32", "q8"])
+@pytest.mark.parametrize("kw", [dict(step=1), dict(step=100000), dict(beta1=0.0, beta2=0.0), dict(beta1=0.95, beta2=0.99, eps=1e-3), dict(lr=0.0),
+                                dict(seed=2 ** 64 - 1)], ids=str)
+def test_adamw_hyper_parameters(env, q8, kw):
+    k = Net(env, [3, 1000, 5000], q8, seed=3)
+    k.step(**kw)
+    torch.cuda.synchronize()
+    k.check(**kw)
+
+
+@pytest.mark.parametrize("q8", [False, True], ids=["f32", "q8"])
+def test_adamw_scale_and_skipped_steps(env, q8):
+    k = Net(env, SIZES, q8, seed=4)
+    k.step(scale=torch.tensor([0.25], device="cuda"))
+    torch.cuda.synchronize()
+    k.check(scale=0.25)
+    for skipped in (0.0, float("nan")):
+        k = Net(env, SIZES, q8, seed=4)
+        before = k.state()
+        k.step(scale=torch.tensor([skipped], device="cuda"))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(before, k.state()))
+
+
+def test_adamw_writes_nothing_outside_its_tensors(env):
+    """Tensors inside larger ones: what lies behind each stays."""
+    dp, O = env
+    for q8 in (False, True):
+        for n in (1, 6, 257, 4099):
+            pad = 64
+            blocks = -(-n // 256)
+            mk = lambda size, dt: torch.full((size + pad,), 3, device="cuda").to(dt)   # noqa: E731
+            sdt = torch.uint8 if q8 else torch.float32
+            big = dict(grad=mk(n, torch.float32), w32=mk(n, torch.float32), w_bf16=mk(n, torch.bfloat16), m=mk(n, sdt), v=mk(n, sdt))
+            if q8:
+                big.update(m_scale=mk(blocks, torch.float32), v_scale=mk(blocks, torch.float32))
+            part = {k: t[:blocks if "scale" in k else n] for k, t in big.items()}
+            dp.dp_adamw_step(dp.param_list([part], int(q8)), dp.adamw_hyper(**HYPER))
+            torch.cuda.synchronize()
+            for k, t in big.items():
+                assert bool((t[blocks if "scale" in k else n:].float() == 3).all()), (k, n)
+            assert bool((big["w32"][:n] != 3).all())
+
+
+def test_adamw_zero_state_and_zero_gradients(env):
+    """The first step from zeros; elements without a gradient keep a zero state and an unchanged weight."""
+    dp, O = env
+    n = 1500
+    r = np.random.RandomState(9)
+    g = np.where(r.rand(n) < 0.5, 0.0, r.randn(n)).astype(np.float32)
+    g[512:768] = 0.0
+    for q8 in (False, True):
+        p = dict(grad=dev(g), w32=torch.ones(n, device="cuda"), m=torch.zeros(n, dtype=torch.uint8 if q8 else torch.float32, device="cuda"))
+        p["v"] = p["m"].clone()
+        if q8:
+            p.update(m_scale=torch.zeros(6, device="cuda"), v_scale=torch.zeros(6, device="cuda"))
+        dp.dp_adamw_step(dp.param_list([p], int(q8)), dp.adamw_hyper(lr=0.01, step=1))
+        torch.cuda.synchronize()
+        w, none = p["w32"].cpu().numpy(), g == 0
+        assert np.all(w[none] == 1) and np.allclose(w[~none], 1 - 0.01 * np.sign(g[~none]), atol=1e-5)
+        assert np.all(p["m"].cpu().numpy()[none] % 128 == 0) and np.all(p["v"].cpu().numpy()[none] == 0)
+        if q8:
+            assert float(p["m_scale"][2]) == 0 and float(p["v_scale"][2]) == 0
+            assert np.all(p["v"].cpu().numpy()[~none] > 0)   # a positive second moment never becomes 0
+
+
+def test_adamw8_not_finite_stays_in_its_block(env):
+    for bad in (float("nan"), float("inf")):
+        k = Net(env, [1000], True, seed=6)
+        k.params[0]["grad"][300] = bad
+        k.step()
+        torch.cuda.synchronize()
+        p = {a: t.cpu().numpy() for a, t in k.params[0].items() if a in ("m_scale", "v_scale", "w32")}
+        assert np.isnan(p["m_scale"][1]) and np.isnan(p["v_scale"][1])
+        assert np.all(np.isfinite(p["m_scale"][[0, 2, 3]])) and np.all(np.isfinite(p["w32"][np.arange(1000) != 300]))
+
+
+def test_adamw8_tracks_the_32_bit_state_on_average(env):
+    """Many steps on gradients of one size: rounding to the nearest would leave v where its first steps put it."""
+    dp, O = env
+    n, steps = 8192, 300
+    gen = torch.Generator("cuda").manual_seed(1)
+    size = torch.exp(torch.randn(n, device="cuda", generator=gen))
+    p = {q: dict(grad=torch.empty(n, device="cuda"), w32=torch.zeros(n, device="cuda"), m=torch.zeros(n, dtype=torch.uint8 if q else torch.float32, device="cuda"),
+                 v=torch.zeros(n, dtype=torch.uint8 if q else torch.float32, device="cuda")) for q in (False, True)}
+    p[True].update(m_scale=torch.zeros(n // 256, device="cuda"), v_scale=torch.zeros(n // 256, device="cuda"))
+    lists = {q: dp.param_list([p[q]], int(q)) for q in p}
+    for step in range(1, steps + 1):
+        g = torch.randn(n, device="cuda", generator=gen) * size
+        for q in p:
+            p[q]["grad"].copy_(g)
+            dp.dp_adamw_step(lists[q], dp.adamw_hyper(lr=1e-3, step=step, seed=step))
+    root = p[True]["v"].view(torch.float8_e4m3fn).float().view(-1, 256) * p[True]["v_scale"][:, None]
+    ratio = (root.view(-1) / p[False]["v"].sqrt())[size > size.median()]
+    # unbiased steps of 6 to 12 %: a random walk around 1 that the decay of v holds together, not a drift
+    assert abs(float(ratio.mean()) - 1) < 0.05 and float(ratio.std()) < 0.5
+    travelled = p[False]["w32"].abs().mean()
+    assert float((p[True]["w32"] - p[False]["w32"]).abs().mean()) < 0.25 * float(travelled)
+
+
+@pytest.mark.parametrize("sizes", [SIZES, [1], [5], [0], [], [4096 * 1500 + 17], [64, 64] * 200], ids=["mixed", "one", "five", "zero", "none", "long", "many"])
+@pytest.mark.parametrize("most", [1.0, 1e9, float("inf")])
+def test_grad_norm(env, sizes, most):
+    dp, O = env
+    r = np.random.RandomState(2)
+    grads = [(r.randn(n) * 10.0 ** (i % 3)).astype(np.float32) for i, n in enumerate(sizes)]
+    lst = dp.param_list([dict(grad=dev(g)) for g in grads])
+    out = torch.full((2,), 9.0, device="cuda")
+    ws = torch.full((dp.dp_grad_norm_workspace_bytes(lst),), 0xff, dtype=torch.uint8, device="cuda")
+    dp.dp_grad_norm(lst, most, out, ws)
+    torch.cuda.synchronize()
+    norm, scale = O.grad_norm(grads, most)
+    assert abs(float(out[0]) - norm) <= 1.2e-7 * norm and abs(float(out[1]) - scale) <= 2.4e-7 * scale
+
+
+@pytest.mark.parametrize("values,norm,scale", [([3e38, 3e38], np.inf, None), ([1e30, 0.0], 1e30, 1e-30), ([1e-30, 0.0], 1e-30, 1.0), ([0.0], 0.0, 1.0),
+                                               ([1.0, float("nan")], np.nan, 0.0), ([1.0, float("inf")], np.inf, 0.0)])
+def test_grad_norm_range(env, values, norm, scale):
+    """Squares beyond fp32's range are summed all the same; a norm that is not finite asks for the step to be skipped."""
+    dp, O = env
+    lst = dp.param_list([dict(grad=torch.tensor(values, device="cuda"))])
+    out = torch.empty(2, device="cuda")
+    dp.dp_grad_norm(lst, 1.0, out, torch.empty(dp.dp_grad_norm_workspace_bytes(lst), dtype=torch.uint8, device="cuda"))
+    got = out.cpu().numpy()
+    assert np.isnan(got[0]) if np.isnan(norm) else got[0] == pytest.approx(norm, rel=1e-6)
+    assert scale is None or got[1] == pytest.approx(scale, rel=1e-6)
+
+
+def test_clipped_step_in_a_graph_and_on_another_stream(env):
+    """Norm, then the step by its factor, as a training step issues them: on a stream of their own, and captured and replayed."""
+    for q8 in (False, True):
+        nets = [Net(env, SIZES, q8, seed=8) for _ in range(3)]
+        dp = nets[0].dp
+        side = torch.cuda.Stream()
+        outs = [torch.empty(2, device="cuda") for _ in nets]
+        wss = [torch.empty(dp.dp_grad_norm_workspace_bytes(k.list), dtype=torch.uint8, device="cuda") for k in nets]
+
+        def once(i, stream=None):
+            dp.dp_grad_norm(nets[i].list, 0.5, outs[i], wss[i], stream)
+            nets[i].step(scale=outs[i][1:], stream=stream)
+
+        torch.cuda.synchronize()
+        before = nets[2].state()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            once(2)
+        assert all(torch.equal(a, b) for a, b in zip(before, nets[2].state()))   # capturing runs nothing
+        for _ in range(3):
+            once(0)
+            with torch.cuda.stream(side):
+                once(1, side)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) and torch.equal(a, c) for a, b, c in zip(*(k.state() for k in nets)))
+
+
+def test_whole_network(env):
+    """All 32 tensors of VGG-16 (138 million elements): slices of the largest against the oracle, the norm against one in 64 bits."""
+    dp, O = env
+    from paper_2112_10065_amd import workloads as W
+    sizes = [s for l in W.vgg16_convs() for s in (l.k * l.r * l.s * l.c, l.k)] + [s for l in W.vgg16_linears() for s in (l.in_f * l.out_f, l.out_f)]
+    gen = torch.Generator("cuda").manual_seed(2)
+    rnd = lambda n, s: torch.randn(n, device="cuda", generator=gen) * s   # noqa: E731
+    params = [dict(grad=rnd(n, 1e-3), w32=rnd(n, 0.05), w_bf16=torch.empty(n, dtype=torch.bfloat16, device="cuda"), m=rnd(n, 1e-4), v=rnd(n, 1e-3).square(),
+                   weight_decay=0.05) for n in sizes]
+    big = max(range(len(sizes)), key=lambda i: sizes[i])
+    cut = slice(sizes[big] - 50001, sizes[big])
+    old = {k: params[big][k][cut].cpu().numpy() for k in ("grad", "w32", "m", "v")}
+    lst = dp.param_list(params)
+    out = torch.empty(2, device="cuda")
+    dp.dp_grad_norm(lst, 1.0, out, torch.empty(dp.dp_grad_norm_workspace_bytes(lst), dtype=torch.uint8, device="cuda"))
+    dp.dp_adamw_step(lst, dp.adamw_hyper(**HYPER), out[1:])
+    torch.cuda.synchronize()
+    norm = float(torch.stack([p["grad"].double().square().sum() for p in params]).sum().sqrt())
+    assert abs(float(out[0]) - norm) <= 2e-7 * norm
+    w, m, v = O.adamw(old["w32"], old["m"], old["v"], old["grad"], weight_decay=float(np.float32(0.05)), scale=float(out[1]), **HYPER)
+    got = {k: params[big][k][cut].cpu().numpy() for k in ("w32", "m", "v")}
+    assert np.abs(got["w32"] - w).max() <= 1e-7 and np.abs(got["m"] - m).max() <= 1e-9 and np.all(np.abs(got["v"] - v) <= 4e-7 * v)
+    assert all(torch.equal(p["w_bf16"], p["w32"].to(torch.bfloat16)) for p in params)
