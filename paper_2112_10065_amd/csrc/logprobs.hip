@@ -11,23 +11,32 @@ namespace {
 
 constexpr int NT = 256;
 
+constexpr int kMaxSplits = 64;
+constexpr int kCandidates = 512;   // of a block, in LDS
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+
+struct Soft { float m, s, t; };   // maximum, sum exp(d), sum d exp(d) with d = z - m; nothing yet: -FLT_MAX, 0, 0
+
 struct LpArgs {
     const void *z;
     const int *ids;
     float *logp, *entropy, *lse, *top_logp;
     int *top_ids;
+    Soft *part;                      // [row][split]
+    unsigned long long *part_top;    // [row][split][k], best first; 0: none
     int rows, classes, k;
+    int splits, seg;                 // classes of a split (the last one may be shorter)
     long long stride;
 };
 
 // Orders scores as whole numbers, larger first: value, then the lower index.  -0 counts as 0, a NaN ranks above everything.
-__device__ __forceinline__ unsigned long long key_of(float z, int index)
+__device__ __forceinline__ unsigned order_of(float z)
 {
     z += 0.f;
-    unsigned u = z != z ? 0x7fffffffu : __float_as_uint(z);
-    u ^= (unsigned)((int)u >> 31) | 0x80000000u;
-    return (unsigned long long)u << 32 | (unsigned)~index;
+    const unsigned u = z != z ? 0x7fffffffu : __float_as_uint(z);
+    return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
 }
+__device__ __forceinline__ unsigned long long key_of(float z, int index) { return (unsigned long long)order_of(z) << 32 | (unsigned)~index; }
 __device__ __forceinline__ float score_of(unsigned long long key)
 {
     unsigned u = (unsigned)(key >> 32);
@@ -36,29 +45,35 @@ __device__ __forceinline__ float score_of(unsigned long long key)
 }
 __device__ __forceinline__ int index_of(unsigned long long key) { return (int)~(unsigned)key; }
 
-struct Soft { float m, s, t; };   // maximum, sum exp, sum (z - m) exp
+__device__ __forceinline__ float exp_d(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
 
-__device__ __forceinline__ void add_score(Soft &a, float z)
+// a larger maximum
+__device__ __forceinline__ void raise(Soft &a, float m)
 {
-    if (z > a.m) {
-        const float f = __expf(a.m - z);   // m = -inf at first: f = 0 and s = t = 0
-        a.t = f > 0.f ? fmaf(a.s, a.m - z, a.t) * f : 0.f;   // s (m - z) may pass the range where f is 0
-        a.s *= f;
-        a.m = z;
-    }
-    if (z != -INFINITY) {
-        const float d = z - a.m, e = __expf(d);
-        a.s += e;
-        if (!(d < -200.f)) a.t = fmaf(d, e, a.t);   // below, e is 0, and d may be -inf
+    const float d = a.m - m, f = exp_d(d);
+    a.t = f > 0.f ? fmaf(a.s, d, a.t) * f : 0.f;   // s d may pass the range where f is 0
+    a.s *= f;
+    a.m = m;
+}
+template <int V> __device__ __forceinline__ void add_scores(Soft &a, const float (&z)[V])
+{
+    float m = z[0];
+#pragma unroll
+    for (int e = 1; e < V; ++e) m = fmaxf(m, z[e]);
+    if (m > a.m) raise(a, m);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        const float d = z[e] - a.m, x = exp_d(d);
+        a.s += x;                                   // NaN and +inf scores make this NaN
+        a.t = fmaf(x, fmaxf(d, -3e38f), a.t);       // exp(-inf) * -inf counts as 0
     }
 }
 __device__ __forceinline__ void join(Soft &a, const Soft &b)
 {
     const float m = fmaxf(a.m, b.m);
-    if (m == -INFINITY) { a.s += b.s; a.t += b.t; return; }   // nothing yet on either side, or NaN sums
-    const float da = a.m - m, db = b.m - m, fa = __expf(da), fb = __expf(db);
+    const float da = a.m - m, db = b.m - m, fa = exp_d(da), fb = exp_d(db);
     const float ta = fa > 0.f ? fmaf(a.s, da, a.t) * fa : 0.f, tb = fb > 0.f ? fmaf(b.s, db, b.t) * fb : 0.f;
-    a.s = a.s * fa + b.s * fb;   // a NaN sum stays one
+    a.s = a.s * fa + b.s * fb;
     a.t = ta + tb;
     a.m = m;
 }
@@ -83,45 +98,271 @@ __device__ __forceinline__ unsigned long long wave_top(unsigned long long v)
     return v;
 }
 
-template <typename T>
-__global__ __launch_bounds__(NT) void k_logprobs(LpArgs a)
+// A run of scores as the block reads it: up to V - 1 single ones in front of the first 16-byte boundary, whole vectors, single ones behind.
+// Thread t takes single t of each end (t < V) and vectors t, t + NT, ...
+template <typename T> struct Run {
+    static constexpr int V = 16 / sizeof(T);
+    const T *z;
+    int n, head, vectors;
+    __device__ __forceinline__ Run(const T *p, int count) : z(p), n(count)
+    {
+        const int off = (int)((reinterpret_cast<uintptr_t>(p) / sizeof(T)) & (V - 1));
+        head = off == 0 ? 0 : min(V - off, count);
+        vectors = (count - head) / V;
+    }
+    __device__ __forceinline__ bool aligned_like(const T *p) const { return ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(z)) & 15u) == 0; }
+    __device__ __forceinline__ int first(int v) const { return head + v * V; }
+    __device__ __forceinline__ Pack<T, V> vector(int v) const { return *reinterpret_cast<const Pack<T, V> *>(z + head + v * V); }
+    __device__ __forceinline__ bool before(int t) const { return t < head; }
+    __device__ __forceinline__ int behind(int t) const { const int i = head + vectors * V + t; return t < V && i < n ? i : -1; }
+    __device__ __forceinline__ bool any(int t) const { return t < head || t < vectors || behind(t) >= 0; }
+    // f(score, index) for every score of thread t
+    template <typename F> __device__ __forceinline__ void each(int t, F &&f) const
+    {
+        if (before(t)) f(as_f32(z[t]), t);
+        for (int v = t; v < vectors; v += NT) {
+            const Pack<T, V> q = vector(v);
+#pragma unroll
+            for (int e = 0; e < V; ++e) f(as_f32(q.v[e]), first(v) + e);
+        }
+        const int i = behind(t);
+        if (i >= 0) f(as_f32(z[i]), i);
+    }
+};
+
+// What thread t makes of its scores.
+template <typename T> __device__ __forceinline__ Soft scan(const Run<T> &run)
+{
+    constexpr int V = Run<T>::V, U = 4;
+    const int t = threadIdx.x;
+    Soft mine = {-3.402823466e38f, 0.f, 0.f};
+    if (run.before(t)) { const float z[1] = {as_f32(run.z[t])}; add_scores<1>(mine, z); }
+    if (run.behind(t) >= 0) { const float z[1] = {as_f32(run.z[run.behind(t)])}; add_scores<1>(mine, z); }
+    int v = t;
+    for (; v + (U - 1) * NT < run.vectors; v += U * NT) {
+        Pack<T, V> q[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) q[u] = run.vector(v + u * NT);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float z[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) z[e] = as_f32(q[u].v[e]);
+            add_scores<V>(mine, z);
+        }
+    }
+    for (; v < run.vectors; v += NT) {
+        const Pack<T, V> q = run.vector(v);
+        float z[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) z[e] = as_f32(q.v[e]);
+        add_scores<V>(mine, z);
+    }
+    return mine;
+}
+// all threads' together, the same for each
+__device__ __forceinline__ Soft block_join(Soft mine)
 {
     __shared__ Soft part[NT / 64];
-    __shared__ unsigned long long best[2][NT / 64];
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, r = blockIdx.x;
-    const T *z = (const T *)a.z + (size_t)r * a.stride;
-    Soft mine = {-INFINITY, 0.f, 0.f};
-    for (int c = t; c < a.classes; c += NT) add_score(mine, as_f32(z[c]));
     wave_join(mine);
-    if (lane == 0) part[wave] = mine;
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = mine;
     __syncthreads();
     Soft all = part[0];
     for (int w = 1; w < NT / 64; ++w) join(all, part[w]);
-    const bool none = all.m == -INFINITY && all.s == 0.f;
-    const float log_s = logf(all.s), lse = none ? -INFINITY : all.m + log_s;
-    if (t == 0) {
-        if (a.lse != nullptr) a.lse[r] = lse;
-        if (a.entropy != nullptr) a.entropy[r] = none ? 0.f : log_s - all.t / all.s;
-        if (a.logp != nullptr) {
-            const int id = a.ids[r];
-            a.logp[r] = id < 0 || id >= a.classes ? 0.f : none ? -INFINITY : as_f32(z[id]) - lse;
+    return all;
+}
+
+// The k largest keys of the block's run, best first, to put(rank, key); all threads call it.  `top`: order of the thread's largest
+// score, 0 if it has none; `odd`: its scores hold a NaN or +inf.
+//
+// The k-th largest of the threads' maxima bounds the k-th largest score from below, so only scores from it on are candidates, and only
+// the threads whose maximum reaches it read their scores again.  They append to a list in LDS; each candidate's place is the number of
+// larger ones.  Where very many scores reach the bound (equal ones, or ruled-out classes where fewer than k are left) the list holds those above
+// it and the first k equal to it by index, and where even that does not fit, k rounds take the largest below the one before.
+template <typename T, typename P>
+__device__ __forceinline__ void block_top(const Run<T> &run, int base, int k, unsigned top, bool odd, P &&put)
+{
+    __shared__ unsigned tops[NT];
+    __shared__ unsigned long long list[kCandidates];
+    __shared__ unsigned bound;
+    __shared__ int count, ties, some_odd;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    tops[t] = top;
+    if (t == 0) { count = 0; bound = 0; some_odd = 0; }
+    __syncthreads();
+    if (odd) some_odd = 1;
+    int above = 0;   // maxima that come before this one
+    for (int i = 0; i < NT; i += 4) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(&tops[i]);
+        above += (q.x > top || (q.x == top && i < t)) + (q.y > top || (q.y == top && i + 1 < t)) + (q.z > top || (q.z == top && i + 2 < t)) +
+                 (q.w > top || (q.w == top && i + 3 < t));
+    }
+    if (above == k - 1) bound = top;
+    __syncthreads();
+    const unsigned least = bound;
+    const bool slow = some_odd != 0;
+    if (!slow && top >= least && top != 0)
+        run.each(t, [&](float z, int i) {
+            if (order_of(z) >= least) {
+                const int at = atomicAdd(&count, 1);
+                if (at < kCandidates) list[at] = key_of(z, base + i);
+            }
+        });
+    __syncthreads();
+    bool fits = !slow && count <= kCandidates;
+    if (!slow && !fits) {
+        __syncthreads();
+        if (t == 0) { count = 0; ties = 0; }
+        __syncthreads();
+        if (top > least)
+            run.each(t, [&](float z, int i) {
+                if (order_of(z) > least) {
+                    const int at = atomicAdd(&count, 1);
+                    if (at < kCandidates) list[at] = key_of(z, base + i);
+                }
+            });
+        __syncthreads();
+        fits = count <= kCandidates - k;
+        if (fits && wave == 0) {   // one wavefront finds the first k in order
+            int found = 0;
+            const int have = count;
+            for (int i0 = 0; i0 < run.n && found < k; i0 += 64) {
+                const int i = i0 + lane;
+                const float z = i < run.n ? as_f32(run.z[i]) : 0.f;
+                const bool hit = i < run.n && order_of(z) == least;
+                const unsigned long long hits = __ballot(hit);
+                const int at = found + __popcll(hits & ((1ull << lane) - 1));
+                if (hit && at < k) list[have + at] = key_of(z, base + i);
+                found += __popcll(hits);
+            }
+            if (lane == 0) ties = min(found, k);
         }
+        __syncthreads();
+        if (fits && t == 0) count += ties;
+        __syncthreads();
+    }
+    if (fits) {
+        const int c = count;
+        for (int i = t; i < c; i += NT) {
+            const unsigned long long key = list[i];
+            int rank = 0;
+            for (int j = 0; j < c; ++j) rank += list[j] > key;
+            if (rank < k) put(rank, key);
+        }
+        for (int r = c + t; r < k; r += NT) put(r, 0ull);   // fewer scores than k
+        return;
     }
     unsigned long long last = ~0ull;
-    for (int j = 0; j < a.k; ++j) {   // the largest below the one before
-        unsigned long long top = 0;
-        for (int c = t; c < a.classes; c += NT) {
-            const unsigned long long key = key_of(as_f32(z[c]), c);
-            if (key < last && key > top) top = key;
-        }
-        top = wave_top(top);
-        if (lane == 0) best[j & 1][wave] = top;
+    for (int j = 0; j < k; ++j) {
+        unsigned long long best = 0;
+        run.each(t, [&](float z, int i) {
+            const unsigned long long key = key_of(z, base + i);
+            if (key < last && key > best) best = key;
+        });
+        best = wave_top(best);
         __syncthreads();
-        last = best[j & 1][0];
-        for (int w = 1; w < NT / 64; ++w) last = last > best[j & 1][w] ? last : best[j & 1][w];
-        if (t == 0) {
-            a.top_ids[(size_t)r * a.k + j] = index_of(last);
-            a.top_logp[(size_t)r * a.k + j] = none ? -INFINITY : score_of(last) - lse;
+        if (lane == 0) list[wave] = best;
+        __syncthreads();
+        last = list[0];
+        for (int w = 1; w < NT / 64; ++w) last = last > list[w] ? last : list[w];
+        if (t == 0) put(j, last);
+    }
+}
+
+// log p of a class: the difference from the maximum first, which is exact where it matters, then log s (their sum, lse, cannot hold log s
+// where the scores are large).  A row of nothing but ruled-out classes has -inf.
+__device__ __forceinline__ float log_p(const Soft &all, float log_s, float score) { return all.s == 0.f ? -INFINITY : (score - all.m) - log_s; }
+
+__device__ __forceinline__ void write_row(const LpArgs &a, int r, const Soft &all, float score, bool valid)
+{
+    const bool none = all.s == 0.f;
+    const float log_s = logf(all.s);
+    if (a.lse != nullptr) a.lse[r] = none ? -INFINITY : all.m + log_s;
+    if (a.entropy != nullptr) a.entropy[r] = none ? 0.f : log_s - all.t / all.s;
+    if (a.logp != nullptr) a.logp[r] = valid ? log_p(all, log_s, score) : 0.f;
+}
+
+// Block = (row, split of its classes).
+template <typename T>
+__global__ __launch_bounds__(NT) void k_logprobs(LpArgs a)
+{
+    const int t = threadIdx.x;
+    const int r = blockIdx.x / a.splits, split = blockIdx.x - r * a.splits;
+    const int c0 = split * a.seg;
+    const T *row = (const T *)a.z + (size_t)r * a.stride;
+    const Run<T> run(row + c0, min(a.seg, a.classes - c0));
+    const Soft mine = scan(run);
+    const unsigned top = !run.any(t) ? 0u : mine.s == 0.f ? order_of(-INFINITY) : order_of(mine.m);
+    const bool odd = mine.s != mine.s;
+    const Soft all = block_join(mine);
+    if (a.splits > 1) {
+        const size_t at = (size_t)r * a.splits + split;
+        if (t == 0) a.part[at] = all;
+        unsigned long long *out = a.part_top + at * a.k;
+        if (a.k > 0) block_top(run, c0, a.k, top, odd, [&](int rank, unsigned long long key) { out[rank] = key; });
+        return;
+    }
+    if (t == 0) {
+        const int id = a.logp != nullptr ? a.ids[r] : -1;
+        const bool valid = id >= 0 && id < a.classes;
+        write_row(a, r, all, valid ? as_f32(row[id]) : 0.f, valid);
+    }
+    if (a.k > 0) {
+        const float log_s = logf(all.s);
+        block_top(run, 0, a.k, top, odd, [&](int rank, unsigned long long key) {
+            a.top_ids[(size_t)r * a.k + rank] = index_of(key);
+            a.top_logp[(size_t)r * a.k + rank] = log_p(all, log_s, score_of(key));
+        });
+    }
+}
+
+// Joins the splits of a row.  Block = row.  Each split's keys are in order: with S splits the `need`-th largest of their `each`-th
+// keys, need * each >= k, bounds the k-th largest from below.
+template <typename T>
+__global__ __launch_bounds__(NT) void k_logprobs_join(LpArgs a)
+{
+    __shared__ Soft part[kMaxSplits];
+    __shared__ unsigned long long heads[kMaxSplits], list[kMaxSplits * DP_LOGPROBS_MAX_TOP], bound;
+    __shared__ int count;
+    const int t = threadIdx.x, r = blockIdx.x;
+    const int each = (a.k + a.splits - 1) / a.splits, need = each > 0 ? (a.k + each - 1) / each : 0;
+    const unsigned long long *keys = a.part_top + (size_t)r * a.splits * a.k;
+    if (t < a.splits) {
+        part[t] = a.part[(size_t)r * a.splits + t];
+        if (a.k > 0) heads[t] = keys[(size_t)t * a.k + each - 1];
+    }
+    if (t == 0) { count = 0; bound = 0; }
+    __syncthreads();
+    Soft all = part[0];
+    for (int s = 1; s < a.splits; ++s) join(all, part[s]);
+    if (t == 0) {
+        const int id = a.logp != nullptr ? a.ids[r] : -1;
+        const bool valid = id >= 0 && id < a.classes;
+        write_row(a, r, all, valid ? as_f32(((const T *)a.z)[(size_t)r * a.stride + id]) : 0.f, valid);
+    }
+    if (a.k == 0) return;
+    if (t < a.splits) {
+        const unsigned long long mine = heads[t];
+        int above = 0;
+        for (int s = 0; s < a.splits; ++s) above += heads[s] > mine || (heads[s] == mine && s < t);   // equal only where 0, no key
+        if (above == need - 1) bound = mine;
+    }
+    __syncthreads();
+    const unsigned long long least = bound;
+    for (int i = t; i < a.splits * a.k; i += NT) {
+        const unsigned long long key = keys[i];
+        if (key != 0 && key >= least) list[atomicAdd(&count, 1)] = key;
+    }
+    __syncthreads();
+    const int c = count;
+    const float log_s = logf(all.s);
+    for (int i = t; i < c; i += NT) {
+        const unsigned long long key = list[i];
+        int rank = 0;
+        for (int j = 0; j < c; ++j) rank += list[j] > key;
+        if (rank < a.k) {
+            a.top_ids[(size_t)r * a.k + rank] = index_of(key);
+            a.top_logp[(size_t)r * a.k + rank] = log_p(all, log_s, score_of(key));
         }
     }
 }
@@ -131,26 +372,78 @@ struct LpGradArgs {
     const int *ids;
     const float *lse, *entropy, *dlogp, *dentropy;
     void *dz;
-    int rows, classes;
+    int rows, classes, splits, seg;
     long long stride;
 };
 
+// Block = (row, split of its classes); in place a row is one block's, which may have to read it twice.
+// p (log p + entropy) is 0 where p is, also for log p = -inf.
 template <typename T>
 __global__ __launch_bounds__(NT) void k_logprobs_grad(LpGradArgs a)
 {
-    const int r = blockIdx.x;
-    const T *z = (const T *)a.z + (size_t)r * a.stride;
-    T *dz = (T *)a.dz + (size_t)r * a.stride;
-    const float lse = a.lse[r], h = a.entropy != nullptr ? a.entropy[r] : 0.f, de = a.dentropy != nullptr ? a.dentropy[r] : 0.f;
+    constexpr int V = Run<T>::V, U = 4;
+    const int t = threadIdx.x, r = blockIdx.x / a.splits, c0 = (blockIdx.x - r * a.splits) * a.seg;
+    const T *row = (const T *)a.z + (size_t)r * a.stride + c0;
+    T *out = (T *)a.dz + (size_t)r * a.stride + c0;
+    const Run<T> run(row, min(a.seg, a.classes - c0));
+    const float lse = a.lse[r], h = a.entropy != nullptr ? a.entropy[r] : 0.f;
+    const bool none = lse == -INFINITY;
     const int id = a.ids != nullptr ? a.ids[r] : -1;
-    const float dl = a.dlogp != nullptr && id >= 0 && id < a.classes ? a.dlogp[r] : 0.f;
-    for (int c = threadIdx.x; c < a.classes; c += NT) {
-        const float lp = as_f32(z[c]) - lse, p = __expf(lp);
-        // p (log p + h) is 0 where p is, also for log p = -inf
-        float g = -p * dl - de * (lp < -200.f ? 0.f : p * (lp + h));
-        if (c == id) g += dl;
-        dz[c] = from_f32<T>(lse == -INFINITY ? 0.f : g);
+    const bool valid = id >= 0 && id < a.classes && !none;
+    const float dl = a.dlogp != nullptr && valid ? a.dlogp[r] : 0.f, de = a.dentropy != nullptr && !none ? a.dentropy[r] : 0.f;
+    // p = exp(z - shift) / s: lse holds both; beyond 256 it loses log s to rounding, and the row is summed again
+    float shift = none ? 0.f : lse, log_s = 0.f;           // none: every score is -inf, p = 0
+    if (fabsf(lse) > 256.f && !none) {
+        const Soft all = block_join(scan(Run<T>((const T *)a.z + (size_t)r * a.stride, a.classes)));
+        shift = all.m;
+        log_s = logf(all.s);
     }
+    // gradient = p (-dl - de (log p + h)) = exp(d) (k0 - k1 d), d = z - shift
+    const float k1 = de * exp_d(-log_s), k0 = -fmaf(de, h - log_s, dl) * exp_d(-log_s);
+    const int at = valid ? id - c0 : -1;                   // the given class in this run, if in [0, n)
+    auto grad = [&](float z) {
+        const float d = z - shift;
+        return exp_d(d) * fmaf(-k1, fmaxf(d, -3e38f), k0);
+    };
+    auto single = [&](int i) { out[i] = from_f32<T>(grad(as_f32(run.z[i])) + (i == at ? dl : 0.f)); };
+    auto vector = [&](int v, const Pack<T, V> &q) {
+        float g[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) g[e] = grad(as_f32(q.v[e]));
+        const int e0 = at - run.first(v);
+        if (e0 >= 0 && e0 < V)
+#pragma unroll
+            for (int e = 0; e < V; ++e) g[e] += e == e0 ? dl : 0.f;
+        Pack<T, V> o;
+#pragma unroll
+        for (int e = 0; e < V; ++e) o.v[e] = from_f32<T>(g[e]);
+        *reinterpret_cast<Pack<T, V> *>(out + run.first(v)) = o;
+    };
+    if (run.aligned_like(out)) {
+        if (run.before(t)) single(t);
+        if (run.behind(t) >= 0) single(run.behind(t));
+        int v = t;
+        for (; v + (U - 1) * NT < run.vectors; v += U * NT) {
+            Pack<T, V> q[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) q[u] = run.vector(v + u * NT);
+#pragma unroll
+            for (int u = 0; u < U; ++u) vector(v + u * NT, q[u]);
+        }
+        for (; v < run.vectors; v += NT) vector(v, run.vector(v));
+    } else {   // dz at another offset from a 16-byte boundary than z
+        for (int i = t; i < run.n; i += NT) single(i);
+    }
+}
+
+// Splits of a row: about four blocks per compute unit, at least 2048 classes each.  Whole vectors, so that all splits of a row
+// are aligned alike.
+void split_rows(int rows, int classes, int &splits, int &seg)
+{
+    int s = std::min({(1024 + rows - 1) / rows, (classes + 2047) / 2048, kMaxSplits});
+    s = std::max(s, 1);
+    seg = ((classes + s - 1) / s + 7) / 8 * 8;
+    splits = (classes + seg - 1) / seg;
 }
 
 long long stride_of(const dp_logprobs_desc &d) { return d.row_stride != 0 ? (long long)d.row_stride : d.classes; }
@@ -171,6 +464,10 @@ dp_status check_desc(const dp_logprobs_desc *d)
     return DP_OK;
 }
 
+// keys first: they need the wider alignment
+size_t top_bytes(int rows, int splits, int k) { return (size_t)rows * splits * k * sizeof(unsigned long long); }
+size_t part_bytes(int rows, int splits, int k) { return splits == 1 ? 0 : top_bytes(rows, splits, k) + (size_t)rows * splits * sizeof(Soft); }
+
 bool misaligned(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
 
 dp_status check_scores(const dp_logprobs_desc &d, const void *z)
@@ -184,8 +481,10 @@ dp_status check_scores(const dp_logprobs_desc &d, const void *z)
 
 extern "C" size_t dp_logprobs_workspace_bytes(const dp_logprobs_desc *desc)
 {
-    (void)desc;
-    return 0;
+    if (check_desc(desc) != DP_OK || desc->rows == 0) return 0;
+    int splits, seg;
+    split_rows(desc->rows, desc->classes, splits, seg);
+    return part_bytes(desc->rows, splits, desc->top_k);
 }
 
 extern "C" dp_status dp_logprobs_fwd(const dp_logprobs_desc *desc, const void *z, const int32_t *ids, float *logp, float *entropy, float *lse,
@@ -201,10 +500,20 @@ extern "C" dp_status dp_logprobs_fwd(const dp_logprobs_desc *desc, const void *z
     if (logp == nullptr && entropy == nullptr && lse == nullptr && d.top_k == 0) { dp_set_error("log-probabilities: no output requested"); return DP_ERR_NULL; }
     for (const void *p : {(const void *)ids, (const void *)logp, (const void *)entropy, (const void *)lse, (const void *)top_logp, (const void *)top_ids})
         if (misaligned(p, 4)) { dp_set_error("log-probabilities: pointers must be 4-byte aligned"); return DP_ERR_BAD_DESC; }
-    (void)ws; (void)ws_bytes;
-    const LpArgs a = {z, ids, logp, entropy, lse, top_logp, top_ids, d.rows, d.classes, d.top_k, stride_of(d)};
-    if (d.io_dtype == DP_BF16) hipLaunchKernelGGL(k_logprobs<bf16_t>, dim3(d.rows), dim3(NT), 0, (hipStream_t)hip_stream, a);
-    else hipLaunchKernelGGL(k_logprobs<float>, dim3(d.rows), dim3(NT), 0, (hipStream_t)hip_stream, a);
+    LpArgs a = {z, ids, logp, entropy, lse, top_logp, top_ids, nullptr, nullptr, d.rows, d.classes, d.top_k, 1, d.classes, stride_of(d)};
+    split_rows(d.rows, d.classes, a.splits, a.seg);
+    const size_t need = part_bytes(d.rows, a.splits, d.top_k);
+    if (need > 0 && (ws == nullptr || ws_bytes < need)) {
+        dp_set_error("log-probabilities need %zu workspace bytes, got %zu", need, ws == nullptr ? (size_t)0 : ws_bytes);
+        return DP_ERR_WORKSPACE;
+    }
+    if (!aligned16(ws)) { dp_set_error("log-probabilities: the workspace must be 16-byte aligned"); return DP_ERR_BAD_DESC; }
+    a.part_top = (unsigned long long *)ws;
+    a.part = (Soft *)((char *)ws + top_bytes(d.rows, a.splits, d.top_k));
+    const bool bf = d.io_dtype == DP_BF16;
+    hipStream_t st = (hipStream_t)hip_stream;
+    hipLaunchKernelGGL(bf ? k_logprobs<bf16_t> : k_logprobs<float>, dim3((unsigned)d.rows * a.splits), dim3(NT), 0, st, a);
+    if (a.splits > 1) hipLaunchKernelGGL(bf ? k_logprobs_join<bf16_t> : k_logprobs_join<float>, dim3(d.rows), dim3(NT), 0, st, a);
     return launched("log-probabilities");
 }
 
@@ -224,8 +533,8 @@ extern "C" dp_status dp_logprobs_bwd(const dp_logprobs_desc *desc, const void *z
     }
     for (const void *p : {(const void *)ids, (const void *)lse, (const void *)entropy, (const void *)dlogp, (const void *)dentropy})
         if (misaligned(p, 4)) { dp_set_error("log-probabilities' gradient: pointers must be 4-byte aligned"); return DP_ERR_BAD_DESC; }
-    const LpGradArgs a = {z, ids, lse, entropy, dlogp, dentropy, dz, d.rows, d.classes, stride_of(d)};
-    if (d.io_dtype == DP_BF16) hipLaunchKernelGGL(k_logprobs_grad<bf16_t>, dim3(d.rows), dim3(NT), 0, (hipStream_t)hip_stream, a);
-    else hipLaunchKernelGGL(k_logprobs_grad<float>, dim3(d.rows), dim3(NT), 0, (hipStream_t)hip_stream, a);
+    LpGradArgs a = {z, ids, lse, entropy, dlogp, dentropy, dz, d.rows, d.classes, 1, d.classes, stride_of(d)};
+    if (dz != z) split_rows(d.rows, d.classes, a.splits, a.seg);
+    hipLaunchKernelGGL(d.io_dtype == DP_BF16 ? k_logprobs_grad<bf16_t> : k_logprobs_grad<float>, dim3((unsigned)d.rows * a.splits), dim3(NT), 0, (hipStream_t)hip_stream, a);
     return launched("log-probabilities' gradient");
 }

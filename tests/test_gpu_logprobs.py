@@ -270,3 +270,38 @@ def test_many_rows_and_long_offsets(env):
     got = room.view(rows, stride)[:, :classes].float().cpu().numpy()
     ref = env[2].logprobs_bwd(z, np.arange(rows), np.ones(rows), np.ones(rows))
     assert np.all(np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + 3e-4)
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("classes", [100, 30000])
+def test_gradient_of_large_scores(env, classes, bf16):
+    """lse cannot hold log(sum) beside a maximum of 10^5, or beside the type's lowest value in a row of nothing else: p comes from the row."""
+    dp = env[0]
+    z = np.zeros((4, classes), np.float32)
+    z[0] = 1e5
+    z[1] = -3.3895314e38
+    z[2] = np.float32(512.0) * (np.arange(classes) % 3 == 0)
+    z[3] = -4096.0
+    z = env[3].round_bf16(z) if bf16 else z
+    k = Run(env, z, [3, 5, 6, classes - 1], 0, bf16)
+    out = k.forward()
+    dlogp, dent = np.array([1.0, -2.0, 0.5, 1.0], np.float32), np.array([0.5, 1.0, -1.0, 0.0], np.float32)
+    want = k.O.logprobs_bwd(z, k.ids, dlogp.astype(np.float64), dent.astype(np.float64))
+    for place in (None, k.room):
+        dz = k.backward(dlogp, dent, out[2], out[1], place=place)[1][:, :classes].float().cpu().numpy()
+        # equal scores: the entropy's bracket is 0 up to the rounding of log(classes)
+        tol = 2e-6 * np.log(classes) / (classes / 3) * 4 + 3e-6 * np.abs(want) + (2.0 ** -8 * np.abs(want) if bf16 else 0)
+        assert np.all(np.abs(dz - want) <= tol)
+
+
+def test_gradient_at_another_alignment(env):
+    """dz need not be aligned as z is."""
+    dp = env[0]
+    z = scores(env[3], "align", 5, 3001, True)
+    k = Run(env, z, [0, 1, 2, 3, 3000], 0, True)
+    out = k.forward()
+    one = torch.ones(5, device="cuda")
+    room = torch.full((5 * 3001 + 16,), 9.0, dtype=torch.bfloat16, device="cuda")
+    dp.dp_logprobs_bwd(k.desc, k.zd, k.idd, out[2], out[1], one, one, room[3:])
+    k.check_backward(room[3:3 + 5 * 3001].view(5, 3001), np.ones(5, np.float32), np.ones(5, np.float32))
+    assert bool((room[:3] == 9).all()) and bool((room[3 + 5 * 3001:] == 9).all())
