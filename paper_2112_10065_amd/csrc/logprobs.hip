@@ -77,16 +77,11 @@ __device__ __forceinline__ void join(Soft &a, const Soft &b)
     a.t = ta + tb;
     a.m = m;
 }
-__device__ __forceinline__ void wave_join(Soft &a)
+// The wavefront's: its maximum, then each lane's sums brought to it.
+__device__ __forceinline__ Soft wave_join(const Soft &a)
 {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-        const Soft b = {__shfl_xor(a.m, o, 64), __shfl_xor(a.s, o, 64), __shfl_xor(a.t, o, 64)};
-        // the same order on both sides: the lanes agree in every bit
-        Soft lo = (threadIdx.x & o) ? b : a;
-        join(lo, (threadIdx.x & o) ? a : b);
-        a = lo;
-    }
+    const float m = wave_max_fast(a.m), d = a.m - m, f = exp_d(d);
+    return {m, wave_sum_fast(a.s * f), wave_sum_fast(f > 0.f ? fmaf(a.s, d, a.t) * f : 0.f)};   // a NaN sum stays one
 }
 __device__ __forceinline__ unsigned long long wave_top(unsigned long long v)
 {
@@ -164,7 +159,7 @@ template <typename T> __device__ __forceinline__ Soft scan(const Run<T> &run)
 __device__ __forceinline__ Soft block_join(Soft mine)
 {
     __shared__ Soft part[NT / 64];
-    wave_join(mine);
+    mine = wave_join(mine);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = mine;
     __syncthreads();
     Soft all = part[0];
@@ -175,53 +170,72 @@ __device__ __forceinline__ Soft block_join(Soft mine)
 // The k largest keys of the block's run, best first, to put(rank, key); all threads call it.  `top`: order of the thread's largest
 // score, 0 if it has none; `odd`: its scores hold a NaN or +inf.
 //
-// The k-th largest of the threads' maxima bounds the k-th largest score from below, so only scores from it on are candidates, and only
-// the threads whose maximum reaches it read their scores again.  They append to a list in LDS; each candidate's place is the number of
-// larger ones.  Where very many scores reach the bound (equal ones, or ruled-out classes where fewer than k are left) the list holds those above
+// At least k threads' maxima reach `least`, so the k largest scores do; only the scores of those threads are looked at again, by all
+// threads together, and appended to a list in LDS; each candidate's place is the number of larger ones.  `least` is the k-th largest maximum to
+// 16 bits (which is all of a bf16 score's), found bit by bit: a count over 256 values is four comparisons of a wavefront.
+// Where very many scores reach it (equal ones, or ruled-out classes where fewer than k are left) the list holds those above
 // it and the first k equal to it by index, and where even that does not fit, k rounds take the largest below the one before.
 template <typename T, typename P>
 __device__ __forceinline__ void block_top(const Run<T> &run, int base, int k, unsigned top, bool odd, P &&put)
 {
+    constexpr int V = Run<T>::V;
     __shared__ unsigned tops[NT];
     __shared__ unsigned long long list[kCandidates];
-    __shared__ unsigned bound;
-    __shared__ int count, ties, some_odd;
+    __shared__ unsigned short leaders[NT];
+    __shared__ int count, ties, lead, some_odd;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     tops[t] = top;
-    if (t == 0) { count = 0; bound = 0; some_odd = 0; }
+    if (t == 0) { count = 0; lead = 0; some_odd = 0; }
     __syncthreads();
     if (odd) some_odd = 1;
-    int above = 0;   // maxima that come before this one
-    for (int i = 0; i < NT; i += 4) {
-        const uint4 q = *reinterpret_cast<const uint4 *>(&tops[i]);
-        above += (q.x > top || (q.x == top && i < t)) + (q.y > top || (q.y == top && i + 1 < t)) + (q.z > top || (q.z == top && i + 2 < t)) +
-                 (q.w > top || (q.w == top && i + 3 < t));
+    const uint4 four = *reinterpret_cast<const uint4 *>(&tops[4 * lane]);
+    unsigned least = 0;
+    for (unsigned bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
+        const unsigned trial = least | bit;
+        const int reach = __popcll(__ballot(four.x >= trial)) + __popcll(__ballot(four.y >= trial)) + __popcll(__ballot(four.z >= trial)) +
+                          __popcll(__ballot(four.w >= trial));
+        if (reach >= k) least = trial;
     }
-    if (above == k - 1) bound = top;
-    __syncthreads();
-    const unsigned least = bound;
+    auto append = [&](float z, int i, unsigned from) {
+        if (order_of(z) >= from) {
+            const int at = atomicAdd(&count, 1);
+            if (at < kCandidates) list[at] = key_of(z, base + i);
+        }
+    };
+    // scores from `from` on: the single ones by their threads, the vectors of the leading threads by everybody
+    auto collect = [&](unsigned from) {
+        if (top >= from && top != 0) {
+            leaders[atomicAdd(&lead, 1)] = (unsigned short)t;
+            if (run.before(t)) append(as_f32(run.z[t]), t, from);
+            if (run.behind(t) >= 0) append(as_f32(run.z[run.behind(t)]), run.behind(t), from);
+        }
+        __syncthreads();
+        const int each = (run.vectors + NT - 1) / NT, total = lead * each;
+        for (int i = t; i < total; i += NT) {
+            const int l = i / each, v = (i - l * each) * NT + leaders[l];
+            if (*(volatile int *)&count > kCandidates) break;   // it does not fit
+            if (v >= run.vectors) continue;
+            const Pack<T, V> q = run.vector(v);
+#pragma unroll
+            for (int e = 0; e < V; ++e) append(as_f32(q.v[e]), run.first(v) + e, from);
+        }
+        __syncthreads();
+    };
+    collect(least);
     const bool slow = some_odd != 0;
-    if (!slow && top >= least && top != 0)
-        run.each(t, [&](float z, int i) {
-            if (order_of(z) >= least) {
-                const int at = atomicAdd(&count, 1);
-                if (at < kCandidates) list[at] = key_of(z, base + i);
-            }
-        });
-    __syncthreads();
     bool fits = !slow && count <= kCandidates;
     if (!slow && !fits) {
+        // `least` to all its bits: the largest value that k maxima reach
+        for (unsigned bit = 0x8000u; bit != 0; bit >>= 1) {
+            const unsigned trial = least | bit;
+            const int reach = __popcll(__ballot(four.x >= trial)) + __popcll(__ballot(four.y >= trial)) + __popcll(__ballot(four.z >= trial)) +
+                              __popcll(__ballot(four.w >= trial));
+            if (reach >= k) least = trial;
+        }
         __syncthreads();
-        if (t == 0) { count = 0; ties = 0; }
+        if (t == 0) { count = 0; lead = 0; ties = 0; }
         __syncthreads();
-        if (top > least)
-            run.each(t, [&](float z, int i) {
-                if (order_of(z) > least) {
-                    const int at = atomicAdd(&count, 1);
-                    if (at < kCandidates) list[at] = key_of(z, base + i);
-                }
-            });
-        __syncthreads();
+        if (least != 0xffffffffu) collect(least + 1);
         fits = count <= kCandidates - k;
         if (fits && wave == 0) {   // one wavefront finds the first k in order
             int found = 0;
@@ -333,8 +347,9 @@ __global__ __launch_bounds__(NT) void k_logprobs_join(LpArgs a)
     }
     if (t == 0) { count = 0; bound = 0; }
     __syncthreads();
-    Soft all = part[0];
-    for (int s = 1; s < a.splits; ++s) join(all, part[s]);
+    static_assert(kMaxSplits == 64, "one per lane");
+    const int s = t & 63;
+    const Soft all = wave_join(s < a.splits ? part[s] : Soft{-3.402823466e38f, 0.f, 0.f});   // every wavefront the same
     if (t == 0) {
         const int id = a.logp != nullptr ? a.ids[r] : -1;
         const bool valid = id >= 0 && id < a.classes;
