@@ -93,6 +93,16 @@ __device__ __forceinline__ unsigned long long wave_top(unsigned long long v)
     return v;
 }
 
+// How many of list[0 .. c) are larger than key.  Eight reads at a time: up to seven zeros stand behind the last entry.
+__device__ __forceinline__ int larger(const unsigned long long *list, int c, unsigned long long key)
+{
+    int rank = 0;
+    for (int j = 0; j < c; j += 8)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) rank += list[j + e] > key;
+    return rank;
+}
+
 // A run of scores as the block reads it: up to V - 1 single ones in front of the first 16-byte boundary, whole vectors, single ones behind.
 // Thread t takes single t of each end (t < V) and vectors t, t + NT, ...
 template <typename T> struct Run {
@@ -180,7 +190,7 @@ __device__ __forceinline__ void block_top(const Run<T> &run, int base, int k, un
 {
     constexpr int V = Run<T>::V;
     __shared__ unsigned tops[NT];
-    __shared__ unsigned long long list[kCandidates];
+    __shared__ unsigned long long list[kCandidates + 8];
     __shared__ unsigned short leaders[NT];
     __shared__ int count, ties, lead, some_odd;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -211,13 +221,22 @@ __device__ __forceinline__ void block_top(const Run<T> &run, int base, int k, un
         }
         __syncthreads();
         const int each = (run.vectors + NT - 1) / NT, total = lead * each;
-        for (int i = t; i < total; i += NT) {
-            const int l = i / each, v = (i - l * each) * NT + leaders[l];
+        constexpr int U = 4;   // a read comes from beyond the L2 where many rows are on their way: four at a time
+        for (int i0 = t; i0 < total; i0 += U * NT) {
             if (*(volatile int *)&count > kCandidates) break;   // it does not fit
-            if (v >= run.vectors) continue;
-            const Pack<T, V> q = run.vector(v);
+            Pack<T, V> q[U];
+            int v[U];
 #pragma unroll
-            for (int e = 0; e < V; ++e) append(as_f32(q.v[e]), run.first(v) + e, from);
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * NT, l = i / each;
+                v[u] = i < total ? (i - l * each) * NT + leaders[l] : run.vectors;
+                if (v[u] < run.vectors) q[u] = run.vector(v[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (v[u] < run.vectors)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) append(as_f32(q[u].v[e]), run.first(v[u]) + e, from);
         }
         __syncthreads();
     };
@@ -257,10 +276,11 @@ __device__ __forceinline__ void block_top(const Run<T> &run, int base, int k, un
     }
     if (fits) {
         const int c = count;
+        if (t < 8) list[c + t] = 0;
+        __syncthreads();
         for (int i = t; i < c; i += NT) {
             const unsigned long long key = list[i];
-            int rank = 0;
-            for (int j = 0; j < c; ++j) rank += list[j] > key;
+            const int rank = larger(list, c, key);
             if (rank < k) put(rank, key);
         }
         for (int r = c + t; r < k; r += NT) put(r, 0ull);   // fewer scores than k
@@ -331,56 +351,165 @@ __global__ __launch_bounds__(NT) void k_logprobs(LpArgs a)
 }
 
 // Joins the splits of a row.  Block = row.  Each split's keys are in order: with S splits the `need`-th largest of their `each`-th
-// keys, need * each >= k, bounds the k-th largest from below.
+// keys, need * each >= k, bounds the k-th largest from below; with about half of the splits (the least of all of them would bound little).
 template <typename T>
 __global__ __launch_bounds__(NT) void k_logprobs_join(LpArgs a)
 {
-    __shared__ Soft part[kMaxSplits];
-    __shared__ unsigned long long heads[kMaxSplits], list[kMaxSplits * DP_LOGPROBS_MAX_TOP], bound;
+    __shared__ unsigned long long heads[kMaxSplits], list[kMaxSplits * DP_LOGPROBS_MAX_TOP + 8], bound;
     __shared__ int count;
+    constexpr int kAhead = 8;   // keys that a thread asks for before it knows which ones matter
     const int t = threadIdx.x, r = blockIdx.x;
-    const int each = (a.k + a.splits - 1) / a.splits, need = each > 0 ? (a.k + each - 1) / each : 0;
-    const unsigned long long *keys = a.part_top + (size_t)r * a.splits * a.k;
-    if (t < a.splits) {
-        part[t] = a.part[(size_t)r * a.splits + t];
-        if (a.k > 0) heads[t] = keys[(size_t)t * a.k + each - 1];
+    const int each = (2 * a.k + a.splits - 1) / a.splits, need = each > 0 ? (a.k + each - 1) / each : 0;
+    const int total = a.splits * a.k;
+    const unsigned long long *keys = a.part_top + (size_t)r * total;
+    Soft mine = {-3.402823466e38f, 0.f, 0.f};
+    const int s = t & 63;
+    static_assert(kMaxSplits == 64, "one per lane");
+    if (s < a.splits) mine = a.part[(size_t)r * a.splits + s];
+    if (t < a.splits && a.k > 0) heads[t] = keys[(size_t)t * a.k + each - 1];
+    unsigned long long ahead[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) ahead[u] = t + u * NT < total ? keys[t + u * NT] : 0ull;
+    bool valid = false;
+    float score = 0.f;
+    if (t == NT - 1 && a.logp != nullptr) {
+        const int id = a.ids[r];
+        valid = id >= 0 && id < a.classes;
+        if (valid) score = as_f32(((const T *)a.z)[(size_t)r * a.stride + id]);
     }
     if (t == 0) { count = 0; bound = 0; }
     __syncthreads();
-    static_assert(kMaxSplits == 64, "one per lane");
-    const int s = t & 63;
-    const Soft all = wave_join(s < a.splits ? part[s] : Soft{-3.402823466e38f, 0.f, 0.f});   // every wavefront the same
-    if (t == 0) {
-        const int id = a.logp != nullptr ? a.ids[r] : -1;
-        const bool valid = id >= 0 && id < a.classes;
-        write_row(a, r, all, valid ? as_f32(((const T *)a.z)[(size_t)r * a.stride + id]) : 0.f, valid);
-    }
+    const Soft all = wave_join(mine);   // every wavefront the same
+    if (t == NT - 1) write_row(a, r, all, score, valid);
     if (a.k == 0) return;
     if (t < a.splits) {
-        const unsigned long long mine = heads[t];
+        const unsigned long long head = heads[t];
         int above = 0;
-        for (int s = 0; s < a.splits; ++s) above += heads[s] > mine || (heads[s] == mine && s < t);   // equal only where 0, no key
-        if (above == need - 1) bound = mine;
+        for (int i = 0; i < a.splits; ++i) above += heads[i] > head || (heads[i] == head && i < t);   // equal only where 0, no key
+        if (above == need - 1) bound = head;
     }
     __syncthreads();
     const unsigned long long least = bound;
-    for (int i = t; i < a.splits * a.k; i += NT) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+        if (ahead[u] != 0 && ahead[u] >= least) list[atomicAdd(&count, 1)] = ahead[u];
+    for (int i = t + kAhead * NT; i < total; i += NT) {
         const unsigned long long key = keys[i];
         if (key != 0 && key >= least) list[atomicAdd(&count, 1)] = key;
     }
     __syncthreads();
     const int c = count;
+    if (t < 8) list[c + t] = 0;
+    __syncthreads();
     const float log_s = logf(all.s);
     for (int i = t; i < c; i += NT) {
         const unsigned long long key = list[i];
-        int rank = 0;
-        for (int j = 0; j < c; ++j) rank += list[j] > key;
+        const int rank = larger(list, c, key);
         if (rank < a.k) {
             a.top_ids[(size_t)r * a.k + rank] = index_of(key);
             a.top_logp[(size_t)r * a.k + rank] = log_p(all, log_s, score_of(key));
         }
     }
 }
+
+// Short rows: a wavefront each, the row in registers (class lane + 64 j in slot j), the same steps without a barrier.  A block per
+// row of 1000 classes spends its time on barriers and idle threads (bf16, 4096 rows, five alternatives: 15.6 us; see the launch for this kernel's).
+constexpr int kRowCandidates = 256;   // of a row, in LDS; a multiple of 64
+template <typename T, int R>
+__global__ __launch_bounds__(NT) void k_logprobs_rows(LpArgs a)
+{
+    __shared__ unsigned long long lists[NT / 64][kRowCandidates + 8];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int r = blockIdx.x * (NT / 64) + wave;
+    if (r >= a.rows) return;   // whole wavefronts; there are no barriers
+    const T *z = (const T *)a.z + (size_t)r * a.stride;
+    float v[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) v[j] = as_f32(z[min(lane + 64 * j, a.classes - 1)]);
+    const int id = a.logp != nullptr ? a.ids[r] : -1;
+    const bool valid = id >= 0 && id < a.classes;
+    const float score = as_f32(z[valid ? id : 0]);
+#pragma unroll
+    for (int j = 0; j < R; ++j) v[j] = lane + 64 * j < a.classes ? v[j] : -INFINITY;
+    Soft mine = {-3.402823466e38f, 0.f, 0.f};
+    add_scores<R>(mine, v);
+    const Soft all = wave_join(mine);
+    if (lane == 0) write_row(a, r, all, score, valid);
+    if (a.k == 0) return;
+    const float log_s = logf(all.s);
+    auto put = [&](int rank, unsigned long long key) {
+        a.top_ids[(size_t)r * a.k + rank] = index_of(key);
+        a.top_logp[(size_t)r * a.k + rank] = log_p(all, log_s, score_of(key));
+    };
+    unsigned long long *list = lists[wave];
+    const int per_lane = (a.classes - lane + 63) / 64;   // classes of this lane, may be 0
+    if (all.s == all.s) {   // no NaN or +inf: the lanes' maxima are what they seem
+        unsigned order[R];
+#pragma unroll
+        for (int j = 0; j < R; ++j) order[j] = j < per_lane ? order_of(v[j]) : 0u;
+        unsigned least = 0;
+        auto reach = [&](unsigned from) {
+            int n = 0;
+#pragma unroll
+            for (int j = 0; j < R; ++j) n += __popcll(__ballot(order[j] >= from));
+            return n;
+        };
+        // by the lanes' maxima as long as a quarter of the lanes may stay below, else by all scores
+        if (a.k <= 48) {
+            const unsigned top = per_lane <= 0 ? 0u : mine.s == 0.f ? order_of(-INFINITY) : order_of(mine.m);
+            for (unsigned bit = 0x80000000u; bit >= 0x10000u; bit >>= 1)
+                if (__popcll(__ballot(top >= (least | bit))) >= a.k) least |= bit;
+        } else {
+            for (unsigned bit = 0x80000000u; bit >= 0x10000u; bit >>= 1)
+                if (reach(least | bit) >= a.k) least |= bit;
+        }
+        const unsigned long long below = (1ull << lane) - 1;
+        int c = 0;
+        auto append = [&](bool hit, int j) {
+            const unsigned long long hits = __ballot(hit);
+            const int at = c + __popcll(hits & below);
+            if (hit && at < kRowCandidates) list[at] = key_of(v[j], lane + 64 * j);
+            c += __popcll(hits);
+        };
+        least = max(least, 1u);
+#pragma unroll
+        for (int j = 0; j < R; ++j) append(order[j] >= least, j);
+        if (c > kRowCandidates) {   // the k-th largest score itself, those above it, and the first equal to it by index
+            least = 0;
+            for (unsigned bit = 0x80000000u; bit != 0; bit >>= 1)
+                if (reach(least | bit) >= a.k) least |= bit;
+            const int above = least == 0xffffffffu ? 0 : reach(least + 1);
+            int equal = above;
+            c = 0;
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                const unsigned long long ties = __ballot(order[j] == least);
+                append(order[j] > least || (order[j] == least && equal + __popcll(ties & below) < a.k), j);
+                equal += __popcll(ties);
+            }
+        }
+        if (lane < 8) list[c + lane] = 0;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // the list as all lanes wrote it
+        for (int i = lane; i < c; i += 64) {
+            const unsigned long long key = list[i];
+            const int rank = larger(list, c, key);
+            if (rank < a.k) put(rank, key);
+        }
+        return;
+    }
+    unsigned long long last = ~0ull;   // the largest below the one before
+    for (int k = 0; k < a.k; ++k) {
+        unsigned long long best = 0;
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const unsigned long long key = key_of(v[j], lane + 64 * j);
+            if (j < per_lane && key < last && key > best) best = key;
+        }
+        last = wave_top(best);
+        if (lane == 0) put(k, last);
+    }
+}
+constexpr int kShortRow = 1024;
 
 struct LpGradArgs {
     const void *z;
@@ -527,6 +656,13 @@ extern "C" dp_status dp_logprobs_fwd(const dp_logprobs_desc *desc, const void *z
     a.part = (Soft *)((char *)ws + top_bytes(d.rows, a.splits, d.top_k));
     const bool bf = d.io_dtype == DP_BF16;
     hipStream_t st = (hipStream_t)hip_stream;
+    if (d.classes <= kShortRow) {
+        const dim3 grid((d.rows + NT / 64 - 1) / (NT / 64));
+        auto *kernel = d.classes <= 128 ? (bf ? k_logprobs_rows<bf16_t, 2> : k_logprobs_rows<float, 2>) : d.classes <= 512 ? (bf ? k_logprobs_rows<bf16_t, 8> : k_logprobs_rows<float, 8>) :
+                       (bf ? k_logprobs_rows<bf16_t, 16> : k_logprobs_rows<float, 16>);
+        hipLaunchKernelGGL(kernel, grid, dim3(NT), 0, st, a);
+        return launched("log-probabilities");
+    }
     hipLaunchKernelGGL(bf ? k_logprobs<bf16_t> : k_logprobs<float>, dim3((unsigned)d.rows * a.splits), dim3(NT), 0, st, a);
     if (a.splits > 1) hipLaunchKernelGGL(bf ? k_logprobs_join<bf16_t> : k_logprobs_join<float>, dim3(d.rows), dim3(NT), 0, st, a);
     return launched("log-probabilities");
