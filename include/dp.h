@@ -271,7 +271,7 @@ dp_status dp_sgd_update(int64_t count, float lr, float momentum, const float *gr
  *   xhat = (x - mean) * rstd;  u = xhat * gamma[c] + beta[c];  y = u, max(u, 0) (DP_RELU) or u * sigmoid(u) (DP_SILU).
  * x, y, dy, dx [n,h,w,c] in io_dtype (DP_BF16 or DP_F32); gamma, beta [c] fp32, NULL = ones / zeros; mean, rstd [n,groups] fp32.
  * Statistics, sums and the normalisation are fp32; deterministic; asynchronous on hip_stream.
- * n*h*w*c < 2^31, h*w <= 2^30, n * ceil(c / 256) <= 2^23. */
+ * n*h*w*c < 2^31, h*w <= 2^30, n * ceil(c / 256) <= 2^22. */
 typedef struct {
     int32_t n, h, w, c, groups; /* groups divides c */
     int32_t io_dtype;           /* dp_dtype */

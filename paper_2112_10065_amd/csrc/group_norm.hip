@@ -1,12 +1,13 @@
 // Group normalisation with an activation, NHWC, forward and backward.  Bound by HBM: the operations per element are few.
 //
 // Both directions are a reduction over (pixels x channels of a group) per sample, then a pointwise pass that needs its result.
-// In NHWC a group is a narrow column of channels, so a block takes whole rows: each thread keeps one vector of channels (16 bytes)
-// and walks pixels.  Partial results per channel meet in `part` [sample][split][channel], two floats each:
-//   forward    mean and sum of squared deviations of the split's pixels: never a difference of large sums, whatever offset x has
-//   backward   A = sum g and B = sum g * xhat of the split's pixels
-// The second kernel combines the partials of the groups that its channels belong to, in a fixed order, and applies them; in the
-// backward pass its first blocks sum dgamma and dbeta over samples and splits instead.
+// In NHWC a group is a narrow column of channels, so a block takes whole rows of a slab of channels: each thread keeps one vector of
+// channels (16 bytes) and walks pixels.  A slab is some whole groups, or, for groups wider than a block, a part of one; a group's part in
+// a slab is a cell.  Partial results go to scratch memory, two floats per [sample][split of the pixels][cell]:
+//   forward    mean and sum of squared deviations of the cell: never a difference of large sums, whatever offset x has
+//   backward   sum t and sum t * xhat, t = g * gamma; and per [sample][split][channel] sum g and sum g * xhat, for dgamma and dbeta
+// The second kernel adds up the partials of its groups in a fixed order and applies them; in the backward pass its first
+// blocks sum dgamma and dbeta instead.
 #include "vec_common.h"
 #include <algorithm>
 #include <cmath>
@@ -22,69 +23,131 @@ struct GnArgs {
     void *out;                       // y or dx
     float *mean_out, *rstd_out;      // forward, may be null
     float *dgamma, *dbeta;           // backward, may be null
-    float2 *part;
+    float2 *part, *chan;             // partials of cells, of channels (backward)
     int n, hw, c, groups, cg;
-    int cs, slabs;                   // channels of a slab (the last one may be narrower), slabs
+    int cs, slabs;                   // channels of a slab (the last one of all, or of a group, may be narrower), slabs
+    int per_group, cells;            // slabs of a group (1: a slab is whole groups), cells in all
     int splits, split_pixels;        // pixels of a split (the last one may be shorter)
     int chunks, chunk_pixels;        // the same for the second kernel's blocks
     int grad_blocks;                 // blocks of the second kernel that sum dgamma / dbeta
     float eps, inv_count;            // 1 / (hw * cg)
 };
 
-template <typename T, int V> __device__ __forceinline__ void load(const T *p, float (&v)[V])
+struct Slab { int ch0, width, g0, gs, cell0; };   // first channel, channels, first group, groups, first cell
+__device__ __forceinline__ Slab slab_of(const GnArgs &a, int slab)
 {
-    const Pack<T, V> q = *reinterpret_cast<const Pack<T, V> *>(p);
-#pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = as_f32(q.v[e]);
+    Slab s;
+    if (a.per_group == 1) {
+        s.ch0 = slab * a.cs;
+        s.width = min(a.cs, a.c - s.ch0);
+        s.g0 = s.ch0 / a.cg;
+        s.gs = s.width / a.cg;
+        s.cell0 = s.g0;
+    } else {
+        s.g0 = slab / a.per_group;
+        const int off = (slab - s.g0 * a.per_group) * a.cs;
+        s.ch0 = s.g0 * a.cg + off;
+        s.width = min(a.cs, a.cg - off);
+        s.gs = 1;
+        s.cell0 = slab;
+    }
+    return s;
 }
 
-__device__ __forceinline__ float sigmoid(float u) { return __builtin_amdgcn_rcpf(1.f + __expf(-u)); }
+// 1 / (1 + exp(-u))
+__device__ __forceinline__ float sigmoid(float u) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u * -1.44269504f)); }
 
-// What a thread's vector of channels needs for the pixel loop.
-template <int V> struct ChannelConst { float mean[V], rstd[V], gamma[V], beta[V]; };
-
-template <int V> __device__ __forceinline__ void affine(const GnArgs &a, int ch, ChannelConst<V> &k)
+template <int V> __device__ __forceinline__ void load_floats(const float *p, float none, float (&v)[V])
 {
+    if (p == nullptr) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-        k.gamma[e] = a.gamma != nullptr ? a.gamma[ch + e] : 1.f;
-        k.beta[e] = a.beta != nullptr ? a.beta[ch + e] : 0.f;
+        for (int e = 0; e < V; ++e) v[e] = none;
+    } else if (V % 4 == 0) {
+#pragma unroll
+        for (int e = 0; e < V; e += 4) *reinterpret_cast<float4 *>(&v[e]) = *reinterpret_cast<const float4 *>(p + e);
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = p[e];
     }
 }
 
-// g = dy * derivative of the activation, and xhat, of one vector
-template <int V, int ACT> __device__ __forceinline__ void gradient(const ChannelConst<V> &k, const float (&x)[V], const float (&dy)[V], const float (&ys)[V],
-                                                                   float (&g)[V], float (&xh)[V])
+// f(e, group of channel ch + e): one division for the vector
+template <int V, typename F> __device__ __forceinline__ void for_groups(int ch, int cg, F &&f)
 {
+    int g = ch / cg, r = ch - g * cg;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        xh[e] = (x[e] - k.mean[e]) * k.rstd[e];
-        g[e] = dy[e];
-        if (ACT == ACT_MASK) g[e] = ys[e] > 0.f ? dy[e] : 0.f;
-        if (ACT == ACT_SILU) {
-            const float u = fmaf(xh[e], k.gamma[e], k.beta[e]), q = sigmoid(u);
-            g[e] = dy[e] * (q * fmaf(u, 1.f - q, 1.f));
-        }
+        f(e, g);
+        if (++r == cg) { r = 0; ++g; }
     }
+}
+
+// g = dy * derivative of the activation at u = xm * scale + beta
+template <int ACT> __device__ __forceinline__ float gradient(float dy, float ys, float xm, float scale, float beta)
+{
+    if (ACT == ACT_MASK) return ys > 0.f ? dy : 0.f;
+    if (ACT == ACT_SILU) {
+        const float u = fmaf(xm, scale, beta), q = sigmoid(u);
+        return dy * (q * fmaf(u, 1.f - q, 1.f));
+    }
+    return dy;
+}
+template <int ACT> __device__ __forceinline__ float activation(float u)
+{
+    if (ACT == ACT_RELU) return u > 0.f ? u : u == u ? 0.f : u;   // a NaN stays one
+    if (ACT == ACT_SILU) return u * sigmoid(u);
+    return u;
 }
 
 // Adds `v` of the threads that have the same channel vector (thread t: vector t % cvs, row t / cvs) and leaves the sums of the
-// slab's channels in sum[0 .. cvs * V).  Fixed order.  sm: NT * V floats.
-template <int V> __device__ __forceinline__ void add_rows(const float (&v)[V], int cvs, int rows, float *sm, float *sum)
+// slab's channels in sum[0 .. cvs * V).  Fixed order.  sm: N * V floats, N threads.
+template <int N, int V> __device__ __forceinline__ void add_rows(const float (&v)[V], int cvs, int rows, float *sm, float *sum)
 {
-    const int t = threadIdx.x;
+    const int t = threadIdx.x, width = cvs * V;
     __syncthreads();
     if (t < rows * cvs)
 #pragma unroll
         for (int e = 0; e < V; ++e) sm[t * V + e] = v[e];
     __syncthreads();
-    const int width = cvs * V;
-    for (int j = t; j < width; j += NT) {
+    int parts = 1;
+    while (2 * parts * width <= N && 2 * parts <= rows) parts *= 2;
+    if (parts == 1) {
+        for (int j = t; j < width; j += N) {
+            float s = 0.f;
+            for (int r = 0; r < rows; ++r) s += sm[r * width + j];
+            sum[j] = s;
+        }
+    } else {   // `parts` threads to a channel, the first of them adds their sums
+        const int part = t / width, j = t - part * width;
         float s = 0.f;
-        for (int r = 0; r < rows; ++r) s += sm[r * width + j];
-        sum[j] = s;
+        if (part < parts)
+            for (int r = part; r < rows; r += parts) s += sm[r * width + j];
+        __syncthreads();
+        if (part < parts) sm[t] = s;
+        __syncthreads();
+        if (t < width) {
+            s = 0.f;
+            for (int q = 0; q < parts; ++q) s += sm[q * width + t];
+            sum[t] = s;
+        }
     }
     __syncthreads();
+}
+
+// put(g, sums) for each of gs groups, from f(g, i, sums) for i in [0, entries): teams of up to 64 lanes share a group.
+template <int N, int K, typename F, typename P> __device__ __forceinline__ void for_teams(int gs, int entries, F &&f, P &&put)
+{
+    int per = 64;
+    while (per > 1 && (per * gs > N || per >= 2 * entries)) per >>= 1;
+    const int sub = threadIdx.x & (per - 1), step = N / per;
+    for (int g = threadIdx.x / per; g < gs; g += step) {   // whole teams
+        float s[K] = {};
+        for (int i = sub; i < entries; i += per) f(g, i, s);
+        for (int o = per >> 1; o >= 1; o >>= 1)
+#pragma unroll
+            for (int k = 0; k < K; ++k) s[k] += __shfl_xor(s[k], o, 64);
+        if (sub == 0) put(g, s);
+    }
 }
 
 // First kernel.  Block = (sample, slab of channels, split of the pixels).
@@ -96,14 +159,16 @@ __global__ __launch_bounds__(NT) void k_gn_reduce(GnArgs a)
     int id = blockIdx.x;
     const int split = id % a.splits;
     id /= a.splits;
-    const int slab = id % a.slabs, n = id / a.slabs;
-    const int ch0 = slab * a.cs, cvs = min(a.cs, a.c - ch0) / V, rows = NT / cvs;
-    const int row = t / cvs, ch = ch0 + (t - row * cvs) * V;
+    const int n = id / a.slabs;
+    const Slab s = slab_of(a, id - n * a.slabs);
+    const int cvs = s.width / V, rows = NT / cvs, row = t / cvs, j0 = (t - row * cvs) * V, ch = s.ch0 + j0;
     const int p0 = split * a.split_pixels, p1 = min(a.hw, p0 + a.split_pixels);
     const bool active = row < rows;
     const size_t base = (size_t)n * a.hw * a.c + ch;
     const T *x = (const T *)a.x + base;
-    float2 *part = a.part + ((size_t)n * a.splits + split) * a.c + ch0;
+    const size_t at = (size_t)n * a.splits + split;
+    float2 *part = a.part + at * a.cells + s.cell0;
+    const int cell_width = s.width / s.gs;
 
     if (!BWD) {
         // running count, mean, sum of squared deviations; eight pixels at a time, whose own mean is subtracted first
@@ -117,10 +182,10 @@ __global__ __launch_bounds__(NT) void k_gn_reduce(GnArgs a)
                 const float total = cnt + 8.f, w = 8.f / total, wn = cnt * w;
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    float s = 0.f, d2 = 0.f;
+                    float sum = 0.f, d2 = 0.f;
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) s += as_f32(q[u].v[e]);
-                    const float mc = s * 0.125f;
+                    for (int u = 0; u < 8; ++u) sum += as_f32(q[u].v[e]);
+                    const float mc = sum * 0.125f;
 #pragma unroll
                     for (int u = 0; u < 8; ++u) { const float d = as_f32(q[u].v[e]) - mc; d2 = fmaf(d, d, d2); }
                     const float delta = mc - mean[e];
@@ -130,38 +195,38 @@ __global__ __launch_bounds__(NT) void k_gn_reduce(GnArgs a)
                 cnt = total;
             }
             for (; p < p1; p += rows) {
-                float v[V];
-                load<T, V>(x + (size_t)p * a.c, v);
+                const Pack<T, V> q = *reinterpret_cast<const Pack<T, V> *>(x + (size_t)p * a.c);
                 const float total = cnt + 1.f, w = 1.f / total, wn = cnt * w;
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float delta = v[e] - mean[e];
+                    const float delta = as_f32(q.v[e]) - mean[e];
                     mean[e] = fmaf(delta, w, mean[e]);
                     m2[e] = fmaf(delta * delta, wn, m2[e]);
                 }
                 cnt = total;
             }
         }
-        // over the rows: the mean first, then the deviations from it
-        const float inv = 1.f / (float)(p1 - p0);
+        // over the rows and the channels of a cell: the mean first, then the deviations from it
+        const float inv = 1.f / ((float)(p1 - p0) * (float)cell_width);
         float v[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) v[e] = mean[e] * cnt;
-        add_rows<V>(v, cvs, rows, sm, sum0);
+        add_rows<NT, V>(v, cvs, rows, sm, sum0);
+        for_teams<NT, 1>(s.gs, cell_width, [&](int g, int i, float (&k)[1]) { k[0] += sum0[g * cell_width + i]; }, [&](int g, float (&k)[1]) { sum1[g] = k[0] * inv; });
+        __syncthreads();
         if (active)
-#pragma unroll
-            for (int e = 0; e < V; ++e) { const float d = mean[e] - sum0[ch - ch0 + e] * inv; v[e] = fmaf(d * d, cnt, m2[e]); }
-        add_rows<V>(v, cvs, rows, sm, sum1);
-        for (int j = t; j < cvs * V; j += NT) part[j] = make_float2(sum0[j] * inv, sum1[j]);
+            for_groups<V>(j0, cell_width, [&](int e, int g) { const float d = mean[e] - sum1[g]; v[e] = fmaf(d * d, cnt, m2[e]); });
+        add_rows<NT, V>(v, cvs, rows, sm, sum0);
+        for_teams<NT, 1>(s.gs, cell_width, [&](int g, int i, float (&k)[1]) { k[0] += sum0[g * cell_width + i]; }, [&](int g, float (&k)[1]) { part[g] = make_float2(sum1[g], k[0]); });
         return;
     }
 
-    ChannelConst<V> k;
-    float A[V] = {}, B[V] = {};
+    float A[V] = {}, B[V] = {}, rstd[V], gamma[V];
     if (active) {
-        affine<V>(a, ch, k);
-#pragma unroll
-        for (int e = 0; e < V; ++e) { const int g = n * a.groups + (ch + e) / a.cg; k.mean[e] = a.mean_in[g]; k.rstd[e] = a.rstd_in[g]; }
+        float mean[V], beta[V], scale[V];
+        load_floats<V>(a.gamma != nullptr ? a.gamma + ch : nullptr, 1.f, gamma);
+        load_floats<V>(a.beta != nullptr ? a.beta + ch : nullptr, 0.f, beta);
+        for_groups<V>(ch, a.cg, [&](int e, int g) { mean[e] = a.mean_in[n * a.groups + g]; rstd[e] = a.rstd_in[n * a.groups + g]; scale[e] = rstd[e] * gamma[e]; });
         const T *dy = (const T *)a.dy + base, *ys = (const T *)a.y_saved + base;
         constexpr int U = 4;
         for (int p = p0 + row; p < p1; p += U * rows) {
@@ -176,18 +241,29 @@ __global__ __launch_bounds__(NT) void k_gn_reduce(GnArgs a)
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (p + u * rows >= p1) continue;
-                float vx[V], vd[V], vy[V] = {}, g[V], xh[V];
 #pragma unroll
-                for (int e = 0; e < V; ++e) { vx[e] = as_f32(qx[u].v[e]); vd[e] = as_f32(qd[u].v[e]); if (ACT == ACT_MASK) vy[e] = as_f32(qy[u].v[e]); }
-                gradient<V, ACT>(k, vx, vd, vy, g, xh);
-#pragma unroll
-                for (int e = 0; e < V; ++e) { A[e] += g[e]; B[e] = fmaf(g[e], xh[e], B[e]); }
+                for (int e = 0; e < V; ++e) {
+                    const float xm = as_f32(qx[u].v[e]) - mean[e];
+                    const float g = gradient<ACT>(as_f32(qd[u].v[e]), ACT == ACT_MASK ? as_f32(qy[u].v[e]) : 0.f, xm, scale[e], beta[e]);
+                    A[e] += g;
+                    B[e] = fmaf(g, xm, B[e]);
+                }
             }
         }
+#pragma unroll
+        for (int e = 0; e < V; ++e) B[e] *= rstd[e];
     }
-    add_rows<V>(A, cvs, rows, sm, sum0);
-    add_rows<V>(B, cvs, rows, sm, sum1);
-    for (int j = t; j < cvs * V; j += NT) part[j] = make_float2(sum0[j], sum1[j]);
+    add_rows<NT, V>(A, cvs, rows, sm, sum0);
+    add_rows<NT, V>(B, cvs, rows, sm, sum1);
+    for (int j = t; j < s.width; j += NT) a.chan[at * a.c + s.ch0 + j] = make_float2(sum0[j], sum1[j]);
+    for_teams<NT, 2>(s.gs, cell_width,
+        [&](int g, int i, float (&k)[2]) {
+            const int j = g * cell_width + i;
+            const float gm = a.gamma != nullptr ? a.gamma[s.ch0 + j] : 1.f;
+            k[0] = fmaf(gm, sum0[j], k[0]);
+            k[1] = fmaf(gm, sum1[j], k[1]);
+        },
+        [&](int g, float (&k)[2]) { part[g] = make_float2(k[0], k[1]); });
 }
 
 // dgamma, dbeta of 32 channels: eight threads each take every eighth (sample, split), their sums are added in order
@@ -201,11 +277,11 @@ __device__ __forceinline__ void sum_gradients(const GnArgs &a, float *sm)
         for (; i + 56 < total; i += 64) {
             float2 v[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = a.part[(size_t)(i + 8 * u) * a.c + ch];
+            for (int u = 0; u < 8; ++u) v[u] = a.chan[(size_t)(i + 8 * u) * a.c + ch];
 #pragma unroll
             for (int u = 0; u < 8; ++u) { s0 += v[u].x; s1 += v[u].y; }
         }
-        for (; i < total; i += 8) { const float2 v = a.part[(size_t)i * a.c + ch]; s0 += v.x; s1 += v.y; }
+        for (; i < total; i += 8) { const float2 v = a.chan[(size_t)i * a.c + ch]; s0 += v.x; s1 += v.y; }
     }
     sm[threadIdx.x] = s0;
     sm[NT + threadIdx.x] = s1;
@@ -218,55 +294,39 @@ __device__ __forceinline__ void sum_gradients(const GnArgs &a, float *sm)
     }
 }
 
-// The two results of each group that channels [ch0, ch0 + width) belong to, from all partials of the group, in st[2 * (group - first)]:
-// forward mean and rstd, backward mean(t) and mean(t * xhat).  `per` threads (a power of two within a wavefront) share a group.
+// The two results of each of a slab's groups in st[2 * (group - first)]: forward mean and rstd, backward mean(t) and mean(t * xhat).
 template <bool BWD>
-__device__ __forceinline__ void group_results(const GnArgs &a, int n, int ch0, int width, float *st)
+__device__ __forceinline__ void group_results(const GnArgs &a, int n, const Slab &s, float *st)
 {
-    const int g0 = ch0 / a.cg, gs = (ch0 + width - 1) / a.cg - g0 + 1;
-    int per = 64;
-    while (per > 1 && per * gs > NT) per >>= 1;
-    const int sub = threadIdx.x & (per - 1), step = NT / per;
-    const int entries = a.cg * a.splits;
-    const float2 *part = a.part + (size_t)n * a.splits * a.c;
-    for (int gb = 0; gb < gs; gb += step) {
-        const int gi = gb + threadIdx.x / per, g = g0 + gi;
-        if (gi >= gs) continue;   // whole teams of `per` lanes
-        const float2 *pg = part + g * a.cg;
-        float s0 = 0.f, s1 = 0.f, s2 = 0.f;
-        const float shift = BWD ? 0.f : pg[0].x;   // deviations from one of the means, so that the sums below stay small
-        for (int i = sub; i < entries; i += per) {
-            const int split = i / a.cg, c = i - split * a.cg;
-            const float2 v = pg[(size_t)split * a.c + c];
+    const float2 *part = a.part + (size_t)n * a.splits * a.cells + s.g0 * a.per_group;
+    for_teams<NT, 3>(s.gs, a.splits * a.per_group,
+        [&](int g, int i, float (&k)[3]) {
+            const int split = a.per_group == 1 ? i : i / a.per_group, cell = g * a.per_group + i - split * a.per_group;
+            const float2 v = part[(size_t)split * a.cells + cell];
             if (BWD) {
-                const float gamma = a.gamma != nullptr ? a.gamma[g * a.cg + c] : 1.f;
-                s0 = fmaf(gamma, v.x, s0);
-                s1 = fmaf(gamma, v.y, s1);
-            } else {
-                const float d = v.x - shift, w = (float)(min(a.hw, (split + 1) * a.split_pixels) - split * a.split_pixels);
-                s0 = fmaf(w, d, s0);
-                s1 = fmaf(w * d, d, s1);
-                s2 += v.y;
+                k[0] += v.x;
+                k[1] += v.y;
+            } else {   // deviations from one of the means, so that the sums stay small
+                const float d = v.x - part[g * a.per_group].x;
+                const int width = a.per_group == 1 ? a.cg : min(a.cs, a.cg - (i - split * a.per_group) * a.cs);
+                const float w = (float)(min(a.hw, (split + 1) * a.split_pixels) - split * a.split_pixels) * (float)width;
+                k[0] = fmaf(w, d, k[0]);
+                k[1] = fmaf(w * d, d, k[1]);
+                k[2] += v.y;
             }
-        }
-        for (int o = per >> 1; o >= 1; o >>= 1) {
-            s0 += __shfl_xor(s0, o, 64);
-            s1 += __shfl_xor(s1, o, 64);
-            if (!BWD) s2 += __shfl_xor(s2, o, 64);
-        }
-        if (sub == 0) {
+        },
+        [&](int g, float (&k)[3]) {
             if (BWD) {
-                st[2 * gi] = s0 * a.inv_count;
-                st[2 * gi + 1] = s1 * a.inv_count;
+                st[2 * g] = k[0] * a.inv_count;
+                st[2 * g + 1] = k[1] * a.inv_count;
             } else {
-                const float off = s0 * a.inv_count;
-                float var = (s2 + s1 - s0 * off) * a.inv_count;
+                const float off = k[0] * a.inv_count;
+                float var = (k[2] + k[1] - k[0] * off) * a.inv_count;
                 if (var < 0.f) var = 0.f;   // a NaN stays one
-                st[2 * gi] = shift + off;
-                st[2 * gi + 1] = 1.f / sqrtf(var + a.eps);
+                st[2 * g] = part[g * a.per_group].x + off;
+                st[2 * g + 1] = 1.f / sqrtf(var + a.eps);
             }
-        }
-    }
+        });
     __syncthreads();
 }
 
@@ -280,36 +340,34 @@ __global__ __launch_bounds__(NT) void k_gn_apply(GnArgs a)
     int id = (int)blockIdx.x - a.grad_blocks;
     const int chunk = id % a.chunks;
     id /= a.chunks;
-    const int slab = id % a.slabs, n = id / a.slabs;
-    const int ch0 = slab * a.cs, width = min(a.cs, a.c - ch0), cvs = width / V, rows = NT / cvs;
-    group_results<BWD>(a, n, ch0, width, st);
-    if (!BWD && chunk == 0) {   // the statistics of the groups that begin in this slab
-        const int g0 = ch0 / a.cg, gs = (ch0 + width - 1) / a.cg - g0 + 1;
-        for (int gi = t; gi < gs; gi += NT) {
-            if ((g0 + gi) * a.cg < ch0) continue;
-            if (a.mean_out != nullptr) a.mean_out[n * a.groups + g0 + gi] = st[2 * gi];
-            if (a.rstd_out != nullptr) a.rstd_out[n * a.groups + g0 + gi] = st[2 * gi + 1];
+    const int n = id / a.slabs;
+    const Slab s = slab_of(a, id - n * a.slabs);
+    group_results<BWD>(a, n, s, st);
+    if (!BWD && chunk == 0 && s.ch0 == s.g0 * a.cg) {   // the slab in which its groups begin
+        for (int g = t; g < s.gs; g += NT) {
+            if (a.mean_out != nullptr) a.mean_out[n * a.groups + s.g0 + g] = st[2 * g];
+            if (a.rstd_out != nullptr) a.rstd_out[n * a.groups + s.g0 + g] = st[2 * g + 1];
         }
     }
-    const int row = t / cvs, ch = ch0 + (t - row * cvs) * V;
+    const int cvs = s.width / V, rows = NT / cvs, row = t / cvs, ch = s.ch0 + (t - row * cvs) * V;
     if (row >= rows) return;
-    ChannelConst<V> k;
-    affine<V>(a, ch, k);
-    float mt[V], mtx[V];   // forward: rstd * gamma in mt
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-        const int gi = (ch + e) / a.cg - ch0 / a.cg;
+    // forward  y = act((x - mean) * scale + beta);  backward  dx = g * scale - (off + (x - mean) * slope)
+    float mean[V], scale[V], beta[V], off[V], slope[V];
+    load_floats<V>(a.gamma != nullptr ? a.gamma + ch : nullptr, 1.f, scale);
+    load_floats<V>(a.beta != nullptr ? a.beta + ch : nullptr, 0.f, beta);
+    for_groups<V>(ch, a.cg, [&](int e, int g) {
+        const float s0 = st[2 * (g - s.g0)], s1 = st[2 * (g - s.g0) + 1];
         if (BWD) {
-            mt[e] = st[2 * gi];
-            mtx[e] = st[2 * gi + 1];
-            const int g = n * a.groups + (ch + e) / a.cg;
-            k.mean[e] = a.mean_in[g];
-            k.rstd[e] = a.rstd_in[g];
+            const float rstd = a.rstd_in[n * a.groups + g];
+            mean[e] = a.mean_in[n * a.groups + g];
+            scale[e] *= rstd;
+            off[e] = rstd * s0;
+            slope[e] = rstd * rstd * s1;
         } else {
-            k.mean[e] = st[2 * gi];
-            k.rstd[e] = st[2 * gi + 1];
+            mean[e] = s0;
+            scale[e] *= s1;
         }
-    }
+    });
     const size_t base = (size_t)n * a.hw * a.c + ch;
     const T *x = (const T *)a.x + base, *dy = (const T *)a.dy + base, *ys = (const T *)a.y_saved + base;
     T *out = (T *)a.out + base;
@@ -328,23 +386,14 @@ __global__ __launch_bounds__(NT) void k_gn_apply(GnArgs a)
         for (int u = 0; u < U; ++u) {
             if (p + u * rows >= p1) continue;
             Pack<T, V> r;
-            float vx[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) vx[e] = as_f32(qx[u].v[e]);
-            if (BWD) {
-                float vd[V], vy[V] = {}, g[V], xh[V];
-#pragma unroll
-                for (int e = 0; e < V; ++e) { vd[e] = as_f32(qd[u].v[e]); if (ACT == ACT_MASK) vy[e] = as_f32(qy[u].v[e]); }
-                gradient<V, ACT>(k, vx, vd, vy, g, xh);
-#pragma unroll
-                for (int e = 0; e < V; ++e) r.v[e] = from_f32<T>(k.rstd[e] * (fmaf(g[e], k.gamma[e], -mt[e]) - xh[e] * mtx[e]));
-            } else {
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    float u1 = fmaf((vx[e] - k.mean[e]) * k.rstd[e], k.gamma[e], k.beta[e]);
-                    if (ACT == ACT_RELU) u1 = u1 > 0.f ? u1 : u1 == u1 ? 0.f : u1;   // a NaN stays one
-                    if (ACT == ACT_SILU) u1 *= sigmoid(u1);
-                    r.v[e] = from_f32<T>(u1);
+            for (int e = 0; e < V; ++e) {
+                const float xm = as_f32(qx[u].v[e]) - mean[e];
+                if (BWD) {
+                    const float g = gradient<ACT>(as_f32(qd[u].v[e]), ACT == ACT_MASK ? as_f32(qy[u].v[e]) : 0.f, xm, scale[e], beta[e]);
+                    r.v[e] = from_f32<T>(fmaf(g, scale[e], -fmaf(xm, slope[e], off[e])));
+                } else {
+                    r.v[e] = from_f32<T>(activation<ACT>(fmaf(xm, scale[e], beta[e])));
                 }
             }
             *reinterpret_cast<Pack<T, V> *>(out + (size_t)(p + u * rows) * a.c) = r;
@@ -354,40 +403,57 @@ __global__ __launch_bounds__(NT) void k_gn_apply(GnArgs a)
 
 // ---- launch shapes ------------------------------------------------------------------------------------------------
 
-int vector_of(const dp_group_norm_desc &d)
+int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+int gcd(int a, int b) { return b == 0 ? a : gcd(b, a % b); }
+
+// Slabs for vectors of V channels: as many whole groups as a block's threads cover, or equal parts of a wider group.  False: a
+// group boundary falls inside a vector that a slab cannot avoid.
+bool slabs_for(int V, GnArgs &a)
 {
-    const int v = d.io_dtype == DP_BF16 ? 8 : 4;
-    return d.c % v == 0 ? v : 1;
+    const int cap = NT * V, unit = V / gcd(V, a.cg);   // groups that fill whole vectors
+    a.per_group = 1;
+    if (a.c % V != 0) return false;
+    if (unit * a.cg <= cap) {
+        const int64_t width = (int64_t)unit * a.cg;
+        a.slabs = ceil_div(a.c, cap / width * width);
+        a.cs = (int)(ceil_div(ceil_div(a.c, width), a.slabs) * width);
+        a.slabs = ceil_div(a.c, a.cs);
+        a.cells = a.groups;
+        return true;
+    }
+    if (unit != 1) return false;
+    a.per_group = ceil_div(a.cg, cap);
+    a.cs = ceil_div(a.cg / V, a.per_group) * V;
+    a.per_group = ceil_div(a.cg, a.cs);
+    a.slabs = a.cells = a.groups * a.per_group;
+    return true;
 }
 
-int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
-
-// Slabs of at most NT vectors, of equal width where possible.  Splits: about four blocks per compute unit, at least eight pixels per
-// thread, and few enough that a block of the second kernel reads at most 8192 partials (64 KB, from L2) or one split's.
-void shape(const dp_group_norm_desc &d, bool bwd, GnArgs &a)
+// Vectors where they fit, single channels else.  Splits: about four blocks per compute unit, at least eight pixels per thread,
+// and few enough that a block of the second kernel reads at most 2048 partials (16 KB, from L2).
+int shape(const dp_group_norm_desc &d, bool bwd, GnArgs &a)
 {
-    const int V = vector_of(d);
     a.n = d.n; a.hw = d.h * d.w; a.c = d.c; a.groups = d.groups; a.cg = d.c / d.groups;
     a.eps = d.eps;
     a.inv_count = (float)(1.0 / ((double)a.hw * a.cg));
-    const int vectors = d.c / V;
-    a.slabs = ceil_div(vectors, NT);
-    a.cs = ceil_div(vectors, a.slabs) * V;
-    a.slabs = ceil_div(d.c, a.cs);
-    const int rows = NT / (a.cs / V);
+    int V = d.io_dtype == DP_BF16 ? 8 : 4;
+    if (!slabs_for(V, a)) slabs_for(V = 1, a);
+    const int rows = NT / (a.cs / V), slab_groups = a.per_group == 1 ? a.cs / a.cg : a.per_group;
     int64_t splits = ceil_div(1024, (int64_t)a.n * a.slabs);
     splits = std::min<int64_t>(splits, ceil_div(a.hw, 8 * rows));
-    splits = std::min<int64_t>(splits, std::max(1, 8192 / a.c));
+    splits = std::min<int64_t>(splits, std::max(1, 2048 / slab_groups));
     a.split_pixels = ceil_div(a.hw, splits);
     a.splits = ceil_div(a.hw, a.split_pixels);
     int64_t chunks = ceil_div(2048, (int64_t)a.n * a.slabs);
-    chunks = std::min<int64_t>(chunks, ceil_div(a.hw, 8 * rows));
+    chunks = std::min<int64_t>(chunks, ceil_div(a.hw, 4 * rows));
     a.chunk_pixels = ceil_div(a.hw, chunks);
     a.chunks = ceil_div(a.hw, a.chunk_pixels);
     a.grad_blocks = bwd ? ceil_div(a.c, 32) : 0;
+    return V;
 }
 
-size_t part_bytes(const GnArgs &a) { return (size_t)a.n * a.splits * a.c * sizeof(float2); }
+size_t cell_bytes(const GnArgs &a) { return ((size_t)a.n * a.splits * a.cells * sizeof(float2) + 15) / 16 * 16; }
+size_t part_bytes(const GnArgs &a, bool bwd) { return cell_bytes(a) + (bwd ? (size_t)a.n * a.splits * a.c * sizeof(float2) : 0); }
 
 template <typename T, int V, bool BWD, int ACT>
 void launch(const GnArgs &a, bool apply, hipStream_t st)
@@ -407,14 +473,13 @@ void launch_act(const GnArgs &a, int act, bool apply, hipStream_t st)
 }
 
 template <bool BWD>
-void launch_type(const dp_group_norm_desc &d, const GnArgs &a, int act, bool apply, hipStream_t st)
+void launch_type(const dp_group_norm_desc &d, int V, const GnArgs &a, int act, bool apply, hipStream_t st)
 {
-    const int v = vector_of(d);
     if (d.io_dtype == DP_BF16) {
-        if (v == 8) launch_act<bf16_t, 8, BWD>(a, act, apply, st);
+        if (V == 8) launch_act<bf16_t, 8, BWD>(a, act, apply, st);
         else launch_act<bf16_t, 1, BWD>(a, act, apply, st);
     } else {
-        if (v == 4) launch_act<float, 4, BWD>(a, act, apply, st);
+        if (V == 4) launch_act<float, 4, BWD>(a, act, apply, st);
         else launch_act<float, 1, BWD>(a, act, apply, st);
     }
 }
@@ -432,7 +497,7 @@ dp_status check_desc(const dp_group_norm_desc *d)
     const int64_t hw = (int64_t)d->h * d->w;
     if (hw >= limit || hw * d->c >= limit || hw * d->c * d->n >= limit) { dp_set_error("group norm: a tensor must hold fewer than 2^31 elements"); return DP_ERR_BAD_DESC; }
     // pixel numbers of a block's last steps pass h * w; a grid has fewer than 2^32 threads
-    if (hw > ((int64_t)1 << 30) || (int64_t)d->n * ceil_div(d->c, NT) > (1 << 23)) { dp_set_error("group norm: h * w > 2^30 or n * ceil(c / 256) > 2^23"); return DP_ERR_BAD_DESC; }
+    if (hw > ((int64_t)1 << 30) || (int64_t)d->n * ceil_div(d->c, NT) > (1 << 22)) { dp_set_error("group norm: h * w > 2^30 or n * ceil(c / 256) > 2^22"); return DP_ERR_BAD_DESC; }
     if (!(d->eps > 0.f) || !std::isfinite(d->eps)) { dp_set_error("group norm: eps must be positive"); return DP_ERR_BAD_DESC; }
     return DP_OK;
 }
@@ -461,7 +526,7 @@ extern "C" size_t dp_group_norm_workspace_bytes(const dp_group_norm_desc *desc, 
     if (check_desc(desc) != DP_OK || (pass != DP_PASS_FWD && pass != DP_PASS_DGRAD)) return 0;
     GnArgs a = {};
     shape(*desc, pass == DP_PASS_DGRAD, a);
-    return part_bytes(a);
+    return part_bytes(a, pass == DP_PASS_DGRAD);
 }
 
 extern "C" dp_status dp_group_norm_fwd(const dp_group_norm_desc *desc, const void *x, const float *gamma, const float *beta, void *y, float *mean,
@@ -470,11 +535,11 @@ extern "C" dp_status dp_group_norm_fwd(const dp_group_norm_desc *desc, const voi
     dp_status s = check_desc(desc);
     if (s != DP_OK) return s;
     GnArgs a = {};
-    shape(*desc, false, a);
-    s = check_ptrs("group norm forward", {x, y}, {gamma, beta, mean, rstd}, ws, ws_bytes, part_bytes(a));
+    const int V = shape(*desc, false, a);
+    s = check_ptrs("group norm forward", {x, y}, {gamma, beta, mean, rstd}, ws, ws_bytes, part_bytes(a, false));
     if (s != DP_OK) return s;
     a.x = x; a.gamma = gamma; a.beta = beta; a.out = y; a.mean_out = mean; a.rstd_out = rstd; a.part = (float2 *)ws;
-    launch_type<false>(*desc, a, desc->flags == DP_RELU ? ACT_RELU : desc->flags == DP_SILU ? ACT_SILU : ACT_NONE, true, (hipStream_t)hip_stream);
+    launch_type<false>(*desc, V, a, desc->flags == DP_RELU ? ACT_RELU : desc->flags == DP_SILU ? ACT_SILU : ACT_NONE, true, (hipStream_t)hip_stream);
     return launched("group norm forward");
 }
 
@@ -486,12 +551,12 @@ extern "C" dp_status dp_group_norm_bwd(const dp_group_norm_desc *desc, const voi
     if (s != DP_OK) return s;
     if (dx == nullptr && dgamma == nullptr && dbeta == nullptr) { dp_set_error("group norm backward: no output requested"); return DP_ERR_NULL; }
     GnArgs a = {};
-    shape(*desc, true, a);
+    const int V = shape(*desc, true, a);
     if (dgamma == nullptr && dbeta == nullptr) a.grad_blocks = 0;
-    s = check_ptrs("group norm backward", {x, dy, mean, rstd}, {y_saved, gamma, beta, dx, dgamma, dbeta}, ws, ws_bytes, part_bytes(a));
+    s = check_ptrs("group norm backward", {x, dy, mean, rstd}, {y_saved, gamma, beta, dx, dgamma, dbeta}, ws, ws_bytes, part_bytes(a, true));
     if (s != DP_OK) return s;
     a.x = x; a.dy = dy; a.y_saved = y_saved; a.gamma = gamma; a.beta = beta; a.mean_in = mean; a.rstd_in = rstd;
-    a.out = dx; a.dgamma = dgamma; a.dbeta = dbeta; a.part = (float2 *)ws;
-    launch_type<true>(*desc, a, desc->flags == DP_SILU ? ACT_SILU : desc->flags == DP_RELU && y_saved != nullptr ? ACT_MASK : ACT_NONE, dx != nullptr, (hipStream_t)hip_stream);
+    a.out = dx; a.dgamma = dgamma; a.dbeta = dbeta; a.part = (float2 *)ws; a.chan = (float2 *)((char *)ws + cell_bytes(a));
+    launch_type<true>(*desc, V, a, desc->flags == DP_SILU ? ACT_SILU : desc->flags == DP_RELU && y_saved != nullptr ? ACT_MASK : ACT_NONE, dx != nullptr, (hipStream_t)hip_stream);
     return launched("group norm backward");
 }
