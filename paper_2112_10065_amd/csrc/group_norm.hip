@@ -31,6 +31,8 @@ struct GnArgs {
     int chunks, chunk_pixels;        // the same for the second kernel's blocks
     int grad_blocks;                 // blocks of the second kernel that sum dgamma / dbeta
     float eps, inv_count;            // 1 / (hw * cg)
+    int past;                        // the second kernel's stores (1), loads too (2) go past the caches
+    int units, units_each;           // one-kernel form: units in all, units of an eighth of them
 };
 
 struct Slab { int ch0, width, g0, gs, cell0; };   // first channel, channels, first group, groups, first cell
@@ -142,6 +144,7 @@ template <int N, int K, typename F, typename P> __device__ __forceinline__ void 
     const int sub = threadIdx.x & (per - 1), step = N / per;
     for (int g = threadIdx.x / per; g < gs; g += step) {   // whole teams
         float s[K] = {};
+#pragma unroll 4
         for (int i = sub; i < entries; i += per) f(g, i, s);
         for (int o = per >> 1; o >= 1; o >>= 1)
 #pragma unroll
@@ -330,8 +333,8 @@ __device__ __forceinline__ void group_results(const GnArgs &a, int n, const Slab
     __syncthreads();
 }
 
-// Second kernel.  Block = (sample, slab of channels, chunk of pixels).
-template <typename T, int V, bool BWD, int ACT>
+// Second kernel.  Block = (sample, slab of channels, chunk of pixels).  PAST: 1: stores go past the caches, 2: loads too.
+template <typename T, int V, bool BWD, int ACT, int PAST>
 __global__ __launch_bounds__(NT) void k_gn_apply(GnArgs a)
 {
     __shared__ float st[2 * NT * V];
@@ -342,6 +345,23 @@ __global__ __launch_bounds__(NT) void k_gn_apply(GnArgs a)
     id /= a.chunks;
     const int n = id / a.slabs;
     const Slab s = slab_of(a, id - n * a.slabs);
+    const int cvs = s.width / V, rows = NT / cvs, row = t / cvs, ch = s.ch0 + (t - row * cvs) * V;
+    const size_t base = (size_t)n * a.hw * a.c + ch;
+    const T *x = (const T *)a.x + base, *dy = (const T *)a.dy + base, *ys = (const T *)a.y_saved + base;
+    T *out = (T *)a.out + base;
+    const int p0 = chunk * a.chunk_pixels + row, p1 = row < rows ? min(a.hw, (chunk + 1) * a.chunk_pixels) : 0;
+    constexpr int U = 4;
+    Pack<T, V> qx[U], qd[U], qy[U];
+    auto fetch = [&](int p) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const size_t o = (size_t)min(p + u * rows, p1 - 1) * a.c;
+            qx[u] = load_vec<Pack<T, V>, PAST == 2>(x + o);
+            if (BWD) qd[u] = load_vec<Pack<T, V>, PAST == 2>(dy + o);
+            if (BWD && ACT == ACT_MASK) qy[u] = load_vec<Pack<T, V>, PAST == 2>(ys + o);
+        }
+    };
+    if (p0 < p1) fetch(p0);   // on their way while the partials are added up
     group_results<BWD>(a, n, s, st);
     if (!BWD && chunk == 0 && s.ch0 == s.g0 * a.cg) {   // the slab in which its groups begin
         for (int g = t; g < s.gs; g += NT) {
@@ -349,8 +369,7 @@ __global__ __launch_bounds__(NT) void k_gn_apply(GnArgs a)
             if (a.rstd_out != nullptr) a.rstd_out[n * a.groups + s.g0 + g] = st[2 * g + 1];
         }
     }
-    const int cvs = s.width / V, rows = NT / cvs, row = t / cvs, ch = s.ch0 + (t - row * cvs) * V;
-    if (row >= rows) return;
+    if (p0 >= p1) return;
     // forward  y = act((x - mean) * scale + beta);  backward  dx = g * scale - (off + (x - mean) * slope)
     float mean[V], scale[V], beta[V], off[V], slope[V];
     load_floats<V>(a.gamma != nullptr ? a.gamma + ch : nullptr, 1.f, scale);
@@ -368,20 +387,7 @@ __global__ __launch_bounds__(NT) void k_gn_apply(GnArgs a)
             scale[e] *= s1;
         }
     });
-    const size_t base = (size_t)n * a.hw * a.c + ch;
-    const T *x = (const T *)a.x + base, *dy = (const T *)a.dy + base, *ys = (const T *)a.y_saved + base;
-    T *out = (T *)a.out + base;
-    const int p0 = chunk * a.chunk_pixels, p1 = min(a.hw, p0 + a.chunk_pixels);
-    constexpr int U = 4;
-    for (int p = p0 + row; p < p1; p += U * rows) {
-        Pack<T, V> qx[U], qd[U], qy[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const size_t o = (size_t)min(p + u * rows, p1 - 1) * a.c;
-            qx[u] = *reinterpret_cast<const Pack<T, V> *>(x + o);
-            if (BWD) qd[u] = *reinterpret_cast<const Pack<T, V> *>(dy + o);
-            if (BWD && ACT == ACT_MASK) qy[u] = *reinterpret_cast<const Pack<T, V> *>(ys + o);
-        }
+    for (int p = p0;;) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (p + u * rows >= p1) continue;
@@ -396,9 +402,217 @@ __global__ __launch_bounds__(NT) void k_gn_apply(GnArgs a)
                     r.v[e] = from_f32<T>(activation<ACT>(fmaf(xm, scale[e], beta[e])));
                 }
             }
-            *reinterpret_cast<Pack<T, V> *>(out + (size_t)(p + u * rows) * a.c) = r;
+            store_vec<Pack<T, V>, PAST != 0>(out + (size_t)(p + u * rows) * a.c, r);
         }
+        p += U * rows;
+        if (p >= p1) break;
+        fetch(p);
     }
+}
+
+// ---- one kernel for small images ----------------------------------------------------------------------------------
+//
+// Where a group's pixels fit in the registers of a team of wavefronts, the tensor is read once and there is no second kernel to wait
+// for.  A unit is the narrowest column of channels that is whole groups and whole vectors: one group of cvs vectors, or the K groups of
+// one vector.  W wavefronts hold a unit, R vectors to a lane; all of them belong to the same K groups, so sums are reductions of whole wavefronts.
+// Units of a cache line are handed to one die (blocks go to the eight dies in turn), whose L2 then reads the line once.
+
+// v of all W wavefronts of the team, in order; sm: W * N floats of the team's own.  A block has one team where W > 1.
+template <int W, int N> __device__ __forceinline__ void team_sum(float (&v)[N], float *sm)
+{
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = wave_sum_fast(v[e]);
+    if (W == 1) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __syncthreads();
+    if (lane == 0)
+#pragma unroll
+        for (int e = 0; e < N; ++e) sm[wave * N + e] = v[e];
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) s += sm[w * N + e];
+        v[e] = s;
+    }
+}
+
+// The same per channel of the unit (lane's vector t % cvs, cvs a power of two): every lane gets its own channels' sums.  sm: W * 64 * V floats.
+template <int W, int V> __device__ __forceinline__ void team_channel_sum(float (&v)[V], int cvs, float *sm)
+{
+    for (int o = cvs; o < 64; o <<= 1)
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] += __shfl_xor(v[e], o, 64);
+    if (W == 1) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, width = cvs * V, j = (lane & (cvs - 1)) * V;
+    __syncthreads();
+    if (lane < cvs)
+#pragma unroll
+        for (int e = 0; e < V; ++e) sm[wave * width + j + e] = v[e];
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        float s = 0.f;
+        for (int w = 0; w < W; ++w) s += sm[w * width + j + e];
+        v[e] = s;
+    }
+}
+
+template <typename T, int V, int K, bool BWD, int ACT, int W, int R>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_gn_unit(GnArgs a)
+{
+    constexpr int P = V / K;   // channels of a vector in one group (all of them where the group is wider)
+    __shared__ float sm[W == 1 ? 1 : BWD ? W * 64 * V : W * K];
+    const int block = (int)(blockIdx.x & 7) * a.units_each + (int)(blockIdx.x >> 3);
+    const int unit = W == 1 ? block * 4 + (int)(threadIdx.x >> 6) : block;
+    if ((int)(blockIdx.x >> 3) >= a.units_each || unit >= a.units) return;   // whole teams
+    const int t = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const int per_sample = a.c / (K > 1 ? V : a.cg), n = unit / per_sample, ch0 = (unit - n * per_sample) * (K > 1 ? V : a.cg);
+    const int cvs = K > 1 ? 1 : a.cg / V, rows = 64 * W / cvs, row = t / cvs, ch = ch0 + (t & (cvs - 1)) * V, g0 = n * a.groups + ch0 / a.cg;
+    const size_t base = ((size_t)n * a.hw + row) * a.c + ch, step = (size_t)rows * a.c;
+    const T *x = (const T *)a.x + base, *dy = (const T *)a.dy + base, *ys = (const T *)a.y_saved + base;
+    typedef Pack<T, V> P16;
+    words4 qx[R], qd[BWD ? R : 1], qy[ACT == ACT_MASK ? R : 1];   // as loaded
+    auto again = [&]() {             // they stay packed between the passes: unpacked once for all they would need twice the registers
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            asm("" : "+v"(qx[i]));
+            if (BWD) asm("" : "+v"(qd[BWD ? i : 0]));
+        }
+    };
+    const int count = row < a.hw ? (a.hw - row + rows - 1) / rows : 0;   // this lane's pixels: row, row + rows, ...
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+        if (i < count) {
+            qx[i] = *reinterpret_cast<const words4 *>(x + i * step);
+            if (BWD) qd[BWD ? i : 0] = *reinterpret_cast<const words4 *>(dy + i * step);
+            if (ACT == ACT_MASK) qy[ACT == ACT_MASK ? i : 0] = *reinterpret_cast<const words4 *>(ys + i * step);
+        }
+    float mean[K], rstd[K];
+    float scale[V], beta[V];
+    load_floats<V>(a.gamma != nullptr ? a.gamma + ch : nullptr, 1.f, scale);
+    load_floats<V>(a.beta != nullptr ? a.beta + ch : nullptr, 0.f, beta);
+    T *out = (T *)a.out + base;
+    if constexpr (!BWD) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) mean[k] = rstd[k] = 0.f;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i < count) {
+                const P16 vx = __builtin_bit_cast(P16, qx[i]);
+#pragma unroll
+                for (int e = 0; e < V; ++e) mean[e / P] += as_f32(vx.v[e]);
+            }
+        again();
+        team_sum<W, K>(mean, sm);
+#pragma unroll
+        for (int k = 0; k < K; ++k) mean[k] *= a.inv_count;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i < count) {
+                const P16 vx = __builtin_bit_cast(P16, qx[i]);
+#pragma unroll
+                for (int e = 0; e < V; ++e) { const float d = as_f32(vx.v[e]) - mean[e / P]; rstd[e / P] = fmaf(d, d, rstd[e / P]); }
+            }
+        again();
+        team_sum<W, K>(rstd, sm);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            rstd[k] = 1.f / sqrtf(fmaf(rstd[k], a.inv_count, a.eps));
+            if (t == 0) {
+                if (a.mean_out != nullptr) a.mean_out[g0 + k] = mean[k];
+                if (a.rstd_out != nullptr) a.rstd_out[g0 + k] = rstd[k];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) scale[e] *= rstd[e / P];
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i < count) {
+                const P16 vx = __builtin_bit_cast(P16, qx[i]);
+                P16 r;
+#pragma unroll
+                for (int e = 0; e < V; ++e) r.v[e] = from_f32<T>(activation<ACT>(fmaf(as_f32(vx.v[e]) - mean[e / P], scale[e], beta[e])));
+                *reinterpret_cast<P16 *>(out + i * step) = r;
+            }
+    } else {
+        if (ACT == ACT_MASK)   // the mask goes into dy at once
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                if (i < count) {
+                    const P16 q = __builtin_bit_cast(P16, qy[ACT == ACT_MASK ? i : 0]);
+                    P16 vd = __builtin_bit_cast(P16, qd[i]);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) vd.v[e] = as_f32(q.v[e]) > 0.f ? vd.v[e] : (T)0;
+                    qd[i] = __builtin_bit_cast(words4, vd);
+                }
+#pragma unroll
+        for (int k = 0; k < K; ++k) { mean[k] = a.mean_in[g0 + k]; rstd[k] = a.rstd_in[g0 + k]; }
+        constexpr int G = ACT == ACT_MASK ? ACT_NONE : ACT;
+        float A[V] = {}, B[V] = {}, gamma[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) { gamma[e] = scale[e]; scale[e] *= rstd[e / P]; }
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i < count) {
+                const P16 vx = __builtin_bit_cast(P16, qx[i]), vd = __builtin_bit_cast(P16, qd[i]);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float xm = as_f32(vx.v[e]) - mean[e / P], g = gradient<G>(as_f32(vd.v[e]), 0.f, xm, scale[e], beta[e]);
+                    A[e] += g;
+                    B[e] = fmaf(g, xm, B[e]);
+                }
+            }
+        again();
+        team_channel_sum<W, V>(A, cvs, sm);
+        team_channel_sum<W, V>(B, cvs, sm);
+        float s0[K], s1[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) s0[k] = s1[k] = 0.f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            B[e] *= rstd[e / P];
+            s0[e / P] = fmaf(gamma[e], A[e], s0[e / P]);
+            s1[e / P] = fmaf(gamma[e], B[e], s1[e / P]);
+        }
+        for (int o = 1; o < cvs; o <<= 1)
+#pragma unroll
+            for (int k = 0; k < K; ++k) { s0[k] += __shfl_xor(s0[k], o, 64); s1[k] += __shfl_xor(s1[k], o, 64); }
+        if (t < cvs) {   // one lane for each vector of channels
+            if (a.n == 1) {
+                for (int e = 0; e < V; ++e) {
+                    if (a.dbeta != nullptr) a.dbeta[ch + e] = A[e];
+                    if (a.dgamma != nullptr) a.dgamma[ch + e] = B[e];
+                }
+            } else if (a.grad_blocks > 0) {
+                for (int e = 0; e < V; ++e) a.chan[(size_t)n * a.c + ch + e] = make_float2(A[e], B[e]);
+            }
+        }
+        if (a.out == nullptr) return;
+        float off[K], slope[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) { off[k] = rstd[k] * s0[k] * a.inv_count; slope[k] = rstd[k] * rstd[k] * s1[k] * a.inv_count; }
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i < count) {
+                const P16 vx = __builtin_bit_cast(P16, qx[i]), vd = __builtin_bit_cast(P16, qd[i]);
+                P16 r;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float xm = as_f32(vx.v[e]) - mean[e / P], g = gradient<G>(as_f32(vd.v[e]), 0.f, xm, scale[e], beta[e]);
+                    r.v[e] = from_f32<T>(fmaf(g, scale[e], -fmaf(xm, slope[e / P], off[e / P])));
+                }
+                *reinterpret_cast<P16 *>(out + i * step) = r;
+            }
+    }
+}
+
+// dgamma, dbeta from the units' sums
+__global__ __launch_bounds__(NT) void k_gn_sums(GnArgs a)
+{
+    __shared__ float sm[2 * NT];
+    sum_gradients(a, sm);
 }
 
 // ---- launch shapes ------------------------------------------------------------------------------------------------
@@ -449,18 +663,68 @@ int shape(const dp_group_norm_desc &d, bool bwd, GnArgs &a)
     a.chunk_pixels = ceil_div(a.hw, chunks);
     a.chunks = ceil_div(a.hw, a.chunk_pixels);
     a.grad_blocks = bwd ? ceil_div(a.c, 32) : 0;
+    const int64_t bytes = (int64_t)a.n * a.hw * a.c * (d.io_dtype == DP_BF16 ? 2 : 4);
+    a.past = bytes * (bwd ? 2 : 1) > (150 << 20) ? 2 : bytes > (32 << 20) ? 1 : 0;
     return V;
+}
+
+// The one-kernel form: wavefronts to a unit (0: the image does not fit), vectors to a lane.  Only for groups that are a power of two of whole
+// vectors or divide one.
+struct UnitForm { int waves, vectors, groups; };
+UnitForm unit_form(const GnArgs &a, int V, bool bwd, bool mask)
+{
+    UnitForm f = {0, 0, 1};
+    if (V == 1) return f;
+    int cvs = 1;
+    if (a.cg % V == 0) cvs = a.cg / V;
+    else if (V % a.cg == 0) f.groups = V / a.cg;
+    else return f;
+    if ((cvs & (cvs - 1)) != 0 || cvs > 64) return f;
+    const int64_t units = (int64_t)a.n * (a.c / std::max(a.cg, V));
+    const int w1 = ceil_div(a.hw, 64 / cvs), w4 = ceil_div(a.hw, 256 / cvs);
+    if (w1 <= 8) { f.waves = 1; f.vectors = 8; }
+    else if (w4 <= 8 && (!bwd || units < 1024 || (cvs > 1 && !mask))) { f.waves = 4; f.vectors = 8; }
+    else if (!bwd && w4 <= 16 && units <= 512) { f.waves = 4; f.vectors = 16; }
+    return f;
 }
 
 size_t cell_bytes(const GnArgs &a) { return ((size_t)a.n * a.splits * a.cells * sizeof(float2) + 15) / 16 * 16; }
 size_t part_bytes(const GnArgs &a, bool bwd) { return cell_bytes(a) + (bwd ? (size_t)a.n * a.splits * a.c * sizeof(float2) : 0); }
 
+template <typename T, int V, int K, bool BWD, int ACT>
+void launch_unit(GnArgs a, const UnitForm &f, hipStream_t st)
+{
+    a.units = a.n * (a.c / std::max(a.cg, V));
+    const int blocks = f.waves == 1 ? (a.units + 3) / 4 : a.units;
+    a.units_each = (blocks + 7) / 8;
+    a.splits = 1;
+    const dim3 grid(8 * a.units_each);
+    if (f.waves == 1) hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 1, 8>), grid, dim3(256), 0, st, a);
+    else if (f.vectors == 8 && f.waves == 4) hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 4, 8>), grid, dim3(256), 0, st, a);
+    else if constexpr (!BWD) hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 4, 16>), grid, dim3(256), 0, st, a);
+    if (BWD && a.grad_blocks > 0 && a.n > 1) hipLaunchKernelGGL(k_gn_sums, dim3(a.grad_blocks), dim3(NT), 0, st, a);
+}
+
 template <typename T, int V, bool BWD, int ACT>
 void launch(const GnArgs &a, bool apply, hipStream_t st)
 {
+    if constexpr (V > 1) {
+        const UnitForm f = unit_form(a, V, BWD, ACT == ACT_MASK);
+        if (f.waves > 0) {
+            if (f.groups == 1) return launch_unit<T, V, 1, BWD, ACT>(a, f, st);
+            if (f.groups == 2) return launch_unit<T, V, 2, BWD, ACT>(a, f, st);
+            if (f.groups == 4) return launch_unit<T, V, 4, BWD, ACT>(a, f, st);
+            if constexpr (V == 8) return launch_unit<T, V, 8, BWD, ACT>(a, f, st);
+        }
+    }
     hipLaunchKernelGGL((k_gn_reduce<T, V, BWD, BWD ? ACT : ACT_NONE>), dim3(a.n * a.slabs * a.splits), dim3(NT), 0, st, a);
     const int blocks = a.grad_blocks + (apply ? a.n * a.slabs * a.chunks : 0);
-    hipLaunchKernelGGL((k_gn_apply<T, V, BWD, ACT>), dim3(blocks), dim3(NT), 0, st, a);
+    if constexpr (V > 1) {
+        if (a.past == 2) hipLaunchKernelGGL((k_gn_apply<T, V, BWD, ACT, 2>), dim3(blocks), dim3(NT), 0, st, a);
+        else if (a.past == 1) hipLaunchKernelGGL((k_gn_apply<T, V, BWD, ACT, 1>), dim3(blocks), dim3(NT), 0, st, a);
+        if (a.past != 0) return;
+    }
+    hipLaunchKernelGGL((k_gn_apply<T, V, BWD, ACT, 0>), dim3(blocks), dim3(NT), 0, st, a);
 }
 
 template <typename T, int V, bool BWD>

@@ -13,6 +13,20 @@ typedef unsigned short bf16_t;
 
 template <typename T, int V> struct alignas(sizeof(T) * V) Pack { T v[V]; };
 
+// A vector that is read or written once: past the caches, where it would push out lines that are still wanted, or dirty ones in the
+// middle of the stream.
+typedef __attribute__((ext_vector_type(4))) unsigned int words4;
+template <typename P, bool PAST> __device__ __forceinline__ P load_vec(const void *p)
+{
+    if constexpr (sizeof(P) == 16 && PAST) return __builtin_bit_cast(P, __builtin_nontemporal_load(reinterpret_cast<const words4 *>(p)));
+    else return *reinterpret_cast<const P *>(p);
+}
+template <typename P, bool PAST> __device__ __forceinline__ void store_vec(void *p, const P &v)
+{
+    if constexpr (sizeof(P) == 16 && PAST) __builtin_nontemporal_store(__builtin_bit_cast(words4, v), reinterpret_cast<words4 *>(p));
+    else *reinterpret_cast<P *>(p) = v;
+}
+
 __device__ __forceinline__ float as_f32(float v) { return v; }
 __device__ __forceinline__ float as_f32(bf16_t v) { return __uint_as_float((unsigned)v << 16); }
 template <typename T> __device__ __forceinline__ T from_f32(float v);
