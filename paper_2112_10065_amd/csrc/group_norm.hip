@@ -144,7 +144,6 @@ template <int N, int K, typename F, typename P> __device__ __forceinline__ void 
     const int sub = threadIdx.x & (per - 1), step = N / per;
     for (int g = threadIdx.x / per; g < gs; g += step) {   // whole teams
         float s[K] = {};
-#pragma unroll 4
         for (int i = sub; i < entries; i += per) f(g, i, s);
         for (int o = per >> 1; o >= 1; o >>= 1)
 #pragma unroll
@@ -298,38 +297,62 @@ __device__ __forceinline__ void sum_gradients(const GnArgs &a, float *sm)
 }
 
 // The two results of each of a slab's groups in st[2 * (group - first)]: forward mean and rstd, backward mean(t) and mean(t * xhat).
+// Teams of up to 64 lanes share a group, eight partials to a lane at a time: they come from other dies, and the wait is the cost.
 template <bool BWD>
 __device__ __forceinline__ void group_results(const GnArgs &a, int n, const Slab &s, float *st)
 {
+    constexpr int U = 8;
+    const int entries = a.splits * a.per_group;
+    int per = 64;
+    while (per > 1 && (per * s.gs > NT || per >= 2 * entries)) per >>= 1;
+    const int sub = threadIdx.x & (per - 1), step = NT / per;
     const float2 *part = a.part + (size_t)n * a.splits * a.cells + s.g0 * a.per_group;
-    for_teams<NT, 3>(s.gs, a.splits * a.per_group,
-        [&](int g, int i, float (&k)[3]) {
-            const int split = a.per_group == 1 ? i : i / a.per_group, cell = g * a.per_group + i - split * a.per_group;
-            const float2 v = part[(size_t)split * a.cells + cell];
-            if (BWD) {
-                k[0] += v.x;
-                k[1] += v.y;
-            } else {   // deviations from one of the means, so that the sums stay small
-                const float d = v.x - part[g * a.per_group].x;
-                const int width = a.per_group == 1 ? a.cg : min(a.cs, a.cg - (i - split * a.per_group) * a.cs);
-                const float w = (float)(min(a.hw, (split + 1) * a.split_pixels) - split * a.split_pixels) * (float)width;
-                k[0] = fmaf(w, d, k[0]);
-                k[1] = fmaf(w * d, d, k[1]);
-                k[2] += v.y;
+    for (int g = threadIdx.x / per; g < s.gs; g += step) {   // whole teams
+        const float2 *pg = part + g * a.per_group;
+        // deviations from one of the means, so that the sums stay small
+        const float shift = BWD ? 0.f : pg->x;
+        float k0 = 0.f, k1 = 0.f, k2 = 0.f;
+        for (int i0 = sub; i0 < entries; i0 += U * per) {
+            float2 v[U];
+            float w[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = min(i0 + u * per, entries - 1), split = a.per_group == 1 ? i : i / a.per_group, sub_cell = i - split * a.per_group;
+                v[u] = pg[(size_t)split * a.cells + sub_cell];
+                const int width = a.per_group == 1 ? a.cg : min(a.cs, a.cg - sub_cell * a.cs);
+                w[u] = (float)(min(a.hw, (split + 1) * a.split_pixels) - split * a.split_pixels) * (float)width;
             }
-        },
-        [&](int g, float (&k)[3]) {
-            if (BWD) {
-                st[2 * g] = k[0] * a.inv_count;
-                st[2 * g + 1] = k[1] * a.inv_count;
-            } else {
-                const float off = k[0] * a.inv_count;
-                float var = (k[2] + k[1] - k[0] * off) * a.inv_count;
-                if (var < 0.f) var = 0.f;   // a NaN stays one
-                st[2 * g] = part[g * a.per_group].x + off;
-                st[2 * g + 1] = 1.f / sqrtf(var + a.eps);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (i0 + u * per >= entries) continue;
+                if (BWD) {
+                    k0 += v[u].x;
+                    k1 += v[u].y;
+                } else {
+                    const float d = v[u].x - shift;
+                    k0 = fmaf(w[u], d, k0);
+                    k1 = fmaf(w[u] * d, d, k1);
+                    k2 += v[u].y;
+                }
             }
-        });
+        }
+        for (int o = per >> 1; o >= 1; o >>= 1) {
+            k0 += __shfl_xor(k0, o, 64);
+            k1 += __shfl_xor(k1, o, 64);
+            if (!BWD) k2 += __shfl_xor(k2, o, 64);
+        }
+        if (sub != 0) continue;
+        if (BWD) {
+            st[2 * g] = k0 * a.inv_count;
+            st[2 * g + 1] = k1 * a.inv_count;
+        } else {
+            const float off = k0 * a.inv_count;
+            float var = (k2 + k1 - k0 * off) * a.inv_count;
+            if (var < 0.f) var = 0.f;   // a NaN stays one
+            st[2 * g] = shift + off;
+            st[2 * g + 1] = 1.f / sqrtf(var + a.eps);
+        }
+    }
     __syncthreads();
 }
 
@@ -441,9 +464,7 @@ template <int W, int N> __device__ __forceinline__ void team_sum(float (&v)[N], 
 // The same per channel of the unit (lane's vector t % cvs, cvs a power of two): every lane gets its own channels' sums.  sm: W * 64 * V floats.
 template <int W, int V> __device__ __forceinline__ void team_channel_sum(float (&v)[V], int cvs, float *sm)
 {
-    for (int o = cvs; o < 64; o <<= 1)
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] += __shfl_xor(v[e], o, 64);
+    stride_sums<V>(v, cvs);
     if (W == 1) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, width = cvs * V, j = (lane & (cvs - 1)) * V;
     __syncthreads();
@@ -652,18 +673,18 @@ int shape(const dp_group_norm_desc &d, bool bwd, GnArgs &a)
     a.inv_count = (float)(1.0 / ((double)a.hw * a.cg));
     int V = d.io_dtype == DP_BF16 ? 8 : 4;
     if (!slabs_for(V, a)) slabs_for(V = 1, a);
+    const int64_t sample_bytes = (int64_t)a.hw * a.c * (d.io_dtype == DP_BF16 ? 2 : 4), bytes = a.n * sample_bytes;
     const int rows = NT / (a.cs / V), slab_groups = a.per_group == 1 ? a.cs / a.cg : a.per_group;
     int64_t splits = ceil_div(1024, (int64_t)a.n * a.slabs);
     splits = std::min<int64_t>(splits, ceil_div(a.hw, 8 * rows));
-    splits = std::min<int64_t>(splits, std::max(1, 2048 / slab_groups));
+    splits = std::min<int64_t>(splits, std::max(1, (sample_bytes >= (16 << 20) ? 4096 : 2048) / slab_groups));
     a.split_pixels = ceil_div(a.hw, splits);
     a.splits = ceil_div(a.hw, a.split_pixels);
-    int64_t chunks = ceil_div(2048, (int64_t)a.n * a.slabs);
+    int64_t chunks = ceil_div(bytes > (64 << 20) ? 2048 : 1024, (int64_t)a.n * a.slabs);
     chunks = std::min<int64_t>(chunks, ceil_div(a.hw, 4 * rows));
     a.chunk_pixels = ceil_div(a.hw, chunks);
     a.chunks = ceil_div(a.hw, a.chunk_pixels);
     a.grad_blocks = bwd ? ceil_div(a.c, 32) : 0;
-    const int64_t bytes = (int64_t)a.n * a.hw * a.c * (d.io_dtype == DP_BF16 ? 2 : 4);
     a.past = bytes * (bwd ? 2 : 1) > (150 << 20) ? 2 : bytes > (32 << 20) ? 1 : 0;
     return V;
 }

@@ -65,6 +65,31 @@ template <typename F> __device__ __forceinline__ float wave_reduce(float v, floa
 __device__ __forceinline__ float wave_sum_fast(float v) { return wave_reduce(v, 0.f, [](float a, float b) { return a + b; }); }
 __device__ __forceinline__ float wave_max_fast(float v) { return wave_reduce(v, -3.402823466e38f, [](float a, float b) { return fmaxf(a, b); }); }
 
+// Sums over the lanes whose number agrees modulo `period` (a power of two up to 64), in every lane: rotations within rows of 16 lanes, longest
+// first, so that each meets the sums that it lacks; then two exchanges across rows.
+template <int CTRL, int N> __device__ __forceinline__ void add_moved(float (&v)[N])
+{
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] += moved<CTRL, 0xf>(v[e], 0.f);
+}
+template <int O, int N> __device__ __forceinline__ void add_exchanged(float (&v)[N])
+{
+    float w[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) w[e] = __shfl_xor(v[e], O, 64);
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] += w[e];
+}
+template <int N> __device__ __forceinline__ void stride_sums(float (&v)[N], int period)
+{
+    if (period <= 8) add_moved<0x128>(v);
+    if (period <= 4) add_moved<0x124>(v);
+    if (period <= 2) add_moved<0x122>(v);
+    if (period <= 1) add_moved<0x121>(v);
+    if (period <= 16) add_exchanged<16>(v);
+    if (period <= 32) add_exchanged<32>(v);
+}
+
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 inline dp_status launched(const char *what)
