@@ -703,7 +703,7 @@ UnitForm unit_form(const GnArgs &a, int V, bool bwd, bool mask)
     if ((cvs & (cvs - 1)) != 0 || cvs > 64) return f;
     const int64_t units = (int64_t)a.n * (a.c / std::max(a.cg, V));
     const int w1 = ceil_div(a.hw, 64 / cvs), w4 = ceil_div(a.hw, 256 / cvs);
-    if (w1 <= 8) { f.waves = 1; f.vectors = 8; }
+    if (w1 <= 8 && units >= 1024) { f.waves = 1; f.vectors = 8; }
     else if (w4 <= 8 && (!bwd || units < 1024 || (cvs > 1 && !mask))) { f.waves = 4; f.vectors = 8; }
     else if (!bwd && w4 <= 16 && units <= 512) { f.waves = 4; f.vectors = 16; }
     return f;
