@@ -32,7 +32,7 @@ static_assert(sizeof(Chunk) == 64, "one scalar load of 16 dwords");
 
 // Squares and sums in 64 bits: the square of a gradient beyond 1e19 is finite, and the result does not depend on how the
 // gradients are spread over the tensors.
-__device__ __forceinline__ double square_sum(const Chunk &c, int t)
+template <bool PAST> __device__ __forceinline__ double square_sum(const Chunk &c, int t)
 {
     double s = 0.0;
     const int nvec = c.count >> 2;
@@ -40,7 +40,7 @@ __device__ __forceinline__ double square_sum(const Chunk &c, int t)
 #pragma unroll
     for (int u = 0; u < kChunk / 1024; ++u) {
         const int i = u * 256 + t;
-        v[u] = i < nvec ? reinterpret_cast<const float4 *>(c.g)[i] : make_float4(0.f, 0.f, 0.f, 0.f);
+        v[u] = i < nvec ? load_vec<float4, PAST>(c.g + 4 * i) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
 #pragma unroll
     for (int u = 0; u < kChunk / 1024; ++u) {
@@ -68,11 +68,11 @@ __device__ __forceinline__ void write_norm(double sum, float max_norm, float *ou
     out[1] = !(norm <= 1.7e308) ? 0.f : norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.f;
 }
 
-__global__ __launch_bounds__(256) void k_norm_partial(const Chunk *__restrict__ table, long long n_chunks, double *__restrict__ partial)
+template <bool PAST> __global__ __launch_bounds__(256) void k_norm_partial(const Chunk *__restrict__ table, long long n_chunks, double *__restrict__ partial)
 {
     __shared__ double sm[4];
     double s = 0.0;
-    for (long long i = blockIdx.x; i < n_chunks; i += gridDim.x) s += square_sum(table[i], threadIdx.x);
+    for (long long i = blockIdx.x; i < n_chunks; i += gridDim.x) s += square_sum<PAST>(table[i], threadIdx.x);
     s = block_sum(s, sm);
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
@@ -115,10 +115,10 @@ __device__ __forceinline__ void adam_moments(const AdamArgs &a, float g, float &
 }
 __device__ __forceinline__ float adam_weight(const AdamArgs &a, float keep, float w, float m, float root)
 {
-    return fmaf(-a.step_size, m / fmaf(root, a.inv_root_bc2, a.eps), keep * w);
+    return fmaf(-a.step_size * m, __builtin_amdgcn_rcpf(fmaf(root, a.inv_root_bc2, a.eps)), keep * w);   // one unit in the last place of the update
 }
 
-__global__ __launch_bounds__(256) void k_adamw(const Chunk *__restrict__ table, AdamArgs a, const float *__restrict__ scale)
+template <bool PAST> __global__ __launch_bounds__(256) void k_adamw(const Chunk *__restrict__ table, AdamArgs a, const float *__restrict__ scale)
 {
     const Chunk c = table[blockIdx.x];
     float s;
@@ -132,10 +132,10 @@ __global__ __launch_bounds__(256) void k_adamw(const Chunk *__restrict__ table, 
     for (int u = 0; u < U; ++u) {
         const int i = u * 256 + t;
         if (i < nvec) {
-            g[u] = reinterpret_cast<const float4 *>(c.g)[i];
-            m[u] = reinterpret_cast<const float4 *>(m32)[i];
-            v[u] = reinterpret_cast<const float4 *>(v32)[i];
-            w[u] = reinterpret_cast<const float4 *>(c.w)[i];
+            g[u] = load_vec<float4, PAST>(c.g + 4 * i);
+            m[u] = load_vec<float4, PAST>(m32 + 4 * i);
+            v[u] = load_vec<float4, PAST>(v32 + 4 * i);
+            w[u] = load_vec<float4, PAST>(c.w + 4 * i);
         }
     }
 #pragma unroll
@@ -151,9 +151,9 @@ __global__ __launch_bounds__(256) void k_adamw(const Chunk *__restrict__ table, 
             we[e] = adam_weight(a, keep, we[e], me[e], sqrtf(ve[e]));
             o.v[e] = from_f32<bf16_t>(we[e]);
         }
-        reinterpret_cast<float4 *>(m32)[i] = m[u];
-        reinterpret_cast<float4 *>(v32)[i] = v[u];
-        reinterpret_cast<float4 *>(c.w)[i] = w[u];
+        store_vec<float4, PAST>(m32 + 4 * i, m[u]);
+        store_vec<float4, PAST>(v32 + 4 * i, v[u]);
+        store_vec<float4, PAST>(c.w + 4 * i, w[u]);
         if (c.w16 != nullptr) reinterpret_cast<Pack<bf16_t, 4> *>(c.w16)[i] = o;
     }
     if (t < (c.count & 3)) {
@@ -203,14 +203,53 @@ __device__ __forceinline__ float scale8(unsigned top_bits, float &inv)
     return top * (1.f / 448.f);
 }
 
-__device__ __forceinline__ unsigned wave_max(unsigned v)
+// One lane's four elements of a block of 256: the new states in m, root, the new weights in w.
+struct Four { float g[4], w[4]; unsigned m8, v8; };
+
+__device__ __forceinline__ void update_four(const AdamArgs &a, float s, float keep, float mscale, float vscale, Four &f, float (&m)[4], float (&root)[4])
 {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v = max(v, (unsigned)__shfl_xor((int)v, o, 64));
-    return v;
+    auto each = [&](int e, float m0, float r0) {
+        m[e] = m0 * mscale;
+        const float r = r0 * vscale;
+        float v = r * r;
+        adam_moments(a, f.g[e] * s, m[e], v);
+        root[e] = sqrtf(v);
+        f.w[e] = adam_weight(a, keep, f.w[e], m[e], root[e]);
+    };
+    each(0, __builtin_amdgcn_cvt_f32_fp8(f.m8, 0), __builtin_amdgcn_cvt_f32_fp8(f.v8, 0));
+    each(1, __builtin_amdgcn_cvt_f32_fp8(f.m8, 1), __builtin_amdgcn_cvt_f32_fp8(f.v8, 1));
+    each(2, __builtin_amdgcn_cvt_f32_fp8(f.m8, 2), __builtin_amdgcn_cvt_f32_fp8(f.v8, 2));
+    each(3, __builtin_amdgcn_cvt_f32_fp8(f.m8, 3), __builtin_amdgcn_cvt_f32_fp8(f.v8, 3));
 }
 
-// A wavefront works on 256 elements that share scales, four per lane; a block's four wavefronts on four times four of them.
+// The wavefront's 256 states as codes in f and the scales.  pair: number of the lane's first pair of elements in the list.
+__device__ __forceinline__ void store_four(const AdamArgs &a, unsigned long long pair, const float (&m)[4], const float (&root)[4], Four &f, float &mscale, float &vscale)
+{
+    unsigned mtop = 0, rtop = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        mtop = max(mtop, __float_as_uint(fabsf(m[e])));
+        rtop = max(rtop, __float_as_uint(fabsf(root[e])));
+    }
+    float minv, rinv;
+    mscale = scale8(wave_max_fast(mtop), minv);
+    vscale = scale8(wave_max_fast(rtop), rinv);
+    f.m8 = f.v8 = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const unsigned long long r = splitmix64(a.seed, pair + (e >> 1)) >> (32 * (e & 1));
+        unsigned code = encode8(fabsf(m[e]) * minv, (unsigned)r & 0xffffu);
+        if (m[e] < 0.f) code |= 0x80u;
+        f.m8 |= code << (8 * e);
+        // a positive sqrt(v) stays positive: as 0 it would let the next step's update grow
+        const float ra = root[e] * rinv;
+        code = encode8(ra, (unsigned)(r >> 16) & 0xffffu);
+        f.v8 |= (ra > 0.f ? max(code, 1u) : code) << (8 * e);
+    }
+}
+
+// A wavefront works on 256 elements that share scales, four per lane; a block's four wavefronts on four times four of them.  A whole chunk's
+// loads are issued together; a tensor's last chunk goes 256 elements at a time, with bounds.
 __global__ __launch_bounds__(256) void k_adamw8(const Chunk *__restrict__ table, AdamArgs a, const float *__restrict__ scale)
 {
     const Chunk c = table[blockIdx.x];
@@ -219,70 +258,67 @@ __global__ __launch_bounds__(256) void k_adamw8(const Chunk *__restrict__ table,
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float keep = fmaf(-a.lr, c.decay, 1.f);
     unsigned char *m8 = (unsigned char *)c.m, *v8 = (unsigned char *)c.v;
-    for (int b = wave; b * kBlock < c.count; b += 4) {
-        const int i = b * kBlock + lane * 4, left = min(max(c.count - i, 0), 4);
-        float ge[4] = {0.f, 0.f, 0.f, 0.f}, we[4] = {0.f, 0.f, 0.f, 0.f};
-        unsigned mc = 0, vc = 0;
-        if (left == 4) {
-            *reinterpret_cast<float4 *>(ge) = *reinterpret_cast<const float4 *>(c.g + i);
-            *reinterpret_cast<float4 *>(we) = *reinterpret_cast<const float4 *>(c.w + i);
-            mc = *reinterpret_cast<const unsigned *>(m8 + i);
-            vc = *reinterpret_cast<const unsigned *>(v8 + i);
-        } else {
-            for (int e = 0; e < left; ++e) {
-                ge[e] = c.g[i + e]; we[e] = c.w[i + e];
-                mc |= (unsigned)m8[i + e] << (8 * e); vc |= (unsigned)v8[i + e] << (8 * e);
-            }
-        }
-        const float msc = c.ms[b], vsc = c.vs[b];
-        float me[4] = {__builtin_amdgcn_cvt_f32_fp8(mc, 0), __builtin_amdgcn_cvt_f32_fp8(mc, 1), __builtin_amdgcn_cvt_f32_fp8(mc, 2), __builtin_amdgcn_cvt_f32_fp8(mc, 3)};
-        float re[4] = {__builtin_amdgcn_cvt_f32_fp8(vc, 0), __builtin_amdgcn_cvt_f32_fp8(vc, 1), __builtin_amdgcn_cvt_f32_fp8(vc, 2), __builtin_amdgcn_cvt_f32_fp8(vc, 3)};
-        unsigned mtop = 0, rtop = 0;
+    const unsigned long long first = (unsigned long long)blockIdx.x * kChunk;
+    if (c.count == kChunk) {
+        constexpr int U = kChunk / kBlock / 4;
+        Four f[U];
+        float ms[U], vs[U];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            me[e] *= msc;
-            const float root = re[e] * vsc;
-            float v = root * root;
-            adam_moments(a, ge[e] * s, me[e], v);
-            if (e >= left) { me[e] = 0.f; v = 0.f; }   // past the end, also with a scale that is NaN
-            re[e] = sqrtf(v);
-            we[e] = adam_weight(a, keep, we[e], me[e], re[e]);
-            mtop = max(mtop, __float_as_uint(fabsf(me[e])));
-            rtop = max(rtop, __float_as_uint(fabsf(re[e])));
+        for (int u = 0; u < U; ++u) {
+            const int b = wave + 4 * u, i = b * kBlock + lane * 4;
+            *reinterpret_cast<float4 *>(f[u].g) = *reinterpret_cast<const float4 *>(c.g + i);
+            *reinterpret_cast<float4 *>(f[u].w) = *reinterpret_cast<const float4 *>(c.w + i);
+            f[u].m8 = *reinterpret_cast<const unsigned *>(m8 + i);
+            f[u].v8 = *reinterpret_cast<const unsigned *>(v8 + i);
+            ms[u] = c.ms[b];
+            vs[u] = c.vs[b];
         }
-        float minv, rinv;
-        const float mscale = scale8(wave_max(mtop), minv), rscale = scale8(wave_max(rtop), rinv);
-        unsigned mo = 0, vo = 0;
-        const unsigned long long pair = ((unsigned long long)blockIdx.x * kChunk + (unsigned)i) >> 1;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const unsigned long long r = splitmix64(a.seed, pair + (e >> 1)) >> (32 * (e & 1));
-            unsigned code = encode8(fabsf(me[e]) * minv, (unsigned)r & 0xffffu);
-            if (me[e] < 0.f) code |= 0x80u;
-            mo |= code << (8 * e);
-            // a positive sqrt(v) stays positive: as 0 it would let the next step's update grow
-            const float ra = re[e] * rinv;
-            code = encode8(ra, (unsigned)(r >> 16) & 0xffffu);
-            vo |= (ra > 0.f ? max(code, 1u) : code) << (8 * e);
-        }
-        if (left == 4) {
-            *reinterpret_cast<float4 *>(c.w + i) = *reinterpret_cast<float4 *>(we);
-            *reinterpret_cast<unsigned *>(m8 + i) = mo;
-            *reinterpret_cast<unsigned *>(v8 + i) = vo;
+        for (int u = 0; u < U; ++u) {
+            const int b = wave + 4 * u, i = b * kBlock + lane * 4;
+            float m[4], root[4];
+            update_four(a, s, keep, ms[u], vs[u], f[u], m, root);
+            *reinterpret_cast<float4 *>(c.w + i) = *reinterpret_cast<float4 *>(f[u].w);
             if (c.w16 != nullptr) {
                 Pack<bf16_t, 4> o;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o.v[e] = from_f32<bf16_t>(we[e]);
+                for (int e = 0; e < 4; ++e) o.v[e] = from_f32<bf16_t>(f[u].w[e]);
                 *reinterpret_cast<Pack<bf16_t, 4> *>(c.w16 + i) = o;
             }
-        } else {
-            for (int e = 0; e < left; ++e) {
-                c.w[i + e] = we[e];
-                m8[i + e] = (unsigned char)(mo >> (8 * e)); v8[i + e] = (unsigned char)(vo >> (8 * e));
-                if (c.w16 != nullptr) c.w16[i + e] = from_f32<bf16_t>(we[e]);
-            }
+            float mscale, vscale;
+            store_four(a, (first + (unsigned)i) >> 1, m, root, f[u], mscale, vscale);
+            *reinterpret_cast<unsigned *>(m8 + i) = f[u].m8;
+            *reinterpret_cast<unsigned *>(v8 + i) = f[u].v8;
+            if (lane == 0) { c.ms[b] = mscale; c.vs[b] = vscale; }
         }
-        if (lane == 0) { c.ms[b] = mscale; c.vs[b] = rscale; }
+        return;
+    }
+    for (int b = wave; b * kBlock < c.count; b += 4) {
+        const int i = b * kBlock + lane * 4;
+        Four f = {};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (i + e < c.count) {
+                f.g[e] = c.g[i + e];
+                f.w[e] = c.w[i + e];
+                f.m8 |= (unsigned)m8[i + e] << (8 * e);
+                f.v8 |= (unsigned)v8[i + e] << (8 * e);
+            }
+        float m[4], root[4], mscale = c.ms[b], vscale = c.vs[b];
+        update_four(a, s, keep, mscale, vscale, f, m, root);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (i + e >= c.count) m[e] = root[e] = 0.f;   // also with a scale that is NaN
+        store_four(a, (first + (unsigned)i) >> 1, m, root, f, mscale, vscale);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (i + e < c.count) {
+                c.w[i + e] = f.w[e];
+                m8[i + e] = (unsigned char)(f.m8 >> (8 * e));
+                v8[i + e] = (unsigned char)(f.v8 >> (8 * e));
+                if (c.w16 != nullptr) c.w16[i + e] = from_f32<bf16_t>(f.w[e]);
+            }
+        if (lane == 0) { c.ms[b] = mscale; c.vs[b] = vscale; }
     }
 }
 
@@ -343,6 +379,10 @@ dp_status check_list(const dp_param_list *list)
     if ((reinterpret_cast<uintptr_t>(list->table) & 63u) != 0) { dp_set_error("parameter list: the table must be 64-byte aligned"); return DP_ERR_BAD_DESC; }
     return DP_OK;
 }
+
+// Gradients of more than half the memory-side cache are not in it any more, and keeping them there helps nobody: all accesses go past the
+// caches then (see the kernels' figures).
+bool past_caches(const dp_param_list *list) { return list->n_elements > (int64_t)32 << 20; }
 
 }  // namespace
 
@@ -430,7 +470,7 @@ extern "C" dp_status dp_grad_norm(const dp_param_list *list, float max_norm, flo
     if (ws == nullptr || ws_bytes < need) { dp_set_error("gradient norm needs %zu workspace bytes, got %zu", need, ws == nullptr ? (size_t)0 : ws_bytes); return DP_ERR_WORKSPACE; }
     hipStream_t st = (hipStream_t)hip_stream;
     const int blocks = norm_blocks(list->n_chunks);
-    hipLaunchKernelGGL(k_norm_partial, dim3(blocks), dim3(256), 0, st, (const Chunk *)list->table, (long long)list->n_chunks, (double *)ws);
+    hipLaunchKernelGGL(past_caches(list) ? k_norm_partial<true> : k_norm_partial<false>, dim3(blocks), dim3(256), 0, st, (const Chunk *)list->table, (long long)list->n_chunks, (double *)ws);
     hipLaunchKernelGGL(k_norm_final, dim3(1), dim3(256), 0, st, (const double *)ws, blocks, max_norm, norm_and_scale);
     return launched("gradient norm");
 }
@@ -456,6 +496,6 @@ extern "C" dp_status dp_adamw_step(const dp_param_list *list, const dp_adamw_hyp
     a.seed = h->seed;
     const dim3 grid((unsigned)list->n_chunks), block(256);
     if (list->state == DP_STATE_Q8) hipLaunchKernelGGL(k_adamw8, grid, block, 0, (hipStream_t)hip_stream, (const Chunk *)list->table, a, grad_scale);
-    else hipLaunchKernelGGL(k_adamw, grid, block, 0, (hipStream_t)hip_stream, (const Chunk *)list->table, a, grad_scale);
+    else hipLaunchKernelGGL(past_caches(list) ? k_adamw<true> : k_adamw<false>, grid, block, 0, (hipStream_t)hip_stream, (const Chunk *)list->table, a, grad_scale);
     return launched("AdamW step");
 }

@@ -65,6 +65,18 @@ template <typename F> __device__ __forceinline__ float wave_reduce(float v, floa
 __device__ __forceinline__ float wave_sum_fast(float v) { return wave_reduce(v, 0.f, [](float a, float b) { return a + b; }); }
 __device__ __forceinline__ float wave_max_fast(float v) { return wave_reduce(v, -3.402823466e38f, [](float a, float b) { return fmaxf(a, b); }); }
 
+__device__ __forceinline__ unsigned wave_max_fast(unsigned v)
+{
+    auto up = [&](auto step) { v = max(v, (unsigned)step((int)v)); };
+    up([](int x) { return __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false); });
+    up([](int x) { return __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false); });
+    up([](int x) { return __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false); });
+    up([](int x) { return __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false); });
+    up([](int x) { return __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false); });
+    up([](int x) { return __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false); });
+    return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
+}
+
 // Sums over the lanes whose number agrees modulo `period` (a power of two up to 64), in every lane: rotations within rows of 16 lanes, longest
 // first, so that each meets the sums that it lacks; then two exchanges across rows.
 template <int CTRL, int N> __device__ __forceinline__ void add_moved(float (&v)[N])
