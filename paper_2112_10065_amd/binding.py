@@ -261,29 +261,30 @@ def param_list(params, state=DP_STATE_F32, device=None):
     torch.float8_e4m3fn, and `m_scale`, `v_scale`), optionally `w_bf16` and `weight_decay`.  The table is copied before this returns."""
     n = len(params)
     arr = (dp_param * max(1, n))()
-    byte_types = [t for t in (torch.uint8, torch.int8, getattr(torch, "float8_e4m3fn", None)) if t is not None]
-    state_types = byte_types if state == DP_STATE_Q8 else [torch.float32]
+    states = (torch.uint8, torch.int8, getattr(torch, "float8_e4m3fn", torch.uint8)) if state == DP_STATE_Q8 else (torch.float32,)
+    kinds = {"grad": (torch.float32,), "w32": (torch.float32,), "w_bf16": (torch.bfloat16,), "m": states, "v": states, "m_scale": (torch.float32,),
+             "v_scale": (torch.float32,)}
     tensors = []
     for i, p in enumerate(params):
-        unknown = set(p) - {"grad", "w32", "w_bf16", "m", "v", "m_scale", "v_scale", "weight_decay"}
-        if unknown:
-            raise ValueError(f"parameter {i}: unknown entries {sorted(unknown)}")
-        count = p["grad"].numel()
-        blocks = (count + 255) // 256
-        arr[i].count, arr[i].weight_decay = count, float(p.get("weight_decay", 0.0))
-        for name, size, types in (("grad", count, [torch.float32]), ("w32", count, [torch.float32]), ("w_bf16", count, [torch.bfloat16]),
-                                  ("m", count, state_types), ("v", count, state_types), ("m_scale", blocks, [torch.float32]),
-                                  ("v_scale", blocks, [torch.float32])):
-            t = p.get(name)
+        grad = p["grad"]
+        count, where, out = grad.numel(), grad.device, arr[i]
+        out.count = count
+        for name, t in p.items():
             if t is None:
                 continue
-            if t.numel() != size or t.dtype not in types or not t.is_contiguous():
-                raise ValueError(f"parameter {i}: {name} must be a contiguous tensor of {size} elements of {' or '.join(map(str, types))}")
-            if t.device != p["grad"].device:
+            if name == "weight_decay":
+                out.weight_decay = t
+                continue
+            if name not in kinds:
+                raise ValueError(f"parameter {i}: unknown entry {name}")
+            size = (count + 255) // 256 if name.endswith("scale") else count
+            if t.numel() != size or t.dtype not in kinds[name] or not t.is_contiguous():
+                raise ValueError(f"parameter {i}: {name} must be a contiguous tensor of {size} elements of {' or '.join(map(str, kinds[name]))}")
+            if t.device != where:
                 raise ValueError(f"parameter {i}: {name} is on another device than grad")
-            setattr(arr[i], name, t.data_ptr())
+            setattr(out, name, t.data_ptr())
             tensors.append(t)
-        device = device if device is not None else p["grad"].device
+        device = where if device is None else device
     nbytes = int(lib.dp_param_table_bytes(arr, n))
     host = torch.zeros(max(nbytes, 64), dtype=torch.uint8)
     table = torch.zeros(max(nbytes, 64), dtype=torch.uint8, device=device if device is not None else "cpu")
