@@ -51,13 +51,17 @@ template <bool PAST> __device__ __forceinline__ double square_sum(const Chunk &c
     return s;
 }
 
-// thread 0 of 256 gets the block's sum: wavefronts by shuffles, their sums in order
-__device__ __forceinline__ double block_sum(double s, double *sm)
+// the block's sum: wavefronts by shuffles, their sums in order
+template <int N> __device__ __forceinline__ double block_sum(double s)
 {
+    __shared__ double sm[N / 64];
     s = wave_sum(s);
     if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = s;
     __syncthreads();
-    return sm[0] + sm[1] + sm[2] + sm[3];
+    s = 0.0;
+#pragma unroll
+    for (int w = 0; w < N / 64; ++w) s += sm[w];
+    return s;
 }
 
 __device__ __forceinline__ void write_norm(double sum, float max_norm, float *out)
@@ -70,19 +74,27 @@ __device__ __forceinline__ void write_norm(double sum, float max_norm, float *ou
 
 template <bool PAST> __global__ __launch_bounds__(256) void k_norm_partial(const Chunk *__restrict__ table, long long n_chunks, double *__restrict__ partial)
 {
-    __shared__ double sm[4];
     double s = 0.0;
     for (long long i = blockIdx.x; i < n_chunks; i += gridDim.x) s += square_sum<PAST>(table[i], threadIdx.x);
-    s = block_sum(s, sm);
+    s = block_sum<256>(s);
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
 __global__ __launch_bounds__(256) void k_norm_final(const double *__restrict__ partial, int n, float max_norm, float *__restrict__ out)
 {
-    __shared__ double sm[4];
     double s = 0.0;
     for (int i = threadIdx.x; i < n; i += 256) s += partial[i];
-    s = block_sum(s, sm);
+    s = block_sum<256>(s);
+    if (threadIdx.x == 0) write_norm(s, max_norm, out);
+}
+
+// A short list in one block, a chunk to every four wavefronts: no second kernel to wait for (8 chunks 6.0 -> 3.3 us, 24: 6.1 -> 5.2; 32: 6.2 by both).
+constexpr int kNormShort = 24;
+__global__ __launch_bounds__(1024) void k_norm_short(const Chunk *__restrict__ table, int n_chunks, float max_norm, float *__restrict__ out)
+{
+    double s = 0.0;
+    for (int i = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8); i < n_chunks; i += 4) s += square_sum<false>(table[i], threadIdx.x & 255);
+    s = block_sum<1024>(s);
     if (threadIdx.x == 0) write_norm(s, max_norm, out);
 }
 
@@ -469,6 +481,10 @@ extern "C" dp_status dp_grad_norm(const dp_param_list *list, float max_norm, flo
     const size_t need = dp_grad_norm_workspace_bytes(list);
     if (ws == nullptr || ws_bytes < need) { dp_set_error("gradient norm needs %zu workspace bytes, got %zu", need, ws == nullptr ? (size_t)0 : ws_bytes); return DP_ERR_WORKSPACE; }
     hipStream_t st = (hipStream_t)hip_stream;
+    if (list->n_chunks <= kNormShort) {
+        hipLaunchKernelGGL(k_norm_short, dim3(1), dim3(1024), 0, st, (const Chunk *)list->table, (int)list->n_chunks, max_norm, norm_and_scale);
+        return launched("gradient norm");
+    }
     const int blocks = norm_blocks(list->n_chunks);
     hipLaunchKernelGGL(past_caches(list) ? k_norm_partial<true> : k_norm_partial<false>, dim3(blocks), dim3(256), 0, st, (const Chunk *)list->table, (long long)list->n_chunks, (double *)ws);
     hipLaunchKernelGGL(k_norm_final, dim3(1), dim3(256), 0, st, (const double *)ws, blocks, max_norm, norm_and_scale);
