@@ -670,8 +670,12 @@ bool slabs_for(int V, GnArgs &a)
     return true;
 }
 
-// Vectors where they fit, single channels else.  Splits: about four blocks per compute unit, at least eight pixels per thread,
-// and few enough that a block of the second kernel reads at most 2048 partials (16 KB, from L2).
+// Vectors where they fit, single channels else.  Splits: about four blocks per compute unit, at least eight pixels per thread, and few enough
+// that a block of the second kernel reads at most 2048 partials: 16 KB that come from other dies (4096: 4 x 224 x 224 x 64 forward 23 -> 27 us),
+// 4096 where a sample is 16 MB or more and the first kernel's blocks are too long otherwise (2 x 400 x 400 x 64 backward 75 -> 61 us).
+// The second kernel has half as many blocks for tensors up to 64 MB (4 x 224 x 224 x 64 backward 43.5 -> 38.8 us; 16 x: 118.5 -> 122).
+// Past the caches: outputs above 32 MB, which would be written back while the next kernel reads (32 x 224 x 224 x 64 forward 133 -> 113 us;
+// 25 MB: no difference), and the second reading of inputs above 150 MB, which have left the memory-side cache (113 -> 105; 103 MB: 50.7 -> 53.4).
 int shape(const dp_group_norm_desc &d, bool bwd, GnArgs &a)
 {
     a.n = d.n; a.hw = d.h * d.w; a.c = d.c; a.groups = d.groups; a.cg = d.c / d.groups;
@@ -695,8 +699,13 @@ int shape(const dp_group_norm_desc &d, bool bwd, GnArgs &a)
     return V;
 }
 
-// The one-kernel form: wavefronts to a unit (0: the image does not fit), vectors to a lane.  Only for groups that are a power of two of whole
-// vectors or divide one.
+// The one-kernel form: wavefronts to a unit (0: two kernels), vectors to a lane, groups of a unit.  Only for groups that are a power of
+// two of whole vectors or divide one.  Measured in both forms (bf16, us, two kernels / one):
+//   up to 8 vectors a lane      8 x 28 x 28 x 512 forward 13.3 / 6.3, backward 16.9 / 13.0; 1 x 14 x 14 x 512 11.1 / 3.8, 11.5 / 5.1
+//   1024 units and more: a wavefront each (32 x 14 x 14 x 1024 forward 17 / 8.3); fewer: four (1 x 14 x 14 x 512 forward 4.9 -> 3.8)
+//   backward of 1024 units of four wavefronts: the pieces of a unit are a fraction of a cache line, and the L2s lose the rest of it
+//     (32 x 28 x 28 x 256, 16-byte pieces 21 / 23; x 512, 32-byte pieces 33.6 / 27.8, with the saved output 39 / 43)
+//   9 to 16 vectors, forward only (backward has two tensors to hold): 8 x 56 x 56 x 256 17.1 / 13.6, but 32 x 56 x 56 x 256 33 / 48
 struct UnitForm { int waves, vectors, groups; };
 UnitForm unit_form(const GnArgs &a, int V, bool bwd, bool mask)
 {
@@ -706,8 +715,8 @@ UnitForm unit_form(const GnArgs &a, int V, bool bwd, bool mask)
     if (a.cg % V == 0) cvs = a.cg / V;
     else if (V % a.cg == 0) f.groups = V / a.cg;
     else return f;
-    if ((cvs & (cvs - 1)) != 0 || cvs > 64) return f;
     const int64_t units = (int64_t)a.n * (a.c / std::max(a.cg, V));
+    if ((cvs & (cvs - 1)) != 0 || cvs > 64 || units > (1 << 23)) return f;   // a grid has fewer than 2^32 threads
     const int w1 = ceil_div(a.hw, 64 / cvs), w4 = ceil_div(a.hw, 256 / cvs);
     if (w1 <= 8 && units >= 1024) { f.waves = 1; f.vectors = 8; }
     else if (w4 <= 8 && (!bwd || units < 1024 || (cvs > 1 && !mask))) { f.waves = 4; f.vectors = 8; }

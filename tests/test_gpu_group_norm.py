@@ -257,3 +257,35 @@ def test_full_size(env):
     assert bool(((dbeta - g.sum(dim=(0, 1, 2))).abs() <= 4e-6 * g.abs().sum(dim=(0, 1, 2))).all())
     gx = g * xh.view(n, h, w, c)
     assert bool(((dgamma - gx.sum(dim=(0, 1, 2))).abs() <= 4e-6 * (g.abs() + gx.abs()).sum(dim=(0, 1, 2))).all())
+
+
+def test_very_many_samples(env):
+    """4 million samples of one pixel: more groups than a grid has teams, offsets beyond 2^31 bytes; some samples against the oracle."""
+    dp, U, O, synth = env
+    n, c, groups = 1 << 22, 256, 32
+    gen = torch.Generator(U.DEV).manual_seed(4)
+    x = torch.randn((n, 1, 1, c), device=U.DEV, generator=gen, dtype=torch.bfloat16)
+    y = torch.empty_like(x)
+    desc = dp.group_norm_desc(n, 1, 1, c, groups, dp.DP_BF16, 0, EPS)
+    ws = U.workspace(dp.dp_group_norm_workspace_bytes(desc, 0))
+    mean, rstd = (torch.empty((n, groups), device=U.DEV) for _ in range(2))
+    dp.dp_group_norm_fwd(desc, x, None, None, y, mean, rstd, ws)
+    pick = torch.tensor([0, 1, 12345, (1 << 21) + 7, n - 2, n - 1], device=U.DEV)
+    want, wm, wr = O.group_norm_fwd(U.to_np(x[pick]), np.ones(c), np.zeros(c), groups, EPS)
+    assert np.abs(U.to_np(mean[pick]) - wm).max() <= 1e-5 and np.abs(U.to_np(rstd[pick]) / wr - 1).max() <= 1e-5
+    assert np.all(np.abs(U.to_np(y[pick]) - want) <= 2.0 ** -8 * np.abs(want) + 1e-4)
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("act", ["relu", "silu"])
+@pytest.mark.parametrize("shape", [(1, 16, 16, 128, 16), (1, 16, 17, 128, 16), (40, 8, 8, 256, 32), (40, 8, 9, 256, 32), (2, 46, 45, 16, 2), (2, 64, 64, 16, 2),
+                                   (2, 64, 65, 16, 2), (1, 3, 5, 1024, 2), (1, 2, 2, 2048, 2), (1, 11, 3, 1024, 4), (33, 45, 46, 256, 32), (2, 7, 7, 32, 8),
+                                   (3, 23, 9, 48, 24), (130, 4, 4, 64, 8)], ids=lambda s: "x".join(map(str, s)))
+def test_at_the_edges_of_the_forms(env, shape, act, bf16):
+    """Images that just fit a wavefront's or a team's registers, and just do not; groups of a fraction of a vector up to 64 vectors."""
+    k = Case(env, shape, act, bf16, scale=1.5, offset=0.5)
+    y, mean, rstd = k.forward()
+    k.check_forward(y, mean, rstd)
+    got = k.backward(y, mean, rstd)
+    torch.cuda.synchronize()
+    k.check_backward(got, y if act == "relu" else None, mean, rstd)
