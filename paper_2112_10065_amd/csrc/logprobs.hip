@@ -582,14 +582,22 @@ __global__ __launch_bounds__(NT) void k_logprobs_grad(LpGradArgs a)
     }
 }
 
-// Splits of a row: about four blocks per compute unit, at least 2048 classes each.  Whole vectors, so that all splits of a row
-// are aligned alike.
-void split_rows(int rows, int classes, int &splits, int &seg)
+// Splits of a row, in whole vectors, so that all splits of a row are aligned alike: about four blocks per compute unit, at least `least`
+// classes each.
+void split_rows(int rows, int classes, int least, int &splits, int &seg)
 {
-    int s = std::min({(1024 + rows - 1) / rows, (classes + 2047) / 2048, kMaxSplits});
-    s = std::max(s, 1);
+    const int s = std::max(1, std::min({(1024 + rows - 1) / rows, (classes + least - 1) / least, kMaxSplits}));
     seg = ((classes + s - 1) / s + 7) / 8 * 8;
     splits = (classes + seg - 1) / seg;
+}
+// Forward, splits cost a second kernel and its wait: one block to a row where there are rows for every compute unit, and for rows that a block
+// reads in the time of that (bf16, five alternatives, us, split / not: 1 x 16384 8.5 / 6.5, 1 x 32000 8.7 / 8.8; 300 x 48000 16.2 / 15.5,
+// 256 x 131072 21.0 / 22.3; 512 x 131072 34 / 32.4).
+void split_forward(int rows, int classes, int &splits, int &seg)
+{
+    splits = 1;
+    seg = classes;
+    if (rows < 512 && classes > (rows >= 256 ? 65536 : 24576)) split_rows(rows, classes, 4096, splits, seg);
 }
 
 long long stride_of(const dp_logprobs_desc &d) { return d.row_stride != 0 ? (long long)d.row_stride : d.classes; }
@@ -629,7 +637,7 @@ extern "C" size_t dp_logprobs_workspace_bytes(const dp_logprobs_desc *desc)
 {
     if (check_desc(desc) != DP_OK || desc->rows == 0) return 0;
     int splits, seg;
-    split_rows(desc->rows, desc->classes, splits, seg);
+    split_forward(desc->rows, desc->classes, splits, seg);
     return part_bytes(desc->rows, splits, desc->top_k);
 }
 
@@ -647,7 +655,7 @@ extern "C" dp_status dp_logprobs_fwd(const dp_logprobs_desc *desc, const void *z
     for (const void *p : {(const void *)ids, (const void *)logp, (const void *)entropy, (const void *)lse, (const void *)top_logp, (const void *)top_ids})
         if (misaligned(p, 4)) { dp_set_error("log-probabilities: pointers must be 4-byte aligned"); return DP_ERR_BAD_DESC; }
     LpArgs a = {z, ids, logp, entropy, lse, top_logp, top_ids, nullptr, nullptr, d.rows, d.classes, d.top_k, 1, d.classes, stride_of(d)};
-    split_rows(d.rows, d.classes, a.splits, a.seg);
+    split_forward(d.rows, d.classes, a.splits, a.seg);
     const size_t need = part_bytes(d.rows, a.splits, d.top_k);
     if (need > 0 && (ws == nullptr || ws_bytes < need)) {
         dp_set_error("log-probabilities need %zu workspace bytes, got %zu", need, ws == nullptr ? (size_t)0 : ws_bytes);
@@ -687,7 +695,7 @@ extern "C" dp_status dp_logprobs_bwd(const dp_logprobs_desc *desc, const void *z
     for (const void *p : {(const void *)ids, (const void *)lse, (const void *)entropy, (const void *)dlogp, (const void *)dentropy})
         if (misaligned(p, 4)) { dp_set_error("log-probabilities' gradient: pointers must be 4-byte aligned"); return DP_ERR_BAD_DESC; }
     LpGradArgs a = {z, ids, lse, entropy, dlogp, dentropy, dz, d.rows, d.classes, 1, d.classes, stride_of(d)};
-    if (dz != z) split_rows(d.rows, d.classes, a.splits, a.seg);
+    if (dz != z) split_rows(d.rows, d.classes, 2048, a.splits, a.seg);   // 256 x 48000: 9.5 us, one block to a row 11.9
     const bool bf = d.io_dtype == DP_BF16, past = (int64_t)d.rows * d.classes * (bf ? 2 : 4) > (32 << 20);
     auto *kernel = bf ? (past ? k_logprobs_grad<bf16_t, true> : k_logprobs_grad<bf16_t, false>) : (past ? k_logprobs_grad<float, true> : k_logprobs_grad<float, false>);
     hipLaunchKernelGGL(kernel, dim3((unsigned)d.rows * a.splits), dim3(NT), 0, (hipStream_t)hip_stream, a);

@@ -84,7 +84,7 @@ class Run:
 
 
 SHAPES = [(1, 1, 1), (1, 2, 2), (3, 10, 10), (5, 63, 5), (4, 64, 64), (32, 1000, 5), (7, 255, 64), (3, 257, 1), (2, 1025, 20), (2, 4099, 64), (33, 333, 0),
-          (1, 50001, 20), (2, 131072, 64), (1, 20000, 0), (300, 17, 3), (9, 8192, 8), (3, 30011, 64)]
+          (1, 50001, 20), (2, 131072, 64), (1, 20000, 0), (1, 600001, 64), (2, 24577, 33), (260, 30000, 2), (300, 17, 3), (9, 8192, 8), (3, 30011, 64)]
 
 
 @pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
