@@ -550,7 +550,7 @@ __global__ __launch_bounds__(NT) void k_logprobs_grad(LpGradArgs a)
     const int at = valid ? id - c0 : -1;                   // the given class in this run, if in [0, n)
     auto grad = [&](float z) {
         const float d = z - shift;
-        return exp_d(d) * fmaf(-k1, fmaxf(d, -3e38f), k0);
+        return exp_d(d) * fmaf(-k1, fmaxf(d, -128.f), k0);   // exp(d) is 0 long before -128; k1 d must not be infinite then
     };
     auto single = [&](int i) { out[i] = from_f32<T>(grad(as_f32(run.z[i])) + (i == at ? dl : 0.f)); };
     auto vector = [&](int v, const Pack<T, V> &q) {

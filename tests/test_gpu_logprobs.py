@@ -294,6 +294,34 @@ def test_gradient_of_large_scores(env, classes, bf16):
         assert np.all(np.abs(dz - want) <= tol)
 
 
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("classes", [12, 1000, 40000])
+def test_gradient_of_ruled_out_classes_by_large_factors(env, classes, bf16):
+    """Classes of probability 0 have gradient 0 whatever dentropy is: their log p is -inf or as large as the type's range."""
+    low = np.float32(-3.3895314e38)
+    z = scores(env[3], "factors", 6, classes, bf16)
+    z[0, 1::2] = -np.inf
+    z[1, 1::2] = low
+    z[2, 1::2] = -3e38 if not bf16 else low
+    z[3, ::3] = -np.inf
+    z[3, 1::3] = low
+    z[4, 1:] = -np.inf
+    z[5, 1::2] = -1e30
+    z = env[3].round_bf16(z) if bf16 else z
+    k = Run(env, z, [0, 1, 2, 3, 0, 4], 0, bf16)
+    out = k.forward()
+    for factor in (2.0, -8.0, 1000.0):
+        dlogp, dent = np.full(6, 0.5 * factor, np.float32), np.full(6, factor, np.float32)
+        want = k.O.logprobs_bwd(z, k.ids, dlogp.astype(np.float64), dent.astype(np.float64))
+        dz = k.backward(dlogp, dent, out[2], out[1])[1][:, :classes].float().cpu().numpy()
+        ruled_out = z < -1e29
+        gone = ruled_out & (np.arange(classes)[None, :] != k.ids[:, None])
+        assert np.all(dz[gone] == 0)
+        m = np.where(ruled_out, 0, np.abs(z)).max(axis=1, keepdims=True)   # exponents of the classes that count
+        tol = (2e-5 + 4e-7 * m) * abs(factor) * (0.5 + 2 + np.log(classes)) + (2.0 ** -8 * np.abs(want) if bf16 else 0)
+        assert np.all(np.abs(dz - want) <= tol)
+
+
 def test_gradient_at_another_alignment(env):
     """dz need not be aligned as z is."""
     dp = env[0]
