@@ -337,7 +337,7 @@ size_t dp_grad_norm_workspace_bytes(const dp_param_list *list);
 dp_status dp_grad_norm(const dp_param_list *list, float max_norm, float *norm_and_scale, void *ws, size_t ws_bytes, void *hip_stream);
 
 typedef struct {
-    double lr, beta1, beta2, eps; /* betas in [0, 1), eps > 0 */
+    double lr, beta1, beta2, eps; /* betas in [0, 1), eps >= 2^-126 */
     int64_t step;                 /* of this update, counted from 1 */
     uint64_t seed;                /* DP_STATE_Q8: of the random rounding; another one for every step */
 } dp_adamw_hyper;

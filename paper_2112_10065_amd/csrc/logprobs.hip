@@ -189,7 +189,7 @@ template <typename T, typename P>
 __device__ __forceinline__ void block_top(const Run<T> &run, int base, int k, unsigned top, bool odd, P &&put)
 {
     constexpr int V = Run<T>::V;
-    __shared__ unsigned tops[NT];
+    __shared__ alignas(16) unsigned tops[NT];   // read by fours
     __shared__ unsigned long long list[kCandidates + 8];
     __shared__ unsigned short leaders[NT];
     __shared__ int count, ties, lead, some_odd;

@@ -7,6 +7,7 @@
 // would be two or more loads that depend on each other) and works on one chunk.
 #include "vec_common.h"
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <vector>
 
@@ -498,8 +499,8 @@ extern "C" dp_status dp_adamw_step(const dp_param_list *list, const dp_adamw_hyp
     if (h == nullptr) { dp_set_error("AdamW: hyper-parameters are NULL"); return DP_ERR_NULL; }
     if (!list->updates && list->n_chunks > 0) { dp_set_error("AdamW: the list has gradients only"); return DP_ERR_NULL; }
     if (!(h->beta1 >= 0.0 && h->beta1 < 1.0 && h->beta2 >= 0.0 && h->beta2 < 1.0)) { dp_set_error("AdamW: beta1 and beta2 must be in [0, 1)"); return DP_ERR_BAD_DESC; }
-    // without eps in fp32 an element that never had a gradient would become 0 / 0
-    if (!std::isfinite((float)h->lr) || !((float)h->eps > 0.f) || !std::isfinite((float)h->eps)) { dp_set_error("AdamW: lr must be finite in fp32, eps finite and positive"); return DP_ERR_BAD_DESC; }
+    // without eps an element that never had a gradient would become 0 / 0, and the reciprocal of a subnormal one is infinite
+    if (!std::isfinite((float)h->lr) || !((float)h->eps >= FLT_MIN) || !std::isfinite((float)h->eps)) { dp_set_error("AdamW: lr must be finite in fp32, eps finite and at least 2^-126"); return DP_ERR_BAD_DESC; }
     if (h->step < 1) { dp_set_error("AdamW: steps count from 1"); return DP_ERR_BAD_DESC; }
     if ((reinterpret_cast<uintptr_t>(grad_scale) & 3u) != 0) { dp_set_error("AdamW: grad_scale must be 4-byte aligned"); return DP_ERR_BAD_DESC; }
     if (list->n_chunks == 0) return DP_OK;

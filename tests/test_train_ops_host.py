@@ -161,6 +161,13 @@ def test_norm_and_adamw_refusals(dp):
     assert adam(l=grads) == dp.DP_ERR_NULL
 
 
+def test_adamw_refuses_subnormal_eps(dp):
+    """Its reciprocal is infinite in fp32: an element that never had a gradient would become 0 * inf."""
+    lst = build(dp, [])[1]   # an empty list: what is not refused launches nothing
+    for eps, want in ((1e-39, dp.DP_ERR_BAD_DESC), (2.0 ** -126, dp.DP_OK), (1e-8, dp.DP_OK)):
+        assert dp.lib.dp_adamw_step(C.byref(lst), C.byref(dp.adamw_hyper(lr=1e-3, eps=eps)), None, None) == want
+
+
 def test_param_list_checks_tensors(dp):
     import torch
     g = torch.zeros(1000)
