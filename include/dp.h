@@ -324,8 +324,8 @@ typedef struct {
 /* Bytes of the table of these parameters; 0 if there are no elements or a count is out of range. */
 size_t dp_param_table_bytes(const dp_param *params, int32_t n_params);
 
-/* Host only.  Checks the parameters (pointers 16-byte aligned; no two may share memory that a step writes) and writes the table's
- * contents to host_table; the caller copies them to device_table (device address, 64-byte aligned, as many bytes) before the first
+/* Host only.  Checks the parameters (pointers 16-byte aligned; memory that a step writes may be named once; gradients may be shared)
+ * and writes the table's contents to host_table; the caller copies them to device_table (device address, 64-byte aligned, as many bytes) before the first
  * call that uses *list, and keeps that memory and all tensors while it is in use.  Where every member but count, grad and
  * weight_decay is NULL the list serves dp_grad_norm only. */
 dp_status dp_param_table_build(const dp_param *params, int32_t n_params, int32_t state, void *host_table, size_t host_table_bytes,

@@ -161,6 +161,19 @@ def test_norm_and_adamw_refusals(dp):
     assert adam(l=grads) == dp.DP_ERR_NULL
 
 
+def test_gradients_in_memory_that_a_step_writes(dp):
+    """Another block may have written there before the gradient is read."""
+    for state in (0, 1):
+        assert build(dp, [param(dp), param(dp, 8, 0x9000000, grad=0x110000 + 3984)], state)[0] == dp.DP_ERR_BAD_DESC   # inside the first's w32
+        assert b"share" in dp.lib.dp_last_error()
+        assert build(dp, [param(dp, grad=0x110000)], state)[0] == dp.DP_ERR_BAD_DESC
+        # the written memory begins inside a gradient, behind another gradient that ends before it
+        assert build(dp, [param(dp, 4096, 0x4000000), param(dp, 4, 0x5000000, grad=0x4000000), param(dp, 4, 0x6000000, v=0x4000000 + 16368)], state)[0] == dp.DP_ERR_BAD_DESC
+        assert build(dp, [param(dp, 4096, 0x4000000), param(dp, 4, 0x5000000, grad=0x4000000), param(dp, 4, 0x6000000, v=0x4000000 + 16384)], state)[0] == dp.DP_OK
+    only = dict(w32=None, w_bf16=None, m=None, v=None, m_scale=None, v_scale=None)
+    assert build(dp, [param(dp, **only), param(dp, **only)])[0] == dp.DP_OK
+
+
 def test_adamw_refuses_subnormal_eps(dp):
     """Its reciprocal is infinite in fp32: an element that never had a gradient would become 0 * inf."""
     lst = build(dp, [])[1]   # an empty list: what is not refused launches nothing
