@@ -73,8 +73,8 @@ __device__ __forceinline__ void write_norm(double sum, float max_norm, float *ou
     out[1] = !(norm <= 1.7e308) ? 0.f : norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.f;
 }
 
-// Bound by reading: 138 M elements 81 us (6.8 TB/s), through the caches 101; 25.5 M in 0.3 TB/s less.  A block takes every gridDim-th chunk, whose four
-// vectors per thread are read before the first is used.
+// Bound by reading: 138 M elements 81 us (6.8 TB/s; through the caches 101), 25.5 M in HBM 20.6 (5.0).  A block takes every gridDim-th chunk; a chunk's
+// four vectors per thread are on their way together.
 template <bool PAST> __global__ __launch_bounds__(256) void k_norm_partial(const Chunk *__restrict__ table, long long n_chunks, double *__restrict__ partial)
 {
     double s = 0.0;
@@ -133,7 +133,9 @@ __device__ __forceinline__ float adam_weight(const AdamArgs &a, float keep, floa
     return fmaf(-a.step_size * m, __builtin_amdgcn_rcpf(fmaf(root, a.inv_root_bc2, a.eps)), keep * w);   // one unit in the last place of the update
 }
 
-template <bool PAST> __global__ __launch_bounds__(256) void k_adamw(const Chunk *__restrict__ table, AdamArgs a, const float *__restrict__ scale)
+// Bound by HBM, 30 bytes per element with the bf16 copy (28 without): 138 M elements 726 us (5.7 TB/s), 25.5 M 140 (5.5; through the caches 147).  All sixteen vectors of a
+// thread are read before the first is used.  PAST: 1: weights and states go past the caches, 2: gradients too.
+template <int PAST> __global__ __launch_bounds__(256) void k_adamw(const Chunk *__restrict__ table, AdamArgs a, const float *__restrict__ scale)
 {
     const Chunk c = table[blockIdx.x];
     float s;
@@ -147,10 +149,10 @@ template <bool PAST> __global__ __launch_bounds__(256) void k_adamw(const Chunk 
     for (int u = 0; u < U; ++u) {
         const int i = u * 256 + t;
         if (i < nvec) {
-            g[u] = load_vec<float4, PAST>(c.g + 4 * i);
-            m[u] = load_vec<float4, PAST>(m32 + 4 * i);
-            v[u] = load_vec<float4, PAST>(v32 + 4 * i);
-            w[u] = load_vec<float4, PAST>(c.w + 4 * i);
+            g[u] = load_vec<float4, PAST == 2>(c.g + 4 * i);
+            m[u] = load_vec<float4, PAST != 0>(m32 + 4 * i);
+            v[u] = load_vec<float4, PAST != 0>(v32 + 4 * i);
+            w[u] = load_vec<float4, PAST != 0>(c.w + 4 * i);
         }
     }
 #pragma unroll
@@ -166,9 +168,9 @@ template <bool PAST> __global__ __launch_bounds__(256) void k_adamw(const Chunk 
             we[e] = adam_weight(a, keep, we[e], me[e], sqrtf(ve[e]));
             o.v[e] = from_f32<bf16_t>(we[e]);
         }
-        store_vec<float4, PAST>(m32 + 4 * i, m[u]);
-        store_vec<float4, PAST>(v32 + 4 * i, v[u]);
-        store_vec<float4, PAST>(c.w + 4 * i, w[u]);
+        store_vec<float4, PAST != 0>(m32 + 4 * i, m[u]);
+        store_vec<float4, PAST != 0>(v32 + 4 * i, v[u]);
+        store_vec<float4, PAST != 0>(c.w + 4 * i, w[u]);
         if (c.w16 != nullptr) reinterpret_cast<Pack<bf16_t, 4> *>(c.w16)[i] = o;
     }
     if (t < (c.count & 3)) {
@@ -264,8 +266,9 @@ __device__ __forceinline__ void store_four(const AdamArgs &a, unsigned long long
 }
 
 // A wavefront works on 256 elements that share scales, four per lane; a block's four wavefronts on four times four of them.  A whole chunk's
-// loads are issued together; a tensor's last chunk goes 256 elements at a time, with bounds.
-__global__ __launch_bounds__(256) void k_adamw8(const Chunk *__restrict__ table, AdamArgs a, const float *__restrict__ scale)
+// loads are issued together; a tensor's last chunk goes 256 elements at a time, with bounds.  18 bytes and 97 vector instructions per element: bound by HBM
+// (25.5 M elements 83 us, 5.5 TB/s; through the caches 90) with the vector units busy for two thirds of that; PAST as above.
+template <int PAST> __global__ __launch_bounds__(256) void k_adamw8(const Chunk *__restrict__ table, AdamArgs a, const float *__restrict__ scale)
 {
     const Chunk c = table[blockIdx.x];
     float s;
@@ -281,10 +284,10 @@ __global__ __launch_bounds__(256) void k_adamw8(const Chunk *__restrict__ table,
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int b = wave + 4 * u, i = b * kBlock + lane * 4;
-            *reinterpret_cast<float4 *>(f[u].g) = *reinterpret_cast<const float4 *>(c.g + i);
-            *reinterpret_cast<float4 *>(f[u].w) = *reinterpret_cast<const float4 *>(c.w + i);
-            f[u].m8 = *reinterpret_cast<const unsigned *>(m8 + i);
-            f[u].v8 = *reinterpret_cast<const unsigned *>(v8 + i);
+            *reinterpret_cast<float4 *>(f[u].g) = load_vec<float4, PAST == 2>(c.g + i);
+            *reinterpret_cast<float4 *>(f[u].w) = load_vec<float4, PAST != 0>(c.w + i);
+            f[u].m8 = load_vec<unsigned, PAST != 0>(m8 + i);
+            f[u].v8 = load_vec<unsigned, PAST != 0>(v8 + i);
             ms[u] = c.ms[b];
             vs[u] = c.vs[b];
         }
@@ -293,7 +296,7 @@ __global__ __launch_bounds__(256) void k_adamw8(const Chunk *__restrict__ table,
             const int b = wave + 4 * u, i = b * kBlock + lane * 4;
             float m[4], root[4];
             update_four(a, s, keep, ms[u], vs[u], f[u], m, root);
-            *reinterpret_cast<float4 *>(c.w + i) = *reinterpret_cast<float4 *>(f[u].w);
+            store_vec<float4, PAST != 0>(c.w + i, *reinterpret_cast<float4 *>(f[u].w));
             if (c.w16 != nullptr) {
                 Pack<bf16_t, 4> o;
 #pragma unroll
@@ -302,8 +305,8 @@ __global__ __launch_bounds__(256) void k_adamw8(const Chunk *__restrict__ table,
             }
             float mscale, vscale;
             store_four(a, (first + (unsigned)i) >> 1, m, root, f[u], mscale, vscale);
-            *reinterpret_cast<unsigned *>(m8 + i) = f[u].m8;
-            *reinterpret_cast<unsigned *>(v8 + i) = f[u].v8;
+            store_vec<unsigned, PAST != 0>(m8 + i, f[u].m8);
+            store_vec<unsigned, PAST != 0>(v8 + i, f[u].v8);
             if (lane == 0) { c.ms[b] = mscale; c.vs[b] = vscale; }
         }
         return;
@@ -404,9 +407,14 @@ dp_status check_list(const dp_param_list *list)
     return DP_OK;
 }
 
-// Gradients of more than half the memory-side cache are not in it any more, and keeping them there helps nobody: all accesses go past the
-// caches then (see the kernels' figures).
-bool past_caches(const dp_param_list *list) { return list->n_elements > (int64_t)32 << 20; }
+// What a step has read is pushed out of the memory-side cache (256 MB) before the next step comes, once it is larger; written there all the
+// same, it leaves dirty lines that are written back while the next kernels read.  Gradients come from the backward pass and are
+// read twice.  Step of a copy into the gradients, norm, AdamW and a reading of the new weights, us, cached / states past / all past:
+//   9 M elements 78 / 82 / 82; 14 M 127 / 115 / 118; 25.5 M 230 / 200 / 207; 33 M 293 / 256 / 262; 45 M 387 / 371 / 356; 138 M 1193 / 1136 / 1122
+//   8-bit states 9 M 68 / 68 / 68; 18 M 122 / 111 / 113; 25.5 M 174 / 159 / 160; 33 M 218 / 196 / 198; 45 M 288 / 273 / 264; 138 M 858 / 820 / 817
+// The bf16 copies of the weights stay in the caches: the next forward pass reads them, and their stores made no difference.
+bool states_past(const dp_param_list *list) { return list->n_elements > (int64_t)10 << 20; }
+bool gradients_past(const dp_param_list *list) { return list->n_elements > (int64_t)32 << 20; }
 
 }  // namespace
 
@@ -498,7 +506,7 @@ extern "C" dp_status dp_grad_norm(const dp_param_list *list, float max_norm, flo
         return launched("gradient norm");
     }
     const int blocks = norm_blocks(list->n_chunks);
-    hipLaunchKernelGGL(past_caches(list) ? k_norm_partial<true> : k_norm_partial<false>, dim3(blocks), dim3(256), 0, st, (const Chunk *)list->table, (long long)list->n_chunks, (double *)ws);
+    hipLaunchKernelGGL(gradients_past(list) ? k_norm_partial<true> : k_norm_partial<false>, dim3(blocks), dim3(256), 0, st, (const Chunk *)list->table, (long long)list->n_chunks, (double *)ws);
     hipLaunchKernelGGL(k_norm_final, dim3(1), dim3(256), 0, st, (const double *)ws, blocks, max_norm, norm_and_scale);
     return launched("gradient norm");
 }
@@ -523,7 +531,9 @@ extern "C" dp_status dp_adamw_step(const dp_param_list *list, const dp_adamw_hyp
     a.eps = (float)h->eps; a.lr = (float)h->lr;
     a.seed = h->seed;
     const dim3 grid((unsigned)list->n_chunks), block(256);
-    if (list->state == DP_STATE_Q8) hipLaunchKernelGGL(k_adamw8, grid, block, 0, (hipStream_t)hip_stream, (const Chunk *)list->table, a, grad_scale);
-    else hipLaunchKernelGGL(past_caches(list) ? k_adamw<true> : k_adamw<false>, grid, block, 0, (hipStream_t)hip_stream, (const Chunk *)list->table, a, grad_scale);
+    const bool q8 = list->state == DP_STATE_Q8;
+    const int past = gradients_past(list) ? 2 : states_past(list) ? 1 : 0;
+    auto *kernel = q8 ? (past == 2 ? k_adamw8<2> : past == 1 ? k_adamw8<1> : k_adamw8<0>) : past == 2 ? k_adamw<2> : past == 1 ? k_adamw<1> : k_adamw<0>;
+    hipLaunchKernelGGL(kernel, grid, block, 0, (hipStream_t)hip_stream, (const Chunk *)list->table, a, grad_scale);
     return launched("AdamW step");
 }

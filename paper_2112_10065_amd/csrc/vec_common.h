@@ -19,11 +19,13 @@ typedef __attribute__((ext_vector_type(4))) unsigned int words4;
 template <typename P, bool PAST> __device__ __forceinline__ P load_vec(const void *p)
 {
     if constexpr (sizeof(P) == 16 && PAST) return __builtin_bit_cast(P, __builtin_nontemporal_load(reinterpret_cast<const words4 *>(p)));
+    else if constexpr (sizeof(P) == 4 && PAST) return __builtin_bit_cast(P, __builtin_nontemporal_load(reinterpret_cast<const unsigned *>(p)));
     else return *reinterpret_cast<const P *>(p);
 }
 template <typename P, bool PAST> __device__ __forceinline__ void store_vec(void *p, const P &v)
 {
     if constexpr (sizeof(P) == 16 && PAST) __builtin_nontemporal_store(__builtin_bit_cast(words4, v), reinterpret_cast<words4 *>(p));
+    else if constexpr (sizeof(P) == 4 && PAST) __builtin_nontemporal_store(__builtin_bit_cast(unsigned, v), reinterpret_cast<unsigned *>(p));
     else *reinterpret_cast<P *>(p) = v;
 }
 

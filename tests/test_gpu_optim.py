@@ -286,3 +286,41 @@ def test_whole_network(env):
     got = {k: params[big][k][cut].cpu().numpy() for k in ("w32", "m", "v")}
     assert np.abs(got["w32"] - w).max() <= 1e-7 and np.abs(got["m"] - m).max() <= 1e-9 and np.all(np.abs(got["v"] - v) <= 4e-7 * v)
     assert all(torch.equal(p["w_bf16"], p["w32"].to(torch.bfloat16)) for p in params)
+
+
+@pytest.mark.parametrize("q8", [False, True], ids=["f32", "q8"])
+@pytest.mark.parametrize("filler", [11_000_001, 34_000_003])
+def test_long_lists(env, q8, filler):
+    """Lists that pass the caches have their tensors stepped as short lists do, to the last bit, and the long tensor too."""
+    dp, O = env
+    short, part = Net(env, SIZES, q8, seed=3), Net(env, SIZES, q8, seed=3)
+    gen = torch.Generator("cuda").manual_seed(filler)
+    rnd = lambda s: torch.randn(filler, device="cuda", generator=gen) * s   # noqa: E731
+    zero = lambda n, dt: torch.zeros(n, dtype=dt, device="cuda")   # noqa: E731
+    p = dict(grad=rnd(1e-3), w32=rnd(0.05), w_bf16=zero(filler, torch.bfloat16), m=zero(filler, torch.uint8 if q8 else torch.float32),
+             v=zero(filler, torch.uint8 if q8 else torch.float32), weight_decay=0.0)
+    if q8:
+        p.update(m_scale=zero(-(-filler // 256), torch.float32), v_scale=zero(-(-filler // 256), torch.float32))
+    old = p["w32"].clone()
+    part.list = dp.param_list(part.params + [p], dp.DP_STATE_Q8 if q8 else dp.DP_STATE_F32)
+    out = torch.empty(2, device="cuda")
+    dp.dp_grad_norm(part.list, 1.0, out, torch.empty(dp.dp_grad_norm_workspace_bytes(part.list), dtype=torch.uint8, device="cuda"))
+    part.step(step=1)
+    short.step(step=1)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(short.state(), part.state()))
+    norm = np.sqrt(sum(float((g.double() ** 2).sum()) for g in [p["grad"]] + [q["grad"] for q in part.params]))
+    assert abs(float(out[0]) - norm) <= 2e-7 * norm
+    # the first step from zero states moves by lr g / (|g| + eps / ...): the rounding of the states has no part in it
+    g = p["grad"].double()
+    want = old.double() - HYPER["lr"] * g / (g.abs() + HYPER["eps"])
+    assert float((p["w32"].double() - want).abs().max()) <= 1e-6 * HYPER["lr"] + 1.2e-7 * float(old.abs().max()) + HYPER["lr"] * 1e-5
+    assert torch.equal(p["w_bf16"], p["w32"].to(torch.bfloat16))
+    if q8:   # codes within one step of e4m3 (1/8 of a value, or 2^-9 below the normal ones) of the moments
+        m = p["m"].view(torch.float8_e4m3fn).float() * p["m_scale"].repeat_interleave(256)[:filler]
+        v = p["v"].view(torch.float8_e4m3fn).float() * p["v_scale"].repeat_interleave(256)[:filler]
+        for got, want, scale in ((m, 0.1 * g, p["m_scale"]), (v, g.abs() * 0.001 ** 0.5, p["v_scale"])):
+            assert bool(((got.double() - want).abs() <= want.abs() * 0.126 + scale.repeat_interleave(256)[:filler] * 2.0 ** -9 * 1.001).all())
+    else:
+        assert float((p["m"].double() - 0.1 * g).abs().max()) <= 4e-7 * 0.1 * float(g.abs().max())
+        assert bool(((p["v"].double() - 0.001 * g * g).abs() <= 4e-7 * 0.001 * g * g).all())
