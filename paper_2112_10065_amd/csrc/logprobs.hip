@@ -117,7 +117,7 @@ template <typename T, int ALIGN = 16> struct Run {
     }
     __device__ __forceinline__ bool aligned_like(const T *p) const { return ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(z)) & 15u) == 0; }
     __device__ __forceinline__ int first(int v) const { return head + v * V; }
-    __device__ __forceinline__ Pack<T, V> vector(int v) const { return *reinterpret_cast<const Pack<T, V> *>(z + head + v * V); }
+    template <bool PAST = false> __device__ __forceinline__ Pack<T, V> vector(int v) const { return load_vec<Pack<T, V>, PAST>(z + head + v * V); }
     __device__ __forceinline__ bool before(int t) const { return t < head; }
     __device__ __forceinline__ int behind(int t) const { const int i = head + vectors * V + t; return t < V && i < n ? i : -1; }
     __device__ __forceinline__ bool any(int t) const { return t < head || t < vectors || behind(t) >= 0; }
@@ -522,8 +522,10 @@ struct LpGradArgs {
 
 // Block = (row, split of its classes); in place a row is one block's, which may have to read it twice.
 // p (log p + entropy) is 0 where p is, also for log p = -inf.
+// Bound by HBM: 2047 x 50001 bf16 62 us (411 MB, 6.6 TB/s).
 // PAST: dz goes past the caches: more than 32 MB of it would push the scores out while they are read, and be written back while the next
-// kernel reads (2047 x 50001 bf16: 71 -> 69 us, and the next forward 69 -> 50).
+// kernel reads (2047 x 50001 bf16: 71 -> 69 us, and the next forward 69 -> 50).  So do the scores, whose last reading this is (66 -> 64;
+// 4095 x 50001 155 -> 133).  The forward's reading stays in the caches for this one: past them it would cost 2047 x 50001 12 us here for 5 more there.
 template <typename T, bool PAST>
 __global__ __launch_bounds__(NT) void k_logprobs_grad(LpGradArgs a)
 {
@@ -573,11 +575,11 @@ __global__ __launch_bounds__(NT) void k_logprobs_grad(LpGradArgs a)
         for (; v + (U - 1) * NT < run.vectors; v += U * NT) {
             Pack<T, V> q[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) q[u] = run.vector(v + u * NT);
+            for (int u = 0; u < U; ++u) q[u] = run.template vector<PAST>(v + u * NT);
 #pragma unroll
             for (int u = 0; u < U; ++u) vector(v + u * NT, q[u]);
         }
-        for (; v < run.vectors; v += NT) vector(v, run.vector(v));
+        for (; v < run.vectors; v += NT) vector(v, run.template vector<PAST>(v));
     } else {   // dz at another offset from a 16-byte boundary than z
         for (int i = t; i < run.n; i += NT) single(i);
     }

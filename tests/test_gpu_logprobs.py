@@ -333,3 +333,30 @@ def test_gradient_at_another_alignment(env):
     dp.dp_logprobs_bwd(k.desc, k.zd, k.idd, out[2], out[1], one, one, room[3:])
     k.check_backward(room[3:3 + 5 * 3001].view(5, 3001), np.ones(5, np.float32), np.ones(5, np.float32))
     assert bool((room[:3] == 9).all()) and bool((room[3 + 5 * 3001:] == 9).all())
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+def test_gradient_of_many_scores(env, bf16):
+    """More scores than one call keeps in the caches: as calls of a few rows give them, to the last bit, between the rows nothing, and in place."""
+    dp = env[0]
+    rows, classes, stride, few = 700 if bf16 else 350, 30001, 30005, 7
+    z = np.tile(scores(env[3], "many", 50, classes, bf16), (rows // 50, 1))
+    k = Run(env, z, (np.arange(rows) * 977) % (classes + 50), 3, bf16, stride, 3)
+    got = k.forward()
+    dlogp, dent = np.linspace(-1, 1, rows).astype(np.float32), np.linspace(3, -2, rows).astype(np.float32)
+    room, dz = k.backward(dlogp, dent, got[2], got[1])
+    torch.cuda.synchronize()
+    keep = torch.ones_like(room, dtype=torch.bool)
+    keep[3:3 + rows * stride].view(rows, stride)[:, :classes] = False
+    assert torch.equal(room[keep], k.room[keep])
+    small = dp.logprobs_desc(few, classes, 3, dp.DP_BF16 if bf16 else dp.DP_F32, stride)
+    dl, de, again = torch.from_numpy(dlogp).cuda(), torch.from_numpy(dent).cuda(), torch.zeros_like(k.zd)
+    for r in range(0, rows, few):
+        cut = slice(r, r + few)
+        dp.dp_logprobs_bwd(small, k.zd[r * stride:], k.idd[r:r + few].clone(), got[2][cut].clone(), got[1][cut].clone(), dl[cut].clone(), de[cut].clone(), again[r * stride:])
+    torch.cuda.synchronize()
+    assert torch.equal(again.view(rows, stride)[:, :classes], dz[:, :classes])
+    part = Run(env, z[:50], k.ids[:50], 3, bf16, stride, 3)
+    part.check_backward(dz[:50], dlogp[:50], dent[:50])
+    placed = k.backward(dlogp, dent, got[2], got[1], place=k.room)[1]
+    assert torch.equal(placed[:, :classes], dz[:, :classes])
