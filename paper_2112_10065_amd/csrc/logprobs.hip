@@ -55,7 +55,7 @@ __device__ __forceinline__ void raise(Soft &a, float m)
     a.s *= f;
     a.m = m;
 }
-template <int V> __device__ __forceinline__ void add_scores(Soft &a, const float (&z)[V])
+template <int V> __device__ __forceinline__ float add_scores(Soft &a, const float (&z)[V])   // returns their largest
 {
     float m = z[0];
 #pragma unroll
@@ -67,6 +67,7 @@ template <int V> __device__ __forceinline__ void add_scores(Soft &a, const float
         a.s += x;                                   // NaN and +inf scores make this NaN
         a.t = fmaf(x, fmaxf(d, -3e38f), a.t);       // exp(-inf) * -inf counts as 0
     }
+    return m;
 }
 __device__ __forceinline__ void join(Soft &a, const Soft &b)
 {
@@ -135,15 +136,32 @@ template <typename T, int ALIGN = 16> struct Run {
     }
 };
 
-// What thread t makes of its scores.
-template <typename T> __device__ __forceinline__ Soft scan(const Run<T> &run)
+constexpr int U = 4;   // vectors of a thread that are on their way together
+
+// A thread's vectors in up to kParts parts of 4 << shift each; part j of thread t has its largest score in tops[j * NT + t].
+constexpr int kParts = 8;
+struct Parts {
+    int shift, count, log;   // log: of a part's vectors, in a single part of those there are
+    __device__ __forceinline__ explicit Parts(int vectors) : shift(0)
+    {
+        const int steps = (vectors + U * NT - 1) / (U * NT);
+        while ((steps - 1) >> shift >= kParts) ++shift;
+        count = steps == 0 ? 0 : ((steps - 1) >> shift) + 1;
+        log = count > 1 || vectors > 2 * NT ? shift + 2 : vectors > NT ? 1 : 0;
+        static_assert(U == 4, "");
+    }
+};
+
+// What thread t makes of its scores; with TOPS, the parts' largest too.
+template <bool TOPS, typename T> __device__ __forceinline__ Soft scan(const Run<T> &run, const Parts &parts, float *tops)
 {
-    constexpr int V = Run<T>::V, U = 4;
+    constexpr int V = Run<T>::V;
     const int t = threadIdx.x;
     Soft mine = {-3.402823466e38f, 0.f, 0.f};
     if (run.before(t)) { const float z[1] = {as_f32(run.z[t])}; add_scores<1>(mine, z); }
     if (run.behind(t) >= 0) { const float z[1] = {as_f32(run.z[run.behind(t)])}; add_scores<1>(mine, z); }
-    int v = t;
+    int v = t, step = 0;
+    float top = -INFINITY;
     for (; v + (U - 1) * NT < run.vectors; v += U * NT) {
         Pack<T, V> q[U];
 #pragma unroll
@@ -153,16 +171,20 @@ template <typename T> __device__ __forceinline__ Soft scan(const Run<T> &run)
             float z[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) z[e] = as_f32(q[u].v[e]);
-            add_scores<V>(mine, z);
+            top = fmaxf(top, add_scores<V>(mine, z));
         }
+        ++step;
+        if (TOPS && (step & ((1 << parts.shift) - 1)) == 0) { tops[((step - 1) >> parts.shift) * NT + t] = top; top = -INFINITY; }
     }
     for (; v < run.vectors; v += NT) {
         const Pack<T, V> q = run.vector(v);
         float z[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) z[e] = as_f32(q.v[e]);
-        add_scores<V>(mine, z);
+        top = fmaxf(top, add_scores<V>(mine, z));
     }
+    // the last part, also where this thread has none of it: another one has
+    if (TOPS && step >> parts.shift < parts.count) tops[(step >> parts.shift) * NT + t] = top;
     return mine;
 }
 // all threads' together, the same for each
@@ -180,31 +202,42 @@ __device__ __forceinline__ Soft block_join(Soft mine)
 // The k largest keys of the block's run, best first, to put(rank, key); all threads call it.  `top`: order of the thread's largest
 // score, 0 if it has none; `odd`: its scores hold a NaN or +inf.
 //
-// At least k threads' maxima reach `least`, so the k largest scores do; only the scores of those threads are looked at again, by all
-// threads together, and appended to a list in LDS; each candidate's place is the number of larger ones.  `least` is the k-th largest maximum to
-// 16 bits (which is all of a bf16 score's), found bit by bit: a count over 256 values is four comparisons of a wavefront.
+// The maxima of at least k groups of threads reach `least`, so the k largest scores do; only the parts of threads that reach it are looked at again, by
+// all threads together, and appended to a list in LDS; each candidate's place is the number of larger ones.  `least` is the k-th largest
+// maximum to 16 bits (which is all of a bf16 score's), found bit by bit: a count over the 64 groups of four threads is one comparison of a wavefront.
+// About 24 scores reach the 20th of 64 maxima; for more than 32 the threads' own 256 serve, four times the instructions.
+// Looking at whole threads' scores again instead of parts: 2047 x 50001 bf16 with 20 leaders 47 -> 55 us, with 64 52 -> 72.
 // Where very many scores reach it (equal ones, or ruled-out classes where fewer than k are left) the list holds those above
 // it and the first k equal to it by index, and where even that does not fit, k rounds take the largest below the one before.
 template <typename T, typename P>
-__device__ __forceinline__ void block_top(const Run<T> &run, int base, int k, unsigned top, bool odd, P &&put)
+__device__ __forceinline__ void block_top(const Run<T> &run, const Parts &parts, const float *part_tops, int base, int k, unsigned top, bool odd, P &&put)
 {
     constexpr int V = Run<T>::V;
-    __shared__ alignas(16) unsigned tops[NT];   // read by fours
+    __shared__ unsigned tops[NT];
     __shared__ unsigned long long list[kCandidates + 8];
-    __shared__ unsigned short leaders[NT];
+    __shared__ unsigned short leaders[NT * kParts];   // thread and part
     __shared__ int count, ties, lead, some_odd;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     tops[t] = top;
     if (t == 0) { count = 0; lead = 0; some_odd = 0; }
     __syncthreads();
     if (odd) some_odd = 1;
-    const uint4 four = *reinterpret_cast<const uint4 *>(&tops[4 * lane]);
+    // a group has a thread of each wavefront: scores in rising or falling order lead in neighbouring threads
+    const unsigned own[4] = {tops[lane], tops[lane + 64], tops[lane + 128], tops[lane + 192]};
+    const unsigned most = max(max(own[0], own[1]), max(own[2], own[3]));
+    auto threads_reach = [&](unsigned from) {
+        int n = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) n += __popcll(__ballot(own[w] >= from));
+        return n;
+    };
     unsigned least = 0;
-    for (unsigned bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
-        const unsigned trial = least | bit;
-        const int reach = __popcll(__ballot(four.x >= trial)) + __popcll(__ballot(four.y >= trial)) + __popcll(__ballot(four.z >= trial)) +
-                          __popcll(__ballot(four.w >= trial));
-        if (reach >= k) least = trial;
+    if (k <= 32) {
+        for (unsigned bit = 0x80000000u; bit >= 0x10000u; bit >>= 1)
+            if (__popcll(__ballot(most >= (least | bit))) >= k) least |= bit;
+    } else {
+        for (unsigned bit = 0x80000000u; bit >= 0x10000u; bit >>= 1)
+            if (threads_reach(least | bit) >= k) least |= bit;
     }
     auto append = [&](float z, int i, unsigned from) {
         if (order_of(z) >= from) {
@@ -212,45 +245,69 @@ __device__ __forceinline__ void block_top(const Run<T> &run, int base, int k, un
             if (at < kCandidates) list[at] = key_of(z, base + i);
         }
     };
-    // scores from `from` on: the single ones by their threads, the vectors of the leading threads by everybody
+    // a wavefront's vectors (`there`: this lane has one) with one addition: each is a wait
+    auto append_vectors = [&](const Pack<T, V> &q, int first, bool there, unsigned from) {
+        unsigned order[V];
+        int hits = 0;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            order[e] = there ? order_of(as_f32(q.v[e])) : 0u;
+            hits += __popcll(__ballot(order[e] >= from));
+        }
+        if (hits == 0) return;
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&count, hits);
+        at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const unsigned long long who = __ballot(order[e] >= from);
+            const int place = at + __popcll(who & ((1ull << lane) - 1));
+            if (order[e] >= from && place < kCandidates) list[place] = (unsigned long long)order[e] << 32 | (unsigned)~(base + first + e);
+            at += __popcll(who);
+        }
+    };
+    // scores from `from` on: the single ones by their threads, the vectors of the parts that reach it by everybody
     auto collect = [&](unsigned from) {
         if (top >= from && top != 0) {
-            leaders[atomicAdd(&lead, 1)] = (unsigned short)t;
+            for (int j = 0; j < parts.count; ++j)
+                if (order_of(part_tops[j * NT + t]) >= from) leaders[atomicAdd(&lead, 1)] = (unsigned short)(j * NT + t);
             if (run.before(t)) append(as_f32(run.z[t]), t, from);
             if (run.behind(t) >= 0) append(as_f32(run.z[run.behind(t)]), run.behind(t), from);
         }
         __syncthreads();
-        const int each = (run.vectors + NT - 1) / NT, total = lead * each;
-        constexpr int U = 4;   // a read comes from beyond the L2 where many rows are on their way: four at a time
-        for (int i0 = t; i0 < total; i0 += U * NT) {
+        const int log = parts.log, total = lead << log;
+        static_assert(NT == 256, "");
+        // a read comes from beyond the L2 where many rows are on their way: two at a time
+        constexpr int W = 1;
+        for (int i0 = t - lane; i0 < total; i0 += W * NT) {   // whole wavefronts
             if (*(volatile int *)&count > kCandidates) break;   // it does not fit
-            Pack<T, V> q[U];
-            int v[U];
+            Pack<T, V> q[W];
+            int v[W];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int i = i0 + u * NT, l = i / each;
-                v[u] = i < total ? (i - l * each) * NT + leaders[l] : run.vectors;
+            for (int u = 0; u < W; ++u) {
+                const int i = i0 + lane + u * NT;
+                v[u] = run.vectors;
+                if (i < total) {
+                    const int l = leaders[i >> log];
+                    v[u] = (((l >> 8) << log) + (i & ((1 << log) - 1))) * NT + (l & (NT - 1));
+                }
                 if (v[u] < run.vectors) q[u] = run.vector(v[u]);
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (v[u] < run.vectors)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) append(as_f32(q[u].v[e]), run.first(v[u]) + e, from);
+            for (int u = 0; u < W; ++u)
+                if (i0 + u * NT < total) append_vectors(q[u], run.first(v[u]), v[u] < run.vectors, from);
         }
         __syncthreads();
     };
+    least = max(least, 1u);   // 0 is a lane without a vector
     collect(least);
     const bool slow = some_odd != 0;
     bool fits = !slow && count <= kCandidates;
     if (!slow && !fits) {
-        // `least` to all its bits: the largest value that k maxima reach
-        for (unsigned bit = 0x8000u; bit != 0; bit >>= 1) {
-            const unsigned trial = least | bit;
-            const int reach = __popcll(__ballot(four.x >= trial)) + __popcll(__ballot(four.y >= trial)) + __popcll(__ballot(four.z >= trial)) +
-                              __popcll(__ballot(four.w >= trial));
-            if (reach >= k) least = trial;
-        }
+        // the largest value that k threads' maxima reach, to all its bits
+        least = 0;
+        for (unsigned bit = 0x80000000u; bit != 0; bit >>= 1)
+            if (threads_reach(least | bit) >= k) least |= bit;
         __syncthreads();
         if (t == 0) { count = 0; lead = 0; ties = 0; }
         __syncthreads();
@@ -316,42 +373,44 @@ __device__ __forceinline__ void write_row(const LpArgs &a, int r, const Soft &al
     if (a.logp != nullptr) a.logp[r] = valid ? log_p(all, log_s, score) : 0.f;
 }
 
-// Block = (row, split of its classes).
+// Block = (row, split of its classes).  Bound by HBM where there are many rows: 2047 x 50001 bf16 47 us with 20 leaders, 42 without (205 MB, 4.9 TB/s); one
+// row of 131072 is two kernels' waits, 9.9 us.  With at most 80 scalar registers eight wavefronts share a SIMD, with more seven: 2048 x 5001 has eight
+// blocks to a compute unit, and they ran in two turns (12.1 -> 14.7 us).
 template <typename T>
-__global__ __launch_bounds__(NT) void k_logprobs(LpArgs a)
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_num_sgpr(80))) void k_logprobs(LpArgs a)
 {
     const int t = threadIdx.x;
     const int r = blockIdx.x / a.splits, split = blockIdx.x - r * a.splits;
     const int c0 = split * a.seg;
     const T *row = (const T *)a.z + (size_t)r * a.stride;
     const Run<T> run(row + c0, min(a.seg, a.classes - c0));
-    const Soft mine = scan(run);
+    __shared__ float tops[kParts * NT];
+    const Parts parts(run.vectors);
+    const Soft mine = a.k > 0 ? scan<true>(run, parts, tops) : scan<false>(run, parts, tops);
     const unsigned top = !run.any(t) ? 0u : mine.s == 0.f ? order_of(-INFINITY) : order_of(mine.m);
     const bool odd = mine.s != mine.s;
     const Soft all = block_join(mine);
-    if (a.splits > 1) {
-        const size_t at = (size_t)r * a.splits + split;
-        if (t == 0) a.part[at] = all;
-        unsigned long long *out = a.part_top + at * a.k;
-        if (a.k > 0) block_top(run, c0, a.k, top, odd, [&](int rank, unsigned long long key) { out[rank] = key; });
-        return;
-    }
-    if (t == 0) {
+    const size_t at = (size_t)r * a.splits + split;
+    if (t == 0 && a.splits > 1) a.part[at] = all;
+    if (t == 0 && a.splits == 1) {
         const int id = a.logp != nullptr ? a.ids[r] : -1;
         const bool valid = id >= 0 && id < a.classes;
         write_row(a, r, all, valid ? as_f32(row[id]) : 0.f, valid);
     }
-    if (a.k > 0) {
-        const float log_s = logf(all.s);
-        block_top(run, 0, a.k, top, odd, [&](int rank, unsigned long long key) {
-            a.top_ids[(size_t)r * a.k + rank] = index_of(key);
-            a.top_logp[(size_t)r * a.k + rank] = log_p(all, log_s, score_of(key));
-        });
-    }
+    if (a.k == 0) return;
+    const float log_s = logf(all.s);
+    block_top(run, parts, tops, c0, a.k, top, odd, [&](int rank, unsigned long long key) {
+        if (a.splits > 1) a.part_top[at * a.k + rank] = key;
+        else {
+            a.top_ids[at * a.k + rank] = index_of(key);
+            a.top_logp[at * a.k + rank] = log_p(all, log_s, score_of(key));
+        }
+    });
 }
 
 // Joins the splits of a row.  Block = row.  Each split's keys are in order: with S splits the `need`-th largest of their `each`-th
 // keys, need * each >= k, bounds the k-th largest from below; with about half of the splits (the least of all of them would bound little).
+// 3.8 us for 32 splits with 20 leaders: a launch, one wait for what other dies wrote, the search.
 template <typename T>
 __global__ __launch_bounds__(NT) void k_logprobs_join(LpArgs a)
 {
@@ -413,7 +472,7 @@ __global__ __launch_bounds__(NT) void k_logprobs_join(LpArgs a)
 }
 
 // Short rows: a wavefront each, the row in registers (class lane + 64 j in slot j), the same steps without a barrier.  A block per
-// row of 1000 classes spends its time on barriers and idle threads (bf16, 4096 rows, five alternatives: 15.6 us; see the launch for this kernel's).
+// row of 1000 classes spends its time on barriers and idle threads (bf16, 4096 rows, five alternatives: 15.6 -> 7.4 us, bound by the search for the leaders).
 constexpr int kRowCandidates = 256;   // of a row, in LDS; a multiple of 64
 template <typename T, int R>
 __global__ __launch_bounds__(NT) void k_logprobs_rows(LpArgs a)
@@ -529,7 +588,7 @@ struct LpGradArgs {
 template <typename T, bool PAST>
 __global__ __launch_bounds__(NT) void k_logprobs_grad(LpGradArgs a)
 {
-    constexpr int V = Run<T>::V, U = 4;
+    constexpr int V = Run<T>::V;
     const int t = threadIdx.x, r = blockIdx.x / a.splits, c0 = (blockIdx.x - r * a.splits) * a.seg;
     const T *row = (const T *)a.z + (size_t)r * a.stride + c0;
     T *out = (T *)a.dz + (size_t)r * a.stride + c0;
@@ -543,7 +602,8 @@ __global__ __launch_bounds__(NT) void k_logprobs_grad(LpGradArgs a)
     // p = exp(z - shift) / s: lse holds both; beyond 256 it loses log s to rounding, and the row is summed again
     float shift = none ? 0.f : lse, log_s = 0.f;           // none: every score is -inf, p = 0
     if (fabsf(lse) > 256.f && !none) {
-        const Soft all = block_join(scan(Run<T>((const T *)a.z + (size_t)r * a.stride, a.classes)));
+        const Run<T> whole((const T *)a.z + (size_t)r * a.stride, a.classes);
+        const Soft all = block_join(scan<false>(whole, Parts(whole.vectors), nullptr));
         shift = all.m;
         log_s = logf(all.s);
     }

@@ -52,11 +52,11 @@ template <bool PAST> __device__ __forceinline__ double square_sum(const Chunk &c
     return s;
 }
 
-// the block's sum: wavefronts by shuffles, their sums in order
+// the block's sum: wavefronts by themselves, their sums in order
 template <int N> __device__ __forceinline__ double block_sum(double s)
 {
     __shared__ double sm[N / 64];
-    s = wave_sum(s);
+    s = wave_sum_fast(s);
     if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = s;
     __syncthreads();
     s = 0.0;
@@ -85,8 +85,14 @@ template <bool PAST> __global__ __launch_bounds__(256) void k_norm_partial(const
 
 __global__ __launch_bounds__(256) void k_norm_final(const double *__restrict__ partial, int n, float max_norm, float *__restrict__ out)
 {
-    double s = 0.0;
-    for (int i = threadIdx.x; i < n; i += 256) s += partial[i];
+    double v[kNormBlocks / 256], s = 0.0;
+#pragma unroll
+    for (int u = 0; u < kNormBlocks / 256; ++u) {
+        const int i = u * 256 + threadIdx.x;
+        v[u] = i < n ? partial[i] : 0.0;
+    }
+#pragma unroll
+    for (int u = 0; u < kNormBlocks / 256; ++u) s += v[u];
     s = block_sum<256>(s);
     if (threadIdx.x == 0) write_norm(s, max_norm, out);
 }

@@ -35,14 +35,7 @@ template <typename T> __device__ __forceinline__ T from_f32(float v);
 template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
 template <> __device__ __forceinline__ bf16_t from_f32<bf16_t>(float v) { return __builtin_bit_cast(bf16_t, (__bf16)v); }   // nearest even
 
-__device__ __forceinline__ double wave_sum(double v)
-{
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
-}
-
-// The same for one value per lane by data-parallel moves, a fifth of the time of six exchanges through LDS: within rows of 16 lanes, then
+// A wavefront's sum or maximum by data-parallel moves, a fifth of the time of six exchanges through LDS: within rows of 16 lanes, then
 // across rows; lane 63 has the result, which every lane gets.  `none`: what an absent neighbour counts as.
 template <int CTRL, int ROWS> __device__ __forceinline__ float moved(float v, float none)
 {
@@ -60,6 +53,26 @@ template <typename F> __device__ __forceinline__ float wave_reduce(float v, floa
 }
 __device__ __forceinline__ float wave_sum_fast(float v) { return wave_reduce(v, 0.f, [](float a, float b) { return a + b; }); }
 __device__ __forceinline__ float wave_max_fast(float v) { return wave_reduce(v, -3.402823466e38f, [](float a, float b) { return fmaxf(a, b); }); }
+
+template <int CTRL, int ROWS> __device__ __forceinline__ double moved(double v)
+{
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)u, CTRL, ROWS, 0xf, false);
+    const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, ROWS, 0xf, false);
+    return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
+__device__ __forceinline__ double wave_sum_fast(double v)
+{
+    v += moved<0x111, 0xf>(v);
+    v += moved<0x112, 0xf>(v);
+    v += moved<0x114, 0xf>(v);
+    v += moved<0x118, 0xf>(v);
+    v += moved<0x142, 0xa>(v);
+    v += moved<0x143, 0xc>(v);
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)u, 63), hi = (unsigned)__builtin_amdgcn_readlane((int)(u >> 32), 63);
+    return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
 
 __device__ __forceinline__ unsigned wave_max_fast(unsigned v)
 {

@@ -360,3 +360,40 @@ def test_gradient_of_many_scores(env, bf16):
     part.check_backward(dz[:50], dlogp[:50], dent[:50])
     placed = k.backward(dlogp, dent, got[2], got[1], place=k.room)[1]
     assert torch.equal(placed[:, :classes], dz[:, :classes])
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("top", [1, 20, 64])
+def test_leaders_of_many_long_rows(env, top, bf16):
+    """Rows long enough that a block looks at them in parts of many vectors: leaders anywhere, in one place, equal, and few."""
+    dp = env[0]
+    rows, classes = 515, 140003 if bf16 else 70003
+    gen = torch.Generator("cuda").manual_seed(top)
+    z = torch.randn((rows, classes), device="cuda", generator=gen) * 3
+    z[1] = 0.5
+    z[2, :] = -float("inf")
+    z[2, [5, classes // 2, classes - 1]] = torch.tensor([1.0, 2.0, 1.0], device="cuda")
+    z[3] = torch.arange(classes, device="cuda") / 8
+    z[4] = -torch.arange(classes, device="cuda") / 8
+    z[5, -100:] += 50
+    z[6, 7 * 256 * 8:7 * 256 * 8 + 300] += 50
+    z[7, ::4096] += 40
+    z[8] = z[8].round()
+    z[9] = -float("inf")
+    if bf16:
+        z = z.to(torch.bfloat16)
+    ids = torch.randint(0, classes, (rows,), device="cuda", dtype=torch.int32, generator=gen)
+    out = [torch.empty(rows, device="cuda") for _ in range(3)]
+    best, at = torch.empty((rows, top), device="cuda"), torch.empty((rows, top), dtype=torch.int32, device="cuda")
+    d = dp.logprobs_desc(rows, classes, top, dp.DP_BF16 if bf16 else dp.DP_F32)
+    dp.dp_logprobs_fwd(d, z, ids, *out, best, at, torch.empty(dp.dp_logprobs_workspace_bytes(d) + 16, dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    for r in range(0, rows, 103):
+        value, order = torch.sort(z[r:r + 103].float() + 0.0, dim=1, descending=True, stable=True)
+        assert torch.equal(at[r:r + 103].long(), order[:, :top])
+        lse = torch.logsumexp(z[r:r + 103].double(), 1)
+        want = torch.where(torch.isinf(lse)[:, None], lse[:, None], value[:, :top].double() - lse[:, None])
+        tol = 1e-5 + 2e-7 * value.double().masked_fill(torch.isinf(value), 0).abs().amax(1, keepdim=True)
+        got = best[r:r + 103].double()
+        assert bool((((got - want).abs() <= tol) | (got == want)).all())
+        assert bool((((out[2][r:r + 103] - lse).abs() <= tol[:, 0]) | (out[2][r:r + 103] == lse)).all())
