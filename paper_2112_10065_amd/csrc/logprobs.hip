@@ -472,7 +472,7 @@ __global__ __launch_bounds__(NT) void k_logprobs_join(LpArgs a)
 }
 
 // Short rows: a wavefront each, the row in registers (class lane + 64 j in slot j), the same steps without a barrier.  A block per
-// row of 1000 classes spends its time on barriers and idle threads (bf16, 4096 rows, five alternatives: 15.6 -> 7.4 us, bound by the search for the leaders).
+// row of 1000 classes spends its time on barriers and idle threads (bf16, 4096 rows, five leaders: 15.6 -> 6.9 us, 4.6 of them without leaders: vector instructions).
 constexpr int kRowCandidates = 256;   // of a row, in LDS; a multiple of 64
 template <typename T, int R>
 __global__ __launch_bounds__(NT) void k_logprobs_rows(LpArgs a)
@@ -503,37 +503,43 @@ __global__ __launch_bounds__(NT) void k_logprobs_rows(LpArgs a)
     unsigned long long *list = lists[wave];
     const int per_lane = (a.classes - lane + 63) / 64;   // classes of this lane, may be 0
     if (all.s == all.s) {   // no NaN or +inf: the lanes' maxima are what they seem
-        unsigned order[R];
-#pragma unroll
-        for (int j = 0; j < R; ++j) order[j] = j < per_lane ? order_of(v[j]) : 0u;
+        // by the lanes' maxima as long as half of the lanes may stay below, else by those of their even and odd classes' slots
         unsigned least = 0;
-        auto reach = [&](unsigned from) {
-            int n = 0;
-#pragma unroll
-            for (int j = 0; j < R; ++j) n += __popcll(__ballot(order[j] >= from));
-            return n;
-        };
-        // by the lanes' maxima as long as a quarter of the lanes may stay below, else by all scores
-        if (a.k <= 48) {
+        if (a.k <= 32) {
             const unsigned top = per_lane <= 0 ? 0u : mine.s == 0.f ? order_of(-INFINITY) : order_of(mine.m);
             for (unsigned bit = 0x80000000u; bit >= 0x10000u; bit >>= 1)
                 if (__popcll(__ballot(top >= (least | bit))) >= a.k) least |= bit;
         } else {
+            float even = v[0], odd = v[1];   // absent ones are -inf
+#pragma unroll
+            for (int j = 2; j < R; j += 2) { even = fmaxf(even, v[j]); odd = fmaxf(odd, v[j + 1]); }
+            const unsigned top0 = per_lane > 0 ? order_of(even) : 0u, top1 = per_lane > 1 ? order_of(odd) : 0u;
             for (unsigned bit = 0x80000000u; bit >= 0x10000u; bit >>= 1)
-                if (reach(least | bit) >= a.k) least |= bit;
+                if (__popcll(__ballot(top0 >= (least | bit))) + __popcll(__ballot(top1 >= (least | bit))) >= a.k) least |= bit;
         }
         const unsigned long long below = (1ull << lane) - 1;
         int c = 0;
         auto append = [&](bool hit, int j) {
             const unsigned long long hits = __ballot(hit);
+            if (hits == 0) return;
             const int at = c + __popcll(hits & below);
             if (hit && at < kRowCandidates) list[at] = key_of(v[j], lane + 64 * j);
             c += __popcll(hits);
         };
-        least = max(least, 1u);
+        // the same bound as a score: one comparison, where the order of a score is six operations
+        const float bound = least <= order_of(-INFINITY) ? -INFINITY : score_of((unsigned long long)least << 32);
 #pragma unroll
-        for (int j = 0; j < R; ++j) append(order[j] >= least, j);
+        for (int j = 0; j < R; ++j) append(j < per_lane && v[j] >= bound, j);
         if (c > kRowCandidates) {   // the k-th largest score itself, those above it, and the first equal to it by index
+            unsigned order[R];
+#pragma unroll
+            for (int j = 0; j < R; ++j) order[j] = j < per_lane ? order_of(v[j]) : 0u;
+            auto reach = [&](unsigned from) {
+                int n = 0;
+#pragma unroll
+                for (int j = 0; j < R; ++j) n += __popcll(__ballot(order[j] >= from));
+                return n;
+            };
             least = 0;
             for (unsigned bit = 0x80000000u; bit != 0; bit >>= 1)
                 if (reach(least | bit) >= a.k) least |= bit;
@@ -579,6 +585,65 @@ struct LpGradArgs {
     long long stride;
 };
 
+// A row's gradient: p (-dl - de (log p + h)) = exp(d) (k0 - k1 d), d = z - shift, and dl more for the given class.
+// sum(): maximum and sums of the row, asked for by all its threads or none.
+struct RowGrad {
+    float shift, k0, k1, dl;
+    int id;   // -1: none
+    template <typename F> __device__ __forceinline__ RowGrad(const LpGradArgs &a, int r, F &&sum)
+    {
+        const float lse = a.lse[r], h = a.entropy != nullptr ? a.entropy[r] : 0.f;
+        const bool none = lse == -INFINITY;
+        id = a.ids != nullptr ? a.ids[r] : -1;
+        const bool valid = id >= 0 && id < a.classes && !none;
+        dl = a.dlogp != nullptr && valid ? a.dlogp[r] : 0.f;
+        if (!valid) id = -1;
+        const float de = a.dentropy != nullptr && !none ? a.dentropy[r] : 0.f;
+        // p = exp(z - shift) / s: lse holds both; beyond 256 it loses log s to rounding, and the row is summed again
+        float log_s = 0.f;
+        shift = none ? 0.f : lse;                          // none: every score is -inf, p = 0
+        if (fabsf(lse) > 256.f && !none) {
+            const Soft all = sum();
+            shift = all.m;
+            log_s = logf(all.s);
+        }
+        k1 = de * exp_d(-log_s);
+        k0 = -fmaf(de, h - log_s, dl) * exp_d(-log_s);
+    }
+    __device__ __forceinline__ float operator()(float z) const
+    {
+        const float d = z - shift;
+        return exp_d(d) * fmaf(-k1, fmaxf(d, -128.f), k0);   // exp(d) is 0 long before -128; k1 d must not be infinite then
+    }
+};
+
+// Short rows: a wavefront each, the row in registers (class lane + 64 j in slot j).  A block to each: bf16 4096 x 1000 6.8 -> 5.8 us, 16384 x 1000
+// 17.9 -> 14.0 (65 MB, 4.7 TB/s), 8192 x 512 9.3 -> 5.6, fp32 65536 x 10 51 -> 9.8.
+template <typename T, int R>
+__global__ __launch_bounds__(NT) void k_logprobs_grad_rows(LpGradArgs a)
+{
+    const int lane = threadIdx.x & 63, r = blockIdx.x * (NT / 64) + (int)(threadIdx.x >> 6);
+    if (r >= a.rows) return;
+    const T *z = (const T *)a.z + (size_t)r * a.stride;
+    T *out = (T *)a.dz + (size_t)r * a.stride;
+    float v[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) v[j] = as_f32(z[min(lane + 64 * j, a.classes - 1)]);
+    const RowGrad grad(a, r, [&]() {
+        float w[R];
+#pragma unroll
+        for (int j = 0; j < R; ++j) w[j] = lane + 64 * j < a.classes ? v[j] : -INFINITY;
+        Soft mine = {-3.402823466e38f, 0.f, 0.f};
+        add_scores<R>(mine, w);
+        return wave_join(mine);
+    });
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const int i = lane + 64 * j;
+        if (i < a.classes) out[i] = from_f32<T>(grad(v[j]) + (i == grad.id ? grad.dl : 0.f));
+    }
+}
+
 // Block = (row, split of its classes); in place a row is one block's, which may have to read it twice.
 // p (log p + entropy) is 0 where p is, also for log p = -inf.
 // Bound by HBM: 2047 x 50001 bf16 62 us (411 MB, 6.6 TB/s).
@@ -594,26 +659,13 @@ __global__ __launch_bounds__(NT) void k_logprobs_grad(LpGradArgs a)
     T *out = (T *)a.dz + (size_t)r * a.stride + c0;
     // from a line's boundary on, a wavefront's kilobyte is eight whole lines, also to store (2047 x 50001 bf16: 90 -> 81 us; reads alone do not care)
     const Run<T, 128> run(row, min(a.seg, a.classes - c0));
-    const float lse = a.lse[r], h = a.entropy != nullptr ? a.entropy[r] : 0.f;
-    const bool none = lse == -INFINITY;
-    const int id = a.ids != nullptr ? a.ids[r] : -1;
-    const bool valid = id >= 0 && id < a.classes && !none;
-    const float dl = a.dlogp != nullptr && valid ? a.dlogp[r] : 0.f, de = a.dentropy != nullptr && !none ? a.dentropy[r] : 0.f;
-    // p = exp(z - shift) / s: lse holds both; beyond 256 it loses log s to rounding, and the row is summed again
-    float shift = none ? 0.f : lse, log_s = 0.f;           // none: every score is -inf, p = 0
-    if (fabsf(lse) > 256.f && !none) {
+    const RowGrad row_grad(a, r, [&]() {
         const Run<T> whole((const T *)a.z + (size_t)r * a.stride, a.classes);
-        const Soft all = block_join(scan<false>(whole, Parts(whole.vectors), nullptr));
-        shift = all.m;
-        log_s = logf(all.s);
-    }
-    // gradient = p (-dl - de (log p + h)) = exp(d) (k0 - k1 d), d = z - shift
-    const float k1 = de * exp_d(-log_s), k0 = -fmaf(de, h - log_s, dl) * exp_d(-log_s);
-    const int at = valid ? id - c0 : -1;                   // the given class in this run, if in [0, n)
-    auto grad = [&](float z) {
-        const float d = z - shift;
-        return exp_d(d) * fmaf(-k1, fmaxf(d, -128.f), k0);   // exp(d) is 0 long before -128; k1 d must not be infinite then
-    };
+        return block_join(scan<false>(whole, Parts(whole.vectors), nullptr));
+    });
+    const int at = row_grad.id < 0 ? -1 : row_grad.id - c0;   // the given class in this run, if in [0, n)
+    const float dl = row_grad.dl;
+    auto grad = [&](float z) { return row_grad(z); };
     auto single = [&](int i) { out[i] = from_f32<T>(grad(as_f32(run.z[i])) + (i == at ? dl : 0.f)); };
     auto vector = [&](int v, const Pack<T, V> &q) {
         float g[V];
@@ -757,10 +809,20 @@ extern "C" dp_status dp_logprobs_bwd(const dp_logprobs_desc *desc, const void *z
     }
     for (const void *p : {(const void *)ids, (const void *)lse, (const void *)entropy, (const void *)dlogp, (const void *)dentropy})
         if (misaligned(p, 4)) { dp_set_error("log-probabilities' gradient: pointers must be 4-byte aligned"); return DP_ERR_BAD_DESC; }
+    const bool bf = d.io_dtype == DP_BF16;
     LpGradArgs a = {z, ids, lse, entropy, dlogp, dentropy, dz, d.rows, d.classes, 1, d.classes, stride_of(d)};
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (d.classes <= kShortRow) {
+        const dim3 grid((d.rows + NT / 64 - 1) / (NT / 64));
+        auto *kernel = d.classes <= 128 ? (bf ? k_logprobs_grad_rows<bf16_t, 2> : k_logprobs_grad_rows<float, 2>) :
+                       d.classes <= 512 ? (bf ? k_logprobs_grad_rows<bf16_t, 8> : k_logprobs_grad_rows<float, 8>) :
+                       (bf ? k_logprobs_grad_rows<bf16_t, 16> : k_logprobs_grad_rows<float, 16>);
+        hipLaunchKernelGGL(kernel, grid, dim3(NT), 0, st, a);
+        return launched("log-probabilities' gradient");
+    }
     if (dz != z) split_rows(d.rows, d.classes, 2048, a.splits, a.seg);   // 256 x 48000: 9.5 us, one block to a row 11.9
-    const bool bf = d.io_dtype == DP_BF16, past = (int64_t)d.rows * d.classes * (bf ? 2 : 4) > (32 << 20);
+    const bool past = (int64_t)d.rows * d.classes * (bf ? 2 : 4) > (32 << 20);
     auto *kernel = bf ? (past ? k_logprobs_grad<bf16_t, true> : k_logprobs_grad<bf16_t, false>) : (past ? k_logprobs_grad<float, true> : k_logprobs_grad<float, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)d.rows * a.splits), dim3(NT), 0, (hipStream_t)hip_stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)d.rows * a.splits), dim3(NT), 0, st, a);
     return launched("log-probabilities' gradient");
 }
