@@ -701,11 +701,13 @@ int shape(const dp_group_norm_desc &d, bool bwd, GnArgs &a)
 
 // The one-kernel form: wavefronts to a unit (0: two kernels), vectors to a lane, groups of a unit.  Only for groups that are a power of
 // two of whole vectors or divide one.  Measured in both forms (bf16, us, two kernels / one):
-//   up to 8 vectors a lane      8 x 28 x 28 x 512 forward 13.3 / 6.3, backward 16.9 / 13.0; 1 x 14 x 14 x 512 11.1 / 3.8, 11.5 / 5.1
+//   up to 8 vectors a lane of four wavefronts   8 x 28 x 28 x 512 forward 13.3 / 5.7, backward 16.9 / 13.0; 1 x 14 x 14 x 512 11.1 / 3.5, 11.5 / 5.1
 //   1024 units and more: a wavefront each (32 x 14 x 14 x 1024 forward 17 / 8.3); fewer: four (1 x 14 x 14 x 512 forward 4.9 -> 3.8)
+//   forward eight instead of four, half as many vectors to a lane: 1 x 28 x 28 x 512 5.1 -> 4.2, 16 x 28 x 28 x 512 9.3 -> 8.7; backward has more to
+//     exchange (16 x 28 x 28 x 512 14.9 -> 16.9)
 //   backward of 1024 units of four wavefronts: the pieces of a unit are a fraction of a cache line, and the L2s lose the rest of it
 //     (32 x 28 x 28 x 256, 16-byte pieces 21 / 23; x 512, 32-byte pieces 33.6 / 27.8, with the saved output 39 / 43)
-//   9 to 16 vectors, forward only (backward has two tensors to hold): 8 x 56 x 56 x 256 17.1 / 13.6, but 32 x 56 x 56 x 256 33 / 48
+//   9 to 16 vectors, forward only (backward has two tensors to hold): 8 x 56 x 56 x 256 17.1 / 13.0, but 32 x 56 x 56 x 256 33 / 48
 struct UnitForm { int waves, vectors, groups; };
 UnitForm unit_form(const GnArgs &a, int V, bool bwd, bool mask)
 {
@@ -719,8 +721,9 @@ UnitForm unit_form(const GnArgs &a, int V, bool bwd, bool mask)
     if ((cvs & (cvs - 1)) != 0 || cvs > 64 || units > (1 << 23)) return f;   // a grid has fewer than 2^32 threads
     const int w1 = ceil_div(a.hw, 64 / cvs), w4 = ceil_div(a.hw, 256 / cvs);
     if (w1 <= 8 && units >= 1024) { f.waves = 1; f.vectors = 8; }
-    else if (w4 <= 8 && (!bwd || units < 1024 || (cvs > 1 && !mask))) { f.waves = 4; f.vectors = 8; }
-    else if (!bwd && w4 <= 16 && units <= 512) { f.waves = 4; f.vectors = 16; }
+    else if (!bwd && w4 <= 8) { f.waves = 8; f.vectors = 4; }
+    else if (bwd && w4 <= 8 && (units < 1024 || (cvs > 1 && !mask))) { f.waves = 4; f.vectors = 8; }
+    else if (!bwd && w4 <= 16 && units <= 512) { f.waves = 8; f.vectors = 8; }
     return f;
 }
 
@@ -736,8 +739,9 @@ void launch_unit(GnArgs a, const UnitForm &f, hipStream_t st)
     a.splits = 1;
     const dim3 grid(8 * a.units_each);
     if (f.waves == 1) hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 1, 8>), grid, dim3(256), 0, st, a);
-    else if (f.vectors == 8 && f.waves == 4) hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 4, 8>), grid, dim3(256), 0, st, a);
-    else if constexpr (!BWD) hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 4, 16>), grid, dim3(256), 0, st, a);
+    else if constexpr (BWD) hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 4, 8>), grid, dim3(256), 0, st, a);
+    else if (f.vectors == 4) hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 8, 4>), grid, dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 8, 8>), grid, dim3(512), 0, st, a);
     if (BWD && a.grad_blocks > 0 && a.n > 1) hipLaunchKernelGGL(k_gn_sums, dim3(a.grad_blocks), dim3(NT), 0, st, a);
 }
 
