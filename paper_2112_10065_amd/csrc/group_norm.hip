@@ -32,7 +32,7 @@ struct GnArgs {
     int grad_blocks;                 // blocks of the second kernel that sum dgamma / dbeta
     float eps, inv_count;            // 1 / (hw * cg)
     int past;                        // the second kernel's stores (1), loads too (2) go past the caches
-    int units, units_each;           // one-kernel form: units in all, units of an eighth of them
+    int units, units_each, cvs;      // one-kernel form: units in all, units of an eighth of them; vectors of a unit's row
 };
 
 struct Slab { int ch0, width, g0, gs, cell0; };   // first channel, channels, first group, groups, first cell
@@ -635,6 +635,175 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_gn_unit(GnArgs a)
     }
 }
 
+// The same for groups of any width: a unit is cvs vectors wide, not necessarily a power of two, and holds G groups; a vector lies in one of them or in
+// two neighbours, its first `cut` channels in group `lg` of the unit.  One team to a block; lanes that whole rows of vectors do not need are idle.
+template <typename T, int V, int G, bool BWD, int ACT, int W, int R>
+__global__ __launch_bounds__(64 * W) void k_gn_column(GnArgs a)
+{
+    constexpr int N = 64 * W;
+    __shared__ float2 chan[BWD ? N * V : 1];
+    __shared__ float sm[BWD ? 2 * G : W * G];
+    const int unit = (int)(blockIdx.x & 7) * a.units_each + (int)(blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= a.units_each || unit >= a.units) return;
+    const int t = threadIdx.x, cvs = a.cvs, width = cvs * V, rows = N / cvs, row = t / cvs, j0 = (t - row * cvs) * V;
+    const int per_sample = a.c / width, n = unit / per_sample, ch0 = (unit - n * per_sample) * width, ch = ch0 + j0, g0 = n * a.groups + ch0 / a.cg;
+    const int lg = G == 1 ? 0 : j0 / a.cg, cut = G == 1 ? V : min(V, (lg + 1) * a.cg - j0), hg = G == 1 ? 0 : min(lg + 1, G - 1);
+    const size_t base = ((size_t)n * a.hw + row) * a.c + ch, step = (size_t)rows * a.c;
+    const T *x = (const T *)a.x + base, *dy = (const T *)a.dy + base, *ys = (const T *)a.y_saved + base;
+    typedef Pack<T, V> P16;
+    words4 qx[R], qd[BWD ? R : 1], qy[ACT == ACT_MASK ? R : 1];
+    auto again = [&]() {   // packed between the passes, as above
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            asm("" : "+v"(qx[i]));
+            if (BWD) asm("" : "+v"(qd[BWD ? i : 0]));
+        }
+    };
+    const int count = row < rows && row < a.hw ? (a.hw - row + rows - 1) / rows : 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+        if (i < count) {
+            qx[i] = *reinterpret_cast<const words4 *>(x + i * step);
+            if (BWD) qd[BWD ? i : 0] = *reinterpret_cast<const words4 *>(dy + i * step);
+            if (ACT == ACT_MASK) qy[ACT == ACT_MASK ? i : 0] = *reinterpret_cast<const words4 *>(ys + i * step);
+        }
+    float scale[V], beta[V], mean[V];
+    load_floats<V>(a.gamma != nullptr ? a.gamma + ch : nullptr, 1.f, scale);
+    load_floats<V>(a.beta != nullptr ? a.beta + ch : nullptr, 0.f, beta);
+    T *out = (T *)a.out + base;
+    if constexpr (!BWD) {
+        // the groups' sums from the channels'
+        auto group_sums = [&](const float (&v)[V], float (&sums)[G]) {
+            float lo = 0.f, hi = 0.f;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                lo += e < cut ? v[e] : 0.f;
+                hi += e < cut ? 0.f : v[e];
+            }
+#pragma unroll
+            for (int k = 0; k < G; ++k) sums[k] = (k == lg ? lo : 0.f) + (k == lg + 1 ? hi : 0.f);
+            team_sum<W, G>(sums, sm);
+        };
+        auto spread = [&](const float (&sums)[G], float (&v)[V]) {
+            float lo = sums[0], hi = sums[0];
+#pragma unroll
+            for (int k = 1; k < G; ++k) { lo = k == lg ? sums[k] : lo; hi = k == hg ? sums[k] : hi; }
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = e < cut ? lo : hi;
+        };
+        float v[V] = {}, stat[G];
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i < count) {
+                const P16 vx = __builtin_bit_cast(P16, qx[i]);
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] += as_f32(vx.v[e]);
+            }
+        again();
+        group_sums(v, stat);
+#pragma unroll
+        for (int k = 0; k < G; ++k) {
+            stat[k] *= a.inv_count;
+            if (t == 0 && a.mean_out != nullptr) a.mean_out[g0 + k] = stat[k];
+        }
+        spread(stat, mean);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i < count) {
+                const P16 vx = __builtin_bit_cast(P16, qx[i]);
+#pragma unroll
+                for (int e = 0; e < V; ++e) { const float d = as_f32(vx.v[e]) - mean[e]; v[e] = fmaf(d, d, v[e]); }
+            }
+        again();
+        group_sums(v, stat);
+#pragma unroll
+        for (int k = 0; k < G; ++k) {
+            stat[k] = 1.f / sqrtf(fmaf(stat[k], a.inv_count, a.eps));
+            if (t == 0 && a.rstd_out != nullptr) a.rstd_out[g0 + k] = stat[k];
+        }
+        spread(stat, v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) scale[e] *= v[e];
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i < count) {
+                const P16 vx = __builtin_bit_cast(P16, qx[i]);
+                P16 r;
+#pragma unroll
+                for (int e = 0; e < V; ++e) r.v[e] = from_f32<T>(activation<ACT>(fmaf(as_f32(vx.v[e]) - mean[e], scale[e], beta[e])));
+                *reinterpret_cast<P16 *>(out + i * step) = r;
+            }
+    } else {
+        if (ACT == ACT_MASK)   // the mask goes into dy at once
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                if (i < count) {
+                    const P16 q = __builtin_bit_cast(P16, qy[ACT == ACT_MASK ? i : 0]);
+                    P16 vd = __builtin_bit_cast(P16, qd[i]);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) vd.v[e] = as_f32(q.v[e]) > 0.f ? vd.v[e] : (T)0;
+                    qd[i] = __builtin_bit_cast(words4, vd);
+                }
+        constexpr int D = ACT == ACT_MASK ? ACT_NONE : ACT;
+        const float mean_lo = a.mean_in[g0 + lg], mean_hi = a.mean_in[g0 + hg], rstd_lo = a.rstd_in[g0 + lg], rstd_hi = a.rstd_in[g0 + hg];
+        float A[V] = {}, B[V] = {};
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            mean[e] = e < cut ? mean_lo : mean_hi;
+            scale[e] *= e < cut ? rstd_lo : rstd_hi;
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i < count) {
+                const P16 vx = __builtin_bit_cast(P16, qx[i]), vd = __builtin_bit_cast(P16, qd[i]);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float xm = as_f32(vx.v[e]) - mean[e], g = gradient<D>(as_f32(vd.v[e]), 0.f, xm, scale[e], beta[e]);
+                    A[e] += g;
+                    B[e] = fmaf(g, xm, B[e]);
+                }
+            }
+        again();
+        float2 v[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = make_float2(A[e], B[e] * (e < cut ? rstd_lo : rstd_hi));
+        add_rows<N, V>(v, cvs, rows, chan);
+        for (int j = t; j < width; j += N) {
+            if (a.n == 1) {
+                if (a.dbeta != nullptr) a.dbeta[ch0 + j] = chan[j].x;
+                if (a.dgamma != nullptr) a.dgamma[ch0 + j] = chan[j].y;
+            } else if (a.grad_blocks > 0) {
+                a.chan[(size_t)n * a.c + ch0 + j] = chan[j];
+            }
+        }
+        if (a.out == nullptr) return;
+        for_teams<N, 2>(G, a.cg,
+            [&](int g, int i, float (&k)[2]) {
+                const int j = g * a.cg + i;
+                const float gm = a.gamma != nullptr ? a.gamma[ch0 + j] : 1.f;
+                k[0] = fmaf(gm, chan[j].x, k[0]);
+                k[1] = fmaf(gm, chan[j].y, k[1]);
+            },
+            [&](int g, float (&k)[2]) { sm[2 * g] = k[0] * a.inv_count; sm[2 * g + 1] = k[1] * a.inv_count; });
+        __syncthreads();
+        const float off_lo = rstd_lo * sm[2 * lg], off_hi = rstd_hi * sm[2 * hg], slope_lo = rstd_lo * rstd_lo * sm[2 * lg + 1], slope_hi = rstd_hi * rstd_hi * sm[2 * hg + 1];
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i < count) {
+                const P16 vx = __builtin_bit_cast(P16, qx[i]), vd = __builtin_bit_cast(P16, qd[i]);
+                P16 r;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float xm = as_f32(vx.v[e]) - mean[e], g = gradient<D>(as_f32(vd.v[e]), 0.f, xm, scale[e], beta[e]);
+                    r.v[e] = from_f32<T>(fmaf(g, scale[e], -fmaf(xm, e < cut ? slope_lo : slope_hi, e < cut ? off_lo : off_hi)));
+                }
+                *reinterpret_cast<P16 *>(out + i * step) = r;
+            }
+    }
+}
+
 // dgamma, dbeta from the units' sums
 __global__ __launch_bounds__(NT) void k_gn_sums(GnArgs a)
 {
@@ -699,31 +868,45 @@ int shape(const dp_group_norm_desc &d, bool bwd, GnArgs &a)
     return V;
 }
 
-// The one-kernel form: wavefronts to a unit (0: two kernels), vectors to a lane, groups of a unit.  Only for groups that are a power of
-// two of whole vectors or divide one.  Measured in both forms (bf16, us, two kernels / one):
+// The one-kernel form: wavefronts to a unit (0: two kernels), vectors to a lane, groups of a unit.  k_gn_unit where groups are a power of two of
+// whole vectors or divide one.  Measured in both forms (bf16, us, two kernels / one):
 //   up to 8 vectors a lane of four wavefronts   8 x 28 x 28 x 512 forward 13.3 / 5.7, backward 16.9 / 13.0; 1 x 14 x 14 x 512 11.1 / 3.5, 11.5 / 5.1
 //   1024 units and more: a wavefront each (32 x 14 x 14 x 1024 forward 17 / 8.3); fewer: four (1 x 14 x 14 x 512 forward 4.9 -> 3.8)
 //   forward eight instead of four, half as many vectors to a lane: 1 x 28 x 28 x 512 5.1 -> 4.2, 16 x 28 x 28 x 512 9.3 -> 8.7; backward has more to
 //     exchange (16 x 28 x 28 x 512 14.9 -> 16.9)
 //   backward of 1024 units of four wavefronts: the pieces of a unit are a fraction of a cache line, and the L2s lose the rest of it
 //     (32 x 28 x 28 x 256, 16-byte pieces 21 / 23; x 512, 32-byte pieces 33.6 / 27.8, with the saved output 39 / 43)
-//   9 to 16 vectors, forward only (backward has two tensors to hold): 8 x 56 x 56 x 256 17.1 / 13.0, but 32 x 56 x 56 x 256 33 / 48
-struct UnitForm { int waves, vectors, groups; };
+//   9 to 16 vectors of four wavefronts: forward eight hold them (8 x 56 x 56 x 256 17.1 / 13.0, but 32 x 56 x 56 x 256 33 / 48); backward pieces of 32 bytes
+//     and more (8 x 40 x 40 x 512 20.3 / 15.5, with the saved output 23.5 / 19.0; 16 x: 29.8 / 24.8, 39 / 41; 16-byte pieces 8 x 64 x 64 x 128 16.6 / 19.2)
+// k_gn_column for the other widths, if a vector lies in two groups at most:
+//   8 x 16 x 16 x 1280 of 32 groups forward 12.1 / 5.1, backward 15.8 / 9.6; 1 x 8 x 8 x 320 9.2 / 4.6, 10.1 / 4.9; 32 x 14 x 14 x 768 15.1 / 7.4, 18.0 / 12.7
+//   9 to 16 vectors: 32 x 28 x 28 x 320 forward 19.9 / 11.2, backward 22.6 / 16.5, but 1024 units 128 x 28 x 28 x 320 36.9 / 40.0, 60 / 65
+//   forward sixteen wavefronts: 32 x 32 x 32 x 320 21.1 / 13.6, 1 x 32 x 32 x 320 10.9 / 9.0; at the limit of their registers and alone a compute unit
+//     draws its piece for too long (40 x 40 x 320: 8 units 10.1 / 10.7, 64 units 14.9 / 12.1)
+struct UnitForm { int waves, vectors, groups, cvs; };   // cvs > 0: k_gn_column
 UnitForm unit_form(const GnArgs &a, int V, bool bwd, bool mask)
 {
-    UnitForm f = {0, 0, 1};
+    UnitForm f = {0, 0, 1, 0};
     if (V == 1) return f;
-    int cvs = 1;
-    if (a.cg % V == 0) cvs = a.cg / V;
-    else if (V % a.cg == 0) f.groups = V / a.cg;
-    else return f;
-    const int64_t units = (int64_t)a.n * (a.c / std::max(a.cg, V));
-    if ((cvs & (cvs - 1)) != 0 || cvs > 64 || units > (1 << 23)) return f;   // a grid has fewer than 2^32 threads
-    const int w1 = ceil_div(a.hw, 64 / cvs), w4 = ceil_div(a.hw, 256 / cvs);
-    if (w1 <= 8 && units >= 1024) { f.waves = 1; f.vectors = 8; }
-    else if (!bwd && w4 <= 8) { f.waves = 8; f.vectors = 4; }
-    else if (bwd && w4 <= 8 && (units < 1024 || (cvs > 1 && !mask))) { f.waves = 4; f.vectors = 8; }
-    else if (!bwd && w4 <= 16 && units <= 512) { f.waves = 8; f.vectors = 8; }
+    const int g = gcd(V, a.cg), width = a.cg / g * V, cvs = width / V;   // channels of the narrowest column of whole groups and vectors
+    const int64_t units = (int64_t)a.n * (a.c / width);
+    if (cvs > 64 || units > (1 << 22)) return f;   // a grid has fewer than 2^32 threads
+    const int w1 = ceil_div(a.hw, 64 / cvs), w4 = ceil_div(a.hw, 256 / cvs), w8 = ceil_div(a.hw, 512 / cvs), w16 = ceil_div(a.hw, 1024 / cvs);
+    f.groups = V / g;
+    if ((f.groups == 1 && (cvs & (cvs - 1)) == 0) || cvs == 1) {
+        if (w1 <= 8 && units >= 1024) { f.waves = 1; f.vectors = 8; }
+        else if (!bwd && w4 <= 8) { f.waves = 8; f.vectors = 4; }
+        else if (bwd && w4 <= 8 && (units < 1024 || (cvs > 1 && !mask))) { f.waves = 4; f.vectors = 8; }
+        else if (!bwd && w4 <= 16 && units <= 512) { f.waves = 8; f.vectors = 8; }
+        else if (bwd && w8 <= 8 && cvs > 1 && units <= (mask ? 256 : 512)) { f.waves = 8; f.vectors = 8; }
+    } else if (f.groups <= 4 && V - g <= a.cg) {   // a vector lies in two groups at most
+        f.cvs = cvs;
+        if (!bwd && w8 <= 4) { f.waves = 8; f.vectors = 4; }
+        else if (bwd && w4 <= 8) { f.waves = 4; f.vectors = 8; }
+        else if (!bwd && w8 <= 8 && units <= 512) { f.waves = 8; f.vectors = 8; }
+        else if (!bwd && w16 <= 8 && (w16 <= 6 || units >= 32) && units <= 512) { f.waves = 16; f.vectors = 8; }
+        else if (bwd && w8 <= 8 && units <= 512) { f.waves = 8; f.vectors = 8; }
+    }
     return f;
 }
 
@@ -739,9 +922,30 @@ void launch_unit(GnArgs a, const UnitForm &f, hipStream_t st)
     a.splits = 1;
     const dim3 grid(8 * a.units_each);
     if (f.waves == 1) hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 1, 8>), grid, dim3(256), 0, st, a);
-    else if constexpr (BWD) hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 4, 8>), grid, dim3(256), 0, st, a);
+    else if constexpr (BWD) {
+        if (f.waves == 4) hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 4, 8>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 8, 8>), grid, dim3(512), 0, st, a);
+    }
     else if (f.vectors == 4) hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 8, 4>), grid, dim3(512), 0, st, a);
     else hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 8, 8>), grid, dim3(512), 0, st, a);
+    if (BWD && a.grad_blocks > 0 && a.n > 1) hipLaunchKernelGGL(k_gn_sums, dim3(a.grad_blocks), dim3(NT), 0, st, a);
+}
+
+template <typename T, int V, int G, bool BWD, int ACT>
+void launch_column(GnArgs a, const UnitForm &f, hipStream_t st)
+{
+    a.cvs = f.cvs;
+    a.units = a.n * (a.c / (f.cvs * V));
+    a.units_each = (a.units + 7) / 8;
+    a.splits = 1;
+    const dim3 grid(8 * a.units_each);
+    if constexpr (BWD) {
+        if (f.waves == 4) hipLaunchKernelGGL((k_gn_column<T, V, G, BWD, ACT, 4, 8>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((k_gn_column<T, V, G, BWD, ACT, 8, 8>), grid, dim3(512), 0, st, a);
+    }
+    else if (f.vectors == 4) hipLaunchKernelGGL((k_gn_column<T, V, G, BWD, ACT, 8, 4>), grid, dim3(512), 0, st, a);
+    else if (f.waves == 8) hipLaunchKernelGGL((k_gn_column<T, V, G, BWD, ACT, 8, 8>), grid, dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((k_gn_column<T, V, G, BWD, ACT, 16, 8>), grid, dim3(1024), 0, st, a);
     if (BWD && a.grad_blocks > 0 && a.n > 1) hipLaunchKernelGGL(k_gn_sums, dim3(a.grad_blocks), dim3(NT), 0, st, a);
 }
 
@@ -750,6 +954,11 @@ void launch(const GnArgs &a, bool apply, hipStream_t st)
 {
     if constexpr (V > 1) {
         const UnitForm f = unit_form(a, V, BWD, ACT == ACT_MASK);
+        if (f.waves > 0 && f.cvs > 0) {
+            if (f.groups == 1) return launch_column<T, V, 1, BWD, ACT>(a, f, st);
+            if (f.groups == 2) return launch_column<T, V, 2, BWD, ACT>(a, f, st);
+            return launch_column<T, V, 4, BWD, ACT>(a, f, st);
+        }
         if (f.waves > 0) {
             if (f.groups == 1) return launch_unit<T, V, 1, BWD, ACT>(a, f, st);
             if (f.groups == 2) return launch_unit<T, V, 2, BWD, ACT>(a, f, st);

@@ -289,3 +289,56 @@ def test_at_the_edges_of_the_forms(env, shape, act, bf16):
     got = k.backward(y, mean, rstd)
     torch.cuda.synchronize()
     k.check_backward(got, y if act == "relu" else None, mean, rstd)
+
+
+# groups that are no power of two of whole vectors: 24, 40, 504 channels (bf16: whole vectors), 12, 20, 28 (two to a column), 6, 10, 14 (four), 5, 7, 3
+# (fp32: four, bf16: eight); images of one pixel, below one row of lanes, at the limits of four, eight and sixteen wavefronts and just past them
+COLUMNS = [(1, 1, 1, 48, 4), (1, 1, 1, 72, 12), (3, 2, 2, 80, 8), (2, 20, 34, 96, 8), (2, 20, 35, 96, 8), (1, 34, 40, 48, 8), (1, 37, 37, 48, 8), (2, 44, 46, 72, 3),
+           (17, 52, 52, 48, 2), (1, 52, 52, 48, 2), (1, 5, 6, 1008, 2), (1, 16, 16, 1008, 2), (9, 7, 7, 640, 32), (5, 9, 9, 160, 16), (40, 6, 6, 160, 8), (4, 11, 12, 112, 8),
+           (2, 13, 9, 56, 2), (3, 13, 11, 40, 8), (2, 13, 11, 56, 8), (2, 13, 11, 24, 8), (70, 3, 5, 320, 32), (1, 31, 33, 320, 32)]
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("act", ["none", "relu", "silu"])
+@pytest.mark.parametrize("shape", COLUMNS, ids=["x".join(map(str, s)) for s in COLUMNS])
+def test_groups_of_any_width(env, shape, act, bf16):
+    k = Case(env, shape, act, bf16, scale=1.5, offset=0.5, affine=shape[1] != 13)
+    y, mean, rstd = k.forward()
+    k.check_forward(y, mean, rstd)
+    got = k.backward(y, mean, rstd)
+    torch.cuda.synchronize()
+    k.check_backward(got, y if act == "relu" else None, mean, rstd)
+    assert torch.equal(k.forward(stats=False)[0], y)
+    for want in ((True, False, False), (False, True, False), (False, True, True)):
+        some = k.backward(y, mean, rstd, want)
+        assert all(not w or torch.equal(a, b) for a, b, w in zip(got, some, want))
+    placed = k.backward(y, mean, rstd, dx=k.dev["dy"])
+    assert all(torch.equal(a, b) for a, b in zip(got, placed))
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("per", [3, 6, 10, 12, 24])
+def test_a_group_keeps_its_infinities(env, per, bf16):
+    """Groups that share vectors: a value that is not finite, in x or in dy, changes its own group and no other."""
+    dp, U, O, synth = env
+    k = Case(env, (2, 9, 9, per * 8, 8), "silu", bf16)
+    y, mean, rstd = k.forward()
+    dx, dgamma, dbeta = k.backward(y, mean, rstd)
+    for g in (0, 1, 2, 7):
+        own = slice(g * per, (g + 1) * per)
+        hit = torch.zeros_like(y, dtype=torch.bool)
+        hit[1, :, :, own] = True
+        for bad in (float("nan"), float("-inf")):
+            k.dev["x"] = upload(U, k.x, bf16)
+            k.dev["x"][1, 4, 5, own.stop - 1] = bad
+            got = k.forward()
+            assert torch.equal(got[0][~hit], y[~hit]) and bool(torch.isnan(got[2][1, g])) and bool(torch.isnan(got[0][1, 4, 5, own.stop - 1]))
+            k.dev["x"] = upload(U, k.x, bf16)
+            k.dev["dy"] = upload(U, k.dy, bf16)
+            k.dev["dy"][1, 4, 5, own.start] = bad
+            got = k.backward(y, mean, rstd)
+            assert torch.equal(got[0][~hit], dx[~hit]) and not bool(torch.isfinite(got[0][1, 0, 0, own]).any())
+            others = torch.ones(per * 8, dtype=torch.bool)
+            others[own.start] = False
+            assert torch.equal(got[1][others], dgamma[others]) and torch.equal(got[2][others], dbeta[others])
+            k.dev["dy"] = upload(U, k.dy, bf16)
