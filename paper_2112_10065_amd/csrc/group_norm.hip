@@ -153,7 +153,8 @@ template <int N, int K, typename F, typename P> __device__ __forceinline__ void 
     }
 }
 
-// First kernel.  Block = (sample, slab of channels, split of the pixels).
+// First kernel.  Block = (sample, slab of channels, split of the pixels).  Bound by HBM: 32 x 224 x 224 x 64 bf16 forward 39 us (205 MB, 5.3 TB/s); backward with
+// SiLU the vector instructions (18 per element) are nearly as long: 32 x 56 x 56 x 256 21.8 us (103 MB, 4.7 TB/s).
 template <typename T, int V, bool BWD, int ACT>
 __global__ __launch_bounds__(NT) void k_gn_reduce(GnArgs a)
 {
@@ -363,6 +364,7 @@ __device__ __forceinline__ void group_results(const GnArgs &a, int n, const Slab
 }
 
 // Second kernel.  Block = (sample, slab of channels, chunk of pixels).  PAST: 1: stores go past the caches, 2: loads too.
+// Bound by HBM: 32 x 224 x 224 x 64 bf16 forward 67 us (411 MB, 6.1 TB/s), 32 x 56 x 56 x 256 backward 29 (154 MB, 5.3 TB/s).
 template <typename T, int V, bool BWD, int ACT, int PAST>
 __global__ __launch_bounds__(NT) void k_gn_apply(GnArgs a)
 {
