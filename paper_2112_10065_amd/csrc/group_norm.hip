@@ -841,9 +841,12 @@ bool slabs_for(int V, GnArgs &a)
     return true;
 }
 
-// Vectors where they fit, single channels else.  Splits: about four blocks per compute unit, at least eight pixels per thread, and few enough
+// Vectors where they fit, single channels else.  Splits: about four blocks per compute unit, at least eight pixels per thread (four at a time
+// backward where blocks are few: 4 x 73 x 80 x 80 fp32 14.2 -> 12.7 us, but 32 x 56 x 56 x 64 23.1 -> 24.4), and few enough
 // that a block of the second kernel reads at most 2048 partials: 16 KB that come from other dies (4096: 4 x 224 x 224 x 64 forward 23 -> 27 us),
 // 4096 where a sample is 16 MB or more and the first kernel's blocks are too long otherwise (2 x 400 x 400 x 64 backward 75 -> 61 us).
+// The second kernel's threads have at least eight pixels too where blocks are many (8 x 56 x 56 x 256 backward 19.4 -> 16.9 us), else four (1 x 80 x 80
+// x 64: with eight 12.5 -> 13.9).
 // The second kernel has half as many blocks for tensors up to 64 MB (4 x 224 x 224 x 64 backward 43.5 -> 38.8 us; 16 x: 118.5 -> 122).
 // Past the caches: outputs above 32 MB, which would be written back while the next kernel reads (32 x 224 x 224 x 64 forward 133 -> 113 us;
 // 25 MB: no difference), and the second reading of inputs above 150 MB, which have left the memory-side cache (113 -> 105; 103 MB: 50.7 -> 53.4).
@@ -856,13 +859,14 @@ int shape(const dp_group_norm_desc &d, bool bwd, GnArgs &a)
     if (!slabs_for(V, a)) slabs_for(V = 1, a);
     const int64_t sample_bytes = (int64_t)a.hw * a.c * (d.io_dtype == DP_BF16 ? 2 : 4), bytes = a.n * sample_bytes;
     const int rows = NT / (a.cs / V), slab_groups = a.per_group == 1 ? a.cs / a.cg : a.per_group;
+    const bool plenty = (int64_t)a.n * a.slabs * ceil_div(a.hw, 8 * rows) >= 256;   // eight pixels a thread leave a block for every compute unit
     int64_t splits = ceil_div(1024, (int64_t)a.n * a.slabs);
-    splits = std::min<int64_t>(splits, ceil_div(a.hw, 8 * rows));
+    splits = std::min<int64_t>(splits, ceil_div(a.hw, (plenty || !bwd ? 8 : 4) * rows));
     splits = std::min<int64_t>(splits, std::max(1, (sample_bytes >= (16 << 20) ? 4096 : 2048) / slab_groups));
     a.split_pixels = ceil_div(a.hw, splits);
     a.splits = ceil_div(a.hw, a.split_pixels);
     int64_t chunks = ceil_div(bytes > (64 << 20) ? 2048 : 1024, (int64_t)a.n * a.slabs);
-    chunks = std::min<int64_t>(chunks, ceil_div(a.hw, 4 * rows));
+    chunks = std::min<int64_t>(chunks, ceil_div(a.hw, (plenty ? 8 : 4) * rows));
     a.chunk_pixels = ceil_div(a.hw, chunks);
     a.chunks = ceil_div(a.hw, a.chunk_pixels);
     a.grad_blocks = bwd ? ceil_div(a.c, 32) : 0;
