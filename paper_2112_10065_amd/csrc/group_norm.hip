@@ -211,10 +211,20 @@ __global__ __launch_bounds__(NT) void k_gn_reduce(GnArgs a)
                 cnt = total;
             }
         }
-        // over the rows and the channels of a cell: deviations from a value near its mean, the first row's mean of its first channel
-        if (row == 0)
-            for_groups<V>(j0, cell_width, [&](int e, int g) { if (j0 + e == g * cell_width) near[g] = mean[e]; });
+        // over the rows and the channels of a cell: deviations from a value near its mean, the first row's mean of its first channel; of
+        // so few pixels that this may be one value, eight rows' (an outlier in front would cost the difference below its bits)
+        const int firsts = p1 - p0 < 4 * rows ? min(min(rows, 8), p1 - p0) : 1;
+        if (row < firsts)
+            for_groups<V>(j0, cell_width, [&](int e, int g) { if (j0 + e == g * cell_width) near[row * s.gs + g] = mean[e]; });
         __syncthreads();
+        if (firsts > 1) {
+            for (int g = t; g < s.gs; g += NT) {
+                float all = near[g];
+                for (int r = 1; r < firsts; ++r) all += near[r * s.gs + g];
+                near[g] = all / (float)firsts;
+            }
+            __syncthreads();
+        }
         float2 v[V];
         if (active)
             for_groups<V>(j0, cell_width, [&](int e, int g) {

@@ -342,3 +342,17 @@ def test_a_group_keeps_its_infinities(env, per, bf16):
             others[own.start] = False
             assert torch.equal(got[1][others], dgamma[others]) and torch.equal(got[2][others], dbeta[others])
             k.dev["dy"] = upload(U, k.dy, bf16)
+
+
+@pytest.mark.parametrize("shape", [(2, 13, 17, 3, 3), (1, 5, 9, 15, 5), (3, 40, 41, 7, 7), (1, 31, 37, 33, 11)])
+def test_an_outlier_in_front(env, shape):
+    """The first value ten spreads away: the sums of squares are still about a value near the mean, and their difference loses a few roundings only."""
+    dp, U, O, synth = env
+    k = Case(env, shape, "none", False)
+    k.x[:, 0, 0, :] = 10.0
+    k.dev["x"] = upload(U, k.x, False)
+    y, mean, rstd = k.forward()
+    want = O.group_norm_fwd(k.x, k.one(k.gamma), k.zero(k.beta), k.groups, EPS, "none")
+    # eight pixels' mean is 1.3 spreads off at most: (1 + 1.3^2) times the rounding of sums of a few hundred terms (1e-6), half of it in the root
+    assert np.abs(U.to_np(rstd) / want[2] - 1).max() <= 1.5e-6
+    k.check_forward(y, mean, rstd)
