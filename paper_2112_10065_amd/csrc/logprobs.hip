@@ -29,11 +29,12 @@ struct LpArgs {
     long long stride;
 };
 
-// Orders scores as whole numbers, larger first: value, then the lower index.  -0 counts as 0, a NaN ranks above everything.
+// Orders scores as whole numbers, larger first: value, then the lower index.  -0 counts as 0, a NaN ranks above everything.  No key has all
+// bits set, also that of a NaN at class 0: the searches that go down from key to key begin there.
 __device__ __forceinline__ unsigned order_of(float z)
 {
     z += 0.f;
-    const unsigned u = z != z ? 0x7fffffffu : __float_as_uint(z);
+    const unsigned u = z != z ? 0x7ffffffeu : __float_as_uint(z);
     return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ unsigned long long key_of(float z, int index) { return (unsigned long long)order_of(z) << 32 | (unsigned)~index; }

@@ -397,3 +397,23 @@ def test_leaders_of_many_long_rows(env, top, bf16):
         got = best[r:r + 103].double()
         assert bool((((got - want).abs() <= tol) | (got == want)).all())
         assert bool((((out[2][r:r + 103] - lse).abs() <= tol[:, 0]) | (out[2][r:r + 103] == lse)).all())
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("classes", [1, 5, 64, 1000, 5001, 40000, 131072])
+def test_nan_in_the_first_class(env, classes, bf16):
+    """NaN ranks above everything also at class 0, in rows of nothing else, and where every class is asked for: no class is lost."""
+    z = scores(env[3], "first", 6, classes, bf16)
+    z[0, 0] = np.nan
+    z[1] = np.nan
+    z[2, 0] = -np.nan
+    z[2, classes - 1] = np.inf
+    z[3, 0] = np.inf
+    z[4, classes // 2:] = np.nan
+    z[4, 0] = np.nan
+    for top in sorted({1, min(classes, 3), min(classes, 64)}):
+        k = Run(env, z, np.zeros(6, np.int32), top, bf16)
+        got = k.forward()
+        at, best = got[4].cpu().numpy(), got[3].cpu().numpy()
+        assert np.array_equal(at, k.O.logprobs(z, k.ids, top)[4])
+        assert np.isnan(best[:5]).all() and np.isfinite(best[5]).all()
