@@ -379,7 +379,8 @@ dp_status dp_logprobs_fwd(const dp_logprobs_desc *desc, const void *z, const int
                           void *hip_stream);
 
 /* dz[r,j] = dlogp[r] * ([j = id] - p_j) - dentropy[r] * p_j * (log p_j + entropy[r]), in io_dtype, with z's strides; may be z's own
- * memory.  lse and entropy are the forward call's.  dlogp (with ids) or dentropy (with entropy) may be NULL, not both. */
+ * memory (not overlap it otherwise).  lse and entropy are the forward call's, of these scores; where |lse| is above 16 its fp32 no longer holds p's last bits,
+ * and the row is summed again.  dlogp (with ids) or dentropy (with entropy) may be NULL, not both. */
 dp_status dp_logprobs_bwd(const dp_logprobs_desc *desc, const void *z, const int32_t *ids_or_null, const float *lse,
                           const float *entropy_or_null, const float *dlogp_or_null, const float *dentropy_or_null, void *dz,
                           void *hip_stream);

@@ -586,9 +586,23 @@ struct LpGradArgs {
     long long stride;
 };
 
-// A row's gradient: p (-dl - de (log p + h)) = exp(d) (k0 - k1 d), d = z - shift, and dl more for the given class.
-// sum(): maximum and sums of the row, asked for by all its threads or none.
-struct RowGrad {
+// exp(d), d in [-128, 0] or a little above, to the last bits: d log2(e) is rounded at its own size, up to 2^-18, so what the product lost goes in behind.
+// For bf16 gradients the product is enough: p is off by 6e-8 of |d|, the output's rounding by 4e-3.
+template <typename T> __device__ __forceinline__ float exp_of(float d)
+{
+    if constexpr (sizeof(T) == 2) return exp_d(d);
+    constexpr float kLost = 1.92596299e-8f;   // log2(e) - kLog2e
+    const float whole = d * kLog2e, x = __builtin_amdgcn_exp2f(whole);
+    return fmaf(x, kLn2 * fmaf(d, kLost, fmaf(d, kLog2e, -whole)), x);
+}
+
+// A row's gradient: p (-dl - de (log p + h)) = exp(d) (k0 - k1 d), d = z - lse, and dl more for the given class.
+// p = exp(d) as long as lse holds its row's sum well enough: its rounding is a relative error of every p, 2^-21 below 16 (that of d itself), but 2^-17 at
+// 250, where 1 - p of a confident row's class is lost.  From 16 on, p = exp(d) / S with S = sum of exp(d), which is 1 up to that error (or up to the
+// number of classes, where lse is too large to hold any of it).
+// sum(): S, asked for by all threads of the row or none.  It is in 64 bits: however the row is spread over blocks, it is the same to the last bit of 32.
+__device__ __forceinline__ bool sums_anew(float lse) { return fabsf(lse) > 16.f && lse != -INFINITY; }
+template <typename T> struct RowGrad {
     float shift, k0, k1, dl;
     int id;   // -1: none
     template <typename F> __device__ __forceinline__ RowGrad(const LpGradArgs &a, int r, F &&sum)
@@ -600,21 +614,20 @@ struct RowGrad {
         dl = a.dlogp != nullptr && valid ? a.dlogp[r] : 0.f;
         if (!valid) id = -1;
         const float de = a.dentropy != nullptr && !none ? a.dentropy[r] : 0.f;
-        // p = exp(z - shift) / s: lse holds both; beyond 256 it loses log s to rounding, and the row is summed again
-        float log_s = 0.f;
-        shift = none ? 0.f : lse;                          // none: every score is -inf, p = 0
-        if (fabsf(lse) > 256.f && !none) {
-            const Soft all = sum();
-            shift = all.m;
-            log_s = logf(all.s);
+        float log_s = 0.f, scale = lse == lse ? 1.f : lse;   // a NaN in the row makes all of it NaN
+        shift = none ? 0.f : lse;                            // none: every score is -inf, p = 0
+        if (sums_anew(lse)) {
+            const float s = (float)sum(lse);
+            log_s = logf(s);
+            scale = 1.f / s;
         }
-        k1 = de * exp_d(-log_s);
-        k0 = -fmaf(de, h - log_s, dl) * exp_d(-log_s);
+        k1 = de * scale;
+        k0 = -fmaf(de, h - log_s, dl) * scale;
     }
     __device__ __forceinline__ float operator()(float z) const
     {
-        const float d = z - shift;
-        return exp_d(d) * fmaf(-k1, fmaxf(d, -128.f), k0);   // exp(d) is 0 long before -128; k1 d must not be infinite then
+        const float d = fmaxf(z - shift, -128.f);   // exp(d) is 0 long before -128; k1 d must not be infinite then
+        return exp_of<T>(d) * fmaf(-k1, d, k0);
     }
 };
 
@@ -630,19 +643,65 @@ __global__ __launch_bounds__(NT) void k_logprobs_grad_rows(LpGradArgs a)
     float v[R];
 #pragma unroll
     for (int j = 0; j < R; ++j) v[j] = as_f32(z[min(lane + 64 * j, a.classes - 1)]);
-    const RowGrad grad(a, r, [&]() {
-        float w[R];
+    const RowGrad<T> grad(a, r, [&](float lse) {
+        double s = 0.0;
 #pragma unroll
-        for (int j = 0; j < R; ++j) w[j] = lane + 64 * j < a.classes ? v[j] : -INFINITY;
-        Soft mine = {-3.402823466e38f, 0.f, 0.f};
-        add_scores<R>(mine, w);
-        return wave_join(mine);
+        for (int j = 0; j < R; ++j) s += lane + 64 * j < a.classes ? (double)exp_d(v[j] - lse) : 0.0;
+        return wave_sum_fast(s);
     });
 #pragma unroll
     for (int j = 0; j < R; ++j) {
         const int i = lane + 64 * j;
         if (i < a.classes) out[i] = from_f32<T>(grad(v[j]) + (i == grad.id ? grad.dl : 0.f));
     }
+}
+
+// Sum of exp(z - lse) over the block's run, the same for all threads.
+template <typename T> __device__ __forceinline__ double block_sum(const Run<T> &run, float lse)
+{
+    constexpr int V = Run<T>::V;
+    __shared__ double part[NT / 64];
+    const int t = threadIdx.x;
+    double s = 0.0;
+    auto add = [&](T z) { s += (double)exp_d(as_f32(z) - lse); };
+    if (run.before(t)) add(run.z[t]);
+    if (run.behind(t) >= 0) add(run.z[run.behind(t)]);
+    int v = t;
+    for (; v + (U - 1) * NT < run.vectors; v += U * NT) {
+        Pack<T, V> q[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) q[u] = run.vector(v + u * NT);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < V; ++e) add(q[u].v[e]);
+    }
+    for (; v < run.vectors; v += NT) {
+        const Pack<T, V> q = run.vector(v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) add(q.v[e]);
+    }
+    s = wave_sum_fast(s);
+    if ((t & 63) == 0) part[t >> 6] = s;
+    __syncthreads();
+    s = part[0];
+    for (int w = 1; w < NT / 64; ++w) s += part[w];
+    return s;
+}
+
+// Where a row is split, the splits' sums of rows that are summed anew lie in dz itself until it is written: each split's part of dz has those of all
+// splits in front (from a multiple of 8 bytes on), and only the block that reads them there writes over them.  Every block summing the whole row instead: 16 x 131072
+// bf16 41 us.
+__device__ __forceinline__ double *sums_in_front(void *part) { return reinterpret_cast<double *>((reinterpret_cast<uintptr_t>(part) + 7) & ~(uintptr_t)7); }
+
+template <typename T>
+__global__ __launch_bounds__(NT) void k_logprobs_grad_sums(LpGradArgs a)
+{
+    const int t = threadIdx.x, r = blockIdx.x / a.splits, split = blockIdx.x - r * a.splits, c0 = split * a.seg;
+    const float lse = a.lse[r];
+    if (!sums_anew(lse)) return;
+    const double s = block_sum(Run<T>((const T *)a.z + (size_t)r * a.stride + c0, min(a.seg, a.classes - c0)), lse);
+    if (t < a.splits) sums_in_front((T *)a.dz + (size_t)r * a.stride + (size_t)t * a.seg)[split] = s;
 }
 
 // Block = (row, split of its classes); in place a row is one block's, which may have to read it twice.
@@ -660,9 +719,12 @@ __global__ __launch_bounds__(NT) void k_logprobs_grad(LpGradArgs a)
     T *out = (T *)a.dz + (size_t)r * a.stride + c0;
     // from a line's boundary on, a wavefront's kilobyte is eight whole lines, also to store (2047 x 50001 bf16: 90 -> 81 us; reads alone do not care)
     const Run<T, 128> run(row, min(a.seg, a.classes - c0));
-    const RowGrad row_grad(a, r, [&]() {
-        const Run<T> whole((const T *)a.z + (size_t)r * a.stride, a.classes);
-        return block_join(scan<false>(whole, Parts(whole.vectors), nullptr));
+    const RowGrad<T> row_grad(a, r, [&](float lse) {
+        if (a.splits == 1) return block_sum(Run<T>(row, a.classes), lse);
+        static_assert(kMaxSplits == 64, "one per lane");
+        const double s = wave_sum_fast((t & 63) < a.splits ? sums_in_front(out)[t & 63] : 0.0);
+        __syncthreads();   // everybody has read before anybody writes there
+        return s;
     });
     const int at = row_grad.id < 0 ? -1 : row_grad.id - c0;   // the given class in this run, if in [0, n)
     const float dl = row_grad.dl;
@@ -698,8 +760,8 @@ __global__ __launch_bounds__(NT) void k_logprobs_grad(LpGradArgs a)
     }
 }
 
-// Splits of a row, in whole vectors, so that all splits of a row are aligned alike: about four blocks per compute unit, at least `least`
-// classes each.
+// Splits of a row, in whole vectors, so that all splits of a row are aligned alike: about four blocks per compute unit, at least half of `least`
+// classes each less 8 for every split (2048: the shortest last one has 1017, and the gradient's sums in front of it take 519 bytes).
 void split_rows(int rows, int classes, int least, int &splits, int &seg)
 {
     const int s = std::max(1, std::min({(1024 + rows - 1) / rows, (classes + least - 1) / least, kMaxSplits}));
@@ -821,9 +883,13 @@ extern "C" dp_status dp_logprobs_bwd(const dp_logprobs_desc *desc, const void *z
         hipLaunchKernelGGL(kernel, grid, dim3(NT), 0, st, a);
         return launched("log-probabilities' gradient");
     }
-    if (dz != z) split_rows(d.rows, d.classes, 2048, a.splits, a.seg);   // 256 x 48000: 9.5 us, one block to a row 11.9
+    // 256 x 48000 bf16: 9.5 us, one block to a row 11.9.  In place there is no room for the splits' sums, and a row that a block sums anew has to be its own until then:
+    // 16 x 131072 14.9 us in place, 5.0 beside (7.5 with all rows summed anew)
+    if (dz != z) split_rows(d.rows, d.classes, 2048, a.splits, a.seg);
     const bool past = (int64_t)d.rows * d.classes * (bf ? 2 : 4) > (32 << 20);
     auto *kernel = bf ? (past ? k_logprobs_grad<bf16_t, true> : k_logprobs_grad<bf16_t, false>) : (past ? k_logprobs_grad<float, true> : k_logprobs_grad<float, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)d.rows * a.splits), dim3(NT), 0, st, a);
+    const dim3 grid((unsigned)d.rows * a.splits);
+    if (a.splits > 1) hipLaunchKernelGGL(bf ? k_logprobs_grad_sums<bf16_t> : k_logprobs_grad_sums<float>, grid, dim3(NT), 0, st, a);
+    hipLaunchKernelGGL(kernel, grid, dim3(NT), 0, st, a);
     return launched("log-probabilities' gradient");
 }

@@ -417,3 +417,44 @@ def test_nan_in_the_first_class(env, classes, bf16):
         at, best = got[4].cpu().numpy(), got[3].cpu().numpy()
         assert np.array_equal(at, k.O.logprobs(z, k.ids, top)[4])
         assert np.isnan(best[:5]).all() and np.isfinite(best[5]).all()
+
+
+@pytest.mark.parametrize("rows,classes", [(16, 10), (16, 1000), (16, 5001), (600, 1500), (1100, 1200), (3, 40000)])
+@pytest.mark.parametrize("offset", [-130.0, 0.0, 14.0, 60.0, 130.0, 200.0, 250.0])
+def test_gradient_keeps_its_bits_at_any_size_of_the_scores(env, offset, rows, classes):
+    """p to a few roundings, whatever the rows are shifted by: half a unit of an lse below 16 (2^-21), the same of z - lse in the tail (twice that
+    from 16 on), the exponential and the sum (5e-7 each): 2.5e-6 of p.  The entropy's bracket is a sum of values up to 16 as well: 3e-6."""
+    z = (scores(env[3], f"bits/{offset}", rows, classes, False) + np.float32(offset)).astype(np.float32)
+    ids = np.arange(rows) % classes
+    k = Run(env, z, ids, 0, False)
+    out = k.forward()
+    d = np.linspace(0.5, 2.0, rows).astype(np.float32)
+    zero = np.zeros(rows)
+    z64 = z.astype(np.float64)
+    logp = z64 - z64.max(axis=1, keepdims=True)
+    logp -= np.log(np.exp(logp).sum(axis=1, keepdims=True))
+    p, h = np.exp(logp), -(np.exp(logp) * logp).sum(axis=1, keepdims=True)
+    for place in (None, k.room.clone()):
+        dz = k.backward(d, None, out[2], None, place=place)[1][:, :classes].cpu().numpy()
+        want = k.O.logprobs_bwd(z, ids, d.astype(np.float64), zero)
+        assert np.all(np.abs(dz - want) <= 2.5e-6 * p * d[:, None] + 6e-8 * np.abs(want) + 1e-37)
+        dz = k.backward(None, d, out[2], out[1])[1][:, :classes].cpu().numpy()
+        want = k.O.logprobs_bwd(z, ids, zero, d.astype(np.float64))
+        assert np.all(np.abs(dz - want) <= (2.5e-6 * (np.abs(logp) + h) + 3e-6) * p * d[:, None] + 6e-8 * np.abs(want) + 1e-37)
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("classes", [20, 1000, 30000])
+def test_gradient_of_confident_rows(env, classes, bf16):
+    """One class far above the others at scores of 40 and 200: 1 - p of the given class is what the others have together."""
+    z = np.zeros((4, classes), np.float32)
+    for r, (top, below) in enumerate(((40.0, 12.0), (200.0, 12.0), (200.0, 10.0), (256.0, 12.0))):
+        z[r] = top - 2 * below
+        z[r, 5], z[r, 7] = top, top - below
+    k = Run(env, z, [5, 5, 7, 5], 0, bf16)
+    out = k.forward()
+    one = np.ones(4, np.float32)
+    dz = k.backward(one, None, out[2], None)[1][:, :classes].float().cpu().numpy()
+    want = k.O.logprobs_bwd(z, k.ids, np.ones(4), np.zeros(4))
+    # p is 1 to four roundings of 1
+    assert np.all(np.abs(dz - want) <= 2.5e-7 + 1e-6 * np.abs(want) + (2.0 ** -8 * np.abs(want) if bf16 else 0))
