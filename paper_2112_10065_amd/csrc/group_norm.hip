@@ -23,7 +23,9 @@ struct GnArgs {
     void *out;                       // y or dx
     float *mean_out, *rstd_out;      // forward, may be null
     float *dgamma, *dbeta;           // backward, may be null
-    float2 *part, *chan;             // partials of cells, of channels (backward)
+    float2 *part, *chan;             // partials of cells, of channels (backward): chan[entry][channel]
+    float2 *runs;                    // sums of runs of entries, if there are many
+    int entries, run;                // entries of chan, entries of a run
     int n, hw, c, groups, cg;
     int cs, slabs;                   // channels of a slab (the last one of all, or of a group, may be narrower), slabs
     int per_group, cells;            // slabs of a group (1: a slab is whole groups), cells in all
@@ -285,32 +287,49 @@ __global__ __launch_bounds__(NT) void k_gn_reduce(GnArgs a)
         [&](int g, float (&k)[2]) { part[g] = make_float2(k[0], k[1]); });
 }
 
-// dgamma, dbeta of 32 channels: eight threads each take every eighth (sample, split), their sums are added in order
-__device__ __forceinline__ void sum_gradients(const GnArgs &a, float *sm)
+// Sums of entries [first, end) of chan for 32 channels, in 64 bits (a chain may be hundreds of terms of one sign long): eight threads each take every eighth
+// entry, their sums are added in order by the first, which gets them.  sm: 2 * NT floats.
+__device__ __forceinline__ bool sum_entries(const float2 *chan, int c, int ch, int first, int end, float *sm, float2 &sum)
 {
-    const int cl = threadIdx.x & 31, part = threadIdx.x >> 5, ch = blockIdx.x * 32 + cl;
-    float s0 = 0.f, s1 = 0.f;
-    if (ch < a.c) {
-        const int total = a.n * a.splits;
-        int i = part;
-        for (; i + 56 < total; i += 64) {
+    const int cl = threadIdx.x & 31, part = threadIdx.x >> 5;
+    double s0 = 0.0, s1 = 0.0;
+    if (ch < c) {
+        int i = first + part;
+        for (; i + 56 < end; i += 64) {
             float2 v[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = a.chan[(size_t)(i + 8 * u) * a.c + ch];
+            for (int u = 0; u < 8; ++u) v[u] = chan[(size_t)(i + 8 * u) * c + ch];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) { s0 += v[u].x; s1 += v[u].y; }
+            for (int u = 0; u < 8; ++u) { s0 += (double)v[u].x; s1 += (double)v[u].y; }
         }
-        for (; i < total; i += 8) { const float2 v = a.chan[(size_t)i * a.c + ch]; s0 += v.x; s1 += v.y; }
+        for (; i < end; i += 8) { const float2 v = chan[(size_t)i * c + ch]; s0 += (double)v.x; s1 += (double)v.y; }
     }
-    sm[threadIdx.x] = s0;
-    sm[NT + threadIdx.x] = s1;
+    sm[threadIdx.x] = (float)s0;
+    sm[NT + threadIdx.x] = (float)s1;
     __syncthreads();
-    if (part == 0 && ch < a.c) {
-        s0 = s1 = 0.f;
-        for (int r = 0; r < 8; ++r) { s0 += sm[r * 32 + cl]; s1 += sm[NT + r * 32 + cl]; }
-        if (a.dbeta != nullptr) a.dbeta[ch] = s0;
-        if (a.dgamma != nullptr) a.dgamma[ch] = s1;
-    }
+    sum = make_float2(0.f, 0.f);
+    if (part != 0 || ch >= c) return false;
+    for (int r = 0; r < 8; ++r) { sum.x += sm[r * 32 + cl]; sum.y += sm[NT + r * 32 + cl]; }
+    return true;
+}
+
+// dgamma, dbeta of 32 channels
+__device__ __forceinline__ void sum_gradients(const GnArgs &a, float *sm)
+{
+    const int ch = blockIdx.x * 32 + (threadIdx.x & 31);
+    float2 sum;
+    if (!sum_entries(a.chan, a.c, ch, 0, a.entries, sm, sum)) return;
+    if (a.dbeta != nullptr) a.dbeta[ch] = sum.x;
+    if (a.dgamma != nullptr) a.dgamma[ch] = sum.y;
+}
+
+// Many entries in two steps: a run of them to a block.
+__global__ __launch_bounds__(NT) void k_gn_runs(GnArgs a)
+{
+    __shared__ float sm[2 * NT];
+    const int run = blockIdx.x / a.grad_blocks, ch = (blockIdx.x - run * a.grad_blocks) * 32 + (threadIdx.x & 31), first = run * a.run;
+    float2 sum;
+    if (sum_entries(a.chan, a.c, ch, first, min(a.entries, first + a.run), sm, sum)) a.runs[(size_t)run * a.c + ch] = sum;
 }
 
 // The two results of each of a slab's groups in st[2 * (group - first)]: forward mean and rstd, backward mean(t) and mean(t * xhat).
@@ -926,8 +945,26 @@ UnitForm unit_form(const GnArgs &a, int V, bool bwd, bool mask)
     return f;
 }
 
+// Entries of the channels' sums of which a block adds up all, and the length of a run beyond (backward, bf16, one step / two: 2049 x 14 x 14 x 64 62 / 52 us, 3000 x 7 x 7 x 64
+// 48 / 33, 1048576 x 1 x 1 x 32 11.7 / 3.7 ms; below, the second kernel has other blocks beside the one).
+constexpr int kEntries = 2048, kRun = 256, kRuns = 1024;
+int run_length(int entries) { return std::max(kRun, ceil_div(entries, kRuns)); }
+size_t runs_bytes(int entries, int c) { return entries <= kEntries ? 0 : (size_t)ceil_div(entries, run_length(entries)) * c * sizeof(float2); }
+// dgamma and dbeta are wanted: leaves at most kRuns entries to sum_gradients
+void sum_runs(GnArgs &a, int entries, hipStream_t st)
+{
+    a.entries = entries;
+    if (entries <= kEntries || a.grad_blocks == 0) return;
+    a.run = run_length(entries);
+    const int runs = ceil_div(entries, a.run);
+    hipLaunchKernelGGL(k_gn_runs, dim3(a.grad_blocks * runs), dim3(NT), 0, st, a);
+    a.chan = a.runs;
+    a.entries = runs;
+}
+
 size_t cell_bytes(const GnArgs &a) { return ((size_t)a.n * a.splits * a.cells * sizeof(float2) + 15) / 16 * 16; }
-size_t part_bytes(const GnArgs &a, bool bwd) { return cell_bytes(a) + (bwd ? (size_t)a.n * a.splits * a.c * sizeof(float2) : 0); }
+size_t chan_bytes(const GnArgs &a) { return (size_t)a.n * a.splits * a.c * sizeof(float2); }
+size_t part_bytes(const GnArgs &a, bool bwd) { return cell_bytes(a) + (bwd ? chan_bytes(a) + runs_bytes(a.n * a.splits, a.c) : 0); }
 
 template <typename T, int V, int K, bool BWD, int ACT>
 void launch_unit(GnArgs a, const UnitForm &f, hipStream_t st)
@@ -935,7 +972,6 @@ void launch_unit(GnArgs a, const UnitForm &f, hipStream_t st)
     a.units = a.n * (a.c / std::max(a.cg, V));
     const int blocks = f.waves == 1 ? (a.units + 3) / 4 : a.units;
     a.units_each = (blocks + 7) / 8;
-    a.splits = 1;
     const dim3 grid(8 * a.units_each);
     if (f.waves == 1) hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 1, 8>), grid, dim3(256), 0, st, a);
     else if constexpr (BWD) {
@@ -944,7 +980,10 @@ void launch_unit(GnArgs a, const UnitForm &f, hipStream_t st)
     }
     else if (f.vectors == 4) hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 8, 4>), grid, dim3(512), 0, st, a);
     else hipLaunchKernelGGL((k_gn_unit<T, V, K, BWD, ACT, 8, 8>), grid, dim3(512), 0, st, a);
-    if (BWD && a.grad_blocks > 0 && a.n > 1) hipLaunchKernelGGL(k_gn_sums, dim3(a.grad_blocks), dim3(NT), 0, st, a);
+    if (BWD && a.grad_blocks > 0 && a.n > 1) {
+        sum_runs(a, a.n, st);
+        hipLaunchKernelGGL(k_gn_sums, dim3(a.grad_blocks), dim3(NT), 0, st, a);
+    }
 }
 
 template <typename T, int V, int G, bool BWD, int ACT>
@@ -953,7 +992,6 @@ void launch_column(GnArgs a, const UnitForm &f, hipStream_t st)
     a.cvs = f.cvs;
     a.units = a.n * (a.c / (f.cvs * V));
     a.units_each = (a.units + 7) / 8;
-    a.splits = 1;
     const dim3 grid(8 * a.units_each);
     if constexpr (BWD) {
         if (f.waves == 4) hipLaunchKernelGGL((k_gn_column<T, V, G, BWD, ACT, 4, 8>), grid, dim3(256), 0, st, a);
@@ -962,11 +1000,14 @@ void launch_column(GnArgs a, const UnitForm &f, hipStream_t st)
     else if (f.vectors == 4) hipLaunchKernelGGL((k_gn_column<T, V, G, BWD, ACT, 8, 4>), grid, dim3(512), 0, st, a);
     else if (f.waves == 8) hipLaunchKernelGGL((k_gn_column<T, V, G, BWD, ACT, 8, 8>), grid, dim3(512), 0, st, a);
     else hipLaunchKernelGGL((k_gn_column<T, V, G, BWD, ACT, 16, 8>), grid, dim3(1024), 0, st, a);
-    if (BWD && a.grad_blocks > 0 && a.n > 1) hipLaunchKernelGGL(k_gn_sums, dim3(a.grad_blocks), dim3(NT), 0, st, a);
+    if (BWD && a.grad_blocks > 0 && a.n > 1) {
+        sum_runs(a, a.n, st);
+        hipLaunchKernelGGL(k_gn_sums, dim3(a.grad_blocks), dim3(NT), 0, st, a);
+    }
 }
 
 template <typename T, int V, bool BWD, int ACT>
-void launch(const GnArgs &a, bool apply, hipStream_t st)
+void launch(GnArgs a, bool apply, hipStream_t st)
 {
     if constexpr (V > 1) {
         const UnitForm f = unit_form(a, V, BWD, ACT == ACT_MASK);
@@ -983,6 +1024,7 @@ void launch(const GnArgs &a, bool apply, hipStream_t st)
         }
     }
     hipLaunchKernelGGL((k_gn_reduce<T, V, BWD, BWD ? ACT : ACT_NONE>), dim3(a.n * a.slabs * a.splits), dim3(NT), 0, st, a);
+    if (BWD) sum_runs(a, a.n * a.splits, st);
     const int blocks = a.grad_blocks + (apply ? a.n * a.slabs * a.chunks : 0);
     if constexpr (V > 1) {
         if (a.past == 2) hipLaunchKernelGGL((k_gn_apply<T, V, BWD, ACT, 2>), dim3(blocks), dim3(NT), 0, st, a);
@@ -1086,6 +1128,7 @@ extern "C" dp_status dp_group_norm_bwd(const dp_group_norm_desc *desc, const voi
     if (s != DP_OK) return s;
     a.x = x; a.dy = dy; a.y_saved = y_saved; a.gamma = gamma; a.beta = beta; a.mean_in = mean; a.rstd_in = rstd;
     a.out = dx; a.dgamma = dgamma; a.dbeta = dbeta; a.part = (float2 *)ws; a.chan = (float2 *)((char *)ws + cell_bytes(a));
+    a.runs = (float2 *)((char *)a.chan + chan_bytes(a));
     launch_type<true>(*desc, V, a, desc->flags == DP_SILU ? ACT_SILU : desc->flags == DP_RELU && y_saved != nullptr ? ACT_MASK : ACT_NONE, dx != nullptr, (hipStream_t)hip_stream);
     return launched("group norm backward");
 }

@@ -356,3 +356,45 @@ def test_an_outlier_in_front(env, shape):
     # eight pixels' mean is 1.3 spreads off at most: (1 + 1.3^2) times the rounding of sums of a few hundred terms (1e-6), half of it in the root
     assert np.abs(U.to_np(rstd) / want[2] - 1).max() <= 1.5e-6
     k.check_forward(y, mean, rstd)
+
+
+def sums_of_one(x, dy, mean, rstd, groups, chunk=4096):
+    """dgamma, dbeta and their magnitudes without activation, in 64 bits on the device."""
+    n, h, w, c = x.shape
+    out = [torch.zeros(c, dtype=torch.float64, device=x.device) for _ in range(4)]
+    for i in range(0, n, chunk):
+        g = dy[i:i + chunk].double()
+        xh = ((x[i:i + chunk].double().view(-1, h * w, groups, c // groups) - mean[i:i + chunk].double()[:, None, :, None]) * rstd[i:i + chunk].double()[:, None, :, None]).view(g.shape)
+        for o, v in zip(out, (g * xh, g, g.abs() * (1 + xh.abs()), g.abs())):
+            o += v.sum(dim=(0, 1, 2))
+    return out
+
+
+def check_sums(env, n, h, w, c, groups, bf16=False):
+    """A gradient of one sign, whose sums' roundings all go one way: 4e-6 of the mass, as elsewhere."""
+    dp, U, _, _ = env
+    gen = torch.Generator(U.DEV).manual_seed(n + h)
+    dt = torch.bfloat16 if bf16 else torch.float32
+    x = torch.randn((n, h, w, c), device=U.DEV, generator=gen).to(dt)
+    dy = torch.full((n, h, w, c), 0.1, device=U.DEV).to(dt)
+    desc = dp.group_norm_desc(n, h, w, c, groups, dp.DP_BF16 if bf16 else dp.DP_F32, 0, EPS)
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd = (torch.empty((n, groups), device=U.DEV) for _ in range(2))
+    dgamma, dbeta = (torch.full((c,), 7.0, device=U.DEV) for _ in range(2))
+    ws = torch.full((max(dp.dp_group_norm_workspace_bytes(desc, p) for p in (0, 1)) + 16,), 0xff, dtype=torch.uint8, device=U.DEV)
+    dp.dp_group_norm_fwd(desc, x, None, None, y, mean, rstd, ws)
+    ws.fill_(0xff)
+    dp.dp_group_norm_bwd(desc, x, dy, None, None, None, mean, rstd, dx, dgamma, dbeta, ws)
+    torch.cuda.synchronize()
+    wg, wb, mg, mb = sums_of_one(x, dy, mean, rstd, groups, max(1, (1 << 25) // (h * w * c)))
+    assert bool(((dgamma - wg).abs() <= 4e-6 * mg).all()) and bool(((dbeta - wb).abs() <= 4e-6 * mb).all())
+    again = [torch.full((c,), 7.0, device=U.DEV) for _ in range(2)]
+    ws.fill_(0xff)
+    dp.dp_group_norm_bwd(desc, x, dy, None, None, None, mean, rstd, None, *again, ws)
+    assert torch.equal(again[0], dgamma) and torch.equal(again[1], dbeta)
+    return x, dy, y, dx, mean, rstd
+
+
+@pytest.mark.parametrize("n,h,w,c,groups", [(65536, 1, 1, 32, 4), (1 << 20, 1, 1, 32, 4), (3001, 5, 3, 24, 2), (40000, 2, 1, 5, 5), (2100, 40, 40, 6, 1), (4099, 3, 3, 40, 4)])
+def test_parameter_gradients_of_very_many_samples(env, n, h, w, c, groups):
+    check_sums(env, n, h, w, c, groups)
