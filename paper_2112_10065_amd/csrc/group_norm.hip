@@ -139,20 +139,18 @@ template <int N, int V, typename X> __device__ __forceinline__ void add_rows(con
     __syncthreads();
 }
 
-// put(g, sums) for each of gs groups, from f(g, i, sums) for i in [0, entries): teams of up to 64 lanes share a group.
-template <int N, int K, typename F, typename P> __device__ __forceinline__ void for_teams(int gs, int entries, F &&f, P &&put)
+// f(g, sub, per, sum) for each of gs groups of about `entries` entries each, by all lanes of a team of `per` up to 64 lanes, this one the sub-th; sum(v) adds
+// up the team's.
+template <int N, typename F> __device__ __forceinline__ void for_teams(int gs, int entries, F &&f)
 {
     int per = 64;
     while (per > 1 && (per * gs > N || per >= 2 * entries)) per >>= 1;
     const int sub = threadIdx.x & (per - 1), step = N / per;
-    for (int g = threadIdx.x / per; g < gs; g += step) {   // whole teams
-        float s[K] = {};
-        for (int i = sub; i < entries; i += per) f(g, i, s);
-        for (int o = per >> 1; o >= 1; o >>= 1)
-#pragma unroll
-            for (int k = 0; k < K; ++k) s[k] += __shfl_xor(s[k], o, 64);
-        if (sub == 0) put(g, s);
-    }
+    for (int g = threadIdx.x / per; g < gs; g += step)   // whole teams
+        f(g, sub, per, [&](float v) {
+            for (int o = per >> 1; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+            return v;
+        });
 }
 
 // First kernel.  Block = (sample, slab of channels, split of the pixels).  Bound by HBM: 32 x 224 x 224 x 64 bf16 forward 39 us (205 MB, 5.3 TB/s); backward with
@@ -213,31 +211,44 @@ __global__ __launch_bounds__(NT) void k_gn_reduce(GnArgs a)
                 cnt = total;
             }
         }
-        // over the rows and the channels of a cell: deviations from a value near its mean, the first row's mean of its first channel; of
-        // so few pixels that this may be one value, eight rows' (an outlier in front would cost the difference below its bits)
-        const int firsts = p1 - p0 < 4 * rows ? min(min(rows, 8), p1 - p0) : 1;
+        // over the rows: deviations from a value near the channel's mean, the first row's mean; a row that lies apart adds its distance's square for
+        // all rows, up to rows / cnt times the sum of squares itself, so where that is more than four times, eight rows' mean
+        const int width = s.width, firsts = (int64_t)4 * (p1 - p0) < (int64_t)rows * rows ? min(min(rows, 8), p1 - p0) : 1;
         if (row < firsts)
-            for_groups<V>(j0, cell_width, [&](int e, int g) { if (j0 + e == g * cell_width) near[row * s.gs + g] = mean[e]; });
+#pragma unroll
+            for (int e = 0; e < V; ++e) near[row * width + j0 + e] = mean[e];
         __syncthreads();
         if (firsts > 1) {
-            for (int g = t; g < s.gs; g += NT) {
-                float all = near[g];
-                for (int r = 1; r < firsts; ++r) all += near[r * s.gs + g];
-                near[g] = all / (float)firsts;
+            for (int j = t; j < width; j += NT) {
+                float all = near[j];
+                for (int r = 1; r < firsts; ++r) all += near[r * width + j];
+                near[j] = all / (float)firsts;
             }
             __syncthreads();
         }
         float2 v[V];
         if (active)
-            for_groups<V>(j0, cell_width, [&](int e, int g) {
-                const float d = mean[e] - near[g];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float d = mean[e] - near[j0 + e];
                 v[e] = make_float2(cnt * d, fmaf(cnt * d, d, m2[e]));
-            });
+            }
         add_rows<NT, V>(v, cvs, rows, sum);
-        const float count = (float)(p1 - p0) * (float)cell_width, inv = 1.f / count;
-        for_teams<NT, 2>(s.gs, cell_width,
-            [&](int g, int i, float (&k)[2]) { k[0] += sum[g * cell_width + i].x; k[1] += sum[g * cell_width + i].y; },
-            [&](int g, float (&k)[2]) { const float off = k[0] * inv; part[g] = make_float2(near[g] + off, fmaxf(fmaf(-k[0], off, k[1]), 0.f)); });
+        // over the channels of a cell: their mean first, then the deviations from it (a channel that lies apart is one of up to 2048)
+        const float count = (float)(p1 - p0), inv = 1.f / count, inv_width = 1.f / (float)cell_width;
+        for_teams<NT>(s.gs, cell_width, [&](int g, int sub, int per, auto &&team_sum_of) {
+            const int first = g * cell_width;
+            const float at = near[first];
+            float off = 0.f, dev = 0.f;
+            for (int i = first + sub; i < first + cell_width; i += per) off += (near[i] - at) + sum[i].x * inv;
+            off = team_sum_of(off) * inv_width;
+            for (int i = first + sub; i < first + cell_width; i += per) {
+                const float o = sum[i].x * inv, d = (near[i] - at) + o - off, own = fmaf(-sum[i].x, o, sum[i].y);
+                dev += fmaf(count * d, d, own < 0.f ? 0.f : own);   // a NaN stays one
+            }
+            dev = team_sum_of(dev);
+            if (sub == 0) part[g] = make_float2(at + off, dev);
+        });
         return;
     }
 
@@ -277,14 +288,17 @@ __global__ __launch_bounds__(NT) void k_gn_reduce(GnArgs a)
     add_rows<NT, V>(A, cvs, rows, sum0);
     add_rows<NT, V>(B, cvs, rows, sum1);
     for (int j = t; j < s.width; j += NT) a.chan[at * a.c + s.ch0 + j] = make_float2(sum0[j], sum1[j]);
-    for_teams<NT, 2>(s.gs, cell_width,
-        [&](int g, int i, float (&k)[2]) {
-            const int j = g * cell_width + i;
+    for_teams<NT>(s.gs, cell_width, [&](int g, int sub, int per, auto &&team_sum_of) {
+        float k0 = 0.f, k1 = 0.f;
+        for (int j = g * cell_width + sub; j < (g + 1) * cell_width; j += per) {
             const float gm = a.gamma != nullptr ? a.gamma[s.ch0 + j] : 1.f;
-            k[0] = fmaf(gm, sum0[j], k[0]);
-            k[1] = fmaf(gm, sum1[j], k[1]);
-        },
-        [&](int g, float (&k)[2]) { part[g] = make_float2(k[0], k[1]); });
+            k0 = fmaf(gm, sum0[j], k0);
+            k1 = fmaf(gm, sum1[j], k1);
+        }
+        k0 = team_sum_of(k0);
+        k1 = team_sum_of(k1);
+        if (sub == 0) part[g] = make_float2(k0, k1);
+    });
 }
 
 // Sums of entries [first, end) of chan for 32 channels, in 64 bits (a chain may be hundreds of terms of one sign long): eight threads each take every eighth
@@ -345,48 +359,61 @@ __device__ __forceinline__ void group_results(const GnArgs &a, int n, const Slab
     const float2 *part = a.part + (size_t)n * a.splits * a.cells + s.g0 * a.per_group;
     for (int g = threadIdx.x / per; g < s.gs; g += step) {   // whole teams
         const float2 *pg = part + g * a.per_group;
-        // deviations from one of the means, so that the sums stay small
-        const float shift = BWD ? 0.f : pg->x;
-        float k0 = 0.f, k1 = 0.f, k2 = 0.f;
-        for (int i0 = sub; i0 < entries; i0 += U * per) {
-            float2 v[U];
-            float w[U];
+        // f(partial, number of values behind it) for this lane's entries
+        auto each = [&](auto &&f) {
+            for (int i0 = sub; i0 < entries; i0 += U * per) {
+                float2 v[U];
+                float w[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int i = min(i0 + u * per, entries - 1), split = a.per_group == 1 ? i : i / a.per_group, sub_cell = i - split * a.per_group;
-                v[u] = pg[(size_t)split * a.cells + sub_cell];
-                const int width = a.per_group == 1 ? a.cg : min(a.cs, a.cg - sub_cell * a.cs);
-                w[u] = (float)(min(a.hw, (split + 1) * a.split_pixels) - split * a.split_pixels) * (float)width;
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (i0 + u * per >= entries) continue;
-                if (BWD) {
-                    k0 += v[u].x;
-                    k1 += v[u].y;
-                } else {
-                    const float d = v[u].x - shift;
-                    k0 = fmaf(w[u], d, k0);
-                    k1 = fmaf(w[u] * d, d, k1);
-                    k2 += v[u].y;
+                for (int u = 0; u < U; ++u) {
+                    const int i = min(i0 + u * per, entries - 1), split = a.per_group == 1 ? i : i / a.per_group, sub_cell = i - split * a.per_group;
+                    v[u] = pg[(size_t)split * a.cells + sub_cell];
+                    const int width = a.per_group == 1 ? a.cg : min(a.cs, a.cg - sub_cell * a.cs);
+                    w[u] = (float)(min(a.hw, (split + 1) * a.split_pixels) - split * a.split_pixels) * (float)width;
                 }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (i0 + u * per < entries) f(v[u], w[u]);
             }
-        }
-        for (int o = per >> 1; o >= 1; o >>= 1) {
-            k0 += __shfl_xor(k0, o, 64);
-            k1 += __shfl_xor(k1, o, 64);
-            if (!BWD) k2 += __shfl_xor(k2, o, 64);
-        }
-        if (sub != 0) continue;
+        };
+        auto team = [&](float v) {
+            for (int o = per >> 1; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+            return v;
+        };
+        float k0 = 0.f, k1 = 0.f;
         if (BWD) {
+            each([&](const float2 &v, float) { k0 += v.x; k1 += v.y; });
+            k0 = team(k0);
+            k1 = team(k1);
+            if (sub != 0) continue;
             st[2 * g] = k0 * a.inv_count;
             st[2 * g + 1] = k1 * a.inv_count;
         } else {
+            // deviations from one of the means, so that the sums stay small; if that one lies apart, once more from the mean
+            const float shift = pg->x;
+            float k2 = 0.f;
+            each([&](const float2 &v, float w) {
+                const float d = v.x - shift;
+                k0 = fmaf(w, d, k0);
+                k1 = fmaf(w * d, d, k1);
+                k2 += v.y;
+            });
+            k0 = team(k0);
+            k1 = team(k1);
+            k2 = team(k2);
             const float off = k0 * a.inv_count;
-            float var = (k2 + k1 - k0 * off) * a.inv_count;
-            if (var < 0.f) var = 0.f;   // a NaN stays one
+            float dev = k2 + fmaf(-k0, off, k1);
+            if (k1 > 4.f * dev) {   // the same for the whole team
+                dev = 0.f;
+                each([&](const float2 &v, float w) {
+                    const float d = v.x - shift - off;
+                    dev += fmaf(w * d, d, v.y);
+                });
+                dev = team(dev);
+            }
+            if (sub != 0) continue;
             st[2 * g] = shift + off;
-            st[2 * g + 1] = 1.f / sqrtf(var + a.eps);
+            st[2 * g + 1] = 1.f / sqrtf(fmaf(dev, a.inv_count, a.eps));   // a NaN stays one
         }
     }
     __syncthreads();
@@ -810,14 +837,17 @@ __global__ __launch_bounds__(64 * W) void k_gn_column(GnArgs a)
             }
         }
         if (a.out == nullptr) return;
-        for_teams<N, 2>(G, a.cg,
-            [&](int g, int i, float (&k)[2]) {
-                const int j = g * a.cg + i;
+        for_teams<N>(G, a.cg, [&](int g, int sub, int per, auto &&team_sum_of) {
+            float k0 = 0.f, k1 = 0.f;
+            for (int j = g * a.cg + sub; j < (g + 1) * a.cg; j += per) {
                 const float gm = a.gamma != nullptr ? a.gamma[ch0 + j] : 1.f;
-                k[0] = fmaf(gm, chan[j].x, k[0]);
-                k[1] = fmaf(gm, chan[j].y, k[1]);
-            },
-            [&](int g, float (&k)[2]) { sm[2 * g] = k[0] * a.inv_count; sm[2 * g + 1] = k[1] * a.inv_count; });
+                k0 = fmaf(gm, chan[j].x, k0);
+                k1 = fmaf(gm, chan[j].y, k1);
+            }
+            k0 = team_sum_of(k0);
+            k1 = team_sum_of(k1);
+            if (sub == 0) { sm[2 * g] = k0 * a.inv_count; sm[2 * g + 1] = k1 * a.inv_count; }
+        });
         __syncthreads();
         const float off_lo = rstd_lo * sm[2 * lg], off_hi = rstd_hi * sm[2 * hg], slope_lo = rstd_lo * rstd_lo * sm[2 * lg + 1], slope_hi = rstd_hi * rstd_hi * sm[2 * hg + 1];
 #pragma unroll

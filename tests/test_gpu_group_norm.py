@@ -398,3 +398,28 @@ def check_sums(env, n, h, w, c, groups, bf16=False):
 @pytest.mark.parametrize("n,h,w,c,groups", [(65536, 1, 1, 32, 4), (1 << 20, 1, 1, 32, 4), (3001, 5, 3, 24, 2), (40000, 2, 1, 5, 5), (2100, 40, 40, 6, 1), (4099, 3, 3, 40, 4)])
 def test_parameter_gradients_of_very_many_samples(env, n, h, w, c, groups):
     check_sums(env, n, h, w, c, groups)
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("shape,where", [((1, 8, 8, 768, 1), "channel"), ((2, 8, 8, 2048, 1), "channel"), ((1, 3, 5, 5000, 1), "channel"), ((1, 8, 8, 4096, 2), "slab"),
+                                         ((1, 256, 256, 16, 1), "front"), ((2, 300, 200, 8, 1), "front"), ((1, 128, 128, 8, 1), "pixel"), ((3, 130, 127, 3, 1), "pixel")])
+def test_outliers_that_lead(env, shape, where, bf16):
+    """The first channel of a wide group, the first channels of a group in parts, the first pixels of a long image or its first one lie a
+    hundred or more spreads away from the rest: every sum of squares is taken about a mean, so rstd is off by the roundings of sums of a few hundred terms,
+    not by these times the number of channels or pixels behind the outlier."""
+    dp, U, O, synth = env
+    k = Case(env, shape, "none", bf16)
+    if where == "channel":
+        k.x[..., 0] += 100
+    elif where == "slab":
+        k.x[..., :64] += 100
+    elif where == "front":
+        k.x.reshape(shape[0], -1, shape[3])[:, :128] += 100
+    else:
+        k.x[:, 0, 0] += 2000
+    k.x = synth.round_bf16(k.x) if bf16 else k.x
+    k.dev["x"] = upload(U, k.x, bf16)
+    y, mean, rstd = k.forward()
+    want = O.group_norm_fwd(k.x, k.one(k.gamma), k.zero(k.beta), k.groups, EPS, "none")
+    assert np.abs(U.to_np(rstd) / want[2] - 1).max() <= 1e-6
+    k.check_forward(y, mean, rstd)
