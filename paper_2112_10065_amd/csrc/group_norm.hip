@@ -260,26 +260,33 @@ __global__ __launch_bounds__(NT) void k_gn_reduce(GnArgs a)
         for_groups<V>(ch, a.cg, [&](int e, int g) { mean[e] = a.mean_in[n * a.groups + g]; rstd[e] = a.rstd_in[n * a.groups + g]; scale[e] = rstd[e] * gamma[e]; });
         const T *dy = (const T *)a.dy + base, *ys = (const T *)a.y_saved + base;
         constexpr int U = 4;
-        for (int p = p0 + row; p < p1; p += U * rows) {
-            Pack<T, V> qx[U], qd[U], qy[U];
+        // sums of 64 pixels, added up: a chain of thousands of one sign would lose 2^-13
+        for (int p = p0 + row; p < p1;) {
+            const int end = min(p1, p + 64 * rows);
+            float A64[V] = {}, B64[V] = {};
+            for (; p < end; p += U * rows) {
+                Pack<T, V> qx[U], qd[U], qy[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const size_t o = (size_t)min(p + u * rows, p1 - 1) * a.c;
-                qx[u] = *reinterpret_cast<const Pack<T, V> *>(x + o);
-                qd[u] = *reinterpret_cast<const Pack<T, V> *>(dy + o);
-                if (ACT == ACT_MASK) qy[u] = *reinterpret_cast<const Pack<T, V> *>(ys + o);
-            }
+                for (int u = 0; u < U; ++u) {
+                    const size_t o = (size_t)min(p + u * rows, p1 - 1) * a.c;
+                    qx[u] = *reinterpret_cast<const Pack<T, V> *>(x + o);
+                    qd[u] = *reinterpret_cast<const Pack<T, V> *>(dy + o);
+                    if (ACT == ACT_MASK) qy[u] = *reinterpret_cast<const Pack<T, V> *>(ys + o);
+                }
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (p + u * rows >= p1) continue;
+                for (int u = 0; u < U; ++u) {
+                    if (p + u * rows >= p1) continue;
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float xm = as_f32(qx[u].v[e]) - mean[e];
-                    const float g = gradient<ACT>(as_f32(qd[u].v[e]), ACT == ACT_MASK ? as_f32(qy[u].v[e]) : 0.f, xm, scale[e], beta[e]);
-                    A[e] += g;
-                    B[e] = fmaf(g, xm, B[e]);
+                    for (int e = 0; e < V; ++e) {
+                        const float xm = as_f32(qx[u].v[e]) - mean[e];
+                        const float g = gradient<ACT>(as_f32(qd[u].v[e]), ACT == ACT_MASK ? as_f32(qy[u].v[e]) : 0.f, xm, scale[e], beta[e]);
+                        A64[e] += g;
+                        B64[e] = fmaf(g, xm, B64[e]);
+                    }
                 }
             }
+#pragma unroll
+            for (int e = 0; e < V; ++e) { A[e] += A64[e]; B[e] += B64[e]; }
         }
 #pragma unroll
         for (int e = 0; e < V; ++e) B[e] *= rstd[e];

@@ -423,3 +423,28 @@ def test_outliers_that_lead(env, shape, where, bf16):
     want = O.group_norm_fwd(k.x, k.one(k.gamma), k.zero(k.beta), k.groups, EPS, "none")
     assert np.abs(U.to_np(rstd) / want[2] - 1).max() <= 1e-6
     k.check_forward(y, mean, rstd)
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("n,h,w,c,groups", [(1, 128, 128, 512, 512), (1, 112, 112, 256, 256), (2, 131, 127, 300, 300), (1, 224, 224, 1024, 512), (1, 96, 97, 250, 250),
+                                            (1, 200, 200, 96, 32), (1, 100, 100, 1536, 256)])
+def test_many_narrow_groups(env, n, h, w, c, groups, bf16):
+    """Norms of a channel or two, images too large for one kernel: statistics and gradients, sums of a gradient of one sign among them."""
+    U = env[1]
+    x, dy, y, dx, mean, rstd = check_sums(env, n, h, w, c, groups, bf16)
+    xd, cg = x.double().view(n, h * w, groups, c // groups), c // groups
+    wm = xd.mean(dim=(1, 3), keepdim=True)
+    wr = 1 / torch.sqrt((xd - wm).square().mean(dim=(1, 3), keepdim=True) + EPS)
+    assert float((mean - wm.view(n, groups)).abs().max()) <= 2e-6 * float(x.abs().max()) and float((rstd / wr.view(n, groups) - 1).abs().max()) <= 2e-6
+    xh, t = (xd - wm) * wr, dy.double().view(xd.shape)
+    big = float(x.abs().max())
+    assert bool(((y.double() - xh.view(x.shape)).abs() <= 8e-6 * big + (2.0 ** -8 * xh.view(x.shape).abs() if bf16 else 0)).all())
+    want = ((t - t.mean(dim=(1, 3), keepdim=True) - xh * (t * xh).mean(dim=(1, 3), keepdim=True)) * wr).view(x.shape)
+    lim = 8e-6 * max(1.0, float(xh.abs().max())) ** 2 * 0.1 * float(wr.max())
+    assert bool(((dx.double() - want).abs() <= lim + (2.0 ** -8 * want.abs() if bf16 else 0)).all())
+
+
+@pytest.mark.parametrize("n,h,w,c,groups", [(1030, 512, 512, 4, 1), (600, 300, 300, 8, 2), (1, 2048, 2048, 32, 32)])
+def test_parameter_gradients_of_many_large_images(env, n, h, w, c, groups):
+    """Thousands of pixels to a thread."""
+    check_sums(env, n, h, w, c, groups)
