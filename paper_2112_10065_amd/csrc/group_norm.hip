@@ -884,11 +884,11 @@ __global__ __launch_bounds__(NT) void k_gn_sums(GnArgs a)
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 int gcd(int a, int b) { return b == 0 ? a : gcd(b, a % b); }
 
-// Slabs for vectors of V channels: as many whole groups as a block's threads cover, or equal parts of a wider group.  False: a
-// group boundary falls inside a vector that a slab cannot avoid.
-bool slabs_for(int V, GnArgs &a)
+// Slabs for vectors of V channels: as many whole groups as fit in `cap` channels, at most what a block's threads cover, or equal parts of a wider
+// group.  False: a group boundary falls inside a vector that a slab cannot avoid.
+bool slabs_for(int V, int cap, GnArgs &a)
 {
-    const int cap = NT * V, unit = V / gcd(V, a.cg);   // groups that fill whole vectors
+    const int unit = V / gcd(V, a.cg);   // groups that fill whole vectors
     a.per_group = 1;
     if (a.c % V != 0) return false;
     if (unit * a.cg <= cap) {
@@ -911,6 +911,9 @@ bool slabs_for(int V, GnArgs &a)
 // backward where blocks are few: 4 x 73 x 80 x 80 fp32 14.2 -> 12.7 us, but 32 x 56 x 56 x 64 23.1 -> 24.4), and few enough
 // that a block of the second kernel reads at most 2048 partials: 16 KB that come from other dies (4096: 4 x 224 x 224 x 64 forward 23 -> 27 us),
 // 4096 where a sample is 16 MB or more and the first kernel's blocks are too long otherwise (2 x 400 x 400 x 64 backward 75 -> 61 us).
+// Where that leaves the first kernel without a block for every compute unit, as with very many narrow groups, slabs are narrower, down to a cache line (us, slabs as wide as
+// a block / narrower: bf16 1 x 224 x 224 x 2048 of 2048 groups forward 3500 / 111, backward 11900 / 211, 1 x 128 x 128 x 512 of 512 71 / 18, 221 / 27; fp32 1 x 112 x 112 x 256 of 256
+// 33 / 14, 110 / 18, 1 x 224 x 224 x 64 of 32 16.5 / 15.8, 28 / 20; bf16 1 x 200 x 200 x 96 of 32 16.0 / 16.5, 25 / 20).
 // The second kernel's threads have at least eight pixels too where blocks are many (8 x 56 x 56 x 256 backward 19.4 -> 16.9 us), else four (1 x 80 x 80
 // x 64: with eight 12.5 -> 13.9).
 // The second kernel has half as many blocks for tensors up to 64 MB (4 x 224 x 224 x 64 backward 43.5 -> 38.8 us; 16 x: 118.5 -> 122).
@@ -922,13 +925,19 @@ int shape(const dp_group_norm_desc &d, bool bwd, GnArgs &a)
     a.eps = d.eps;
     a.inv_count = (float)(1.0 / ((double)a.hw * a.cg));
     int V = d.io_dtype == DP_BF16 ? 8 : 4;
-    if (!slabs_for(V, a)) slabs_for(V = 1, a);
+    if (!slabs_for(V, NT * V, a)) slabs_for(V = 1, NT, a);
     const int64_t sample_bytes = (int64_t)a.hw * a.c * (d.io_dtype == DP_BF16 ? 2 : 4), bytes = a.n * sample_bytes;
+    const int line = d.io_dtype == DP_BF16 ? 64 : 32, partials = sample_bytes >= (16 << 20) ? 4096 : 2048;
+    for (int cap = NT * V / 2; a.per_group == 1 && cap >= std::max(line, V / gcd(V, a.cg) * a.cg); cap /= 2) {
+        const int most = std::max(1, partials / (a.cs / a.cg));
+        if (most >= ceil_div(a.hw, 8 * (NT / (a.cs / V))) || (int64_t)a.n * a.slabs * most >= 256) break;
+        slabs_for(V, cap, a);
+    }
     const int rows = NT / (a.cs / V), slab_groups = a.per_group == 1 ? a.cs / a.cg : a.per_group;
     const bool plenty = (int64_t)a.n * a.slabs * ceil_div(a.hw, 8 * rows) >= 256;   // eight pixels a thread leave a block for every compute unit
     int64_t splits = ceil_div(1024, (int64_t)a.n * a.slabs);
     splits = std::min<int64_t>(splits, ceil_div(a.hw, (plenty || !bwd ? 8 : 4) * rows));
-    splits = std::min<int64_t>(splits, std::max(1, (sample_bytes >= (16 << 20) ? 4096 : 2048) / slab_groups));
+    splits = std::min<int64_t>(splits, std::max(1, partials / slab_groups));
     a.split_pixels = ceil_div(a.hw, splits);
     a.splits = ceil_div(a.hw, a.split_pixels);
     int64_t chunks = ceil_div(bytes > (64 << 20) ? 2048 : 1024, (int64_t)a.n * a.slabs);

@@ -225,3 +225,13 @@ def test_logprobs_valid_calls_reach_the_missing_gpu(dp):
         need = dp.dp_logprobs_workspace_bytes(d)
         assert dp.lib.dp_logprobs_fwd(C.byref(d), A + 4, A, A, None, None, A, A, A, need, None) == dp.DP_ERR_HIP
     assert dp.lib.dp_logprobs_bwd(C.byref(d), A + 4, None, A, A, None, A, A, None) == dp.DP_ERR_HIP
+
+
+def test_many_narrow_groups_have_blocks_for_the_whole_card(dp):
+    """The forward workspace holds 8 bytes for each split of the pixels and group: norms of a channel or two of large images are cut into slabs of down to a cache line of
+    channels, of which a block of the second kernel reads 2048 partials: 32 splits of 64 groups, or 64 of 32."""
+    for io, line in ((dp.DP_BF16, 64), (dp.DP_F32, 32)):
+        for n, h, w, c, groups in ((1, 224, 224, 2048, 2048), (1, 128, 128, 512, 512), (1, 112, 112, 256, 256), (4, 112, 112, 256, 256), (1, 224, 224, 1024, 512), (1, 160, 160, 250, 250)):
+            d = dp.group_norm_desc(n, h, w, c, groups, io)
+            splits = dp.dp_group_norm_workspace_bytes(d, dp.DP_PASS_FWD) // (8 * n * groups)
+            assert n * splits * -(-c // line) >= min(256, n * -(-c // line) * (2048 // line)), (n, h, w, c, groups, io)
