@@ -58,8 +58,12 @@ __device__ __forceinline__ Slab slab_of(const GnArgs &a, int slab)
     return s;
 }
 
-// 1 / (1 + exp(-u))
-__device__ __forceinline__ float sigmoid(float u) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u * -1.44269504f)); }
+// 1 / (1 + exp(-u)); in fp32 tensors to the last bits, down to exp(-88).  bf16 ones lose nothing by the product's rounding.
+template <typename T> __device__ __forceinline__ float sigmoid(float u)
+{
+    const float x = sizeof(T) == 2 ? __builtin_amdgcn_exp2f(-u * kLog2e) : exp_full(__builtin_amdgcn_fmed3f(-u, -128.f, 88.f));
+    return __builtin_amdgcn_rcpf(1.f + x);
+}
 
 template <int V> __device__ __forceinline__ void load_floats(const float *p, float none, float (&v)[V])
 {
@@ -87,19 +91,19 @@ template <int V, typename F> __device__ __forceinline__ void for_groups(int ch, 
 }
 
 // g = dy * derivative of the activation at u = xm * scale + beta
-template <int ACT> __device__ __forceinline__ float gradient(float dy, float ys, float xm, float scale, float beta)
+template <typename T, int ACT> __device__ __forceinline__ float gradient(float dy, float ys, float xm, float scale, float beta)
 {
     if (ACT == ACT_MASK) return ys > 0.f ? dy : 0.f;
     if (ACT == ACT_SILU) {
-        const float u = fmaf(xm, scale, beta), q = sigmoid(u);
+        const float u = fmaf(xm, scale, beta), q = sigmoid<T>(u);
         return dy * (q * fmaf(u, 1.f - q, 1.f));
     }
     return dy;
 }
-template <int ACT> __device__ __forceinline__ float activation(float u)
+template <typename T, int ACT> __device__ __forceinline__ float activation(float u)
 {
     if (ACT == ACT_RELU) return u > 0.f ? u : u == u ? 0.f : u;   // a NaN stays one
-    if (ACT == ACT_SILU) return u * sigmoid(u);
+    if (ACT == ACT_SILU) return u * sigmoid<T>(u);
     return u;
 }
 
@@ -279,7 +283,7 @@ __global__ __launch_bounds__(NT) void k_gn_reduce(GnArgs a)
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
                         const float xm = as_f32(qx[u].v[e]) - mean[e];
-                        const float g = gradient<ACT>(as_f32(qd[u].v[e]), ACT == ACT_MASK ? as_f32(qy[u].v[e]) : 0.f, xm, scale[e], beta[e]);
+                        const float g = gradient<T, ACT>(as_f32(qd[u].v[e]), ACT == ACT_MASK ? as_f32(qy[u].v[e]) : 0.f, xm, scale[e], beta[e]);
                         A64[e] += g;
                         B64[e] = fmaf(g, xm, B64[e]);
                     }
@@ -490,10 +494,10 @@ __global__ __launch_bounds__(NT) void k_gn_apply(GnArgs a)
             for (int e = 0; e < V; ++e) {
                 const float xm = as_f32(qx[u].v[e]) - mean[e];
                 if (BWD) {
-                    const float g = gradient<ACT>(as_f32(qd[u].v[e]), ACT == ACT_MASK ? as_f32(qy[u].v[e]) : 0.f, xm, scale[e], beta[e]);
+                    const float g = gradient<T, ACT>(as_f32(qd[u].v[e]), ACT == ACT_MASK ? as_f32(qy[u].v[e]) : 0.f, xm, scale[e], beta[e]);
                     r.v[e] = from_f32<T>(fmaf(g, scale[e], -fmaf(xm, slope[e], off[e])));
                 } else {
-                    r.v[e] = from_f32<T>(activation<ACT>(fmaf(xm, scale[e], beta[e])));
+                    r.v[e] = from_f32<T>(activation<T, ACT>(fmaf(xm, scale[e], beta[e])));
                 }
             }
             store_vec<Pack<T, V>, PAST != 0>(out + (size_t)(p + u * rows) * a.c, r);
@@ -625,7 +629,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_gn_unit(GnArgs a)
                 const P16 vx = __builtin_bit_cast(P16, qx[i]);
                 P16 r;
 #pragma unroll
-                for (int e = 0; e < V; ++e) r.v[e] = from_f32<T>(activation<ACT>(fmaf(as_f32(vx.v[e]) - mean[e / P], scale[e], beta[e])));
+                for (int e = 0; e < V; ++e) r.v[e] = from_f32<T>(activation<T, ACT>(fmaf(as_f32(vx.v[e]) - mean[e / P], scale[e], beta[e])));
                 *reinterpret_cast<P16 *>(out + i * step) = r;
             }
     } else {
@@ -651,7 +655,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_gn_unit(GnArgs a)
                 const P16 vx = __builtin_bit_cast(P16, qx[i]), vd = __builtin_bit_cast(P16, qd[i]);
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float xm = as_f32(vx.v[e]) - mean[e / P], g = gradient<G>(as_f32(vd.v[e]), 0.f, xm, scale[e], beta[e]);
+                    const float xm = as_f32(vx.v[e]) - mean[e / P], g = gradient<T, G>(as_f32(vd.v[e]), 0.f, xm, scale[e], beta[e]);
                     A[e] += g;
                     B[e] = fmaf(g, xm, B[e]);
                 }
@@ -692,7 +696,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_gn_unit(GnArgs a)
                 P16 r;
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float xm = as_f32(vx.v[e]) - mean[e / P], g = gradient<G>(as_f32(vd.v[e]), 0.f, xm, scale[e], beta[e]);
+                    const float xm = as_f32(vx.v[e]) - mean[e / P], g = gradient<T, G>(as_f32(vd.v[e]), 0.f, xm, scale[e], beta[e]);
                     r.v[e] = from_f32<T>(fmaf(g, scale[e], -fmaf(xm, slope[e / P], off[e / P])));
                 }
                 *reinterpret_cast<P16 *>(out + i * step) = r;
@@ -797,7 +801,7 @@ __global__ __launch_bounds__(64 * W) void k_gn_column(GnArgs a)
                 const P16 vx = __builtin_bit_cast(P16, qx[i]);
                 P16 r;
 #pragma unroll
-                for (int e = 0; e < V; ++e) r.v[e] = from_f32<T>(activation<ACT>(fmaf(as_f32(vx.v[e]) - mean[e], scale[e], beta[e])));
+                for (int e = 0; e < V; ++e) r.v[e] = from_f32<T>(activation<T, ACT>(fmaf(as_f32(vx.v[e]) - mean[e], scale[e], beta[e])));
                 *reinterpret_cast<P16 *>(out + i * step) = r;
             }
     } else {
@@ -825,7 +829,7 @@ __global__ __launch_bounds__(64 * W) void k_gn_column(GnArgs a)
                 const P16 vx = __builtin_bit_cast(P16, qx[i]), vd = __builtin_bit_cast(P16, qd[i]);
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float xm = as_f32(vx.v[e]) - mean[e], g = gradient<D>(as_f32(vd.v[e]), 0.f, xm, scale[e], beta[e]);
+                    const float xm = as_f32(vx.v[e]) - mean[e], g = gradient<T, D>(as_f32(vd.v[e]), 0.f, xm, scale[e], beta[e]);
                     A[e] += g;
                     B[e] = fmaf(g, xm, B[e]);
                 }
@@ -864,7 +868,7 @@ __global__ __launch_bounds__(64 * W) void k_gn_column(GnArgs a)
                 P16 r;
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float xm = as_f32(vx.v[e]) - mean[e], g = gradient<D>(as_f32(vd.v[e]), 0.f, xm, scale[e], beta[e]);
+                    const float xm = as_f32(vx.v[e]) - mean[e], g = gradient<T, D>(as_f32(vd.v[e]), 0.f, xm, scale[e], beta[e]);
                     r.v[e] = from_f32<T>(fmaf(g, scale[e], -fmaf(xm, e < cut ? slope_lo : slope_hi, e < cut ? off_lo : off_hi)));
                 }
                 *reinterpret_cast<P16 *>(out + i * step) = r;

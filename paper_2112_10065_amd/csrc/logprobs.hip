@@ -13,7 +13,6 @@ constexpr int NT = 256;
 
 constexpr int kMaxSplits = 64;
 constexpr int kCandidates = 512;   // of a block, in LDS
-constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
 struct Soft { float m, s, t; };   // maximum, sum exp(d), sum d exp(d) with d = z - m; nothing yet: -FLT_MAX, 0, 0
 
@@ -586,15 +585,8 @@ struct LpGradArgs {
     long long stride;
 };
 
-// exp(d), d in [-128, 0] or a little above, to the last bits: d log2(e) is rounded at its own size, up to 2^-18, so what the product lost goes in behind.
-// For bf16 gradients the product is enough: p is off by 6e-8 of |d|, the output's rounding by 4e-3.
-template <typename T> __device__ __forceinline__ float exp_of(float d)
-{
-    if constexpr (sizeof(T) == 2) return exp_d(d);
-    constexpr float kLost = 1.92596299e-8f;   // log2(e) - kLog2e
-    const float whole = d * kLog2e, x = __builtin_amdgcn_exp2f(whole);
-    return fmaf(x, kLn2 * fmaf(d, kLost, fmaf(d, kLog2e, -whole)), x);
-}
+// exp(d), d in [-128, 0] or a little above.  For bf16 gradients the product is enough: p is off by 6e-8 of |d|, the output's rounding by 4e-3.
+template <typename T> __device__ __forceinline__ float exp_of(float d) { return sizeof(T) == 2 ? exp_d(d) : exp_full(d); }
 
 // A row's gradient: p (-dl - de (log p + h)) = exp(d) (k0 - k1 d), d = z - lse, and dl more for the given class.
 // p = exp(d) as long as lse holds its row's sum well enough: its rounding is a relative error of every p, 2^-21 below 16 (that of d itself), but 2^-17 at

@@ -35,6 +35,15 @@ template <typename T> __device__ __forceinline__ T from_f32(float v);
 template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
 template <> __device__ __forceinline__ bf16_t from_f32<bf16_t>(float v) { return __builtin_bit_cast(bf16_t, (__bf16)v); }   // nearest even
 
+// exp(d), d in [-128, 88], to the last bits: d log2(e) is rounded at its own size (6e-8 of |d| in the result), so what the product lost goes in behind.
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+__device__ __forceinline__ float exp_full(float d)
+{
+    constexpr float kLost = 1.92596299e-8f;   // log2(e) - kLog2e
+    const float whole = d * kLog2e, x = __builtin_amdgcn_exp2f(whole);
+    return fmaf(x, kLn2 * fmaf(d, kLost, fmaf(d, kLog2e, -whole)), x);
+}
+
 // A wavefront's sum or maximum by data-parallel moves, a fifth of the time of six exchanges through LDS: within rows of 16 lanes, then
 // across rows; lane 63 has the result, which every lane gets.  `none`: what an absent neighbour counts as.
 template <int CTRL, int ROWS> __device__ __forceinline__ float moved(float v, float none)

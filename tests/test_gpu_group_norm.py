@@ -448,3 +448,25 @@ def test_many_narrow_groups(env, n, h, w, c, groups, bf16):
 def test_parameter_gradients_of_many_large_images(env, n, h, w, c, groups):
     """Thousands of pixels to a thread."""
     check_sums(env, n, h, w, c, groups)
+
+
+def test_silu_to_the_last_bits(env):
+    """u in single channels by beta alone (gamma 0), from -80 to 80: u * sigmoid(u) and its derivative to a few roundings of fp32 (2^-24 each: two of the
+    exponential, the sum, two of the reciprocal, three products), relative to the value and to the derivative's two terms."""
+    dp, U, _, _ = env
+    for shape, groups in (((1, 1, 1, 4096), 8), ((1, 1, 1, 4100), 1), ((1, 1, 1, 4099), 1)):
+        c = shape[3]
+        beta = np.linspace(-80, 80, c).astype(np.float32)
+        desc = dp.group_norm_desc(*shape, groups, dp.DP_F32, dp.DP_SILU, EPS)
+        x = torch.randn(shape, device=U.DEV, generator=torch.Generator(U.DEV).manual_seed(1))
+        gamma, bd, dy = torch.zeros(c, device=U.DEV), torch.from_numpy(beta).to(U.DEV), torch.ones(shape, device=U.DEV)
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        mean, rstd = (torch.empty((1, groups), device=U.DEV) for _ in range(2))
+        dgamma, dbeta = (torch.empty(c, device=U.DEV) for _ in range(2))
+        ws = U.workspace(max(dp.dp_group_norm_workspace_bytes(desc, p) for p in (0, 1)))
+        dp.dp_group_norm_fwd(desc, x, gamma, bd, y, mean, rstd, ws)
+        dp.dp_group_norm_bwd(desc, x, dy, None, gamma, bd, mean, rstd, dx, dgamma, dbeta, ws)
+        u = beta.astype(np.float64)
+        q, not_q = 1 / (1 + np.exp(-u)), 1 / (1 + np.exp(u))
+        assert np.all(np.abs(U.to_np(y).reshape(-1) - u * q) <= 6e-7 * np.abs(u * q))
+        assert np.all(np.abs(U.to_np(dbeta) - q * (1 + u * not_q)) <= 8e-7 * q * (1 + np.abs(u) * (not_q + 1.2e-7 / 8e-7)))
