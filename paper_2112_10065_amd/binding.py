@@ -257,14 +257,14 @@ class ParamList:
 
 def param_list(params, state=DP_STATE_F32, device=None):
     """Makes the device table of a network's parameters (once; the tensors must stay where they are).  `params`: dicts with the
-    contiguous tensors `grad` and, unless only gradients are listed, `w32`, `m`, `v` (fp32; with DP_STATE_Q8 m and v of one byte per element, e.g.
+    contiguous tensors (all on one GPU) `grad` and, unless only gradients are listed, `w32`, `m`, `v` (fp32; with DP_STATE_Q8 m and v of one byte per element, e.g.
     torch.float8_e4m3fn, and `m_scale`, `v_scale`), optionally `w_bf16` and `weight_decay`.  The table is copied before this returns."""
     n = len(params)
     arr = (dp_param * max(1, n))()
     states = (torch.uint8, torch.int8, getattr(torch, "float8_e4m3fn", torch.uint8)) if state == DP_STATE_Q8 else (torch.float32,)
     kinds = {"grad": (torch.float32,), "w32": (torch.float32,), "w_bf16": (torch.bfloat16,), "m": states, "v": states, "m_scale": (torch.float32,),
              "v_scale": (torch.float32,)}
-    tensors = []
+    tensors, on = [], None
     for i, p in enumerate(params):
         grad = p["grad"]
         count, where, out = grad.numel(), grad.device, arr[i]
@@ -284,7 +284,15 @@ def param_list(params, state=DP_STATE_F32, device=None):
                 raise ValueError(f"parameter {i}: {name} is on another device than grad")
             setattr(out, name, t.data_ptr())
             tensors.append(t)
-        device = where if device is None else device
+        if count > 0:
+            on = where if on is None else on
+            if where != on:
+                raise ValueError(f"parameter {i} is on {where}, those before it on {on}")
+    if device is not None and on is not None:
+        device = torch.device(device)
+        if device.type != on.type or device.index not in (None, on.index):
+            raise ValueError(f"the parameters are on {on}, not on {device}")
+    device = on if on is not None else device
     nbytes = int(lib.dp_param_table_bytes(arr, n))
     host = torch.zeros(max(nbytes, 64), dtype=torch.uint8)
     table = torch.zeros(max(nbytes, 64), dtype=torch.uint8, device=device if device is not None else "cpu")
@@ -294,11 +302,18 @@ def param_list(params, state=DP_STATE_F32, device=None):
     return ParamList(desc, table, tensors)
 
 
+def _check_list(params):
+    """A kernel reads the addresses in the table: host memory there would fault."""
+    if params.desc.n_chunks > 0 and not params.table.is_cuda:
+        raise ValueError(f"the parameters are on {params.table.device}, not on a GPU")
+
+
 def dp_grad_norm_workspace_bytes(params):
     return int(lib.dp_grad_norm_workspace_bytes(C.byref(params.desc)))
 
 
 def dp_grad_norm(params, max_norm, norm_and_scale, ws=None, stream=None):
+    _check_list(params)
     p, b = _ws(ws)
     _check(lib.dp_grad_norm(C.byref(params.desc), max_norm, _ptr(norm_and_scale), p, b, _stream(stream)))
 
@@ -309,6 +324,7 @@ def adamw_hyper(lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0):
 
 def dp_adamw_step(params, hyper, grad_scale=None, stream=None):
     """grad_scale: a device tensor with the factor first in it, e.g. norm_and_scale[1:]; None = 1."""
+    _check_list(params)
     _check(lib.dp_adamw_step(C.byref(params.desc), C.byref(hyper), _ptr(grad_scale), _stream(stream)))
 
 

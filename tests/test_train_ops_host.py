@@ -235,3 +235,21 @@ def test_many_narrow_groups_have_blocks_for_the_whole_card(dp):
             d = dp.group_norm_desc(n, h, w, c, groups, io)
             splits = dp.dp_group_norm_workspace_bytes(d, dp.DP_PASS_FWD) // (8 * n * groups)
             assert n * splits * -(-c // line) >= min(256, n * -(-c // line) * (2048 // line)), (n, h, w, c, groups, io)
+
+
+def test_param_list_is_on_one_gpu(dp):
+    """A kernel reads every address of the table: parameters of two devices are refused, and host memory before anything is launched."""
+    import torch
+    def tensors(device):
+        return {k: torch.zeros(1000, device=device) for k in ("grad", "w32", "m", "v")}
+    here = tensors("cpu")
+    for params, device in (([here, tensors("meta")], None), ([tensors("meta"), here], None), ([here], "meta"), ([here], "cuda"), ([dict(grad=here["grad"]), dict(grad=tensors("meta")["grad"])], None)):
+        with pytest.raises(ValueError, match=" on "):
+            dp.param_list(params, device=device)
+    lst = dp.param_list([here, dict(grad=torch.zeros(0, device="meta"), w32=None, m=None, v=None)])   # without elements: no address
+    assert lst.desc.n_chunks == 1 and lst.desc.updates == 1 and lst.table.device == here["grad"].device
+    out, ws = torch.zeros(4), torch.zeros(4096, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="GPU"):
+        dp.dp_grad_norm(lst, 1.0, out, ws, stream=0)
+    with pytest.raises(ValueError, match="GPU"):
+        dp.dp_adamw_step(lst, dp.adamw_hyper(lr=1e-3), stream=0)
