@@ -968,6 +968,8 @@ int shape(const dp_group_norm_desc &d, bool bwd, GnArgs &a)
 //   9 to 16 vectors: 32 x 28 x 28 x 320 forward 19.9 / 11.2, backward 22.6 / 16.5, but 1024 units 128 x 28 x 28 x 320 36.9 / 40.0, 60 / 65
 //   forward sixteen wavefronts: 32 x 32 x 32 x 320 21.1 / 13.6, 1 x 32 x 32 x 320 10.9 / 9.0; at the limit of their registers and alone a compute unit
 //     draws its piece for too long (40 x 40 x 320: 8 units 10.1 / 10.7, 64 units 14.9 / 12.1)
+// fp32, half the channels to a vector, by the same limits: in 23 of these shapes both ways the one kernel is never slower where it is taken (8 x 28 x 28 x 512 forward 14.7 / 7.1,
+//   backward 18.4 / 13.1, 32 x 28 x 28 x 256 18.4 / 13.5, 28.5 / 24.5, 32 x 14 x 14 x 768 17.5 / 9.4, 25.9 / 19.1, 32 x 32 x 32 x 320 forward 25.3 / 21.2)
 struct UnitForm { int waves, vectors, groups, cvs; };   // cvs > 0: k_gn_column
 UnitForm unit_form(const GnArgs &a, int V, bool bwd, bool mask)
 {

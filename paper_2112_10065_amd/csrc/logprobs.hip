@@ -208,7 +208,9 @@ __device__ __forceinline__ Soft block_join(Soft mine)
 // About 24 scores reach the 20th of 64 maxima; for more than 32 the threads' own 256 serve, four times the instructions.
 // Looking at whole threads' scores again instead of parts: 2047 x 50001 bf16 with 20 leaders 47 -> 55 us, with 64 52 -> 72.
 // Where very many scores reach it (equal ones, or ruled-out classes where fewer than k are left) the list holds those above
-// it and the first k equal to it by index, and where even that does not fit, k rounds take the largest below the one before.
+// it and the first k equal to it by index, and where even that does not fit, k rounds take the largest below the one before: a NaN or +inf in the row, or
+// more than 512 - k scores above the k-th largest of the threads' maxima, as where all leaders are neighbours.  That is the slow case: with k = 64 and scores in
+// rising order bf16 1 x 131072 118 us (in random order 12.6), 2047 x 50001 1900 (47), fp32 64 (12.6), 102 (85).
 template <typename T, typename P>
 __device__ __forceinline__ void block_top(const Run<T> &run, const Parts &parts, const float *part_tops, int base, int k, unsigned top, bool odd, P &&put)
 {
@@ -277,25 +279,17 @@ __device__ __forceinline__ void block_top(const Run<T> &run, const Parts &parts,
         __syncthreads();
         const int log = parts.log, total = lead << log;
         static_assert(NT == 256, "");
-        // a read comes from beyond the L2 where many rows are on their way: two at a time
-        constexpr int W = 1;
-        for (int i0 = t - lane; i0 < total; i0 += W * NT) {   // whole wavefronts
+        for (int i0 = t - lane; i0 < total; i0 += NT) {   // whole wavefronts
             if (*(volatile int *)&count > kCandidates) break;   // it does not fit
-            Pack<T, V> q[W];
-            int v[W];
-#pragma unroll
-            for (int u = 0; u < W; ++u) {
-                const int i = i0 + lane + u * NT;
-                v[u] = run.vectors;
-                if (i < total) {
-                    const int l = leaders[i >> log];
-                    v[u] = (((l >> 8) << log) + (i & ((1 << log) - 1))) * NT + (l & (NT - 1));
-                }
-                if (v[u] < run.vectors) q[u] = run.vector(v[u]);
+            const int i = i0 + lane;
+            Pack<T, V> q;
+            int v = run.vectors;
+            if (i < total) {
+                const int l = leaders[i >> log];
+                v = (((l >> 8) << log) + (i & ((1 << log) - 1))) * NT + (l & (NT - 1));
             }
-#pragma unroll
-            for (int u = 0; u < W; ++u)
-                if (i0 + u * NT < total) append_vectors(q[u], run.first(v[u]), v[u] < run.vectors, from);
+            if (v < run.vectors) q = run.vector(v);
+            append_vectors(q, run.first(v), v < run.vectors, from);
         }
         __syncthreads();
     };
@@ -311,7 +305,7 @@ __device__ __forceinline__ void block_top(const Run<T> &run, const Parts &parts,
         __syncthreads();
         if (t == 0) { count = 0; lead = 0; ties = 0; }
         __syncthreads();
-        if (least != 0xffffffffu) collect(least + 1);
+        collect(least + 1);   // no NaN here: least is below all bits
         fits = count <= kCandidates - k;
         if (fits && wave == 0) {   // one wavefront finds the first k in order
             int found = 0;
@@ -543,7 +537,7 @@ __global__ __launch_bounds__(NT) void k_logprobs_rows(LpArgs a)
             least = 0;
             for (unsigned bit = 0x80000000u; bit != 0; bit >>= 1)
                 if (reach(least | bit) >= a.k) least |= bit;
-            const int above = least == 0xffffffffu ? 0 : reach(least + 1);
+            const int above = reach(least + 1);   // no NaN here: least is below all bits
             int equal = above;
             c = 0;
 #pragma unroll
@@ -762,7 +756,8 @@ void split_rows(int rows, int classes, int least, int &splits, int &seg)
 }
 // Forward, splits cost a second kernel and its wait: one block to a row where there are rows for every compute unit, and for rows that a block
 // reads in the time of that (bf16, five alternatives, us, split / not: 1 x 16384 8.5 / 6.5, 1 x 32000 8.7 / 8.8; 300 x 48000 16.2 / 15.5,
-// 256 x 131072 21.0 / 22.3; 512 x 131072 34 / 32.4).
+// 256 x 131072 21.0 / 22.3; 512 x 131072 34 / 32.4; fp32, with twice the bytes but as many scores to weigh, 1 x 16384 8.1 / 7.3, 1 x 24576 8.4 / 8.7, 64 x 24576 9.6 / 8.8,
+// 64 x 32000 10.0 / 10.1, 300 x 65536 21.8 / 20.5, 300 x 131072 33.5 / 33.9: the same limits).
 void split_forward(int rows, int classes, int &splits, int &seg)
 {
     splits = 1;

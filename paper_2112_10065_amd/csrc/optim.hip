@@ -139,7 +139,7 @@ __device__ __forceinline__ float adam_weight(const AdamArgs &a, float keep, floa
     return fmaf(-a.step_size * m, __builtin_amdgcn_rcpf(fmaf(root, a.inv_root_bc2, a.eps)), keep * w);   // one unit in the last place of the update
 }
 
-// Bound by HBM, 30 bytes per element with the bf16 copy (28 without): 138 M elements 726 us (5.7 TB/s), 25.5 M 140 (5.5; through the caches 147).  All sixteen vectors of a
+// Bound by HBM, 30 bytes per element with the bf16 copy (28 without): 138 M elements 749 us (5.5 TB/s), 25.5 M 140 (5.5; through the caches 147).  All sixteen vectors of a
 // thread are read before the first is used.  PAST: 1: weights and states go past the caches, 2: gradients too.
 template <int PAST> __global__ __launch_bounds__(256) void k_adamw(const Chunk *__restrict__ table, AdamArgs a, const float *__restrict__ scale)
 {
