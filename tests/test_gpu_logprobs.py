@@ -458,3 +458,44 @@ def test_gradient_of_confident_rows(env, classes, bf16):
     want = k.O.logprobs_bwd(z, k.ids, np.ones(4), np.zeros(4))
     # p is 1 to four roundings of 1
     assert np.all(np.abs(dz - want) <= 2.5e-7 + 1e-6 * np.abs(want) + (2.0 ** -8 * np.abs(want) if bf16 else 0))
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("classes,stride,skew,shift", [(2049, 2049, 1, 0), (5001, 5006, 3, 2), (9000, 9003, 5, 1), (40000, 40007, 1, 7), (131073, 131073, 7, 3), (1500, 1501, 1, 1)])
+def test_rows_that_are_summed_anew_at_any_alignment(env, classes, stride, skew, shift, bf16):
+    """Rows of lse below and above 16 in turn, ruled-out classes and rows among them: p as from the definition, nothing written between the rows or around them,
+    dz at an alignment of its own, the same from call to call."""
+    dp, rows = env[0], 7
+    z = scores(env[3], "anew", rows, classes, False) + np.array([0, 60, 0, -200, 500, 60, 0], np.float32)[:, None]
+    z = env[3].round_bf16(z.astype(np.float32)) if bf16 else z.astype(np.float32)
+    z[1, ::3] = -np.inf
+    z[5] = -np.inf
+    ids = np.array([0, classes - 1, 5, 2048 % classes, -1, 3, 1], np.int32)
+    k = Run(env, z, ids, 0, bf16, stride, skew)
+    out = k.forward()
+    d, e = np.linspace(0.5, 2, rows).astype(np.float32), np.linspace(-1, 1, rows).astype(np.float32)
+    dd, ee = torch.from_numpy(d).cuda(), torch.from_numpy(e).cuda()
+    room = torch.full((skew + shift + rows * stride + 64,), 9.0, dtype=k.tdt, device="cuda")
+    dz = room[skew + shift:]
+    dp.dp_logprobs_bwd(k.desc, k.zd, k.idd, out[2], out[1], dd, ee, dz)
+    torch.cuda.synchronize()
+    first = room.clone()
+    got = dz[:rows * stride].view(rows, stride)[:, :classes].float().cpu().numpy()
+    want = k.O.logprobs_bwd(z, ids, d.astype(np.float64), e.astype(np.float64))
+    with np.errstate(invalid="ignore"):
+        logp = z.astype(np.float64) - z.max(axis=1, keepdims=True)
+        logp -= np.log(np.exp(logp).sum(axis=1, keepdims=True))
+    logp[5] = -np.inf
+    p = np.exp(logp)
+    weight = np.where(p > 0, np.abs(np.where(p > 0, logp, 0)), 0)
+    h = (p * weight).sum(axis=1, keepdims=True)
+    # fp32: as above, both terms together; bf16: p = exp(d) by one product, 6e-8 of |d| more, and the output's rounding
+    tol = 2.5e-6 * p * d[:, None] + (2.5e-6 * (weight + h) + 3e-6) * p * np.abs(e)[:, None] + 6e-8 * np.abs(want) + 1e-37
+    if bf16:
+        tol = tol + 6e-8 * weight * p * (d[:, None] + np.abs(e)[:, None] * (weight + h)) + 2.0 ** -8 * np.abs(want)
+    assert np.all(np.abs(got - want) <= tol)
+    keep = torch.ones_like(room, dtype=torch.bool)
+    keep[skew + shift:skew + shift + rows * stride].view(rows, stride)[:, :classes] = False
+    assert bool((room[keep] == 9).all())
+    dp.dp_logprobs_bwd(k.desc, k.zd, k.idd, out[2], out[1], dd, ee, dz)
+    assert torch.equal(room, first)
