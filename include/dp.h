@@ -61,7 +61,9 @@ enum {
                               backward, dx *= [x > 0], in its epilogue (needs the saved input: dp_conv2d_bwd_data_relu,
                               or x in dp_linear_fwd_bwd).  The gradient then reaches the preceding layer already
                               masked, so that layer passes y_saved = NULL and needs no pointwise pass of its own */
-    DP_SILU = 32u          /* group norm only: the activation is u * sigmoid(u) */
+    DP_SILU = 32u,         /* group norm only: the activation is u * sigmoid(u) */
+    DP_QK_NORM = 64u,      /* dp_qk_rotary_*: every head is normalised before it is turned */
+    DP_ROTARY_HALVES = 128u /* dp_qk_rotary_*: channel j is turned with channel j + pairs, not channel 2j with 2j + 1 */
 };
 
 enum { DP_PASS_FWD = 0, DP_PASS_DGRAD = 1, DP_PASS_WGRAD = 2 };
@@ -384,6 +386,86 @@ dp_status dp_logprobs_fwd(const dp_logprobs_desc *desc, const void *z, const int
 dp_status dp_logprobs_bwd(const dp_logprobs_desc *desc, const void *z, const int32_t *ids_or_null, const float *lse,
                           const float *entropy_or_null, const float *dlogp_or_null, const float *dentropy_or_null, void *dz,
                           void *hip_stream);
+
+/* ---- Norm and rotary position of queries and keys ---------------------------------------------------------
+ * Behind the projection that makes queries and keys, in front of their attention.  For every row (token) and every head x [dim] of the
+ * queries and of the keys: with DP_QK_NORM u = x * rstd * gamma, rstd = 1/sqrt(mean x^2 + eps) over the head's channels, else u = x; then its
+ * first 2 P channels are turned, P = pairs[0] + ... + pairs[axes-1]: pair p, which belongs to axis a, by the angle pos[row][a] * freq[p]:
+ *   (y_first, y_second) = (u_first cos - u_second sin, u_first sin + u_second cos)
+ * where pair p is channels 2p and 2p + 1, or with DP_ROTARY_HALVES channels p and p + P.  Channels behind the first 2 P stay as u.
+ * Rows hold their heads side by side; row r of a tensor is at its address + r * stride elements, so that queries and keys may be parts of
+ * one projection's rows.  Strides are whole multiples of 16 bytes; a 0 stands for the heads' own width.  pos is fp32 [rows][axes] (also
+ * fractions), freq 64-bit [P]; the angle is computed in 64 bits, all else in fp32.  gamma_q, gamma_k fp32 [dim], NULL: ones (also where
+ * only one of them is).  rows, kv_heads and each pairs[a] may be 0 (keys are then not looked at). */
+typedef struct {
+    int32_t rows, heads, kv_heads;
+    int32_t dim;                /* a multiple of 8, at most 256 */
+    int32_t axes, pairs[3];     /* axes 1 ... 3; 2 P <= dim */
+    int32_t io_dtype;           /* dp_dtype of every tensor but gamma, pos and freq */
+    uint32_t flags;             /* DP_QK_NORM, DP_ROTARY_HALVES */
+    float eps;                  /* > 0 with DP_QK_NORM */
+    int32_t reserved;           /* 0 */
+    int64_t q_stride, k_stride; /* elements between rows of q and k */
+    int64_t q_out_stride, k_out_stride; /* of q_out and k_out, and of dq_out and dk_out */
+    int64_t dq_stride, dk_stride;
+} dp_qk_rotary_desc;
+
+/* DP_PASS_DGRAD: of dp_qk_rotary_bwd; the forward pass needs none. */
+size_t dp_qk_rotary_workspace_bytes(const dp_qk_rotary_desc *desc, int pass);
+
+/* q_out, k_out may be q's and k's own memory with the same strides (not overlap them otherwise). */
+dp_status dp_qk_rotary_fwd(const dp_qk_rotary_desc *desc, const void *q, const void *k, const float *gamma_q_or_null, const float *gamma_k_or_null,
+                           const float *pos, const double *freq, void *q_out, void *k_out, void *hip_stream);
+
+/* dq, dk: gradients with regard to q and k, from dq_out and dk_out, whose memory they may be (with the same strides); dgamma_q, dgamma_k fp32
+ * [dim], each may be NULL.  q and k are the forward call's inputs and are read only with DP_QK_NORM (else they may be NULL). */
+dp_status dp_qk_rotary_bwd(const dp_qk_rotary_desc *desc, const void *q, const void *k, const float *gamma_q_or_null, const float *gamma_k_or_null,
+                           const float *pos, const double *freq, const void *dq_out, const void *dk_out, void *dq, void *dk,
+                           float *dgamma_q_or_null, float *dgamma_k_or_null, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* ---- Attention ---------------------------------------------------------------------------------------------
+ * For each of n sequences of lq queries and lk keys, head h of the queries reading head h / (heads / kv_heads) of keys and values:
+ *   s_ij = scale * q_i . k_j;  p_ij = exp(s_ij) / sum of exp(s_ij') over the keys that query i sees;  o_i = sum_j p_ij v_j;  lse_i = log of that sum.
+ * Query i stands at place i + lk - lq (the last query at the last key) and sees key j if place - left <= j <= place + right; left or right
+ * -1: no bound on that side.  left = right = -1: all keys; right = 0: causal.  A query that sees nothing has o = 0, lse = -inf and no gradient.
+ * Sequences: without q_starts, sequence b's queries are rows b * q_len ... of which q_lens[b] (NULL: all q_len) are in use; the others' o,
+ * lse and dq are written as 0, -inf and 0 and their other rows not read.  With q_starts [n + 1] (packed), they are the rows q_starts[b] ... q_starts[b+1] - 1, at
+ * most q_len; rows of no sequence are left as they are.  The same for keys with kv_starts, kv_lens, kv_len (dk, dv of unused rows: 0).  The two
+ * sides are independent: packed queries over padded caches, for instance.  Starts and lengths are int32 in DEVICE memory, read by the kernels; starts
+ * ascend.  What lies outside [0, rows] or is longer than q_len / kv_len is cut to them.
+ * Rows hold their heads side by side, row r at r * stride elements; strides are whole multiples of 16 bytes, 0 stands for the heads' own width.
+ * o, dout: o_stride; dq, dk, dv: the strides of q, k, v.  lse: fp32 [heads][q_rows].
+ * Arithmetic: products on the matrix cores with fp32 sums; softmax, its statistics and all sums fp32.  With DP_BF16 the probabilities (and in the
+ * backward pass p and dp's product with it) are rounded to bf16 as operands of the second product.  A value or gradient row that is NaN or infinite
+ * may make NaN also of queries that do not see it, if they share a tile with ones that do; unused rows never do.
+ * Tensors may hold more than 2^31 elements here. */
+typedef struct {
+    int32_t n, q_len, kv_len;   /* n, q_len, kv_len >= 0 */
+    int32_t heads, kv_heads;    /* heads a multiple of kv_heads */
+    int32_t dim;                /* a multiple of 8, at most 128 */
+    int32_t left, right;        /* >= -1 */
+    int32_t io_dtype;
+    float scale;                /* > 0; 0 stands for 1/sqrt(dim) */
+    int64_t q_rows, kv_rows;    /* rows in memory; 0 stands for n * q_len, n * kv_len */
+    int64_t q_stride, k_stride, v_stride, o_stride;
+} dp_attention_desc;
+
+typedef struct {
+    const int32_t *q_starts, *kv_starts; /* [n + 1] or NULL */
+    const int32_t *q_lens, *kv_lens;     /* [n] or NULL; not together with starts of the same side */
+} dp_attention_seqs;
+
+/* DP_PASS_FWD or DP_PASS_DGRAD; 0 is a valid answer. */
+size_t dp_attention_workspace_bytes(const dp_attention_desc *desc, int pass);
+
+/* lse may be NULL.  seqs NULL: n sequences of q_len and kv_len. */
+dp_status dp_attention_fwd(const dp_attention_desc *desc, const void *q, const void *k, const void *v, void *o, float *lse_or_null,
+                           const dp_attention_seqs *seqs_or_null, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* o and lse are the forward call's.  dk and dv of a head of keys are sums over the heads of queries that share it. */
+dp_status dp_attention_bwd(const dp_attention_desc *desc, const void *q, const void *k, const void *v, const void *o, const void *dout,
+                           const float *lse, void *dq, void *dk, void *dv, const dp_attention_seqs *seqs_or_null, void *ws, size_t ws_bytes,
+                           void *hip_stream);
 
 /* ---- Burst-parallel plan of a chain of layers (host only: no GPU call, all pointers host) -------
  * Paper section 4.2, algorithm "Search Linear": dynamic programming over two tables,

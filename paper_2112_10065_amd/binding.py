@@ -11,7 +11,7 @@ from . import build as _build
 
 DP_OK, DP_ERR_NULL, DP_ERR_BAD_DESC, DP_ERR_UNSUPPORTED, DP_ERR_WORKSPACE, DP_ERR_HIP = range(6)
 DP_F32, DP_BF16 = 0, 1
-DP_BIAS, DP_RELU, DP_DETERMINISTIC, DP_DX_F32, DP_RELU_IN, DP_SILU = 1, 2, 4, 8, 16, 32
+DP_BIAS, DP_RELU, DP_DETERMINISTIC, DP_DX_F32, DP_RELU_IN, DP_SILU, DP_QK_NORM, DP_ROTARY_HALVES = 1, 2, 4, 8, 16, 32, 64, 128
 DP_STATE_F32, DP_STATE_Q8 = 0, 1
 DP_LOGPROBS_MAX_TOP = 64
 DP_PASS_FWD, DP_PASS_DGRAD, DP_PASS_WGRAD = 0, 1, 2
@@ -22,6 +22,7 @@ EXPORTS = ["dp_conv2d_workspace_bytes", "dp_linear_workspace_bytes", "dp_conv2d_
            "dp_plan_cost_tables", "dp_plan_graph", "dp_maxpool2x2_fwd", "dp_maxpool2x2_bwd", "dp_softmax_xent", "dp_sgd_update",
            "dp_group_norm_workspace_bytes", "dp_group_norm_fwd", "dp_group_norm_bwd", "dp_param_table_bytes", "dp_param_table_build",
            "dp_grad_norm_workspace_bytes", "dp_grad_norm", "dp_adamw_step", "dp_logprobs_workspace_bytes", "dp_logprobs_fwd", "dp_logprobs_bwd",
+           "dp_qk_rotary_workspace_bytes", "dp_qk_rotary_fwd", "dp_qk_rotary_bwd", "dp_attention_workspace_bytes", "dp_attention_fwd", "dp_attention_bwd",
            "dp_last_error", "dp_version"]
 
 
@@ -83,6 +84,21 @@ class dp_logprobs_desc(C.Structure):
     _fields_ = [("rows", C.c_int32), ("classes", C.c_int32), ("row_stride", C.c_int64), ("top_k", C.c_int32), ("io_dtype", C.c_int32)]
 
 
+class dp_qk_rotary_desc(C.Structure):
+    _fields_ = [(f, C.c_int32) for f in ("rows", "heads", "kv_heads", "dim", "axes")] + [("pairs", C.c_int32 * 3), ("io_dtype", C.c_int32), ("flags", C.c_uint32),
+                                                                                        ("eps", C.c_float), ("reserved", C.c_int32)] + \
+               [(f, C.c_int64) for f in ("q_stride", "k_stride", "q_out_stride", "k_out_stride", "dq_stride", "dk_stride")]
+
+
+class dp_attention_desc(C.Structure):
+    _fields_ = [(f, C.c_int32) for f in ("n", "q_len", "kv_len", "heads", "kv_heads", "dim", "left", "right", "io_dtype")] + [("scale", C.c_float)] + \
+               [(f, C.c_int64) for f in ("q_rows", "kv_rows", "q_stride", "k_stride", "v_stride", "o_stride")]
+
+
+class dp_attention_seqs(C.Structure):
+    _fields_ = [(f, C.c_void_p) for f in ("q_starts", "kv_starts", "q_lens", "kv_lens")]
+
+
 class DpError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"dp status {status}: {msg}")
@@ -132,10 +148,15 @@ def _load():
     lib.dp_adamw_step.argtypes = [P(dp_param_list), P(dp_adamw_hyper), vp, vp]
     lib.dp_logprobs_fwd.argtypes = [P(dp_logprobs_desc), vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.dp_logprobs_bwd.argtypes = [P(dp_logprobs_desc), vp, vp, vp, vp, vp, vp, vp, vp]
-    for name in ("dp_group_norm_fwd", "dp_group_norm_bwd", "dp_param_table_build", "dp_grad_norm", "dp_adamw_step", "dp_logprobs_fwd", "dp_logprobs_bwd"):
+    lib.dp_qk_rotary_fwd.argtypes = [P(dp_qk_rotary_desc)] + [vp] * 9
+    lib.dp_qk_rotary_bwd.argtypes = [P(dp_qk_rotary_desc)] + [vp] * 13 + [sz, vp]
+    lib.dp_attention_fwd.argtypes = [P(dp_attention_desc)] + [vp] * 5 + [P(dp_attention_seqs), vp, sz, vp]
+    lib.dp_attention_bwd.argtypes = [P(dp_attention_desc)] + [vp] * 9 + [P(dp_attention_seqs), vp, sz, vp]
+    for name in ("dp_qk_rotary_fwd", "dp_qk_rotary_bwd", "dp_attention_fwd", "dp_attention_bwd", "dp_group_norm_fwd", "dp_group_norm_bwd", "dp_param_table_build", "dp_grad_norm", "dp_adamw_step", "dp_logprobs_fwd", "dp_logprobs_bwd"):
         getattr(lib, name).restype = C.c_int
     for name, args in (("dp_group_norm_workspace_bytes", [P(dp_group_norm_desc), C.c_int]), ("dp_param_table_bytes", [P(dp_param), i32]),
-                       ("dp_grad_norm_workspace_bytes", [P(dp_param_list)]), ("dp_logprobs_workspace_bytes", [P(dp_logprobs_desc)])):
+                       ("dp_grad_norm_workspace_bytes", [P(dp_param_list)]), ("dp_logprobs_workspace_bytes", [P(dp_logprobs_desc)]),
+                       ("dp_qk_rotary_workspace_bytes", [P(dp_qk_rotary_desc), C.c_int]), ("dp_attention_workspace_bytes", [P(dp_attention_desc), C.c_int])):
         getattr(lib, name).restype, getattr(lib, name).argtypes = sz, args
     for name in ("dp_conv2d_fwd", "dp_conv2d_bwd_data", "dp_conv2d_bwd_filter", "dp_conv2d_bwd_filter_noalloc", "dp_linear_fwd_bwd",
                  "dp_relu_bias_grad", "dp_profile_layer", "dp_trace_begin", "dp_trace_end", "dp_set_override", "dp_set_autotune", "dp_plan_chain",
@@ -344,6 +365,61 @@ def dp_logprobs_fwd(desc, z, ids=None, logp=None, entropy=None, lse=None, top_lo
 
 def dp_logprobs_bwd(desc, z, ids, lse, entropy, dlogp, dentropy, dz, stream=None):
     _check(lib.dp_logprobs_bwd(C.byref(desc), _ptr(z), _ptr(ids), _ptr(lse), _ptr(entropy), _ptr(dlogp), _ptr(dentropy), _ptr(dz), _stream(stream)))
+
+
+def qk_rotary_desc(rows, heads, kv_heads, dim, pairs, io_dtype=DP_BF16, flags=0, eps=1e-6, q_stride=0, k_stride=0, q_out_stride=0, k_out_stride=0,
+                   dq_stride=0, dk_stride=0):
+    """pairs: how many pairs of channels each axis turns, one to three numbers."""
+    axes = len(pairs)
+    return dp_qk_rotary_desc(rows, heads, kv_heads, dim, axes, (C.c_int32 * 3)(*(list(pairs) + [0, 0, 0])[:3]), io_dtype, flags, eps, 0, q_stride, k_stride,
+                             q_out_stride, k_out_stride, dq_stride, dk_stride)
+
+
+def dp_qk_rotary_workspace_bytes(desc, pass_):
+    return int(lib.dp_qk_rotary_workspace_bytes(C.byref(desc), pass_))
+
+
+def dp_qk_rotary_fwd(desc, q, k, gamma_q, gamma_k, pos, freq, q_out, k_out, stream=None):
+    """pos: fp32 [rows, axes]; freq: float64 [sum of pairs]."""
+    _check(lib.dp_qk_rotary_fwd(C.byref(desc), _ptr(q), _ptr(k), _ptr(gamma_q), _ptr(gamma_k), _ptr(pos), _ptr(freq), _ptr(q_out), _ptr(k_out),
+                                _stream(stream)))
+
+
+def dp_qk_rotary_bwd(desc, q, k, gamma_q, gamma_k, pos, freq, dq_out, dk_out, dq, dk, dgamma_q=None, dgamma_k=None, ws=None, stream=None):
+    p, b = _ws(ws)
+    _check(lib.dp_qk_rotary_bwd(C.byref(desc), _ptr(q), _ptr(k), _ptr(gamma_q), _ptr(gamma_k), _ptr(pos), _ptr(freq), _ptr(dq_out), _ptr(dk_out), _ptr(dq),
+                                _ptr(dk), _ptr(dgamma_q), _ptr(dgamma_k), p, b, _stream(stream)))
+
+
+def attention_desc(n, q_len, kv_len, heads, kv_heads, dim, io_dtype=DP_BF16, left=-1, right=-1, scale=0.0, q_rows=0, kv_rows=0, q_stride=0, k_stride=0,
+                   v_stride=0, o_stride=0):
+    return dp_attention_desc(n, q_len, kv_len, heads, kv_heads, dim, left, right, io_dtype, scale, q_rows, kv_rows, q_stride, k_stride, v_stride, o_stride)
+
+
+def attention_seqs(q_starts=None, kv_starts=None, q_lens=None, kv_lens=None):
+    """Where sequences lie and how long they are: contiguous int32 tensors on the GPU, or None.  Keeps the tensors."""
+    for name, t in (("q_starts", q_starts), ("kv_starts", kv_starts), ("q_lens", q_lens), ("kv_lens", kv_lens)):
+        if isinstance(t, torch.Tensor) and (t.dtype != torch.int32 or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous int32 tensor")
+    seqs = dp_attention_seqs(_ptr(q_starts), _ptr(kv_starts), _ptr(q_lens), _ptr(kv_lens))
+    seqs.tensors = (q_starts, kv_starts, q_lens, kv_lens)
+    return seqs
+
+
+def dp_attention_workspace_bytes(desc, pass_):
+    return int(lib.dp_attention_workspace_bytes(C.byref(desc), pass_))
+
+
+def dp_attention_fwd(desc, q, k, v, o, lse=None, seqs=None, ws=None, stream=None):
+    p, b = _ws(ws)
+    _check(lib.dp_attention_fwd(C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), C.byref(seqs) if seqs is not None else None, p, b,
+                                _stream(stream)))
+
+
+def dp_attention_bwd(desc, q, k, v, o, dout, lse, dq, dk, dv, seqs=None, ws=None, stream=None):
+    p, b = _ws(ws)
+    _check(lib.dp_attention_bwd(C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(dout), _ptr(lse), _ptr(dq), _ptr(dk), _ptr(dv),
+                                C.byref(seqs) if seqs is not None else None, p, b, _stream(stream)))
 
 
 def _doubles(rows, n):

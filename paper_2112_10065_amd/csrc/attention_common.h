@@ -1,0 +1,287 @@
+// What the attention kernels share: the call's arguments, the sequences, tiles of rows in LDS and the two kinds of matrix-core products on them.
+//
+// Every kernel keeps 32 columns per wavefront in registers (queries forward and for dq, keys for dk and dv) and lets tiles of rows of the other side pass
+// through LDS.  A product of the first kind, rows x columns over a head's channels, gives lane l the 16 rows 8 (v / 4) + 4 (l / 32) + v % 4 of column
+// l % 32.  Those registers are as they stand the second operand of a product of the second kind, channels x columns over rows: the order of a reduction
+// is free, so its first operand, the tile transposed, is read from LDS in the same order of rows.  Softmax is then a matter of single lanes, and nothing is
+// exchanged but one value between the two halves of a wavefront.
+#pragma once
+#include "../../include/dp.h"
+#include "dma_common.h"
+#include <initializer_list>
+
+void dp_set_error(const char *fmt, ...);   // dp_api.hip
+
+struct AttnSide {
+    const int *starts, *lens;
+    int len;                // the longest sequence's
+    long long rows;
+};
+
+struct AttnArgs {
+    AttnSide q, kv;
+    int n, heads, kv_heads, shared, dim;   // shared: heads of queries to one of keys
+    int left, right;                       // no bound: kFar
+    float scale, scale2;                   // scale2 = scale log2(e)
+    long long q_stride, k_stride, v_stride, o_stride;
+    const void *qp, *kp, *vp, *op_in, *dout;
+    void *op;
+    float *lse;
+    const float *lse_in;
+    void *dq, *dk, *dv;
+    float *lse2, *delta;                   // backward's workspace: lse log2(e) (+inf: sees nothing) and sum dout o, [heads][q_rows]
+    int tiles;                             // of a sequence and head of keys
+    int splits, split_keys;                // forward: keys dealt out to so many blocks, split_keys each
+    float *part_o, *part_ml;               // [split][head][q_rows][dim] and [split][head][q_rows][2]
+};
+
+namespace {
+
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+constexpr int kFar = 1 << 30;
+
+// Rows of one sequence: where they begin, how many are in use, and how many are its own to be written.
+struct Rows { long long first; int used, own; };
+DEVFN Rows rows_of(const AttnSide &s, int b)
+{
+    Rows r;
+    if (s.starts != nullptr) {
+        const long long lo = min(max((long long)s.starts[b], 0ll), s.rows), hi = min(max((long long)s.starts[b + 1], lo), s.rows);
+        r.first = lo;
+        r.used = r.own = (int)min(hi - lo, (long long)s.len);
+    } else {
+        r.first = (long long)b * s.len;
+        r.own = s.len;
+        r.used = s.lens != nullptr ? min(max(s.lens[b], 0), s.len) : s.len;
+    }
+    return r;
+}
+
+// Halves of a wavefront: v of lane l and lane l ^ 32.
+DEVFN float other_half(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+// A tile in LDS: rows of RB bytes (a power of two, channels behind the head's own are zero) in chunks of 16 bytes, chunk c of row r at c ^ swizzle(r), so
+// that reads of one chunk of 16 rows and transposed reads of four rows both touch every bank once.
+template <typename T, int DP> struct Tile {
+    static constexpr int E = 16 / sizeof(T);                              // elements of a chunk
+    static constexpr int RB = (int)sizeof(T) * (sizeof(T) == 2 ? (DP <= 64 ? 64 : 128) : DP <= 32 ? 32 : DP <= 64 ? 64 : 128);
+    static constexpr int CR = RB / 16;                                    // chunks of a row
+    static constexpr int SLICES = DP / (2 * E);                           // of the first kind of product
+    static DEVFN int swizzle(int r)
+    {
+        if constexpr (CR == 8) return ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
+        else if constexpr (CR == 16) return (r & 3) << 2 | ((r >> 2) & 3);
+        else return r & 15;
+    }
+};
+
+// One block's copies of ROWS rows of a matrix into a tile, THREADS threads taking part.  Rows behind the last one and channels behind the head's own become zero.
+template <typename T, int DP, int ROWS, int THREADS> struct TileCopy {
+    using L = Tile<T, DP>;
+    static constexpr int N = ROWS * L::CR / THREADS;   // 16-byte copies of a thread
+    static_assert(ROWS * L::CR % THREADS == 0, "whole copies");
+    unsigned off[N];
+    DEVFN void init(int tid, int dim, long long stride)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = i * THREADS + tid, row = p / L::CR, c = (p % L::CR) ^ L::swizzle(row);
+            off[i] = c * L::E < dim ? (unsigned)(row * (int)stride * (int)sizeof(T) + c * 16) : OOR;
+        }
+    }
+    // rows: how many there are from `base` on (at least 1)
+    DEVFN void issue(const T *base, int rows, int dim, long long stride, unsigned lds, int wave) const
+    {
+        const unsigned bytes = (unsigned)(min(rows, ROWS) - 1) * (unsigned)(stride * (int)sizeof(T)) + (unsigned)dim * (unsigned)sizeof(T);
+        const auto r = make_rsrc(base, bytes);
+#pragma unroll
+        for (int i = 0; i < N; ++i) dma16(r, lds + (i * THREADS + wave * 64) * 16, off[i]);
+    }
+};
+
+template <typename T> struct Mma;
+template <> struct Mma<bf16_t> {
+    static DEVFN void first(const u32x4 &a, const u32x4 &b, f32x16 &c)
+    {
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Mma<float> {
+    static DEVFN void first(const u32x4 &a, const u32x4 &b, f32x16 &c)
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
+    }
+};
+
+// Reads that a pipeline has under way, oldest first: read(i) issues NR reads of item i, wait(i) makes them ready, use(i) takes them.
+template <int NR, int LEFT> DEVFN void wait_reads()
+{
+    constexpr int n = NR * LEFT < 15 ? NR * LEFT : 15;
+    asm volatile("s_waitcnt lgkmcnt(%0)" ::"n"(n));
+}
+DEVFN void tie(u32x4 &v) { asm volatile("" : "+v"(v)); }
+DEVFN void tie(u32x2 &v) { asm volatile("" : "+v"(v)); }
+DEVFN void tie(float &v) { asm volatile("" : "+v"(v)); }
+
+// First kind: acc[block] (32 rows each) += tile rows x `cols`, over the channels.  NB blocks of 32 rows from row `addr` on.
+template <typename T, int DP, int NB, int DEPTH> struct First {
+    using L = Tile<T, DP>;
+    static constexpr int N = NB * L::SLICES, D = DEPTH < N ? DEPTH : N;
+    u32x4 buf[D];
+    template <int I> DEVFN void read(unsigned base, unsigned x)   // base: the lane's row in block 0; x: its swizzled chunk of slice 0, in bytes
+    {
+        constexpr int block = I % NB, s = I / NB;   // neighbours in time add to different sums
+        buf[I % D] = lds_read16<block * 32 * L::RB>(base + (x ^ (unsigned)(s * 32)));
+    }
+    DEVFN void begin(unsigned base, unsigned x) { for_constant<D>([&](auto i) { read<decltype(i)::value>(base, x); }); }
+    DEVFN void run(unsigned base, unsigned x, const u32x4 (&cols)[L::SLICES], f32x16 (&acc)[NB])
+    {
+        for_constant<N>([&](auto ic) {
+            constexpr int i = decltype(ic)::value, left = (N - i < D ? N - i : D) - 1;
+            wait_reads<1, left>();
+            tie(buf[i % D]);
+            Mma<T>::first(buf[i % D], cols[i / NB], acc[i % NB]);
+            if constexpr (i + D < N) read<i + D>(base, x);
+        });
+    }
+};
+
+// The lane's addresses in a tile.
+template <typename T, int DP> struct TileLane {
+    using L = Tile<T, DP>;
+    unsigned row, x;          // first kind: own row's offset, swizzled chunk of slice 0
+    unsigned lo, hi;          // second kind, bf16: rows 4 (l / 32) + (l % 16) / 4 of a slice of 16, and 8 further (relative to 8 rows further)
+    DEVFN void init(int lane)
+    {
+        const int r = lane & 31, h = lane >> 5;
+        row = r * L::RB;
+        x = (unsigned)(h ^ L::swizzle(r)) * 16;
+        if constexpr (sizeof(T) == 2) {
+            const int j = lane & 15, rr = 4 * h + (j >> 2), c = ((lane >> 4) & 1) * 2 + ((j & 3) >> 1);
+            lo = rr * L::RB + (unsigned)(c ^ L::swizzle(rr)) * 16 + (j & 1) * 8;
+            hi = rr * L::RB + (unsigned)(c ^ L::swizzle(rr + 8)) * 16 + (j & 1) * 8;
+        } else {
+            lo = 4 * h * L::RB + (r & 3) * 4;   // the chunk, r / 4, is swizzled by each row
+            hi = h;
+        }
+    }
+};
+
+// Second kind: acc[db] (32 channels each) += tile^T x cols, over NS slices of 16 rows.
+template <typename T, int DP, int NS> struct Second;
+template <int DP, int NS> struct Second<bf16_t, DP, NS> {
+    using L = Tile<bf16_t, DP>;
+    static constexpr int DB = DP / 32, N = NS * DB, D = N < 6 ? N : 6;
+    u32x2 lo[D], hi[D];
+    // a channel block of 32 is 64 bytes on: bits above the two lowest of the chunk's number, which the swizzle may have set
+    template <int I> DEVFN void read(unsigned tile, const TileLane<bf16_t, DP> &l)
+    {
+        constexpr int s = I / DB, db = I % DB;
+        lo[I % D] = lds_read_tr<s * 16 * L::RB>(tile + (l.lo ^ (unsigned)(db * 64)));
+        hi[I % D] = lds_read_tr<(s * 16 + 8) * L::RB>(tile + (l.hi ^ (unsigned)(db * 64)));
+    }
+    DEVFN void begin(unsigned tile, const TileLane<bf16_t, DP> &l) { for_constant<D>([&](auto i) { read<decltype(i)::value>(tile, l); }); }
+    // cols(s): the eight rows of slice s of the lane's column, packed
+    template <typename F> DEVFN void run(unsigned tile, const TileLane<bf16_t, DP> &l, F &&cols, f32x16 (&acc)[DB])
+    {
+        for_constant<N>([&](auto ic) {
+            constexpr int i = decltype(ic)::value, left = (N - i < D ? N - i : D) - 1;
+            wait_reads<2, left>();
+            tie(lo[i % D]);
+            tie(hi[i % D]);
+            const u32x4 a = {lo[i % D].x, lo[i % D].y, hi[i % D].x, hi[i % D].y};
+            Mma<bf16_t>::first(a, cols(std::integral_constant<int, i / DB>{}), acc[i % DB]);
+            if constexpr (i + D < N) read<i + D>(tile, l);
+        });
+    }
+};
+template <int OFF> DEVFN float lds_read4(unsigned addr)
+{
+    float v;
+    asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
+    return v;
+}
+template <int DP, int NS> struct Second<float, DP, NS> {
+    using L = Tile<float, DP>;
+    static constexpr int DB = DP / 32, N = NS * DB;
+    float buf[8];
+    DEVFN void begin(unsigned, const TileLane<float, DP> &) {}
+    // register v of a lane's column is row 8 (v / 4) + 4 half + v % 4: one 32x32x2 product takes v of both halves
+    template <typename F> DEVFN void run(unsigned tile, const TileLane<float, DP> &l, F &&cols, f32x16 (&acc)[DB])
+    {
+        int chunk = (threadIdx.x & 31) >> 2;
+        const int h = (int)l.hi;
+        asm volatile("" : "+v"(chunk));   // addresses are made where they are used: kept for the whole loop they would take registers that the sums need
+        for_constant<N>([&](auto ic) {
+            constexpr int i = decltype(ic)::value, s = i / DB, db = i % DB;
+            for_constant<8>([&](auto ec) {
+                constexpr int e = decltype(ec)::value, row = s * 16 + 8 * (e / 4) + e % 4;   // and 4 h
+                buf[e] = lds_read4<row * L::RB>(tile + l.lo + (unsigned)(((db * 8 + chunk) ^ L::swizzle(row + 4 * h)) * 16));
+            });
+            wait_reads<1, 0>();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) tie(buf[e]);
+            const auto c = cols(std::integral_constant<int, s>{});
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(buf[e], c[e], acc[db], 0, 0, 0);
+        });
+    }
+};
+
+// Eight registers of a column (slice s: 8 s ... 8 s + 7) as the second operand of a product of the second kind.
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+template <typename T> DEVFN auto column(const f32x16 &v, int half)
+{
+    const int b = 8 * half;
+    if constexpr (sizeof(T) == 2) return u32x4{pack_bf16(v[b], v[b + 1]), pack_bf16(v[b + 2], v[b + 3]), pack_bf16(v[b + 4], v[b + 5]), pack_bf16(v[b + 6], v[b + 7])};
+    else return f32x8{v[b], v[b + 1], v[b + 2], v[b + 3], v[b + 4], v[b + 5], v[b + 6], v[b + 7]};
+}
+
+// The lane's column of a matrix as the second operand of products of the first kind: chunks l / 32, l / 32 + 2, ... of its row; zero where there is none.
+template <typename T, int DP> DEVFN void load_column(const T *row, bool on, int dim, int half, u32x4 (&v)[Tile<T, DP>::SLICES])
+{
+    using L = Tile<T, DP>;
+#pragma unroll
+    for (int s = 0; s < L::SLICES; ++s) {
+        const int c = (2 * s + half) * L::E;
+        v[s] = on && c < dim ? *reinterpret_cast<const u32x4 *>(row + c) : u32x4{0, 0, 0, 0};
+    }
+}
+
+// A column's results, channels 32 db + 8 (v / 4) + 4 half + v % 4, times f, to its row.
+template <typename T, int DB> DEVFN void store_column(const f32x16 (&acc)[DB], float f, T *row, int dim, int half)
+{
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int c = db * 32 + 8 * g + 4 * half;
+            if (c >= dim) continue;
+            const float v0 = acc[db][4 * g] * f, v1 = acc[db][4 * g + 1] * f, v2 = acc[db][4 * g + 2] * f, v3 = acc[db][4 * g + 3] * f;
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2 *>(row + c) = u32x2{pack_bf16(v0, v1), pack_bf16(v2, v3)};
+            else *reinterpret_cast<f32x4 *>(row + c) = f32x4{v0, v1, v2, v3};
+        }
+}
+
+template <int N> DEVFN void clear(f32x16 (&acc)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[i][v] = 0.f;
+}
+
+}  // namespace
+
+// attention_fwd.hip: what both passes check and take from the descriptor and the sequences
+dp_status attn_check(const dp_attention_desc *desc, const dp_attention_seqs *seqs);
+void attn_args(const dp_attention_desc &d, const dp_attention_seqs *seqs, AttnArgs &a);
+dp_status attn_pointers(std::initializer_list<const void *> needed, const void *lse, const void *ws);
+dp_status attn_workspace(size_t need, const void *ws, size_t ws_bytes);
+dp_status attn_launched(const char *what);
+size_t attn_bwd_bytes(const dp_attention_desc &d);   // attention_bwd.hip

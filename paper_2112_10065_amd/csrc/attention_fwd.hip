@@ -1,0 +1,353 @@
+// Attention, forward: o = softmax(scale q k^T) v, one pass over the keys with the running maximum and sum of every query's softmax.
+//
+// Columns of a wavefront are pairs (query, head) of the heads that share one head of keys, so that a single token's heads are read against the
+// cache together and neighbouring columns share their keys.  Per tile of keys: S = K q (lane: one query, half of the tile's keys in registers), p = exp2(S scale2 - m),
+// o += V^T p.  m is a maximum of S scale2 that may be up to 8 short of the true one: p <= 2^8 costs 32-bit sums nothing, and o is rescaled
+// only in the few tiles where the maximum grows by more.
+#include "attention_common.h"
+#include <algorithm>
+#include <cmath>
+
+namespace {
+
+constexpr float kSlack = 8.f;
+
+template <typename T> constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;   // of a tile
+
+template <typename T, int DP, int NW, bool SPLIT> __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void k_attention(AttnArgs a)
+{
+    using L = Tile<T, DP>;
+    constexpr int KT = kKeys<T>, NB = KT / 32, DB = DP / 32, BYTES = KT * L::RB, COLS = NW * 32;
+    __shared__ alignas(1024) char s_tiles[4 * BYTES];   // K and V, two stages of each
+    const int lane = threadIdx.x & 63, wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    int id = logical_block(blockIdx.x, gridDim.x);
+    const int split = SPLIT ? id % a.splits : 0;
+    if (SPLIT) id /= a.splits;
+    const int bh = id / a.tiles, hk = bh % a.kv_heads, b = bh / a.kv_heads;
+    const int col0 = (a.tiles - 1 - id % a.tiles) * COLS;   // causal: the longest first
+    const Rows rq = rows_of(a.q, b), rk = rows_of(a.kv, b);
+    if (col0 >= rq.own * a.shared) return;
+
+    const int col = col0 + wave * 32 + (lane & 31), i = col / a.shared, head = hk * a.shared + col % a.shared;
+    const bool own = i < rq.own, on = i < rq.used;
+    const int ahead = rk.used - rq.used;
+    // the keys that the block's queries see, and the wavefront's
+    const int wcol = col0 + wave * 32, last = rq.used * a.shared - 1;
+    long long lo = 0, hi = 0;
+    const long long i0 = col0 / a.shared, i1 = min(col0 + COLS - 1, last) / a.shared, w0 = wcol / a.shared, w1 = min(wcol + 31, last) / a.shared;
+    if (col0 <= last) {
+        lo = max(0ll, i0 + ahead - a.left);
+        hi = min((long long)rk.used, i1 + ahead + a.right + 1);
+    }
+    if (SPLIT) {
+        lo = max(lo, (long long)split * a.split_keys);
+        hi = min(hi, (long long)(split + 1) * a.split_keys);
+    }
+    const int first = (int)lo, keys = (int)max(0ll, hi - lo);
+    const long long row = rq.first + i;
+
+    u32x4 q[L::SLICES];
+    load_column<T, DP>(reinterpret_cast<const T *>(a.qp) + row * a.q_stride + (long long)head * a.dim, on, a.dim, half, q);
+    // the lane's keys, counted from the first one
+    const long long see0 = max((long long)i + ahead - a.left - first, 0ll), see1 = min((long long)i + ahead + a.right + 1 - first, (long long)keys);
+    const int seen0 = (int)min(see0, (long long)kFar);
+    const unsigned seen = on ? (unsigned)max(see1 - seen0, 0ll) : 0u;
+    // tiles that begin from `all0` to `all1` are seen by every query of the wavefront; tiles behind `none` by none of them
+    const int all0 = (int)min(max(w1 + ahead - a.left - first, 0ll), (long long)kFar), all1 = (int)max(min(w0 + ahead + a.right + 1 - first, (long long)keys) - KT, -1ll);
+    const int none0 = (int)(min(max(w0 + ahead - a.left - first, 0ll), (long long)kFar) - KT), none1 = (int)min(w1 + ahead + a.right + 1 - first, (long long)kFar);
+
+    f32x16 acc[DB];
+    clear(acc);
+    float m = -INFINITY, mu = 0.f, l = 0.f;
+    if (keys > 0) {
+        TileCopy<T, DP, KT, NW * 64> ck, cv;
+        ck.init(threadIdx.x, a.dim, a.k_stride);
+        cv.init(threadIdx.x, a.dim, a.v_stride);
+        const T *kp = reinterpret_cast<const T *>(a.kp) + (rk.first + first) * a.k_stride + (long long)hk * a.dim;
+        const T *vp = reinterpret_cast<const T *>(a.vp) + (rk.first + first) * a.v_stride + (long long)hk * a.dim;
+        const unsigned base = lds_offset(s_tiles);
+        TileLane<T, DP> tl;
+        tl.init(lane);
+        ck.issue(kp, keys, a.dim, a.k_stride, base, wave);
+        cv.issue(vp, keys, a.dim, a.v_stride, base + 2 * BYTES, wave);
+        unsigned stage = 0;
+        for (int t = 0; t < keys; t += KT, stage ^= BYTES) {
+            wait_vmcnt<0>();
+            __builtin_amdgcn_s_barrier();   // the tile has arrived, and the one before is done with
+            if (t + KT < keys) {
+                kp += KT * a.k_stride;
+                vp += KT * a.v_stride;
+                ck.issue(kp, keys - t - KT, a.dim, a.k_stride, base + (stage ^ BYTES), wave);
+                cv.issue(vp, keys - t - KT, a.dim, a.v_stride, base + 2 * BYTES + (stage ^ BYTES), wave);
+            }
+            if (t <= none0 || t >= none1) continue;
+            const unsigned kt = base + stage, vt = base + 2 * BYTES + stage;
+            f32x16 s[NB];
+            clear(s);
+            First<T, DP, NB, 8> kq;
+            kq.begin(kt + tl.row, tl.x);
+            kq.run(kt + tl.row, tl.x, q, s);
+            Second<T, DP, NB * 2> pv;
+            pv.begin(vt, tl);
+            if (t < all0 || t > all1) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        if ((unsigned)(t + 32 * nb + 8 * (v >> 2) + 4 * half + (v & 3) - seen0) >= seen) s[nb][v] = -INFINITY;
+            }
+            float mx = s[0][0];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[nb][v]);
+            mx = fmaxf(mx, other_half(mx)) * a.scale2;
+            if (__any(mx > m + kSlack)) {
+                const float mn = fmaxf(m, mx), f = mn == m ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+                m = mn;
+                mu = m == -INFINITY ? 0.f : m;
+                l *= f;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) acc[db][v] *= f;
+            }
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    s[nb][v] = __builtin_amdgcn_exp2f(fmaf(s[nb][v], a.scale2, -mu));
+                    sum[v & 3] += s[nb][v];
+                }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            pv.run(vt, tl, [&](auto sc) { constexpr int sl = decltype(sc)::value; return column<T>(s[sl / 2], sl % 2); }, acc);
+        }
+    }
+    l += other_half(l);
+    if (!own) return;
+    if constexpr (SPLIT) {
+        const long long at = ((long long)split * a.heads + head) * a.q.rows + row;
+        if (half == 0) *reinterpret_cast<float2 *>(a.part_ml + 2 * at) = make_float2(m, on ? l : 0.f);
+        if (keys > 0 && on) store_column<float, DB>(acc, 1.f, a.part_o + at * a.dim, a.dim, half);
+    } else {
+        const bool some = on && l != 0.f;
+        if (!some) clear(acc);
+        store_column<T, DB>(acc, some ? 1.f / l : 0.f, reinterpret_cast<T *>(a.op) + row * a.o_stride + (long long)head * a.dim, a.dim, half);
+        if (half == 0 && a.lse != nullptr) a.lse[(long long)head * a.q.rows + row] = some ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    }
+}
+
+// Splits of the keys put together: 32 lanes to a column, four channels each.
+constexpr int kJoinThreads = 256;
+template <typename T> __global__ __launch_bounds__(kJoinThreads) void k_attention_join(AttnArgs a)
+{
+    const int bh = blockIdx.x / a.tiles, hk = bh % a.kv_heads, b = bh / a.kv_heads;
+    const int col = (blockIdx.x % a.tiles) * (kJoinThreads / 32) + (threadIdx.x >> 5), i = col / a.shared, head = hk * a.shared + col % a.shared;
+    const Rows rq = rows_of(a.q, b);
+    if (i >= rq.own) return;
+    const long long row = rq.first + i, at = (long long)head * a.q.rows + row, step = (long long)a.heads * a.q.rows;
+    float m = -INFINITY, l = 0.f;
+    for (int s = 0; s < a.splits; ++s) {
+        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (at + s * step));
+        if (ml.y == 0.f) continue;
+        const float mn = fmaxf(m, ml.x);
+        l = l * (m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn)) + ml.y * (ml.x == mn ? 1.f : __builtin_amdgcn_exp2f(ml.x - mn));
+        m = mn;
+    }
+    const int c = (threadIdx.x & 31) * 4;
+    if (c < a.dim) {
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < a.splits; ++s) {
+            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (at + s * step));
+            if (ml.y == 0.f) continue;   // its o was not written
+            const float f = (ml.x == m ? 1.f : __builtin_amdgcn_exp2f(ml.x - m)) / l;
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(a.part_o + (at + s * step) * a.dim + c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(f, v[e], o[e]);
+        }
+        T *to = reinterpret_cast<T *>(a.op) + row * a.o_stride + (long long)head * a.dim + c;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2 *>(to) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+        else *reinterpret_cast<f32x4 *>(to) = o;
+    }
+    if (c == 0 && a.lse != nullptr) a.lse[at] = l != 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+}
+
+// ---- entry points -------------------------------------------------------------------------------------------------
+
+const char *const kName = "attention";
+
+struct Form { int waves, splits, split_keys; };   // wavefronts to a block; blocks that the keys of a column are dealt out to
+
+// Blocks of four wavefronts share a tile of keys; where they would not fill the card, or a block's columns would not be there, one wavefront works by itself, and the
+// keys are split until about eight of them are on each compute unit (at least two tiles each).
+Form form_of(const dp_attention_desc &d)
+{
+    const long long cols = (long long)d.q_len * (d.heads / d.kv_heads), groups = (long long)d.n * d.kv_heads;
+    const int kt = d.io_dtype == DP_BF16 ? 64 : 32;
+    if (cols > 32 && groups * ((cols + 127) / 128) >= 256) return {4, 1, 0};
+    const long long blocks = std::max<long long>(1, groups * ((cols + 31) / 32));
+    long long span = d.kv_len;   // keys that a block looks at
+    if (d.left >= 0 && d.right >= 0) span = std::min<long long>(span, (long long)d.left + d.right + 32);
+    const long long most = std::min<long long>(64, (span + 2 * kt - 1) / (2 * kt));
+    const long long want = std::min<long long>(most, 2048 / blocks);
+    if (want < 2) return {1, 1, 0};
+    // whole tiles; a window is anywhere in the sequence, so its split counts over all keys
+    const long long per = ((d.kv_len + want - 1) / want + kt - 1) / kt * kt;
+    return {1, (int)((d.kv_len + per - 1) / per), (int)per};
+}
+
+long long rows_or(long long rows, long long dense) { return rows != 0 ? rows : dense; }
+
+size_t split_bytes(const dp_attention_desc &d, const Form &f)
+{
+    if (f.splits < 2) return 0;
+    return (size_t)f.splits * d.heads * (size_t)rows_or(d.q_rows, (long long)d.n * d.q_len) * (d.dim + 2) * sizeof(float);
+}
+
+template <typename T, int DP> void launch(const AttnArgs &a, const Form &f, unsigned blocks, hipStream_t st)
+{
+    if (f.waves == 4) hipLaunchKernelGGL((k_attention<T, DP, 4, false>), dim3(blocks), dim3(256), 0, st, a);
+    else if (f.splits == 1) hipLaunchKernelGGL((k_attention<T, DP, 1, false>), dim3(blocks), dim3(64), 0, st, a);
+    else hipLaunchKernelGGL((k_attention<T, DP, 1, true>), dim3(blocks), dim3(64), 0, st, a);
+}
+template <typename T> void launch(const AttnArgs &a, const Form &f, unsigned blocks, hipStream_t st)
+{
+    if (a.dim <= 32) launch<T, 32>(a, f, blocks, st);
+    else if (a.dim <= 64) launch<T, 64>(a, f, blocks, st);
+    else if (a.dim <= 96) launch<T, 96>(a, f, blocks, st);
+    else launch<T, 128>(a, f, blocks, st);
+}
+
+}  // namespace
+
+dp_status attn_check(const dp_attention_desc *desc, const dp_attention_seqs *seqs)
+{
+    if (desc == nullptr) { dp_set_error("%s: descriptor is NULL", kName); return DP_ERR_NULL; }
+    const dp_attention_desc &d = *desc;
+    if (d.io_dtype != DP_BF16 && d.io_dtype != DP_F32) { dp_set_error("%s: unknown io_dtype %d", kName, d.io_dtype); return DP_ERR_UNSUPPORTED; }
+    if (d.n < 0 || d.q_len < 0 || d.kv_len < 0 || d.q_len > (1 << 28) || d.kv_len > (1 << 28)) {
+        dp_set_error("%s: %d sequences of %d and %d", kName, d.n, d.q_len, d.kv_len);
+        return DP_ERR_BAD_DESC;
+    }
+    if (d.heads < 1 || d.kv_heads < 1 || d.heads % d.kv_heads != 0) { dp_set_error("%s: %d heads of queries, %d of keys", kName, d.heads, d.kv_heads); return DP_ERR_BAD_DESC; }
+    if (d.dim < 8 || d.dim > 128 || d.dim % 8 != 0) { dp_set_error("%s: dim %d is not a multiple of 8 up to 128", kName, d.dim); return DP_ERR_BAD_DESC; }
+    if (d.left < -1 || d.right < -1) { dp_set_error("%s: window %d, %d", kName, d.left, d.right); return DP_ERR_BAD_DESC; }
+    if (!(d.scale >= 0.f && d.scale < INFINITY)) { dp_set_error("%s: scale must be above 0 (0: 1/sqrt(dim))", kName); return DP_ERR_BAD_DESC; }
+    const long long wq = (long long)d.heads * d.dim, wk = (long long)d.kv_heads * d.dim;
+    const int vec = d.io_dtype == DP_BF16 ? 8 : 4;
+    const long long strides[] = {d.q_stride, d.o_stride, d.k_stride, d.v_stride}, widths[] = {wq, wq, wk, wk};
+    for (int i = 0; i < 4; ++i) {
+        const long long s = strides[i] != 0 ? strides[i] : widths[i];
+        if (s < widths[i] || s % vec != 0 || s > (1 << 22)) {
+            dp_set_error("%s: strides must be whole multiples of 16 bytes, hold the heads, and be at most 2^22 elements", kName);
+            return DP_ERR_BAD_DESC;
+        }
+    }
+    const bool q_packed = seqs != nullptr && seqs->q_starts != nullptr, kv_packed = seqs != nullptr && seqs->kv_starts != nullptr;
+    if (seqs != nullptr) {
+        if ((q_packed && seqs->q_lens != nullptr) || (kv_packed && seqs->kv_lens != nullptr)) {
+            dp_set_error("%s: starts and lengths of one side exclude each other", kName);
+            return DP_ERR_UNSUPPORTED;
+        }
+        for (const void *p : {(const void *)seqs->q_starts, (const void *)seqs->kv_starts, (const void *)seqs->q_lens, (const void *)seqs->kv_lens})
+            if ((reinterpret_cast<uintptr_t>(p) & 3u) != 0) { dp_set_error("%s: starts and lengths must be 4-byte aligned", kName); return DP_ERR_BAD_DESC; }
+    }
+    const long long q_dense = (long long)d.n * d.q_len, kv_dense = (long long)d.n * d.kv_len;
+    if (d.q_rows < 0 || d.kv_rows < 0 || d.q_rows > (1ll << 31) || d.kv_rows > (1ll << 31) || rows_or(d.q_rows, q_dense) > (1ll << 31) || rows_or(d.kv_rows, kv_dense) > (1ll << 31) ||
+        (!q_packed && rows_or(d.q_rows, q_dense) < q_dense) || (!kv_packed && rows_or(d.kv_rows, kv_dense) < kv_dense)) {
+        dp_set_error("%s: %lld and %lld rows do not hold the sequences, or are more than 2^31", kName, (long long)d.q_rows, (long long)d.kv_rows);
+        return DP_ERR_BAD_DESC;
+    }
+    // blocks are counted in 31 bits, at the smallest tile and the most splits
+    const long long shared = d.heads / d.kv_heads;
+    if ((long long)d.q_len * shared >= (1ll << 30) || (double)d.n * d.kv_heads * (((double)d.q_len * shared + 7) / 8) >= 2147483000.0 || (double)d.n * d.kv_heads * (d.kv_len / 32 + 1) >= 2147483000.0) {
+        dp_set_error("%s: too many sequences, heads and tokens for one launch", kName);
+        return DP_ERR_BAD_DESC;
+    }
+    return DP_OK;
+}
+
+void attn_args(const dp_attention_desc &d, const dp_attention_seqs *seqs, AttnArgs &a)
+{
+    a = {};
+    a.q = {seqs != nullptr ? seqs->q_starts : nullptr, seqs != nullptr ? seqs->q_lens : nullptr, d.q_len, rows_or(d.q_rows, (long long)d.n * d.q_len)};
+    a.kv = {seqs != nullptr ? seqs->kv_starts : nullptr, seqs != nullptr ? seqs->kv_lens : nullptr, d.kv_len, rows_or(d.kv_rows, (long long)d.n * d.kv_len)};
+    a.n = d.n; a.heads = d.heads; a.kv_heads = d.kv_heads; a.shared = d.heads / d.kv_heads; a.dim = d.dim;
+    a.left = d.left < 0 ? kFar : std::min(d.left, kFar);
+    a.right = d.right < 0 ? kFar : std::min(d.right, kFar);
+    a.scale = d.scale != 0.f ? d.scale : (float)(1.0 / std::sqrt((double)d.dim));
+    a.scale2 = (float)((d.scale != 0.f ? (double)d.scale : 1.0 / std::sqrt((double)d.dim)) * 1.4426950408889634);
+    const long long wq = (long long)d.heads * d.dim, wk = (long long)d.kv_heads * d.dim;
+    a.q_stride = d.q_stride != 0 ? d.q_stride : wq;
+    a.k_stride = d.k_stride != 0 ? d.k_stride : wk;
+    a.v_stride = d.v_stride != 0 ? d.v_stride : wk;
+    a.o_stride = d.o_stride != 0 ? d.o_stride : wq;
+    a.splits = 1;
+}
+
+dp_status attn_pointers(std::initializer_list<const void *> needed, const void *lse, const void *ws)
+{
+    for (const void *p : needed) if (p == nullptr) { dp_set_error("%s: a required pointer is NULL", kName); return DP_ERR_NULL; }
+    for (const void *p : needed) if ((reinterpret_cast<uintptr_t>(p) & 15u) != 0) { dp_set_error("%s: pointers must be 16-byte aligned", kName); return DP_ERR_BAD_DESC; }
+    if ((reinterpret_cast<uintptr_t>(lse) & 3u) != 0 || (reinterpret_cast<uintptr_t>(ws) & 15u) != 0) { dp_set_error("%s: lse must be 4-byte, the workspace 16-byte aligned", kName); return DP_ERR_BAD_DESC; }
+    return DP_OK;
+}
+
+dp_status attn_workspace(size_t need, const void *ws, size_t ws_bytes)
+{
+    if (need == 0 || (ws != nullptr && ws_bytes >= need)) return DP_OK;
+    dp_set_error("%s needs %zu workspace bytes, got %zu", kName, need, ws == nullptr ? (size_t)0 : ws_bytes);
+    return DP_ERR_WORKSPACE;
+}
+
+dp_status attn_launched(const char *what)
+{
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return DP_OK;
+    dp_set_error("%s launch: %s", what, hipGetErrorString(e));
+    return DP_ERR_HIP;
+}
+
+extern "C" size_t dp_attention_workspace_bytes(const dp_attention_desc *desc, int pass)
+{
+    // packed rows may be fewer than n q_len: checked with starts
+    const int32_t none = 0;
+    const dp_attention_seqs packed = {&none, &none, nullptr, nullptr};
+    if (attn_check(desc, &packed) != DP_OK) return 0;
+    const dp_attention_desc &d = *desc;
+    if (pass == DP_PASS_FWD) return split_bytes(d, form_of(d));
+    if (pass == DP_PASS_DGRAD) return attn_bwd_bytes(d);
+    return 0;
+}
+
+extern "C" dp_status dp_attention_fwd(const dp_attention_desc *desc, const void *q, const void *k, const void *v, void *o, float *lse,
+                                      const dp_attention_seqs *seqs, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    dp_status s = attn_check(desc, seqs);
+    if (s != DP_OK) return s;
+    const dp_attention_desc &d = *desc;
+    AttnArgs a;
+    attn_args(d, seqs, a);
+    if (d.n == 0 || d.q_len == 0 || a.q.rows == 0) return DP_OK;
+    if ((s = attn_pointers({q, o}, lse, ws)) != DP_OK || (d.kv_len > 0 && a.kv.rows > 0 && (s = attn_pointers({k, v}, nullptr, nullptr)) != DP_OK)) return s;
+    const Form f = form_of(d);
+    if ((s = attn_workspace(split_bytes(d, f), ws, ws_bytes)) != DP_OK) return s;
+    a.qp = q; a.kp = k; a.vp = v; a.op = o; a.lse = lse;
+    a.splits = f.splits;
+    a.split_keys = f.split_keys;
+    a.part_o = (float *)ws;
+    if (f.splits > 1) a.part_ml = a.part_o + (long long)f.splits * d.heads * a.q.rows * d.dim;
+    const long long cols = (long long)d.q_len * a.shared, groups = (long long)d.n * d.kv_heads;
+    a.tiles = (int)((cols + 32 * f.waves - 1) / (32 * f.waves));
+    hipStream_t st = (hipStream_t)hip_stream;
+    const bool bf = d.io_dtype == DP_BF16;
+    const unsigned blocks = (unsigned)(groups * a.tiles * f.splits);
+    if (bf) launch<bf16_t>(a, f, blocks, st);
+    else launch<float>(a, f, blocks, st);
+    if (f.splits > 1) {
+        a.tiles = (int)((cols + kJoinThreads / 32 - 1) / (kJoinThreads / 32));
+        hipLaunchKernelGGL(bf ? k_attention_join<bf16_t> : k_attention_join<float>, dim3((unsigned)(groups * a.tiles)), dim3(kJoinThreads), 0, st, a);
+    }
+    return attn_launched(kName);
+}

@@ -1,0 +1,387 @@
+// Norm of every head of queries and keys over its own channels, and the rotation of pairs of channels by the token's place on up to three axes.
+// Bound by HBM: forward reads and writes each element once, backward reads two and writes one.
+//
+//   u = x r gamma, r = 1/sqrt(mean x^2 + eps);   y = R(angle) u
+//   backward, g = R(-angle) dy, t = g gamma:   dgamma = sum g x r,   dx = r (t - x r^2 mean(t x))
+//
+// A rotation is written per channel: y_c = C_c u_c + S_c u_partner(c) with S of opposite signs in the two channels of a pair, and C = 1, S = 0 behind
+// the turned channels.  A wavefront takes one row: its lanes compute the row's angles once, then hold C and S of their own eight channels in registers
+// while they go over the heads, several heads at a time.
+#include "vec_common.h"
+#include <algorithm>
+
+namespace {
+
+constexpr int NT = 256, WAVES = NT / 64, V = 8;   // V channels per lane
+constexpr int kMaxDim = 256, kMaxAxes = 3;
+constexpr int kGradBlocks = 1024;                 // each leaves one partial sum of dgamma
+
+struct QkSide {
+    const void *x, *dy;      // forward: x alone
+    void *out;               // y or dx
+    const float *gamma;
+    long long x_stride, dy_stride, out_stride;
+    int heads;
+};
+
+struct QkArgs {
+    QkSide q, k;
+    const float *pos;
+    const double *freq;
+    float *part;             // [block][2][dim] sums of dgamma, or NULL
+    int rows, dim, axes, pairs[kMaxAxes], turned;   // turned: pairs of all axes
+    int parts;               // a row's heads are dealt out to this many wavefronts
+    float eps;
+};
+
+template <typename T> __device__ __forceinline__ void load8(const T *p, float (&v)[V])
+{
+    if constexpr (sizeof(T) == 2) {
+        const auto w = *reinterpret_cast<const Pack<T, V> *>(p);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = as_f32(w.v[e]);
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const auto w = *reinterpret_cast<const Pack<T, 4> *>(p + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * h + e] = w.v[e];
+        }
+    }
+}
+template <typename T> __device__ __forceinline__ void store8(T *p, const float (&v)[V])
+{
+    constexpr int W = 16 / sizeof(T);
+#pragma unroll
+    for (int h = 0; h < V / W; ++h) {
+        Pack<T, W> w;
+#pragma unroll
+        for (int e = 0; e < W; ++e) w.v[e] = from_f32<T>(v[W * h + e]);
+        *reinterpret_cast<Pack<T, W> *>(p + W * h) = w;
+    }
+}
+
+// Sum over neighbouring LPH lanes, in each of them.
+template <int LPH> __device__ __forceinline__ float head_sum(float v)
+{
+    if constexpr (LPH >= 2) v += moved<0xb1, 0xf>(v, 0.f);     // lanes 1 0 3 2
+    if constexpr (LPH >= 4) v += moved<0x4e, 0xf>(v, 0.f);     // lanes 2 3 0 1
+    if constexpr (LPH >= 8) v += moved<0x141, 0xf>(v, 0.f);    // eights mirrored
+    if constexpr (LPH >= 16) v += moved<0x140, 0xf>(v, 0.f);   // sixteens mirrored
+    if constexpr (LPH >= 32) v += __shfl_xor(v, 16, 64);
+    return v;
+}
+
+// cos and sin of 2 pi turns: the nearest quarter is taken off in 64 bits, what is left (within pi / 4) goes through the Taylor series, whose next terms are
+// below 3e-9; error 1e-7 at the most, whatever the place.
+__device__ __forceinline__ void cos_sin_turns(double turns, float &c, float &s)
+{
+    const double rest = turns - rint(turns), quarter = rint(4.0 * rest);
+    const float a = (float)((rest - 0.25 * quarter) * 6.283185307179586), a2 = a * a;
+    const float sn = a * fmaf(a2, fmaf(a2, fmaf(a2, fmaf(a2, 1.f / 362880, -1.f / 5040), 1.f / 120), -1.f / 6), 1.f);
+    const float cs = fmaf(a2, fmaf(a2, fmaf(a2, fmaf(a2, fmaf(a2, -1.f / 3628800, 1.f / 40320), -1.f / 720), 1.f / 24), -0.5f), 1.f);
+    const int n = (int)quarter;   // -2 ... 2; NaN: 0, and a is NaN
+    const bool odd = (n & 1) != 0;
+    c = odd ? sn : cs;
+    s = odd ? cs : sn;
+    c = n == 1 || n == 2 || n == -2 ? -c : c;
+    s = n == -1 || n == 2 || n == -2 ? -s : s;
+}
+
+__device__ __forceinline__ void add_by(float (&v)[V], int o)
+{
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] += __shfl_xor(v[e], o, 64);
+}
+
+// LDS of one wavefront: the row's table, then the heads in flight.
+__device__ __forceinline__ void own_lds_written() { __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront"); __builtin_amdgcn_wave_barrier(); __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront"); }
+
+template <typename T, int LPH, bool HALVES, bool NORM, bool BWD> __global__ __launch_bounds__(NT) void k_qk_rotary(QkArgs a)
+{
+    constexpr int GROUPS = 64 / LPH, ROOM = LPH * V;   // heads at a time; channels of a head with those of idle lanes
+    __shared__ alignas(16) float s_cs[WAVES][2][kMaxDim / 2];
+    __shared__ alignas(16) float s_x[WAVES][HALVES ? GROUPS * ROOM : 1];
+    __shared__ float s_g[BWD && NORM ? WAVES * 2 * ROOM : 1];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, group = lane / LPH, c0 = (lane % LPH) * V;
+    const bool live = c0 < a.dim;
+    float *cs = s_cs[wave][0], *sn = s_cs[wave][1];
+    const int P = a.turned;
+    const bool whole = HALVES && P % V == 0;   // a lane's partners are one other lane's channels
+
+    float gq[V], gk[V], sum_q[V], sum_k[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        sum_q[e] = sum_k[e] = 0.f;
+        gq[e] = NORM && live && a.q.gamma != nullptr ? a.q.gamma[c0 + e] : 1.f;
+        gk[e] = NORM && live && a.k.gamma != nullptr ? a.k.gamma[c0 + e] : 1.f;
+    }
+    const int turns_q = (a.q.heads + GROUPS - 1) / GROUPS, turns_k = (a.k.heads + GROUPS - 1) / GROUPS;
+    const long long units = (long long)a.rows * a.parts;
+    for (long long unit = (long long)blockIdx.x * WAVES + wave; unit < units; unit += (long long)gridDim.x * WAVES) {
+        const int row = (int)(unit / a.parts), part = (int)(unit % a.parts);
+        for (int p = lane; p < P; p += 64) {
+            const int axis = p < a.pairs[0] ? 0 : p < a.pairs[0] + a.pairs[1] ? 1 : 2;
+            cos_sin_turns((double)a.pos[(long long)row * a.axes + axis] * a.freq[p] * 0.15915494309189535, cs[p], sn[p]);
+        }
+        own_lds_written();
+        float C[V], S[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const int c = c0 + e;
+            const bool first = HALVES ? c < P : (c & 1) == 0, turned = c < 2 * P;
+            const int p = HALVES ? (first ? c : c - P) : c >> 1;
+            C[e] = turned ? cs[turned ? p : 0] : 1.f;
+            const float s = turned ? sn[turned ? p : 0] : 0.f;
+            S[e] = first != BWD ? -s : s;   // the gradient turns back
+        }
+        own_lds_written();
+        for (int t = part; t < turns_q + turns_k; t += a.parts) {
+            const bool is_q = t < turns_q;
+            const QkSide &side = is_q ? a.q : a.k;
+            const int head = (is_q ? t : t - turns_q) * GROUPS + group;
+            const bool on = live && head < side.heads;
+            const int at = head * a.dim + c0;
+            float x[V] = {}, dy[V] = {};
+            if (on && (NORM || !BWD)) load8(reinterpret_cast<const T *>(side.x) + row * side.x_stride + at, x);
+            if constexpr (BWD) if (on) load8(reinterpret_cast<const T *>(side.dy) + row * side.dy_stride + at, dy);
+            float r = 1.f, ss = 0.f, y[V];
+            if constexpr (NORM) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) ss = fmaf(x[e], x[e], ss);
+                r = 1.f / sqrtf(head_sum<LPH>(ss) / a.dim + a.eps);
+            }
+            float u[V], w[V];   // what is turned, and its partners
+#pragma unroll
+            for (int e = 0; e < V; ++e) u[e] = BWD ? dy[e] : NORM ? x[e] * r * (is_q ? gq[e] : gk[e]) : x[e];
+            if constexpr (HALVES) {
+                float *mine = s_x[wave] + group * ROOM;
+#pragma unroll
+                for (int e = 0; e < V; e += 4) *reinterpret_cast<float4 *>(mine + c0 + e) = make_float4(u[e], u[e + 1], u[e + 2], u[e + 3]);
+                own_lds_written();
+                if (whole) {
+                    const int from = c0 < P ? c0 + P : c0 < 2 * P ? c0 - P : c0;
+#pragma unroll
+                    for (int e = 0; e < V; e += 4) {
+                        const float4 f = *reinterpret_cast<const float4 *>(mine + from + e);
+                        w[e] = f.x; w[e + 1] = f.y; w[e + 2] = f.z; w[e + 3] = f.w;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const int c = c0 + e;
+                        w[e] = mine[c < P ? c + P : c < 2 * P ? c - P : c];
+                    }
+                }
+                own_lds_written();
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; ++e) w[e] = u[e ^ 1];
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) y[e] = C[e] == 1.f && S[e] == 0.f ? u[e] : fmaf(C[e], u[e], S[e] * w[e]);
+            if constexpr (BWD && NORM) {
+                float tx = 0.f;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float gx = y[e] * x[e] * r;
+                    if (is_q) sum_q[e] += gx; else sum_k[e] += gx;
+                    y[e] *= is_q ? gq[e] : gk[e];
+                    tx = fmaf(y[e], x[e], tx);
+                }
+                const float f = head_sum<LPH>(tx) / a.dim * r * r;
+#pragma unroll
+                for (int e = 0; e < V; ++e) y[e] = r * fmaf(-x[e], f, y[e]);
+            }
+            if (on) store8(reinterpret_cast<T *>(side.out) + row * side.out_stride + at, y);
+        }
+    }
+    if constexpr (BWD && NORM) {
+        if (a.part == nullptr) return;
+        // the heads of a wavefront, then the wavefronts of the block
+#pragma unroll
+        for (int o = LPH; o < 64; o *= 2) { add_by(sum_q, o); add_by(sum_k, o); }
+        if (group == 0) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) { s_g[(wave * 2) * ROOM + c0 + e] = sum_q[e]; s_g[(wave * 2 + 1) * ROOM + c0 + e] = sum_k[e]; }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * a.dim; i += NT) {
+            const int which = i >= a.dim, c = i - which * a.dim;
+            float s = 0.f;
+            for (int w = 0; w < WAVES; ++w) s += s_g[(w * 2 + which) * ROOM + c];
+            a.part[(long long)blockIdx.x * 2 * a.dim + i] = s;
+        }
+    }
+}
+
+// dgamma of 16 channels: sixteen threads to each go over the blocks' sums, in 64 bits.
+__global__ __launch_bounds__(NT) void k_qk_rotary_dgamma(const float *part, int blocks, int dim, float *dgamma_q, float *dgamma_k)
+{
+    __shared__ double s[NT];
+    const int i = blockIdx.x * 16 + (threadIdx.x & 15);
+    double sum = 0;
+    for (int b = threadIdx.x >> 4; b < blocks; b += NT / 16) sum += part[(long long)b * 2 * dim + i];
+    s[threadIdx.x] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 16) return;
+    for (int j = 1; j < NT / 16; ++j) sum += s[threadIdx.x + 16 * j];
+    float *to = i < dim ? dgamma_q : dgamma_k;
+    if (to != nullptr) to[i < dim ? i : i - dim] = (float)sum;
+}
+
+// ---- entry points -------------------------------------------------------------------------------------------------
+
+const char *const kName = "norm and rotary position";
+
+long long width(const dp_qk_rotary_desc &d, bool keys) { return (long long)(keys ? d.kv_heads : d.heads) * d.dim; }
+
+dp_status check_desc(const dp_qk_rotary_desc *desc)
+{
+    if (desc == nullptr) { dp_set_error("%s: descriptor is NULL", kName); return DP_ERR_NULL; }
+    const dp_qk_rotary_desc &d = *desc;
+    if (d.io_dtype != DP_BF16 && d.io_dtype != DP_F32) { dp_set_error("%s: unknown io_dtype %d", kName, d.io_dtype); return DP_ERR_UNSUPPORTED; }
+    if ((d.flags & ~(DP_QK_NORM | DP_ROTARY_HALVES)) != 0) { dp_set_error("%s: unknown flags 0x%x", kName, d.flags); return DP_ERR_UNSUPPORTED; }
+    if (d.rows < 0 || d.heads < 1 || d.kv_heads < 0) { dp_set_error("%s: %d rows, %d and %d heads", kName, d.rows, d.heads, d.kv_heads); return DP_ERR_BAD_DESC; }
+    if (d.dim < 8 || d.dim > kMaxDim || d.dim % 8 != 0) { dp_set_error("%s: dim %d is not a multiple of 8 up to %d", kName, d.dim, kMaxDim); return DP_ERR_BAD_DESC; }
+    if (d.axes < 1 || d.axes > kMaxAxes) { dp_set_error("%s: %d axes", kName, d.axes); return DP_ERR_BAD_DESC; }
+    long long turned = 0;
+    for (int i = 0; i < d.axes; ++i) {
+        if (d.pairs[i] < 0) { dp_set_error("%s: %d pairs on axis %d", kName, d.pairs[i], i); return DP_ERR_BAD_DESC; }
+        turned += d.pairs[i];
+    }
+    if (2 * turned > d.dim) { dp_set_error("%s: %lld pairs in %d channels", kName, turned, d.dim); return DP_ERR_BAD_DESC; }
+    if ((d.flags & DP_QK_NORM) != 0 && !(d.eps > 0.f && d.eps < INFINITY)) { dp_set_error("%s: eps must be above 0", kName); return DP_ERR_BAD_DESC; }
+    if (width(d, false) + width(d, true) > INT32_MAX) { dp_set_error("%s: a row has 2^31 elements or more", kName); return DP_ERR_BAD_DESC; }
+    const int vec = d.io_dtype == DP_BF16 ? 8 : 4;
+    const long long q[] = {d.q_stride, d.q_out_stride, d.dq_stride}, k[] = {d.k_stride, d.k_out_stride, d.dk_stride};
+    for (int i = 0; i < 3; ++i)
+        if ((q[i] != 0 && (q[i] < width(d, false) || q[i] % vec != 0)) || (k[i] != 0 && (k[i] < width(d, true) || k[i] % vec != 0)) ||
+            q[i] > (1ll << 40) || k[i] > (1ll << 40)) {
+            dp_set_error("%s: strides must be whole multiples of 16 bytes and hold the heads", kName);
+            return DP_ERR_BAD_DESC;
+        }
+    return DP_OK;
+}
+
+long long stride_or(long long stride, long long dense) { return stride != 0 ? stride : dense; }
+
+struct Launch { int blocks, parts; };
+
+// Wavefronts of a row: one goes over all its heads unless rows are few (at 8 rows of 28 heads of 128 channels the row's last head is
+// then seven waits for memory away instead of one).
+Launch launch_of(const dp_qk_rotary_desc &d, bool sums)
+{
+    int lph = 2;
+    while (lph * V < d.dim) lph *= 2;
+    const int groups = 64 / lph, turns = (d.heads + groups - 1) / groups + (d.kv_heads + groups - 1) / groups;
+    const long long wanted = 256 * 16;
+    Launch l;
+    l.parts = (int)std::min<long long>(turns, std::max<long long>(1, wanted / std::max(1, d.rows)));
+    const long long waves = (long long)d.rows * l.parts;
+    l.blocks = (int)std::min<long long>((waves + WAVES - 1) / WAVES, sums ? kGradBlocks : 256 * 64);
+    return l;
+}
+
+size_t sums_bytes(const dp_qk_rotary_desc &d) { return (size_t)launch_of(d, true).blocks * 2 * d.dim * sizeof(float); }
+
+template <typename T, int LPH, bool HALVES> auto pick(bool norm, bool bwd)
+{
+    return bwd ? (norm ? k_qk_rotary<T, LPH, HALVES, true, true> : k_qk_rotary<T, LPH, HALVES, false, true>)
+               : (norm ? k_qk_rotary<T, LPH, HALVES, true, false> : k_qk_rotary<T, LPH, HALVES, false, false>);
+}
+template <typename T, bool HALVES> auto pick(int dim, bool norm, bool bwd)
+{
+    return dim <= 16 ? pick<T, 2, HALVES>(norm, bwd) : dim <= 32 ? pick<T, 4, HALVES>(norm, bwd) : dim <= 64 ? pick<T, 8, HALVES>(norm, bwd)
+         : dim <= 128 ? pick<T, 16, HALVES>(norm, bwd) : pick<T, 32, HALVES>(norm, bwd);
+}
+
+dp_status run(const dp_qk_rotary_desc &d, QkArgs &a, bool bwd, hipStream_t st)
+{
+    const bool norm = (d.flags & DP_QK_NORM) != 0, halves = (d.flags & DP_ROTARY_HALVES) != 0, bf = d.io_dtype == DP_BF16;
+    a.rows = d.rows; a.dim = d.dim; a.axes = d.axes; a.eps = d.eps;
+    a.turned = 0;
+    for (int i = 0; i < kMaxAxes; ++i) { a.pairs[i] = i < d.axes ? d.pairs[i] : 0; a.turned += a.pairs[i]; }
+    a.q.heads = d.heads; a.k.heads = d.kv_heads;
+    const Launch l = launch_of(d, a.part != nullptr);
+    a.parts = l.parts;
+    auto *kernel = bf ? (halves ? pick<bf16_t, true>(d.dim, norm, bwd) : pick<bf16_t, false>(d.dim, norm, bwd))
+                      : (halves ? pick<float, true>(d.dim, norm, bwd) : pick<float, false>(d.dim, norm, bwd));
+    hipLaunchKernelGGL(kernel, dim3(l.blocks), dim3(NT), 0, st, a);
+    return launched(kName);
+}
+
+dp_status check_pointers(std::initializer_list<const void *> needed, std::initializer_list<const void *> given)
+{
+    for (const void *p : needed) if (p == nullptr) { dp_set_error("%s: a required pointer is NULL", kName); return DP_ERR_NULL; }
+    for (auto &list : {needed, given})
+        for (const void *p : list) if (!aligned16(p)) { dp_set_error("%s: pointers must be 16-byte aligned", kName); return DP_ERR_BAD_DESC; }
+    return DP_OK;
+}
+
+}  // namespace
+
+extern "C" size_t dp_qk_rotary_workspace_bytes(const dp_qk_rotary_desc *desc, int pass)
+{
+    if (check_desc(desc) != DP_OK || pass != DP_PASS_DGRAD || desc->rows == 0 || (desc->flags & DP_QK_NORM) == 0) return 0;
+    return sums_bytes(*desc);
+}
+
+extern "C" dp_status dp_qk_rotary_fwd(const dp_qk_rotary_desc *desc, const void *q, const void *k, const float *gamma_q, const float *gamma_k,
+                                      const float *pos, const double *freq, void *q_out, void *k_out, void *hip_stream)
+{
+    dp_status s = check_desc(desc);
+    if (s != DP_OK) return s;
+    const dp_qk_rotary_desc &d = *desc;
+    if (d.rows == 0) return DP_OK;
+    const bool keys = d.kv_heads > 0;
+    if ((s = check_pointers({q, pos, freq, q_out}, {gamma_q, gamma_k})) != DP_OK || (keys && (s = check_pointers({k, k_out}, {})) != DP_OK)) return s;
+    const long long wq = width(d, false), wk = width(d, true);
+    QkArgs a = {};
+    a.q = {q, nullptr, q_out, gamma_q, stride_or(d.q_stride, wq), 0, stride_or(d.q_out_stride, wq), 0};
+    a.k = {k, nullptr, k_out, gamma_k, stride_or(d.k_stride, wk), 0, stride_or(d.k_out_stride, wk), 0};
+    if ((q == q_out && a.q.x_stride != a.q.out_stride) || (keys && k == k_out && a.k.x_stride != a.k.out_stride)) {
+        dp_set_error("%s: in place, a result's stride must be its input's", kName);
+        return DP_ERR_BAD_DESC;
+    }
+    a.pos = pos; a.freq = freq;
+    return run(d, a, false, (hipStream_t)hip_stream);
+}
+
+extern "C" dp_status dp_qk_rotary_bwd(const dp_qk_rotary_desc *desc, const void *q, const void *k, const float *gamma_q, const float *gamma_k,
+                                      const float *pos, const double *freq, const void *dq_out, const void *dk_out, void *dq, void *dk,
+                                      float *dgamma_q, float *dgamma_k, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    dp_status s = check_desc(desc);
+    if (s != DP_OK) return s;
+    const dp_qk_rotary_desc &d = *desc;
+    hipStream_t st = (hipStream_t)hip_stream;
+    const bool norm = (d.flags & DP_QK_NORM) != 0, keys = d.kv_heads > 0, sums = dgamma_q != nullptr || dgamma_k != nullptr;
+    if (sums && !norm) { dp_set_error("%s: dgamma without DP_QK_NORM", kName); return DP_ERR_UNSUPPORTED; }
+    if (d.rows > 0) {
+        if ((s = check_pointers({pos, freq, dq_out, dq}, {q, k, gamma_q, gamma_k})) != DP_OK || (keys && (s = check_pointers({dk_out, dk}, {})) != DP_OK) ||
+            (norm && (s = check_pointers({q}, {})) != DP_OK) || (norm && keys && (s = check_pointers({k}, {})) != DP_OK)) return s;
+    }
+    if ((s = check_pointers({}, {dgamma_q, dgamma_k, ws})) != DP_OK) return s;
+    const long long wq = width(d, false), wk = width(d, true);
+    QkArgs a = {};
+    a.q = {q, dq_out, dq, gamma_q, stride_or(d.q_stride, wq), stride_or(d.q_out_stride, wq), stride_or(d.dq_stride, wq), 0};
+    a.k = {k, dk_out, dk, gamma_k, stride_or(d.k_stride, wk), stride_or(d.k_out_stride, wk), stride_or(d.dk_stride, wk), 0};
+    if ((dq_out == dq && a.q.dy_stride != a.q.out_stride) || (keys && dk_out == dk && a.k.dy_stride != a.k.out_stride) ||
+        (norm && q == dq && a.q.x_stride != a.q.out_stride) || (norm && keys && k == dk && a.k.x_stride != a.k.out_stride)) {
+        dp_set_error("%s: in place, a result's stride must be its input's", kName);
+        return DP_ERR_BAD_DESC;
+    }
+    const size_t need = sums && d.rows > 0 ? sums_bytes(d) : 0;
+    if (need > 0 && (ws == nullptr || ws_bytes < need)) {
+        dp_set_error("%s: the gradient needs %zu workspace bytes, got %zu", kName, need, ws == nullptr ? (size_t)0 : ws_bytes);
+        return DP_ERR_WORKSPACE;
+    }
+    a.pos = pos; a.freq = freq;
+    a.part = sums ? (float *)ws : nullptr;
+    if (d.rows > 0 && (s = run(d, a, true, st)) != DP_OK) return s;
+    if (!sums) return DP_OK;
+    // without rows the gradients are zero
+    hipLaunchKernelGGL(k_qk_rotary_dgamma, dim3(2 * d.dim / 16), dim3(NT), 0, st, (const float *)ws, d.rows > 0 ? launch_of(d, true).blocks : 0, d.dim, dgamma_q, dgamma_k);
+    return launched(kName);
+}

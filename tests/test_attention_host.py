@@ -1,0 +1,139 @@
+"""Host-side checks of the head norm with rotary positions and of attention: every refusal comes before any launch (no GPU needed)."""
+import ctypes as C
+
+import pytest
+
+A = 0x1000   # made-up aligned addresses: validation fails first
+
+
+@pytest.fixture(scope="module")
+def dp():
+    from paper_2112_10065_amd import binding
+    return binding
+
+
+def no_gpu():
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("would launch on the addresses made up here")
+
+
+def test_struct_sizes(dp):
+    assert C.sizeof(dp.dp_qk_rotary_desc) == 96 and C.sizeof(dp.dp_attention_desc) == 88 and C.sizeof(dp.dp_attention_seqs) == 32
+
+
+def rot(dp, **kw):
+    args = dict(rows=7, heads=4, kv_heads=2, dim=32, pairs=[8, 8], flags=dp.DP_QK_NORM)
+    args.update(kw)
+    return dp.qk_rotary_desc(**args)
+
+
+def test_qk_rotary_refusals(dp):
+    lib = dp.lib
+    good = rot(dp)
+    need = dp.dp_qk_rotary_workspace_bytes(good, dp.DP_PASS_DGRAD)
+    assert need > 0 and dp.dp_qk_rotary_workspace_bytes(good, dp.DP_PASS_FWD) == 0 and dp.dp_qk_rotary_workspace_bytes(good, 9) == 0
+
+    def fwd(d=good, q=A, k=A, gq=A, gk=A, pos=A, freq=A, qo=A + 64, ko=A + 64):
+        return lib.dp_qk_rotary_fwd(C.byref(d) if d is not None else None, q, k, gq, gk, pos, freq, qo, ko, None)
+
+    def bwd(d=good, q=A, k=A, gq=A, gk=A, pos=A, freq=A, dqo=A + 64, dko=A + 64, dq=A + 128, dk=A + 128, dgq=A, dgk=A, ws=A, nbytes=1 << 30):
+        return lib.dp_qk_rotary_bwd(C.byref(d) if d is not None else None, q, k, gq, gk, pos, freq, dqo, dko, dq, dk, dgq, dgk, ws, nbytes, None)
+
+    assert fwd(d=None) == bwd(d=None) == dp.DP_ERR_NULL
+    for name in ("q", "k", "pos", "freq", "qo", "ko"):
+        assert fwd(**{name: None}) == dp.DP_ERR_NULL
+        assert fwd(**{name: A + 8}) == dp.DP_ERR_BAD_DESC
+    for name in ("q", "k", "pos", "freq", "dqo", "dko", "dq", "dk"):
+        assert bwd(**{name: None}) == dp.DP_ERR_NULL
+    for name in ("gq", "gk", "dgq", "dgk", "ws", "dq"):
+        assert bwd(**{name: A + 4}) == dp.DP_ERR_BAD_DESC
+    assert bwd(ws=None) == bwd(nbytes=need - 1) == dp.DP_ERR_WORKSPACE
+    for bad in (dict(rows=-1), dict(heads=0), dict(kv_heads=-1), dict(dim=4), dict(dim=36), dict(dim=264), dict(pairs=[]), dict(pairs=[8, -1]), dict(pairs=[8, 9]),
+                dict(eps=0.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(q_stride=120), dict(q_stride=132), dict(k_stride=56), dict(k_out_stride=1 << 41),
+                dict(dq_stride=4), dict(dk_stride=-64), dict(heads=1 << 27)):
+        assert fwd(d=rot(dp, **bad)) == bwd(d=rot(dp, **bad)) == dp.DP_ERR_BAD_DESC, bad
+        assert dp.dp_qk_rotary_workspace_bytes(rot(dp, **bad), dp.DP_PASS_DGRAD) == 0
+    over = rot(dp)
+    over.axes = 4
+    assert fwd(d=over) == dp.DP_ERR_BAD_DESC
+    for bad in (dict(io_dtype=2), dict(flags=dp.DP_RELU)):
+        assert fwd(d=rot(dp, **bad)) == bwd(d=rot(dp, **bad)) == dp.DP_ERR_UNSUPPORTED
+    assert bwd(d=rot(dp, flags=0)) == dp.DP_ERR_UNSUPPORTED                  # dgamma without a norm
+    assert fwd(d=rot(dp, q_out_stride=256), qo=A) == dp.DP_ERR_BAD_DESC      # in place with another stride
+    assert bwd(d=rot(dp, dq_stride=256), dq=A + 64) == dp.DP_ERR_BAD_DESC
+    assert b"rotary" in lib.dp_last_error()
+
+
+def test_qk_rotary_valid_calls(dp):
+    no_gpu()
+    assert dp.lib.dp_qk_rotary_fwd(C.byref(rot(dp, rows=0)), None, None, None, None, None, None, None, None, None) == dp.DP_OK
+    for d in (rot(dp), rot(dp, kv_heads=0), rot(dp, io_dtype=dp.DP_F32, q_stride=132, flags=dp.DP_ROTARY_HALVES), rot(dp, dim=256, pairs=[128]), rot(dp, pairs=[0])):
+        keys = A if d.kv_heads else None
+        assert dp.lib.dp_qk_rotary_fwd(C.byref(d), A, keys, None, None, A, A, A + 64, A + 64, None) == dp.DP_ERR_HIP
+        x = A if d.flags & dp.DP_QK_NORM else None
+        assert dp.lib.dp_qk_rotary_bwd(C.byref(d), x, x and keys, None, None, A, A, A, keys, A + 64, A + 64, None, None, None, 0, None) == dp.DP_ERR_HIP
+
+
+def att(dp, **kw):
+    args = dict(n=2, q_len=5, kv_len=7, heads=4, kv_heads=2, dim=32)
+    args.update(kw)
+    return dp.attention_desc(**args)
+
+
+def test_attention_refusals(dp):
+    lib = dp.lib
+    good = att(dp)
+    back = dp.dp_attention_workspace_bytes(good, dp.DP_PASS_DGRAD)
+    assert back > 0 and dp.dp_attention_workspace_bytes(good, 7) == 0
+    long = att(dp, n=1, q_len=1, kv_len=100000)
+    split = dp.dp_attention_workspace_bytes(long, dp.DP_PASS_FWD)
+    assert split > 0
+
+    def seqs(**kw):
+        return dp.attention_seqs(**kw)
+
+    def fwd(d=good, q=A, k=A, v=A, o=A, lse=A, s=None, ws=A, nbytes=1 << 40):
+        return lib.dp_attention_fwd(C.byref(d) if d is not None else None, q, k, v, o, lse, C.byref(s) if s is not None else None, ws, nbytes, None)
+
+    def bwd(d=good, q=A, k=A, v=A, o=A, do=A, lse=A, dq=A, dk=A, dv=A, s=None, ws=A, nbytes=1 << 40):
+        return lib.dp_attention_bwd(C.byref(d) if d is not None else None, q, k, v, o, do, lse, dq, dk, dv, C.byref(s) if s is not None else None, ws, nbytes, None)
+
+    assert fwd(d=None) == bwd(d=None) == dp.DP_ERR_NULL
+    for name in ("q", "k", "v", "o"):
+        assert fwd(**{name: None}) == dp.DP_ERR_NULL
+        assert fwd(**{name: A + 8}) == dp.DP_ERR_BAD_DESC
+    for name in ("q", "k", "v", "o", "do", "lse", "dq", "dk", "dv"):
+        assert bwd(**{name: None}) == dp.DP_ERR_NULL
+        assert bwd(**{name: A + 2}) == dp.DP_ERR_BAD_DESC
+    assert fwd(lse=A + 2) == fwd(ws=A + 8) == dp.DP_ERR_BAD_DESC
+    assert fwd(d=long, ws=None) == fwd(d=long, nbytes=split - 1) == bwd(nbytes=back - 1) == bwd(ws=None) == dp.DP_ERR_WORKSPACE
+    for bad in (dict(n=-1), dict(q_len=-1), dict(kv_len=-1), dict(q_len=1 << 29), dict(heads=0), dict(kv_heads=0), dict(heads=5), dict(dim=4), dict(dim=20), dict(dim=136),
+                dict(left=-2), dict(right=-2), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(q_stride=64), dict(q_stride=132), dict(o_stride=-128),
+                dict(v_stride=60), dict(k_stride=1 << 23), dict(q_rows=9), dict(kv_rows=13), dict(q_rows=-1), dict(kv_rows=1 << 32), dict(n=1 << 16, q_len=1 << 20),
+                dict(n=1 << 30, q_len=1, kv_len=1), dict(q_len=1 << 28, heads=16)):
+        assert fwd(d=att(dp, **bad)) == bwd(d=att(dp, **bad)) == dp.DP_ERR_BAD_DESC, bad
+    assert fwd(d=att(dp, io_dtype=2)) == bwd(d=att(dp, io_dtype=2)) == dp.DP_ERR_UNSUPPORTED
+    for bad in (seqs(q_starts=A, q_lens=A), seqs(kv_starts=A, kv_lens=A)):
+        assert fwd(s=bad) == bwd(s=bad) == dp.DP_ERR_UNSUPPORTED
+    assert fwd(s=seqs(q_lens=A + 2)) == bwd(s=seqs(kv_starts=A + 1)) == dp.DP_ERR_BAD_DESC
+    assert fwd(d=att(dp, q_rows=9), s=seqs(kv_starts=A)) == dp.DP_ERR_BAD_DESC     # only packed rows may be fewer than n q_len
+    assert b"attention" in lib.dp_last_error()
+    import torch
+    with pytest.raises(ValueError, match="int32"):
+        seqs(q_lens=torch.zeros(2, dtype=torch.int64))
+
+
+def test_attention_valid_calls(dp):
+    no_gpu()
+    lib = dp.lib
+    for d in (att(dp, n=0), att(dp, q_len=0)):
+        assert lib.dp_attention_fwd(C.byref(d), None, None, None, None, None, None, None, 0, None) == dp.DP_OK
+    assert lib.dp_attention_bwd(C.byref(att(dp, q_len=0, kv_len=0)), *[None] * 9, None, None, 0, None) == dp.DP_OK
+    packed = dp.attention_seqs(q_starts=A, kv_starts=A)
+    for d, s in ((att(dp), None), (att(dp, kv_len=0), None), (att(dp, q_rows=3, kv_rows=2), packed), (att(dp, left=1 << 30, right=(1 << 31) - 1, io_dtype=dp.DP_F32), None),
+                 (att(dp, n=1, q_len=1, kv_len=200000), None), (att(dp, n=64, q_len=1000, kv_len=1000, heads=32, kv_heads=8, dim=128, right=0), None)):
+        byref = C.byref(s) if s is not None else None
+        need = dp.dp_attention_workspace_bytes(d, dp.DP_PASS_FWD), dp.dp_attention_workspace_bytes(d, dp.DP_PASS_DGRAD)
+        assert lib.dp_attention_fwd(C.byref(d), A, A, A, A, None, byref, A, need[0], None) == dp.DP_ERR_HIP
+        assert lib.dp_attention_bwd(C.byref(d), A, A, A, A, A, A, A, A, A, byref, A, need[1], None) == dp.DP_ERR_HIP
