@@ -71,6 +71,7 @@ template <typename T, int DP> struct Tile {
     static constexpr int RB = (int)sizeof(T) * (sizeof(T) == 2 ? (DP <= 64 ? 64 : 128) : DP <= 32 ? 32 : DP <= 64 ? 64 : 128);
     static constexpr int CR = RB / 16;                                    // chunks of a row
     static constexpr int SLICES = DP / (2 * E);                           // of the first kind of product
+    static constexpr int DB = (DP + 31) / 32;                             // blocks of 32 channels of the second
     static DEVFN int swizzle(int r)
     {
         if constexpr (CR == 8) return ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
@@ -151,6 +152,28 @@ template <typename T, int DP, int NB, int DEPTH> struct First {
     }
 };
 
+// Two products of the first kind on two tiles of 32 rows, their slices in turn: sa += rows a x ca, sb += rows b x cb.  between(i), i = 0 ... 2 SLICES - 1, is what the vector
+// unit does beside the matrix products.
+template <typename T, int DP, int DEPTH> struct TwoFirst {
+    using L = Tile<T, DP>;
+    static constexpr int N = 2 * L::SLICES, D = DEPTH < N ? DEPTH : N;
+    u32x4 buf[D];
+    template <int I> DEVFN void read(unsigned a, unsigned b, unsigned x) { buf[I % D] = lds_read16<0>((I % 2 == 0 ? a : b) + (x ^ (unsigned)(I / 2 * 32))); }
+    DEVFN void begin(unsigned a, unsigned b, unsigned x) { for_constant<D>([&](auto i) { read<decltype(i)::value>(a, b, x); }); }
+    template <typename F> DEVFN void run(unsigned a, unsigned b, unsigned x, const u32x4 (&ca)[L::SLICES], const u32x4 (&cb)[L::SLICES], f32x16 &sa, f32x16 &sb, F &&between)
+    {
+        for_constant<N>([&](auto ic) {
+            constexpr int i = decltype(ic)::value, left = (N - i < D ? N - i : D) - 1;
+            wait_reads<1, left>();
+            tie(buf[i % D]);
+            if constexpr (i % 2 == 0) Mma<T>::first(buf[i % D], ca[i / 2], sa);
+            else Mma<T>::first(buf[i % D], cb[i / 2], sb);
+            if constexpr (i + D < N) read<i + D>(a, b, x);
+            between(ic);
+        });
+    }
+};
+
 // The lane's addresses in a tile.
 template <typename T, int DP> struct TileLane {
     using L = Tile<T, DP>;
@@ -176,7 +199,7 @@ template <typename T, int DP> struct TileLane {
 template <typename T, int DP, int NS> struct Second;
 template <int DP, int NS> struct Second<bf16_t, DP, NS> {
     using L = Tile<bf16_t, DP>;
-    static constexpr int DB = DP / 32, N = NS * DB, D = N < 6 ? N : 6;
+    static constexpr int DB = L::DB, N = NS * DB, D = N < 6 ? N : 6;
     u32x2 lo[D], hi[D];
     // a channel block of 32 is 64 bytes on: bits above the two lowest of the chunk's number, which the swizzle may have set
     template <int I> DEVFN void read(unsigned tile, const TileLane<bf16_t, DP> &l)
@@ -208,7 +231,7 @@ template <int OFF> DEVFN float lds_read4(unsigned addr)
 }
 template <int DP, int NS> struct Second<float, DP, NS> {
     using L = Tile<float, DP>;
-    static constexpr int DB = DP / 32, N = NS * DB;
+    static constexpr int DB = L::DB, N = NS * DB;
     float buf[8];
     DEVFN void begin(unsigned, const TileLane<float, DP> &) {}
     // register v of a lane's column is row 8 (v / 4) + 4 half + v % 4: one 32x32x2 product takes v of both halves
@@ -253,19 +276,50 @@ template <typename T, int DP> DEVFN void load_column(const T *row, bool on, int 
     }
 }
 
-// A column's results, channels 32 db + 8 (v / 4) + 4 half + v % 4, times f, to its row.
+// A block of a column's results, channels c0 + 8 (v / 4) + 4 half + v % 4, times f, to its row.
+template <typename T> DEVFN void store_block(const f32x16 &acc, float f, T *row, int c0, int dim, int half)
+{
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const int c = c0 + 8 * g + 4 * half;
+        if (c >= dim) continue;
+        const float v0 = acc[4 * g] * f, v1 = acc[4 * g + 1] * f, v2 = acc[4 * g + 2] * f, v3 = acc[4 * g + 3] * f;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2 *>(row + c) = u32x2{pack_bf16(v0, v1), pack_bf16(v2, v3)};
+        else *reinterpret_cast<f32x4 *>(row + c) = f32x4{v0, v1, v2, v3};
+    }
+}
 template <typename T, int DB> DEVFN void store_column(const f32x16 (&acc)[DB], float f, T *row, int dim, int half)
 {
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+    for (int db = 0; db < DB; ++db) store_block<T>(acc[db], f, row, db * 32, dim, half);
+}
+
+// Wavefronts that went over different rows for the same columns: their sums, block i in acc of wavefront i % WAVES (the others' are left as they are).
+// `room`: N blocks of 4 KB for each wavefront; free for use by all of them.
+template <int WAVES, int N> DEVFN void sum_waves(f32x16 (&acc)[N], float *room, int wave, int lane)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<f32x4 *>(room + ((wave * N + i) * 4 + g) * 256 + lane * 4) = f32x4{acc[i][4 * g], acc[i][4 * g + 1], acc[i][4 * g + 2], acc[i][4 * g + 3]};
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (i % WAVES != wave) continue;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const int c = db * 32 + 8 * g + 4 * half;
-            if (c >= dim) continue;
-            const float v0 = acc[db][4 * g] * f, v1 = acc[db][4 * g + 1] * f, v2 = acc[db][4 * g + 2] * f, v3 = acc[db][4 * g + 3] * f;
-            if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2 *>(row + c) = u32x2{pack_bf16(v0, v1), pack_bf16(v2, v3)};
-            else *reinterpret_cast<f32x4 *>(row + c) = f32x4{v0, v1, v2, v3};
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                const f32x4 v = *reinterpret_cast<const f32x4 *>(room + ((w * N + i) * 4 + g) * 256 + lane * 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e] += v[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][4 * g + e] = sum[e];
         }
+    }
 }
 
 template <int N> DEVFN void clear(f32x16 (&acc)[N])
@@ -277,6 +331,18 @@ template <int N> DEVFN void clear(f32x16 (&acc)[N])
 }
 
 }  // namespace
+
+// f(integral_constant): the smallest size of a head's rows in LDS and registers that holds `dim` channels
+template <typename F> void for_dim(int dim, F &&f)
+{
+    if (dim <= 32) f(std::integral_constant<int, 32>{});
+    else if (dim <= 48) f(std::integral_constant<int, 48>{});
+    else if (dim <= 64) f(std::integral_constant<int, 64>{});
+    else if (dim <= 80) f(std::integral_constant<int, 80>{});
+    else if (dim <= 96) f(std::integral_constant<int, 96>{});
+    else if (dim <= 112) f(std::integral_constant<int, 112>{});
+    else f(std::integral_constant<int, 128>{});
+}
 
 // attention_fwd.hip: what both passes check and take from the descriptor and the sequences
 dp_status attn_check(const dp_attention_desc *desc, const dp_attention_seqs *seqs);

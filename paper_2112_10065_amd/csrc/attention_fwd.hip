@@ -12,27 +12,34 @@ namespace {
 
 constexpr float kSlack = 8.f;
 
-template <typename T> constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;   // of a tile
+// Wavefronts of a block: CW of them side by side in columns, 4 / CW share the keys of each tile among them.
+template <typename T, int DP, int CW> struct Shape {
+    static constexpr int RW = 4 / CW, NB = sizeof(T) == 2 && CW == 4 ? 2 : 1, KT = RW * NB * 32, BYTES = KT * Tile<T, DP>::RB;   // NB: blocks of 32 keys of a wavefront
+    static constexpr int STAGES = 4 * BYTES <= 131072 ? 2 : 1;
+};
 
-template <typename T, int DP, int NW, bool SPLIT> __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void k_attention(AttnArgs a)
+template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(256, CW == 4 && (sizeof(T) == 2 || DP <= 64) ? 2 : 1) void k_attention(AttnArgs a)
 {
     using L = Tile<T, DP>;
-    constexpr int KT = kKeys<T>, NB = KT / 32, DB = DP / 32, BYTES = KT * L::RB, COLS = NW * 32;
-    __shared__ alignas(1024) char s_tiles[4 * BYTES];   // K and V, two stages of each
-    const int lane = threadIdx.x & 63, wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    using S = Shape<T, DP, CW>;
+    constexpr int RW = S::RW, NB = S::NB, KT = S::KT, DB = L::DB, BYTES = S::BYTES, STAGES = S::STAGES, COLS = CW * 32;
+    constexpr int ROOM = 2 * STAGES * BYTES > (RW > 1 ? 4 * DB * 4096 : 0) ? 2 * STAGES * BYTES : 4 * DB * 4096;
+    __shared__ alignas(1024) char s_tiles[ROOM];   // K and V of each stage
+    __shared__ float2 s_ml[RW > 1 ? 256 : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, wc = wave % CW, wr = wave / CW;
     int id = logical_block(blockIdx.x, gridDim.x);
     const int split = SPLIT ? id % a.splits : 0;
     if (SPLIT) id /= a.splits;
-    const int bh = id / a.tiles, hk = bh % a.kv_heads, b = bh / a.kv_heads;
+    // head by head, so that each die gets sequences of all lengths
+    const int hb = id / a.tiles, b = hb % a.n, hk = hb / a.n;
     const int col0 = (a.tiles - 1 - id % a.tiles) * COLS;   // causal: the longest first
     const Rows rq = rows_of(a.q, b), rk = rows_of(a.kv, b);
     if (col0 >= rq.own * a.shared) return;
 
-    const int col = col0 + wave * 32 + (lane & 31), i = col / a.shared, head = hk * a.shared + col % a.shared;
+    const int wcol = col0 + wc * 32, col = wcol + (lane & 31), i = col / a.shared, head = hk * a.shared + col % a.shared;
     const bool own = i < rq.own, on = i < rq.used;
-    const int ahead = rk.used - rq.used;
+    const int ahead = rk.used - rq.used, last = rq.used * a.shared - 1;
     // the keys that the block's queries see, and the wavefront's
-    const int wcol = col0 + wave * 32, last = rq.used * a.shared - 1;
     long long lo = 0, hi = 0;
     const long long i0 = col0 / a.shared, i1 = min(col0 + COLS - 1, last) / a.shared, w0 = wcol / a.shared, w1 = min(wcol + 31, last) / a.shared;
     if (col0 <= last) {
@@ -48,19 +55,20 @@ template <typename T, int DP, int NW, bool SPLIT> __global__ __launch_bounds__(N
 
     u32x4 q[L::SLICES];
     load_column<T, DP>(reinterpret_cast<const T *>(a.qp) + row * a.q_stride + (long long)head * a.dim, on, a.dim, half, q);
-    // the lane's keys, counted from the first one
+    // the lane's keys, counted from the wavefront's place in the first tile
+    const int mine = wr * NB * 32;
     const long long see0 = max((long long)i + ahead - a.left - first, 0ll), see1 = min((long long)i + ahead + a.right + 1 - first, (long long)keys);
     const int seen0 = (int)min(see0, (long long)kFar);
     const unsigned seen = on ? (unsigned)max(see1 - seen0, 0ll) : 0u;
-    // tiles that begin from `all0` to `all1` are seen by every query of the wavefront; tiles behind `none` by none of them
-    const int all0 = (int)min(max(w1 + ahead - a.left - first, 0ll), (long long)kFar), all1 = (int)max(min(w0 + ahead + a.right + 1 - first, (long long)keys) - KT, -1ll);
-    const int none0 = (int)(min(max(w0 + ahead - a.left - first, 0ll), (long long)kFar) - KT), none1 = (int)min(w1 + ahead + a.right + 1 - first, (long long)kFar);
+    // a wavefront's keys from t on are seen by all of its queries if all0 <= t <= all1, by none if t <= none0 or t >= none1
+    const int all0 = (int)min(max(w1 + ahead - a.left - first, 0ll), (long long)kFar), all1 = (int)max(min(w0 + ahead + a.right + 1 - first, (long long)keys) - NB * 32, -1ll);
+    const int none0 = (int)(min(max(w0 + ahead - a.left - first, 0ll), (long long)kFar) - NB * 32), none1 = (int)min(min(w1 + ahead + a.right + 1 - first, (long long)keys), (long long)kFar);
 
     f32x16 acc[DB];
     clear(acc);
     float m = -INFINITY, mu = 0.f, l = 0.f;
     if (keys > 0) {
-        TileCopy<T, DP, KT, NW * 64> ck, cv;
+        TileCopy<T, DP, KT, 256> ck, cv;
         ck.init(threadIdx.x, a.dim, a.k_stride);
         cv.init(threadIdx.x, a.dim, a.v_stride);
         const T *kp = reinterpret_cast<const T *>(a.kp) + (rk.first + first) * a.k_stride + (long long)hk * a.dim;
@@ -69,128 +77,180 @@ template <typename T, int DP, int NW, bool SPLIT> __global__ __launch_bounds__(N
         TileLane<T, DP> tl;
         tl.init(lane);
         ck.issue(kp, keys, a.dim, a.k_stride, base, wave);
-        cv.issue(vp, keys, a.dim, a.v_stride, base + 2 * BYTES, wave);
+        cv.issue(vp, keys, a.dim, a.v_stride, base + STAGES * BYTES, wave);
         unsigned stage = 0;
-        for (int t = 0; t < keys; t += KT, stage ^= BYTES) {
+        for (int t = 0; t < keys; t += KT) {
             wait_vmcnt<0>();
             __builtin_amdgcn_s_barrier();   // the tile has arrived, and the one before is done with
-            if (t + KT < keys) {
+            const unsigned kt = base + stage + mine * L::RB, vt = kt + STAGES * BYTES;
+            const auto next = [&] {
+                if (t + KT >= keys) return;
+                if (STAGES == 2) stage ^= BYTES;
                 kp += KT * a.k_stride;
                 vp += KT * a.v_stride;
-                ck.issue(kp, keys - t - KT, a.dim, a.k_stride, base + (stage ^ BYTES), wave);
-                cv.issue(vp, keys - t - KT, a.dim, a.v_stride, base + 2 * BYTES + (stage ^ BYTES), wave);
-            }
-            if (t <= none0 || t >= none1) continue;
-            const unsigned kt = base + stage, vt = base + 2 * BYTES + stage;
-            f32x16 s[NB];
-            clear(s);
-            First<T, DP, NB, 8> kq;
-            kq.begin(kt + tl.row, tl.x);
-            kq.run(kt + tl.row, tl.x, q, s);
-            Second<T, DP, NB * 2> pv;
-            pv.begin(vt, tl);
-            if (t < all0 || t > all1) {
+                ck.issue(kp, keys - t - KT, a.dim, a.k_stride, base + stage, wave);
+                cv.issue(vp, keys - t - KT, a.dim, a.v_stride, base + STAGES * BYTES + stage, wave);
+            };
+            if constexpr (STAGES == 2) next();
+            const int w = t + mine;
+            if (w > none0 && w < none1) {
+                f32x16 s[NB];
+                clear(s);
+                First<T, DP, NB, 8> kq;
+                kq.begin(kt + tl.row, tl.x);
+                kq.run(kt + tl.row, tl.x, q, s);
+                Second<T, DP, NB * 2> pv;
+                pv.begin(vt, tl);
+                if (w < all0 || w > all1) {
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v)
+                            if ((unsigned)(w + 32 * nb + 8 * (v >> 2) + 4 * half + (v & 3) - seen0) >= seen) s[nb][v] = -INFINITY;
+                }
+                float mx = s[0][0];
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                    for (int v = 0; v < 16; ++v)
-                        if ((unsigned)(t + 32 * nb + 8 * (v >> 2) + 4 * half + (v & 3) - seen0) >= seen) s[nb][v] = -INFINITY;
-            }
-            float mx = s[0][0];
+                    for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[nb][v]);
+                mx = fmaxf(mx, other_half(mx)) * a.scale2;
+                if (__any(mx > m + kSlack)) {
+                    const float mn = fmaxf(m, mx), f = mn == m ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+                    m = mn;
+                    mu = m == -INFINITY ? 0.f : m;
+                    l *= f;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+                    for (int db = 0; db < DB; ++db)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[nb][v]);
-            mx = fmaxf(mx, other_half(mx)) * a.scale2;
-            if (__any(mx > m + kSlack)) {
-                const float mn = fmaxf(m, mx), f = mn == m ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-                m = mn;
-                mu = m == -INFINITY ? 0.f : m;
-                l *= f;
-#pragma unroll
-                for (int db = 0; db < DB; ++db)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) acc[db][v] *= f;
-            }
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    s[nb][v] = __builtin_amdgcn_exp2f(fmaf(s[nb][v], a.scale2, -mu));
-                    sum[v & 3] += s[nb][v];
+                        for (int v = 0; v < 16; ++v) acc[db][v] *= f;
                 }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            pv.run(vt, tl, [&](auto sc) { constexpr int sl = decltype(sc)::value; return column<T>(s[sl / 2], sl % 2); }, acc);
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        s[nb][v] = __builtin_amdgcn_exp2f(fmaf(s[nb][v], a.scale2, -mu));
+                        sum[v & 3] += s[nb][v];
+                    }
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                pv.run(vt, tl, [&](auto sc) { constexpr int sl = decltype(sc)::value; return column<T>(s[sl / 2], sl % 2); }, acc);
+            }
+            if constexpr (STAGES == 1) {
+                __builtin_amdgcn_s_barrier();
+                next();
+            }
         }
     }
     l += other_half(l);
+    if constexpr (RW > 1) {   // the wavefronts' results brought to one maximum and added up
+        s_ml[wave * 64 + lane] = make_float2(m, l);
+        __syncthreads();
+        float most = m;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) most = fmaxf(most, s_ml[w * 64 + lane].x);
+        l = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float2 ml = s_ml[w * 64 + lane];
+            l += ml.x == most ? ml.y : ml.y * __builtin_amdgcn_exp2f(ml.x - most);
+        }
+        const float f = m == most ? 1.f : __builtin_amdgcn_exp2f(m - most);
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[db][v] *= f;
+        m = most;
+        sum_waves<4>(acc, reinterpret_cast<float *>(s_tiles), wave, lane);
+    }
     if (!own) return;
-    if constexpr (SPLIT) {
-        const long long at = ((long long)split * a.heads + head) * a.q.rows + row;
-        if (half == 0) *reinterpret_cast<float2 *>(a.part_ml + 2 * at) = make_float2(m, on ? l : 0.f);
-        if (keys > 0 && on) store_column<float, DB>(acc, 1.f, a.part_o + at * a.dim, a.dim, half);
-    } else {
-        const bool some = on && l != 0.f;
-        if (!some) clear(acc);
-        store_column<T, DB>(acc, some ? 1.f / l : 0.f, reinterpret_cast<T *>(a.op) + row * a.o_stride + (long long)head * a.dim, a.dim, half);
-        if (half == 0 && a.lse != nullptr) a.lse[(long long)head * a.q.rows + row] = some ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    const bool some = on && l != 0.f;
+    const long long at = (long long)head * a.q.rows + row, part = split * (long long)a.heads * a.q.rows + at;
+    const float f = SPLIT ? 1.f : some ? 1.f / l : 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+        if (RW > 1 && db != wr) continue;
+        if (!some) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[db][v] = 0.f;
+        }
+        if constexpr (SPLIT) { if (some) store_block<float>(acc[db], f, a.part_o + part * a.dim, db * 32, a.dim, half); }
+        else store_block<T>(acc[db], f, reinterpret_cast<T *>(a.op) + row * a.o_stride + (long long)head * a.dim, db * 32, a.dim, half);
+    }
+    if (half == 0 && wr == 0) {
+        if constexpr (SPLIT) *reinterpret_cast<float2 *>(a.part_ml + 2 * part) = make_float2(m, on ? l : 0.f);
+        else if (a.lse != nullptr) a.lse[at] = some ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
     }
 }
 
-// Splits of the keys put together: 32 lanes to a column, four channels each.
-constexpr int kJoinThreads = 256;
+// Splits of the keys put together: 32 lanes to a column, four channels each; for the statistics a lane has splits lane and lane + 32.
+constexpr int kJoinThreads = 256, kMaxSplits = 64;
 template <typename T> __global__ __launch_bounds__(kJoinThreads) void k_attention_join(AttnArgs a)
 {
-    const int bh = blockIdx.x / a.tiles, hk = bh % a.kv_heads, b = bh / a.kv_heads;
+    const int hb = blockIdx.x / a.tiles, b = hb % a.n, hk = hb / a.n, lane = threadIdx.x & 31;
     const int col = (blockIdx.x % a.tiles) * (kJoinThreads / 32) + (threadIdx.x >> 5), i = col / a.shared, head = hk * a.shared + col % a.shared;
     const Rows rq = rows_of(a.q, b);
-    if (i >= rq.own) return;
+    const bool own = i < rq.own;
     const long long row = rq.first + i, at = (long long)head * a.q.rows + row, step = (long long)a.heads * a.q.rows;
-    float m = -INFINITY, l = 0.f;
-    for (int s = 0; s < a.splits; ++s) {
-        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (at + s * step));
-        if (ml.y == 0.f) continue;
-        const float mn = fmaxf(m, ml.x);
-        l = l * (m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn)) + ml.y * (ml.x == mn ? 1.f : __builtin_amdgcn_exp2f(ml.x - mn));
-        m = mn;
-    }
-    const int c = (threadIdx.x & 31) * 4;
-    if (c < a.dim) {
-        f32x4 o = {0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < a.splits; ++s) {
-            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (at + s * step));
-            if (ml.y == 0.f) continue;   // its o was not written
-            const float f = (ml.x == m ? 1.f : __builtin_amdgcn_exp2f(ml.x - m)) / l;
-            const f32x4 v = *reinterpret_cast<const f32x4 *>(a.part_o + (at + s * step) * a.dim + c);
+    float2 ml[2] = {{-INFINITY, 0.f}, {-INFINITY, 0.f}};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = fmaf(f, v[e], o[e]);
-        }
-        T *to = reinterpret_cast<T *>(a.op) + row * a.o_stride + (long long)head * a.dim + c;
-        if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2 *>(to) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
-        else *reinterpret_cast<f32x4 *>(to) = o;
+    for (int h = 0; h < 2; ++h)
+        if (own && lane + 32 * h < a.splits) ml[h] = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (at + (lane + 32 * h) * step));
+    float m = fmaxf(ml[0].y != 0.f ? ml[0].x : -INFINITY, ml[1].y != 0.f ? ml[1].x : -INFINITY);
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) m = fmaxf(m, __shfl_xor(m, o, 32));
+    float f[2], l = 0.f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        f[h] = ml[h].y == 0.f ? 0.f : ml[h].x == m ? 1.f : __builtin_amdgcn_exp2f(ml[h].x - m);
+        l += f[h] * ml[h].y;
     }
-    if (c == 0 && a.lse != nullptr) a.lse[at] = l != 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) l += __shfl_xor(l, o, 32);
+    const int c = lane * 4;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < a.splits; s0 += 8) {   // eight at a time are under way
+        f32x4 v[8];
+        float g[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int s = s0 + u;
+            g[u] = __shfl(s < 32 ? f[0] : f[1], s & 31, 32);
+            v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (own && s < a.splits && g[u] != 0.f && c < a.dim) v[u] = *reinterpret_cast<const f32x4 *>(a.part_o + (at + s * step) * a.dim + c);   // 0: its o was not written, or vanishes
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(g[u], v[u][e], o[e]);
+    }
+    if (!own) return;
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+    if (c < a.dim) {
+        T *to = reinterpret_cast<T *>(a.op) + row * a.o_stride + (long long)head * a.dim + c;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2 *>(to) = u32x2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
+        else *reinterpret_cast<f32x4 *>(to) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    }
+    if (lane == 0 && a.lse != nullptr) a.lse[at] = l != 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // ---- entry points -------------------------------------------------------------------------------------------------
 
 const char *const kName = "attention";
 
-struct Form { int waves, splits, split_keys; };   // wavefronts to a block; blocks that the keys of a column are dealt out to
+struct Form { int cw, splits, split_keys; };   // wavefronts side by side in a block; blocks that the keys of a column are dealt out to
 
-// Blocks of four wavefronts share a tile of keys; where they would not fill the card, or a block's columns would not be there, one wavefront works by itself, and the
-// keys are split until about eight of them are on each compute unit (at least two tiles each).
+// Four wavefronts side by side share the copies of a tile of keys; where such blocks would not fill the card, or a block's columns would not be there, the four of them take
+// the same 32 columns and share the keys, and if that leaves compute units without work too, blocks share them.
 Form form_of(const dp_attention_desc &d)
 {
     const long long cols = (long long)d.q_len * (d.heads / d.kv_heads), groups = (long long)d.n * d.kv_heads;
-    const int kt = d.io_dtype == DP_BF16 ? 64 : 32;
     if (cols > 32 && groups * ((cols + 127) / 128) >= 256) return {4, 1, 0};
     const long long blocks = std::max<long long>(1, groups * ((cols + 31) / 32));
+    constexpr int kt = 128;
     long long span = d.kv_len;   // keys that a block looks at
     if (d.left >= 0 && d.right >= 0) span = std::min<long long>(span, (long long)d.left + d.right + 32);
-    const long long most = std::min<long long>(64, (span + 2 * kt - 1) / (2 * kt));
-    const long long want = std::min<long long>(most, 2048 / blocks);
+    const long long most = std::min<long long>(kMaxSplits, (span + 4 * kt - 1) / (4 * kt));   // four tiles at least: the join takes as long as two
+    const long long want = std::min<long long>(most, 1024 / blocks);
     if (want < 2) return {1, 1, 0};
     // whole tiles; a window is anywhere in the sequence, so its split counts over all keys
     const long long per = ((d.kv_len + want - 1) / want + kt - 1) / kt * kt;
@@ -205,18 +265,13 @@ size_t split_bytes(const dp_attention_desc &d, const Form &f)
     return (size_t)f.splits * d.heads * (size_t)rows_or(d.q_rows, (long long)d.n * d.q_len) * (d.dim + 2) * sizeof(float);
 }
 
-template <typename T, int DP> void launch(const AttnArgs &a, const Form &f, unsigned blocks, hipStream_t st)
-{
-    if (f.waves == 4) hipLaunchKernelGGL((k_attention<T, DP, 4, false>), dim3(blocks), dim3(256), 0, st, a);
-    else if (f.splits == 1) hipLaunchKernelGGL((k_attention<T, DP, 1, false>), dim3(blocks), dim3(64), 0, st, a);
-    else hipLaunchKernelGGL((k_attention<T, DP, 1, true>), dim3(blocks), dim3(64), 0, st, a);
-}
 template <typename T> void launch(const AttnArgs &a, const Form &f, unsigned blocks, hipStream_t st)
 {
-    if (a.dim <= 32) launch<T, 32>(a, f, blocks, st);
-    else if (a.dim <= 64) launch<T, 64>(a, f, blocks, st);
-    else if (a.dim <= 96) launch<T, 96>(a, f, blocks, st);
-    else launch<T, 128>(a, f, blocks, st);
+    for_dim(a.dim, [&](auto dc) {
+        constexpr int DP = decltype(dc)::value;
+        auto *kernel = f.cw == 4 ? k_attention<T, DP, 4, false> : f.splits == 1 ? k_attention<T, DP, 1, false> : k_attention<T, DP, 1, true>;
+        hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, st, a);
+    });
 }
 
 }  // namespace
@@ -339,7 +394,7 @@ extern "C" dp_status dp_attention_fwd(const dp_attention_desc *desc, const void 
     a.part_o = (float *)ws;
     if (f.splits > 1) a.part_ml = a.part_o + (long long)f.splits * d.heads * a.q.rows * d.dim;
     const long long cols = (long long)d.q_len * a.shared, groups = (long long)d.n * d.kv_heads;
-    a.tiles = (int)((cols + 32 * f.waves - 1) / (32 * f.waves));
+    a.tiles = (int)((cols + 32 * f.cw - 1) / (32 * f.cw));
     hipStream_t st = (hipStream_t)hip_stream;
     const bool bf = d.io_dtype == DP_BF16;
     const unsigned blocks = (unsigned)(groups * a.tiles * f.splits);
