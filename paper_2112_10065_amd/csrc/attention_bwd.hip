@@ -61,7 +61,7 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
             const float x = a.lse_in[stat];
             lse2 = x == -INFINITY ? INFINITY : x * kLog2e;
         }
-        if (on && half == 0 && wr == 0) { a.lse2[stat] = lse2; a.delta[stat] = delta; }
+        if (on && half == 0 && wr == 0) { a.lse2[stat] = lse2; a.delta[stat] = -delta; }
     }
     const int mine = wr * NB * 32;
     const long long see0 = max((long long)i + ahead - a.left - first, 0ll), see1 = min((long long)i + ahead + a.right + 1 - first, (long long)keys);
@@ -108,7 +108,7 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
                 clear(dp);
                 TwoFirst<T, DP, 8> kv;
                 kv.begin(kt + tl.row, vt + tl.row, tl.x);
-                kv.run(kt + tl.row, vt + tl.row, tl.x, q, g, s[0], dp[0], [](auto) {});
+                kv.run(kt + tl.row, vt + tl.row, tl.x, q, g, s[0], dp[0]);
                 Second<T, DP, 2> ks;
                 ks.begin(kt, tl);
                 if (w < all0 || w > all1) {
@@ -143,214 +143,262 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
     }
 }
 
-// dk and dv.  PIPE: one wavefront on each SIMD (its sums and operands take most of the registers), so nothing else runs while it exponentiates: the
-// products of the next 32 queries are put between the exponentials of these.
-template <typename T, int DP, int CW> constexpr bool kPipe = sizeof(T) == 2 && CW == 4 && DP > 64;
-template <typename T, int DP, int CW> struct KvShape : Shape<T, DP, CW> {};
-template <int DP> struct KvShape<bf16_t, DP, 4> {
-    static constexpr bool P = kPipe<bf16_t, DP, 4>;
-    static constexpr int RW = 1, NB = P ? 1 : 2, RT = NB * 32, BYTES = RT * Tile<bf16_t, DP>::RB, STAGES = P ? 4 : 2;
-};
+// The rows (queries) that a block of keys, from col0 on, is seen by, and the wavefront's part of them.
+struct Seen { int first, count, seen0, all0, all1, none0, none1; unsigned seen; };
+template <int COLS> DEVFN Seen seen_by(const AttnArgs &a, const Rows &rq, const Rows &rk, int col0, int wcol, int j)
+{
+    const long long ahead = rk.used - rq.used, w0 = wcol, last = rk.used - 1, j1 = min((long long)col0 + COLS - 1, last), w1 = min(w0 + 31, last);
+    long long lo = 0, hi = 0;
+    if (col0 <= last) {
+        lo = max(0ll, col0 - a.right - ahead);
+        hi = min((long long)rq.used, j1 + a.left - ahead + 1);
+    }
+    Seen s;
+    s.first = (int)min(lo, (long long)kFar);
+    s.count = (int)max(0ll, hi - lo);
+    const long long see0 = max(j - a.right - ahead - s.first, 0ll), see1 = min(j + a.left - ahead + 1 - s.first, (long long)s.count);
+    s.seen0 = (int)min(see0, (long long)kFar);
+    s.seen = j < rk.used ? (unsigned)max(see1 - s.seen0, 0ll) : 0u;
+    // queries t ... t + 31 see all of the wavefront's keys if all0 <= t <= all1 (those behind the last one add zeros), none of them if t <= none0 or t >= none1
+    s.all0 = (int)min(max(w1 - a.right - ahead - s.first, 0ll), (long long)kFar);
+    s.all1 = (int)max(min(w0 + a.left - ahead + 1 - s.first, (long long)kFar) - 32, -1ll);
+    s.none0 = (int)(min(max(w0 - a.right - ahead - s.first, 0ll), (long long)kFar) - 32);
+    s.none1 = (int)min(min(w1 + a.left - ahead + 1 - s.first, (long long)s.count), (long long)kFar);
+    return s;
+}
+DEVFN void hide(f32x16 &s, const Seen &w, int t, int half)
+{
+    if (t >= w.all0 && t <= w.all1) return;
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
+        if ((unsigned)(t + 8 * (v >> 2) + 4 * half + (v & 3) - w.seen0) >= w.seen) s[v] = -INFINITY;
+}
 
-template <typename T, int DP, int CW> __global__ __launch_bounds__(256, sizeof(T) == 2 && CW == 4 && DP <= 64 ? 2 : 1) void k_attention_dkv(AttnArgs a)
+// dk and dv for 128 keys.  The sums of both and the operands k and v take more registers than two wavefronts on a SIMD have, and one alone has nothing to run beside its
+// exponentials; so two of them share 32 keys: the first makes p and dv, the second, a tile of queries behind, dp, ds and dk.  p goes from one to the other through LDS, in
+// 32 bits, lane by lane.  Both do the same on exchanged tiles: x = rows a . column (q k, or dout v), then sum += rows b^T x (dout p, or q ds).
+template <typename T, int DP> __global__ __launch_bounds__(512, 2) void k_attention_dkv(AttnArgs a)
 {
     using L = Tile<T, DP>;
-    using S = KvShape<T, DP, CW>;
-    constexpr bool PIPE = kPipe<T, DP, CW>;
-    constexpr int RW = S::RW, NB = S::NB, QT = S::RT, DB = L::DB, BYTES = S::BYTES, STAGES = S::STAGES, COLS = CW * 32;
-    constexpr int ROOM = 2 * STAGES * BYTES > (RW > 1 ? 4 * DB * 4096 : 0) ? 2 * STAGES * BYTES : 4 * DB * 4096;
-    __shared__ alignas(1024) char s_tiles[ROOM];                  // q and dout of each stage
-    __shared__ alignas(16) float s_stats[STAGES][2][QT < 64 ? 64 : QT];   // lse2 and delta
-    constexpr unsigned STATS = sizeof(s_stats[0]), SIDE = STATS / 2;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, wc = wave % CW, wr = wave / CW;
+    constexpr int NB = 64 * L::RB <= 16384 ? 2 : 1, QT = NB * 32, DB = L::DB, BYTES = QT * L::RB, STAGES = 3, COLS = 128;
+    using Copy = TileCopy<T, DP, QT, 256>;
+    __shared__ alignas(1024) char s_tiles[2 * STAGES * BYTES];   // q and dout of each stage
+    __shared__ alignas(16) float s_stats[2][STAGES][64];         // lse2 and delta
+    __shared__ alignas(16) float s_p[4][NB * 16 * 64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, pair = wave & 3, second = wave >> 2;
     const int id = logical_block(blockIdx.x, gridDim.x);
     const int hb = id / a.tiles, b = hb % a.n, hk = hb / a.n;
     const int col0 = (id % a.tiles) * COLS;             // causal: the longest first
     const Rows rq = rows_of(a.q, b), rk = rows_of(a.kv, b);
     if (col0 >= rk.own) return;
-    const int wcol = col0 + wc * 32, j = wcol + (lane & 31);
+    const int wcol = col0 + pair * 32, j = wcol + (lane & 31);
     const bool own = j < rk.own, on = j < rk.used;
-    const long long ahead = rk.used - rq.used;
-    // the queries that see the block's keys, and the wavefront's
-    const int last = rk.used - 1;
-    long long lo = 0, hi = 0;
-    const long long j1 = min(col0 + COLS - 1, last), w0 = wcol, w1 = min(wcol + 31, last);
-    if (col0 <= last) {
-        lo = max(0ll, col0 - a.right - ahead);
-        hi = min((long long)rq.used, j1 + a.left - ahead + 1);
-    }
-    const int first = (int)min(lo, (long long)kFar), count = (int)max(0ll, hi - lo);
+    const Seen w = seen_by<COLS>(a, rq, rk, col0, wcol, j);
     const long long row = rk.first + j;
-    const int mine = wr * NB * 32;
-    const long long see0 = max(j - a.right - ahead - first, 0ll), see1 = min(j + a.left - ahead + 1 - first, (long long)count);
-    const int seen0 = (int)min(see0, (long long)kFar);
-    const unsigned seen = on ? (unsigned)max(see1 - seen0, 0ll) : 0u;
-    // queries t ... t + 31 see all of the wavefront's keys if all0 <= t <= all1 (those behind the last one add zeros), none of them if t <= none0 or t >= none1
-    const int all0 = (int)min(max(w1 - a.right - ahead - first, 0ll), (long long)kFar), all1 = (int)max(min(w0 + a.left - ahead + 1 - first, (long long)kFar) - 32, -1ll);
-    const int none0 = (int)(min(max(w0 - a.right - ahead - first, 0ll), (long long)kFar) - 32), none1 = (int)min(min(w1 + a.left - ahead + 1 - first, (long long)count), (long long)kFar);
 
-    f32x16 sum[2 * DB];   // dk, then dv
+    f32x16 sum[DB];
     clear(sum);
-    f32x16(&dk)[DB] = *reinterpret_cast<f32x16(*)[DB]>(&sum[0]);
-    f32x16(&dv)[DB] = *reinterpret_cast<f32x16(*)[DB]>(&sum[DB]);
-    if (count > 0) {
+    if (w.count > 0) {
+        u32x4 column_of[L::SLICES];
+        load_column<T, DP>((second ? reinterpret_cast<const T *>(a.vp) + row * a.v_stride : reinterpret_cast<const T *>(a.kp) + row * a.k_stride) + (long long)hk * a.dim, on, a.dim, half, column_of);
+        const unsigned base = lds_offset(s_tiles), mine = base + second * STAGES * BYTES, other = base + (second ^ 1) * STAGES * BYTES, stats = lds_offset(s_stats) + second * sizeof(s_stats[0]),
+                       pt = lds_offset(s_p) + pair * sizeof(s_p[0]) + lane * 16;
+        const long long stride = second ? a.o_stride : a.q_stride;
+        const T *from = reinterpret_cast<const T *>(second ? a.dout : a.qp);
+        const float *stat_from = second ? a.delta : a.lse2;
+        Copy copy;
+        copy.init(threadIdx.x & 255, a.dim, stride);
+        TileLane<T, DP> tl;
+        tl.init(lane);
+        const int tiles = (w.count + QT - 1) / QT, all = tiles * a.shared;
+        // tile n: queries first + QT (n % tiles) ... of the n / tiles-th head; rows behind the last query arrive as zeros, also their statistics: nothing is added then.
+        // The first wavefronts copy q and lse2, the second dout and delta.
+        int ih = hk * a.shared, it = 0, slot_in = 0;
+        auto issue = [&] {
+            const long long at = rq.first + w.first + it;
+            const int rows = w.count - it;
+            copy.issue(from + at * stride + (long long)ih * a.dim, rows, a.dim, stride, mine + slot_in * BYTES, pair);
+            if (pair == 0) {
+                const auto r = make_rsrc(stat_from + (long long)ih * a.q.rows + at, (unsigned)min(rows, QT) * 4);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void)(size_t)(stats + slot_in * 256), 4, lane * 4, 0, 0, 0);
+            }
+            slot_in = slot_in + 1 == STAGES ? 0 : slot_in + 1;
+            it += QT;
+            if (it >= w.count) { it = 0; ++ih; }
+        };
+        issue();
+        int t = 0, slot = 0;
+        for (int n = 0; n <= all; ++n) {
+            // tile n has arrived, p of tile n - 1 too, and tile n - 2 is done with: its room takes tile n + 1
+            wait_vmcnt<0>();
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            if (n + 1 < all) issue();
+            const bool part = second ? n > 0 : n < all;
+            f32x16 x[NB];
+            bool some[NB], any = false;
+            const int at = t;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                some[nb] = part && at + 32 * nb > w.none0 && at + 32 * nb < w.none1;
+                any |= some[nb];
+            }
+            if (any) {
+                const unsigned xt = mine + slot * BYTES, yt = other + slot * BYTES, st = stats + slot * 256 + half * 16;
+                First<T, DP, NB, 6> first;
+                u32x4 f[NB][4];   // statistics of rows 8 g + 4 half ..., or p
+                if (second) {     // dp - delta: the sum begins at -delta
+                    for_constant<NB * 4>([&](auto ic) { constexpr int i = decltype(ic)::value; f[i / 4][i % 4] = lds_read16<i * 32>(st); });
+                    first.begin(xt + tl.row, tl.x);
+                    wait_reads<1, decltype(first)::D>();
+#pragma unroll
+                    for (int i = 0; i < NB * 4; ++i) tie(f[i / 4][i % 4]);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) x[nb][v] = __uint_as_float(f[nb][v >> 2][v & 3]);
+                } else {
+                    clear(x);
+                    first.begin(xt + tl.row, tl.x);
+                }
+                first.run(xt + tl.row, tl.x, column_of, x);
+                Second<T, DP, 2 * NB> next;
+                if (second) for_constant<NB * 4>([&](auto ic) { constexpr int i = decltype(ic)::value; f[i / 4][i % 4] = lds_read16<i * 1024>(pt); });
+                else for_constant<NB * 4>([&](auto ic) { constexpr int i = decltype(ic)::value; f[i / 4][i % 4] = lds_read16<i * 32>(st); });
+                next.begin(yt, tl);
+                wait_reads<1, decltype(next)::READS>();
+#pragma unroll
+                for (int i = 0; i < NB * 4; ++i) tie(f[i / 4][i % 4]);
+                if (second) {
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) x[nb][v] *= __uint_as_float(f[nb][v >> 2][v & 3]);
+                } else {
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        hide(x[nb], w, at + 32 * nb, half);
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) x[nb][v] = __builtin_amdgcn_exp2f(fmaf(x[nb][v], a.scale2, -__uint_as_float(f[nb][v >> 2][v & 3])));
+                    }
+                }
+                next.run(yt, tl, [&](auto sc) { constexpr int sl = decltype(sc)::value; return column<T>(x[sl / 2], sl % 2); }, sum);
+            }
+            if (part) {
+                t = t + QT >= w.count ? 0 : t + QT;
+                slot = slot + 1 == STAGES ? 0 : slot + 1;
+            }
+            __builtin_amdgcn_s_barrier();   // p of the tile before is read
+            if (any && !second) for_constant<NB * 4>([&](auto ic) {
+                constexpr int i = decltype(ic)::value, nb = i / 4, g = i % 4;
+                lds_write16(pt + i * 1024, __builtin_bit_cast(u32x4, f32x4{x[nb][4 * g], x[nb][4 * g + 1], x[nb][4 * g + 2], x[nb][4 * g + 3]}));
+            });
+        }
+    }
+    if (!own) return;
+    if (!on) clear(sum);
+    if (second) store_column<T, DB>(sum, a.scale, reinterpret_cast<T *>(a.dk) + row * a.k_stride + (long long)hk * a.dim, a.dim, half);
+    else store_column<T, DB>(sum, 1.f, reinterpret_cast<T *>(a.dv) + row * a.v_stride + (long long)hk * a.dim, a.dim, half);
+}
+
+// dk and dv for 32 keys, where there are few: four wavefronts share each tile of queries.
+template <typename T, int DP> __global__ __launch_bounds__(256, 1) void k_attention_dkv_few(AttnArgs a)
+{
+    using L = Tile<T, DP>;
+    using S = Shape<T, DP, 1>;
+    constexpr int QT = S::RT, DB = L::DB, BYTES = S::BYTES, STAGES = S::STAGES, COLS = 32;
+    constexpr int ROOM = 2 * STAGES * BYTES > 4 * DB * 4096 ? 2 * STAGES * BYTES : 4 * DB * 4096;
+    __shared__ alignas(1024) char s_tiles[ROOM];            // q and dout of each stage
+    __shared__ alignas(16) float s_stats[STAGES][2][QT];    // lse2 and delta
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int id = logical_block(blockIdx.x, gridDim.x);
+    const int hb = id / a.tiles, b = hb % a.n, hk = hb / a.n;
+    const int col0 = (id % a.tiles) * COLS;
+    const Rows rq = rows_of(a.q, b), rk = rows_of(a.kv, b);
+    if (col0 >= rk.own) return;
+    const int j = col0 + (lane & 31);
+    const bool own = j < rk.own, on = j < rk.used;
+    const Seen w = seen_by<COLS>(a, rq, rk, col0, col0, j);
+    const long long row = rk.first + j;
+    const int mine = wave * 32;
+
+    f32x16 dk[DB], dv[DB];
+    clear(dk);
+    clear(dv);
+    if (w.count > 0) {
         u32x4 kc[L::SLICES], vc[L::SLICES];
         load_column<T, DP>(reinterpret_cast<const T *>(a.kp) + row * a.k_stride + (long long)hk * a.dim, on, a.dim, half, kc);
         load_column<T, DP>(reinterpret_cast<const T *>(a.vp) + row * a.v_stride + (long long)hk * a.dim, on, a.dim, half, vc);
-        using Copy = TileCopy<T, DP, QT, 256>;
-        Copy cq, cg;
+        TileCopy<T, DP, QT, 256> cq, cg;
         cq.init(threadIdx.x, a.dim, a.q_stride);
         cg.init(threadIdx.x, a.dim, a.o_stride);
         const unsigned base = lds_offset(s_tiles), stats = lds_offset(s_stats);
         TileLane<T, DP> tl;
         tl.init(lane);
-        const int tiles = (count + QT - 1) / QT, all = tiles * a.shared;
-        // tile n: queries first + (n % tiles) QT ... of the n / tiles-th head; rows behind the last query arrive as zeros, also their statistics: nothing is added then
+        const int tiles = (w.count + QT - 1) / QT, all = tiles * a.shared;
         int ih = hk * a.shared, it = 0, slot_in = 0;
-        constexpr int STAT_COPIES = QT > 64 ? QT / 64 : 1;
         auto issue = [&] {
-            const long long at = rq.first + first + it;
-            const int rows = count - it;
+            const long long at = rq.first + w.first + it;
+            const int rows = w.count - it;
             cq.issue(reinterpret_cast<const T *>(a.qp) + at * a.q_stride + (long long)ih * a.dim, rows, a.dim, a.q_stride, base + slot_in * BYTES, wave);
             cg.issue(reinterpret_cast<const T *>(a.dout) + at * a.o_stride + (long long)ih * a.dim, rows, a.dim, a.o_stride, base + (STAGES + slot_in) * BYTES, wave);
-            // wavefronts 0 and 2 copy the same, 1 and 3 too: each has as many copies under way as the others
-            const auto r = make_rsrc(((wave & 1) == 0 ? a.lse2 : a.delta) + (long long)ih * a.q.rows + at, (unsigned)min(rows, QT) * 4);
-#pragma unroll
-            for (int c = 0; c < STAT_COPIES; ++c)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void)(size_t)(stats + slot_in * STATS + (wave & 1) * SIDE + c * 256), 4, (c * 64 + lane) * 4, 0, 0, 0);
-            slot_in = slot_in + 1 == STAGES ? 0 : slot_in + 1;
+            // wavefront w: half w % 2 of the statistics w / 2
+            const auto r = make_rsrc((wave < 2 ? a.lse2 : a.delta) + (long long)ih * a.q.rows + at, (unsigned)min(rows, QT) * 4);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void)(size_t)(stats + slot_in * 2 * QT * 4 + wave * 256), 4, ((wave & 1) * 64 + lane) * 4, 0, 0, 0);
+            if (STAGES == 2) slot_in ^= 1;
             it += QT;
-            if (it >= count) { it = 0; ++ih; }
+            if (it >= w.count) { it = 0; ++ih; }
         };
-        u32x4 l2[4], de[4];   // statistics of rows 8 g + 4 half ...
-        const auto read_stats = [&](unsigned st) {
-            l2[0] = lds_read16<0>(st); l2[1] = lds_read16<32>(st); l2[2] = lds_read16<64>(st); l2[3] = lds_read16<96>(st);
-            de[0] = lds_read16<SIDE>(st); de[1] = lds_read16<SIDE + 32>(st); de[2] = lds_read16<SIDE + 64>(st); de[3] = lds_read16<SIDE + 96>(st);
-        };
-        const auto stats_there = [&] {
+        static_assert(QT == 128, "the statistics are copied by four wavefronts of 64 lanes");
+        issue();
+        int slot = 0, t = 0;
+        for (int n = 0; n < all; ++n) {
+            wait_vmcnt<0>();
+            __builtin_amdgcn_s_barrier();   // the tile has arrived, and the one before is done with
+            if (STAGES == 2 && n + 1 < all) issue();
+            const int at = t + mine;
+            if (at > w.none0 && at < w.none1) {
+                const unsigned qt = base + slot * BYTES + mine * L::RB, gt = qt + STAGES * BYTES, st = stats + slot * 2 * QT * 4 + mine * 4 + half * 16;
+                f32x16 s[1], dp[1];
+                clear(s);
+                clear(dp);
+                u32x4 l2[4], de[4];   // of rows 8 g + 4 half ...
+                l2[0] = lds_read16<0>(st); l2[1] = lds_read16<32>(st); l2[2] = lds_read16<64>(st); l2[3] = lds_read16<96>(st);
+                de[0] = lds_read16<QT * 4>(st); de[1] = lds_read16<QT * 4 + 32>(st); de[2] = lds_read16<QT * 4 + 64>(st); de[3] = lds_read16<QT * 4 + 96>(st);
+                TwoFirst<T, DP, 6> ab;
+                ab.begin(qt + tl.row, gt + tl.row, tl.x);
+                ab.run(qt + tl.row, gt + tl.row, tl.x, kc, vc, s[0], dp[0]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { tie(l2[e]); tie(de[e]); }
-        };
-        const auto hide = [&](f32x16 &s, int w) {
-            if (w >= all0 && w <= all1) return;
-#pragma unroll
-            for (int v = 0; v < 16; ++v)
-                if ((unsigned)(w + 8 * (v >> 2) + 4 * half + (v & 3) - seen0) >= seen) s[v] = -INFINITY;
-        };
-        const auto soften = [&](f32x16 &s, f32x16 &dp, int v) {   // s -> p, dp -> ds
-            const float p = __builtin_amdgcn_exp2f(fmaf(s[v], a.scale2, -__uint_as_float(l2[v >> 2][v & 3])));
-            dp[v] = p * (dp[v] - __uint_as_float(de[v >> 2][v & 3]));
-            s[v] = p;
-        };
-        if constexpr (PIPE) {
-            constexpr int COPIES = 2 * Copy::N + 1;
-            issue();
-            if (all > 1) issue();
-            if (all > 2) issue();
-            if (all > 2) wait_vmcnt<2 * COPIES>();
-            else if (all > 1) wait_vmcnt<COPIES>();
-            else wait_vmcnt<0>();
-            __builtin_amdgcn_s_barrier();
-            f32x16 s[2], dp[2];
-            clear(s);
-            clear(dp);
-            TwoFirst<T, DP, 6> ab;
-            read_stats(stats + half * 16);
-            ab.begin(base + tl.row, base + STAGES * BYTES + tl.row, tl.x);
-            ab.run(base + tl.row, base + STAGES * BYTES + tl.row, tl.x, kc, vc, s[0], dp[0], [](auto) {});
-            stats_there();
-            int slot = 0, t = 0;
-            hide(s[0], 0);
-            const auto step = [&](int n, f32x16 &sc, f32x16 &dc, f32x16 &sn, f32x16 &dn) {
-                const unsigned qt = base + slot * BYTES, gt = qt + STAGES * BYTES;
-                u32x4 p[2], ds[2];
-                if (n + 1 < all) {
-                    // the next tile has arrived, and the one before this is done with: its room takes the third from here
-                    if (n + 2 < all) wait_vmcnt<COPIES>();
-                    else wait_vmcnt<0>();
-                    __builtin_amdgcn_s_barrier();
-                    if (n + 3 < all) issue();
-                    slot = slot + 1 == STAGES ? 0 : slot + 1;
-                    t = t + QT >= count ? 0 : t + QT;
-                    const unsigned qn = base + slot * BYTES + tl.row, gn = qn + STAGES * BYTES;
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) sn[v] = dn[v] = 0.f;
-                    ab.begin(qn, gn, tl.x);
-                    ab.run(qn, gn, tl.x, kc, vc, sn, dn, [&](auto ic) {
-                        constexpr int i = decltype(ic)::value, N = 2 * L::SLICES;
-#pragma unroll
-                        for (int v = i * 16 / N; v < (i + 1) * 16 / N; ++v) soften(sc, dc, v);
-                    });
-                    hide(sn, t);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) { p[h] = column<T>(sc, h); ds[h] = column<T>(dc, h); }
-                    read_stats(stats + slot * STATS + half * 16);
-                } else {
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) soften(sc, dc, v);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) { p[h] = column<T>(sc, h); ds[h] = column<T>(dc, h); }
-                }
+                for (int e = 0; e < 4; ++e) { tie(l2[e]); tie(de[e]); }   // older than the reads that were waited for
                 Second<T, DP, 2> gp, qs;
                 gp.begin(gt, tl);
-                gp.run(gt, tl, [&](auto sl) { return p[decltype(sl)::value]; }, dv);
+                hide(s[0], w, at, half);
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    s[0][v] = __builtin_amdgcn_exp2f(fmaf(s[0][v], a.scale2, -__uint_as_float(l2[v >> 2][v & 3])));
+                    dp[0][v] = s[0][v] * (dp[0][v] + __uint_as_float(de[v >> 2][v & 3]));
+                }
+                gp.run(gt, tl, [&](auto sc) { return column<T>(s[0], decltype(sc)::value); }, dv);
                 qs.begin(qt, tl);
-                qs.run(qt, tl, [&](auto sl) { return ds[decltype(sl)::value]; }, dk);
-                stats_there();   // older than the reads that were waited for
-            };
-            for (int n = 0; n < all; ++n) {
-                step(n, s[0], dp[0], s[1], dp[1]);
-                s[0] = s[1];
-                dp[0] = dp[1];
+                qs.run(qt, tl, [&](auto sc) { return column<T>(dp[0], decltype(sc)::value); }, dk);
             }
-        } else {
-            issue();
-            int slot = 0, t = 0;
-            for (int n = 0; n < all; ++n) {
-                wait_vmcnt<0>();
-                __builtin_amdgcn_s_barrier();   // the tile has arrived, and the one before is done with
-                if (STAGES == 2 && n + 1 < all) issue();
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    const int w = t + mine + 32 * nb;
-                    if (w <= none0 || w >= none1) continue;
-                    const unsigned at = (mine + nb * 32) * L::RB, qt = base + slot * BYTES + at, gt = base + (STAGES + slot) * BYTES + at;
-                    f32x16 s[1], dp[1];
-                    clear(s);
-                    clear(dp);
-                    read_stats(stats + slot * STATS + (mine + nb * 32) * 4 + half * 16);
-                    TwoFirst<T, DP, 6> ab;
-                    ab.begin(qt + tl.row, gt + tl.row, tl.x);
-                    ab.run(qt + tl.row, gt + tl.row, tl.x, kc, vc, s[0], dp[0], [](auto) {});
-                    stats_there();   // older than the reads that were waited for
-                    Second<T, DP, 2> gp, qs;
-                    gp.begin(gt, tl);
-                    hide(s[0], w);
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) soften(s[0], dp[0], v);
-                    gp.run(gt, tl, [&](auto sc) { return column<T>(s[0], decltype(sc)::value); }, dv);
-                    qs.begin(qt, tl);
-                    qs.run(qt, tl, [&](auto sc) { return column<T>(dp[0], decltype(sc)::value); }, dk);
-                }
-                if (STAGES == 1 && n + 1 < all) {
-                    __builtin_amdgcn_s_barrier();
-                    issue();
-                }
-                if (STAGES == 2) slot ^= 1;
-                t = t + QT >= count ? 0 : t + QT;
+            if (STAGES == 1 && n + 1 < all) {
+                __builtin_amdgcn_s_barrier();
+                issue();
             }
+            if (STAGES == 2) slot ^= 1;
+            t = t + QT >= w.count ? 0 : t + QT;
         }
     }
-    if constexpr (RW > 1) {   // one after the other: the room of dk's sums takes dv's
-        __syncthreads();
-        sum_waves<4>(dk, reinterpret_cast<float *>(s_tiles), wave, lane);
-        __syncthreads();
-        sum_waves<4>(dv, reinterpret_cast<float *>(s_tiles), wave, lane);
-    }
+    // one after the other: the room of dk's sums takes dv's
+    __syncthreads();
+    sum_waves<4>(dk, reinterpret_cast<float *>(s_tiles), wave, lane);
+    __syncthreads();
+    sum_waves<4>(dv, reinterpret_cast<float *>(s_tiles), wave, lane);
     if (!own) return;
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
-        if (RW > 1 && db != wr) continue;
+        if (db != wave) continue;
         if (!on) {
 #pragma unroll
             for (int v = 0; v < 16; ++v) dk[db][v] = dv[db][v] = 0.f;
@@ -360,7 +408,7 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, sizeof(T
     }
 }
 
-// Four wavefronts side by side where such blocks fill the card; else they take the same 32 columns and share the rows of the other side.
+// Blocks of 128 columns where they fill the card; else of 32, whose wavefronts share the rows of the other side.
 template <typename T> void launch(AttnArgs &a, long long groups, hipStream_t st)
 {
     for_dim(a.dim, [&](auto dc) {
@@ -371,7 +419,7 @@ template <typename T> void launch(AttnArgs &a, long long groups, hipStream_t st)
         a.tiles = (int)((qc + (wq ? 127 : 31)) / (wq ? 128 : 32));
         if (a.tiles > 0 && a.q.rows > 0) hipLaunchKernelGGL((wq ? k_attention_dq<T, DP, 4> : k_attention_dq<T, DP, 1>), dim3((unsigned)(groups * a.tiles)), dim3(256), 0, st, a);
         a.tiles = (int)((kc + (wk ? 127 : 31)) / (wk ? 128 : 32));
-        if (a.tiles > 0 && a.kv.rows > 0) hipLaunchKernelGGL((wk ? k_attention_dkv<T, DP, 4> : k_attention_dkv<T, DP, 1>), dim3((unsigned)(groups * a.tiles)), dim3(256), 0, st, a);
+        if (a.tiles > 0 && a.kv.rows > 0) hipLaunchKernelGGL((wk ? k_attention_dkv<T, DP> : k_attention_dkv_few<T, DP>), dim3((unsigned)(groups * a.tiles)), dim3(wk ? 512 : 256), 0, st, a);
     });
 }
 

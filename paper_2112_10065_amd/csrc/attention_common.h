@@ -29,7 +29,7 @@ struct AttnArgs {
     float *lse;
     const float *lse_in;
     void *dq, *dk, *dv;
-    float *lse2, *delta;                   // backward's workspace: lse log2(e) (+inf: sees nothing) and sum dout o, [heads][q_rows]
+    float *lse2, *delta;                   // backward's workspace: lse log2(e) (+inf: sees nothing) and -sum dout o, [heads][q_rows]
     int tiles;                             // of a sequence and head of keys
     int splits, split_keys;                // forward: keys dealt out to so many blocks, split_keys each
     float *part_o, *part_ml;               // [split][head][q_rows][dim] and [split][head][q_rows][2]
@@ -152,15 +152,14 @@ template <typename T, int DP, int NB, int DEPTH> struct First {
     }
 };
 
-// Two products of the first kind on two tiles of 32 rows, their slices in turn: sa += rows a x ca, sb += rows b x cb.  between(i), i = 0 ... 2 SLICES - 1, is what the vector
-// unit does beside the matrix products.
+// Two products of the first kind on two tiles of 32 rows, their slices in turn: sa += rows a x ca, sb += rows b x cb.
 template <typename T, int DP, int DEPTH> struct TwoFirst {
     using L = Tile<T, DP>;
     static constexpr int N = 2 * L::SLICES, D = DEPTH < N ? DEPTH : N;
     u32x4 buf[D];
     template <int I> DEVFN void read(unsigned a, unsigned b, unsigned x) { buf[I % D] = lds_read16<0>((I % 2 == 0 ? a : b) + (x ^ (unsigned)(I / 2 * 32))); }
     DEVFN void begin(unsigned a, unsigned b, unsigned x) { for_constant<D>([&](auto i) { read<decltype(i)::value>(a, b, x); }); }
-    template <typename F> DEVFN void run(unsigned a, unsigned b, unsigned x, const u32x4 (&ca)[L::SLICES], const u32x4 (&cb)[L::SLICES], f32x16 &sa, f32x16 &sb, F &&between)
+    DEVFN void run(unsigned a, unsigned b, unsigned x, const u32x4 (&ca)[L::SLICES], const u32x4 (&cb)[L::SLICES], f32x16 &sa, f32x16 &sb)
     {
         for_constant<N>([&](auto ic) {
             constexpr int i = decltype(ic)::value, left = (N - i < D ? N - i : D) - 1;
@@ -169,7 +168,6 @@ template <typename T, int DP, int DEPTH> struct TwoFirst {
             if constexpr (i % 2 == 0) Mma<T>::first(buf[i % D], ca[i / 2], sa);
             else Mma<T>::first(buf[i % D], cb[i / 2], sb);
             if constexpr (i + D < N) read<i + D>(a, b, x);
-            between(ic);
         });
     }
 };
@@ -199,7 +197,7 @@ template <typename T, int DP> struct TileLane {
 template <typename T, int DP, int NS> struct Second;
 template <int DP, int NS> struct Second<bf16_t, DP, NS> {
     using L = Tile<bf16_t, DP>;
-    static constexpr int DB = L::DB, N = NS * DB, D = N < 6 ? N : 6;
+    static constexpr int DB = L::DB, N = NS * DB, D = N < 6 ? N : 6, READS = 2 * D;   // READS: under way behind begin()
     u32x2 lo[D], hi[D];
     // a channel block of 32 is 64 bytes on: bits above the two lowest of the chunk's number, which the swizzle may have set
     template <int I> DEVFN void read(unsigned tile, const TileLane<bf16_t, DP> &l)
@@ -231,7 +229,7 @@ template <int OFF> DEVFN float lds_read4(unsigned addr)
 }
 template <int DP, int NS> struct Second<float, DP, NS> {
     using L = Tile<float, DP>;
-    static constexpr int DB = L::DB, N = NS * DB;
+    static constexpr int DB = L::DB, N = NS * DB, READS = 0;
     float buf[8];
     DEVFN void begin(unsigned, const TileLane<float, DP> &) {}
     // register v of a lane's column is row 8 (v / 4) + 4 half + v % 4: one 32x32x2 product takes v of both halves

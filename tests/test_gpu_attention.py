@@ -197,6 +197,16 @@ def test_few_queries_over_many_keys(env, case, bf16):
 
 
 @pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("mask", [(-1, -1), (-1, 0), (50, 9)], ids=str)
+@pytest.mark.parametrize("dim", [24, 40, 64, 72, 96, 104, 128])
+def test_many_blocks(env, dim, mask, bf16):
+    """Enough of them to fill the card: blocks of 128 columns, forward and backward."""
+    Case(env, 33, 70, 150, 16, 8, dim, *mask, bf16).check()
+    lq, lk = [(b * 37) % 71 for b in range(33)], [(b * 61) % 151 for b in range(33)]
+    Case(env, 33, 70, 150, 8, 8, dim, *mask, bf16, q_side=("packed", lq, 1, 2), kv_side=lk).check(True, False)
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
 def test_large_scores_and_scale(env, bf16):
     """Scores of hundreds: the running maximum grows again and again, most probabilities vanish."""
     Case(env, 1, 150, 400, 2, 1, 64, bf16=bf16, spread=30.0).check()
