@@ -403,7 +403,7 @@ typedef struct {
     int32_t axes, pairs[3];     /* axes 1 ... 3; 2 P <= dim */
     int32_t io_dtype;           /* dp_dtype of every tensor but gamma, pos and freq */
     uint32_t flags;             /* DP_QK_NORM, DP_ROTARY_HALVES */
-    float eps;                  /* > 0 with DP_QK_NORM */
+    float eps;                  /* >= 2^-126 with DP_QK_NORM */
     int32_t reserved;           /* 0 */
     int64_t q_stride, k_stride; /* elements between rows of q and k */
     int64_t q_out_stride, k_out_stride; /* of q_out and k_out, and of dq_out and dk_out */

@@ -39,6 +39,18 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
     const int first = (int)lo, keys = (int)max(0ll, hi - lo);
     const long long row = rq.first + i, stat = (long long)head * a.q.rows + row;
 
+    TileCopy<T, DP, KT, 256> ck, cv;
+    ck.init(threadIdx.x, a.dim, a.k_stride);
+    cv.init(threadIdx.x, a.dim, a.v_stride);
+    const T *kp = reinterpret_cast<const T *>(a.kp) + (rk.first + first) * a.k_stride + (long long)hk * a.dim;
+    const T *vp = reinterpret_cast<const T *>(a.vp) + (rk.first + first) * a.v_stride + (long long)hk * a.dim;
+    const unsigned base = lds_offset(s_tiles);
+    TileLane<T, DP> tl;
+    tl.init(lane);
+    if (keys > 0) {   // under way while the queries' rows are loaded
+        ck.issue(kp, keys, a.dim, a.k_stride, base, wave);
+        cv.issue(vp, keys, a.dim, a.v_stride, base + STAGES * BYTES, wave);
+    }
     u32x4 q[L::SLICES], g[L::SLICES];
     load_column<T, DP>(reinterpret_cast<const T *>(a.qp) + row * a.q_stride + (long long)head * a.dim, on, a.dim, half, q);
     float delta = 0.f, lse2 = INFINITY;
@@ -74,16 +86,6 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
     f32x16 acc[DB];
     clear(acc);
     if (keys > 0) {
-        TileCopy<T, DP, KT, 256> ck, cv;
-        ck.init(threadIdx.x, a.dim, a.k_stride);
-        cv.init(threadIdx.x, a.dim, a.v_stride);
-        const T *kp = reinterpret_cast<const T *>(a.kp) + (rk.first + first) * a.k_stride + (long long)hk * a.dim;
-        const T *vp = reinterpret_cast<const T *>(a.vp) + (rk.first + first) * a.v_stride + (long long)hk * a.dim;
-        const unsigned base = lds_offset(s_tiles);
-        TileLane<T, DP> tl;
-        tl.init(lane);
-        ck.issue(kp, keys, a.dim, a.k_stride, base, wave);
-        cv.issue(vp, keys, a.dim, a.v_stride, base + STAGES * BYTES, wave);
         unsigned stage = 0;
         for (int t = 0; t < keys; t += KT) {
             wait_vmcnt<0>();
@@ -199,8 +201,6 @@ template <typename T, int DP> __global__ __launch_bounds__(512, 2) void k_attent
     f32x16 sum[DB];
     clear(sum);
     if (w.count > 0) {
-        u32x4 column_of[L::SLICES];
-        load_column<T, DP>((second ? reinterpret_cast<const T *>(a.vp) + row * a.v_stride : reinterpret_cast<const T *>(a.kp) + row * a.k_stride) + (long long)hk * a.dim, on, a.dim, half, column_of);
         const unsigned base = lds_offset(s_tiles), mine = base + second * STAGES * BYTES, other = base + (second ^ 1) * STAGES * BYTES, stats = lds_offset(s_stats) + second * sizeof(s_stats[0]),
                        pt = lds_offset(s_p) + pair * sizeof(s_p[0]) + lane * 16;
         const long long stride = second ? a.o_stride : a.q_stride;
@@ -227,6 +227,8 @@ template <typename T, int DP> __global__ __launch_bounds__(512, 2) void k_attent
             if (it >= w.count) { it = 0; ++ih; }
         };
         issue();
+        u32x4 column_of[L::SLICES];
+        load_column<T, DP>((second ? reinterpret_cast<const T *>(a.vp) + row * a.v_stride : reinterpret_cast<const T *>(a.kp) + row * a.k_stride) + (long long)hk * a.dim, on, a.dim, half, column_of);
         int t = 0, slot = 0;
         for (int n = 0; n <= all; ++n) {
             // tile n has arrived, p of tile n - 1 too, and tile n - 2 is done with: its room takes tile n + 1
@@ -301,34 +303,31 @@ template <typename T, int DP> __global__ __launch_bounds__(512, 2) void k_attent
     else store_column<T, DB>(sum, 1.f, reinterpret_cast<T *>(a.dv) + row * a.v_stride + (long long)hk * a.dim, a.dim, half);
 }
 
-// dk and dv for 32 keys, where there are few: four wavefronts share each tile of queries.
-template <typename T, int DP> __global__ __launch_bounds__(256, 1) void k_attention_dkv_few(AttnArgs a)
+// dk and dv with both sums in one wavefront: for 32 keys, where there are few (four wavefronts share each tile of queries), and for 128 of narrow heads, whose sums leave room.
+template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 ? 2 : 1) void k_attention_dkv_whole(AttnArgs a)
 {
     using L = Tile<T, DP>;
-    using S = Shape<T, DP, 1>;
-    constexpr int QT = S::RT, DB = L::DB, BYTES = S::BYTES, STAGES = S::STAGES, COLS = 32;
-    constexpr int ROOM = 2 * STAGES * BYTES > 4 * DB * 4096 ? 2 * STAGES * BYTES : 4 * DB * 4096;
-    __shared__ alignas(1024) char s_tiles[ROOM];            // q and dout of each stage
-    __shared__ alignas(16) float s_stats[STAGES][2][QT];    // lse2 and delta
+    using S = Shape<T, DP, CW>;
+    constexpr int RW = S::RW, NB = S::NB, QT = S::RT, DB = L::DB, BYTES = S::BYTES, STAGES = S::STAGES, COLS = CW * 32;
+    constexpr int ROOM = 2 * STAGES * BYTES > (RW > 1 ? 4 * DB * 4096 : 0) ? 2 * STAGES * BYTES : 4 * DB * 4096, SIDE = QT < 64 ? 64 : QT;
+    __shared__ alignas(1024) char s_tiles[ROOM];              // q and dout of each stage
+    __shared__ alignas(16) float s_stats[STAGES][2][SIDE];    // lse2 and delta
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int id = logical_block(blockIdx.x, gridDim.x);
     const int hb = id / a.tiles, b = hb % a.n, hk = hb / a.n;
-    const int col0 = (id % a.tiles) * COLS;
+    const int col0 = (id % a.tiles) * COLS, wcol = col0 + wave % CW * 32, wr = wave / CW;
     const Rows rq = rows_of(a.q, b), rk = rows_of(a.kv, b);
     if (col0 >= rk.own) return;
-    const int j = col0 + (lane & 31);
+    const int j = wcol + (lane & 31);
     const bool own = j < rk.own, on = j < rk.used;
-    const Seen w = seen_by<COLS>(a, rq, rk, col0, col0, j);
+    const Seen w = seen_by<COLS>(a, rq, rk, col0, wcol, j);
     const long long row = rk.first + j;
-    const int mine = wave * 32;
+    const int mine = wr * NB * 32;
 
     f32x16 dk[DB], dv[DB];
     clear(dk);
     clear(dv);
     if (w.count > 0) {
-        u32x4 kc[L::SLICES], vc[L::SLICES];
-        load_column<T, DP>(reinterpret_cast<const T *>(a.kp) + row * a.k_stride + (long long)hk * a.dim, on, a.dim, half, kc);
-        load_column<T, DP>(reinterpret_cast<const T *>(a.vp) + row * a.v_stride + (long long)hk * a.dim, on, a.dim, half, vc);
         TileCopy<T, DP, QT, 256> cq, cg;
         cq.init(threadIdx.x, a.dim, a.q_stride);
         cg.init(threadIdx.x, a.dim, a.o_stride);
@@ -342,29 +341,36 @@ template <typename T, int DP> __global__ __launch_bounds__(256, 1) void k_attent
             const int rows = w.count - it;
             cq.issue(reinterpret_cast<const T *>(a.qp) + at * a.q_stride + (long long)ih * a.dim, rows, a.dim, a.q_stride, base + slot_in * BYTES, wave);
             cg.issue(reinterpret_cast<const T *>(a.dout) + at * a.o_stride + (long long)ih * a.dim, rows, a.dim, a.o_stride, base + (STAGES + slot_in) * BYTES, wave);
-            // wavefront w: half w % 2 of the statistics w / 2
-            const auto r = make_rsrc((wave < 2 ? a.lse2 : a.delta) + (long long)ih * a.q.rows + at, (unsigned)min(rows, QT) * 4);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void)(size_t)(stats + slot_in * 2 * QT * 4 + wave * 256), 4, ((wave & 1) * 64 + lane) * 4, 0, 0, 0);
+            // wavefronts 0 and 1: lse2, 64 rows each; 2 and 3: delta
+            if ((wave & 1) * 64 < QT) {
+                const auto r = make_rsrc((wave < 2 ? a.lse2 : a.delta) + (long long)ih * a.q.rows + at, (unsigned)min(rows, QT) * 4);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void)(size_t)(stats + ((slot_in * 2 + (wave >> 1)) * SIDE + (wave & 1) * 64) * 4), 4, ((wave & 1) * 64 + lane) * 4, 0, 0, 0);
+            }
             if (STAGES == 2) slot_in ^= 1;
             it += QT;
             if (it >= w.count) { it = 0; ++ih; }
         };
-        static_assert(QT == 128, "the statistics are copied by four wavefronts of 64 lanes");
+        static_assert(QT <= 128, "two wavefronts copy a statistic");
         issue();
+        u32x4 kc[L::SLICES], vc[L::SLICES];
+        load_column<T, DP>(reinterpret_cast<const T *>(a.kp) + row * a.k_stride + (long long)hk * a.dim, on, a.dim, half, kc);
+        load_column<T, DP>(reinterpret_cast<const T *>(a.vp) + row * a.v_stride + (long long)hk * a.dim, on, a.dim, half, vc);
         int slot = 0, t = 0;
         for (int n = 0; n < all; ++n) {
             wait_vmcnt<0>();
             __builtin_amdgcn_s_barrier();   // the tile has arrived, and the one before is done with
             if (STAGES == 2 && n + 1 < all) issue();
-            const int at = t + mine;
-            if (at > w.none0 && at < w.none1) {
-                const unsigned qt = base + slot * BYTES + mine * L::RB, gt = qt + STAGES * BYTES, st = stats + slot * 2 * QT * 4 + mine * 4 + half * 16;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const int in = mine + 32 * nb, at = t + in;
+                if (at <= w.none0 || at >= w.none1) continue;
+                const unsigned qt = base + slot * BYTES + in * L::RB, gt = qt + STAGES * BYTES, st = stats + (slot * 2 * SIDE + in) * 4 + half * 16;
                 f32x16 s[1], dp[1];
                 clear(s);
                 clear(dp);
                 u32x4 l2[4], de[4];   // of rows 8 g + 4 half ...
                 l2[0] = lds_read16<0>(st); l2[1] = lds_read16<32>(st); l2[2] = lds_read16<64>(st); l2[3] = lds_read16<96>(st);
-                de[0] = lds_read16<QT * 4>(st); de[1] = lds_read16<QT * 4 + 32>(st); de[2] = lds_read16<QT * 4 + 64>(st); de[3] = lds_read16<QT * 4 + 96>(st);
+                de[0] = lds_read16<SIDE * 4>(st); de[1] = lds_read16<SIDE * 4 + 32>(st); de[2] = lds_read16<SIDE * 4 + 64>(st); de[3] = lds_read16<SIDE * 4 + 96>(st);
                 TwoFirst<T, DP, 6> ab;
                 ab.begin(qt + tl.row, gt + tl.row, tl.x);
                 ab.run(qt + tl.row, gt + tl.row, tl.x, kc, vc, s[0], dp[0]);
@@ -390,15 +396,16 @@ template <typename T, int DP> __global__ __launch_bounds__(256, 1) void k_attent
             t = t + QT >= w.count ? 0 : t + QT;
         }
     }
-    // one after the other: the room of dk's sums takes dv's
-    __syncthreads();
-    sum_waves<4>(dk, reinterpret_cast<float *>(s_tiles), wave, lane);
-    __syncthreads();
-    sum_waves<4>(dv, reinterpret_cast<float *>(s_tiles), wave, lane);
+    if constexpr (RW > 1) {   // one after the other: the room of dk's sums takes dv's
+        __syncthreads();
+        sum_waves<4>(dk, reinterpret_cast<float *>(s_tiles), wave, lane);
+        __syncthreads();
+        sum_waves<4>(dv, reinterpret_cast<float *>(s_tiles), wave, lane);
+    }
     if (!own) return;
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
-        if (db != wave) continue;
+        if (RW > 1 && db != wr) continue;
         if (!on) {
 #pragma unroll
             for (int v = 0; v < 16; ++v) dk[db][v] = dv[db][v] = 0.f;
@@ -406,6 +413,12 @@ template <typename T, int DP> __global__ __launch_bounds__(256, 1) void k_attent
         store_block<T>(dk[db], a.scale, reinterpret_cast<T *>(a.dk) + row * a.k_stride + (long long)hk * a.dim, db * 32, a.dim, half);
         store_block<T>(dv[db], 1.f, reinterpret_cast<T *>(a.dv) + row * a.v_stride + (long long)hk * a.dim, db * 32, a.dim, half);
     }
+}
+
+template <typename T, int DP, bool WHOLE> auto wide_kernel()
+{
+    if constexpr (WHOLE) return k_attention_dkv_whole<T, DP, 4>;
+    else return k_attention_dkv<T, DP>;
 }
 
 // Blocks of 128 columns where they fill the card; else of 32, whose wavefronts share the rows of the other side.
@@ -419,7 +432,11 @@ template <typename T> void launch(AttnArgs &a, long long groups, hipStream_t st)
         a.tiles = (int)((qc + (wq ? 127 : 31)) / (wq ? 128 : 32));
         if (a.tiles > 0 && a.q.rows > 0) hipLaunchKernelGGL((wq ? k_attention_dq<T, DP, 4> : k_attention_dq<T, DP, 1>), dim3((unsigned)(groups * a.tiles)), dim3(256), 0, st, a);
         a.tiles = (int)((kc + (wk ? 127 : 31)) / (wk ? 128 : 32));
-        if (a.tiles > 0 && a.kv.rows > 0) hipLaunchKernelGGL((wk ? k_attention_dkv<T, DP> : k_attention_dkv_few<T, DP>), dim3((unsigned)(groups * a.tiles)), dim3(wk ? 512 : 256), 0, st, a);
+        if (a.tiles > 0 && a.kv.rows > 0) {
+            constexpr bool whole = sizeof(T) == 2 && DP <= 64;
+            auto *kernel = !wk ? k_attention_dkv_whole<T, DP, 1> : wide_kernel<T, DP, whole>();
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(groups * a.tiles)), dim3(wk && !whole ? 512 : 256), 0, st, a);
+        }
     });
 }
 

@@ -13,15 +13,16 @@ namespace {
 constexpr float kSlack = 8.f;
 
 // Wavefronts of a block: CW of them side by side in columns, 4 / CW share the keys of each tile among them.
-template <typename T, int DP, int CW> struct Shape {
+// With split keys there are many blocks, and two of them on a compute unit with one tile each load more than one with two.
+template <typename T, int DP, int CW, bool SPLIT> struct Shape {
     static constexpr int RW = 4 / CW, NB = sizeof(T) == 2 && CW == 4 ? 2 : 1, KT = RW * NB * 32, BYTES = KT * Tile<T, DP>::RB;   // NB: blocks of 32 keys of a wavefront
-    static constexpr int STAGES = 4 * BYTES <= 131072 ? 2 : 1;
+    static constexpr int STAGES = 4 * BYTES <= (SPLIT ? 65536 : 131072) ? 2 : 1;
 };
 
-template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(256, CW == 4 && (sizeof(T) == 2 || DP <= 64) ? 2 : 1) void k_attention(AttnArgs a)
+template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(256, (CW == 4 || SPLIT) && (sizeof(T) == 2 || DP <= 64) ? 2 : 1) void k_attention(AttnArgs a)
 {
     using L = Tile<T, DP>;
-    using S = Shape<T, DP, CW>;
+    using S = Shape<T, DP, CW, SPLIT>;
     constexpr int RW = S::RW, NB = S::NB, KT = S::KT, DB = L::DB, BYTES = S::BYTES, STAGES = S::STAGES, COLS = CW * 32;
     constexpr int ROOM = 2 * STAGES * BYTES > (RW > 1 ? 4 * DB * 4096 : 0) ? 2 * STAGES * BYTES : 4 * DB * 4096;
     __shared__ alignas(1024) char s_tiles[ROOM];   // K and V of each stage
@@ -53,8 +54,6 @@ template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(2
     const int first = (int)lo, keys = (int)max(0ll, hi - lo);
     const long long row = rq.first + i;
 
-    u32x4 q[L::SLICES];
-    load_column<T, DP>(reinterpret_cast<const T *>(a.qp) + row * a.q_stride + (long long)head * a.dim, on, a.dim, half, q);
     // the lane's keys, counted from the wavefront's place in the first tile
     const int mine = wr * NB * 32;
     const long long see0 = max((long long)i + ahead - a.left - first, 0ll), see1 = min((long long)i + ahead + a.right + 1 - first, (long long)keys);
@@ -78,6 +77,8 @@ template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(2
         tl.init(lane);
         ck.issue(kp, keys, a.dim, a.k_stride, base, wave);
         cv.issue(vp, keys, a.dim, a.v_stride, base + STAGES * BYTES, wave);
+        u32x4 q[L::SLICES];
+        load_column<T, DP>(reinterpret_cast<const T *>(a.qp) + row * a.q_stride + (long long)head * a.dim, on, a.dim, half, q);
         unsigned stage = 0;
         for (int t = 0; t < keys; t += KT) {
             wait_vmcnt<0>();
@@ -250,7 +251,7 @@ Form form_of(const dp_attention_desc &d)
     long long span = d.kv_len;   // keys that a block looks at
     if (d.left >= 0 && d.right >= 0) span = std::min<long long>(span, (long long)d.left + d.right + 32);
     const long long most = std::min<long long>(kMaxSplits, (span + 4 * kt - 1) / (4 * kt));   // four tiles at least: the join takes as long as two
-    const long long want = std::min<long long>(most, 1024 / blocks);
+    const long long want = std::min<long long>(most, 2048 / blocks);
     if (want < 2) return {1, 1, 0};
     // whole tiles; a window is anywhere in the sequence, so its split counts over all keys
     const long long per = ((d.kv_len + want - 1) / want + kt - 1) / kt * kt;
