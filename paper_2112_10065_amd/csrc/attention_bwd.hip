@@ -176,17 +176,19 @@ DEVFN void hide(f32x16 &s, const Seen &w, int t, int half)
         if ((unsigned)(t + 8 * (v >> 2) + 4 * half + (v & 3) - w.seen0) >= w.seen) s[v] = -INFINITY;
 }
 
-// dk and dv for 128 keys.  The sums of both and the operands k and v take more registers than two wavefronts on a SIMD have, and one alone has nothing to run beside its
-// exponentials; so two of them share 32 keys: the first makes p and dv, the second, a tile of queries behind, dp, ds and dk.  p goes from one to the other through LDS, in
-// 32 bits, lane by lane.  Both do the same on exchanged tiles: x = rows a . column (q k, or dout v), then sum += rows b^T x (dout p, or q ds).
-template <typename T, int DP> __global__ __launch_bounds__(512, 2) void k_attention_dkv(AttnArgs a)
+// dk and dv for 128 keys of wide heads.  Both sums and the operands k and v take more registers than each of two wavefronts on a SIMD has, and one alone has nothing to run
+// beside its exponentials; so two share 32 keys.  Of each tile of 64 queries each makes p and ds for its half of the queries, and then one adds up dk, the other dv, over all of
+// them: what the other wavefront's half needs of p or ds goes through LDS, already rounded, lane by lane.  The sums are one tile behind the products, so that
+// a wavefront's exponentials lie between matrix products that do not wait for them.
+template <int DP> __global__ __launch_bounds__(512, 2) void k_attention_dkv(AttnArgs a)
 {
+    using T = bf16_t;
     using L = Tile<T, DP>;
-    constexpr int NB = 64 * L::RB <= 16384 ? 2 : 1, QT = NB * 32, DB = L::DB, BYTES = QT * L::RB, STAGES = 3, COLS = 128;
+    constexpr int QT = 64, DB = L::DB, BYTES = QT * L::RB, STAGES = 3, COLS = 128;
     using Copy = TileCopy<T, DP, QT, 256>;
     __shared__ alignas(1024) char s_tiles[2 * STAGES * BYTES];   // q and dout of each stage
-    __shared__ alignas(16) float s_stats[2][STAGES][64];         // lse2 and delta
-    __shared__ alignas(16) float s_p[4][NB * 16 * 64];
+    __shared__ alignas(16) float s_stats[STAGES][2][QT];         // lse2 and -delta
+    __shared__ alignas(16) u32x4 s_packs[2][8][2][64];           // [tile][wavefront][slice][lane]: the first's p, the second's ds
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, pair = wave & 3, second = wave >> 2;
     const int id = logical_block(blockIdx.x, gridDim.x);
     const int hb = id / a.tiles, b = hb % a.n, hk = hb / a.n;
@@ -198,11 +200,10 @@ template <typename T, int DP> __global__ __launch_bounds__(512, 2) void k_attent
     const Seen w = seen_by<COLS>(a, rq, rk, col0, wcol, j);
     const long long row = rk.first + j;
 
-    f32x16 sum[DB];
+    f32x16 sum[DB];   // the first's dk, the second's dv
     clear(sum);
     if (w.count > 0) {
-        const unsigned base = lds_offset(s_tiles), mine = base + second * STAGES * BYTES, other = base + (second ^ 1) * STAGES * BYTES, stats = lds_offset(s_stats) + second * sizeof(s_stats[0]),
-                       pt = lds_offset(s_p) + pair * sizeof(s_p[0]) + lane * 16;
+        const unsigned tiles_q = lds_offset(s_tiles), tiles_g = tiles_q + STAGES * BYTES, stats = lds_offset(s_stats), packs = lds_offset(s_packs) + lane * 16;
         const long long stride = second ? a.o_stride : a.q_stride;
         const T *from = reinterpret_cast<const T *>(second ? a.dout : a.qp);
         const float *stat_from = second ? a.delta : a.lse2;
@@ -212,99 +213,108 @@ template <typename T, int DP> __global__ __launch_bounds__(512, 2) void k_attent
         tl.init(lane);
         const int tiles = (w.count + QT - 1) / QT, all = tiles * a.shared;
         // tile n: queries first + QT (n % tiles) ... of the n / tiles-th head; rows behind the last query arrive as zeros, also their statistics: nothing is added then.
-        // The first wavefronts copy q and lse2, the second dout and delta.
+        // The first wavefronts copy q and lse2, the second dout and -delta.
         int ih = hk * a.shared, it = 0, slot_in = 0;
         auto issue = [&] {
             const long long at = rq.first + w.first + it;
             const int rows = w.count - it;
-            copy.issue(from + at * stride + (long long)ih * a.dim, rows, a.dim, stride, mine + slot_in * BYTES, pair);
+            copy.issue(from + at * stride + (long long)ih * a.dim, rows, a.dim, stride, (second ? tiles_g : tiles_q) + slot_in * BYTES, pair);
             if (pair == 0) {
                 const auto r = make_rsrc(stat_from + (long long)ih * a.q.rows + at, (unsigned)min(rows, QT) * 4);
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void)(size_t)(stats + slot_in * 256), 4, lane * 4, 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void)(size_t)(stats + (slot_in * 2 + second) * QT * 4), 4, lane * 4, 0, 0, 0);
             }
             slot_in = slot_in + 1 == STAGES ? 0 : slot_in + 1;
             it += QT;
             if (it >= w.count) { it = 0; ++ih; }
         };
         issue();
-        u32x4 column_of[L::SLICES];
-        load_column<T, DP>((second ? reinterpret_cast<const T *>(a.vp) + row * a.v_stride : reinterpret_cast<const T *>(a.kp) + row * a.k_stride) + (long long)hk * a.dim, on, a.dim, half, column_of);
-        int t = 0, slot = 0;
-        for (int n = 0; n <= all; ++n) {
-            // tile n has arrived, p of tile n - 1 too, and tile n - 2 is done with: its room takes tile n + 1
+        u32x4 kc[L::SLICES], vc[L::SLICES];
+        load_column<T, DP>(reinterpret_cast<const T *>(a.kp) + row * a.k_stride + (long long)hk * a.dim, on, a.dim, half, kc);
+        load_column<T, DP>(reinterpret_cast<const T *>(a.vp) + row * a.v_stride + (long long)hk * a.dim, on, a.dim, half, vc);
+        u32x4 mine[2];   // ds (the first's) or p (the second's) of the own half of the tile before
+        int t = 0, slot = 0, before = 0;
+        f32x16 s, dp;
+        u32x4 l2[4];     // of rows 8 g + 4 half ... of the own half
+        const auto arrive = [&](int n) {   // tile n, and the packs of tile n - 1; tile n - 2 is done with: its room takes tile n + 1
             wait_vmcnt<0>();
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             if (n + 1 < all) issue();
-            const bool part = second ? n > 0 : n < all;
-            f32x16 x[NB];
-            bool some[NB], any = false;
-            const int at = t;
+        };
+        const auto products = [&] {
+            const unsigned qt = tiles_q + slot * BYTES + second * 32 * L::RB + tl.row, gt = qt + STAGES * BYTES, st = stats + slot * 2 * QT * 4 + second * 128 + half * 16;
+            u32x4 de[4];
+            de[0] = lds_read16<QT * 4>(st); de[1] = lds_read16<QT * 4 + 32>(st); de[2] = lds_read16<QT * 4 + 64>(st); de[3] = lds_read16<QT * 4 + 96>(st);
+            l2[0] = lds_read16<0>(st); l2[1] = lds_read16<32>(st); l2[2] = lds_read16<64>(st); l2[3] = lds_read16<96>(st);
+            TwoFirst<T, DP, 6> ab;
+            ab.begin(qt, gt, tl.x);
+            wait_reads<1, 6>();
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                some[nb] = part && at + 32 * nb > w.none0 && at + 32 * nb < w.none1;
-                any |= some[nb];
+            for (int e = 0; e < 4; ++e) { tie(de[e]); tie(l2[e]); }
+#pragma unroll
+            for (int v = 0; v < 16; ++v) { s[v] = 0.f; dp[v] = __uint_as_float(de[v >> 2][v & 3]); }   // dp - delta: the sum begins at -delta
+            ab.run(qt, gt, tl.x, kc, vc, s, dp);
+            hide(s, w, t + 32 * second, half);
+        };
+        const auto soften = [&](int v) {   // s -> p, dp -> ds
+            s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], a.scale2, -__uint_as_float(l2[v >> 2][v & 3])));
+            dp[v] *= s[v];
+        };
+        const auto pack = [&](int n) {
+            const unsigned pk = packs + (n & 1) * sizeof(s_packs[0]) + wave * sizeof(s_packs[0][0]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const u32x4 p = column<T>(s, h), ds = column<T>(dp, h);
+                mine[h] = second ? p : ds;
+                lds_write16(pk + h * 1024, second ? ds : p);
             }
-            if (any) {
-                const unsigned xt = mine + slot * BYTES, yt = other + slot * BYTES, st = stats + slot * 256 + half * 16;
-                First<T, DP, NB, 6> first;
-                u32x4 f[NB][4];   // statistics of rows 8 g + 4 half ..., or p
-                if (second) {     // dp - delta: the sum begins at -delta
-                    for_constant<NB * 4>([&](auto ic) { constexpr int i = decltype(ic)::value; f[i / 4][i % 4] = lds_read16<i * 32>(st); });
-                    first.begin(xt + tl.row, tl.x);
-                    wait_reads<1, decltype(first)::D>();
+            before = slot;
+            slot = slot + 1 == STAGES ? 0 : slot + 1;
+            t = t + QT >= w.count ? 0 : t + QT;
+        };
+        // the sums of tile n: the own half of its queries, then the other's; beside(i), i = 0 ... 4 DB - 1
+        const auto add = [&](int n, auto &&beside) {
+            const unsigned yt = (second ? tiles_g : tiles_q) + before * BYTES, pk = packs + (n & 1) * sizeof(s_packs[0]) + (wave ^ 4) * sizeof(s_packs[0][0]);
+            u32x4 other[2];
+            other[0] = lds_read16<0>(pk);
+            other[1] = lds_read16<1024>(pk);
+            const unsigned at = yt + second * 32 * L::RB, back = yt + (second ^ 1) * 32 * L::RB;
+            Second<T, DP, 2> x, y;
+            x.begin(at, tl);
+            wait_reads<1, decltype(x)::READS>();
+            tie(other[0]);
+            tie(other[1]);
+            x.run_beside(at, tl, [&](auto sl) { return mine[decltype(sl)::value]; }, sum, [&](auto i) { beside(std::integral_constant<int, decltype(i)::value>{}); });
+            y.begin(back, tl);
+            y.run_beside(back, tl, [&](auto sl) { return other[decltype(sl)::value]; }, sum, [&](auto i) { beside(std::integral_constant<int, decltype(i)::value + 2 * DB>{}); });
+        };
+        arrive(0);
+        products();
 #pragma unroll
-                    for (int i = 0; i < NB * 4; ++i) tie(f[i / 4][i % 4]);
+        for (int v = 0; v < 16; ++v) soften(v);
+        pack(0);
+        for (int n = 1; n < all; ++n) {
+            arrive(n);
+            products();
+            add(n - 1, [&](auto ic) {
+                constexpr int i = decltype(ic)::value, N = 4 * DB;
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) x[nb][v] = __uint_as_float(f[nb][v >> 2][v & 3]);
-                } else {
-                    clear(x);
-                    first.begin(xt + tl.row, tl.x);
-                }
-                first.run(xt + tl.row, tl.x, column_of, x);
-                Second<T, DP, 2 * NB> next;
-                if (second) for_constant<NB * 4>([&](auto ic) { constexpr int i = decltype(ic)::value; f[i / 4][i % 4] = lds_read16<i * 1024>(pt); });
-                else for_constant<NB * 4>([&](auto ic) { constexpr int i = decltype(ic)::value; f[i / 4][i % 4] = lds_read16<i * 32>(st); });
-                next.begin(yt, tl);
-                wait_reads<1, decltype(next)::READS>();
-#pragma unroll
-                for (int i = 0; i < NB * 4; ++i) tie(f[i / 4][i % 4]);
-                if (second) {
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) x[nb][v] *= __uint_as_float(f[nb][v >> 2][v & 3]);
-                } else {
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) {
-                        hide(x[nb], w, at + 32 * nb, half);
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) x[nb][v] = __builtin_amdgcn_exp2f(fmaf(x[nb][v], a.scale2, -__uint_as_float(f[nb][v >> 2][v & 3])));
-                    }
-                }
-                next.run(yt, tl, [&](auto sc) { constexpr int sl = decltype(sc)::value; return column<T>(x[sl / 2], sl % 2); }, sum);
-            }
-            if (part) {
-                t = t + QT >= w.count ? 0 : t + QT;
-                slot = slot + 1 == STAGES ? 0 : slot + 1;
-            }
-            __builtin_amdgcn_s_barrier();   // p of the tile before is read
-            if (any && !second) for_constant<NB * 4>([&](auto ic) {
-                constexpr int i = decltype(ic)::value, nb = i / 4, g = i % 4;
-                lds_write16(pt + i * 1024, __builtin_bit_cast(u32x4, f32x4{x[nb][4 * g], x[nb][4 * g + 1], x[nb][4 * g + 2], x[nb][4 * g + 3]}));
+                for (int v = i * 16 / N; v < (i + 1) * 16 / N; ++v) soften(v);
             });
+            pack(n);
         }
+        arrive(all);
+        add(all - 1, [](auto) {});
     }
     if (!own) return;
     if (!on) clear(sum);
-    if (second) store_column<T, DB>(sum, a.scale, reinterpret_cast<T *>(a.dk) + row * a.k_stride + (long long)hk * a.dim, a.dim, half);
-    else store_column<T, DB>(sum, 1.f, reinterpret_cast<T *>(a.dv) + row * a.v_stride + (long long)hk * a.dim, a.dim, half);
+    if (second) store_column<T, DB>(sum, 1.f, reinterpret_cast<T *>(a.dv) + row * a.v_stride + (long long)hk * a.dim, a.dim, half);
+    else store_column<T, DB>(sum, a.scale, reinterpret_cast<T *>(a.dk) + row * a.k_stride + (long long)hk * a.dim, a.dim, half);
 }
 
-// dk and dv with both sums in one wavefront: for 32 keys, where there are few (four wavefronts share each tile of queries), and for 128 of narrow heads, whose sums leave room.
-template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 ? 2 : 1) void k_attention_dkv_whole(AttnArgs a)
+// dk and dv with both sums in one wavefront: for 32 keys, where there are few (four wavefronts share each tile of queries), and for 128 of narrow heads, whose sums leave room, or
+// in fp32, where the matrix products take sixteen times as long as with bf16 and hide the rest.
+template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 && sizeof(T) == 2 ? 2 : 1) void k_attention_dkv_whole(AttnArgs a)
 {
     using L = Tile<T, DP>;
     using S = Shape<T, DP, CW>;
@@ -418,7 +428,7 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
 template <typename T, int DP, bool WHOLE> auto wide_kernel()
 {
     if constexpr (WHOLE) return k_attention_dkv_whole<T, DP, 4>;
-    else return k_attention_dkv<T, DP>;
+    else return k_attention_dkv<DP>;
 }
 
 // Blocks of 128 columns where they fill the card; else of 32, whose wavefronts share the rows of the other side.
@@ -433,7 +443,7 @@ template <typename T> void launch(AttnArgs &a, long long groups, hipStream_t st)
         if (a.tiles > 0 && a.q.rows > 0) hipLaunchKernelGGL((wq ? k_attention_dq<T, DP, 4> : k_attention_dq<T, DP, 1>), dim3((unsigned)(groups * a.tiles)), dim3(256), 0, st, a);
         a.tiles = (int)((kc + (wk ? 127 : 31)) / (wk ? 128 : 32));
         if (a.tiles > 0 && a.kv.rows > 0) {
-            constexpr bool whole = sizeof(T) == 2 && DP <= 64;
+            constexpr bool whole = sizeof(T) == 4 || DP <= 64;
             auto *kernel = !wk ? k_attention_dkv_whole<T, DP, 1> : wide_kernel<T, DP, whole>();
             hipLaunchKernelGGL(kernel, dim3((unsigned)(groups * a.tiles)), dim3(wk && !whole ? 512 : 256), 0, st, a);
         }

@@ -207,17 +207,28 @@ template <int DP, int NS> struct Second<bf16_t, DP, NS> {
         hi[I % D] = lds_read_tr<(s * 16 + 8) * L::RB>(tile + (l.hi ^ (unsigned)(db * 64)));
     }
     DEVFN void begin(unsigned tile, const TileLane<bf16_t, DP> &l) { for_constant<D>([&](auto i) { read<decltype(i)::value>(tile, l); }); }
+    template <int I, typename F> DEVFN void item(unsigned tile, const TileLane<bf16_t, DP> &l, F &&cols, f32x16 (&acc)[DB])
+    {
+        constexpr int left = (N - I < D ? N - I : D) - 1;
+        wait_reads<2, left>();
+        tie(lo[I % D]);
+        tie(hi[I % D]);
+        const u32x4 a = {lo[I % D].x, lo[I % D].y, hi[I % D].x, hi[I % D].y};
+        Mma<bf16_t>::first(a, cols(std::integral_constant<int, I / DB>{}), acc[I % DB]);
+        if constexpr (I + D < N) read<I + D>(tile, l);
+    }
     // cols(s): the eight rows of slice s of the lane's column, packed
     template <typename F> DEVFN void run(unsigned tile, const TileLane<bf16_t, DP> &l, F &&cols, f32x16 (&acc)[DB])
     {
-        for_constant<N>([&](auto ic) {
-            constexpr int i = decltype(ic)::value, left = (N - i < D ? N - i : D) - 1;
-            wait_reads<2, left>();
-            tie(lo[i % D]);
-            tie(hi[i % D]);
-            const u32x4 a = {lo[i % D].x, lo[i % D].y, hi[i % D].x, hi[i % D].y};
-            Mma<bf16_t>::first(a, cols(std::integral_constant<int, i / DB>{}), acc[i % DB]);
-            if constexpr (i + D < N) read<i + D>(tile, l);
+        for_constant<N>([&](auto i) { item<decltype(i)::value>(tile, l, cols, acc); });
+    }
+    // between(i): what the vector unit does beside matrix product i of N; kept in this order
+    template <typename F, typename G> DEVFN void run_beside(unsigned tile, const TileLane<bf16_t, DP> &l, F &&cols, f32x16 (&acc)[DB], G &&between)
+    {
+        for_constant<N>([&](auto i) {
+            item<decltype(i)::value>(tile, l, cols, acc);
+            between(i);
+            __builtin_amdgcn_sched_barrier(0);
         });
     }
 };
