@@ -22,9 +22,9 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
     constexpr int ROOM = 2 * STAGES * BYTES > (RW > 1 ? 4 * DB * 4096 : 0) ? 2 * STAGES * BYTES : 4 * DB * 4096;
     __shared__ alignas(1024) char s_tiles[ROOM];   // K and V of each stage
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, wc = wave % CW, wr = wave / CW;
-    const int id = logical_block(blockIdx.x, gridDim.x);
-    const int hb = id / a.tiles, b = hb % a.n, hk = hb / a.n;
-    const int col0 = (a.tiles - 1 - id % a.tiles) * COLS;
+    const Item item = item_of<COLS, false, true>(a, a.q, a.shared);
+    if (!item.any) return;
+    const int b = item.b, hk = item.hk, col0 = item.tile * COLS;
     const Rows rq = rows_of(a.q, b), rk = rows_of(a.kv, b);
     if (col0 >= rq.own * a.shared) return;
     const int wcol = col0 + wc * 32, col = wcol + (lane & 31), i = col / a.shared, head = hk * a.shared + col % a.shared;
@@ -190,9 +190,9 @@ template <int DP> __global__ __launch_bounds__(512, 2) void k_attention_dkv(Attn
     __shared__ alignas(16) float s_stats[STAGES][2][QT];         // lse2 and -delta
     __shared__ alignas(16) u32x4 s_packs[2][8][2][64];           // [tile][wavefront][slice][lane]: the first's p, the second's ds
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, pair = wave & 3, second = wave >> 2;
-    const int id = logical_block(blockIdx.x, gridDim.x);
-    const int hb = id / a.tiles, b = hb % a.n, hk = hb / a.n;
-    const int col0 = (id % a.tiles) * COLS;             // causal: the longest first
+    const Item item = item_of<COLS, false, false>(a, a.kv, 1);
+    if (!item.any) return;
+    const int b = item.b, hk = item.hk, col0 = item.tile * COLS;
     const Rows rq = rows_of(a.q, b), rk = rows_of(a.kv, b);
     if (col0 >= rk.own) return;
     const int wcol = col0 + pair * 32, j = wcol + (lane & 31);
@@ -323,9 +323,9 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
     __shared__ alignas(1024) char s_tiles[ROOM];              // q and dout of each stage
     __shared__ alignas(16) float s_stats[STAGES][2][SIDE];    // lse2 and delta
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int id = logical_block(blockIdx.x, gridDim.x);
-    const int hb = id / a.tiles, b = hb % a.n, hk = hb / a.n;
-    const int col0 = (id % a.tiles) * COLS, wcol = col0 + wave % CW * 32, wr = wave / CW;
+    const Item item = item_of<COLS, false, false>(a, a.kv, 1);
+    if (!item.any) return;
+    const int b = item.b, hk = item.hk, col0 = item.tile * COLS, wcol = col0 + wave % CW * 32, wr = wave / CW;
     const Rows rq = rows_of(a.q, b), rk = rows_of(a.kv, b);
     if (col0 >= rk.own) return;
     const int j = wcol + (lane & 31);

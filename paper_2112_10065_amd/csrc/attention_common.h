@@ -32,6 +32,7 @@ struct AttnArgs {
     float *lse2, *delta;                   // backward's workspace: lse log2(e) (+inf: sees nothing) and -sum dout o, [heads][q_rows]
     int tiles;                             // of a sequence and head of keys
     int splits, split_keys;                // forward: keys dealt out to so many blocks, split_keys each
+    bool ragged;                           // lengths differ: blocks are numbered by the work there is
     float *part_o, *part_ml;               // [split][head][q_rows][dim] and [split][head][q_rows][2]
 };
 
@@ -54,6 +55,79 @@ DEVFN Rows rows_of(const AttnSide &s, int b)
         r.own = s.len;
         r.used = s.lens != nullptr ? min(max(s.lens[b], 0), s.len) : s.len;
     }
+    return r;
+}
+
+// What a block does: sequence, head of keys, tile of columns and part of the keys.
+struct Item { int b, hk, tile, split; bool any; };
+
+DEVFN int prefix_sum(int v)   // over the lanes up to this one
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // one, two, four, eight lanes up
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // the last lane of a row to the next row
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // lane 31 to the upper half
+    return v;
+}
+
+// The grid has room for sequences of the longest length.  Whole sequences: tile by tile, head by head, a contiguous eighth for each die, so that the tiles of one head read their
+// rows from one L2.  Lengths that differ: the same over the tiles that there are, counted by each block for itself (a lane to a sequence), since tiles of nothing, numbered
+// among the others, would leave some dies with much more work than others (9 sequences of up to 1500 of 4 heads of keys, dk and dv: 73 us, 53 this way).  Tiles that hold padding alone come last.
+// `mult` columns to a row of `side`; SPLIT: every part of the keys that a sequence has; LAST_FIRST: a causal mask makes a sequence's last tiles the longest.
+constexpr int kMostRagged = 256;   // sequences: more of them are counted for longer than it helps
+template <int COLS, bool SPLIT, bool LAST_FIRST> DEVFN Item item_of(const AttnArgs &a, const AttnSide &side, int mult)
+{
+    Item r;
+    if (!a.ragged) {
+        int id = logical_block(blockIdx.x, gridDim.x);
+        r.split = SPLIT ? id % a.splits : 0;
+        if (SPLIT) id /= a.splits;
+        const int hb = id / a.tiles;
+        r.tile = LAST_FIRST ? a.tiles - 1 - id % a.tiles : id % a.tiles;
+        r.b = hb % a.n;
+        r.hk = hb / a.n;
+        r.any = true;
+        return r;
+    }
+    const int lane = threadIdx.x & 63;
+    // parts, and tiles with rows in use and in all, of sequence b
+    const auto count = [&](int b, int list, int &parts, int &used) {
+        parts = used = 0;
+        if (b >= a.n) return 0;
+        const Rows rows = rows_of(side, b);
+        parts = SPLIT ? (rows_of(a.kv, b).used + a.split_keys - 1) / a.split_keys : 1;
+        const int own = (int)(((long long)rows.own * mult + COLS - 1) / COLS);
+        used = SPLIT ? own : (int)(((long long)rows.used * mult + COLS - 1) / COLS);
+        return (list == 0 ? used : own - used) * parts;
+    };
+    int id = blockIdx.x, parts, used;
+    for (int list = 0; list < (SPLIT ? 1 : 2); ++list) {
+        int total = 0;
+        for (int base = 0; base < a.n; base += 64) total += __builtin_amdgcn_readlane(prefix_sum(count(base + lane, list, parts, used)), 63);
+        const int blocks = total * a.kv_heads;
+        if (id >= blocks) { id -= blocks; continue; }
+        id = logical_block(id, blocks);
+        r.hk = id / total;
+        id %= total;
+        for (int base = 0; base < a.n; base += 64) {
+            const int c = count(base + lane, list, parts, used), sum = prefix_sum(c);
+            const unsigned long long found = __ballot(sum > id);
+            if (found == 0) { id -= __builtin_amdgcn_readlane(sum, 63); continue; }
+            const int l = __ffsll(found) - 1;
+            id -= __builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(c, l);
+            parts = __builtin_amdgcn_readlane(parts, l);
+            r.b = base + l;
+            r.split = id % parts;
+            used = __builtin_amdgcn_readlane(used, l);
+            r.tile = list != 0 ? used + id : LAST_FIRST ? used - 1 - id / parts : id / parts;
+            break;
+        }
+        r.any = true;
+        return r;
+    }
+    r.any = false;
     return r;
 }
 

@@ -28,12 +28,10 @@ template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(2
     __shared__ alignas(1024) char s_tiles[ROOM];   // K and V of each stage
     __shared__ float2 s_ml[RW > 1 ? 256 : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, wc = wave % CW, wr = wave / CW;
-    int id = logical_block(blockIdx.x, gridDim.x);
-    const int split = SPLIT ? id % a.splits : 0;
-    if (SPLIT) id /= a.splits;
-    // head by head, so that each die gets sequences of all lengths
-    const int hb = id / a.tiles, b = hb % a.n, hk = hb / a.n;
-    const int col0 = (a.tiles - 1 - id % a.tiles) * COLS;   // causal: the longest first
+    const Item item = item_of<COLS, SPLIT, true>(a, a.q, a.shared);
+    if (!item.any) return;
+    const int b = item.b, hk = item.hk, split = item.split;
+    const int col0 = item.tile * COLS;
     const Rows rq = rows_of(a.q, b), rk = rows_of(a.kv, b);
     if (col0 >= rq.own * a.shared) return;
 
@@ -191,11 +189,12 @@ template <typename T> __global__ __launch_bounds__(kJoinThreads) void k_attentio
     const int col = (blockIdx.x % a.tiles) * (kJoinThreads / 32) + (threadIdx.x >> 5), i = col / a.shared, head = hk * a.shared + col % a.shared;
     const Rows rq = rows_of(a.q, b);
     const bool own = i < rq.own;
+    const int splits = a.ragged ? (rows_of(a.kv, b).used + a.split_keys - 1) / a.split_keys : a.splits;
     const long long row = rq.first + i, at = (long long)head * a.q.rows + row, step = (long long)a.heads * a.q.rows;
     float2 ml[2] = {{-INFINITY, 0.f}, {-INFINITY, 0.f}};
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-        if (own && lane + 32 * h < a.splits) ml[h] = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (at + (lane + 32 * h) * step));
+        if (own && lane + 32 * h < splits) ml[h] = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (at + (lane + 32 * h) * step));
     float m = fmaxf(ml[0].y != 0.f ? ml[0].x : -INFINITY, ml[1].y != 0.f ? ml[1].x : -INFINITY);
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) m = fmaxf(m, __shfl_xor(m, o, 32));
@@ -209,7 +208,7 @@ template <typename T> __global__ __launch_bounds__(kJoinThreads) void k_attentio
     for (int o = 16; o > 0; o /= 2) l += __shfl_xor(l, o, 32);
     const int c = lane * 4;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < a.splits; s0 += 8) {   // eight at a time are under way
+    for (int s0 = 0; s0 < splits; s0 += 8) {   // eight at a time are under way
         f32x4 v[8];
         float g[8];
 #pragma unroll
@@ -217,7 +216,7 @@ template <typename T> __global__ __launch_bounds__(kJoinThreads) void k_attentio
             const int s = s0 + u;
             g[u] = __shfl(s < 32 ? f[0] : f[1], s & 31, 32);
             v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (own && s < a.splits && g[u] != 0.f && c < a.dim) v[u] = *reinterpret_cast<const f32x4 *>(a.part_o + (at + s * step) * a.dim + c);   // 0: its o was not written, or vanishes
+            if (own && s < splits && g[u] != 0.f && c < a.dim) v[u] = *reinterpret_cast<const f32x4 *>(a.part_o + (at + s * step) * a.dim + c);   // 0: its o was not written, or vanishes
         }
 #pragma unroll
         for (int u = 0; u < 8; ++u)
@@ -340,6 +339,7 @@ void attn_args(const dp_attention_desc &d, const dp_attention_seqs *seqs, AttnAr
     a.v_stride = d.v_stride != 0 ? d.v_stride : wk;
     a.o_stride = d.o_stride != 0 ? d.o_stride : wq;
     a.splits = 1;
+    a.ragged = seqs != nullptr && d.n <= kMostRagged && (seqs->q_starts != nullptr || seqs->kv_starts != nullptr || seqs->q_lens != nullptr || seqs->kv_lens != nullptr);
 }
 
 dp_status attn_pointers(std::initializer_list<const void *> needed, const void *lse, const void *ws)
