@@ -436,7 +436,7 @@ template <typename T> void launch(AttnArgs &a, long long groups, hipStream_t st)
 {
     for_dim(a.dim, [&](auto dc) {
         constexpr int DP = decltype(dc)::value;
-        const auto wide = [&](long long cols) { return cols > 32 && groups * ((cols + 127) / 128) >= 256; };
+        const auto wide = [&](long long cols) { return cols > 32 && groups * ((cols + 127) / 128) >= kFull; };
         const long long qc = (long long)a.q.len * a.shared, kc = a.kv.len;
         const bool wq = wide(qc), wk = wide(kc);
         a.tiles = (int)((qc + (wq ? 127 : 31)) / (wq ? 128 : 32));

@@ -65,7 +65,8 @@ template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(2
     clear(acc);
     float m = -INFINITY, mu = 0.f, l = 0.f;
     if (keys > 0) {
-        TileCopy<T, DP, KT, 256> ck, cv;
+        using Copy = TileCopy<T, DP, KT, 256>;
+        Copy ck, cv;
         ck.init(threadIdx.x, a.dim, a.k_stride);
         cv.init(threadIdx.x, a.dim, a.v_stride);
         const T *kp = reinterpret_cast<const T *>(a.kp) + (rk.first + first) * a.k_stride + (long long)hk * a.dim;
@@ -79,25 +80,40 @@ template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(2
         load_column<T, DP>(reinterpret_cast<const T *>(a.qp) + row * a.q_stride + (long long)head * a.dim, on, a.dim, half, q);
         unsigned stage = 0;
         for (int t = 0; t < keys; t += KT) {
-            wait_vmcnt<0>();
+            const bool more = t + KT < keys;
+            if (STAGES == 2) wait_vmcnt<0>();
+            else wait_vmcnt<Copy::N>();     // K alone
             __builtin_amdgcn_s_barrier();   // the tile has arrived, and the one before is done with
             const unsigned kt = base + stage + mine * L::RB, vt = kt + STAGES * BYTES;
-            const auto next = [&] {
-                if (t + KT >= keys) return;
-                if (STAGES == 2) stage ^= BYTES;
+            const auto next_k = [&] {
                 kp += KT * a.k_stride;
-                vp += KT * a.v_stride;
                 ck.issue(kp, keys - t - KT, a.dim, a.k_stride, base + stage, wave);
+            };
+            const auto next_v = [&] {
+                vp += KT * a.v_stride;
                 cv.issue(vp, keys - t - KT, a.dim, a.v_stride, base + STAGES * BYTES + stage, wave);
             };
-            if constexpr (STAGES == 2) next();
+            if (STAGES == 2 && more) {
+                stage ^= BYTES;
+                next_k();
+                next_v();
+            }
             const int w = t + mine;
-            if (w > none0 && w < none1) {
-                f32x16 s[NB];
+            const bool some = w > none0 && w < none1;
+            f32x16 s[NB];
+            if (some) {
                 clear(s);
                 First<T, DP, NB, 8> kq;
                 kq.begin(kt + tl.row, tl.x);
                 kq.run(kt + tl.row, tl.x, q, s);
+            }
+            if constexpr (STAGES == 1) {    // K's room takes the next keys, then V has to be there
+                __builtin_amdgcn_s_barrier();
+                if (more) { next_k(); wait_vmcnt<Copy::N>(); }
+                else wait_vmcnt<0>();
+                __builtin_amdgcn_s_barrier();
+            }
+            if (some) {
                 Second<T, DP, NB * 2> pv;
                 pv.begin(vt, tl);
                 if (w < all0 || w > all1) {
@@ -134,9 +150,9 @@ template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(2
                 l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                 pv.run(vt, tl, [&](auto sc) { constexpr int sl = decltype(sc)::value; return column<T>(s[sl / 2], sl % 2); }, acc);
             }
-            if constexpr (STAGES == 1) {
+            if (STAGES == 1 && more) {
                 __builtin_amdgcn_s_barrier();
-                next();
+                next_v();
             }
         }
     }
@@ -244,7 +260,7 @@ struct Form { int cw, splits, split_keys; };   // wavefronts side by side in a b
 Form form_of(const dp_attention_desc &d)
 {
     const long long cols = (long long)d.q_len * (d.heads / d.kv_heads), groups = (long long)d.n * d.kv_heads;
-    if (cols > 32 && groups * ((cols + 127) / 128) >= 256) return {4, 1, 0};
+    if (cols > 32 && groups * ((cols + 127) / 128) >= kFull) return {4, 1, 0};
     const long long blocks = std::max<long long>(1, groups * ((cols + 31) / 32));
     constexpr int kt = 128;
     long long span = d.kv_len;   // keys that a block looks at
