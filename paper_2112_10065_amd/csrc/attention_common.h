@@ -141,17 +141,19 @@ DEVFN float other_half(float v)
     return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
 }
 
-// A tile in LDS: rows of RB bytes (a power of two, channels behind the head's own are zero) in chunks of 16 bytes, chunk c of row r at c ^ swizzle(r), so
-// that reads of one chunk of 16 rows and transposed reads of four rows both touch every bank once.
+// A tile in LDS: rows of RB bytes (whole blocks of 32 channels; those behind the head's own are zero) in chunks of 16 bytes, chunk c of row r at c ^ swizzle(r).  The 64 banks
+// hold sixteen chunks, so chunk c' of row r lies in banks (CR r + c') % 16: the swizzle makes reads of one chunk of 16 rows, and transposed reads of four chunks
+// of four rows, touch every bank once.  Where CR is an odd multiple of four, four rows lie apart by themselves and the swizzle stays within four chunks (FLAT).
 template <typename T, int DP> struct Tile {
     static constexpr int E = 16 / sizeof(T);                              // elements of a chunk
-    static constexpr int RB = (int)sizeof(T) * (sizeof(T) == 2 ? (DP <= 64 ? 64 : 128) : DP <= 32 ? 32 : DP <= 64 ? 64 : 128);
-    static constexpr int CR = RB / 16;                                    // chunks of a row
     static constexpr int SLICES = DP / (2 * E);                           // of the first kind of product
     static constexpr int DB = (DP + 31) / 32;                             // blocks of 32 channels of the second
+    static constexpr int RB = DB * 32 * (int)sizeof(T), CR = RB / 16;     // CR: chunks of a row
+    static constexpr bool FLAT = CR % 8 == 4;
     static DEVFN int swizzle(int r)
     {
-        if constexpr (CR == 8) return ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
+        if constexpr (FLAT) return (r >> 2) & 3;
+        else if constexpr (CR % 16 == 8) return ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
         else if constexpr (CR == 16) return (r & 3) << 2 | ((r >> 2) & 3);
         else return r & 15;
     }
@@ -214,7 +216,8 @@ template <typename T, int DP, int NB, int DEPTH> struct First {
     template <int I> DEVFN void read(unsigned base, unsigned x)   // base: the lane's row in block 0; x: its swizzled chunk of slice 0, in bytes
     {
         constexpr int block = I % NB, s = I / NB;   // neighbours in time add to different sums
-        buf[I % D] = lds_read16<block * 32 * L::RB>(base + (x ^ (unsigned)(s * 32)));
+        if constexpr (L::FLAT) buf[I % D] = lds_read16<block * 32 * L::RB + s / 2 * 64>(base + (x ^ (unsigned)(s % 2 * 32)));
+        else buf[I % D] = lds_read16<block * 32 * L::RB>(base + (x ^ (unsigned)(s * 32)));
     }
     DEVFN void begin(unsigned base, unsigned x) { for_constant<D>([&](auto i) { read<decltype(i)::value>(base, x); }); }
     DEVFN void run(unsigned base, unsigned x, const u32x4 (&cols)[L::SLICES], f32x16 (&acc)[NB])
@@ -234,7 +237,12 @@ template <typename T, int DP, int DEPTH> struct TwoFirst {
     using L = Tile<T, DP>;
     static constexpr int N = 2 * L::SLICES, D = DEPTH < N ? DEPTH : N;
     u32x4 buf[D];
-    template <int I> DEVFN void read(unsigned a, unsigned b, unsigned x) { buf[I % D] = lds_read16<0>((I % 2 == 0 ? a : b) + (x ^ (unsigned)(I / 2 * 32))); }
+    template <int I> DEVFN void read(unsigned a, unsigned b, unsigned x)
+    {
+        constexpr int s = I / 2;
+        if constexpr (L::FLAT) buf[I % D] = lds_read16<s / 2 * 64>((I % 2 == 0 ? a : b) + (x ^ (unsigned)(s % 2 * 32)));
+        else buf[I % D] = lds_read16<0>((I % 2 == 0 ? a : b) + (x ^ (unsigned)(s * 32)));
+    }
     DEVFN void begin(unsigned a, unsigned b, unsigned x) { for_constant<D>([&](auto i) { read<decltype(i)::value>(a, b, x); }); }
     DEVFN void run(unsigned a, unsigned b, unsigned x, const u32x4 (&ca)[L::SLICES], const u32x4 (&cb)[L::SLICES], f32x16 &sa, f32x16 &sb)
     {
@@ -280,8 +288,13 @@ template <int DP, int NS> struct Second<bf16_t, DP, NS> {
     template <int I> DEVFN void read(unsigned tile, const TileLane<bf16_t, DP> &l)
     {
         constexpr int s = I / DB, db = I % DB;
-        lo[I % D] = lds_read_tr<s * 16 * L::RB>(tile + (l.lo ^ (unsigned)(db * 64)));
-        hi[I % D] = lds_read_tr<(s * 16 + 8) * L::RB>(tile + (l.hi ^ (unsigned)(db * 64)));
+        if constexpr (L::FLAT) {
+            lo[I % D] = lds_read_tr<s * 16 * L::RB + db * 64>(tile + l.lo);
+            hi[I % D] = lds_read_tr<(s * 16 + 8) * L::RB + db * 64>(tile + l.hi);
+        } else {
+            lo[I % D] = lds_read_tr<s * 16 * L::RB>(tile + (l.lo ^ (unsigned)(db * 64)));
+            hi[I % D] = lds_read_tr<(s * 16 + 8) * L::RB>(tile + (l.hi ^ (unsigned)(db * 64)));
+        }
     }
     DEVFN void begin(unsigned tile, const TileLane<bf16_t, DP> &l) { for_constant<D>([&](auto i) { read<decltype(i)::value>(tile, l); }); }
     template <int I, typename F> DEVFN void item(unsigned tile, const TileLane<bf16_t, DP> &l, F &&cols, f32x16 (&acc)[DB])

@@ -19,7 +19,7 @@ template <typename T, int DP, int CW, bool SPLIT> struct Shape {
     static constexpr int STAGES = 4 * BYTES <= (SPLIT ? 65536 : 131072) ? 2 : 1;
 };
 
-template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(256, (CW == 4 || SPLIT) && (sizeof(T) == 2 || DP <= 64) ? 2 : 1) void k_attention(AttnArgs a)
+template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(256, CW == 4 && sizeof(T) == 2 && DP <= 96 ? 3 : (CW == 4 || SPLIT) && (sizeof(T) == 2 || DP <= 64) ? 2 : 1) void k_attention(AttnArgs a)
 {
     using L = Tile<T, DP>;
     using S = Shape<T, DP, CW, SPLIT>;
