@@ -377,22 +377,24 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
                 const unsigned qt = base + slot * BYTES + in * L::RB, gt = qt + STAGES * BYTES, st = stats + (slot * 2 * SIDE + in) * 4 + half * 16;
                 f32x16 s[1], dp[1];
                 clear(s);
-                clear(dp);
                 u32x4 l2[4], de[4];   // of rows 8 g + 4 half ...
-                l2[0] = lds_read16<0>(st); l2[1] = lds_read16<32>(st); l2[2] = lds_read16<64>(st); l2[3] = lds_read16<96>(st);
                 de[0] = lds_read16<SIDE * 4>(st); de[1] = lds_read16<SIDE * 4 + 32>(st); de[2] = lds_read16<SIDE * 4 + 64>(st); de[3] = lds_read16<SIDE * 4 + 96>(st);
+                l2[0] = lds_read16<0>(st); l2[1] = lds_read16<32>(st); l2[2] = lds_read16<64>(st); l2[3] = lds_read16<96>(st);
                 TwoFirst<T, DP, 6> ab;
                 ab.begin(qt + tl.row, gt + tl.row, tl.x);
-                ab.run(qt + tl.row, gt + tl.row, tl.x, kc, vc, s[0], dp[0]);
+                wait_reads<1, decltype(ab)::D>();
 #pragma unroll
-                for (int e = 0; e < 4; ++e) { tie(l2[e]); tie(de[e]); }   // older than the reads that were waited for
+                for (int e = 0; e < 4; ++e) { tie(l2[e]); tie(de[e]); }
+#pragma unroll
+                for (int v = 0; v < 16; ++v) dp[0][v] = __uint_as_float(de[v >> 2][v & 3]);   // dp - delta: the sum begins at -delta
+                ab.run(qt + tl.row, gt + tl.row, tl.x, kc, vc, s[0], dp[0]);
                 Second<T, DP, 2> gp, qs;
                 gp.begin(gt, tl);
                 hide(s[0], w, at, half);
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     s[0][v] = __builtin_amdgcn_exp2f(fmaf(s[0][v], a.scale2, -__uint_as_float(l2[v >> 2][v & 3])));
-                    dp[0][v] = s[0][v] * (dp[0][v] + __uint_as_float(de[v >> 2][v & 3]));
+                    dp[0][v] *= s[0][v];
                 }
                 gp.run(gt, tl, [&](auto sc) { return column<T>(s[0], decltype(sc)::value); }, dv);
                 qs.begin(qt, tl);
@@ -443,7 +445,7 @@ template <typename T> void launch(AttnArgs &a, long long groups, hipStream_t st)
         if (a.tiles > 0 && a.q.rows > 0) hipLaunchKernelGGL((wq ? k_attention_dq<T, DP, 4> : k_attention_dq<T, DP, 1>), dim3((unsigned)(groups * a.tiles)), dim3(256), 0, st, a);
         a.tiles = (int)((kc + (wk ? 127 : 31)) / (wk ? 128 : 32));
         if (a.tiles > 0 && a.kv.rows > 0) {
-            constexpr bool whole = sizeof(T) == 4 || DP <= 64;
+            constexpr bool whole = sizeof(T) == 4 || DP <= 96;
             auto *kernel = !wk ? k_attention_dkv_whole<T, DP, 1> : wide_kernel<T, DP, whole>();
             hipLaunchKernelGGL(kernel, dim3((unsigned)(groups * a.tiles)), dim3(wk && !whole ? 512 : 256), 0, st, a);
         }

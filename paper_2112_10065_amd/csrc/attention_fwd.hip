@@ -103,7 +103,7 @@ template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(2
             f32x16 s[NB];
             if (some) {
                 clear(s);
-                First<T, DP, NB, 8> kq;
+                First<T, DP, NB, DP <= 96 ? 6 : 8> kq;
                 kq.begin(kt + tl.row, tl.x);
                 kq.run(kt + tl.row, tl.x, q, s);
             }
