@@ -367,6 +367,25 @@ def dp_logprobs_bwd(desc, z, ids, lse, entropy, dlogp, dentropy, dz, stream=None
     _check(lib.dp_logprobs_bwd(C.byref(desc), _ptr(z), _ptr(ids), _ptr(lse), _ptr(entropy), _ptr(dlogp), _ptr(dentropy), _ptr(dz), _stream(stream)))
 
 
+def _ptrs(*tensors):
+    """Addresses of tensors that a kernel reads or writes: a kernel of the current device would fault on memory of the host or of another one."""
+    out, device = [], None
+    for t in tensors:
+        if t is None or isinstance(t, int):
+            out.append(t)
+            continue
+        if device is None:
+            device = torch.cuda.current_device() if torch.cuda.is_available() else -2
+        if t.get_device() != device:
+            raise ValueError(f"a tensor is on {t.device}, not on the current GPU")
+        out.append(t.data_ptr())
+    return out
+
+
+def _ws_on(ws):
+    return (None, 0) if ws is None else (_ptrs(ws)[0], ws.numel() * ws.element_size())
+
+
 def qk_rotary_desc(rows, heads, kv_heads, dim, pairs, io_dtype=DP_BF16, flags=0, eps=1e-6, q_stride=0, k_stride=0, q_out_stride=0, k_out_stride=0,
                    dq_stride=0, dk_stride=0):
     """pairs: how many pairs of channels each axis turns, one to three numbers."""
@@ -381,14 +400,11 @@ def dp_qk_rotary_workspace_bytes(desc, pass_):
 
 def dp_qk_rotary_fwd(desc, q, k, gamma_q, gamma_k, pos, freq, q_out, k_out, stream=None):
     """pos: fp32 [rows, axes]; freq: float64 [sum of pairs]."""
-    _check(lib.dp_qk_rotary_fwd(C.byref(desc), _ptr(q), _ptr(k), _ptr(gamma_q), _ptr(gamma_k), _ptr(pos), _ptr(freq), _ptr(q_out), _ptr(k_out),
-                                _stream(stream)))
+    _check(lib.dp_qk_rotary_fwd(C.byref(desc), *_ptrs(q, k, gamma_q, gamma_k, pos, freq, q_out, k_out), _stream(stream)))
 
 
 def dp_qk_rotary_bwd(desc, q, k, gamma_q, gamma_k, pos, freq, dq_out, dk_out, dq, dk, dgamma_q=None, dgamma_k=None, ws=None, stream=None):
-    p, b = _ws(ws)
-    _check(lib.dp_qk_rotary_bwd(C.byref(desc), _ptr(q), _ptr(k), _ptr(gamma_q), _ptr(gamma_k), _ptr(pos), _ptr(freq), _ptr(dq_out), _ptr(dk_out), _ptr(dq),
-                                _ptr(dk), _ptr(dgamma_q), _ptr(dgamma_k), p, b, _stream(stream)))
+    _check(lib.dp_qk_rotary_bwd(C.byref(desc), *_ptrs(q, k, gamma_q, gamma_k, pos, freq, dq_out, dk_out, dq, dk, dgamma_q, dgamma_k), *_ws_on(ws), _stream(stream)))
 
 
 def attention_desc(n, q_len, kv_len, heads, kv_heads, dim, io_dtype=DP_BF16, left=-1, right=-1, scale=0.0, q_rows=0, kv_rows=0, q_stride=0, k_stride=0,
@@ -401,7 +417,7 @@ def attention_seqs(q_starts=None, kv_starts=None, q_lens=None, kv_lens=None):
     for name, t in (("q_starts", q_starts), ("kv_starts", kv_starts), ("q_lens", q_lens), ("kv_lens", kv_lens)):
         if isinstance(t, torch.Tensor) and (t.dtype != torch.int32 or not t.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous int32 tensor")
-    seqs = dp_attention_seqs(_ptr(q_starts), _ptr(kv_starts), _ptr(q_lens), _ptr(kv_lens))
+    seqs = dp_attention_seqs(*_ptrs(q_starts, kv_starts, q_lens, kv_lens))
     seqs.tensors = (q_starts, kv_starts, q_lens, kv_lens)
     return seqs
 
@@ -411,15 +427,12 @@ def dp_attention_workspace_bytes(desc, pass_):
 
 
 def dp_attention_fwd(desc, q, k, v, o, lse=None, seqs=None, ws=None, stream=None):
-    p, b = _ws(ws)
-    _check(lib.dp_attention_fwd(C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), C.byref(seqs) if seqs is not None else None, p, b,
-                                _stream(stream)))
+    _check(lib.dp_attention_fwd(C.byref(desc), *_ptrs(q, k, v, o, lse), C.byref(seqs) if seqs is not None else None, *_ws_on(ws), _stream(stream)))
 
 
 def dp_attention_bwd(desc, q, k, v, o, dout, lse, dq, dk, dv, seqs=None, ws=None, stream=None):
-    p, b = _ws(ws)
-    _check(lib.dp_attention_bwd(C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(dout), _ptr(lse), _ptr(dq), _ptr(dk), _ptr(dv),
-                                C.byref(seqs) if seqs is not None else None, p, b, _stream(stream)))
+    _check(lib.dp_attention_bwd(C.byref(desc), *_ptrs(q, k, v, o, dout, lse, dq, dk, dv), C.byref(seqs) if seqs is not None else None, *_ws_on(ws),
+                                _stream(stream)))
 
 
 def _doubles(rows, n):

@@ -434,20 +434,20 @@ template <typename T, int DP, bool WHOLE> auto wide_kernel()
 }
 
 // Blocks of 128 columns where they fill the card; else of 32, whose wavefronts share the rows of the other side.
-template <typename T> void launch(AttnArgs &a, long long groups, hipStream_t st)
+template <typename T> void launch(AttnArgs &a, hipStream_t st)
 {
     for_dim(a.dim, [&](auto dc) {
         constexpr int DP = decltype(dc)::value;
-        const auto wide = [&](long long cols) { return cols > 32 && groups * ((cols + 127) / 128) >= kFull; };
+        const auto wide = [&](const AttnSide &s, long long mult) { return s.len * mult > 32 && a.kv_heads * attn_tiles(a.n, s.len, s.rows, mult, 128) >= kFull; };
         const long long qc = (long long)a.q.len * a.shared, kc = a.kv.len;
-        const bool wq = wide(qc), wk = wide(kc);
+        const bool wq = wide(a.q, a.shared), wk = wide(a.kv, 1);
         a.tiles = (int)((qc + (wq ? 127 : 31)) / (wq ? 128 : 32));
-        if (a.tiles > 0 && a.q.rows > 0) hipLaunchKernelGGL((wq ? k_attention_dq<T, DP, 4> : k_attention_dq<T, DP, 1>), dim3((unsigned)(groups * a.tiles)), dim3(256), 0, st, a);
+        if (a.tiles > 0 && a.q.rows > 0) hipLaunchKernelGGL((wq ? k_attention_dq<T, DP, 4> : k_attention_dq<T, DP, 1>), dim3(attn_blocks(a, a.q, a.shared, wq ? 128 : 32)), dim3(256), 0, st, a);
         a.tiles = (int)((kc + (wk ? 127 : 31)) / (wk ? 128 : 32));
         if (a.tiles > 0 && a.kv.rows > 0) {
             constexpr bool whole = sizeof(T) == 4 || DP <= 96;
             auto *kernel = !wk ? k_attention_dkv_whole<T, DP, 1> : wide_kernel<T, DP, whole>();
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(groups * a.tiles)), dim3(wk && !whole ? 512 : 256), 0, st, a);
+            hipLaunchKernelGGL(kernel, dim3(attn_blocks(a, a.kv, 1, wk ? 128 : 32)), dim3(wk && !whole ? 512 : 256), 0, st, a);
         }
     });
 }
@@ -479,8 +479,7 @@ extern "C" dp_status dp_attention_bwd(const dp_attention_desc *desc, const void 
     a.dq = dq; a.dk = dk; a.dv = dv;
     a.lse2 = (float *)ws;
     a.delta = (float *)((char *)ws + stat_bytes(d));
-    const long long groups = (long long)d.n * d.kv_heads;
-    if (d.io_dtype == DP_BF16) launch<bf16_t>(a, groups, (hipStream_t)hip_stream);
-    else launch<float>(a, groups, (hipStream_t)hip_stream);
+    if (d.io_dtype == DP_BF16) launch<bf16_t>(a, (hipStream_t)hip_stream);
+    else launch<float>(a, (hipStream_t)hip_stream);
     return attn_launched("attention's gradient");
 }

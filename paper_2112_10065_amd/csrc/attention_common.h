@@ -449,4 +449,16 @@ void attn_args(const dp_attention_desc &d, const dp_attention_seqs *seqs, AttnAr
 dp_status attn_pointers(std::initializer_list<const void *> needed, const void *lse, const void *ws);
 dp_status attn_workspace(size_t need, const void *ws, size_t ws_bytes);
 dp_status attn_launched(const char *what);
+// tiles of `columns` that n sequences of up to `len` rows can have, `mult` columns to a row; packed ones have no more rows than there are in memory
+inline long long attn_tiles(long long n, long long len, long long rows, long long mult, int columns)
+{
+    const long long all = n * ((len * mult + columns - 1) / columns), packed = rows * mult / columns + n;
+    return rows < n * len && packed < all ? packed : all;
+}
+// blocks of a call: where they are numbered by what there is, no more than that can be
+inline unsigned attn_blocks(const AttnArgs &a, const AttnSide &side, long long mult, int columns)
+{
+    const long long tiles = a.ragged && side.starts != nullptr ? attn_tiles(a.n, side.len, side.rows, mult, columns) : (long long)a.n * a.tiles;
+    return (unsigned)(tiles * a.kv_heads * a.splits);
+}
 size_t attn_bwd_bytes(const dp_attention_desc &d);   // attention_bwd.hip

@@ -103,7 +103,7 @@ template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(2
             f32x16 s[NB];
             if (some) {
                 clear(s);
-                First<T, DP, NB, DP <= 96 ? 6 : 8> kq;
+                First<T, DP, NB, DP == 96 ? 6 : 8> kq;
                 kq.begin(kt + tl.row, tl.x);
                 kq.run(kt + tl.row, tl.x, q, s);
             }
@@ -257,11 +257,13 @@ struct Form { int cw, splits, split_keys; };   // wavefronts side by side in a b
 
 // Four wavefronts side by side share the copies of a tile of keys; where such blocks would not fill the card, or a block's columns would not be there, the four of them take
 // the same 32 columns and share the keys, and if that leaves compute units without work too, blocks share them.
+long long rows_or(long long rows, long long dense) { return rows != 0 ? rows : dense; }
+
 Form form_of(const dp_attention_desc &d)
 {
-    const long long cols = (long long)d.q_len * (d.heads / d.kv_heads), groups = (long long)d.n * d.kv_heads;
-    if (cols > 32 && groups * ((cols + 127) / 128) >= kFull) return {4, 1, 0};
-    const long long blocks = std::max<long long>(1, groups * ((cols + 31) / 32));
+    const long long shared = d.heads / d.kv_heads, cols = d.q_len * shared, rows = rows_or(d.q_rows, (long long)d.n * d.q_len);
+    if (cols > 32 && d.kv_heads * attn_tiles(d.n, d.q_len, rows, shared, 128) >= kFull) return {4, 1, 0};
+    const long long blocks = std::max<long long>(1, d.kv_heads * attn_tiles(d.n, d.q_len, rows, shared, 32));
     constexpr int kt = 128;
     long long span = d.kv_len;   // keys that a block looks at
     if (d.left >= 0 && d.right >= 0) span = std::min<long long>(span, (long long)d.left + d.right + 32);
@@ -272,8 +274,6 @@ Form form_of(const dp_attention_desc &d)
     const long long per = ((d.kv_len + want - 1) / want + kt - 1) / kt * kt;
     return {1, (int)((d.kv_len + per - 1) / per), (int)per};
 }
-
-long long rows_or(long long rows, long long dense) { return rows != 0 ? rows : dense; }
 
 size_t split_bytes(const dp_attention_desc &d, const Form &f)
 {
@@ -414,7 +414,7 @@ extern "C" dp_status dp_attention_fwd(const dp_attention_desc *desc, const void 
     a.tiles = (int)((cols + 32 * f.cw - 1) / (32 * f.cw));
     hipStream_t st = (hipStream_t)hip_stream;
     const bool bf = d.io_dtype == DP_BF16;
-    const unsigned blocks = (unsigned)(groups * a.tiles * f.splits);
+    const unsigned blocks = attn_blocks(a, a.q, a.shared, 32 * f.cw);
     if (bf) launch<bf16_t>(a, f, blocks, st);
     else launch<float>(a, f, blocks, st);
     if (f.splits > 1) {

@@ -122,6 +122,22 @@ def test_attention_refusals(dp):
     import torch
     with pytest.raises(ValueError, match="int32"):
         seqs(q_lens=torch.zeros(2, dtype=torch.int64))
+    with pytest.raises(ValueError, match="not on the current GPU"):
+        seqs(kv_lens=torch.zeros(2, dtype=torch.int32))
+
+
+def test_tensors_of_the_host_are_refused(dp):
+    """A kernel would fault on them."""
+    import torch
+    t = torch.zeros(4096)
+    with pytest.raises(ValueError, match="not on the current GPU"):
+        dp.dp_attention_fwd(att(dp), A, A, t, A)
+    with pytest.raises(ValueError, match="not on the current GPU"):
+        dp.dp_attention_bwd(att(dp), A, A, A, A, A, A, A, A, A, ws=t)
+    with pytest.raises(ValueError, match="not on the current GPU"):
+        dp.dp_qk_rotary_fwd(rot(dp), A, A, None, None, t, A, A, A)
+    with pytest.raises(ValueError, match="not on the current GPU"):
+        dp.dp_qk_rotary_bwd(rot(dp), A, A, None, None, A, A, A, A, A, A, dgamma_q=t)
 
 
 def test_attention_valid_calls(dp):

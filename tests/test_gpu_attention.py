@@ -294,3 +294,83 @@ def test_without_lse(env):
     a, _ = c.forward()
     b, _ = c.forward(lse=False)
     assert torch.equal(a, b)
+
+
+def test_rows_far_apart(env):
+    """Offsets beyond 2^31 elements: the second sequence's cache begins 2.3e9 elements behind the first one's."""
+    dp, O = env
+    kv_len, hk, dim, lens = 2_250_000, 8, 128, (5, 300)
+    k, v = (torch.empty((2 * kv_len, hk * dim), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    g = torch.Generator(device="cuda").manual_seed(1)
+    used = torch.cat([torch.arange(lens[0]), kv_len + torch.arange(lens[1])]).cuda()
+    for t in (k, v):
+        t[used] = torch.randn((len(used), hk * dim), generator=g, device="cuda").bfloat16()
+    q = torch.randn((2, 2 * hk * dim), generator=g, device="cuda").bfloat16()
+    d = dp.attention_desc(2, 1, kv_len, 2 * hk, hk, dim, right=0)
+    o, lse = torch.empty_like(q), torch.empty((2 * hk, 2), device="cuda")
+    seqs = dp.attention_seqs(kv_lens=torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    ws = torch.empty(dp.dp_attention_workspace_bytes(d, dp.DP_PASS_FWD) + 16, dtype=torch.uint8, device="cuda")
+    dp.dp_attention_fwd(d, q, k, v, o, lse, seqs, ws)
+    want, want_lse, size = O.attention(q.double().cpu().numpy().reshape(2, -1, dim), *(t[used].double().cpu().numpy().reshape(-1, hk, dim) for t in (k, v)), [(0, 1, 0, 5), (1, 1, 5, 300)],
+                                       dim ** -0.5, -1, 0)
+    # bf16: p and o are rounded by at most 2^-8, the rest is far below
+    assert np.all(np.abs(o.double().cpu().numpy().reshape(want.shape) - want) <= 2.0 ** -8 * (np.abs(want) + size) * 1.02)
+    assert np.allclose(lse.cpu().numpy(), want_lse, rtol=0, atol=1e-4)
+
+
+@pytest.mark.parametrize("n", [65, 200, 300])
+def test_many_short_sequences(env, n):
+    """More sequences than a wavefront has lanes, and than blocks count; packed in less memory than n of the longest would need."""
+    r = np.random.default_rng(n)
+    lq, lk = r.integers(0, 90, n).tolist(), r.integers(0, 140, n).tolist()
+    Case(env, n, 90, 140, 2, 1, 64, -1, 0, q_side=("packed", lq, 1, 2), kv_side=("packed", lk, 0, 3)).check(True, True)
+    Case(env, n, 1, 3000, 2, 1, 64, -1, 0, kv_side=r.integers(0, 3001, n).tolist()).check()
+
+
+def test_tokens_one_by_one_give_the_whole(env):
+    """A sequence taken token by token over its growing cache: the causal result's rows, whatever lies behind the cache's end."""
+    dp, _ = env
+    n, total, h, hk, dim = 3, 150, 8, 2, 64
+    c = Case(env, n, total, total, h, hk, dim, -1, 0)
+    whole, lse = c.forward()
+    k, v = (torch.full((n, total, hk * dim), float("nan"), device="cuda").bfloat16() for _ in range(2))
+    q, ks, vs = (t.reshape(n, total, -1) for t in (c.q, c.k, c.v))
+    d = dp.attention_desc(n, 1, total, h, hk, dim, right=0)
+    ws = torch.empty(dp.dp_attention_workspace_bytes(d, dp.DP_PASS_FWD) + 16, dtype=torch.uint8, device="cuda")
+    lens = torch.zeros(n, dtype=torch.int32, device="cuda")
+    seqs = dp.attention_seqs(kv_lens=lens)
+    for t in range(total):
+        k[:, t], v[:, t] = ks[:, t], vs[:, t]
+        lens.fill_(t + 1)
+        o, l1 = torch.empty((n, h * dim), device="cuda").bfloat16(), torch.empty((h, n), device="cuda")
+        dp.dp_attention_fwd(d, q[:, t].contiguous(), k, v, o, l1, seqs, ws)
+        want = whole.reshape(n, total, -1)[:, t].float()
+        # p and o are each rounded twice on both sides, and p at most 2^-8 of a value whose weighted mean is at most the largest |v| seen
+        tol = 2.0 ** -8 * 2 * (want.abs() + vs[:, :t + 1].float().abs().amax(dim=(1, 2))[:, None])
+        assert torch.all((o.float() - want).abs() <= tol)
+        assert torch.all((l1 - lse.reshape(h, n, total)[:, :, t]).abs() <= 1e-4)
+
+
+def test_gradient_against_differences(env):
+    """(f(x + h d) - f(x - h d)) / 2h of f = sum(o dout) in fp32, summed in 64 bits; how far it may be off: what the results' own tolerance gives, and the step of 2h beside that of h."""
+    for left, right in ((-1, -1), (-1, 0), (9, 2)):
+        c = Case(env, 2, 37, 50, 4, 2, 40, left, right, bf16=False, gap=8)
+        o, lse = c.forward()
+        grads = c.backward(o, lse)
+        rel, terms = c.sizes()
+        base = [c.q.clone(), c.k.clone(), c.v.clone()]
+        noise = float(((rel + terms) * c.O.attention(c.host(c.q), c.host(c.k), c.host(c.v), c.seqs_list, c.scale, left, right)[2] * np.abs(c.host(c.dout))).sum())
+        for i, g in enumerate(grads):
+            gen = torch.Generator(device="cuda").manual_seed(i)
+            d = torch.randn(base[i].shape, generator=gen, device="cuda")
+            w = c.widths[min(i, 1)]
+
+            def f(step):
+                for t, b in zip((c.q, c.k, c.v), base):
+                    t.copy_(b)
+                (c.q, c.k, c.v)[i].add_(d * step)
+                return float((c.forward()[0].double() * c.dout.reshape(c.q_rows, -1).double()).sum())
+            slope = {h: (f(h) - f(-h)) / (2 * h) for h in (0.01, 0.02)}
+            f(0.0)
+            want = float((g[:, :w].double() * d.reshape(-1, w).double()).sum())
+            assert abs(want - slope[0.01]) <= 2 * noise / 0.01 + abs(slope[0.02] - slope[0.01]), (i, want, slope, noise)
