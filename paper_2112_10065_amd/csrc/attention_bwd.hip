@@ -22,7 +22,7 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
     constexpr int ROOM = 2 * STAGES * BYTES > (RW > 1 ? 4 * DB * 4096 : 0) ? 2 * STAGES * BYTES : 4 * DB * 4096;
     __shared__ alignas(1024) char s_tiles[ROOM];   // K and V of each stage
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, wc = wave % CW, wr = wave / CW;
-    const Item item = item_of<COLS, false, true>(a, a.q, a.shared);
+    const Item item = item_of<COLS, false, true>(a, a.q, a.shared, blockIdx.x, gridDim.x);
     if (!item.any) return;
     const int b = item.b, hk = item.hk, col0 = item.tile * COLS;
     const Rows rq = rows_of(a.q, b), rk = rows_of(a.kv, b);
@@ -190,7 +190,7 @@ template <int DP> __global__ __launch_bounds__(512, 2) void k_attention_dkv(Attn
     __shared__ alignas(16) float s_stats[STAGES][2][QT];         // lse2 and -delta
     __shared__ alignas(16) u32x4 s_packs[2][8][2][64];           // [tile][wavefront][slice][lane]: the first's p, the second's ds
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, pair = wave & 3, second = wave >> 2;
-    const Item item = item_of<COLS, false, false>(a, a.kv, 1);
+    const Item item = item_of<COLS, false, false>(a, a.kv, 1, blockIdx.x, gridDim.x);
     if (!item.any) return;
     const int b = item.b, hk = item.hk, col0 = item.tile * COLS;
     const Rows rq = rows_of(a.q, b), rk = rows_of(a.kv, b);
@@ -314,7 +314,7 @@ template <int DP> __global__ __launch_bounds__(512, 2) void k_attention_dkv(Attn
 
 // dk and dv with both sums in one wavefront: for 32 keys, where there are few (four wavefronts share each tile of queries), and for 128 of narrow heads, whose sums leave room, or
 // in fp32, where the matrix products take sixteen times as long as with bf16 and hide the rest.
-template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 && sizeof(T) == 2 ? 2 : 1) void k_attention_dkv_whole(AttnArgs a)
+template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(256, CW == 4 && sizeof(T) == 2 ? 2 : 1) void k_attention_dkv_whole(AttnArgs a)
 {
     using L = Tile<T, DP>;
     using S = Shape<T, DP, CW>;
@@ -323,7 +323,8 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
     __shared__ alignas(1024) char s_tiles[ROOM];              // q and dout of each stage
     __shared__ alignas(16) float s_stats[STAGES][2][SIDE];    // lse2 and delta
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const Item item = item_of<COLS, false, false>(a, a.kv, 1);
+    const int part = SPLIT ? blockIdx.x % a.kv_parts : 0;
+    const Item item = SPLIT ? item_of<COLS, false, false>(a, a.kv, 1, blockIdx.x / a.kv_parts, gridDim.x / a.kv_parts) : item_of<COLS, false, false>(a, a.kv, 1, blockIdx.x, gridDim.x);
     if (!item.any) return;
     const int b = item.b, hk = item.hk, col0 = item.tile * COLS, wcol = col0 + wave % CW * 32, wr = wave / CW;
     const Rows rq = rows_of(a.q, b), rk = rows_of(a.kv, b);
@@ -344,8 +345,10 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
         const unsigned base = lds_offset(s_tiles), stats = lds_offset(s_stats);
         TileLane<T, DP> tl;
         tl.init(lane);
-        const int tiles = (w.count + QT - 1) / QT, all = tiles * a.shared;
-        int ih = hk * a.shared, it = 0, slot_in = 0;
+        const int tiles = (w.count + QT - 1) / QT, total = tiles * a.shared;
+        // with SPLIT a part of the tiles, all heads' one behind the other
+        const int from = SPLIT ? (int)((long long)total * part / a.kv_parts) : 0, all = SPLIT ? (int)((long long)total * (part + 1) / a.kv_parts) - from : total;
+        int ih = hk * a.shared + from / tiles, it = from % tiles * QT, slot_in = 0;
         auto issue = [&] {
             const long long at = rq.first + w.first + it;
             const int rows = w.count - it;
@@ -361,11 +364,11 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
             if (it >= w.count) { it = 0; ++ih; }
         };
         static_assert(QT <= 128, "two wavefronts copy a statistic");
-        issue();
+        if (!SPLIT || all > 0) issue();
         u32x4 kc[L::SLICES], vc[L::SLICES];
         load_column<T, DP>(reinterpret_cast<const T *>(a.kp) + row * a.k_stride + (long long)hk * a.dim, on, a.dim, half, kc);
         load_column<T, DP>(reinterpret_cast<const T *>(a.vp) + row * a.v_stride + (long long)hk * a.dim, on, a.dim, half, vc);
-        int slot = 0, t = 0;
+        int slot = 0, t = from % tiles * QT;
         for (int n = 0; n < all; ++n) {
             wait_vmcnt<0>();
             __builtin_amdgcn_s_barrier();   // the tile has arrived, and the one before is done with
@@ -422,33 +425,85 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
 #pragma unroll
             for (int v = 0; v < 16; ++v) dk[db][v] = dv[db][v] = 0.f;
         }
-        store_block<T>(dk[db], a.scale, reinterpret_cast<T *>(a.dk) + row * a.k_stride + (long long)hk * a.dim, db * 32, a.dim, half);
-        store_block<T>(dv[db], 1.f, reinterpret_cast<T *>(a.dv) + row * a.v_stride + (long long)hk * a.dim, db * 32, a.dim, half);
+        if constexpr (SPLIT) {
+            const long long at = ((part * a.kv.rows + row) * a.kv_heads + hk) * a.dim;
+            store_block<float>(dk[db], a.scale, a.part_dk + at, db * 32, a.dim, half);
+            store_block<float>(dv[db], 1.f, a.part_dv + at, db * 32, a.dim, half);
+        } else {
+            store_block<T>(dk[db], a.scale, reinterpret_cast<T *>(a.dk) + row * a.k_stride + (long long)hk * a.dim, db * 32, a.dim, half);
+            store_block<T>(dv[db], 1.f, reinterpret_cast<T *>(a.dv) + row * a.v_stride + (long long)hk * a.dim, db * 32, a.dim, half);
+        }
     }
 }
 
-template <typename T, int DP, bool WHOLE> auto wide_kernel()
+// The parts' sums added up, in their order: 32 lanes to a row of one head, four channels each.
+constexpr int kSumThreads = 256;
+template <typename T> __global__ __launch_bounds__(kSumThreads) void k_attention_dkv_sum(AttnArgs a)
 {
-    if constexpr (WHOLE) return k_attention_dkv_whole<T, DP, 4>;
-    else return k_attention_dkv<DP>;
+    const int b = blockIdx.x / a.tiles, col = (blockIdx.x % a.tiles) * (kSumThreads / 32) + (threadIdx.x >> 5), j = col / a.kv_heads, hk = col % a.kv_heads, c = (threadIdx.x & 31) * 4;
+    const Rows rk = rows_of(a.kv, b);
+    if (j >= rk.own || c >= a.dim) return;
+    const long long row = rk.first + j, step = a.kv.rows * a.kv_heads * a.dim, at = (row * a.kv_heads + hk) * a.dim + c;
+    f32x4 dk = {0.f, 0.f, 0.f, 0.f}, dv = dk;
+#pragma unroll 4
+    for (int p = 0; p < a.kv_parts; ++p) {
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(a.part_dk + at + p * step), y = *reinterpret_cast<const f32x4 *>(a.part_dv + at + p * step);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { dk[e] += x[e]; dv[e] += y[e]; }
+    }
+    T *to_k = reinterpret_cast<T *>(a.dk) + row * a.k_stride + (long long)hk * a.dim + c, *to_v = reinterpret_cast<T *>(a.dv) + row * a.v_stride + (long long)hk * a.dim + c;
+    if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<u32x2 *>(to_k) = u32x2{pack_bf16(dk[0], dk[1]), pack_bf16(dk[2], dk[3])};
+        *reinterpret_cast<u32x2 *>(to_v) = u32x2{pack_bf16(dv[0], dv[1]), pack_bf16(dv[2], dv[3])};
+    } else {
+        *reinterpret_cast<f32x4 *>(to_k) = dk;
+        *reinterpret_cast<f32x4 *>(to_v) = dv;
+    }
 }
 
-// Blocks of 128 columns where they fill the card; else of 32, whose wavefronts share the rows of the other side.
+// Whether a side's blocks are of 128 columns (kFull); and if those of dk and dv are of 32 and few, how many share the queries: no more than there are compute units, and enough tiles for
+// each to be worth the third kernel (2000 causal tokens, 8 heads of 128 over 2: 145 us whole, 111 in halves, fp32 830 and 516; 590 x 3, 8 heads of 64 over one 60 and 35).
+bool wide(long long n, long long len, long long rows, long long mult, long long kv_heads)
+{
+    return len * mult > 32 && kv_heads * attn_tiles(n, len, rows, mult, 128) >= kFull;
+}
+int parts_of(const dp_attention_desc &d)
+{
+    const long long rows = d.kv_rows != 0 ? d.kv_rows : (long long)d.n * d.kv_len, shared = d.heads / d.kv_heads;
+    if (d.q_len == 0 || rows == 0 || wide(d.n, d.kv_len, rows, 1, d.kv_heads)) return 1;
+    long long span = d.q_len;   // queries that see a block's keys
+    if (d.left >= 0 && d.right >= 0) span = std::min<long long>(span, (long long)d.left + d.right + 32);
+    const long long tiles = shared * ((span + 127) / 128), blocks = std::max<long long>(1, d.kv_heads * attn_tiles(d.n, d.kv_len, rows, 1, 32));
+    return (int)std::max<long long>(1, std::min<long long>({tiles / (d.io_dtype == DP_BF16 ? 4 : 2), 256 / blocks, 16}));
+}
+
+template <typename T, int DP> auto dkv_kernel(bool wide_one, bool split, int &threads)
+{
+    threads = 256;
+    if (!wide_one) return split ? k_attention_dkv_whole<T, DP, 1, true> : k_attention_dkv_whole<T, DP, 1, false>;
+    if constexpr (sizeof(T) == 4 || DP <= 96) return k_attention_dkv_whole<T, DP, 4, false>;
+    else {
+        threads = 512;
+        return k_attention_dkv<DP>;
+    }
+}
+
 template <typename T> void launch(AttnArgs &a, hipStream_t st)
 {
     for_dim(a.dim, [&](auto dc) {
         constexpr int DP = decltype(dc)::value;
-        const auto wide = [&](const AttnSide &s, long long mult) { return s.len * mult > 32 && a.kv_heads * attn_tiles(a.n, s.len, s.rows, mult, 128) >= kFull; };
         const long long qc = (long long)a.q.len * a.shared, kc = a.kv.len;
-        const bool wq = wide(a.q, a.shared), wk = wide(a.kv, 1);
+        const bool wq = wide(a.n, a.q.len, a.q.rows, a.shared, a.kv_heads), wk = wide(a.n, a.kv.len, a.kv.rows, 1, a.kv_heads);
         a.tiles = (int)((qc + (wq ? 127 : 31)) / (wq ? 128 : 32));
         if (a.tiles > 0 && a.q.rows > 0) hipLaunchKernelGGL((wq ? k_attention_dq<T, DP, 4> : k_attention_dq<T, DP, 1>), dim3(attn_blocks(a, a.q, a.shared, wq ? 128 : 32)), dim3(256), 0, st, a);
         a.tiles = (int)((kc + (wk ? 127 : 31)) / (wk ? 128 : 32));
-        if (a.tiles > 0 && a.kv.rows > 0) {
-            constexpr bool whole = sizeof(T) == 4 || DP <= 96;
-            auto *kernel = !wk ? k_attention_dkv_whole<T, DP, 1> : wide_kernel<T, DP, whole>();
-            hipLaunchKernelGGL(kernel, dim3(attn_blocks(a, a.kv, 1, wk ? 128 : 32)), dim3(wk && !whole ? 512 : 256), 0, st, a);
-        }
+        if (a.tiles == 0 || a.kv.rows == 0) return;
+        int threads;
+        auto *kernel = dkv_kernel<T, DP>(wk, a.kv_parts > 1, threads);
+        hipLaunchKernelGGL(kernel, dim3(attn_blocks(a, a.kv, 1, wk ? 128 : 32) * a.kv_parts), dim3(threads), 0, st, a);
+        if (a.kv_parts == 1) return;
+        a.tiles = (int)((kc * a.kv_heads + kSumThreads / 32 - 1) / (kSumThreads / 32));
+        hipLaunchKernelGGL(k_attention_dkv_sum<T>, dim3((unsigned)((long long)a.n * a.tiles)), dim3(kSumThreads), 0, st, a);
     });
 }
 
@@ -458,9 +513,15 @@ size_t stat_bytes(const dp_attention_desc &d)
     return ((size_t)d.heads * rows * sizeof(float) + 15) / 16 * 16;
 }
 
+size_t sum_bytes(const dp_attention_desc &d)   // of dk's, or of dv's parts
+{
+    const int parts = parts_of(d);
+    return parts == 1 ? 0 : (size_t)parts * (size_t)(d.kv_rows != 0 ? d.kv_rows : (long long)d.n * d.kv_len) * d.kv_heads * d.dim * sizeof(float);
+}
+
 }  // namespace
 
-size_t attn_bwd_bytes(const dp_attention_desc &d) { return 2 * stat_bytes(d); }
+size_t attn_bwd_bytes(const dp_attention_desc &d) { return 2 * (stat_bytes(d) + sum_bytes(d)); }
 
 extern "C" dp_status dp_attention_bwd(const dp_attention_desc *desc, const void *q, const void *k, const void *v, const void *o, const void *dout,
                                       const float *lse, void *dq, void *dk, void *dv, const dp_attention_seqs *seqs, void *ws, size_t ws_bytes,
@@ -473,12 +534,16 @@ extern "C" dp_status dp_attention_bwd(const dp_attention_desc *desc, const void 
     attn_args(d, seqs, a);
     const bool queries = d.n > 0 && d.q_len > 0 && a.q.rows > 0, keys = d.n > 0 && d.kv_len > 0 && a.kv.rows > 0;
     if (!queries && !keys) return DP_OK;
-    if (queries && ((s = attn_pointers({q, o, dout, dq, lse}, nullptr, ws)) != DP_OK || (s = attn_workspace(attn_bwd_bytes(d), ws, ws_bytes)) != DP_OK)) return s;
+    if (queries && (s = attn_pointers({q, o, dout, dq, lse}, nullptr, nullptr)) != DP_OK) return s;
     if (keys && (s = attn_pointers({k, v, dk, dv}, nullptr, nullptr)) != DP_OK) return s;
+    if ((s = attn_pointers({}, nullptr, ws)) != DP_OK || (s = attn_workspace(attn_bwd_bytes(d), ws, ws_bytes)) != DP_OK) return s;
     a.qp = q; a.kp = k; a.vp = v; a.op_in = o; a.dout = dout; a.lse_in = lse;
     a.dq = dq; a.dk = dk; a.dv = dv;
     a.lse2 = (float *)ws;
     a.delta = (float *)((char *)ws + stat_bytes(d));
+    a.kv_parts = parts_of(d);
+    a.part_dk = (float *)((char *)ws + 2 * stat_bytes(d));
+    a.part_dv = (float *)((char *)a.part_dk + sum_bytes(d));
     if (d.io_dtype == DP_BF16) launch<bf16_t>(a, (hipStream_t)hip_stream);
     else launch<float>(a, (hipStream_t)hip_stream);
     return attn_launched("attention's gradient");

@@ -34,6 +34,8 @@ struct AttnArgs {
     int splits, split_keys;                // forward: keys dealt out to so many blocks, split_keys each
     bool ragged;                           // lengths differ: blocks are numbered by the work there is
     float *part_o, *part_ml;               // [split][head][q_rows][dim] and [split][head][q_rows][2]
+    int kv_parts;                          // backward: the queries of a block of keys dealt out to so many blocks,
+    float *part_dk, *part_dv;              // which leave their sums in [part][kv_rows][kv_heads][dim]
 };
 
 namespace {
@@ -80,11 +82,11 @@ DEVFN int prefix_sum(int v)   // over the lanes up to this one
 // among the others, would leave some dies with much more work than others (9 sequences of up to 1500 of 4 heads of keys, dk and dv: 73 us, 53 this way).  Tiles that hold padding alone come last.
 // `mult` columns to a row of `side`; SPLIT: every part of the keys that a sequence has; LAST_FIRST: a causal mask makes a sequence's last tiles the longest.
 constexpr int kMostRagged = 256;   // sequences: more of them are counted for longer than it helps
-template <int COLS, bool SPLIT, bool LAST_FIRST> DEVFN Item item_of(const AttnArgs &a, const AttnSide &side, int mult)
+template <int COLS, bool SPLIT, bool LAST_FIRST> DEVFN Item item_of(const AttnArgs &a, const AttnSide &side, int mult, int block, int of)
 {
     Item r;
     if (!a.ragged) {
-        int id = logical_block(blockIdx.x, gridDim.x);
+        int id = logical_block(block, of);
         r.split = SPLIT ? id % a.splits : 0;
         if (SPLIT) id /= a.splits;
         const int hb = id / a.tiles;
@@ -105,7 +107,7 @@ template <int COLS, bool SPLIT, bool LAST_FIRST> DEVFN Item item_of(const AttnAr
         used = SPLIT ? own : (int)(((long long)rows.used * mult + COLS - 1) / COLS);
         return (list == 0 ? used : own - used) * parts;
     };
-    int id = blockIdx.x, parts, used;
+    int id = block, parts, used;
     for (int list = 0; list < (SPLIT ? 1 : 2); ++list) {
         int total = 0;
         for (int base = 0; base < a.n; base += 64) total += __builtin_amdgcn_readlane(prefix_sum(count(base + lane, list, parts, used)), 63);
@@ -330,27 +332,36 @@ template <int OFF> DEVFN float lds_read4(unsigned addr)
 }
 template <int DP, int NS> struct Second<float, DP, NS> {
     using L = Tile<float, DP>;
-    static constexpr int DB = L::DB, N = NS * DB, READS = 0;
-    float buf[8];
-    DEVFN void begin(unsigned, const TileLane<float, DP> &) {}
+    static constexpr int DB = L::DB, N = NS * DB, READS = 8;
+    float buf[2][8];   // an item's reads are under way while the products of the one before run
     // register v of a lane's column is row 8 (v / 4) + 4 half + v % 4: one 32x32x2 product takes v of both halves
-    template <typename F> DEVFN void run(unsigned tile, const TileLane<float, DP> &l, F &&cols, f32x16 (&acc)[DB])
+    template <int I> DEVFN void read(unsigned tile, const TileLane<float, DP> &l, int chunk)
+    {
+        constexpr int s = I / DB, db = I % DB;
+        for_constant<8>([&](auto ec) {
+            constexpr int e = decltype(ec)::value, row = s * 16 + 8 * (e / 4) + e % 4;   // and 4 h
+            buf[I % 2][e] = lds_read4<row * L::RB>(tile + l.lo + (unsigned)(((db * 8 + chunk) ^ L::swizzle(row + 4 * (int)l.hi)) * 16));
+        });
+    }
+    static DEVFN int own_chunk()
     {
         int chunk = (threadIdx.x & 31) >> 2;
-        const int h = (int)l.hi;
         asm volatile("" : "+v"(chunk));   // addresses are made where they are used: kept for the whole loop they would take registers that the sums need
+        return chunk;
+    }
+    DEVFN void begin(unsigned tile, const TileLane<float, DP> &l) { read<0>(tile, l, own_chunk()); }
+    template <typename F> DEVFN void run(unsigned tile, const TileLane<float, DP> &l, F &&cols, f32x16 (&acc)[DB])
+    {
+        const int chunk = own_chunk();
         for_constant<N>([&](auto ic) {
-            constexpr int i = decltype(ic)::value, s = i / DB, db = i % DB;
-            for_constant<8>([&](auto ec) {
-                constexpr int e = decltype(ec)::value, row = s * 16 + 8 * (e / 4) + e % 4;   // and 4 h
-                buf[e] = lds_read4<row * L::RB>(tile + l.lo + (unsigned)(((db * 8 + chunk) ^ L::swizzle(row + 4 * h)) * 16));
-            });
-            wait_reads<1, 0>();
+            constexpr int i = decltype(ic)::value;
+            if constexpr (i + 1 < N) read<i + 1>(tile, l, chunk);
+            wait_reads<8, (i + 1 < N ? 1 : 0)>();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) tie(buf[e]);
-            const auto c = cols(std::integral_constant<int, s>{});
+            for (int e = 0; e < 8; ++e) tie(buf[i % 2][e]);
+            const auto c = cols(std::integral_constant<int, i / DB>{});
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(buf[e], c[e], acc[db], 0, 0, 0);
+            for (int e = 0; e < 8; ++e) acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x2f32(buf[i % 2][e], c[e], acc[i % DB], 0, 0, 0);
         });
     }
 };

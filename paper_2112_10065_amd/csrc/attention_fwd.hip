@@ -28,7 +28,7 @@ template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(2
     __shared__ alignas(1024) char s_tiles[ROOM];   // K and V of each stage
     __shared__ float2 s_ml[RW > 1 ? 256 : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, wc = wave % CW, wr = wave / CW;
-    const Item item = item_of<COLS, SPLIT, true>(a, a.q, a.shared);
+    const Item item = item_of<COLS, SPLIT, true>(a, a.q, a.shared, blockIdx.x, gridDim.x);
     if (!item.any) return;
     const int b = item.b, hk = item.hk, split = item.split;
     const int col0 = item.tile * COLS;
@@ -268,7 +268,9 @@ Form form_of(const dp_attention_desc &d)
     long long span = d.kv_len;   // keys that a block looks at
     if (d.left >= 0 && d.right >= 0) span = std::min<long long>(span, (long long)d.left + d.right + 32);
     const long long most = std::min<long long>(kMaxSplits, (span + 4 * kt - 1) / (4 * kt));   // four tiles at least: the join takes as long as two
-    const long long want = std::min<long long>(most, 2048 / blocks);
+    // A single token's columns fit one block, which waits for memory most of the time: four rounds of blocks at least.  Others compute, and are split only to give every compute unit work
+    // (2000 causal tokens fp32, 8 heads of 128 over 2, 500 blocks: 221 us in four parts).
+    const long long want = std::min<long long>(most, (cols <= 32 ? 2048 : 512) / blocks);
     if (want < 2) return {1, 1, 0};
     // whole tiles; a window is anywhere in the sequence, so its split counts over all keys
     const long long per = ((d.kv_len + want - 1) / want + kt - 1) / kt * kt;
