@@ -462,7 +462,7 @@ template <typename T> __global__ __launch_bounds__(kSumThreads) void k_attention
 }
 
 // Whether a side's blocks are of 128 columns (kFull); and if those of dk and dv are of 32 and few, how many share the queries: no more than there are compute units, and enough tiles for
-// each to be worth the third kernel (2000 causal tokens, 8 heads of 128 over 2: 145 us whole, 111 in halves, fp32 830 and 516; 590 x 3, 8 heads of 64 over one 60 and 35).
+// each to be worth the third kernel (2000 causal tokens, 8 heads of 128 over 2: 145 us whole, 111 in halves, fp32 830 and 530).
 bool wide(long long n, long long len, long long rows, long long mult, long long kv_heads)
 {
     return len * mult > 32 && kv_heads * attn_tiles(n, len, rows, mult, 128) >= kFull;
