@@ -188,7 +188,6 @@ def _current_stream():
     """Handle of the current device's current stream.  torch.cuda.current_stream() builds a Stream object on every call, most of
     the host time of a small layer's call; once the device is initialised the handle is read directly, if this torch has the two
     functions for it (they are not part of its public interface)."""
-    import torch
     if torch.cuda.is_initialized():
         try:
             return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
@@ -367,23 +366,28 @@ def dp_logprobs_bwd(desc, z, ids, lse, entropy, dlogp, dentropy, dz, stream=None
     _check(lib.dp_logprobs_bwd(C.byref(desc), _ptr(z), _ptr(ids), _ptr(lse), _ptr(entropy), _ptr(dlogp), _ptr(dentropy), _ptr(dz), _stream(stream)))
 
 
+def _elsewhere(t):
+    raise ValueError(f"a tensor is on {t.device}, not on the current GPU")
+
+
 def _ptrs(*tensors):
     """Addresses of tensors that a kernel reads or writes: a kernel of the current device would fault on memory of the host or of another one."""
-    out, device = [], None
+    device = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else None
+    out = []
     for t in tensors:
-        if t is None or isinstance(t, int):
-            out.append(t)
-            continue
-        if device is None:
-            device = torch.cuda.current_device() if torch.cuda.is_available() else -2
-        if t.get_device() != device:
-            raise ValueError(f"a tensor is on {t.device}, not on the current GPU")
-        out.append(t.data_ptr())
+        if t is not None:
+            try:
+                if t.get_device() != device:
+                    _elsewhere(t)
+                t = t.data_ptr()
+            except AttributeError:   # an address as it is
+                pass
+        out.append(t)
     return out
 
 
 def _ws_on(ws):
-    return (None, 0) if ws is None else (_ptrs(ws)[0], ws.numel() * ws.element_size())
+    return (None, 0) if ws is None else (_ptrs(ws)[0], ws.nbytes)
 
 
 def qk_rotary_desc(rows, heads, kv_heads, dim, pairs, io_dtype=DP_BF16, flags=0, eps=1e-6, q_stride=0, k_stride=0, q_out_stride=0, k_out_stride=0,
@@ -400,11 +404,11 @@ def dp_qk_rotary_workspace_bytes(desc, pass_):
 
 def dp_qk_rotary_fwd(desc, q, k, gamma_q, gamma_k, pos, freq, q_out, k_out, stream=None):
     """pos: fp32 [rows, axes]; freq: float64 [sum of pairs]."""
-    _check(lib.dp_qk_rotary_fwd(C.byref(desc), *_ptrs(q, k, gamma_q, gamma_k, pos, freq, q_out, k_out), _stream(stream)))
+    _check(lib.dp_qk_rotary_fwd(desc, *_ptrs(q, k, gamma_q, gamma_k, pos, freq, q_out, k_out), _stream(stream)))
 
 
 def dp_qk_rotary_bwd(desc, q, k, gamma_q, gamma_k, pos, freq, dq_out, dk_out, dq, dk, dgamma_q=None, dgamma_k=None, ws=None, stream=None):
-    _check(lib.dp_qk_rotary_bwd(C.byref(desc), *_ptrs(q, k, gamma_q, gamma_k, pos, freq, dq_out, dk_out, dq, dk, dgamma_q, dgamma_k), *_ws_on(ws), _stream(stream)))
+    _check(lib.dp_qk_rotary_bwd(desc, *_ptrs(q, k, gamma_q, gamma_k, pos, freq, dq_out, dk_out, dq, dk, dgamma_q, dgamma_k), *_ws_on(ws), _stream(stream)))
 
 
 def attention_desc(n, q_len, kv_len, heads, kv_heads, dim, io_dtype=DP_BF16, left=-1, right=-1, scale=0.0, q_rows=0, kv_rows=0, q_stride=0, k_stride=0,
@@ -427,11 +431,11 @@ def dp_attention_workspace_bytes(desc, pass_):
 
 
 def dp_attention_fwd(desc, q, k, v, o, lse=None, seqs=None, ws=None, stream=None):
-    _check(lib.dp_attention_fwd(C.byref(desc), *_ptrs(q, k, v, o, lse), C.byref(seqs) if seqs is not None else None, *_ws_on(ws), _stream(stream)))
+    _check(lib.dp_attention_fwd(desc, *_ptrs(q, k, v, o, lse), seqs, *_ws_on(ws), _stream(stream)))
 
 
 def dp_attention_bwd(desc, q, k, v, o, dout, lse, dq, dk, dv, seqs=None, ws=None, stream=None):
-    _check(lib.dp_attention_bwd(C.byref(desc), *_ptrs(q, k, v, o, dout, lse, dq, dk, dv), C.byref(seqs) if seqs is not None else None, *_ws_on(ws),
+    _check(lib.dp_attention_bwd(desc, *_ptrs(q, k, v, o, dout, lse, dq, dk, dv), seqs, *_ws_on(ws),
                                 _stream(stream)))
 
 

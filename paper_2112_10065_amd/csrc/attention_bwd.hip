@@ -502,7 +502,7 @@ template <typename T> void launch(AttnArgs &a, hipStream_t st)
         auto *kernel = dkv_kernel<T, DP>(wk, a.kv_parts > 1, threads);
         hipLaunchKernelGGL(kernel, dim3(attn_blocks(a, a.kv, 1, wk ? 128 : 32) * a.kv_parts), dim3(threads), 0, st, a);
         if (a.kv_parts == 1) return;
-        a.tiles = (int)((kc * a.kv_heads + kSumThreads / 32 - 1) / (kSumThreads / 32));
+        a.tiles = (int)((std::min<long long>(kc, a.kv.rows) * a.kv_heads + kSumThreads / 32 - 1) / (kSumThreads / 32));
         hipLaunchKernelGGL(k_attention_dkv_sum<T>, dim3((unsigned)((long long)a.n * a.tiles)), dim3(kSumThreads), 0, st, a);
     });
 }

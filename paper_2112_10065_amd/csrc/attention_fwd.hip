@@ -420,7 +420,7 @@ extern "C" dp_status dp_attention_fwd(const dp_attention_desc *desc, const void 
     if (bf) launch<bf16_t>(a, f, blocks, st);
     else launch<float>(a, f, blocks, st);
     if (f.splits > 1) {
-        a.tiles = (int)((cols + kJoinThreads / 32 - 1) / (kJoinThreads / 32));
+        a.tiles = (int)((std::min<long long>(d.q_len, a.q.rows) * a.shared + kJoinThreads / 32 - 1) / (kJoinThreads / 32));
         hipLaunchKernelGGL(bf ? k_attention_join<bf16_t> : k_attention_join<float>, dim3((unsigned)(groups * a.tiles)), dim3(kJoinThreads), 0, st, a);
     }
     return attn_launched(kName);
