@@ -2,7 +2,12 @@
 //   dv_j = sum_i p_ij dout_i;   ds_ij = p_ij (dp_ij - delta_i);   dq_i = scale sum_j ds_ij k_j;   dk_j = scale sum_i ds_ij q_i
 // Two kernels, each with its sums in registers from the first to the last tile: one holds queries and lets keys pass (dq; it computes delta and leaves it for the other),
 // one holds keys and lets the queries of all heads that share them pass (dk, dv).  p and dp are computed in both, seven products for the five that the formulas
-// have, in return for sums without atomics in a fixed order and without partial sums in memory (dq's would be 32 bits per query and block of keys).
+// have, in return for sums without atomics in a fixed order and without partial sums in memory (dq's would be 32 bits per query and block of keys: 2 GB written and read for two
+// sequences of 4096 causal tokens, 0.8 ms, where the two products take 0.25).
+// With bf16, p and ds are rounded as operands of the second products; p, dp and delta themselves stay in 32 bits.
+//
+// Bound by the matrix cores: two sequences of 4096 causal tokens, 32 heads of 128 over 8: dq 385-398 us (1.05 PFLOP/s of the products that it computes), dk and dv 557 (0.99).
+// Short sequences wait: 32 x 197 tokens, 12 heads of 64, 20 + 26 us for four tiles a block in one round and one and a half.
 #include "attention_common.h"
 #include <algorithm>
 

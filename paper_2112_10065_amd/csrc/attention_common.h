@@ -200,7 +200,8 @@ template <> struct Mma<float> {
     }
 };
 
-// Reads that a pipeline has under way, oldest first: read(i) issues NR reads of item i, wait(i) makes them ready, use(i) takes them.
+// Waits until LEFT items of NR reads each are under way at most (reads from LDS arrive in their order, so the older ones are there), and the
+// mark of a register that such a read fills: nothing that uses it is moved in front of the wait.
 template <int NR, int LEFT> DEVFN void wait_reads()
 {
     constexpr int n = NR * LEFT < 15 ? NR * LEFT : 15;
