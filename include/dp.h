@@ -438,7 +438,7 @@ dp_status dp_qk_rotary_bwd(const dp_qk_rotary_desc *desc, const void *q, const v
  * Arithmetic: products on the matrix cores with fp32 sums; softmax, its statistics and all sums fp32.  With DP_BF16 the probabilities (and in the
  * backward pass p and dp's product with it) are rounded to bf16 as operands of the second product.  A value or gradient row that is NaN or infinite
  * may make NaN also of queries that do not see it, if they share a tile with ones that do; unused rows never do.
- * Tensors may hold more than 2^31 elements here. */
+ * Results may not overlap inputs or each other (dq, dk and dv may lie side by side in the same rows).  Tensors may hold more than 2^31 elements here. */
 typedef struct {
     int32_t n, q_len, kv_len;   /* n, q_len, kv_len >= 0 */
     int32_t heads, kv_heads;    /* heads a multiple of kv_heads */

@@ -541,7 +541,8 @@ extern "C" dp_status dp_attention_bwd(const dp_attention_desc *desc, const void 
     if (!queries && !keys) return DP_OK;
     if (queries && (s = attn_pointers({q, o, dout, dq, lse}, nullptr, nullptr)) != DP_OK) return s;
     if (keys && (s = attn_pointers({k, v, dk, dv}, nullptr, nullptr)) != DP_OK) return s;
-    if ((s = attn_pointers({}, nullptr, ws)) != DP_OK || (s = attn_workspace(attn_bwd_bytes(d), ws, ws_bytes)) != DP_OK) return s;
+    // dk and dv are made behind dq, from all inputs but o
+    if ((s = attn_apart({queries ? dq : nullptr, keys ? dk : nullptr, keys ? dv : nullptr}, {q, k, v, o, dout, lse})) != DP_OK || (s = attn_pointers({}, nullptr, ws)) != DP_OK || (s = attn_workspace(attn_bwd_bytes(d), ws, ws_bytes)) != DP_OK) return s;
     a.qp = q; a.kp = k; a.vp = v; a.op_in = o; a.dout = dout; a.lse_in = lse;
     a.dq = dq; a.dk = dk; a.dv = dv;
     a.lse2 = (float *)ws;

@@ -459,6 +459,7 @@ template <typename F> void for_dim(int dim, F &&f)
 dp_status attn_check(const dp_attention_desc *desc, const dp_attention_seqs *seqs);
 void attn_args(const dp_attention_desc &d, const dp_attention_seqs *seqs, AttnArgs &a);
 dp_status attn_pointers(std::initializer_list<const void *> needed, const void *lse, const void *ws);
+dp_status attn_apart(std::initializer_list<const void *> results, std::initializer_list<const void *> inputs);
 dp_status attn_workspace(size_t need, const void *ws, size_t ws_bytes);
 dp_status attn_launched(const char *what);
 // tiles of `columns` that n sequences of up to `len` rows can have, `mult` columns to a row; packed ones have no more rows than there are in memory

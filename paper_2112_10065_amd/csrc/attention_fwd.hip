@@ -338,9 +338,9 @@ dp_status attn_check(const dp_attention_desc *desc, const dp_attention_seqs *seq
         dp_set_error("%s: %lld and %lld rows do not hold the sequences, or are more than 2^31", kName, (long long)d.q_rows, (long long)d.kv_rows);
         return DP_ERR_BAD_DESC;
     }
-    // blocks are counted in 31 bits, at the smallest tile and the most splits
-    const long long shared = d.heads / d.kv_heads;
-    if ((long long)d.q_len * shared >= (1ll << 30) || (double)d.n * d.kv_heads * (((double)d.q_len * shared + 7) / 8) >= 2147483000.0 || (double)d.n * d.kv_heads * (d.kv_len / 32 + 1) >= 2147483000.0) {
+    // a launch has fewer than 2^32 threads, 512 to a block at the most
+    const double shared = d.heads / d.kv_heads, most = (double)std::max<double>(d.q_len * shared, d.kv_len);
+    if (d.q_len * shared >= (double)(1 << 30) || (double)d.n * d.kv_heads * (std::floor(most / 128) + 1) >= (double)(1 << 23)) {
         dp_set_error("%s: too many sequences, heads and tokens for one launch", kName);
         return DP_ERR_BAD_DESC;
     }
@@ -371,6 +371,14 @@ dp_status attn_pointers(std::initializer_list<const void *> needed, const void *
     for (const void *p : needed) if (p == nullptr) { dp_set_error("%s: a required pointer is NULL", kName); return DP_ERR_NULL; }
     for (const void *p : needed) if ((reinterpret_cast<uintptr_t>(p) & 15u) != 0) { dp_set_error("%s: pointers must be 16-byte aligned", kName); return DP_ERR_BAD_DESC; }
     if ((reinterpret_cast<uintptr_t>(lse) & 3u) != 0 || (reinterpret_cast<uintptr_t>(ws) & 15u) != 0) { dp_set_error("%s: lse must be 4-byte, the workspace 16-byte aligned", kName); return DP_ERR_BAD_DESC; }
+    return DP_OK;
+}
+
+dp_status attn_apart(std::initializer_list<const void *> results, std::initializer_list<const void *> inputs)
+{
+    for (const void *r : results)
+        for (const void *i : inputs)
+            if (r == i && r != nullptr) { dp_set_error("%s: a result may not take the place of an input", kName); return DP_ERR_BAD_DESC; }
     return DP_OK;
 }
 
@@ -411,6 +419,7 @@ extern "C" dp_status dp_attention_fwd(const dp_attention_desc *desc, const void 
     attn_args(d, seqs, a);
     if (d.n == 0 || d.q_len == 0 || a.q.rows == 0) return DP_OK;
     if ((s = attn_pointers({q, o}, lse, ws)) != DP_OK || (d.kv_len > 0 && a.kv.rows > 0 && (s = attn_pointers({k, v}, nullptr, nullptr)) != DP_OK)) return s;
+    if ((s = attn_apart({o}, {q, k, v})) != DP_OK) return s;
     const Form f = form_of(d);
     if ((s = attn_workspace(split_bytes(d, f), ws, ws_bytes)) != DP_OK) return s;
     a.qp = q; a.kp = k; a.vp = v; a.op = o; a.lse = lse;

@@ -93,10 +93,10 @@ def test_attention_refusals(dp):
     def seqs(**kw):
         return dp.attention_seqs(**kw)
 
-    def fwd(d=good, q=A, k=A, v=A, o=A, lse=A, s=None, ws=A, nbytes=1 << 40):
+    def fwd(d=good, q=A, k=A, v=A, o=A + 64, lse=A, s=None, ws=A, nbytes=1 << 40):
         return lib.dp_attention_fwd(C.byref(d) if d is not None else None, q, k, v, o, lse, C.byref(s) if s is not None else None, ws, nbytes, None)
 
-    def bwd(d=good, q=A, k=A, v=A, o=A, do=A, lse=A, dq=A, dk=A, dv=A, s=None, ws=A, nbytes=1 << 40):
+    def bwd(d=good, q=A, k=A, v=A, o=A, do=A, lse=A, dq=A + 64, dk=A + 128, dv=A + 192, s=None, ws=A, nbytes=1 << 40):
         return lib.dp_attention_bwd(C.byref(d) if d is not None else None, q, k, v, o, do, lse, dq, dk, dv, C.byref(s) if s is not None else None, ws, nbytes, None)
 
     assert fwd(d=None) == bwd(d=None) == dp.DP_ERR_NULL
@@ -111,13 +111,17 @@ def test_attention_refusals(dp):
     for bad in (dict(n=-1), dict(q_len=-1), dict(kv_len=-1), dict(q_len=1 << 29), dict(heads=0), dict(kv_heads=0), dict(heads=5), dict(dim=4), dict(dim=20), dict(dim=136),
                 dict(left=-2), dict(right=-2), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(q_stride=64), dict(q_stride=132), dict(o_stride=-128),
                 dict(v_stride=60), dict(k_stride=1 << 23), dict(q_rows=9), dict(kv_rows=13), dict(q_rows=-1), dict(kv_rows=1 << 32), dict(n=1 << 16, q_len=1 << 20),
-                dict(n=1 << 30, q_len=1, kv_len=1), dict(q_len=1 << 28, heads=16)):
+                dict(n=1 << 30, q_len=1, kv_len=1), dict(n=1 << 22, q_len=1, kv_len=1), dict(n=1 << 12, q_len=1 << 17), dict(q_len=1 << 28, heads=16)):
         assert fwd(d=att(dp, **bad)) == bwd(d=att(dp, **bad)) == dp.DP_ERR_BAD_DESC, bad
     assert fwd(d=att(dp, io_dtype=2)) == bwd(d=att(dp, io_dtype=2)) == dp.DP_ERR_UNSUPPORTED
     for bad in (seqs(q_starts=A, q_lens=A), seqs(kv_starts=A, kv_lens=A)):
         assert fwd(s=bad) == bwd(s=bad) == dp.DP_ERR_UNSUPPORTED
     assert fwd(s=seqs(q_lens=A + 2)) == bwd(s=seqs(kv_starts=A + 1)) == dp.DP_ERR_BAD_DESC
     assert fwd(d=att(dp, q_rows=9), s=seqs(kv_starts=A)) == dp.DP_ERR_BAD_DESC     # only packed rows may be fewer than n q_len
+    for name in ('q', 'k', 'v'):
+        assert fwd(o=A, **{name: A}) == dp.DP_ERR_BAD_DESC                       # in place
+    for name in ('dq', 'dk', 'dv'):
+        assert bwd(**{name: A}) == dp.DP_ERR_BAD_DESC
     assert b"attention" in lib.dp_last_error()
     import torch
     with pytest.raises(ValueError, match="int32"):
@@ -151,5 +155,5 @@ def test_attention_valid_calls(dp):
                  (att(dp, n=1, q_len=1, kv_len=200000), None), (att(dp, n=64, q_len=1000, kv_len=1000, heads=32, kv_heads=8, dim=128, right=0), None)):
         byref = C.byref(s) if s is not None else None
         need = dp.dp_attention_workspace_bytes(d, dp.DP_PASS_FWD), dp.dp_attention_workspace_bytes(d, dp.DP_PASS_DGRAD)
-        assert lib.dp_attention_fwd(C.byref(d), A, A, A, A, None, byref, A, need[0], None) == dp.DP_ERR_HIP
-        assert lib.dp_attention_bwd(C.byref(d), A, A, A, A, A, A, A, A, A, byref, A, need[1], None) == dp.DP_ERR_HIP
+        assert lib.dp_attention_fwd(C.byref(d), A, A, A, A + 64, None, byref, A, need[0], None) == dp.DP_ERR_HIP
+        assert lib.dp_attention_bwd(C.byref(d), A, A, A, A, A, A, A + 64, A + 128, A + 192, byref, A, need[1], None) == dp.DP_ERR_HIP

@@ -197,6 +197,25 @@ def test_few_queries_over_many_keys(env, case, bf16):
 
 
 @pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+def test_few_queries_padded_and_packed_over_many_keys(env, bf16):
+    """Splits of the keys with queries that are not in use, or packed; every workspace begins as NaN."""
+    Case(env, 4, 3, 2100, 8, 2, 64, -1, 0, bf16, q_side=[3, 0, 1, 2], kv_side=[2100, 1700, 0, 1]).check()
+    Case(env, 4, 3, 2100, 8, 2, 72, -1, -1, bf16, q_side=("packed", [3, 0, 1, 2], 1, 2), kv_side=("packed", [2100, 1700, 0, 1], 0, 1)).check(True, True)
+    Case(env, 4, 3, 2100, 8, 2, 128, 900, 0, bf16, q_side=("packed", [3, 0, 1, 2], 1, 2)).check(True, False)
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("dim", [40, 64, 128])
+def test_queries_dealt_out(env, dim, bf16):
+    """Few blocks of keys with many queries: dk and dv are sums over several blocks, some of them of nothing."""
+    for left, right in ((-1, -1), (-1, 0), (300, 40)):
+        c = Case(env, 1, 900, 70, 6, 1, dim, left, right, bf16)
+        assert c.dp.dp_attention_workspace_bytes(c.desc, c.dp.DP_PASS_DGRAD) > 2 * 4 * 6 * 900
+        c.check()
+    Case(env, 3, 900, 70, 6, 1, dim, -1, 0, bf16, q_side=[900, 0, 130], kv_side=("packed", [70, 5, 33], 1, 2)).check(False, True)
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
 @pytest.mark.parametrize("mask", [(-1, -1), (-1, 0), (50, 9)], ids=str)
 @pytest.mark.parametrize("dim", [24, 40, 64, 72, 96, 104, 128])
 def test_many_blocks(env, dim, mask, bf16):
