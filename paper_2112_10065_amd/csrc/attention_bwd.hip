@@ -35,13 +35,13 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
     const int wcol = col0 + wc * 32, col = wcol + (lane & 31), i = col / a.shared, head = hk * a.shared + col % a.shared;
     const bool own = i < rq.own, on = i < rq.used;
     const int ahead = rk.used - rq.used, last = rq.used * a.shared - 1;
-    long long lo = 0, hi = 0;
-    const long long i0 = col0 / a.shared, i1 = min(col0 + COLS - 1, last) / a.shared, w0 = wcol / a.shared, w1 = min(wcol + 31, last) / a.shared;
+    int lo = 0, hi = 0;   // lengths are at most 2^28 and bounds 2^30: no sum here passes 31 bits
+    const int i0 = col0 / a.shared, i1 = min(col0 + COLS - 1, last) / a.shared, w0 = wcol / a.shared, w1 = min(wcol + 31, last) / a.shared;
     if (col0 <= last) {
-        lo = max(0ll, i0 + ahead - a.left);
-        hi = min((long long)rk.used, i1 + ahead + a.right + 1);
+        lo = max(0, i0 + ahead - a.left);
+        hi = min(rk.used, i1 + ahead + a.right + 1);
     }
-    const int first = (int)lo, keys = (int)max(0ll, hi - lo);
+    const int first = lo, keys = max(0, hi - lo);
     const long long row = rq.first + i, stat = (long long)head * a.q.rows + row;
 
     TileCopy<T, DP, KT, 256> ck, cv;
@@ -81,12 +81,11 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
         if (on && half == 0 && wr == 0) { a.lse2[stat] = lse2; a.delta[stat] = -delta; }
     }
     const int mine = wr * NB * 32;
-    const long long see0 = max((long long)i + ahead - a.left - first, 0ll), see1 = min((long long)i + ahead + a.right + 1 - first, (long long)keys);
-    const int seen0 = (int)min(see0, (long long)kFar);
-    const unsigned seen = on ? (unsigned)max(see1 - seen0, 0ll) : 0u;
+    const int seen0 = max(i + ahead - a.left - first, 0);
+    const unsigned seen = on ? (unsigned)max(min(i + ahead + a.right + 1 - first, keys) - seen0, 0) : 0u;
     // keys t ... t + 31 are seen by all of the wavefront's queries if all0 <= t <= all1, by none if t <= none0 or t >= none1
-    const int all0 = (int)min(max(w1 + ahead - a.left - first, 0ll), (long long)kFar), all1 = (int)max(min(w0 + ahead + a.right + 1 - first, (long long)keys) - 32, -1ll);
-    const int none0 = (int)(min(max(w0 + ahead - a.left - first, 0ll), (long long)kFar) - 32), none1 = (int)min(min(w1 + ahead + a.right + 1 - first, (long long)keys), (long long)kFar);
+    const int all0 = max(w1 + ahead - a.left - first, 0), all1 = max(min(w0 + ahead + a.right + 1 - first, keys) - 32, -1);
+    const int none0 = max(w0 + ahead - a.left - first, 0) - 32, none1 = min(w1 + ahead + a.right + 1 - first, keys);
 
     f32x16 acc[DB];
     clear(acc);
@@ -154,23 +153,22 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
 struct Seen { int first, count, seen0, all0, all1, none0, none1; unsigned seen; };
 template <int COLS> DEVFN Seen seen_by(const AttnArgs &a, const Rows &rq, const Rows &rk, int col0, int wcol, int j)
 {
-    const long long ahead = rk.used - rq.used, w0 = wcol, last = rk.used - 1, j1 = min((long long)col0 + COLS - 1, last), w1 = min(w0 + 31, last);
-    long long lo = 0, hi = 0;
+    const int ahead = rk.used - rq.used, w0 = wcol, last = rk.used - 1, j1 = min(col0 + COLS - 1, last), w1 = min(w0 + 31, last);
+    int lo = 0, hi = 0;   // lengths are at most 2^28 and bounds 2^30: no sum here passes 31 bits
     if (col0 <= last) {
-        lo = max(0ll, col0 - a.right - ahead);
-        hi = min((long long)rq.used, j1 + a.left - ahead + 1);
+        lo = max(0, col0 - a.right - ahead);
+        hi = min(rq.used, j1 + a.left - ahead + 1);
     }
     Seen s;
-    s.first = (int)min(lo, (long long)kFar);
-    s.count = (int)max(0ll, hi - lo);
-    const long long see0 = max(j - a.right - ahead - s.first, 0ll), see1 = min(j + a.left - ahead + 1 - s.first, (long long)s.count);
-    s.seen0 = (int)min(see0, (long long)kFar);
-    s.seen = j < rk.used ? (unsigned)max(see1 - s.seen0, 0ll) : 0u;
+    s.first = lo;
+    s.count = max(0, hi - lo);
+    s.seen0 = max(j - a.right - ahead - s.first, 0);
+    s.seen = j < rk.used ? (unsigned)max(min(j + a.left - ahead + 1 - s.first, s.count) - s.seen0, 0) : 0u;
     // queries t ... t + 31 see all of the wavefront's keys if all0 <= t <= all1 (those behind the last one add zeros), none of them if t <= none0 or t >= none1
-    s.all0 = (int)min(max(w1 - a.right - ahead - s.first, 0ll), (long long)kFar);
-    s.all1 = (int)max(min(w0 + a.left - ahead + 1 - s.first, (long long)kFar) - 32, -1ll);
-    s.none0 = (int)(min(max(w0 - a.right - ahead - s.first, 0ll), (long long)kFar) - 32);
-    s.none1 = (int)min(min(w1 + a.left - ahead + 1 - s.first, (long long)s.count), (long long)kFar);
+    s.all0 = max(w1 - a.right - ahead - s.first, 0);
+    s.all1 = max(w0 + a.left - ahead + 1 - s.first - 32, -1);
+    s.none0 = max(w0 - a.right - ahead - s.first, 0) - 32;
+    s.none1 = min(w1 + a.left - ahead + 1 - s.first, s.count);
     return s;
 }
 DEVFN void hide(f32x16 &s, const Seen &w, int t, int half)

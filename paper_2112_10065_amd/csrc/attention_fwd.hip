@@ -44,28 +44,27 @@ template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(2
     const int wcol = col0 + wc * 32, col = wcol + (lane & 31), i = col / a.shared, head = hk * a.shared + col % a.shared;
     const bool own = i < rq.own, on = i < rq.used;
     const int ahead = rk.used - rq.used, last = rq.used * a.shared - 1;
-    // the keys that the block's queries see, and the wavefront's
-    long long lo = 0, hi = 0;
-    const long long i0 = col0 / a.shared, i1 = min(col0 + COLS - 1, last) / a.shared, w0 = wcol / a.shared, w1 = min(wcol + 31, last) / a.shared;
+    // the keys that the block's queries see, and the wavefront's (lengths are at most 2^28 and bounds 2^30: no sum here passes 31 bits)
+    int lo = 0, hi = 0;
+    const int i0 = col0 / a.shared, i1 = min(col0 + COLS - 1, last) / a.shared, w0 = wcol / a.shared, w1 = min(wcol + 31, last) / a.shared;
     if (col0 <= last) {
-        lo = max(0ll, i0 + ahead - a.left);
-        hi = min((long long)rk.used, i1 + ahead + a.right + 1);
+        lo = max(0, i0 + ahead - a.left);
+        hi = min(rk.used, i1 + ahead + a.right + 1);
     }
     if (SPLIT) {
-        lo = max(lo, (long long)split * a.split_keys);
-        hi = min(hi, (long long)(split + 1) * a.split_keys);
+        lo = max(lo, split * a.split_keys);
+        hi = min(hi, (split + 1) * a.split_keys);
     }
-    const int first = (int)lo, keys = (int)max(0ll, hi - lo);
+    const int first = lo, keys = max(0, hi - lo);
     const long long row = rq.first + i;
 
     // the lane's keys, counted from the wavefront's place in the first tile
     const int mine = wr * NB * 32;
-    const long long see0 = max((long long)i + ahead - a.left - first, 0ll), see1 = min((long long)i + ahead + a.right + 1 - first, (long long)keys);
-    const int seen0 = (int)min(see0, (long long)kFar);
-    const unsigned seen = on ? (unsigned)max(see1 - seen0, 0ll) : 0u;
+    const int seen0 = max(i + ahead - a.left - first, 0);
+    const unsigned seen = on ? (unsigned)max(min(i + ahead + a.right + 1 - first, keys) - seen0, 0) : 0u;
     // a wavefront's keys from t on are seen by all of its queries if all0 <= t <= all1, by none if t <= none0 or t >= none1
-    const int all0 = (int)min(max(w1 + ahead - a.left - first, 0ll), (long long)kFar), all1 = (int)max(min(w0 + ahead + a.right + 1 - first, (long long)keys) - NB * 32, -1ll);
-    const int none0 = (int)(min(max(w0 + ahead - a.left - first, 0ll), (long long)kFar) - NB * 32), none1 = (int)min(min(w1 + ahead + a.right + 1 - first, (long long)keys), (long long)kFar);
+    const int all0 = max(w1 + ahead - a.left - first, 0), all1 = max(min(w0 + ahead + a.right + 1 - first, keys) - NB * 32, -1);
+    const int none0 = max(w0 + ahead - a.left - first, 0) - NB * 32, none1 = min(w1 + ahead + a.right + 1 - first, keys);
 
     f32x16 acc[DB];
     clear(acc);
