@@ -464,16 +464,12 @@ template <typename T> __global__ __launch_bounds__(kSumThreads) void k_attention
     }
 }
 
-// Whether a side's blocks are of 128 columns (kFull); and if those of dk and dv are of 32 and few, how many share the queries: no more than there are compute units, and enough tiles for
+// If the blocks of dk and dv are of 32 columns and few, how many share the queries: no more than there are compute units, and enough tiles for
 // each to be worth the third kernel (2000 causal tokens, 8 heads of 128 over 2: 145 us whole, 111 in halves, fp32 830 and 530).
-bool wide(long long n, long long len, long long rows, long long mult, long long kv_heads)
-{
-    return len * mult > 32 && kv_heads * attn_tiles(n, len, rows, mult, 128) >= kFull;
-}
 int parts_of(const dp_attention_desc &d)
 {
     const long long rows = d.kv_rows != 0 ? d.kv_rows : (long long)d.n * d.kv_len, shared = d.heads / d.kv_heads;
-    if (d.q_len == 0 || rows == 0 || wide(d.n, d.kv_len, rows, 1, d.kv_heads)) return 1;
+    if (d.q_len == 0 || rows == 0 || attn_wide(d, d.kv_len, rows, 1)) return 1;
     long long span = d.q_len;   // queries that see a block's keys
     if (d.left >= 0 && d.right >= 0) span = std::min<long long>(span, (long long)d.left + d.right + 32);
     const long long tiles = shared * ((span + 127) / 128), blocks = std::max<long long>(1, d.kv_heads * attn_tiles(d.n, d.kv_len, rows, 1, 32));
@@ -491,12 +487,12 @@ template <typename T, int DP> auto dkv_kernel(bool wide_one, bool split, int &th
     }
 }
 
-template <typename T> void launch(AttnArgs &a, hipStream_t st)
+template <typename T> void launch(const dp_attention_desc &d, AttnArgs &a, hipStream_t st)
 {
     for_dim(a.dim, [&](auto dc) {
         constexpr int DP = decltype(dc)::value;
         const long long qc = (long long)a.q.len * a.shared, kc = a.kv.len;
-        const bool wq = wide(a.n, a.q.len, a.q.rows, a.shared, a.kv_heads), wk = wide(a.n, a.kv.len, a.kv.rows, 1, a.kv_heads);
+        const bool wq = attn_wide(d, a.q.len, a.q.rows, a.shared), wk = attn_wide(d, a.kv.len, a.kv.rows, 1);
         a.tiles = (int)((qc + (wq ? 127 : 31)) / (wq ? 128 : 32));
         if (a.tiles > 0 && a.q.rows > 0) hipLaunchKernelGGL((wq ? k_attention_dq<T, DP, 4> : k_attention_dq<T, DP, 1>), dim3(attn_blocks(a, a.q, a.shared, wq ? 128 : 32)), dim3(256), 0, st, a);
         a.tiles = (int)((kc + (wk ? 127 : 31)) / (wk ? 128 : 32));
@@ -548,7 +544,7 @@ extern "C" dp_status dp_attention_bwd(const dp_attention_desc *desc, const void 
     a.kv_parts = parts_of(d);
     a.part_dk = (float *)((char *)ws + 2 * stat_bytes(d));
     a.part_dv = (float *)((char *)a.part_dk + sum_bytes(d));
-    if (d.io_dtype == DP_BF16) launch<bf16_t>(a, (hipStream_t)hip_stream);
-    else launch<float>(a, (hipStream_t)hip_stream);
+    if (d.io_dtype == DP_BF16) launch<bf16_t>(d, a, (hipStream_t)hip_stream);
+    else launch<float>(d, a, (hipStream_t)hip_stream);
     return attn_launched("attention's gradient");
 }

@@ -468,6 +468,17 @@ inline long long attn_tiles(long long n, long long len, long long rows, long lon
     const long long all = n * ((len * mult + columns - 1) / columns), packed = rows * mult / columns + n;
     return rows < n * len && packed < all ? packed : all;
 }
+// Whether blocks are of 128 columns.  bf16: from kFull on.  fp32, whose matrix products take sixteen times as long and hide the rest: a block of 32 columns takes only 1.3 times as long for its
+// work, so that the larger ones have to come out even: full rounds of 256, or, where a causal mask makes them unequal, enough of them (2 x 1788 causal tokens, 12 heads of 72, 336
+// blocks: 276 us, in small ones 183; 4 x 1024 tokens, 8 heads of 64, 256 blocks: 82 and 107).
+inline bool attn_wide(const dp_attention_desc &d, long long len, long long rows, long long mult)
+{
+    const long long blocks = d.kv_heads * attn_tiles(d.n, len, rows, mult, 128);
+    if (len * mult <= 32 || blocks < kFull) return false;
+    if (d.io_dtype == DP_BF16) return true;
+    const double rounds = blocks / 256.0;
+    return (d.left < 0) != (d.right < 0) ? 0.5 * rounds + 0.75 <= 0.65 * rounds + 0.2 : (double)((blocks + 255) / 256) <= 1.3 * rounds + 0.2;
+}
 // blocks of a call: where they are numbered by what there is, no more than that can be
 inline unsigned attn_blocks(const AttnArgs &a, const AttnSide &side, long long mult, int columns)
 {

@@ -267,7 +267,7 @@ long long rows_or(long long rows, long long dense) { return rows != 0 ? rows : d
 Form form_of(const dp_attention_desc &d)
 {
     const long long shared = d.heads / d.kv_heads, cols = d.q_len * shared, rows = rows_or(d.q_rows, (long long)d.n * d.q_len);
-    if (cols > 32 && d.kv_heads * attn_tiles(d.n, d.q_len, rows, shared, 128) >= kFull) return {4, 1, 0};
+    if (attn_wide(d, d.q_len, rows, shared)) return {4, 1, 0};
     const long long blocks = std::max<long long>(1, d.kv_heads * attn_tiles(d.n, d.q_len, rows, shared, 32));
     constexpr int kt = 128;
     long long span = d.kv_len;   // keys that a block looks at

@@ -225,6 +225,15 @@ def test_many_blocks(env, dim, mask, bf16):
     Case(env, 33, 70, 150, 8, 8, dim, *mask, bf16, q_side=("packed", lq, 1, 2), kv_side=lk).check(True, False)
 
 
+@pytest.mark.parametrize("mask", [(-1, -1), (-1, 0), (13, 5)], ids=str)
+@pytest.mark.parametrize("dim", [32, 40, 64, 80, 96, 112, 128])
+def test_many_blocks_in_full_rounds(env, dim, mask):
+    """fp32 takes blocks of 128 columns where they come out even, or where there are many."""
+    Case(env, 64, 40, 50, 16, 16, dim, *mask, False).check()
+    if dim in (64, 80):
+        Case(env, 64, 131, 150, 16, 8, dim, *mask, False, q_side=[131 - b % 7 for b in range(64)], kv_side=[150 - b % 40 for b in range(64)]).check()
+
+
 @pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
 def test_large_scores_and_scale(env, bf16):
     """Scores of hundreds: the running maximum grows again and again, most probabilities vanish."""
