@@ -469,10 +469,8 @@ template <typename T> __global__ __launch_bounds__(kSumThreads) void k_attention
 int parts_of(const dp_attention_desc &d)
 {
     const long long rows = d.kv_rows != 0 ? d.kv_rows : (long long)d.n * d.kv_len, shared = d.heads / d.kv_heads;
-    if (d.q_len == 0 || rows == 0 || attn_wide(d, d.kv_len, rows, 1)) return 1;
-    long long span = d.q_len;   // queries that see a block's keys
-    if (d.left >= 0 && d.right >= 0) span = std::min<long long>(span, (long long)d.left + d.right + 32);
-    const long long tiles = shared * ((span + 127) / 128), blocks = std::max<long long>(1, d.kv_heads * attn_tiles(d.n, d.kv_len, rows, 1, 32));
+    if (d.q_len == 0 || rows == 0 || attn_wide(d, d.kv_len, rows, 1, shared * attn_seen(d, d.q_len, 128))) return 1;
+    const long long tiles = shared * ((attn_seen(d, d.q_len, 32) + 127) / 128), blocks = std::max<long long>(1, d.kv_heads * attn_tiles(d.n, d.kv_len, rows, 1, 32));
     return (int)std::max<long long>(1, std::min<long long>({tiles / (d.io_dtype == DP_BF16 ? 4 : 2), 256 / blocks, 16}));
 }
 
@@ -492,7 +490,7 @@ template <typename T> void launch(const dp_attention_desc &d, AttnArgs &a, hipSt
     for_dim(a.dim, [&](auto dc) {
         constexpr int DP = decltype(dc)::value;
         const long long qc = (long long)a.q.len * a.shared, kc = a.kv.len;
-        const bool wq = attn_wide(d, a.q.len, a.q.rows, a.shared), wk = attn_wide(d, a.kv.len, a.kv.rows, 1);
+        const bool wq = attn_wide(d, a.q.len, a.q.rows, a.shared, attn_seen(d, a.kv.len, std::max(1, 128 / a.shared))), wk = attn_wide(d, a.kv.len, a.kv.rows, 1, a.shared * attn_seen(d, a.q.len, 128));
         a.tiles = (int)((qc + (wq ? 127 : 31)) / (wq ? 128 : 32));
         if (a.tiles > 0 && a.q.rows > 0) hipLaunchKernelGGL((wq ? k_attention_dq<T, DP, 4> : k_attention_dq<T, DP, 1>), dim3(attn_blocks(a, a.q, a.shared, wq ? 128 : 32)), dim3(256), 0, st, a);
         a.tiles = (int)((kc + (wk ? 127 : 31)) / (wk ? 128 : 32));

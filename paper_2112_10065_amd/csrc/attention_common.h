@@ -42,10 +42,6 @@ namespace {
 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 constexpr int kFar = 1 << 30;
-// Blocks of four wavefronts side by side do two and a half times the work of the same four on one set of columns in the same time (24 packed sequences: 87 and 267 us; 32 of 197
-// tokens, backward: 46 and 93), and there is a quarter of them: from so many on they are the faster ones, though the card has room for more.
-constexpr int kFull = 160;
-
 // Rows of one sequence: where they begin, how many are in use, and how many are its own to be written.
 struct Rows { long long first; int used, own; };
 DEVFN Rows rows_of(const AttnSide &s, int b)
@@ -468,16 +464,28 @@ inline long long attn_tiles(long long n, long long len, long long rows, long lon
     const long long all = n * ((len * mult + columns - 1) / columns), packed = rows * mult / columns + n;
     return rows < n * len && packed < all ? packed : all;
 }
-// Whether blocks are of 128 columns.  bf16: from kFull on.  fp32, whose matrix products take sixteen times as long and hide the rest: a block of 32 columns takes only 1.3 times as long for its
-// work, so that the larger ones have to come out even: full rounds of 256, or, where a causal mask makes them unequal, enough of them (2 x 1788 causal tokens, 12 heads of 72, 336
-// blocks: 276 us, in small ones 183; 4 x 1024 tokens, 8 heads of 64, 256 blocks: 82 and 107).
-inline bool attn_wide(const dp_attention_desc &d, long long len, long long rows, long long mult)
+// Whether blocks are of 128 columns, four wavefronts side by side, or of 32, whose wavefronts share the other side's rows: what is shorter by this count of microseconds.  A block takes 3 for
+// its beginning and its end, and t for each 64 (128 columns) or 128 (32 columns) rows of the other side; a compute unit works on one of the former at a time or as fast on several,
+// on one or (narrow heads) two of the latter.  Blocks of a causal mask need half of their rows on average, the first ones all.  Measured, forward in small and in large blocks (us): 2000 tokens of 8 heads of
+// 64 22 / 28, 4000 causal 43 / 50, 2 x 1000 of 128 28 / 23, 8 x 197 of 12 heads of 64 11.4 / 7.8, 24 packed sequences of 16 heads of 80 267 / 75; fp32 2 x 1788 causal, 12 heads of 72, 183 / 276,
+// 4 x 1024, 8 heads of 64, 107 / 82.
+inline bool attn_wide(const dp_attention_desc &d, long long len, long long rows, long long mult, long long other)
 {
-    const long long blocks = d.kv_heads * attn_tiles(d.n, len, rows, mult, 128);
-    if (len * mult <= 32 || blocks < kFull) return false;
-    if (d.io_dtype == DP_BF16) return true;
-    const double rounds = blocks / 256.0;
-    return (d.left < 0) != (d.right < 0) ? 0.5 * rounds + 0.75 <= 0.65 * rounds + 0.2 : (double)((blocks + 255) / 256) <= 1.3 * rounds + 0.2;
+    if (len * mult <= 32) return false;
+    const bool bf = d.io_dtype == DP_BF16, causal = (d.left < 0) != (d.right < 0);
+    const int size = d.dim <= 64 ? 0 : d.dim <= 96 ? 1 : 2;
+    constexpr double t_wide[2][3] = {{4.8, 6.5, 9.4}, {0.72, 0.9, 1.09}}, t_few[2][3] = {{2.9, 4.2, 5.9}, {0.92, 1.05, 1.19}};
+    const double wide = d.kv_heads * (double)attn_tiles(d.n, len, rows, mult, 128) / 256, few = d.kv_heads * (double)attn_tiles(d.n, len, rows, mult, 32) / (bf && size == 0 ? 512 : 256);
+    const auto whole = [](double x) { return (double)(long long)(x + 0.999); };
+    const auto longest = [](double x) { return x > 1 ? x : 1; };
+    const double rounds_wide = longest(bf ? (causal ? 0.5 * wide + 0.25 : wide) : (causal ? 0.5 * wide + 0.75 : whole(wide))), rounds_few = longest(causal ? 0.5 * few + 0.25 : few);
+    return 3 + other / 64.0 * t_wide[bf][size] * rounds_wide <= 3 * whole(few) + other / 128.0 * t_few[bf][size] * rounds_few;
+}
+// rows of the other side that a block of `columns` sees, at most
+inline long long attn_seen(const dp_attention_desc &d, long long len, int columns)
+{
+    const long long window = d.left >= 0 && d.right >= 0 ? (long long)d.left + d.right + columns : len;
+    return window < len ? window : len;
 }
 // blocks of a call: where they are numbered by what there is, no more than that can be
 inline unsigned attn_blocks(const AttnArgs &a, const AttnSide &side, long long mult, int columns)

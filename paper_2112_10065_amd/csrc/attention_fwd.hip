@@ -267,11 +267,10 @@ long long rows_or(long long rows, long long dense) { return rows != 0 ? rows : d
 Form form_of(const dp_attention_desc &d)
 {
     const long long shared = d.heads / d.kv_heads, cols = d.q_len * shared, rows = rows_or(d.q_rows, (long long)d.n * d.q_len);
-    if (attn_wide(d, d.q_len, rows, shared)) return {4, 1, 0};
+    if (attn_wide(d, d.q_len, rows, shared, attn_seen(d, d.kv_len, 128 / (int)std::min<long long>(shared, 128)))) return {4, 1, 0};
     const long long blocks = std::max<long long>(1, d.kv_heads * attn_tiles(d.n, d.q_len, rows, shared, 32));
     constexpr int kt = 128;
-    long long span = d.kv_len;   // keys that a block looks at
-    if (d.left >= 0 && d.right >= 0) span = std::min<long long>(span, (long long)d.left + d.right + 32);
+    const long long span = attn_seen(d, d.kv_len, 32);   // keys that a block looks at
     const long long most = std::min<long long>(kMaxSplits, (span + 4 * kt - 1) / (4 * kt));   // four tiles at least: the join takes as long as two
     // A single token's columns fit one block, which waits for memory most of the time: four rounds of blocks at least.  Others compute, and are split only to give every compute unit work
     // (2000 causal tokens fp32, 8 heads of 128 over 2, 500 blocks: 221 us in four parts).
