@@ -258,12 +258,12 @@ template <typename T> __global__ __launch_bounds__(kJoinThreads) void k_attentio
 
 const char *const kName = "attention";
 
-struct Form { int cw, splits, split_keys; };   // wavefronts side by side in a block; blocks that the keys of a column are dealt out to
-
-// Four wavefronts side by side share the copies of a tile of keys; where such blocks would not fill the card, or a block's columns would not be there, the four of them take
-// the same 32 columns and share the keys, and if that leaves compute units without work too, blocks share them.
 long long rows_or(long long rows, long long dense) { return rows != 0 ? rows : dense; }
 
+struct Form { int cw, splits, split_keys; };   // wavefronts side by side in a block; blocks that the keys of a column are dealt out to
+
+// Four wavefronts side by side share the copies of a tile of keys; where that takes longer (attn_wide) the four of them take the same 32 columns and share the keys, and if that leaves
+// compute units without work too, blocks share them.
 Form form_of(const dp_attention_desc &d)
 {
     const long long shared = d.heads / d.kv_heads, cols = d.q_len * shared, rows = rows_or(d.q_rows, (long long)d.n * d.q_len);
@@ -273,7 +273,7 @@ Form form_of(const dp_attention_desc &d)
     const long long span = attn_seen(d, d.kv_len, 32);   // keys that a block looks at
     const long long most = std::min<long long>(kMaxSplits, (span + 4 * kt - 1) / (4 * kt));   // four tiles at least: the join takes as long as two
     // A single token's columns fit one block, which waits for memory most of the time: four rounds of blocks at least.  Others compute, and are split only to give every compute unit work
-    // (2000 causal tokens fp32, 8 heads of 128 over 2, 500 blocks: 221 us in four parts).
+    // (2000 causal tokens fp32, 8 heads of 128 over 2, 500 blocks: 167 us, 221 in four parts).
     const long long want = std::min<long long>(most, (cols <= 32 ? 2048 : 512) / blocks);
     if (want < 2) return {1, 1, 0};
     // whole tiles; a window is anywhere in the sequence, so its split counts over all keys
