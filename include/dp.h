@@ -437,7 +437,7 @@ dp_status dp_qk_rotary_bwd(const dp_qk_rotary_desc *desc, const void *q, const v
  * o, dout: o_stride; dq, dk, dv: the strides of q, k, v.  lse: fp32 [heads][q_rows].
  * Arithmetic: products on the matrix cores with fp32 sums; softmax, its statistics and all sums fp32.  With DP_BF16 the probabilities (and in the
  * backward pass p and dp's product with it) are rounded to bf16 as operands of the second product.  A value or gradient row that is NaN or infinite
- * may make NaN also of queries that do not see it, if they share a tile with ones that do; unused rows never do.
+ * may make NaN also of queries and keys that do not see it, if they share a tile with ones that do; unused rows never do.
  * Results may not overlap inputs or each other (dq, dk and dv may lie side by side in the same rows).  Tensors may hold more than 2^31 elements here. */
 typedef struct {
     int32_t n, q_len, kv_len;   /* n, q_len, kv_len >= 0 */
@@ -445,7 +445,7 @@ typedef struct {
     int32_t dim;                /* a multiple of 8, at most 128 */
     int32_t left, right;        /* >= -1 */
     int32_t io_dtype;
-    float scale;                /* > 0; 0 stands for 1/sqrt(dim) */
+    float scale;                /* > 0, at most 2^126; 0 stands for 1/sqrt(dim) */
     int64_t q_rows, kv_rows;    /* rows in memory; 0 stands for n * q_len, n * kv_len */
     int64_t q_stride, k_stride, v_stride, o_stride;
 } dp_attention_desc;

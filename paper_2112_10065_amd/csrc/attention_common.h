@@ -472,6 +472,7 @@ inline long long attn_tiles(long long n, long long len, long long rows, long lon
 inline bool attn_wide(const dp_attention_desc &d, long long len, long long rows, long long mult, long long other)
 {
     if (len * mult <= 32) return false;
+    if ((double)d.n * d.kv_heads * (double)(len * mult / 32 + 1) >= (double)(1 << 23)) return true;   // a launch has fewer than 2^32 threads
     const bool bf = d.io_dtype == DP_BF16, causal = (d.left < 0) != (d.right < 0);
     const int size = d.dim <= 64 ? 0 : d.dim <= 96 ? 1 : 2;
     constexpr double t_wide[2][3] = {{4.8, 6.5, 9.4}, {0.72, 0.9, 1.09}}, t_few[2][3] = {{2.9, 4.2, 5.9}, {0.92, 1.05, 1.19}};

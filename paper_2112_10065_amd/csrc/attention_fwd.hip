@@ -310,7 +310,7 @@ dp_status attn_check(const dp_attention_desc *desc, const dp_attention_seqs *seq
     if (d.heads < 1 || d.kv_heads < 1 || d.heads % d.kv_heads != 0) { dp_set_error("%s: %d heads of queries, %d of keys", kName, d.heads, d.kv_heads); return DP_ERR_BAD_DESC; }
     if (d.dim < 8 || d.dim > 128 || d.dim % 8 != 0) { dp_set_error("%s: dim %d is not a multiple of 8 up to 128", kName, d.dim); return DP_ERR_BAD_DESC; }
     if (d.left < -1 || d.right < -1) { dp_set_error("%s: window %d, %d", kName, d.left, d.right); return DP_ERR_BAD_DESC; }
-    if (!(d.scale >= 0.f && d.scale < INFINITY)) { dp_set_error("%s: scale must be above 0 (0: 1/sqrt(dim))", kName); return DP_ERR_BAD_DESC; }
+    if (!(d.scale >= 0.f && d.scale <= 0x1p126f)) { dp_set_error("%s: scale must be above 0 and at most 2^126 (0: 1/sqrt(dim))", kName); return DP_ERR_BAD_DESC; }
     const long long wq = (long long)d.heads * d.dim, wk = (long long)d.kv_heads * d.dim;
     const int vec = d.io_dtype == DP_BF16 ? 8 : 4;
     const long long strides[] = {d.q_stride, d.o_stride, d.k_stride, d.v_stride}, widths[] = {wq, wq, wk, wk};
@@ -336,7 +336,7 @@ dp_status attn_check(const dp_attention_desc *desc, const dp_attention_seqs *seq
         dp_set_error("%s: %lld and %lld rows do not hold the sequences, or are more than 2^31", kName, (long long)d.q_rows, (long long)d.kv_rows);
         return DP_ERR_BAD_DESC;
     }
-    // a launch has fewer than 2^32 threads, 512 to a block at the most
+    // a launch has fewer than 2^32 threads, 512 to a block at the most (blocks of 32 columns: attn_wide)
     const double shared = d.heads / d.kv_heads, most = (double)std::max<double>(d.q_len * shared, d.kv_len);
     if (d.q_len * shared >= (double)(1 << 30) || (double)d.n * d.kv_heads * (std::floor(most / 128) + 1) >= (double)(1 << 23)) {
         dp_set_error("%s: too many sequences, heads and tokens for one launch", kName);

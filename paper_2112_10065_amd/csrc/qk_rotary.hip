@@ -9,8 +9,8 @@
 // while they go over the heads, several heads at a time.
 //
 // 16 x 28 x 28 tokens, 32 heads of 128 bf16, backward: 67 us for 308 MB (4.6 TB/s; a large copy reaches 4.8-5.2) and 4.5 for the sums of dgamma.  32 x 14 x 14 tokens, 24 heads of 64,
-// forward: 14 us for 39 MB: a wavefront has one row, and a launch's start and a row's waits (its place, then one turn of heads after the other) are half of it.  Four turns under
-// way at once took 17, and 63 in the backward case.
+// forward: 14 us for 39 MB: a wavefront has one row, and a launch's start and a row's waits (its place, then one turn of heads after the other) are half of it.  With four
+// turns under way at once (backward two) they took 17 and 63.
 #include "vec_common.h"
 #include <algorithm>
 

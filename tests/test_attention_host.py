@@ -109,7 +109,7 @@ def test_attention_refusals(dp):
     assert fwd(lse=A + 2) == fwd(ws=A + 8) == dp.DP_ERR_BAD_DESC
     assert fwd(d=long, ws=None) == fwd(d=long, nbytes=split - 1) == bwd(nbytes=back - 1) == bwd(ws=None) == dp.DP_ERR_WORKSPACE
     for bad in (dict(n=-1), dict(q_len=-1), dict(kv_len=-1), dict(q_len=1 << 29), dict(heads=0), dict(kv_heads=0), dict(heads=5), dict(dim=4), dict(dim=20), dict(dim=136),
-                dict(left=-2), dict(right=-2), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(q_stride=64), dict(q_stride=132), dict(o_stride=-128),
+                dict(left=-2), dict(right=-2), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=2e38), dict(q_stride=64), dict(q_stride=132), dict(o_stride=-128),
                 dict(v_stride=60), dict(k_stride=1 << 23), dict(q_rows=9), dict(kv_rows=13), dict(q_rows=-1), dict(kv_rows=1 << 32), dict(n=1 << 16, q_len=1 << 20),
                 dict(n=1 << 30, q_len=1, kv_len=1), dict(n=1 << 22, q_len=1, kv_len=1), dict(n=1 << 12, q_len=1 << 17), dict(q_len=1 << 28, heads=16)):
         assert fwd(d=att(dp, **bad)) == bwd(d=att(dp, **bad)) == dp.DP_ERR_BAD_DESC, bad

@@ -355,6 +355,13 @@ def test_many_short_sequences(env, n):
     Case(env, n, 1, 3000, 2, 1, 64, -1, 0, kv_side=r.integers(0, 3001, n).tolist()).check()
 
 
+def test_a_far_longer_longest_sequence(env):
+    """What may be the longest is millions of rows, none is: blocks of 32 columns for each of them would be more than a launch has."""
+    r = np.random.default_rng(5)
+    lq, lk = r.integers(0, 50, 300).tolist(), r.integers(0, 60, 300).tolist()
+    Case(env, 300, 3_500_000, 3_500_000, 1, 1, 32, -1, 0, q_side=("packed", lq, 1, 2), kv_side=("packed", lk, 0, 3)).check(True, True)
+
+
 def test_tokens_one_by_one_give_the_whole(env):
     """A sequence taken token by token over its growing cache: the causal result's rows, whatever lies behind the cache's end."""
     dp, _ = env
