@@ -27,7 +27,7 @@ template <typename T, int DP, int CW> __global__ __launch_bounds__(256, CW == 4 
     constexpr int ROOM = 2 * STAGES * BYTES > (RW > 1 ? 4 * DB * 4096 : 0) ? 2 * STAGES * BYTES : 4 * DB * 4096;
     __shared__ alignas(1024) char s_tiles[ROOM];   // K and V of each stage
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, wc = wave % CW, wr = wave / CW;
-    const Item item = item_of<COLS, false, true>(a, a.q, a.shared, blockIdx.x, gridDim.x);
+    const Item item = item_of<COLS, false, true, CW == 4 && sizeof(T) == 2 ? 2 : 1>(a, a.q, a.shared, blockIdx.x, gridDim.x);
     if (!item.any) return;
     const int b = item.b, hk = item.hk, col0 = item.tile * COLS;
     const Rows rq = rows_of(a.q, b), rk = rows_of(a.kv, b);
@@ -179,11 +179,14 @@ DEVFN void hide(f32x16 &s, const Seen &w, int t, int half)
         if ((unsigned)(t + 8 * (v >> 2) + 4 * half + (v & 3) - w.seen0) >= w.seen) s[v] = -INFINITY;
 }
 
+// With SPLIT: where part `part` of `parts` of `total` tiles begins.
+template <bool SPLIT> DEVFN int part_of(int total, int part, int parts) { return SPLIT ? (int)((long long)total * part / parts) : 0; }
+
 // dk and dv for 128 keys of wide heads.  Both sums and the operands k and v take more registers than each of two wavefronts on a SIMD has, and one alone has nothing to run
 // beside its exponentials; so two share 32 keys.  Of each tile of 64 queries each makes p and ds for its half of the queries, and then one adds up dk, the other dv, over all of
 // them: what the other wavefront's half needs of p or ds goes through LDS, already rounded, lane by lane.  The sums are one tile behind the products, so that
 // a wavefront's exponentials lie between matrix products that do not wait for them.
-template <int DP> __global__ __launch_bounds__(512, 2) void k_attention_dkv(AttnArgs a)
+template <int DP, bool SPLIT> __global__ __launch_bounds__(512, 2) void k_attention_dkv(AttnArgs a)
 {
     using T = bf16_t;
     using L = Tile<T, DP>;
@@ -193,7 +196,8 @@ template <int DP> __global__ __launch_bounds__(512, 2) void k_attention_dkv(Attn
     __shared__ alignas(16) float s_stats[STAGES][2][QT];         // lse2 and -delta
     __shared__ alignas(16) u32x4 s_packs[2][8][2][64];           // [tile][wavefront][slice][lane]: the first's p, the second's ds
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, pair = wave & 3, second = wave >> 2;
-    const Item item = item_of<COLS, false, false>(a, a.kv, 1, blockIdx.x, gridDim.x);
+    const int blocks = SPLIT ? gridDim.x / a.kv_parts : gridDim.x, part = SPLIT ? blockIdx.x / blocks : 0;
+    const Item item = item_of<COLS, false, false>(a, a.kv, 1, SPLIT ? blockIdx.x % blocks : blockIdx.x, blocks);
     if (!item.any) return;
     const int b = item.b, hk = item.hk, col0 = item.tile * COLS;
     const Rows rq = rows_of(a.q, b), rk = rows_of(a.kv, b);
@@ -205,23 +209,25 @@ template <int DP> __global__ __launch_bounds__(512, 2) void k_attention_dkv(Attn
 
     f32x16 sum[DB];   // the first's dk, the second's dv
     clear(sum);
-    if (w.count > 0) {
+    // a part may have nothing to add up
+    if (w.count > 0 && (!SPLIT || part_of<SPLIT>((w.count + QT - 1) / QT * a.shared, part + 1, a.kv_parts) > part_of<SPLIT>((w.count + QT - 1) / QT * a.shared, part, a.kv_parts))) {
         const unsigned tiles_q = lds_offset(s_tiles), tiles_g = tiles_q + STAGES * BYTES, stats = lds_offset(s_stats), packs = lds_offset(s_packs) + lane * 16;
         const long long stride = second ? a.o_stride : a.q_stride;
-        const T *from = reinterpret_cast<const T *>(second ? a.dout : a.qp);
+        const T *source = reinterpret_cast<const T *>(second ? a.dout : a.qp);
         const float *stat_from = second ? a.delta : a.lse2;
         Copy copy;
         copy.init(threadIdx.x & 255, a.dim, stride);
         TileLane<T, DP> tl;
         tl.init(lane);
-        const int tiles = (w.count + QT - 1) / QT, all = tiles * a.shared;
-        // tile n: queries first + QT (n % tiles) ... of the n / tiles-th head; rows behind the last query arrive as zeros, also their statistics: nothing is added then.
+        // tiles of all heads, one head's behind the other's; with SPLIT a part of them
+        const int tiles = (w.count + QT - 1) / QT, total = tiles * a.shared, from = part_of<SPLIT>(total, part, a.kv_parts), all = SPLIT ? part_of<SPLIT>(total, part + 1, a.kv_parts) - from : total;
+        // tile n: queries first + QT (n % tiles) ... of the n / tiles-th head, n from `from` on; rows behind the last query arrive as zeros, also their statistics: nothing is added then.
         // The first wavefronts copy q and lse2, the second dout and -delta.
-        int ih = hk * a.shared, it = 0, slot_in = 0;
+        int ih = hk * a.shared + from / tiles, it = from % tiles * QT, slot_in = 0;
         auto issue = [&] {
             const long long at = rq.first + w.first + it;
             const int rows = w.count - it;
-            copy.issue(from + at * stride + (long long)ih * a.dim, rows, a.dim, stride, (second ? tiles_g : tiles_q) + slot_in * BYTES, pair);
+            copy.issue(source + at * stride + (long long)ih * a.dim, rows, a.dim, stride, (second ? tiles_g : tiles_q) + slot_in * BYTES, pair);
             if (pair == 0) {
                 const auto r = make_rsrc(stat_from + (long long)ih * a.q.rows + at, (unsigned)min(rows, QT) * 4);
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void)(size_t)(stats + (slot_in * 2 + second) * QT * 4), 4, lane * 4, 0, 0, 0);
@@ -235,7 +241,7 @@ template <int DP> __global__ __launch_bounds__(512, 2) void k_attention_dkv(Attn
         load_column<T, DP>(reinterpret_cast<const T *>(a.kp) + row * a.k_stride + (long long)hk * a.dim, on, a.dim, half, kc);
         load_column<T, DP>(reinterpret_cast<const T *>(a.vp) + row * a.v_stride + (long long)hk * a.dim, on, a.dim, half, vc);
         u32x4 mine[2];   // ds (the first's) or p (the second's) of the own half of the tile before
-        int t = 0, slot = 0, before = 0;
+        int t = from % tiles * QT, slot = 0, before = 0;
         f32x16 s, dp;
         u32x4 l2[4];     // of rows 8 g + 4 half ... of the own half
         const auto arrive = [&](int n) {   // tile n, and the packs of tile n - 1; tile n - 2 is done with: its room takes tile n + 1
@@ -311,7 +317,9 @@ template <int DP> __global__ __launch_bounds__(512, 2) void k_attention_dkv(Attn
     }
     if (!own) return;
     if (!on) clear(sum);
-    if (second) store_column<T, DB>(sum, 1.f, reinterpret_cast<T *>(a.dv) + row * a.v_stride + (long long)hk * a.dim, a.dim, half);
+    if constexpr (SPLIT) {
+        store_column<float, DB>(sum, second ? 1.f : a.scale, (second ? a.part_dv : a.part_dk) + ((part * a.kv.rows + row) * a.kv_heads + hk) * a.dim, a.dim, half);
+    } else if (second) store_column<T, DB>(sum, 1.f, reinterpret_cast<T *>(a.dv) + row * a.v_stride + (long long)hk * a.dim, a.dim, half);
     else store_column<T, DB>(sum, a.scale, reinterpret_cast<T *>(a.dk) + row * a.k_stride + (long long)hk * a.dim, a.dim, half);
 }
 
@@ -326,8 +334,8 @@ template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(2
     __shared__ alignas(1024) char s_tiles[ROOM];              // q and dout of each stage
     __shared__ alignas(16) float s_stats[STAGES][2][SIDE];    // lse2 and delta
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int part = SPLIT ? blockIdx.x % a.kv_parts : 0;
-    const Item item = SPLIT ? item_of<COLS, false, false>(a, a.kv, 1, blockIdx.x / a.kv_parts, gridDim.x / a.kv_parts) : item_of<COLS, false, false>(a, a.kv, 1, blockIdx.x, gridDim.x);
+    const int blocks = SPLIT ? gridDim.x / a.kv_parts : gridDim.x, part = SPLIT ? blockIdx.x / blocks : 0;
+    const Item item = item_of<COLS, false, false>(a, a.kv, 1, SPLIT ? blockIdx.x % blocks : blockIdx.x, blocks);
     if (!item.any) return;
     const int b = item.b, hk = item.hk, col0 = item.tile * COLS, wcol = col0 + wave % CW * 32, wr = wave / CW;
     const Rows rq = rows_of(a.q, b), rk = rows_of(a.kv, b);
@@ -349,8 +357,7 @@ template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(2
         TileLane<T, DP> tl;
         tl.init(lane);
         const int tiles = (w.count + QT - 1) / QT, total = tiles * a.shared;
-        // with SPLIT a part of the tiles, all heads' one behind the other
-        const int from = SPLIT ? (int)((long long)total * part / a.kv_parts) : 0, all = SPLIT ? (int)((long long)total * (part + 1) / a.kv_parts) - from : total;
+        const int from = part_of<SPLIT>(total, part, a.kv_parts), all = SPLIT ? part_of<SPLIT>(total, part + 1, a.kv_parts) - from : total;   // a part of the tiles, all heads' one behind the other
         int ih = hk * a.shared + from / tiles, it = from % tiles * QT, slot_in = 0;
         auto issue = [&] {
             const long long at = rq.first + w.first + it;
@@ -464,33 +471,63 @@ template <typename T> __global__ __launch_bounds__(kSumThreads) void k_attention
     }
 }
 
-// If the blocks of dk and dv are of 32 columns and few, how many share the queries: no more than there are compute units, and enough tiles for
-// each to be worth the third kernel (2000 causal tokens, 8 heads of 128 over 2: 145 us whole, 111 in halves, fp32 830 and 530).
-int parts_of(const dp_attention_desc &d)
+// Blocks of dk and dv: of 128 columns or of 32, and how many share the queries of a column.
+struct DkvForm { bool wide; int parts; };
+
+// As attn_wide says, unless an estimate of microseconds finds that the queries dealt out to several blocks take less, the sums' kernel included; where a causal mask makes blocks of different lengths that evens
+// them out too.  Measured whole and so (us): causal, 8192 tokens, 8 heads of 128 over 2 491 / 424, of 64 293 / 219, 4096 tokens, 32 heads of 128 over 8 435 / 376, 2000 tokens, 8 over 2 95 / 45, fp32
+// 4096 tokens 1198 / 750; all to all, 8192 tokens, 4 over 1 392 / 271.  Not: two sequences of 4096 tokens, 32 over 8, 525 / 662.
+DkvForm dkv_form(const dp_attention_desc &d)
 {
     const long long rows = d.kv_rows != 0 ? d.kv_rows : (long long)d.n * d.kv_len, shared = d.heads / d.kv_heads;
-    if (d.q_len == 0 || rows == 0 || attn_wide(d, d.kv_len, rows, 1, shared * attn_seen(d, d.q_len, 128))) return 1;
-    const long long tiles = shared * ((attn_seen(d, d.q_len, 32) + 127) / 128), blocks = std::max<long long>(1, d.kv_heads * attn_tiles(d.n, d.kv_len, rows, 1, 32));
-    return (int)std::max<long long>(1, std::min<long long>({tiles / (d.io_dtype == DP_BF16 ? 4 : 2), 256 / blocks, 16}));
+    const bool bf = d.io_dtype == DP_BF16, causal = (d.left < 0) != (d.right < 0);
+    const DkvForm plain = {attn_wide(d, d.kv_len, rows, 1, shared * attn_seen(d, d.q_len, 128)), 1};
+    if (d.q_len == 0 || rows == 0 || d.n > kMostRagged) return plain;
+    const int size = d.dim <= 64 ? 0 : d.dim <= 96 ? 1 : 2;
+    // of a tile, 64 rows to 128 columns or 128 to 32, on a busy card; on one whose compute units have a block of 128 columns each
+    constexpr double t_wide[2][3] = {{9.6, 13, 18.8}, {1.25, 1.8, 2}}, t_few[2][3] = {{5.1, 7.5, 9.3}, {1.14, 1.37, 1.55}}, t_alone[3] = {1.2, 1.4, 1.55};
+    const double sums = (double)rows * d.kv_heads * d.dim * 8 / 2.5e6;   // written, then read
+    DkvForm best = plain;
+    double limit = 0;
+    for (const bool wide : {plain.wide, !plain.wide}) {
+        if (wide && !plain.wide && (!bf || d.kv_len <= 32)) continue;
+        const long long tiles = wide ? (attn_seen(d, d.q_len, 128) + 63) / 64 : (attn_seen(d, d.q_len, 32) + 127) / 128, longest = tiles * shared;
+        const double blocks = (double)d.kv_heads * attn_tiles(d.n, d.kv_len, rows, 1, wide ? 128 : 32), t = wide ? t_wide[bf][size] : t_few[bf][size], alone = wide && bf ? t_alone[size] : t;
+        const double share = causal ? (tiles + 1) / (2.0 * tiles) : 1;   // of the longest block's tiles that a block has on average
+        for (int p = wide == plain.wide ? 1 : 2; p <= 16 && p <= longest && blocks * p <= 2048; ++p) {
+            // causal: what a unit has on average, and what the last blocks leave idle
+            const double busy = causal ? t * blocks * share / 256 + (p == 1 ? 0.1 : wide ? 0.4 : 0.5 * t) / p : t * (double)(long long)(blocks * p / 256 + 0.999) / p;
+            const double us = (8 + longest * std::max(alone / p, busy) + (p > 1 ? 4 + p * sums : 0)) * (p > 1 && blocks * p > 256 ? 1.03 : 1);
+            if (wide == plain.wide && p == 1) {
+                if (us < 25) return plain;
+                limit = 0.9 * us;
+            } else if (us < limit) {
+                limit = us;
+                best = {wide, p};
+            }
+        }
+        if (limit == 0) return plain;   // more blocks than need be
+    }
+    return best;
 }
 
 template <typename T, int DP> auto dkv_kernel(bool wide_one, bool split, int &threads)
 {
     threads = 256;
     if (!wide_one) return split ? k_attention_dkv_whole<T, DP, 1, true> : k_attention_dkv_whole<T, DP, 1, false>;
-    if constexpr (sizeof(T) == 4 || DP <= 96) return k_attention_dkv_whole<T, DP, 4, false>;
+    if constexpr (sizeof(T) == 4 || DP <= 96) return split ? k_attention_dkv_whole<T, DP, 4, true> : k_attention_dkv_whole<T, DP, 4, false>;
     else {
         threads = 512;
-        return k_attention_dkv<DP>;
+        return split ? k_attention_dkv<DP, true> : k_attention_dkv<DP, false>;
     }
 }
 
-template <typename T> void launch(const dp_attention_desc &d, AttnArgs &a, hipStream_t st)
+template <typename T> void launch(const dp_attention_desc &d, AttnArgs &a, bool wk, hipStream_t st)
 {
     for_dim(a.dim, [&](auto dc) {
         constexpr int DP = decltype(dc)::value;
         const long long qc = (long long)a.q.len * a.shared, kc = a.kv.len;
-        const bool wq = attn_wide(d, a.q.len, a.q.rows, a.shared, attn_seen(d, a.kv.len, std::max(1, 128 / a.shared))), wk = attn_wide(d, a.kv.len, a.kv.rows, 1, a.shared * attn_seen(d, a.q.len, 128));
+        const bool wq = attn_wide(d, a.q.len, a.q.rows, a.shared, attn_seen(d, a.kv.len, std::max(1, 128 / a.shared)));
         a.tiles = (int)((qc + (wq ? 127 : 31)) / (wq ? 128 : 32));
         if (a.tiles > 0 && a.q.rows > 0) hipLaunchKernelGGL((wq ? k_attention_dq<T, DP, 4> : k_attention_dq<T, DP, 1>), dim3(attn_blocks(a, a.q, a.shared, wq ? 128 : 32)), dim3(256), 0, st, a);
         a.tiles = (int)((kc + (wk ? 127 : 31)) / (wk ? 128 : 32));
@@ -510,15 +547,14 @@ size_t stat_bytes(const dp_attention_desc &d)
     return ((size_t)d.heads * rows * sizeof(float) + 15) / 16 * 16;
 }
 
-size_t sum_bytes(const dp_attention_desc &d)   // of dk's, or of dv's parts
+size_t sum_bytes(const dp_attention_desc &d, const DkvForm &f)   // of dk's, or of dv's parts
 {
-    const int parts = parts_of(d);
-    return parts == 1 ? 0 : (size_t)parts * (size_t)(d.kv_rows != 0 ? d.kv_rows : (long long)d.n * d.kv_len) * d.kv_heads * d.dim * sizeof(float);
+    return f.parts == 1 ? 0 : (size_t)f.parts * (size_t)(d.kv_rows != 0 ? d.kv_rows : (long long)d.n * d.kv_len) * d.kv_heads * d.dim * sizeof(float);
 }
 
 }  // namespace
 
-size_t attn_bwd_bytes(const dp_attention_desc &d) { return 2 * (stat_bytes(d) + sum_bytes(d)); }
+size_t attn_bwd_bytes(const dp_attention_desc &d) { return 2 * (stat_bytes(d) + sum_bytes(d, dkv_form(d))); }
 
 extern "C" dp_status dp_attention_bwd(const dp_attention_desc *desc, const void *q, const void *k, const void *v, const void *o, const void *dout,
                                       const float *lse, void *dq, void *dk, void *dv, const dp_attention_seqs *seqs, void *ws, size_t ws_bytes,
@@ -533,16 +569,17 @@ extern "C" dp_status dp_attention_bwd(const dp_attention_desc *desc, const void 
     if (!queries && !keys) return DP_OK;
     if (queries && (s = attn_pointers({q, o, dout, dq, lse}, nullptr, nullptr)) != DP_OK) return s;
     if (keys && (s = attn_pointers({k, v, dk, dv}, nullptr, nullptr)) != DP_OK) return s;
+    const DkvForm f = dkv_form(d);
     // dk and dv are made behind dq, from all inputs but o
-    if ((s = attn_apart({queries ? dq : nullptr, keys ? dk : nullptr, keys ? dv : nullptr}, {q, k, v, o, dout, lse})) != DP_OK || (s = attn_pointers({}, nullptr, ws)) != DP_OK || (s = attn_workspace(attn_bwd_bytes(d), ws, ws_bytes)) != DP_OK) return s;
+    if ((s = attn_apart({queries ? dq : nullptr, keys ? dk : nullptr, keys ? dv : nullptr}, {q, k, v, o, dout, lse})) != DP_OK || (s = attn_pointers({}, nullptr, ws)) != DP_OK || (s = attn_workspace(2 * (stat_bytes(d) + sum_bytes(d, f)), ws, ws_bytes)) != DP_OK) return s;
     a.qp = q; a.kp = k; a.vp = v; a.op_in = o; a.dout = dout; a.lse_in = lse;
     a.dq = dq; a.dk = dk; a.dv = dv;
     a.lse2 = (float *)ws;
     a.delta = (float *)((char *)ws + stat_bytes(d));
-    a.kv_parts = parts_of(d);
+    a.kv_parts = f.parts;
     a.part_dk = (float *)((char *)ws + 2 * stat_bytes(d));
-    a.part_dv = (float *)((char *)a.part_dk + sum_bytes(d));
-    if (d.io_dtype == DP_BF16) launch<bf16_t>(d, a, (hipStream_t)hip_stream);
-    else launch<float>(d, a, (hipStream_t)hip_stream);
+    a.part_dv = (float *)((char *)a.part_dk + sum_bytes(d, f));
+    if (d.io_dtype == DP_BF16) launch<bf16_t>(d, a, f.wide, (hipStream_t)hip_stream);
+    else launch<float>(d, a, f.wide, (hipStream_t)hip_stream);
     return attn_launched("attention's gradient");
 }

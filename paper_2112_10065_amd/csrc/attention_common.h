@@ -32,6 +32,7 @@ struct AttnArgs {
     float *lse2, *delta;                   // backward's workspace: lse log2(e) (+inf: sees nothing) and -sum dout o, [heads][q_rows]
     int tiles;                             // of a sequence and head of keys
     int splits, split_keys;                // forward: keys dealt out to so many blocks, split_keys each
+    bool causal;                           // a bound on one side alone: tiles of a sequence see more or fewer rows
     bool ragged;                           // lengths differ: blocks are numbered by the work there is
     float *part_o, *part_ml;               // [split][head][q_rows][dim] and [split][head][q_rows][2]
     int kv_parts;                          // backward: the queries of a block of keys dealt out to so many blocks,
@@ -73,16 +74,28 @@ DEVFN int prefix_sum(int v)   // over the lanes up to this one
     return v;
 }
 
+// The number of block `block` of `of` among the tiles of `groups` heads, one head's behind the other's, where tiles of a head take different times.  A contiguous eighth for each die
+// is as much work for all of them only if it holds whole heads; else as many dies as hold whole ones together take the tiles in turn.
+DEVFN int dealt(int block, int of, int groups)
+{
+    if (groups % 8 == 0) return logical_block(block, of);
+    const int dies = of % 8 != 0 ? 8 : groups % 4 == 0 ? 2 : groups % 2 == 0 ? 4 : 8, die = block & 7;
+    return die / dies * (of / 8 * dies) + (block >> 3) * dies + die % dies;
+}
+
 // The grid has room for sequences of the longest length.  Whole sequences: tile by tile, head by head, a contiguous eighth for each die, so that the tiles of one head read their
-// rows from one L2.  Lengths that differ: the same over the tiles that there are, counted by each block for itself (a lane to a sequence), since tiles of nothing, numbered
+// rows from one L2 (with a causal mask: dealt).  Lengths that differ: the same over the tiles that there are, counted by each block for itself (a lane to a sequence), since tiles of nothing, numbered
 // among the others, would leave some dies with much more work than others (9 sequences of up to 1500 of 4 heads of keys, dk and dv: 73 us, 53 this way).  Tiles that hold padding alone come last.
-// `mult` columns to a row of `side`; SPLIT: every part of the keys that a sequence has; LAST_FIRST: a causal mask makes a sequence's last tiles the longest.
+// `mult` columns to a row of `side`; SPLIT: every part of the keys that a sequence has; LAST_FIRST: a causal mask makes a sequence's last tiles the longest.  Where all blocks of such a call
+// are on the card at once, SLOTS to a compute unit, each die's second 32 are taken in reverse, so that a long one shares its unit with a short one (4096 causal tokens, 16 heads of 128: 105 -> 97 us
+// forward, dq 147 -> 136).
 constexpr int kMostRagged = 256;   // sequences: more of them are counted for longer than it helps
-template <int COLS, bool SPLIT, bool LAST_FIRST> DEVFN Item item_of(const AttnArgs &a, const AttnSide &side, int mult, int block, int of)
+template <int COLS, bool SPLIT, bool LAST_FIRST, int SLOTS = 1> DEVFN Item item_of(const AttnArgs &a, const AttnSide &side, int mult, int block, int of)
 {
     Item r;
     if (!a.ragged) {
-        int id = logical_block(block, of);
+        if (SLOTS > 1 && LAST_FIRST && of <= 256 * SLOTS && a.causal && (block & 256) != 0 && (block | 255) < of) block ^= 31 << 3;
+        int id = a.causal ? dealt(block, of, a.n * a.kv_heads) : logical_block(block, of);
         r.split = SPLIT ? id % a.splits : 0;
         if (SPLIT) id /= a.splits;
         const int hb = id / a.tiles;

@@ -34,7 +34,7 @@ template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(2
     __shared__ alignas(1024) char s_tiles[ROOM];   // K and V of each stage
     __shared__ float2 s_ml[RW > 1 ? 256 : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, wc = wave % CW, wr = wave / CW;
-    const Item item = item_of<COLS, SPLIT, true>(a, a.q, a.shared, blockIdx.x, gridDim.x);
+    const Item item = item_of<COLS, SPLIT, true, CW == 4 && sizeof(T) == 2 ? DP <= 96 ? 3 : 2 : 1>(a, a.q, a.shared, blockIdx.x, gridDim.x);
     if (!item.any) return;
     const int b = item.b, hk = item.hk, split = item.split;
     const int col0 = item.tile * COLS;
@@ -361,6 +361,7 @@ void attn_args(const dp_attention_desc &d, const dp_attention_seqs *seqs, AttnAr
     a.v_stride = d.v_stride != 0 ? d.v_stride : wk;
     a.o_stride = d.o_stride != 0 ? d.o_stride : wq;
     a.splits = 1;
+    a.causal = (d.left < 0) != (d.right < 0);
     a.ragged = seqs != nullptr && d.n <= kMostRagged && (seqs->q_starts != nullptr || seqs->kv_starts != nullptr || seqs->q_lens != nullptr || seqs->kv_lens != nullptr);
 }
 

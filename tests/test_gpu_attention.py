@@ -215,6 +215,23 @@ def test_queries_dealt_out(env, dim, bf16):
     Case(env, 3, 900, 70, 6, 1, dim, -1, 0, bf16, q_side=[900, 0, 130], kv_side=("packed", [70, 5, 33], 1, 2)).check(False, True)
 
 
+@pytest.mark.parametrize("dim", [48, 64, 96, 112, 128])
+def test_queries_dealt_out_to_wide_blocks(env, dim):
+    """Long sequences of few heads: dk and dv of 128 keys are sums over several blocks; a short sequence has fewer tiles of queries than there are blocks to share them."""
+    for c, packed in ((Case(env, 1, 1500, 1500, 8, 1, dim, -1, 0), False), (Case(env, 2, 1400, 1400, 6, 2, dim, -1, 0, q_side=[1400, 900]), False),
+                      (Case(env, 2, 2600, 2600, 4, 1, dim, q_side=("packed", [2600, 20], 1, 2), kv_side=("packed", [2600, 33], 0, 3)), True)):
+        assert c.dp.dp_attention_workspace_bytes(c.desc, c.dp.DP_PASS_DGRAD) > 2 * (4 * c.heads * c.q_rows + 16)
+        c.check(packed, packed)
+
+
+@pytest.mark.parametrize("kv_heads", [1, 2, 3, 4, 6, 8])
+def test_causal_tiles_dealt_to_dies(env, kv_heads):
+    """Whole sequences whose tiles are numbered by how many heads there are, and whose number may be a multiple of eight or not."""
+    for length in (1024, 1100):
+        Case(env, 1, length, length, 2 * kv_heads, kv_heads, 64, -1, 0).check()
+    Case(env, 2, 520, 700, 2 * kv_heads, kv_heads, 128, -1, 0).check()
+
+
 @pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
 @pytest.mark.parametrize("mask", [(-1, -1), (-1, 0), (50, 9)], ids=str)
 @pytest.mark.parametrize("dim", [24, 40, 64, 72, 96, 104, 128])
