@@ -75,7 +75,8 @@ DEVFN int prefix_sum(int v)   // over the lanes up to this one
 }
 
 // The number of block `block` of `of` among the tiles of `groups` heads, one head's behind the other's, where tiles of a head take different times.  A contiguous eighth for each die
-// is as much work for all of them only if it holds whole heads; else as many dies as hold whole ones together take the tiles in turn.
+// is as much work for all of them only if it holds whole heads; else as many dies as hold whole ones together take the tiles in turn (8192 causal tokens, 8 heads of 128 over 2: forward
+// 226 -> 178 us, dq 319 -> 242, dk and dv 695 -> 480).
 DEVFN int dealt(int block, int of, int groups)
 {
     if (groups % 8 == 0) return logical_block(block, of);

@@ -273,7 +273,7 @@ Form form_of(const dp_attention_desc &d)
     const long long span = attn_seen(d, d.kv_len, 32);   // keys that a block looks at
     const long long most = std::min<long long>(kMaxSplits, (span + 4 * kt - 1) / (4 * kt));   // four tiles at least: the join takes as long as two
     // A single token's columns fit one block, which waits for memory most of the time: four rounds of blocks at least.  Others compute, and are split only to give every compute unit work
-    // (2000 causal tokens fp32, 8 heads of 128 over 2, 500 blocks: 167 us, 221 in four parts).
+    // (2000 causal tokens fp32, 8 heads of 128 over 2, 500 blocks: 113 us, 205 in four parts; bf16 33 and 53).
     const long long want = std::min<long long>(most, (cols <= 32 ? 2048 : 512) / blocks);
     if (want < 2) return {1, 1, 0};
     // whole tiles; a window is anywhere in the sequence, so its split counts over all keys
