@@ -370,15 +370,31 @@ def _elsewhere(t):
     raise ValueError(f"a tensor is on {t.device}, not on the current GPU")
 
 
-def _ptrs(*tensors):
-    """Addresses of tensors that a kernel reads or writes: a kernel of the current device would fault on memory of the host or of another one."""
+def _types(kinds):
+    """What a call's tensors have to be, for each io_dtype: one letter each, i of the descriptor's type, f fp32, d float64; the kernel takes the latter two's elements one behind the other."""
+    return {io: [(t if k == "i" else torch.float32 if k == "f" else torch.float64, k != "i") for k in kinds] for io, t in ((DP_F32, torch.float32), (DP_BF16, torch.bfloat16))}
+
+
+def _wrong(t, dtype):
+    if t.dtype is not dtype:
+        raise ValueError(f"a tensor is {t.dtype} where the call takes {dtype}")
+    raise ValueError("a tensor is not contiguous where the call takes its elements one behind the other")
+
+
+def _ptrs(tensors, types=None):
+    """Addresses of tensors that a kernel reads or writes: a kernel of the current device would fault on memory of the host or of another one, and would read past the end of a
+    tensor of a smaller type.  types: none are looked at."""
     device = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else None
     out = []
-    for t in tensors:
+    for t, want in zip(tensors, types or [None] * len(tensors)):
         if t is not None:
             try:
                 if t.get_device() != device:
                     _elsewhere(t)
+                if want is not None:
+                    dtype, flat = want
+                    if t.dtype is not dtype or flat and not t.is_contiguous():
+                        _wrong(t, dtype)
                 t = t.data_ptr()
             except AttributeError:   # an address as it is
                 pass
@@ -386,8 +402,15 @@ def _ptrs(*tensors):
     return out
 
 
+def _typed(desc, types, *tensors):
+    return _ptrs(tensors, types.get(getattr(desc, "io_dtype", None)))
+
+
 def _ws_on(ws):
-    return (None, 0) if ws is None else (_ptrs(ws)[0], ws.nbytes)
+    return (None, 0) if ws is None else (_ptrs((ws,))[0], ws.nbytes)
+
+
+_ROTARY_FWD, _ROTARY_BWD, _ATTENTION_FWD, _ATTENTION_BWD = map(_types, ("iifffdii", "iifffdiiiiff", "iiiif", "iiiiifiii"))
 
 
 def qk_rotary_desc(rows, heads, kv_heads, dim, pairs, io_dtype=DP_BF16, flags=0, eps=1e-6, q_stride=0, k_stride=0, q_out_stride=0, k_out_stride=0,
@@ -403,12 +426,12 @@ def dp_qk_rotary_workspace_bytes(desc, pass_):
 
 
 def dp_qk_rotary_fwd(desc, q, k, gamma_q, gamma_k, pos, freq, q_out, k_out, stream=None):
-    """pos: fp32 [rows, axes]; freq: float64 [sum of pairs]."""
-    _check(lib.dp_qk_rotary_fwd(desc, *_ptrs(q, k, gamma_q, gamma_k, pos, freq, q_out, k_out), _stream(stream)))
+    """pos: fp32 [rows, axes]; freq: float64 [sum of pairs].  Tensors of another type than the call takes are refused, here and below."""
+    _check(lib.dp_qk_rotary_fwd(desc, *_typed(desc, _ROTARY_FWD, q, k, gamma_q, gamma_k, pos, freq, q_out, k_out), _stream(stream)))
 
 
 def dp_qk_rotary_bwd(desc, q, k, gamma_q, gamma_k, pos, freq, dq_out, dk_out, dq, dk, dgamma_q=None, dgamma_k=None, ws=None, stream=None):
-    _check(lib.dp_qk_rotary_bwd(desc, *_ptrs(q, k, gamma_q, gamma_k, pos, freq, dq_out, dk_out, dq, dk, dgamma_q, dgamma_k), *_ws_on(ws), _stream(stream)))
+    _check(lib.dp_qk_rotary_bwd(desc, *_typed(desc, _ROTARY_BWD, q, k, gamma_q, gamma_k, pos, freq, dq_out, dk_out, dq, dk, dgamma_q, dgamma_k), *_ws_on(ws), _stream(stream)))
 
 
 def attention_desc(n, q_len, kv_len, heads, kv_heads, dim, io_dtype=DP_BF16, left=-1, right=-1, scale=0.0, q_rows=0, kv_rows=0, q_stride=0, k_stride=0,
@@ -421,7 +444,7 @@ def attention_seqs(q_starts=None, kv_starts=None, q_lens=None, kv_lens=None):
     for name, t in (("q_starts", q_starts), ("kv_starts", kv_starts), ("q_lens", q_lens), ("kv_lens", kv_lens)):
         if isinstance(t, torch.Tensor) and (t.dtype != torch.int32 or not t.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous int32 tensor")
-    seqs = dp_attention_seqs(*_ptrs(q_starts, kv_starts, q_lens, kv_lens))
+    seqs = dp_attention_seqs(*_ptrs((q_starts, kv_starts, q_lens, kv_lens)))
     seqs.tensors = (q_starts, kv_starts, q_lens, kv_lens)
     return seqs
 
@@ -431,12 +454,11 @@ def dp_attention_workspace_bytes(desc, pass_):
 
 
 def dp_attention_fwd(desc, q, k, v, o, lse=None, seqs=None, ws=None, stream=None):
-    _check(lib.dp_attention_fwd(desc, *_ptrs(q, k, v, o, lse), seqs, *_ws_on(ws), _stream(stream)))
+    _check(lib.dp_attention_fwd(desc, *_typed(desc, _ATTENTION_FWD, q, k, v, o, lse), seqs, *_ws_on(ws), _stream(stream)))
 
 
 def dp_attention_bwd(desc, q, k, v, o, dout, lse, dq, dk, dv, seqs=None, ws=None, stream=None):
-    _check(lib.dp_attention_bwd(desc, *_ptrs(q, k, v, o, dout, lse, dq, dk, dv), seqs, *_ws_on(ws),
-                                _stream(stream)))
+    _check(lib.dp_attention_bwd(desc, *_typed(desc, _ATTENTION_BWD, q, k, v, o, dout, lse, dq, dk, dv), seqs, *_ws_on(ws), _stream(stream)))
 
 
 def _doubles(rows, n):

@@ -144,6 +144,47 @@ def test_tensors_of_the_host_are_refused(dp):
         dp.dp_qk_rotary_bwd(rot(dp), A, A, None, None, A, A, A, A, A, A, dgamma_q=t)
 
 
+class OnGpu:
+    """A tensor that says it is on the current GPU; calls without rows look at its type alone."""
+
+    def __init__(self, t):
+        self.t, self.dtype, self.nbytes = t, t.dtype, t.nbytes
+
+    def get_device(self):
+        import torch
+        return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else None
+
+    def data_ptr(self):
+        return A
+
+    def is_contiguous(self):
+        return self.t.is_contiguous()
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+def test_tensors_of_another_type_are_refused(dp, bf16):
+    """A kernel would read past the end of a smaller type's memory, or other numbers than are there."""
+    import torch
+    io, other = (torch.bfloat16, torch.float32) if bf16 else (torch.float32, torch.bfloat16)
+    made = lambda t: OnGpu(torch.zeros(64, dtype=t))   # noqa: E731
+    x, f32, f64 = made(io), made(torch.float32), made(torch.float64)
+    empty = dict(io_dtype=dp.DP_BF16 if bf16 else dp.DP_F32)
+    calls = ((dp.dp_qk_rotary_fwd, rot(dp, rows=0, **empty), dict(q=x, k=x, gamma_q=f32, gamma_k=f32, pos=f32, freq=f64, q_out=x, k_out=x)),
+             (dp.dp_qk_rotary_bwd, rot(dp, rows=0, **empty), dict(q=x, k=x, gamma_q=f32, gamma_k=f32, pos=f32, freq=f64, dq_out=x, dk_out=x, dq=x, dk=x, dgamma_q=f32, dgamma_k=f32)),
+             (dp.dp_attention_fwd, att(dp, n=0, **empty), dict(q=x, k=x, v=x, o=x, lse=f32)),
+             (dp.dp_attention_bwd, att(dp, n=0, **empty), dict(q=x, k=x, v=x, o=x, dout=x, lse=f32, dq=x, dk=x, dv=x)))
+    for call, desc, args in calls:
+        if "dgamma_q" not in args:
+            call(desc, **args, stream=A)
+        for name, right in args.items():
+            for t in {torch.float16, torch.int64, torch.float64, torch.float32, other} - {right.dtype}:
+                with pytest.raises(ValueError, match=f"{t} where the call takes {right.dtype}"):
+                    call(desc, **{**args, name: made(t)}, stream=A)
+            if right is not x:
+                with pytest.raises(ValueError, match="not contiguous"):
+                    call(desc, **{**args, name: OnGpu(torch.zeros(128, dtype=right.dtype)[::2])}, stream=A)
+
+
 def test_attention_valid_calls(dp):
     no_gpu()
     lib = dp.lib
