@@ -560,7 +560,7 @@ extern "C" dp_status dp_attention_bwd(const dp_attention_desc *desc, const void 
                                       const float *lse, void *dq, void *dk, void *dv, const dp_attention_seqs *seqs, void *ws, size_t ws_bytes,
                                       void *hip_stream)
 {
-    dp_status s = attn_check(desc, seqs);
+    dp_status s = attn_check(desc, seqs, true);
     if (s != DP_OK) return s;
     const dp_attention_desc &d = *desc;
     AttnArgs a;

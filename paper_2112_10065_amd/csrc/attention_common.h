@@ -466,7 +466,7 @@ template <typename F> void for_dim(int dim, F &&f)
 }
 
 // attention_fwd.hip: what both passes check and take from the descriptor and the sequences
-dp_status attn_check(const dp_attention_desc *desc, const dp_attention_seqs *seqs);
+dp_status attn_check(const dp_attention_desc *desc, const dp_attention_seqs *seqs, bool gradient);
 void attn_args(const dp_attention_desc &d, const dp_attention_seqs *seqs, AttnArgs &a);
 dp_status attn_pointers(std::initializer_list<const void *> needed, const void *lse, const void *ws);
 dp_status attn_apart(std::initializer_list<const void *> results, std::initializer_list<const void *> inputs);

@@ -298,7 +298,7 @@ template <typename T> void launch(const AttnArgs &a, const Form &f, unsigned blo
 
 }  // namespace
 
-dp_status attn_check(const dp_attention_desc *desc, const dp_attention_seqs *seqs)
+dp_status attn_check(const dp_attention_desc *desc, const dp_attention_seqs *seqs, bool gradient)
 {
     if (desc == nullptr) { dp_set_error("%s: descriptor is NULL", kName); return DP_ERR_NULL; }
     const dp_attention_desc &d = *desc;
@@ -336,8 +336,8 @@ dp_status attn_check(const dp_attention_desc *desc, const dp_attention_seqs *seq
         dp_set_error("%s: %lld and %lld rows do not hold the sequences, or are more than 2^31", kName, (long long)d.q_rows, (long long)d.kv_rows);
         return DP_ERR_BAD_DESC;
     }
-    // a launch has fewer than 2^32 threads, 512 to a block at the most (blocks of 32 columns: attn_wide)
-    const double shared = d.heads / d.kv_heads, most = (double)std::max<double>(d.q_len * shared, d.kv_len);
+    // a launch has fewer than 2^32 threads, 512 to a block at the most (blocks of 32 columns: attn_wide); columns of queries, and of keys for dk and dv
+    const double shared = d.heads / d.kv_heads, most = std::max<double>(d.q_len * shared, gradient ? d.kv_len : 0);
     if (d.q_len * shared >= (double)(1 << 30) || (double)d.n * d.kv_heads * (std::floor(most / 128) + 1) >= (double)(1 << 23)) {
         dp_set_error("%s: too many sequences, heads and tokens for one launch", kName);
         return DP_ERR_BAD_DESC;
@@ -401,7 +401,7 @@ extern "C" size_t dp_attention_workspace_bytes(const dp_attention_desc *desc, in
     // packed rows may be fewer than n q_len: checked with starts
     const int32_t none = 0;
     const dp_attention_seqs packed = {&none, &none, nullptr, nullptr};
-    if (attn_check(desc, &packed) != DP_OK) return 0;
+    if (attn_check(desc, &packed, pass != DP_PASS_FWD) != DP_OK) return 0;
     const dp_attention_desc &d = *desc;
     if (pass == DP_PASS_FWD) return split_bytes(d, form_of(d));
     if (pass == DP_PASS_DGRAD) return attn_bwd_bytes(d);
@@ -411,7 +411,7 @@ extern "C" size_t dp_attention_workspace_bytes(const dp_attention_desc *desc, in
 extern "C" dp_status dp_attention_fwd(const dp_attention_desc *desc, const void *q, const void *k, const void *v, void *o, float *lse,
                                       const dp_attention_seqs *seqs, void *ws, size_t ws_bytes, void *hip_stream)
 {
-    dp_status s = attn_check(desc, seqs);
+    dp_status s = attn_check(desc, seqs, false);
     if (s != DP_OK) return s;
     const dp_attention_desc &d = *desc;
     AttnArgs a;

@@ -198,3 +198,13 @@ def test_attention_valid_calls(dp):
         need = dp.dp_attention_workspace_bytes(d, dp.DP_PASS_FWD), dp.dp_attention_workspace_bytes(d, dp.DP_PASS_DGRAD)
         assert lib.dp_attention_fwd(C.byref(d), A, A, A, A + 64, None, byref, A, need[0], None) == dp.DP_ERR_HIP
         assert lib.dp_attention_bwd(C.byref(d), A, A, A, A, A, A, A + 64, A + 128, A + 192, byref, A, need[1], None) == dp.DP_ERR_HIP
+
+
+def test_keys_limit_the_gradient_alone(dp):
+    """The forward pass launches nothing for each tile of keys: next tokens of many sequences, the longest of which may be very long."""
+    s = dp.attention_seqs(kv_starts=A)
+    for d in (att(dp, n=1024, q_len=1, kv_len=131072, heads=32, kv_heads=8, dim=128, kv_rows=1 << 20), att(dp, n=1000, q_len=1, kv_len=1 << 28, heads=16, kv_heads=16, kv_rows=5000)):
+        need = dp.dp_attention_workspace_bytes(d, dp.DP_PASS_FWD)
+        assert dp.lib.dp_attention_fwd(C.byref(d), A, A, None, A + 64, None, C.byref(s), A, need, None) == dp.DP_ERR_NULL     # what comes behind the limits
+        assert dp.lib.dp_attention_bwd(C.byref(d), A, A, None, A, A, A, A + 64, A + 128, A + 192, C.byref(s), A, 1 << 40, None) == dp.DP_ERR_BAD_DESC
+        assert dp.dp_attention_workspace_bytes(d, dp.DP_PASS_DGRAD) == 0

@@ -426,3 +426,12 @@ def test_gradient_against_differences(env):
             f(0.0)
             want = float((g[:, :w].double() * d.reshape(-1, w).double()).sum())
             assert abs(want - slope[0.01]) <= 2 * noise / 0.01 + abs(slope[0.02] - slope[0.01]), (i, want, slope, noise)
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+def test_next_tokens_of_very_many_sequences(env, bf16):
+    """More tiles of keys, if every sequence were as long as the longest may be, than a gradient's launch has blocks: the forward pass has none for them."""
+    r = np.random.default_rng(6)
+    c = Case(env, 1024, 1, 131072, 8, 8, 32, -1, 0, bf16, kv_side=("packed", r.integers(0, 9, 1024).tolist(), 1, 2))
+    assert c.dp.dp_attention_workspace_bytes(c.desc, c.dp.DP_PASS_DGRAD) == 0
+    c.check_forward(c.forward())
