@@ -31,7 +31,7 @@ struct AttnArgs {
     void *dq, *dk, *dv;
     float *lse2, *delta;                   // backward's workspace: lse log2(e) (+inf: sees nothing) and -sum dout o, [heads][q_rows]
     int tiles;                             // of a sequence and head of keys
-    int splits, split_keys;                // forward: keys dealt out to so many blocks, split_keys each
+    int splits, split_keys, span;          // forward: the keys that a block's queries see, at most span, dealt out to so many blocks, split_keys each
     bool causal;                           // a bound on one side alone: tiles of a sequence see more or fewer rows
     bool ragged;                           // lengths differ: blocks are numbered by the work there is
     float *part_o, *part_ml;               // [split][head][q_rows][dim] and [split][head][q_rows][2]
@@ -59,6 +59,9 @@ DEVFN Rows rows_of(const AttnSide &s, int b)
     }
     return r;
 }
+
+// Forward, split keys: how many parts the keys of a sequence have, where sequences differ.
+DEVFN int parts_of(const AttnArgs &a, int b) { return (min(rows_of(a.kv, b).used, a.span) + a.split_keys - 1) / a.split_keys; }
 
 // What a block does: sequence, head of keys, tile of columns and part of the keys.
 struct Item { int b, hk, tile, split; bool any; };
@@ -112,7 +115,7 @@ template <int COLS, bool SPLIT, bool LAST_FIRST, int SLOTS = 1> DEVFN Item item_
         parts = used = 0;
         if (b >= a.n) return 0;
         const Rows rows = rows_of(side, b);
-        parts = SPLIT ? (rows_of(a.kv, b).used + a.split_keys - 1) / a.split_keys : 1;
+        parts = SPLIT ? parts_of(a, b) : 1;
         const int own = (int)(((long long)rows.own * mult + COLS - 1) / COLS);
         used = SPLIT ? own : (int)(((long long)rows.used * mult + COLS - 1) / COLS);
         return (list == 0 ? used : own - used) * parts;

@@ -52,8 +52,8 @@ template <typename T, int DP, int CW, bool SPLIT> __global__ __launch_bounds__(2
         hi = min(rk.used, i1 + ahead + a.right + 1);
     }
     if (SPLIT) {
-        lo = max(lo, split * a.split_keys);
-        hi = min(hi, (split + 1) * a.split_keys);
+        lo += split * a.split_keys;
+        hi = min(hi, lo + a.split_keys);
     }
     const int first = lo, keys = max(0, hi - lo);
     const long long row = rq.first + i;
@@ -210,7 +210,7 @@ template <typename T> __global__ __launch_bounds__(kJoinThreads) void k_attentio
     const int col = (blockIdx.x % a.tiles) * (kJoinThreads / 32) + (threadIdx.x >> 5), i = col / a.shared, head = hk * a.shared + col % a.shared;
     const Rows rq = rows_of(a.q, b);
     const bool own = i < rq.own;
-    const int splits = a.ragged ? (rows_of(a.kv, b).used + a.split_keys - 1) / a.split_keys : a.splits;
+    const int splits = a.ragged ? parts_of(a, b) : a.splits;
     const long long row = rq.first + i, at = (long long)head * a.q.rows + row, step = (long long)a.heads * a.q.rows;
     float2 ml[2] = {{-INFINITY, 0.f}, {-INFINITY, 0.f}};
 #pragma unroll
@@ -260,25 +260,27 @@ const char *const kName = "attention";
 
 long long rows_or(long long rows, long long dense) { return rows != 0 ? rows : dense; }
 
-struct Form { int cw, splits, split_keys; };   // wavefronts side by side in a block; blocks that the keys of a column are dealt out to
+struct Form { int cw, splits, split_keys, span; };   // wavefronts side by side in a block; blocks that the keys of a column are dealt out to, each one's keys, and all of them at most
 
 // Four wavefronts side by side share the copies of a tile of keys; where that takes longer (attn_wide) the four of them take the same 32 columns and share the keys, and if that leaves
 // compute units without work too, blocks share them.
 Form form_of(const dp_attention_desc &d)
 {
     const long long shared = d.heads / d.kv_heads, cols = d.q_len * shared, rows = rows_or(d.q_rows, (long long)d.n * d.q_len);
-    if (attn_wide(d, d.q_len, rows, shared, attn_seen(d, d.kv_len, 128 / (int)std::min<long long>(shared, 128)))) return {4, 1, 0};
+    if (attn_wide(d, d.q_len, rows, shared, attn_seen(d, d.kv_len, 128 / (int)std::min<long long>(shared, 128)))) return {4, 1, 0, 0};
     const long long blocks = std::max<long long>(1, d.kv_heads * attn_tiles(d.n, d.q_len, rows, shared, 32));
     constexpr int kt = 128;
-    const long long span = attn_seen(d, d.kv_len, 32);   // keys that a block looks at
+    // keys that a block looks at: of its queries; behind the last query's place there are none
+    const long long queries = std::min<long long>(d.q_len, 32 / shared + (32 % shared != 0 ? 2 : 0)), behind = std::max<long long>(0, d.right < 0 ? d.q_len - 1 : std::min(d.right, d.q_len - 1));
+    const long long span = d.left < 0 ? d.kv_len : std::min<long long>(d.kv_len, d.left + behind + queries);
     const long long most = std::min<long long>(kMaxSplits, (span + 4 * kt - 1) / (4 * kt));   // four tiles at least: the join takes as long as two
     // A single token's columns fit one block, which waits for memory most of the time: four rounds of blocks at least.  Others compute, and are split only to give every compute unit work
     // (2000 causal tokens fp32, 8 heads of 128 over 2, 500 blocks: 113 us, 205 in four parts; bf16 33 and 53).
     const long long want = std::min<long long>(most, (cols <= 32 ? 2048 : 512) / blocks);
-    if (want < 2) return {1, 1, 0};
-    // whole tiles; a window is anywhere in the sequence, so its split counts over all keys
-    const long long per = ((d.kv_len + want - 1) / want + kt - 1) / kt * kt;
-    return {1, (int)((d.kv_len + per - 1) / per), (int)per};
+    if (want < 2) return {1, 1, 0, 0};
+    // whole tiles, from the first key on that a block's queries see (one token that sees 4096 of 131072 keys, 32 heads of 128 over 8: 9.0 us, 35.9 where the parts are of all keys and one of nine holds those)
+    const long long per = ((span + want - 1) / want + kt - 1) / kt * kt;
+    return {1, (int)((span + per - 1) / per), (int)per, (int)span};
 }
 
 size_t split_bytes(const dp_attention_desc &d, const Form &f)
@@ -424,6 +426,7 @@ extern "C" dp_status dp_attention_fwd(const dp_attention_desc *desc, const void 
     a.qp = q; a.kp = k; a.vp = v; a.op = o; a.lse = lse;
     a.splits = f.splits;
     a.split_keys = f.split_keys;
+    a.span = f.span;
     a.part_o = (float *)ws;
     if (f.splits > 1) a.part_ml = a.part_o + (long long)f.splits * d.heads * a.q.rows * d.dim;
     const long long cols = (long long)d.q_len * a.shared, groups = (long long)d.n * d.kv_heads;

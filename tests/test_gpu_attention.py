@@ -435,3 +435,30 @@ def test_next_tokens_of_very_many_sequences(env, bf16):
     c = Case(env, 1024, 1, 131072, 8, 8, 32, -1, 0, bf16, kv_side=("packed", r.integers(0, 9, 1024).tolist(), 1, 2))
     assert c.dp.dp_attention_workspace_bytes(c.desc, c.dp.DP_PASS_DGRAD) == 0
     c.check_forward(c.forward())
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("case", [(1, 1, 20000, 8, 2, 128, 2047, 0), (1, 1, 9000, 4, 4, 64, 1000, 500), (2, 1, 7001, 6, 2, 40, 1300, 0), (1, 1, 5000, 2, 1, 96, 1600, -1)], ids=str)
+def test_keys_of_a_window_dealt_out(env, case, bf16):
+    """One token, few of its keys: every block that the keys are dealt out to has some of them (it writes its part of o into the workspace, [part][head][row][channel] fp32)."""
+    c = Case(env, *case, bf16)
+    dp, need = c.dp, c.dp.dp_attention_workspace_bytes(c.desc, c.dp.DP_PASS_FWD)
+    per = 4 * c.heads * c.q_rows * (c.dim + 2)
+    parts, rest = divmod(need, per)
+    assert rest == 0 and parts >= 2
+    ws = torch.full((need // 4,), float("nan"), device="cuda")
+    o, lse = torch.full((c.q_rows, c.widths[0]), 7.0, dtype=c.tdt, device="cuda"), torch.full((c.heads, c.q_rows), 7.0, device="cuda")
+    dp.dp_attention_fwd(c.desc, c.wide(c.q), c.wide(c.k), c.wide(c.v), o, lse, c.seqs, ws)
+    c.check_forward((o, lse))
+    written = ws[:parts * c.heads * c.q_rows * c.dim].reshape(parts, -1).isfinite().all(dim=1)
+    assert written.all(), written
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("heads", [(8, 2), (6, 2), (5, 1), (80, 2)], ids=str)
+@pytest.mark.parametrize("window", [(1500, 0), (1100, 700), (1900, -1), (-1, 300)], ids=str)
+def test_few_queries_with_windows_over_many_keys(env, heads, window, bf16):
+    """Blocks that see different keys, split; padded and packed sequences with fewer keys than a window has, or none."""
+    Case(env, 1, 37, 5000, *heads, 64, *window, bf16).check()
+    Case(env, 5, 3, 5000, *heads, 40, *window, bf16, q_side=[3, 1, 0, 2, 3], kv_side=[5000, 900, 3000, 0, 2]).check()
+    Case(env, 4, 9, 5000, *heads, 72, *window, bf16, q_side=("packed", [9, 0, 1, 4], 1, 2), kv_side=("packed", [4100, 20, 1999, 5000], 2, 1)).check(True, True)
