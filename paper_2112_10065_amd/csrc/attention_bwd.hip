@@ -493,10 +493,11 @@ DkvForm dkv_form(const dp_attention_desc &d)
         if (wide && !plain.wide && (!bf || d.kv_len <= 32)) continue;
         const long long tiles = wide ? (attn_seen(d, d.q_len, 128) + 63) / 64 : (attn_seen(d, d.q_len, 32) + 127) / 128, longest = tiles * shared;
         const double blocks = (double)d.kv_heads * attn_tiles(d.n, d.kv_len, rows, 1, wide ? 128 : 32), t = wide ? t_wide[bf][size] : t_few[bf][size], alone = wide && bf ? t_alone[size] : t;
-        const double share = causal ? (tiles + 1) / (2.0 * tiles) : 1;   // of the longest block's tiles that a block has on average
+        const double seen = attn_share(d);
         for (int p = wide == plain.wide ? 1 : 2; p <= 16 && p <= longest && blocks * p <= 2048; ++p) {
             // causal: what a unit has on average, and what the last blocks leave idle
-            const double busy = causal ? t * blocks * share / 256 + (p == 1 ? 0.1 : wide ? 0.4 : 0.5 * t) / p : t * (double)(long long)(blocks * p / 256 + 0.999) / p;
+            const double even = t * (double)(long long)(blocks * p / 256 + 0.999) / p;
+            const double busy = causal ? attn_between(seen, t * blocks * (0.5 + 0.5 / tiles) / 256 + (p == 1 ? 0.1 : wide ? 0.4 : 0.5 * t) / p, even) : even;
             const double us = (8 + longest * std::max(alone / p, busy) + (p > 1 ? 4 + p * sums : 0)) * (p > 1 && blocks * p > 256 ? 1.03 : 1);
             if (wide == plain.wide && p == 1) {
                 if (us < 25) return plain;

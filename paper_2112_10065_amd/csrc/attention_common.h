@@ -8,6 +8,7 @@
 #pragma once
 #include "../../include/dp.h"
 #include "dma_common.h"
+#include <algorithm>
 #include <initializer_list>
 
 void dp_set_error(const char *fmt, ...);   // dp_api.hip
@@ -481,22 +482,36 @@ inline long long attn_tiles(long long n, long long len, long long rows, long lon
     const long long all = n * ((len * mult + columns - 1) / columns), packed = rows * mult / columns + n;
     return rows < n * len && packed < all ? packed : all;
 }
+// The share of a sequence's pairs of a query and a key that a mask with a bound on one side leaves: a half of a square, nearly all for a few queries behind many keys.  Never below a half: where
+// there are more queries than keys, the blocks that see nothing end at once and the others are as those of a square (4 x 1500 queries, 500 keys, 16 heads of 128 over 4: dk and dv 33 us, 43 as the share has it).
+inline double attn_share(const dp_attention_desc &d)
+{
+    if ((d.left < 0) == (d.right < 0) || d.q_len == 0 || d.kv_len == 0) return 1;
+    // as areas: query i sees min(i + from, kv_len) keys, if that is any (left: counted from the last query back)
+    const double q = d.q_len, k = d.kv_len, from = d.right >= 0 ? k - q + d.right : d.left;
+    const double whole = std::min(q, std::max(0.0, from + q - k)), first = std::max(0.0, from), rest = std::max(0.0, q - whole - std::max(0.0, -from));
+    return std::max(0.5, (whole * k + rest * (first + std::min(k, first + rest)) / 2) / (q * k));
+}
+// Between what is true of a half and of all pairs
+inline double attn_between(double share, double half, double all) { return (2 - 2 * share) * half + (2 * share - 1) * all; }
 // Whether blocks are of 128 columns, four wavefronts side by side, or of 32, whose wavefronts share the other side's rows: what is shorter by this count of microseconds.  A block takes 3 for
 // its beginning and its end, and t for each 64 (128 columns) or 128 (32 columns) rows of the other side; a compute unit works on one of the former at a time or as fast on several,
-// on one or (narrow heads) two of the latter.  Blocks of a causal mask need half of their rows on average, the first ones all.  Measured, forward in small and in large blocks (us): 2000 tokens of 8 heads of
+// on one or (narrow heads) two of the latter.  Blocks of a causal mask need attn_share of their rows on average, the first ones all.  Measured, forward in small and in large blocks (us): 2000 tokens of 8 heads of
 // 64 22 / 28, 4000 causal 43 / 50, 2 x 1000 of 128 28 / 23, 8 x 197 of 12 heads of 64 11.4 / 7.8, 24 packed sequences of 16 heads of 80 267 / 75; fp32 2 x 1788 causal, 12 heads of 72, 183 / 276,
-// 4 x 1024, 8 heads of 64, 107 / 82.
+// 4 x 1024, 8 heads of 64, 107 / 82; 512 causal queries behind 32768 keys, 32 heads of 128 over 8, 630 / 518 (dq 659 / 695).
 inline bool attn_wide(const dp_attention_desc &d, long long len, long long rows, long long mult, long long other)
 {
     if (len * mult <= 32) return false;
     if ((double)d.n * d.kv_heads * (double)(len * mult / 32 + 1) >= (double)(1 << 23)) return true;   // a launch has fewer than 2^32 threads
     const bool bf = d.io_dtype == DP_BF16, causal = (d.left < 0) != (d.right < 0);
     const int size = d.dim <= 64 ? 0 : d.dim <= 96 ? 1 : 2;
+    const double share = attn_share(d);
     constexpr double t_wide[2][3] = {{4.8, 6.5, 9.4}, {0.72, 0.9, 1.09}}, t_few[2][3] = {{2.9, 4.2, 5.9}, {0.92, 1.05, 1.19}};
     const double wide = d.kv_heads * (double)attn_tiles(d.n, len, rows, mult, 128) / 256, few = d.kv_heads * (double)attn_tiles(d.n, len, rows, mult, 32) / (bf && size == 0 ? 512 : 256);
     const auto whole = [](double x) { return (double)(long long)(x + 0.999); };
     const auto longest = [](double x) { return x > 1 ? x : 1; };
-    const double rounds_wide = longest(bf ? (causal ? 0.5 * wide + 0.25 : wide) : (causal ? 0.5 * wide + 0.75 : whole(wide))), rounds_few = longest(causal ? 0.5 * few + 0.25 : few);
+    const auto rounds = [&](double blocks, double tail, double all) { return longest(causal ? attn_between(share, 0.5 * blocks + tail, all) : all); };
+    const double rounds_wide = bf ? rounds(wide, 0.25, wide) : rounds(wide, 0.75, whole(wide)), rounds_few = rounds(few, 0.25, few);
     return 3 + other / 64.0 * t_wide[bf][size] * rounds_wide <= 3 * whole(few) + other / 128.0 * t_few[bf][size] * rounds_few;
 }
 // rows of the other side that a block of `columns` sees, at most

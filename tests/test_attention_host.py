@@ -208,3 +208,51 @@ def test_keys_limit_the_gradient_alone(dp):
         assert dp.lib.dp_attention_fwd(C.byref(d), A, A, None, A + 64, None, C.byref(s), A, need, None) == dp.DP_ERR_NULL     # what comes behind the limits
         assert dp.lib.dp_attention_bwd(C.byref(d), A, A, None, A, A, A, A + 64, A + 128, A + 192, C.byref(s), A, 1 << 40, None) == dp.DP_ERR_BAD_DESC
         assert dp.dp_attention_workspace_bytes(d, dp.DP_PASS_DGRAD) == 0
+
+
+RULES = """
+#include "attention_common.h"
+extern "C" bool wide(const dp_attention_desc *d, long long len, long long rows, long long mult, long long other) { return attn_wide(*d, len, rows, mult, other); }
+extern "C" double share(const dp_attention_desc *d) { return attn_share(*d); }
+"""
+
+
+@pytest.fixture(scope="module")
+def rules(dp, tmp_path_factory):
+    """The rules that choose a call's blocks, built by themselves for the host."""
+    import os
+    import shutil
+    import subprocess
+    if shutil.which("hipcc") is None:
+        pytest.skip("no compiler")
+    path = tmp_path_factory.mktemp("rules")
+    (path / "rules.hip").write_text(RULES)
+    csrc = os.path.join(os.path.dirname(dp.__file__), "csrc")
+    subprocess.check_call(["hipcc", "--cuda-host-only", "-O1", "-std=c++17", "-fPIC", "-shared", "-I", csrc, str(path / "rules.hip"), "-o", str(path / "rules.so")])
+    lib = C.CDLL(str(path / "rules.so"))
+    lib.wide.argtypes, lib.wide.restype = [C.POINTER(dp.dp_attention_desc)] + [C.c_longlong] * 4, C.c_bool
+    lib.share.argtypes, lib.share.restype = [C.POINTER(dp.dp_attention_desc)], C.c_double
+    return lib
+
+
+def test_a_chunk_behind_many_keys_takes_the_blocks_of_all_keys(dp, rules):
+    """A causal mask hides nearly nothing from few queries at the end of many keys: the choice is that of a call without a mask.  Queries' blocks, then keys'."""
+    for q, kv, heads, kv_heads, dim, io in ((512, 32768, 32, 8, 128, dp.DP_BF16), (700, 50000, 32, 8, 96, dp.DP_BF16), (512, 8192, 8, 8, 128, dp.DP_F32), (1024, 65536, 16, 2, 64, dp.DP_F32),
+                                            (256, 16384, 32, 8, 128, dp.DP_BF16)):
+        args = dict(n=1, q_len=q, kv_len=kv, heads=heads, kv_heads=kv_heads, dim=dim, io_dtype=io)
+        masked, whole = att(dp, right=0, **args), att(dp, **args)
+        shared = heads // kv_heads
+        assert rules.wide(masked, q, q, shared, kv) == rules.wide(whole, q, q, shared, kv), args
+        assert rules.wide(masked, kv, kv, 1, q * shared) == rules.wide(whole, kv, kv, 1, q * shared), args
+
+
+def test_the_share_of_pairs_that_a_mask_leaves(dp, rules):
+    """Beside a count; as an area it is off by less than one key of every query.  At least a half."""
+    for q, kv in ((1, 1), (1, 50), (50, 1), (40, 40), (30, 100), (100, 30), (7, 90)):
+        for left, right in ((-1, 0), (-1, 5), (-1, 33), (-1, 200), (0, -1), (9, -1), (64, -1), (300, -1), (3, 3), (-1, -1)):
+            seen = sum(sum((left < 0 or j >= i + kv - q - left) and (right < 0 or j <= i + kv - q + right) for j in range(kv)) for i in range(q)) / (q * kv)
+            got = rules.share(att(dp, q_len=q, kv_len=kv, left=left, right=right))
+            one_side = (left < 0) != (right < 0)
+            assert abs(got - max(0.5, seen)) <= 1 / kv + 1e-12 if one_side else got == 1, (q, kv, left, right, got, seen)
+    for n in (1, 197, 4096):
+        assert rules.share(att(dp, q_len=n, kv_len=n, right=0)) == rules.share(att(dp, q_len=n, kv_len=n, left=0)) == 0.5
