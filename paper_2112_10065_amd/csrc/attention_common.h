@@ -88,18 +88,25 @@ DEVFN int dealt(int block, int of, int groups)
     return die / dies * (of / 8 * dies) + (block >> 3) * dies + die % dies;
 }
 
+// Block 256 ... 511 of a launch of `of`: the one in its place where each die takes its blocks of these, as many as there are, in reverse.
+inline __host__ __device__ int second_reversed(int block, int of)
+{
+    const int die = block & 7, there = ((of < 512 ? of : 512) - 256 - die + 7) >> 3;
+    return (63 + there - (block >> 3)) << 3 | die;
+}
+
 // The grid has room for sequences of the longest length.  Whole sequences: tile by tile, head by head, a contiguous eighth for each die, so that the tiles of one head read their
 // rows from one L2 (with a causal mask: dealt).  Lengths that differ: the same over the tiles that there are, counted by each block for itself (a lane to a sequence), since tiles of nothing, numbered
 // among the others, would leave some dies with much more work than others (9 sequences of up to 1500 of 4 heads of keys, dk and dv: 73 us, 53 this way).  Tiles that hold padding alone come last.
 // `mult` columns to a row of `side`; SPLIT: every part of the keys that a sequence has; LAST_FIRST: a causal mask makes a sequence's last tiles the longest.  Where all blocks of such a call
-// are on the card at once, SLOTS to a compute unit, each die's second 32 are taken in reverse, so that a long one shares its unit with a short one (4096 causal tokens, 16 heads of 128: 105 -> 97 us
-// forward, dq 147 -> 136).
+// are on the card at once, SLOTS to a compute unit, each die's second 32, or as many as there are, are taken in reverse, so that a long one shares its unit with a short one (4096 causal tokens, 16 heads
+// of 128: 105 -> 97 us forward, dq 147 -> 136; 12 heads, 384 blocks, 108 -> 81 and 149 -> 112).
 constexpr int kMostRagged = 256;   // sequences: more of them are counted for longer than it helps
 template <int COLS, bool SPLIT, bool LAST_FIRST, int SLOTS = 1> DEVFN Item item_of(const AttnArgs &a, const AttnSide &side, int mult, int block, int of)
 {
     Item r;
     if (!a.ragged) {
-        if (SLOTS > 1 && LAST_FIRST && of <= 256 * SLOTS && a.causal && (block & 256) != 0 && (block | 255) < of) block ^= 31 << 3;
+        if (SLOTS > 1 && LAST_FIRST && of <= 256 * SLOTS && a.causal && (block & 256) != 0) block = second_reversed(block, of);
         int id = a.causal ? dealt(block, of, a.n * a.kv_heads) : logical_block(block, of);
         r.split = SPLIT ? id % a.splits : 0;
         if (SPLIT) id /= a.splits;

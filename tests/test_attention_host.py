@@ -214,6 +214,7 @@ RULES = """
 #include "attention_common.h"
 extern "C" bool wide(const dp_attention_desc *d, long long len, long long rows, long long mult, long long other) { return attn_wide(*d, len, rows, mult, other); }
 extern "C" double share(const dp_attention_desc *d) { return attn_share(*d); }
+extern "C" int second(int block, int of) { return second_reversed(block, of); }
 """
 
 
@@ -256,3 +257,11 @@ def test_the_share_of_pairs_that_a_mask_leaves(dp, rules):
             assert abs(got - max(0.5, seen)) <= 1 / kv + 1e-12 if one_side else got == 1, (q, kv, left, right, got, seen)
     for n in (1, 197, 4096):
         assert rules.share(att(dp, q_len=n, kv_len=n, right=0)) == rules.share(att(dp, q_len=n, kv_len=n, left=0)) == 0.5
+
+
+def test_second_blocks_of_a_die_in_reverse(rules):
+    """Each of 256 ... 511 once, on the die that it was on, the last first; however many there are."""
+    for of in range(257, 769):
+        for die in range(8):
+            blocks = list(range(256 + die, min(of, 512), 8))
+            assert [rules.second(b, of) for b in blocks] == blocks[::-1], (of, die)

@@ -462,3 +462,11 @@ def test_few_queries_with_windows_over_many_keys(env, heads, window, bf16):
     Case(env, 1, 37, 5000, *heads, 64, *window, bf16).check()
     Case(env, 5, 3, 5000, *heads, 40, *window, bf16, q_side=[3, 1, 0, 2, 3], kv_side=[5000, 900, 3000, 0, 2]).check()
     Case(env, 4, 9, 5000, *heads, 72, *window, bf16, q_side=("packed", [9, 0, 1, 4], 1, 2), kv_side=("packed", [4100, 20, 1999, 5000], 2, 1)).check(True, True)
+
+
+@pytest.mark.parametrize("dim", [64, 96, 112, 128])
+@pytest.mark.parametrize("case", [(16, 512, 8), (12, 640, 8), (13, 600, 7), (3, 1100, 12), (16, 1024, 5)], ids=str)
+def test_causal_blocks_that_share_compute_units(env, case, dim):
+    """512 blocks of 128 columns, 480, 455, 324 and 640, forward and for dq: those behind the first 256 in reverse."""
+    n, length, heads = case
+    Case(env, n, length, length, heads, heads, dim, -1, 0).check()
