@@ -396,7 +396,7 @@ dp_status dp_logprobs_bwd(const dp_logprobs_desc *desc, const void *z, const int
  * Rows hold their heads side by side; row r of a tensor is at its address + r * stride elements, so that queries and keys may be parts of
  * one projection's rows.  Strides are whole multiples of 16 bytes; a 0 stands for the heads' own width.  pos is fp32 [rows][axes] (also
  * fractions), freq 64-bit [P]; the angle is computed in 64 bits, all else in fp32.  gamma_q, gamma_k fp32 [dim], NULL: ones (also where
- * only one of them is).  rows, kv_heads and each pairs[a] may be 0 (keys are then not looked at). */
+ * only one of them is).  rows, kv_heads and each pairs[a] may be 0 (keys are then not looked at; without any pairs pos and freq may be NULL). */
 typedef struct {
     int32_t rows, heads, kv_heads;
     int32_t dim;                /* a multiple of 8, at most 256 */

@@ -312,6 +312,8 @@ dp_status check_desc(const dp_qk_rotary_desc *desc)
 
 long long stride_or(long long stride, long long dense) { return stride != 0 ? stride : dense; }
 
+bool turns(const dp_qk_rotary_desc &d) { return d.pairs[0] > 0 || (d.axes > 1 && d.pairs[1] > 0) || (d.axes > 2 && d.pairs[2] > 0); }   // else pos and freq are not read
+
 struct Launch { int blocks, parts; };
 
 // Wavefronts of a row: one goes over all its heads unless rows are few (at 8 rows of 28 heads of 128 channels the row's last head is then seven waits for memory away
@@ -382,7 +384,7 @@ extern "C" dp_status dp_qk_rotary_fwd(const dp_qk_rotary_desc *desc, const void 
     const dp_qk_rotary_desc &d = *desc;
     if (d.rows == 0) return DP_OK;
     const bool keys = d.kv_heads > 0;
-    if ((s = check_pointers({q, pos, freq, q_out}, {gamma_q, gamma_k})) != DP_OK || (keys && (s = check_pointers({k, k_out}, {})) != DP_OK)) return s;
+    if ((s = check_pointers({q, q_out}, {gamma_q, gamma_k, pos, freq})) != DP_OK || (turns(d) && (s = check_pointers({pos, freq}, {})) != DP_OK) || (keys && (s = check_pointers({k, k_out}, {})) != DP_OK)) return s;
     const long long wq = width(d, false), wk = width(d, true);
     QkArgs a = {};
     a.q = {q, nullptr, q_out, gamma_q, stride_or(d.q_stride, wq), 0, stride_or(d.q_out_stride, wq), 0};
@@ -406,7 +408,7 @@ extern "C" dp_status dp_qk_rotary_bwd(const dp_qk_rotary_desc *desc, const void 
     const bool norm = (d.flags & DP_QK_NORM) != 0, keys = d.kv_heads > 0, sums = dgamma_q != nullptr || dgamma_k != nullptr;
     if (sums && !norm) { dp_set_error("%s: dgamma without DP_QK_NORM", kName); return DP_ERR_UNSUPPORTED; }
     if (d.rows > 0) {
-        if ((s = check_pointers({pos, freq, dq_out, dq}, {q, k, gamma_q, gamma_k})) != DP_OK || (keys && (s = check_pointers({dk_out, dk}, {})) != DP_OK) ||
+        if ((s = check_pointers({dq_out, dq}, {q, k, gamma_q, gamma_k, pos, freq})) != DP_OK || (turns(d) && (s = check_pointers({pos, freq}, {})) != DP_OK) || (keys && (s = check_pointers({dk_out, dk}, {})) != DP_OK) ||
             (norm && (s = check_pointers({q}, {})) != DP_OK) || (norm && keys && (s = check_pointers({k}, {})) != DP_OK)) return s;
     }
     if ((s = check_pointers({}, {dgamma_q, dgamma_k, ws})) != DP_OK) return s;

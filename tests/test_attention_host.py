@@ -265,3 +265,15 @@ def test_second_blocks_of_a_die_in_reverse(rules):
         for die in range(8):
             blocks = list(range(256 + die, min(of, 512), 8))
             assert [rules.second(b, of) for b in blocks] == blocks[::-1], (of, die)
+
+
+def test_nothing_to_turn_needs_no_places(dp):
+    """Without pairs freq has no elements, whose address is NULL: the call goes on to its other checks."""
+    for pairs in ([0], [0, 0], [0, 0, 0]):
+        d = rot(dp, pairs=pairs)
+        assert dp.lib.dp_qk_rotary_fwd(C.byref(d), A, A, A + 4, A, None, None, A + 64, A + 64, None) == dp.DP_ERR_BAD_DESC
+        assert dp.lib.dp_qk_rotary_bwd(C.byref(d), A, A, A, A, A, None, A + 64, A + 64, A + 128, A + 128, A, A, None, 0, None) == dp.DP_ERR_WORKSPACE
+    d = rot(dp, pairs=[0, 4])
+    assert dp.lib.dp_qk_rotary_fwd(C.byref(d), A, A, A + 4, A, A, None, A + 64, A + 64, None) != dp.DP_OK
+    assert dp.lib.dp_qk_rotary_fwd(C.byref(d), A, A, A, A, A, None, A + 64, A + 64, None) == dp.DP_ERR_NULL
+    assert dp.lib.dp_qk_rotary_fwd(C.byref(d), A, A, A, A, None, A, A + 64, A + 64, None) == dp.DP_ERR_NULL

@@ -213,3 +213,14 @@ def test_same_bits_on_another_stream_and_in_a_graph(env):
         torch.cuda.synchronize()
         for a, b, e in zip(y + dx + dg, y2 + dx2 + dg2, out + dx3 + dg3):
             assert torch.equal(a, b) and torch.equal(a, e)
+
+
+@pytest.mark.parametrize("halves", [True, False])
+def test_nothing_to_turn(env, halves):
+    """The norm alone: freq has no elements, and no places need be given."""
+    for pairs in ([0], [0, 0]):
+        c = Case(env, 23, 5, 2, 72, pairs, halves, True, False)
+        c.check_forward(c.forward())
+        c.check_backward(*c.backward())
+        c.pd = c.fd = None
+        c.check_forward(c.forward())
