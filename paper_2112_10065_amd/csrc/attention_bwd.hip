@@ -568,7 +568,8 @@ extern "C" dp_status dp_attention_bwd(const dp_attention_desc *desc, const void 
     attn_args(d, seqs, a);
     const bool queries = d.n > 0 && d.q_len > 0 && a.q.rows > 0, keys = d.n > 0 && d.kv_len > 0 && a.kv.rows > 0;
     if (!queries && !keys) return DP_OK;
-    if (queries && (s = attn_pointers({q, o, dout, dq, lse}, nullptr, nullptr)) != DP_OK) return s;
+    if (queries && (s = attn_pointers({q, o, dout, dq}, lse, nullptr)) != DP_OK) return s;
+    if (queries && lse == nullptr) { dp_set_error("attention's gradient: lse is NULL"); return DP_ERR_NULL; }
     if (keys && (s = attn_pointers({k, v, dk, dv}, nullptr, nullptr)) != DP_OK) return s;
     const DkvForm f = dkv_form(d);
     // dk and dv are made behind dq, from all inputs but o

@@ -277,3 +277,9 @@ def test_nothing_to_turn_needs_no_places(dp):
     assert dp.lib.dp_qk_rotary_fwd(C.byref(d), A, A, A + 4, A, A, None, A + 64, A + 64, None) != dp.DP_OK
     assert dp.lib.dp_qk_rotary_fwd(C.byref(d), A, A, A, A, A, None, A + 64, A + 64, None) == dp.DP_ERR_NULL
     assert dp.lib.dp_qk_rotary_fwd(C.byref(d), A, A, A, A, None, A, A + 64, A + 64, None) == dp.DP_ERR_NULL
+
+
+def test_lse_has_the_alignment_of_its_elements(dp):
+    """In the gradient as in the forward call: what one writes the other takes."""
+    for lse, status in ((A + 4, dp.DP_ERR_WORKSPACE), (A + 12, dp.DP_ERR_WORKSPACE), (A + 1, dp.DP_ERR_BAD_DESC), (None, dp.DP_ERR_NULL)):
+        assert dp.lib.dp_attention_bwd(C.byref(att(dp)), A, A, A, A, A, lse, A + 64, A + 128, A + 192, None, None, 0, None) == status, lse

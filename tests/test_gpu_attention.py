@@ -470,3 +470,17 @@ def test_causal_blocks_that_share_compute_units(env, case, dim):
     """512 blocks of 128 columns, 480, 455, 324 and 640, forward and for dq: those behind the first 256 in reverse."""
     n, length, heads = case
     Case(env, n, length, length, heads, heads, dim, -1, 0).check()
+
+
+def test_lse_of_any_element(env):
+    """lse inside a larger buffer, not at a multiple of 16 bytes: the bits of a call with one of its own."""
+    c = Case(env, 2, 61, 90, 4, 2, 64, -1, 0)
+    dp = c.dp
+    o, lse = c.forward()
+    grads = c.backward(o, lse)
+    for shift in (1, 2, 3):
+        room = torch.full((lse.numel() + 8,), 7.0, device="cuda")
+        inside = room[shift:shift + lse.numel()].view(lse.shape)
+        dp.dp_attention_fwd(c.desc, c.wide(c.q), c.wide(c.k), c.wide(c.v), torch.empty_like(o), inside, c.seqs)
+        assert torch.equal(inside, lse) and (room[:shift] == 7).all() and (room[shift + lse.numel():] == 7).all()
+        assert all(torch.equal(a, b) for a, b in zip(c.backward(o, inside), grads))
