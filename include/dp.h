@@ -436,8 +436,8 @@ dp_status dp_qk_rotary_bwd(const dp_qk_rotary_desc *desc, const void *q, const v
  * Rows hold their heads side by side, row r at r * stride elements; strides are whole multiples of 16 bytes, 0 stands for the heads' own width.
  * o, dout: o_stride; dq, dk, dv: the strides of q, k, v.  lse: fp32 [heads][q_rows].
  * Arithmetic: products on the matrix cores with fp32 sums; softmax, its statistics and all sums fp32.  With DP_BF16 the probabilities (and in the
- * backward pass p and dp's product with it) are rounded to bf16 as operands of the second product.  A value or gradient row that is NaN or infinite
- * may make NaN also of queries and keys that do not see it, if they share a tile with ones that do; unused rows never do.
+ * backward pass p and dp's product with it) are rounded to bf16 as operands of the second product.  A value or gradient row that is NaN or infinite,
+ * in the backward pass also a query or key row, may make NaN also of queries and keys that do not see it, if they share a tile with ones that do; unused rows never do.
  * Results may not overlap inputs or each other (dq, dk and dv may lie side by side in the same rows).  Tensors may hold more than 2^31 elements here. */
 typedef struct {
     int32_t n, q_len, kv_len;   /* n, q_len, kv_len >= 0 */

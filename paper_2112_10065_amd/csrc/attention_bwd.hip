@@ -6,7 +6,7 @@
 // sequences of 4096 causal tokens, 0.8 ms, where the two products take 0.25).
 // With bf16, p and ds are rounded as operands of the second products; p, dp and delta themselves stay in 32 bits.
 //
-// Bound by the matrix cores: two sequences of 4096 causal tokens, 32 heads of 128 over 8: dq 385-398 us (1.05 PFLOP/s of the products that it computes), dk and dv 557 (0.99).
+// Bound by the matrix cores: two sequences of 4096 causal tokens, 32 heads of 128 over 8: dq 385-403 us (1.02-1.07 PFLOP/s of the products that it computes), dk and dv 543-590 (0.93-1.01).
 // Short sequences wait: 32 x 197 tokens, 12 heads of 64, 20 + 26 us for four tiles a block in one round and one and a half.
 #include "attention_common.h"
 #include <algorithm>

@@ -6,10 +6,10 @@
 // only in the few tiles where the maximum grows by more.  p is rounded to bf16 as an operand of the second product (its sum is not): 2^-9 of each value at random, a third of the
 // rounding of o itself.
 //
-// Long sequences are bound by the matrix cores and the power they draw: 8192 x 8192, 16 heads of 128, bf16, 507-521 us or 1055-1085 TFLOP/s (a product of 8192^3
+// Long sequences are bound by the matrix cores and the power they draw: 8192 x 8192, 16 heads of 128, bf16, 507-536 us or 1025-1085 TFLOP/s (a product of 8192^3
 // reaches 1235), matrix instructions in 59 % of the cycles at the 1.6 GHz that the card then keeps.  S a tile ahead, between the exponentials, and eight wavefronts to a tile changed nothing
 // there.  Fewer heads' channels leave more cycles to the exponentials: 24 x 1024 tokens, 16 heads, 64 channels 126 us (819 TFLOP/s), 80 160, 96 177.  Two or three blocks share a compute
-// unit, one exponentiates while another multiplies.  Single tokens are bound by memory: 16 sequences of up to 8192 keys, 8 heads of 128, 352 MB in 70.5 us.
+// unit, one exponentiates while another multiplies.  Single tokens are bound by memory: 16 sequences of up to 8192 keys, 8 heads of 128, 352 MB in 71 us.
 #include "attention_common.h"
 #include <algorithm>
 #include <cmath>
